@@ -14,6 +14,9 @@ Entry points (same names as the C ABI):
 * :func:`search_host`       -- the same with host queries and host results
 * :func:`rq_encode`, :func:`build_rq_layout`, :func:`rq_search` -- the local
   search over RaBitQ-style codes (the paper's IVF_RQ7 index)
+* :func:`layer_norm`, :func:`attention`, :func:`unit_pool` and their
+  ``*_backward`` -- the encoder operators that make the rows
+  (:mod:`paper_2608_03199_gb300.encoder`)
 """
 from __future__ import annotations
 
@@ -698,3 +701,10 @@ def search_noalloc(index: Index, Q, tau, k, nprobe, W, lookahead=True, query_ids
                                       C.byref(p), _ptr(ids), _ptr(scores), _ptr(count),
                                       _ptr(probes), None, _stream(stream)), "sieve_search_noalloc")
     return ids, scores, count, probes
+
+
+from . import encoder as _encoder  # noqa: E402  (uses this module's helpers)
+from .encoder import (attention, attention_backward, encoder_status, layer_norm,  # noqa: E402,F401
+                      layer_norm_backward, relative_buckets, unit_pool, unit_pool_backward)
+
+_SIGNATURES.update(_encoder.SIGNATURES)

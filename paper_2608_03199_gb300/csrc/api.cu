@@ -6,6 +6,7 @@
 #include <mutex>
 #include <vector>
 
+#include "encoder.cuh"
 #include "search.cuh"
 
 using namespace sieve;
@@ -691,6 +692,11 @@ sieve_status check_search(const sieve_index_view *ix, const float *Q, int64_t nq
 }  // namespace
 
 // ---------------------------------------------------------------------------
+namespace sieve {
+sieve_status record_cuda_error(cudaError_t e) { return cuda_fail(e); }
+sieve_status check_current_device() { return check_device(); }
+}  // namespace sieve
+
 extern "C" {
 
 const char *sieve_version(void) { return "libsieve 0.1 (sm_103a)"; }
