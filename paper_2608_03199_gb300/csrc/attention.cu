@@ -1,5 +1,5 @@
 // attention.cu -- attention over packed documents with a relative position
-// bias, forward and backward: one warp per row, straight from the formulas.
+// bias, backward: one warp per row, straight from the formulas.
 #include "encoder.cuh"
 
 namespace sieve {
@@ -39,60 +39,6 @@ __device__ __forceinline__ float dot_row(const float *q, const T *row, int d) {
         for (int e = 0; e < 8; ++e) s = fmaf(q[c + e], v[e], s);
     }
     return s;
-}
-
-template <typename T>
-__global__ void __launch_bounds__(kWarps * 32) k_attend(const AttentionArgs p) {
-    __shared__ float qs[kWarps][kMaxDim];
-    const sieve_attention_args &a = p.a;
-    if (blockIdx.x == 0 && threadIdx.x == 0) p.ctl->status = 0;
-    const int warp = threadIdx.x >> 5, lane = lane_id();
-    const int64_t w = (int64_t)blockIdx.x * kWarps + warp;
-    if (w >= a.q_tokens * a.heads) return;
-    const int t = (int)(w / a.heads), h = (int)(w % a.heads), hk = h / (a.heads / a.kv_heads);
-    const int s = a.new_tokens > 0 ? t / a.new_tokens : doc_of_row(a.q_offsets, (int)a.nseq, t);
-    const Doc doc = doc_at(a, s);
-    const int i = t - doc.q0;
-    if (i < 0 || i >= doc.nq) return;
-    const int d = a.head_dim;
-    const T *q = static_cast<const T *>(a.q) + t * a.q_token_stride + h * a.q_head_stride;
-    for (int c = lane; c < d; c += 32) qs[warp][c] = to_f32<T>(q[c]);
-    __syncwarp();
-    const int place = i + doc.nk - doc.nq;
-    const int nk = a.causal ? min(doc.nk, place + 1) : doc.nk;
-    const T *k = static_cast<const T *>(a.k) + doc.k0 * a.k_token_stride + hk * a.k_head_stride;
-    const T *v = static_cast<const T *>(a.v) + doc.k0 * a.v_token_stride + hk * a.v_head_stride;
-    float top = -INFINITY, sum = 0.f, o[kMaxDim / 32] = {};
-    for (int j0 = 0; j0 < nk; j0 += 32) {
-        const int j = j0 + lane;
-        float x = -INFINITY;
-        if (j < nk)
-            x = fmaf(dot_row<T>(qs[warp], k + j * a.k_token_stride, d), a.scale, bias_at(a, j - place, h));
-        float m = x;
-#pragma unroll
-        for (int f = 16; f; f >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, f));
-        m = fmaxf(m, top);
-        const float base = m == -INFINITY ? 0.f : m;
-        const float old = expf(top - base), e = expf(x - base);
-        top = m;
-        sum = sum * old + warp_sum(e);
-#pragma unroll
-        for (int c = 0; c < kMaxDim / 32; ++c) o[c] *= old;
-        const int n = min(32, nk - j0);
-        for (int jj = 0; jj < n; ++jj) {
-            const float pj = __shfl_sync(0xffffffffu, e, jj);
-#pragma unroll
-            for (int c = 0; c < kMaxDim / 32; ++c)
-                if (c * 32 + lane < d)
-                    o[c] = fmaf(pj, to_f32<T>(v[(j0 + jj) * a.v_token_stride + c * 32 + lane]), o[c]);
-        }
-    }
-    T *out = static_cast<T *>(p.out) + w * d;
-    const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);
-#pragma unroll
-    for (int c = 0; c < kMaxDim / 32; ++c)
-        if (c * 32 + lane < d) out[c * 32 + lane] = from_f32<T>(sum == 0.f ? 0.f : o[c] * inv);
-    if (lane == 0) p.lse[(int64_t)h * a.q_tokens + t] = sum == 0.f ? -INFINITY : top + logf(sum);
 }
 
 // dq, delta and the table's gradient: a warp per query row and head.
@@ -243,11 +189,6 @@ __global__ void __launch_bounds__(kWarps * 32) k_attend_dkv(const AttentionArgs 
 }
 
 template <typename T>
-cudaError_t forward(const AttentionArgs &p, cudaStream_t st) {
-    k_attend<T><<<(unsigned)ceil_div(p.a.q_tokens * p.a.heads, kWarps), kWarps * 32, 0, st>>>(p);
-    return cudaGetLastError();
-}
-template <typename T>
 cudaError_t backward(const AttentionArgs &p, cudaStream_t st) {
     cudaError_t e;
     if (p.a.q_tokens > 0) {
@@ -268,25 +209,18 @@ cudaError_t backward(const AttentionArgs &p, cudaStream_t st) {
 
 }  // namespace
 
-size_t attention_workspace_bytes(const sieve_attention_args &) { return kCtlBytes; }
-
 size_t attention_backward_workspace_bytes(const sieve_attention_args &a) {
     // delta of every query row, and its sums of ds by bucket
     return kCtlBytes + (size_t)round_up((int64_t)a.heads * a.q_tokens * (1 + a.num_buckets) * (int64_t)sizeof(float), 256);
 }
 
-cudaError_t launch_attention_forward(const AttentionArgs &p0, void *ws, cudaStream_t st) {
-    AttentionArgs p = p0;
-    p.ctl = static_cast<EncCtl *>(ws);
-    return p.a.dtype == SIEVE_F16 ? forward<__half>(p, st) : forward<__nv_bfloat16>(p, st);
-}
-
-cudaError_t launch_attention_backward(const AttentionArgs &p0, void *ws, cudaStream_t st) {
+sieve_status launch_attention_backward(const AttentionArgs &p0, void *ws, cudaStream_t st) {
     AttentionArgs p = p0;
     p.ctl = static_cast<EncCtl *>(ws);
     p.delta = reinterpret_cast<float *>(static_cast<unsigned char *>(ws) + kCtlBytes);
     p.row_sums = p.delta + (int64_t)p.a.heads * p.a.q_tokens;
-    return p.a.dtype == SIEVE_F16 ? backward<__half>(p, st) : backward<__nv_bfloat16>(p, st);
+    const cudaError_t e = p.a.dtype == SIEVE_F16 ? backward<__half>(p, st) : backward<__nv_bfloat16>(p, st);
+    return e == cudaSuccess ? SIEVE_OK : record_cuda_error(e);
 }
 
 }  // namespace enc

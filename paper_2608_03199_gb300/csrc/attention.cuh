@@ -1,0 +1,173 @@
+// attention.cuh -- what the attention kernels share: the documents' rows,
+// operand descriptors and tensor maps, the bias by distance, bounded waits.
+//
+// Operand tiles.  A tile of 128 rows (queries or keys) of one head is loaded
+// by TMA as one or two column blocks of 64 elements: 128 rows of 128 bytes,
+// 128-byte swizzle, 16 KB a block.  Columns past head_dim arrive as zeros, so
+// every head_dim up to 64 runs as 64 and every one up to 128 as 128.  One tile
+// serves two products: as a K-major operand its row is the contraction axis'
+// vector (q k^T, dout v^T), as an MN-major operand its rows are the
+// contraction axis (p v, ds k).
+//
+// Rows past a document's end belong to the next document and may hold
+// anything.  Scores of such keys are replaced before they are used; where such
+// rows are the contraction axis their probabilities are exact zeros, but
+// 0 x NaN is NaN, so the warp that issues the products first clears those
+// rows of the tile (at most once per block and operand, in its idle time).
+#pragma once
+
+#include <cuda.h>
+
+#include <type_traits>
+
+#include "encoder.cuh"
+#include "tcgen05.cuh"
+
+namespace sieve {
+namespace enc {
+
+constexpr int kTile = 128;                    // rows of a tile
+constexpr uint32_t kBlockBytes = kTile * 128;   // one 64-column block of a tile
+constexpr uint32_t kPolls = 1u << 24;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// K-major operand with 128-byte swizzle: tc::desc_k_sw128.  MN-major: the
+// 64-element blocks of the M or N axis lie `block_bytes` apart (leading
+// offset), groups of 8 rows of the contraction axis 1024 bytes apart.
+__device__ __forceinline__ uint64_t desc_mn_sw128(uint32_t saddr, uint32_t block_bytes) {
+    uint64_t d = 0;
+    d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
+    d |= (uint64_t)(block_bytes >> 4) << 16;
+    d |= (uint64_t)(1024 >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+
+// Instruction descriptor of kind::f16, fp32 accumulation, M = 128: both
+// operands fp16 (format 0) or bf16 (format 1), B K-major or MN-major (bit 16).
+template <typename T>
+__host__ __device__ constexpr uint32_t idesc(int N, bool b_mn) {
+    const uint32_t f = std::is_same_v<T, __half> ? 0u : 1u;
+    return (1u << 4) | (f << 7) | (f << 10) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) |
+           ((uint32_t)(kTile >> 4) << 24);
+}
+
+// D (+)= A B^T, both operands in shared memory and K-major: COLS contraction
+// columns in blocks of 64, the blocks of A and B kBlockBytes apart.
+template <int COLS>
+__device__ __forceinline__ void mma_kk(uint32_t lead, uint32_t d_tmem, uint32_t a, uint32_t b, uint32_t id) {
+#pragma unroll
+    for (int k = 0; k < COLS / 16; ++k) {
+        const uint32_t o = (k / 4) * kBlockBytes + (k % 4) * 32;
+        tc::mma_f16(lead, d_tmem, tc::desc_k_sw128(a + o), tc::desc_k_sw128(b + o), id, k > 0);
+    }
+}
+// D (+)= A B with A (128 x 128, 16-bit pairs) in tensor memory and B a tile
+// whose 128 rows are the contraction axis.
+__device__ __forceinline__ void mma_tn(uint32_t lead, uint32_t d_tmem, uint32_t a_tmem, uint32_t b, uint32_t id,
+                                       uint32_t accumulate) {
+#pragma unroll
+    for (int k = 0; k < kTile / 16; ++k)
+        tc::mma_f16_ta(lead, d_tmem, a_tmem + 8 * k, desc_mn_sw128(b + k * 2048, kBlockBytes), id,
+                       accumulate || k > 0);
+}
+
+__device__ __forceinline__ void tma_load(uint32_t lead, void *dst, const CUtensorMap *map, int c, int h, int t,
+                                         uint64_t *bar) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+        "@q cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+        "[%0], [%1, {%2, %3, %4}], [%5];\n\t}" ::"r"(tc::smem_u32(dst)),
+        "l"(map), "r"(c), "r"(h), "r"(t), "r"(tc::smem_u32(bar)), "r"(lead)
+        : "memory");
+}
+__device__ __forceinline__ void prefetch_map(const CUtensorMap *map) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+
+// store 32 consecutive 32-bit columns of this thread's tensor-memory lane
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,"
+        "%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+        "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+        "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// A bounded wait: gives up after the poll limit, or once another role of the
+// block has; the block then records SIEVE_ETIMEOUT and every role winds down.
+struct Waiter {
+    int *abort_flag;   // shared memory
+    int32_t *status;   // global
+    __device__ __forceinline__ bool operator()(uint64_t *bar, uint32_t parity) const {
+        if (tc::mbar_test_wait(bar, parity)) return true;
+        for (uint32_t it = 0; it < kPolls; ++it) {
+            if (tc::mbar_try_wait(bar, parity)) return true;
+            if ((it & 255u) == 255u && *(volatile int *)abort_flag) return false;
+        }
+        atomicExch(abort_flag, 1);
+        atomicExch(status, SIEVE_ETIMEOUT);
+        return false;
+    }
+    // the same for a whole warp in step
+    __device__ __forceinline__ bool warp(uint64_t *bar, uint32_t parity) const {
+        return __all_sync(0xffffffffu, (*this)(bar, parity));
+    }
+};
+
+struct Doc {
+    int q0, nq, k0, nk;   // first rows and lengths
+};
+__device__ __forceinline__ Doc doc_at(const sieve_attention_args &a, int s) {
+    Doc d;
+    doc_range(a.k_offsets, s, (int)a.k_tokens, d.k0, d.nk);
+    if (a.new_tokens > 0) {
+        d.q0 = s * a.new_tokens;
+        d.nq = a.new_tokens;
+    } else {
+        doc_range(a.q_offsets, s, (int)a.q_tokens, d.q0, d.nq);
+    }
+    return d;
+}
+
+// Clear the rows [first, 128) of a tile of `blocks` column blocks (a warp).
+__device__ __forceinline__ void clear_rows(unsigned char *tile, int first, int blocks) {
+    for (int b = 0; b < blocks; ++b)
+        for (int c = first * 8 + (int)lane_id(); c < kTile * 8; c += 32)
+            *reinterpret_cast<uint4 *>(tile + b * kBlockBytes + c * 16) = make_uint4(0, 0, 0, 0);
+    tc::fence_proxy_async_smem();
+    __syncwarp();
+}
+
+// The bias by distance of one head, times log2(e), for distances
+// -reach - kPad .. reach + kPad: 32 rows by 32 columns that hold any distance
+// inside (-reach, reach) hold none outside this range, so their lookups need
+// no clamp.  Finite values stay finite: the type's lowest must not become -inf,
+// which hides a key.
+constexpr int kPad = 64;
+__host__ __device__ __forceinline__ int bias_entries(int reach) { return 2 * (reach + kPad) + 1; }
+__device__ __forceinline__ float scaled_bias(const sieve_attention_args &a, int dist, int head) {
+    const int b = __ldg(a.bucket_map + a.reach + min(max(dist, -a.reach), a.reach));
+    const float v = __ldg(a.table + min(max(b, 0), a.num_buckets - 1) * a.heads + head);
+    const float w = v * kLog2e;
+    return isinf(w) && !isinf(v) ? copysignf(3.402823466e38f, v) : w;
+}
+
+// host: a map of [tokens][heads][head_dim], boxes of 64 columns x `box_heads`
+// x `box_tokens`
+sieve_status make_map(CUtensorMap *map, int dtype, const void *base, int head_dim, int heads, int64_t tokens,
+                      int64_t token_stride, int64_t head_stride, int box_heads, int box_tokens);
+
+}  // namespace enc
+}  // namespace sieve

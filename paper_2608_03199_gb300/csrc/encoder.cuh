@@ -190,8 +190,8 @@ struct AttentionArgs {
 };
 size_t attention_workspace_bytes(const sieve_attention_args &a);
 size_t attention_backward_workspace_bytes(const sieve_attention_args &a);
-cudaError_t launch_attention_forward(const AttentionArgs &p, void *ws, cudaStream_t st);
-cudaError_t launch_attention_backward(const AttentionArgs &p, void *ws, cudaStream_t st);
+sieve_status launch_attention_forward(const AttentionArgs &p, void *ws, cudaStream_t st);
+sieve_status launch_attention_backward(const AttentionArgs &p, void *ws, cudaStream_t st);
 
 }  // namespace enc
 }  // namespace sieve

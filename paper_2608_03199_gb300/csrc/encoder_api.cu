@@ -173,8 +173,7 @@ sieve_status sieve_attention(const sieve_attention_args *a, void *out, float *ls
     p.a = resolved(a);
     p.out = out;
     p.lse = lse;
-    ENC_CUDA(launch_attention_forward(p, ws, static_cast<cudaStream_t>(stream)));
-    return SIEVE_OK;
+    return launch_attention_forward(p, ws, static_cast<cudaStream_t>(stream));
 }
 
 sieve_status sieve_attention_backward_workspace_size(const sieve_attention_args *a, size_t *bytes) {
@@ -216,8 +215,7 @@ sieve_status sieve_attention_backward(const sieve_attention_args *a, const void 
     p.dv_ts = grad_strides[4];
     p.dv_hs = grad_strides[5];
     p.dtable = dtable;
-    ENC_CUDA(launch_attention_backward(p, ws, static_cast<cudaStream_t>(stream)));
-    return SIEVE_OK;
+    return launch_attention_backward(p, ws, static_cast<cudaStream_t>(stream));
 }
 
 sieve_status sieve_encoder_status(const void *ws, size_t ws_bytes, int32_t *status, void *stream) {
