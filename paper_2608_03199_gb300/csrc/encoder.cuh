@@ -184,8 +184,6 @@ struct AttentionArgs {
     void *dq, *dk, *dv;
     int64_t dq_ts, dq_hs, dk_ts, dk_hs, dv_ts, dv_hs;
     float *dtable;
-    float *delta;      // backward workspace [heads][q_tokens]
-    float *row_sums;   // [q_tokens][heads][num_buckets]
     EncCtl *ctl;
 };
 size_t attention_workspace_bytes(const sieve_attention_args &a);
