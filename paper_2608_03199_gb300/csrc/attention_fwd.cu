@@ -12,9 +12,10 @@
 // more than 2^8 (its sum uses the same one, so the result is the same softmax;
 // P stays below 2^8, exact in scale): then the thread rescales its row of O.
 //
-// Warps 0-3: softmax and epilogue; warp 4: TMA loads; warp 5: products.  Two
-// blocks share an SM (256 tensor-memory columns each): one's products run
-// under the other's softmax.
+// Warps 0-7 make P (two warps to the 32 lanes of a quarter, 64 columns each,
+// so that a row's scores stay in registers); warp 8 loads and issues the
+// products.  Two blocks share an SM (256 tensor-memory columns each): one's
+// products run under the other's softmax.
 //
 // Where every document has a few new queries against many keys, a block takes
 // the rows of all heads that share a key head (up to 128) over one chunk of
@@ -27,8 +28,10 @@ namespace sieve {
 namespace enc {
 namespace {
 
-constexpr int kSoftmaxWarps = 4;
-constexpr int kThreads = (kSoftmaxWarps + 2) * 32;
+constexpr int kSoftmaxWarps = 8;
+constexpr int kSoftmax = kSoftmaxWarps * 32;
+constexpr int kThreads = kSoftmax + 32;
+constexpr int kHalf = kTile / 2;
 constexpr int kBlocksPerSm = 2;
 constexpr uint32_t kTmemCols = 256;
 constexpr float kRaise = 8.f;
@@ -36,6 +39,12 @@ constexpr float kRaise = 8.f;
 // softmax of this one and the next V under the scores of the next: that is
 // enough, and at 128 columns it lets two blocks share an SM.
 __host__ __device__ constexpr int stages(int dp) { return dp == 64 ? 2 : 1; }
+
+// What the roles of a block need to know of its work.
+struct Work {
+    int q_row, rows, query0;      // first row of q, rows used, query of row 0
+    int k_row, k_first, nk, n_tiles, shift;
+};
 
 struct FwdArgs {
     AttentionArgs p;
@@ -49,38 +58,21 @@ struct FwdArgs {
     float2 *part_ml;     // split: [chunk number][head groups][rows]: maximum (base 2), sum
 };
 
-template <typename T, int DP, bool BIAS, bool SPLIT>
-__global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_constant__ FwdArgs f) {
-    constexpr int kB = DP / 64;                       // column blocks of a tile
-    constexpr int kStages = stages(DP);
-    constexpr uint32_t kTileBytes = kB * kBlockBytes;
-    // tensor memory: S, P and O; with 64 columns of O the three fit side by
-    // side and S of the next tile is computed while P is made, else P takes
-    // the place of S
-    constexpr bool kApart = DP == 64;
-    constexpr uint32_t kPCol = kApart ? 128 : 0, kOCol = kApart ? 192 : 128;
-    extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t q_full, k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages],
-        s_full, s_free, p_full, o_full, drained;
-    __shared__ uint32_t tmem_slot;
-    __shared__ int s_abort;
+template <bool SPLIT>
+__device__ __forceinline__ Work find_work(const FwdArgs &f, int t) {
     const sieve_attention_args &a = f.p.a;
-    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = lane_id();
-
-    if (blockIdx.x == 0 && threadIdx.x == 0) f.p.ctl->status = 0;
-    // ---- the block's work
-    const int groups = a.heads / f.pack;               // tiles' heads
-    const int t = blockIdx.x / groups, hg = blockIdx.x % groups;
-    int s, k_first, k_end, row0, rows;                 // key range, first query of the tile, rows used
+    Work w;
+    w.n_tiles = -1;                                    // nothing to do
+    int s, k_end;
     Doc doc;
     if (SPLIT) {
         s = find_doc(a.k_offsets, (int)a.nseq, (int)a.k_tokens, f.chunk, t);
         doc = doc_at(a, s);
-        k_first = (t - first_tile(a.k_offsets, s, (int)a.k_tokens, f.chunk)) * f.chunk;
-        if (k_first < 0 || k_first >= doc.nk) return;
-        k_end = min(doc.nk, k_first + f.chunk);
-        row0 = 0;
-        rows = f.rows_per_doc;
+        w.k_first = (t - first_tile(a.k_offsets, s, (int)a.k_tokens, f.chunk)) * f.chunk;
+        if (w.k_first < 0 || w.k_first >= doc.nk) return w;
+        k_end = min(doc.nk, w.k_first + f.chunk);
+        w.query0 = 0;
+        w.rows = f.rows_per_doc;
     } else {
         int tile;
         if (a.new_tokens > 0) {
@@ -92,140 +84,187 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
         }
         doc = doc_at(a, s);
         const int tiles = (int)ceil_div(doc.nq, kTile);
-        if (tile < 0 || tile >= tiles) return;
-        row0 = (tiles - 1 - tile) * kTile;             // the tiles that see most keys first
-        rows = min(kTile, doc.nq - row0);
-        k_first = 0;
+        if (tile < 0 || tile >= tiles) return w;
+        w.query0 = (tiles - 1 - tile) * kTile;         // the tiles that see most keys first
+        w.rows = min(kTile, doc.nq - w.query0);
+        w.k_first = 0;
         k_end = doc.nk;
     }
-    const int shift = doc.nk - doc.nq;                 // place of query 0
-    if (a.causal) k_end = min(k_end, (SPLIT ? doc.nq : row0 + rows) + shift);
-    const int n_tiles = k_end > k_first ? (k_end - k_first + kTile - 1) / kTile : 0;
-    const int head0 = hg * f.pack, hk = head0 / (a.heads / a.kv_heads);
+    w.shift = doc.nk - doc.nq;                         // place of query 0
+    w.nk = doc.nk;
+    w.q_row = doc.q0 + w.query0;
+    w.k_row = doc.k0 + w.k_first;
+    if (a.causal) k_end = min(k_end, (SPLIT ? doc.nq : w.query0 + w.rows) + w.shift);
+    w.n_tiles = k_end > w.k_first ? (k_end - w.k_first + kTile - 1) / kTile : 0;
+    return w;
+}
 
+template <typename T, int DP, bool BIAS, bool SPLIT>
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_constant__ FwdArgs f) {
+    constexpr int kB = DP / 64;                       // column blocks of a tile
+    constexpr int kStages = stages(DP);
+    constexpr uint32_t kTileBytes = kB * kBlockBytes;
+    // tensor memory: S, P and O; with 64 columns of O the three fit side by
+    // side and S of the next tile is computed while P is made, else P takes
+    // the place of S (each warp's half within its own columns)
+    constexpr bool kApart = DP == 64;
+    constexpr uint32_t kPCol = kApart ? 128 : 0, kPHalf = kApart ? 32 : 64, kOCol = kApart ? 192 : 128;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t q_full, k_full[kStages], v_full[kStages], s_full, s_free, p_full, o_full, drained,
+        pair_bar[4];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int s_abort;
+    __shared__ Work s_work;
+    __shared__ float s_top[2][2][kTile];
+    const sieve_attention_args &a = f.p.a;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = lane_id();
+
+    const int groups = a.heads / f.pack;               // a tile's heads
+    const int t = blockIdx.x / groups, hg = blockIdx.x % groups;
+    const int head0 = hg * f.pack, hk = head0 / (a.heads / a.kv_heads);
     unsigned char *base = reinterpret_cast<unsigned char *>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     unsigned char *q_tile = base, *k_tiles = base + kTileBytes, *v_tiles = k_tiles + kStages * kTileBytes;
     float *bias = reinterpret_cast<float *>(v_tiles + kStages * kTileBytes);
 
-    if (threadIdx.x == 0) {
-        tc::mbar_init(&q_full, 1);
-        for (int i = 0; i < kStages; ++i) {
-            tc::mbar_init(&k_full[i], 1);
-            tc::mbar_init(&k_empty[i], 1);
-            tc::mbar_init(&v_full[i], 1);
-            tc::mbar_init(&v_empty[i], 1);
+    auto load_k = [&](const Work &w, int j) {
+        const uint32_t lead = lane == 0;
+        const int st = j % kStages;
+        tc::mbar_arrive_expect_tx(lead, &k_full[st], kTileBytes);
+        for (int b = 0; b < kB; ++b)
+            tma_load(lead, k_tiles + st * kTileBytes + b * kBlockBytes, &f.k, 64 * b, hk, w.k_row + j * kTile, &k_full[st]);
+    };
+    auto load_v = [&](const Work &w, int j) {
+        const uint32_t lead = lane == 0;
+        const int st = j % kStages;
+        tc::mbar_arrive_expect_tx(lead, &v_full[st], kTileBytes);
+        for (int b = 0; b < kB; ++b)
+            tma_load(lead, v_tiles + st * kTileBytes + b * kBlockBytes, &f.v, 64 * b, hk, w.k_row + j * kTile, &v_full[st]);
+    };
+
+    Work w;
+    if (warp == kSoftmaxWarps) {
+        // find the work and start its loads while the others set the block up
+        if (lane == 0) {
+            if (blockIdx.x == 0) f.p.ctl->status = 0;
+            tc::mbar_init(&q_full, 1);
+            for (int i = 0; i < kStages; ++i) {
+                tc::mbar_init(&k_full[i], 1);
+                tc::mbar_init(&v_full[i], 1);
+            }
+            tc::mbar_init(&s_full, 1);
+            tc::mbar_init(&s_free, kSoftmax);
+            tc::mbar_init(&p_full, kSoftmax);
+            tc::mbar_init(&o_full, 1);
+            tc::mbar_init(&drained, 1);
+            for (int i = 0; i < 4; ++i) tc::mbar_init(&pair_bar[i], 64);
+            s_abort = 0;
+            tc::mbar_init_fence();
         }
-        tc::mbar_init(&s_full, 1);
-        tc::mbar_init(&s_free, kSoftmaxWarps * 32);
-        tc::mbar_init(&p_full, kSoftmaxWarps * 32);
-        tc::mbar_init(&o_full, 1);
-        tc::mbar_init(&drained, 1);
-        s_abort = 0;
-        tc::mbar_init_fence();
+        __syncwarp();
+        w = find_work<SPLIT>(f, t);
+        if (w.n_tiles > 0) {
+            const uint32_t lead = lane == 0;
+            tc::mbar_arrive_expect_tx(lead, &q_full, kB * 128u * (uint32_t)(f.pack * (kTile / f.pack)));
+            for (int b = 0; b < kB; ++b) tma_load(lead, q_tile + b * kBlockBytes, &f.q, 64 * b, head0, w.q_row, &q_full);
+            for (int j = 0; j < kStages && j < w.n_tiles; ++j) {
+                load_k(w, j);
+                load_v(w, j);
+            }
+        }
+        if (lane == 0) s_work = w;
+    } else {
+        if (warp == 0) tc::tmem_alloc(&tmem_slot, kTmemCols);
+        if (BIAS)
+            for (int h = 0; h < f.pack; ++h)
+                for (int i = threadIdx.x; i < bias_entries(a.reach); i += kSoftmax)
+                    bias[h * f.bias_stride + i] = a.table ? scaled_bias(a, i - a.reach - kPad, head0 + h) : 0.f;
     }
-    if (warp == 5) tc::tmem_alloc(&tmem_slot, kTmemCols);
-    if (BIAS)
-        for (int h = 0; h < f.pack; ++h)
-            for (int i = threadIdx.x; i < bias_entries(a.reach); i += kThreads)
-                bias[h * f.bias_stride + i] = a.table ? scaled_bias(a, i - a.reach - kPad, head0 + h) : 0.f;
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
     const Waiter wait{&s_abort, &f.p.ctl->status};
+    w = s_work;
+    const int n_tiles = w.n_tiles;
 
-    if (warp == 4) {
-        // ---------------- loads ----------------
-        const uint32_t lead = lane == 0;
-        bool ok = n_tiles > 0;
-        int k_issued = 0, v_issued = 0;
-        if (lane == 0) {
-            prefetch_map(&f.q);
-            prefetch_map(&f.k);
-            prefetch_map(&f.v);
-        }
-        if (ok) {
-            tc::mbar_arrive_expect_tx(lead, &q_full, kB * 128u * (uint32_t)(f.pack * (kTile / f.pack)));
-            for (int b = 0; b < kB; ++b)
-                tma_load(lead, q_tile + b * kBlockBytes, &f.q, 64 * b, head0, doc.q0 + row0, &q_full);
-        }
-        for (int j = 0; ok && j < n_tiles; ++j) {
-            const int st = j % kStages;
-            const uint32_t ph = (uint32_t)(j / kStages) & 1u;
-            const int row = doc.k0 + k_first + j * kTile;
-            if (!(ok = wait.warp(&k_empty[st], ph ^ 1u))) break;
-            tc::mbar_arrive_expect_tx(lead, &k_full[st], kTileBytes);
-            for (int b = 0; b < kB; ++b)
-                tma_load(lead, k_tiles + st * kTileBytes + b * kBlockBytes, &f.k, 64 * b, hk, row, &k_full[st]);
-            k_issued = j + 1;
-            if (!(ok = wait.warp(&v_empty[st], ph ^ 1u))) break;
-            tc::mbar_arrive_expect_tx(lead, &v_full[st], kTileBytes);
-            for (int b = 0; b < kB; ++b)
-                tma_load(lead, v_tiles + st * kTileBytes + b * kBlockBytes, &f.v, 64 * b, hk, row, &v_full[st]);
-            v_issued = j + 1;
-        }
-        if (!ok && n_tiles > 0) {
-            // after an abort: the copies in flight land before the block ends
-            auto landed = [&](uint64_t *bar, uint32_t parity) {
-                for (uint32_t it = 0; it < kPolls; ++it)
-                    if (tc::mbar_try_wait(bar, parity)) return;
-            };
-            landed(&q_full, 0);
-            for (int j = max(0, k_issued - kStages); j < k_issued; ++j)
-                landed(&k_full[j % kStages], (uint32_t)(j / kStages) & 1u);
-            for (int j = max(0, v_issued - kStages); j < v_issued; ++j)
-                landed(&v_full[j % kStages], (uint32_t)(j / kStages) & 1u);
-        }
-    } else if (warp == 5) {
-        // ---------------- products ----------------
+    if (n_tiles < 0) {
+        // a tile number that no document uses
+    } else if (warp == kSoftmaxWarps) {
+        // ---------------- loads and products ----------------
         const uint32_t lead = lane == 0;
         constexpr uint32_t id_s = idesc<T>(kTile, false), id_o = idesc<T>(DP, true);
         const uint32_t qa = tc::smem_u32(q_tile);
+        int k_issued = min(kStages, n_tiles), v_issued = k_issued;
         bool ok = n_tiles > 0;
         auto score = [&](int j) {
             const int st = j % kStages;
             if (!wait.warp(&k_full[st], (uint32_t)(j / kStages) & 1u)) return false;
             tc::fence_after_sync();
             mma_kk<DP>(lead, tmem, qa, tc::smem_u32(k_tiles + st * kTileBytes), id_s);
-            tc::mma_commit(lead, &k_empty[st]);
             tc::mma_commit(lead, &s_full);
             return true;
         };
         if (ok) ok = wait.warp(&q_full, 0) && score(0);
         for (int j = 0; ok && j < n_tiles; ++j) {
             const int st = j % kStages;
-            if (kApart && j + 1 < n_tiles) {
-                if (!(ok = wait.warp(&s_free, (uint32_t)j & 1u))) break;
-                if (!(ok = score(j + 1))) break;
+            // the scores are in registers: so their product is done and its K
+            // tile free
+            if (!(ok = wait.warp(&s_free, (uint32_t)j & 1u))) break;
+            if (j + kStages < n_tiles) {
+                load_k(w, j + kStages);
+                k_issued = j + kStages + 1;
             }
+            if (kApart && j + 1 < n_tiles && !(ok = score(j + 1))) break;
             if (!(ok = wait.warp(&v_full[st], (uint32_t)(j / kStages) & 1u))) break;
-            const int left = doc.nk - (k_first + j * kTile);     // keys of the document from this tile on
+            const int left = w.nk - (w.k_first + j * kTile);     // keys of the document from this tile on
             if (left < kTile) clear_rows(v_tiles + st * kTileBytes, left, kB);
             if (!(ok = wait.warp(&p_full, (uint32_t)j & 1u))) break;
             tc::fence_after_sync();
-            mma_tn(lead, tmem + kOCol, tmem + kPCol, tc::smem_u32(v_tiles + st * kTileBytes), id_o, j > 0);
-            tc::mma_commit(lead, &v_empty[st]);
+#pragma unroll
+            for (int k = 0; k < kTile / 16; ++k)
+                tc::mma_f16_ta(lead, tmem + kOCol, tmem + kPCol + (k / 4) * kPHalf + (k % 4) * 8,
+                               desc_mn_sw128(tc::smem_u32(v_tiles + st * kTileBytes) + k * 2048, kBlockBytes), id_o,
+                               j > 0 || k > 0);
             tc::mma_commit(lead, &o_full);
-            if (!kApart && j + 1 < n_tiles) ok = score(j + 1);
+            if (!kApart && j + 1 < n_tiles && !(ok = score(j + 1))) break;
+            // P of this tile was written after the product before it was
+            // done, so with two stages that one's V tile is free; with one
+            // stage this product has to end first
+            if (kStages == 1 && j + 1 < n_tiles && !(ok = wait.warp(&o_full, (uint32_t)j & 1u))) break;
+            if (j + 1 >= kStages && j + 1 < n_tiles) {
+                load_v(w, j + 1);
+                v_issued = j + 2;
+            }
         }
-        // every product issued ends before the block frees its memory (waited
-        // for even after an abort, within the poll limit)
+        // every product issued ends before the block frees its memory, and
+        // after an abort so does every copy (within the poll limit)
+        auto landed = [&](uint64_t *bar, uint32_t parity) {
+            for (uint32_t it = 0; it < kPolls; ++it)
+                if (tc::mbar_try_wait(bar, parity)) return;
+        };
         tc::mma_commit(lead, &drained);
-        for (uint32_t it = 0; it < kPolls; ++it)
-            if (tc::mbar_try_wait(&drained, 0)) break;
+        landed(&drained, 0);
+        if (!ok && n_tiles > 0) {
+            landed(&q_full, 0);
+            for (int j = max(0, k_issued - kStages); j < k_issued; ++j)
+                landed(&k_full[j % kStages], (uint32_t)(j / kStages) & 1u);
+            for (int j = max(0, v_issued - kStages); j < v_issued; ++j)
+                landed(&v_full[j % kStages], (uint32_t)(j / kStages) & 1u);
+        }
         __syncwarp();
     } else {
         // ---------------- softmax and epilogue ----------------
-        const int r = warp * 32 + lane;
-        const bool live = r < rows;
-        const int qi = row0 + (SPLIT ? r / f.pack : r);          // query of the document
+        const int quarter = warp & 3, half = warp >> 2;
+        const int r = quarter * 32 + lane;
+        const bool live = r < w.rows;
+        const int qi = w.query0 + (SPLIT ? r / f.pack : r);      // query of the document
         const int head = head0 + (SPLIT ? r % f.pack : 0);
-        const int place = qi + shift;
-        // keys that this row sees, counted from k_first
-        const int seen = live ? (a.causal ? min(doc.nk, place + 1) : doc.nk) - k_first : 0;
+        const int place = qi + w.shift;
+        // keys that this row sees, counted from this half's first column
+        const int seen = (live ? (a.causal ? min(w.nk, place + 1) : w.nk) - w.k_first : 0) - half * kHalf;
         const float c = a.scale * kLog2e;
-        const uint32_t lane_base = tmem + ((uint32_t)(warp * 32) << 16);
+        const uint32_t lane_base = tmem + ((uint32_t)(quarter * 32) << 16);
         // the warp's places, for the distances that a chunk of keys can have
         int place_lo = live ? place : INT32_MAX, place_hi = live ? place : INT32_MIN;
         if (BIAS) {
@@ -236,61 +275,65 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
             }
         }
         const float *lut = bias + (SPLIT && live ? head - head0 : 0) * f.bias_stride + a.reach + kPad;
-        const float bias_before = BIAS ? lut[-a.reach] : 0.f, bias_after = BIAS ? lut[a.reach] : 0.f;
         float m = -INFINITY, l = 0.f;
         bool ok = true;
         for (int j = 0; j < n_tiles; ++j) {
             if (!(ok = wait.warp(&s_full, (uint32_t)j & 1u))) break;
             tc::fence_after_sync();
-            uint32_t raw[4][32];
+            float x[2][32];
+            {
+                uint32_t raw[2][32];
+                tc::tmem_ld32_issue(lane_base + half * kHalf, raw[0]);
+                tc::tmem_ld32_issue(lane_base + half * kHalf + 32, raw[1]);
+                tc::tmem_ld_wait(raw[0]);
+                tc::tmem_ld_wait(raw[1]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) tc::tmem_ld32_issue(lane_base + 32 * i, raw[i]);
+                for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) tc::tmem_ld_wait(raw[i]);
-            if (kApart) {
-                tc::fence_before_sync();
-                tc::mbar_arrive(&s_free);
+                    for (int e = 0; e < 32; ++e) x[i][e] = __uint_as_float(raw[i][e]);
             }
-            float x[4][32];
-            const int key0 = k_first + j * kTile;                // key of the document in column 0
-            float top = -INFINITY;
+            tc::fence_before_sync();
+            tc::mbar_arrive(&s_free);
+            if (BIAS) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (BIAS) {
-                    const int d0 = key0 + 32 * i;                // distances d0 - place + 0 .. 31
-                    if (d0 - place_hi >= a.reach) {
+                for (int i = 0; i < 2; ++i) {
+                    // distances d0 - place + 0 .. 31
+                    const int d0 = w.k_first + j * kTile + half * kHalf + 32 * i;
+                    const bool after = d0 - place_hi >= a.reach, before = d0 + 31 - place_lo <= -a.reach;
+                    if (after || before) {
+                        const float b = lut[after ? a.reach : -a.reach];
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) x[i][e] = fmaf(__uint_as_float(raw[i][e]), c, bias_after);
-                    } else if (d0 + 31 - place_lo <= -a.reach) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) x[i][e] = fmaf(__uint_as_float(raw[i][e]), c, bias_before);
+                        for (int e = 0; e < 32; ++e) x[i][e] = fmaf(x[i][e], c, b);
                     } else {
                         const float *at = lut + (live ? d0 - place : 0);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) x[i][e] = fmaf(__uint_as_float(raw[i][e]), c, at[e]);
+                        for (int e = 0; e < 32; ++e) x[i][e] = fmaf(x[i][e], c, at[e]);
                     }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) x[i][e] = __uint_as_float(raw[i][e]) * c;
                 }
             }
-            const int vis = seen - j * kTile;                    // columns that this row sees
-            if (!__all_sync(0xffffffffu, vis >= kTile)) {
+            const int vis = seen - j * kTile;                    // columns of the half that this row sees
+            if (!__all_sync(0xffffffffu, vis >= kHalf)) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int e = 0; e < 32; ++e)
                         if (32 * i + e >= vis) x[i][e] = -INFINITY;
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) top = fmaxf(top, max_of_32(x[i]));
-            const bool raise = top > m + kRaise || m == -INFINITY;
+            // the row's maximum over both halves (without a bias the scale is
+            // not negative, so it can be applied after the comparison)
+            float top = fmaxf(max_of_32(x[0]), max_of_32(x[1]));
+            if (!BIAS) top *= c;
+            s_top[j & 1][half][r] = top;
+            tc::mbar_arrive(&pair_bar[quarter]);
+            if (!(ok = wait.warp(&pair_bar[quarter], (uint32_t)j & 1u))) break;
+            top = fmaxf(top, s_top[j & 1][half ^ 1][r]);
             if (j > 0) {
                 // the last tile's product is done with P (and O) before they
                 // are written
                 if (!(ok = wait.warp(&o_full, (uint32_t)(j - 1) & 1u))) break;
                 tc::fence_after_sync();
             }
+            const bool raise = top > m + kRaise || m == -INFINITY;
             if (j == 0) {
                 m = top;
             } else if (__any_sync(0xffffffffu, raise)) {
@@ -300,78 +343,81 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
                 l *= scale;
 #pragma unroll
                 for (int i = 0; i < DP / 32; ++i) {
-                    float o[32];
-                    tc::tmem_ld32(lane_base + kOCol + 32 * i, o);
-                    uint32_t w[32];
+                    uint32_t o[16];
+                    tmem_ld16(lane_base + kOCol + half * (DP / 2) + 16 * i, o);
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(o[e] * scale);
-                    tmem_st32(lane_base + kOCol + 32 * i, w);
+                    for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * scale);
+                    tc::tmem_st16(lane_base + kOCol + half * (DP / 2) + 16 * i, o);
                 }
             }
             const float sub = m == -INFINITY ? 0.f : m;
             float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                uint32_t w[32];
+                uint32_t pk[16];
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    const float p0 = exp2_approx(x[2 * i + e / 16][2 * (e % 16)] - sub);
-                    const float p1 = exp2_approx(x[2 * i + e / 16][2 * (e % 16) + 1] - sub);
-                    sum[e & 3] += p0 + p1;
-                    w[e] = pack2<T>(p0, p1);
+                for (int e = 0; e < 16; ++e) {
+                    const float p0 = exp2_approx(BIAS ? x[i][2 * e] - sub : fmaf(x[i][2 * e], c, -sub));
+                    const float p1 = exp2_approx(BIAS ? x[i][2 * e + 1] - sub : fmaf(x[i][2 * e + 1], c, -sub));
+                    sum[2 * (e & 1)] += p0;
+                    sum[2 * (e & 1) + 1] += p1;
+                    pk[e] = pack2<T>(p0, p1);
                 }
-                tmem_st32(lane_base + kPCol + 32 * i, w);
+                tc::tmem_st16(lane_base + kPCol + half * kPHalf + 16 * i, pk);
             }
             l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
             tc::tmem_st_wait();
             tc::fence_before_sync();
             tc::mbar_arrive(&p_full);
         }
+        // the row's sum over both halves
+        if (ok) {
+            s_top[n_tiles & 1][half][r] = l;
+            tc::mbar_arrive(&pair_bar[quarter]);
+            ok = wait.warp(&pair_bar[quarter], (uint32_t)n_tiles & 1u);
+            l += s_top[n_tiles & 1][half ^ 1][r];
+        }
         if (ok && n_tiles > 0) ok = wait.warp(&o_full, (uint32_t)(n_tiles - 1) & 1u);
         if (ok) {
             tc::fence_after_sync();
             const int d = a.head_dim;
-            if (SPLIT) {
-                const int64_t at = ((int64_t)t * groups + hg) * f.rows_per_doc + r;
-                if (live) f.part_ml[at] = make_float2(m, l);
+            const bool none = n_tiles == 0 || l == 0.f;
+            const float inv = SPLIT ? 1.f : 1.f / l;
+            const int64_t at = ((int64_t)t * groups + hg) * f.rows_per_doc + r;         // split
+            const int64_t row = w.q_row + r;                                            // not split
+            if (live && half == 0) {
+                if (SPLIT) f.part_ml[at] = make_float2(m, l);
+                else f.p.lse[(int64_t)head * a.q_tokens + row] = none ? -INFINITY : m * kLn2 + logf(l);
+            }
 #pragma unroll
-                for (int i = 0; i < DP / 32; ++i) {
-                    float o[32];
-                    if (n_tiles > 0) tc::tmem_ld32(lane_base + kOCol + 32 * i, o);
-                    if (live)
+            for (int i = 0; i < DP / 64; ++i) {
+                const int col = half * (DP / 2) + 32 * i;
+                float o[32];
+                if (n_tiles > 0) tc::tmem_ld32(lane_base + kOCol + col, o);
+                if (!live) continue;
 #pragma unroll
-                        for (int e = 0; e < 32; e += 4)
-                            if (32 * i + e < d)
-                                *reinterpret_cast<float4 *>(f.part_o + at * d + 32 * i + e) =
-                                    n_tiles > 0 ? make_float4(o[e], o[e + 1], o[e + 2], o[e + 3])
-                                                : make_float4(0.f, 0.f, 0.f, 0.f);
-                }
-            } else {
-                const float inv = 1.f / l;
-                const bool none = n_tiles == 0 || l == 0.f;
-                const int64_t row = doc.q0 + qi;
-                T *out = static_cast<T *>(f.p.out) + (row * a.heads + head) * d;
-                if (live) f.p.lse[(int64_t)head * a.q_tokens + row] = none ? -INFINITY : m * kLn2 + logf(l);
+                for (int e = 0; e < 32; ++e) o[e] = none ? 0.f : o[e] * inv;
+                if (SPLIT) {
 #pragma unroll
-                for (int i = 0; i < DP / 32; ++i) {
-                    float o[32];
-                    if (n_tiles > 0) tc::tmem_ld32(lane_base + kOCol + 32 * i, o);
-                    if (live)
+                    for (int e = 0; e < 32; e += 4)
+                        if (col + e < d)
+                            *reinterpret_cast<float4 *>(f.part_o + at * d + col + e) =
+                                make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                } else {
+                    T *out = static_cast<T *>(f.p.out) + (row * a.heads + head) * d;
 #pragma unroll
-                        for (int e = 0; e < 32; e += 8)
-                            if (32 * i + e < d) {
-                                float v[8];
-#pragma unroll
-                                for (int u = 0; u < 8; ++u) v[u] = none ? 0.f : o[e + u] * inv;
-                                store_vec<T, 8>(out + 32 * i + e, v);
-                            }
+                    for (int e = 0; e < 32; e += 8)
+                        if (col + e < d)
+                            *reinterpret_cast<uint4 *>(out + col + e) =
+                                make_uint4(pack2<T>(o[e], o[e + 1]), pack2<T>(o[e + 2], o[e + 3]),
+                                           pack2<T>(o[e + 4], o[e + 5]), pack2<T>(o[e + 6], o[e + 7]));
                 }
             }
         }
     }
     tc::fence_before_sync();
     __syncthreads();
-    if (warp == 5) {
+    if (warp == 0) {
         tc::fence_after_sync();
         tc::tmem_dealloc(tmem, kTmemCols);
     }
