@@ -32,47 +32,75 @@ constexpr uint32_t kPolls = 1u << 24;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-// K-major operand with 128-byte swizzle: tc::desc_k_sw128.  MN-major: the
-// 64-element blocks of the M or N axis lie `block_bytes` apart (leading
-// offset), groups of 8 rows of the contraction axis 1024 bytes apart.
-__device__ __forceinline__ uint64_t desc_mn_sw128(uint32_t saddr, uint32_t block_bytes) {
-    uint64_t d = 0;
-    d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
-    d |= (uint64_t)(block_bytes >> 4) << 16;
-    d |= (uint64_t)(1024 >> 4) << 32;
-    d |= (uint64_t)1 << 46;
-    d |= (uint64_t)2 << 61;
-    return d;
-}
+// Operand descriptors with 128-byte swizzle.  K-major: as in tcgen05.cuh.
+// MN-major: the 64-element blocks of the M or N axis lie kBlockBytes apart
+// (leading offset), groups of 8 rows of the contraction axis 1024 bytes apart.
 
 // Instruction descriptor of kind::f16, fp32 accumulation, M = 128: both
 // operands fp16 (format 0) or bf16 (format 1), B K-major or MN-major (bit 16).
 template <typename T>
-__host__ __device__ constexpr uint32_t idesc(int N, bool b_mn) {
+__host__ __device__ constexpr uint32_t idesc(int N, bool b_mn) {   // N a multiple of 16
     const uint32_t f = std::is_same_v<T, __half> ? 0u : 1u;
     return (1u << 4) | (f << 7) | (f << 10) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) |
            ((uint32_t)(kTile >> 4) << 24);
 }
 
-// D (+)= A B^T, both operands in shared memory and K-major: COLS contraction
+// The products are issued by one elected thread of their warp, whole groups of
+// them under one branch (measured 76 instructions for a group of 12 products
+// and its wait; 175 with every instruction predicated on the lane).
+__device__ __forceinline__ bool elected() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(p));
+    return p != 0;
+}
+__device__ __forceinline__ uint64_t desc_k(const void *tile) {      // K-major
+    return tc::desc_k_sw128(tc::smem_u32(tile));
+}
+__device__ __forceinline__ uint64_t desc_mn(const void *tile) {     // MN-major
+    return (tc::desc_k_sw128(tc::smem_u32(tile)) & ~((uint64_t)0x3FFF << 16)) | (uint64_t)(kBlockBytes >> 4) << 16;
+}
+constexpr uint32_t kBlockStep = kBlockBytes >> 4;                   // in a descriptor's units
+__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(a), "l"(b), "r"(id), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b, uint32_t id, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_tmem), "l"(b), "r"(id), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void commit(uint64_t *bar) { tc::mma_commit(1u, bar); }
+// D = A B^T, both operands in shared memory and K-major: COLS contraction
 // columns in blocks of 64, the blocks of A and B kBlockBytes apart.
 template <int COLS>
-__device__ __forceinline__ void mma_kk(uint32_t lead, uint32_t d_tmem, uint32_t a, uint32_t b, uint32_t id) {
+__device__ __forceinline__ void mma_kk(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t id) {
 #pragma unroll
     for (int k = 0; k < COLS / 16; ++k) {
-        const uint32_t o = (k / 4) * kBlockBytes + (k % 4) * 32;
-        tc::mma_f16(lead, d_tmem, tc::desc_k_sw128(a + o), tc::desc_k_sw128(b + o), id, k > 0);
+        const uint64_t o = (k / 4) * kBlockStep + (k % 4) * 2;
+        mma_ss(d_tmem, a + o, b + o, id, k > 0);
     }
 }
-// D (+)= A B with A (128 x 128, 16-bit pairs) in tensor memory and B a tile
-// whose 128 rows are the contraction axis.
-__device__ __forceinline__ void mma_tn(uint32_t lead, uint32_t d_tmem, uint32_t a_tmem, uint32_t b, uint32_t id,
-                                       uint32_t accumulate) {
+// D (+)= A B with A (128 x 128, 16-bit pairs) in tensor memory, its two halves
+// of 64 columns `kHalfCols` 32-bit columns apart, and B a tile whose rows are
+// the contraction axis.
+template <uint32_t kHalfCols>
+__device__ __forceinline__ void mma_halves(uint32_t d_tmem, uint32_t a_tmem, uint64_t b, uint32_t id,
+                                           uint32_t accumulate) {
 #pragma unroll
     for (int k = 0; k < kTile / 16; ++k)
-        tc::mma_f16_ta(lead, d_tmem, a_tmem + 8 * k, desc_mn_sw128(b + k * 2048, kBlockBytes), id,
-                       accumulate || k > 0);
+        mma_ts(d_tmem, a_tmem + (k / 4) * kHalfCols + (k % 4) * 8, b + k * 128, id, k > 0 ? 1u : accumulate);
 }
+
+// a value that is the same in the whole warp, made so for the compiler too:
+// control flow and operands that depend on it stay in uniform registers (a
+// product issued from others first moves every operand there; measured 2-3K
+// cycles a step)
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 
 __device__ __forceinline__ void tma_load(uint32_t lead, void *dst, const CUtensorMap *map, int c, int h, int t,
                                          uint64_t *bar) {
@@ -116,6 +144,17 @@ __device__ __forceinline__ float exp2_approx(float x) {
     return y;
 }
 
+__device__ __forceinline__ float log2_approx(float x) {   // absolute error at most 2^-22
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp_approx(float x) {    // relative error at most 2^-23
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 // A bounded wait: gives up after the poll limit, or once another role of the
 // block has; the block then records SIEVE_ETIMEOUT and every role winds down.
 struct Waiter {
@@ -137,6 +176,51 @@ struct Waiter {
     }
 };
 
+// Work stealing between the blocks of one grid: a running block asks for the
+// index of one that has not started and takes its place (the grid's hardware
+// scheduler hands each index out once).  Asked by one thread; the answer
+// arrives as 16 bytes in shared memory and completes on `bar`.
+__device__ __forceinline__ void steal_block(uint32_t lead, uint4 *answer, uint64_t *bar) {
+    tc::mbar_arrive_expect_tx(lead, bar, 16);
+    asm volatile(
+        "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t"
+        "@q clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];\n\t}" ::"r"(
+            tc::smem_u32(answer)),
+        "r"(tc::smem_u32(bar)), "r"(lead)
+        : "memory");
+}
+// the stolen block's index, or -1 when none was left (then never ask again)
+__device__ __forceinline__ int stolen_block(const uint4 *answer) {
+    int x;
+    asm volatile(
+        "{\n\t.reg .b128 r;\n\t.reg .pred p;\n\t.reg .b32 x, y, z, w;\n\tld.shared.b128 r, [%1];\n\t"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\tmov.b32 %0, -1;\n\t"
+        "@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {x, y, z, w}, r;\n\t"
+        "@p mov.b32 %0, x;\n\t}"
+        : "=r"(x)
+        : "r"(tc::smem_u32(answer))
+        : "memory");
+    return x;
+}
+
+// two fp32 operations in one instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+        "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+        "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+
 struct Doc {
     int q0, nq, k0, nk;   // first rows and lengths
 };
@@ -152,10 +236,10 @@ __device__ __forceinline__ Doc doc_at(const sieve_attention_args &a, int s) {
     return d;
 }
 
-// Clear the rows [first, 128) of a tile of `blocks` column blocks (a warp).
-__device__ __forceinline__ void clear_rows(unsigned char *tile, int first, int blocks) {
+// Clear the rows [first, end) of a tile of `blocks` column blocks (a warp).
+__device__ __forceinline__ void clear_rows(unsigned char *tile, int first, int blocks, int end = kTile) {
     for (int b = 0; b < blocks; ++b)
-        for (int c = first * 8 + (int)lane_id(); c < kTile * 8; c += 32)
+        for (int c = first * 8 + (int)lane_id(); c < end * 8; c += 32)
             *reinterpret_cast<uint4 *>(tile + b * kBlockBytes + c * 16) = make_uint4(0, 0, 0, 0);
     tc::fence_proxy_async_smem();
     __syncwarp();
@@ -164,15 +248,47 @@ __device__ __forceinline__ void clear_rows(unsigned char *tile, int first, int b
 // The bias by distance of one head, times log2(e), for distances
 // -reach - kPad .. reach + kPad: 32 rows by 32 columns that hold any distance
 // inside (-reach, reach) hold none outside this range, so their lookups need
-// no clamp.  Finite values stay finite: the type's lowest must not become -inf,
-// which hides a key.
+// no clamp.  Finite values stay finite: the type's lowest must not become
+// -inf, which hides a key.
+//
+// A thread needs 32 consecutive entries, from a start that falls by one from
+// lane to lane.  So the table is kept four times, copy s shifted by s entries:
+// whatever its start, a lane reads it from one of them in aligned vectors of
+// four (8 shared-memory instructions for 32 entries; measured 1.5K cycles a
+// tile with single reads).  Copies lie 8 banks apart, and zero distance sits
+// at an index of 3 mod 4: then the 8 lanes of a phase, whose tiles start at
+// multiples of four, hit 32 different banks.
 constexpr int kPad = 64;
 __host__ __device__ __forceinline__ int bias_entries(int reach) { return 2 * (reach + kPad) + 1; }
+__host__ __device__ __forceinline__ int bias_zero(int reach) { return (reach + kPad + 3) / 4 * 4 + 3; }
+__host__ __device__ __forceinline__ int bias_stride(int reach) {   // floats from copy to copy: 8 mod 32
+    return (bias_zero(reach) + reach + kPad + 4 + 31) / 32 * 32 + 8;
+}
+__host__ __device__ __forceinline__ int bias_floats(int reach, int copies = 4) { return copies * bias_stride(reach); }
 __device__ __forceinline__ float scaled_bias(const sieve_attention_args &a, int dist, int head) {
     const int b = __ldg(a.bucket_map + a.reach + min(max(dist, -a.reach), a.reach));
     const float v = __ldg(a.table + min(max(b, 0), a.num_buckets - 1) * a.heads + head);
     const float w = v * kLog2e;
     return isinf(w) && !isinf(v) ? copysignf(3.402823466e38f, v) : w;
+}
+
+// fill the four copies (threads `tid` of `n`); sign = 1: entry i holds distance
+// i - zero, -1: the distance zero - i
+template <int kCopies = 4>
+__device__ __forceinline__ void fill_bias(float *table, const sieve_attention_args &a, int head, int sign, int tid,
+                                          int n) {
+    const int stride = bias_stride(a.reach), zero = bias_zero(a.reach);
+    for (int i = tid; i < stride; i += n) {
+        const float v = a.table ? scaled_bias(a, sign * (i - zero), head) : 0.f;
+#pragma unroll
+        for (int s = 0; s < kCopies; ++s)
+            if (i >= s) table[s * stride + i - s] = v;
+    }
+}
+// the 32 entries from distance `first` on (in the table's direction)
+__device__ __forceinline__ const float4 *bias_at(const float *table, int reach, int first) {
+    const int i = bias_zero(reach) + first;
+    return reinterpret_cast<const float4 *>(table + (i & 3) * bias_stride(reach) + (i & ~3));
 }
 
 // host: a map of [tokens][heads][head_dim], boxes of 64 columns x `box_heads`

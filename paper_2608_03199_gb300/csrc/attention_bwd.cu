@@ -63,16 +63,6 @@ __device__ __forceinline__ int first_q_tile(const BwdArgs &f, int s) {
     return f.p.a.new_tokens > 0 ? s * f.doc_tiles : first_tile(f.p.a.q_offsets, s, (int)f.p.a.q_tokens, kTile);
 }
 
-// D += A B with A's 128 columns in two halves of 64, `half` 32-bit columns
-// apart in tensor memory, B a tile whose rows are the contraction axis
-__device__ __forceinline__ void mma_halves(uint32_t lead, uint32_t d_tmem, uint32_t a_tmem, uint32_t b, uint32_t id,
-                                           uint32_t accumulate) {
-#pragma unroll
-    for (int k = 0; k < kTile / 16; ++k)
-        tc::mma_f16_ta(lead, d_tmem, a_tmem + (k / 4) * kHalf + (k % 4) * 8, desc_mn_sw128(b + k * 2048, kBlockBytes),
-                       id, accumulate || k > 0);
-}
-
 // The eight compute warps meet: bounded like every wait, so a warp that gave
 // up leaves none behind.
 struct Meeting {
@@ -143,7 +133,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dq(const __grid_constant
     }
     if (warp == kWarps + 1) tc::tmem_alloc(&tmem_slot, 512);
     if (BIAS)
-        for (int i = threadIdx.x; i < f.entries; i += kThreads) bias[i] = scaled_bias(a, i - a.reach - kPad, head);
+        fill_bias(bias, a, head, 1, threadIdx.x, kThreads);
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
@@ -185,9 +175,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dq(const __grid_constant
         }
     } else if (warp == kWarps + 1) {
         // ---------------- products ----------------
-        const uint32_t lead = lane == 0;
         constexpr uint32_t id_s = idesc<T>(kTile, false), id_o = idesc<T>(DP, true);
-        const uint32_t qa = tc::smem_u32(q_tile), doa = tc::smem_u32(do_tile);
+        const uint64_t qa = desc_k(q_tile), doa = desc_k(do_tile);
         bool ok = n_tiles > 0;
         auto k_of = [&](int j) { return kv + (j % kStages) * 2 * kTileBytes; };
         auto loaded = [&](int j) {
@@ -200,12 +189,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dq(const __grid_constant
             return true;
         };
         auto score = [&](int j) {
-            mma_kk<DP>(lead, tmem + kSCol + (j & 1) * kTile, qa, tc::smem_u32(k_of(j)), id_s);
-            tc::mma_commit(lead, &s_full[j & 1]);
+            if (elected()) {
+                mma_kk<DP>(tmem + kSCol + (j & 1) * kTile, qa, desc_k(k_of(j)), id_s);
+                commit(&s_full[j & 1]);
+            }
+            __syncwarp();
         };
         auto dprob = [&](int j) {
-            mma_kk<DP>(lead, tmem + kDpCol, doa, tc::smem_u32(k_of(j) + kTileBytes), id_s);
-            tc::mma_commit(lead, &dp_full);
+            if (elected()) {
+                mma_kk<DP>(tmem + kDpCol, doa, desc_k(k_of(j) + kTileBytes), id_s);
+                commit(&dp_full);
+            }
+            __syncwarp();
         };
         if (ok) ok = wait.warp(&q_full, 0) && loaded(0);
         if (ok) {
@@ -223,13 +218,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dq(const __grid_constant
             }
             if (!(ok = wait.warp(&ds_full, (uint32_t)j & 1u))) break;
             tc::fence_after_sync();
-            mma_halves(lead, tmem + kDqCol, tmem + kDpCol, tc::smem_u32(k_of(j)), id_o, j > 0);
-            tc::mma_commit(lead, &kv_empty[j % kStages]);
+            if (elected()) {
+                mma_halves<kHalf>(tmem + kDqCol, tmem + kDpCol, desc_mn(k_of(j)), id_o, j > 0);
+                commit(&kv_empty[j % kStages]);
+            }
+            __syncwarp();
             if (j + 1 < n_tiles) dprob(j + 1);
         }
         // every product issued ends before the block reads dQ or frees its
         // memory (waited for even after an abort, within the poll limit)
-        tc::mma_commit(lead, &done);
+        if (elected()) commit(&done);
+        __syncwarp();
         for (uint32_t it = 0; it < kPolls; ++it)
             if (tc::mbar_try_wait(&done, 0)) break;
         __syncwarp();
@@ -269,8 +268,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dq(const __grid_constant
             place_lo = row0 + quarter * 32 + shift;
             place_hi = place_lo + 31;
         }
-        const float *lut = bias + a.reach + kPad;
-        const float bias_before = BIAS ? lut[-a.reach] : 0.f, bias_after = BIAS ? lut[a.reach] : 0.f;
+        const float bias_before = BIAS ? bias[bias_zero(a.reach) - a.reach] : 0.f;
+        const float bias_after = BIAS ? bias[bias_zero(a.reach) + a.reach] : 0.f;
         float row_sum = 0.f;
         for (int j = 0; ok && j < n_tiles; ++j) {
             if (!(ok = wait.warp(&s_full[j & 1], (uint32_t)(j / 2) & 1u))) break;
@@ -293,10 +292,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dq(const __grid_constant
 #pragma unroll
                         for (int e = 0; e < 32; ++e) p[i][e] = exp2_approx(fmaf(__uint_as_float(raw[i][e]), c, b));
                     } else {
-                        const float *at = lut + (d0 - place);
+                        const float4 *at = bias_at(bias, a.reach, d0 - place);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            p[i][e] = exp2_approx(fmaf(__uint_as_float(raw[i][e]), c, at[e] + nl));
+                        for (int e = 0; e < 8; ++e) {
+                            const float4 b = at[e];
+                            p[i][4 * e + 0] = exp2_approx(fmaf(__uint_as_float(raw[i][4 * e + 0]), c, b.x + nl));
+                            p[i][4 * e + 1] = exp2_approx(fmaf(__uint_as_float(raw[i][4 * e + 1]), c, b.y + nl));
+                            p[i][4 * e + 2] = exp2_approx(fmaf(__uint_as_float(raw[i][4 * e + 2]), c, b.z + nl));
+                            p[i][4 * e + 3] = exp2_approx(fmaf(__uint_as_float(raw[i][4 * e + 3]), c, b.w + nl));
+                        }
                     }
                 }
             }
@@ -336,7 +340,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dq(const __grid_constant
             for (int i = 0; i < DP / 64; ++i) {
                 const int col = half * (DP / 2) + 32 * i;
                 float o[32];
-                if (n_tiles > 0) tc::tmem_ld32(lane_base + kDqCol + col, o);
+                tc::tmem_ld32(lane_base + kDqCol + col, o);
                 if (live)
 #pragma unroll
                     for (int e = 0; e < 32; e += 8)
@@ -399,7 +403,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dkv(const __grid_constan
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     unsigned char *k_tile = base, *v_tile = base + kTileBytes, *qd = v_tile + kTileBytes;
     float *bias = reinterpret_cast<float *>(qd + kStages * 2 * kTileBytes);
-    float *by_distance = bias + f.entries;                     // [warps][entries]
+    // the bias by minus the distance (columns run that way)
+    constexpr int kCopies = DP == 64 ? 4 : 1;
+    float *by_distance = bias + (BIAS ? bias_floats(a.reach, kCopies) : 0);   // [warps][entries]
     float *scratch = by_distance + kWarps * f.entries;         // [warps][kScratch]
 
     if (threadIdx.x == 0) {
@@ -466,9 +472,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dkv(const __grid_constan
         }
     } else if (warp == kWarps + 1) {
         // ---------------- products ----------------
-        const uint32_t lead = lane == 0;
         constexpr uint32_t id_s = idesc<T>(kTile, false), id_o = idesc<T>(DP, true);
-        const uint32_t ka = tc::smem_u32(k_tile), va = tc::smem_u32(v_tile);
+        const uint64_t ka = desc_k(k_tile), va = desc_k(v_tile);
         bool ok = n > 0;
         auto q_of = [&](int i) { return qd + (i % kStages) * 2 * kTileBytes; };
         int qt_loaded = q_first;
@@ -483,12 +488,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dkv(const __grid_constan
             return true;
         };
         auto score = [&](int i) {
-            mma_kk<DP>(lead, tmem + kSCol, ka, tc::smem_u32(q_of(i)), id_s);
-            tc::mma_commit(lead, &s_full);
+            if (elected()) {
+                mma_kk<DP>(tmem + kSCol, ka, desc_k(q_of(i)), id_s);
+                commit(&s_full);
+            }
+            __syncwarp();
         };
         auto dprob = [&](int i) {
-            mma_kk<DP>(lead, tmem + kDpCol, va, tc::smem_u32(q_of(i) + kTileBytes), id_s);
-            tc::mma_commit(lead, &dp_full);
+            if (elected()) {
+                mma_kk<DP>(tmem + kDpCol, va, desc_k(q_of(i) + kTileBytes), id_s);
+                commit(&dp_full);
+            }
+            __syncwarp();
         };
         if (ok) ok = wait.warp(&kv_full, 0) && loaded(0);
         if (ok) {
@@ -499,7 +510,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dkv(const __grid_constan
         for (int i = 0; ok && i < n; ++i) {
             if (!(ok = wait.warp(&p_full, (uint32_t)i & 1u))) break;
             tc::fence_after_sync();
-            mma_halves(lead, tmem + kDvCol, tmem + kSCol, tc::smem_u32(q_of(i) + kTileBytes), id_o, i > 0);
+            if (elected()) mma_halves<kHalf>(tmem + kDvCol, tmem + kSCol, desc_mn(q_of(i) + kTileBytes), id_o, i > 0);
+            __syncwarp();
             if (i + 1 < n) {
                 if (!(ok = loaded(i + 1))) break;
                 tc::fence_after_sync();
@@ -507,13 +519,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dkv(const __grid_constan
             }
             if (!(ok = wait.warp(&ds_full, (uint32_t)i & 1u))) break;
             tc::fence_after_sync();
-            mma_halves(lead, tmem + kDkCol, tmem + kDpCol, tc::smem_u32(q_of(i)), id_o, i > 0);
-            tc::mma_commit(lead, &q_empty[i % kStages]);
+            if (elected()) {
+                mma_halves<kHalf>(tmem + kDkCol, tmem + kDpCol, desc_mn(q_of(i)), id_o, i > 0);
+                commit(&q_empty[i % kStages]);
+            }
+            __syncwarp();
             if (i + 1 < n) dprob(i + 1);
         }
         // every product issued ends before the block reads dK and dV or frees
         // its memory (waited for even after an abort, within the poll limit)
-        tc::mma_commit(lead, &done);
+        if (elected()) commit(&done);
+        __syncwarp();
         for (uint32_t it = 0; it < kPolls; ++it)
             if (tc::mbar_try_wait(&done, 0)) break;
         __syncwarp();
@@ -526,7 +542,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dkv(const __grid_constan
         const float c = a.scale * kLog2e;
         const uint32_t lane_base = tmem + ((uint32_t)(quarter * 32) << 16);
         const int key_lo = key0 + quarter * 32;
-        const float *lut = bias + a.reach + kPad;
         float *mine = by_distance + warp * f.entries, *line = scratch + warp * kScratch;
         const float not_first = lane == 0 ? 0.f : 1.f;
         constexpr float kDown = 1.f / (float)(1 << kPShift<T>);
@@ -539,7 +554,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dkv(const __grid_constan
             if (BIAS && qt == q_first) {
                 // a new head: its bias, and its sums from zero
                 if (!(ok = meet(wait))) break;
-                for (int e = threadIdx.x; e < f.entries; e += kCompute) bias[e] = scaled_bias(a, e - a.reach - kPad, head);
+                fill_bias<kCopies>(bias, a, head, -1, threadIdx.x, kCompute);
                 for (int e = lane; e < f.entries; e += 32) mine[e] = 0.f;
                 far_before = far_after = 0.f;
                 if (!(ok = meet(wait))) break;
@@ -558,7 +573,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dkv(const __grid_constan
                 const int lo = key_lo - (place0 + 32 * q) - 31, hi = key_lo + 31 - (place0 + 32 * q);
                 tc::tmem_ld_wait(raw);
                 if (!BIAS || lo >= a.reach || hi <= -a.reach) {
-                    const float b = !BIAS ? 0.f : lut[lo >= a.reach ? a.reach : -a.reach];
+                    const float b = !BIAS ? 0.f : bias[bias_zero(a.reach) + (lo >= a.reach ? -a.reach : a.reach)];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float4 x = nl[e];
@@ -568,14 +583,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dkv(const __grid_constan
                         p[q][4 * e + 3] = exp2_approx(fmaf(__uint_as_float(raw[4 * e + 3]), c, x.w + b));
                     }
                 } else {
-                    const float *at = lut + (key - (place0 + 32 * q));
+                    const int first = place0 + 32 * q - key;
+                    const float4 *at = bias_at(bias, a.reach, first);
+                    const float *one = bias + bias_zero(a.reach) + first;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float4 x = nl[e];
-                        p[q][4 * e + 0] = exp2_approx(fmaf(__uint_as_float(raw[4 * e + 0]), c, x.x + at[-4 * e - 0]));
-                        p[q][4 * e + 1] = exp2_approx(fmaf(__uint_as_float(raw[4 * e + 1]), c, x.y + at[-4 * e - 1]));
-                        p[q][4 * e + 2] = exp2_approx(fmaf(__uint_as_float(raw[4 * e + 2]), c, x.z + at[-4 * e - 2]));
-                        p[q][4 * e + 3] = exp2_approx(fmaf(__uint_as_float(raw[4 * e + 3]), c, x.w + at[-4 * e - 3]));
+                        const float4 b = kCopies == 4 ? at[e] : make_float4(one[4 * e], one[4 * e + 1], one[4 * e + 2], one[4 * e + 3]);
+                        p[q][4 * e + 0] = exp2_approx(fmaf(__uint_as_float(raw[4 * e + 0]), c, x.x + b.x));
+                        p[q][4 * e + 1] = exp2_approx(fmaf(__uint_as_float(raw[4 * e + 1]), c, x.y + b.y));
+                        p[q][4 * e + 2] = exp2_approx(fmaf(__uint_as_float(raw[4 * e + 2]), c, x.z + b.z));
+                        p[q][4 * e + 3] = exp2_approx(fmaf(__uint_as_float(raw[4 * e + 3]), c, x.w + b.w));
                     }
                 }
             }
@@ -690,7 +708,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dkv(const __grid_constan
 #pragma unroll
             for (int i = 0; i < DP / 32; ++i) {
                 float o[32];
-                if (n > 0) tc::tmem_ld32(lane_base + (half ? kDkCol : kDvCol) + 32 * i, o);
+                tc::tmem_ld32(lane_base + (half ? kDkCol : kDvCol) + 32 * i, o);
                 if (live)
 #pragma unroll
                     for (int e = 0; e < 32; e += 8)
@@ -774,14 +792,14 @@ cudaError_t run(const BwdArgs &f, const Layout &l, unsigned char *ws, cudaStream
     cudaError_t e;
     if (a.q_tokens > 0) {
         auto dq = k_attend_dq<T, DP, BIAS>;
-        const size_t smem = tiles + (size_t)f.entries * 4;
+        const size_t smem = tiles + (BIAS ? (size_t)bias_floats(a.reach) * 4 : 0);
         if ((e = cudaFuncSetAttribute(dq, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
         dq<<<(unsigned)(l.q_tiles * a.heads), kThreads, smem, st>>>(f);
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
     }
     if (a.k_tokens > 0) {
         auto dkv = k_attend_dkv<T, DP, BIAS>;
-        const size_t smem = tiles + (BIAS ? (size_t)f.entries * 4 * (1 + kWarps) + kWarps * kScratch * 4 : 0);
+        const size_t smem = tiles + (BIAS ? (size_t)(bias_floats(a.reach, DP == 64 ? 4 : 1) + f.entries * kWarps + kWarps * kScratch) * 4 : 0);
         if ((e = cudaFuncSetAttribute(dkv, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
         dkv<<<(unsigned)(l.k_tiles * a.kv_heads), kThreads, smem, st>>>(f);
         if ((e = cudaGetLastError()) != cudaSuccess) return e;

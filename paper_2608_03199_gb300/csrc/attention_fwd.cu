@@ -14,8 +14,12 @@
 //
 // Warps 0-7 make P (two warps to the 32 lanes of a quarter, 64 columns each,
 // so that a row's scores stay in registers); warp 8 loads and issues the
-// products.  Two blocks share an SM (256 tensor-memory columns each): one's
-// products run under the other's softmax.
+// products; warp 9 finds the work and loads.  Two blocks share an SM (256
+// tensor-memory columns each): one's products run under the other's softmax.
+// A block that is done takes over one that has not started, found while it
+// still worked, so its loads and products run on from document to document.
+// (Blocks that each set up, worked and ended spent half of their time outside
+// the steps on documents of a few tiles.)
 //
 // Where every document has a few new queries against many keys, a block takes
 // the rows of all heads that share a key head (up to 128) over one chunk of
@@ -30,7 +34,8 @@ namespace {
 
 constexpr int kSoftmaxWarps = 8;
 constexpr int kSoftmax = kSoftmaxWarps * 32;
-constexpr int kThreads = kSoftmax + 32;
+constexpr int kThreads = kSoftmax + 64;
+constexpr int kSlots = 2;     // the work in hand and the next
 constexpr int kHalf = kTile / 2;
 constexpr int kBlocksPerSm = 2;
 constexpr uint32_t kTmemCols = 256;
@@ -40,10 +45,13 @@ constexpr float kRaise = 8.f;
 // enough, and at 128 columns it lets two blocks share an SM.
 __host__ __device__ constexpr int stages(int dp) { return dp == 64 ? 2 : 1; }
 
-// What the roles of a block need to know of its work.
+// One block's work: some tiles of queries of one document, each against the
+// document's keys (or a chunk of them).
 struct Work {
-    int q_row, rows, query0;      // first row of q, rows used, query of row 0
-    int k_row, k_first, nk, n_tiles, shift;
+    int q_row, nq, tile_lo, tile_hi;   // first row of q, queries; tiles, walked from hi - 1 down
+    int k_row, k_first, k_end, nk;     // first row and key of the chunk, its end, the document's keys
+    int group, number;                 // heads, tile or chunk number; group < 0: no more work
+    int table;                         // which bias table
 };
 
 struct FwdArgs {
@@ -52,57 +60,64 @@ struct FwdArgs {
     int pack;            // heads of one key head in a tile (1: a tile is 128 queries of one head)
     int rows_per_doc;    // split: new_tokens * pack
     int chunk;           // split: keys per block
-    int doc_tiles;       // new_tokens > 0, not split: tiles of a document
-    int bias_stride;     // floats between the bias tables of packed heads
+    int doc_tiles;       // new_tokens > 0, not split: blocks of a document
+    int q_tiles;         // not split: tiles of queries per block
+    int numbers;         // tile or chunk numbers; blocks run over them head by head
     float *part_o;       // split: [chunk number][head groups][rows][head_dim]
     float2 *part_ml;     // split: [chunk number][head groups][rows]: maximum (base 2), sum
 };
 
+// False where the block's number is one that no document uses.
 template <bool SPLIT>
-__device__ __forceinline__ Work find_work(const FwdArgs &f, int t) {
+__device__ __forceinline__ bool find_work(const FwdArgs &f, int t, Work &w) {
     const sieve_attention_args &a = f.p.a;
-    Work w;
-    w.n_tiles = -1;                                    // nothing to do
-    int s, k_end;
     Doc doc;
     if (SPLIT) {
-        s = find_doc(a.k_offsets, (int)a.nseq, (int)a.k_tokens, f.chunk, t);
+        const int s = find_doc(a.k_offsets, (int)a.nseq, (int)a.k_tokens, f.chunk, t);
         doc = doc_at(a, s);
         w.k_first = (t - first_tile(a.k_offsets, s, (int)a.k_tokens, f.chunk)) * f.chunk;
-        if (w.k_first < 0 || w.k_first >= doc.nk) return w;
-        k_end = min(doc.nk, w.k_first + f.chunk);
-        w.query0 = 0;
-        w.rows = f.rows_per_doc;
+        if (w.k_first < 0 || w.k_first >= doc.nk) return false;
+        w.k_end = min(doc.nk, w.k_first + f.chunk);
+        w.tile_lo = 0;
+        w.tile_hi = 1;
     } else {
-        int tile;
+        int s, group;
         if (a.new_tokens > 0) {
             s = t / f.doc_tiles;
-            tile = t % f.doc_tiles;
+            group = t % f.doc_tiles;
         } else {
-            s = find_doc(a.q_offsets, (int)a.nseq, (int)a.q_tokens, kTile, t);
-            tile = t - first_tile(a.q_offsets, s, (int)a.q_tokens, kTile);
+            const int step = kTile * f.q_tiles;
+            s = find_doc(a.q_offsets, (int)a.nseq, (int)a.q_tokens, step, t);
+            group = t - first_tile(a.q_offsets, s, (int)a.q_tokens, step);
         }
         doc = doc_at(a, s);
         const int tiles = (int)ceil_div(doc.nq, kTile);
-        if (tile < 0 || tile >= tiles) return w;
-        w.query0 = (tiles - 1 - tile) * kTile;         // the tiles that see most keys first
-        w.rows = min(kTile, doc.nq - w.query0);
+        w.tile_hi = tiles - group * f.q_tiles;         // the tiles that see most keys first
+        if (group < 0 || w.tile_hi <= 0) return false;
+        w.tile_lo = max(0, w.tile_hi - f.q_tiles);
         w.k_first = 0;
-        k_end = doc.nk;
+        w.k_end = doc.nk;
     }
-    w.shift = doc.nk - doc.nq;                         // place of query 0
-    w.nk = doc.nk;
-    w.q_row = doc.q0 + w.query0;
+    w.number = t;
+    w.q_row = doc.q0;
+    w.nq = doc.nq;
     w.k_row = doc.k0 + w.k_first;
-    if (a.causal) k_end = min(k_end, (SPLIT ? doc.nq : w.query0 + w.rows) + w.shift);
-    w.n_tiles = k_end > w.k_first ? (k_end - w.k_first + kTile - 1) / kTile : 0;
-    return w;
+    w.nk = doc.nk;
+    return true;
+}
+
+// key tiles of a tile of queries
+template <bool SPLIT>
+__device__ __forceinline__ int key_tiles(const Work &w, int causal, int tile) {
+    int end = w.k_end;
+    if (causal) end = min(end, (SPLIT ? w.nq : min(w.nq, (tile + 1) * kTile)) + w.nk - w.nq);
+    return end > w.k_first ? (end - w.k_first + kTile - 1) / kTile : 0;
 }
 
 template <typename T, int DP, bool BIAS, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_constant__ FwdArgs f) {
     constexpr int kB = DP / 64;                       // column blocks of a tile
-    constexpr int kStages = stages(DP);
+    constexpr int kStages = stages(DP), kQStages = kStages;
     constexpr uint32_t kTileBytes = kB * kBlockBytes;
     // tensor memory: S, P and O; with 64 columns of O the three fit side by
     // side and S of the next tile is computed while P is made, else P takes
@@ -110,309 +125,461 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
     constexpr bool kApart = DP == 64;
     constexpr uint32_t kPCol = kApart ? 128 : 0, kPHalf = kApart ? 32 : 64, kOCol = kApart ? 192 : 128;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t q_full, k_full[kStages], v_full[kStages], s_full, s_free, p_full, o_full, drained,
-        pair_bar[4];
+    __shared__ __align__(8) uint64_t q_full[kQStages], k_full[kStages], v_full[kStages], s_full, s_free, p_full, o_full,
+        drained, pair_bar[4], work_full[kSlots], work_empty[kSlots], steal_bar, q_empty[kQStages],
+        k_empty[kStages], v_empty[kStages];
+    __shared__ __align__(16) uint4 s_answer;
     __shared__ uint32_t tmem_slot;
     __shared__ int s_abort;
-    __shared__ Work s_work;
+    __shared__ Work s_work[kSlots];
     __shared__ float s_top[2][2][kTile];
     const sieve_attention_args &a = f.p.a;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = lane_id();
-
-    const int groups = a.heads / f.pack;               // a tile's heads
-    const int t = blockIdx.x / groups, hg = blockIdx.x % groups;
-    const int head0 = hg * f.pack, hk = head0 / (a.heads / a.kv_heads);
+    const int share = a.heads / a.kv_heads;
     unsigned char *base = reinterpret_cast<unsigned char *>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-    unsigned char *q_tile = base, *k_tiles = base + kTileBytes, *v_tiles = k_tiles + kStages * kTileBytes;
-    float *bias = reinterpret_cast<float *>(v_tiles + kStages * kTileBytes);
+    unsigned char *q_tiles = base, *k_tiles = q_tiles + kQStages * kTileBytes, *v_tiles = k_tiles + kStages * kTileBytes;
+    float *bias = reinterpret_cast<float *>(v_tiles + kStages * kTileBytes);   // two sets of `pack` tables
+    constexpr int kCopies = SPLIT ? 1 : 4;     // (a chunk of many keys hardly meets the near ones)
+    const int bias_set = BIAS ? f.pack * bias_floats(a.reach, kCopies) : 0;
 
-    auto load_k = [&](const Work &w, int j) {
-        const uint32_t lead = lane == 0;
-        const int st = j % kStages;
-        tc::mbar_arrive_expect_tx(lead, &k_full[st], kTileBytes);
-        for (int b = 0; b < kB; ++b)
-            tma_load(lead, k_tiles + st * kTileBytes + b * kBlockBytes, &f.k, 64 * b, hk, w.k_row + j * kTile, &k_full[st]);
-    };
-    auto load_v = [&](const Work &w, int j) {
-        const uint32_t lead = lane == 0;
-        const int st = j % kStages;
-        tc::mbar_arrive_expect_tx(lead, &v_full[st], kTileBytes);
-        for (int b = 0; b < kB; ++b)
-            tma_load(lead, v_tiles + st * kTileBytes + b * kBlockBytes, &f.v, 64 * b, hk, w.k_row + j * kTile, &v_full[st]);
-    };
-
-    Work w;
-    if (warp == kSoftmaxWarps) {
-        // find the work and start its loads while the others set the block up
-        if (lane == 0) {
-            if (blockIdx.x == 0) f.p.ctl->status = 0;
-            tc::mbar_init(&q_full, 1);
-            for (int i = 0; i < kStages; ++i) {
-                tc::mbar_init(&k_full[i], 1);
-                tc::mbar_init(&v_full[i], 1);
-            }
-            tc::mbar_init(&s_full, 1);
-            tc::mbar_init(&s_free, kSoftmax);
-            tc::mbar_init(&p_full, kSoftmax);
-            tc::mbar_init(&o_full, 1);
-            tc::mbar_init(&drained, 1);
-            for (int i = 0; i < 4; ++i) tc::mbar_init(&pair_bar[i], 64);
-            s_abort = 0;
-            tc::mbar_init_fence();
+    if (threadIdx.x == 0) {
+        if (blockIdx.x == 0) f.p.ctl->status = 0;
+        for (int i = 0; i < kQStages; ++i) {
+            tc::mbar_init(&q_full[i], 1);
+            tc::mbar_init(&q_empty[i], 1);
         }
-        __syncwarp();
-        w = find_work<SPLIT>(f, t);
-        if (w.n_tiles > 0) {
-            const uint32_t lead = lane == 0;
-            tc::mbar_arrive_expect_tx(lead, &q_full, kB * 128u * (uint32_t)(f.pack * (kTile / f.pack)));
-            for (int b = 0; b < kB; ++b) tma_load(lead, q_tile + b * kBlockBytes, &f.q, 64 * b, head0, w.q_row, &q_full);
-            for (int j = 0; j < kStages && j < w.n_tiles; ++j) {
-                load_k(w, j);
-                load_v(w, j);
-            }
+        for (int i = 0; i < kStages; ++i) {
+            tc::mbar_init(&k_empty[i], 1);
+            tc::mbar_init(&v_empty[i], 1);
+            tc::mbar_init(&k_full[i], 1);
+            tc::mbar_init(&v_full[i], 1);
         }
-        if (lane == 0) s_work = w;
-    } else {
-        if (warp == 0) tc::tmem_alloc(&tmem_slot, kTmemCols);
-        if (BIAS)
-            for (int h = 0; h < f.pack; ++h)
-                for (int i = threadIdx.x; i < bias_entries(a.reach); i += kSoftmax)
-                    bias[h * f.bias_stride + i] = a.table ? scaled_bias(a, i - a.reach - kPad, head0 + h) : 0.f;
+        tc::mbar_init(&s_full, 1);
+        tc::mbar_init(&s_free, kSoftmax);
+        tc::mbar_init(&p_full, kSoftmax);
+        tc::mbar_init(&o_full, 1);
+        tc::mbar_init(&drained, 1);
+        tc::mbar_init(&steal_bar, 1);
+        for (int i = 0; i < 4; ++i) tc::mbar_init(&pair_bar[i], 64);
+        for (int i = 0; i < kSlots; ++i) {
+            tc::mbar_init(&work_full[i], 1);
+            tc::mbar_init(&work_empty[i], kSoftmaxWarps + 1);
+        }
+        s_abort = 0;
+        tc::mbar_init_fence();
     }
+    if (warp == 0) tc::tmem_alloc(&tmem_slot, kTmemCols);
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
     const Waiter wait{&s_abort, &f.p.ctl->status};
-    w = s_work;
-    const int n_tiles = w.n_tiles;
 
-    if (n_tiles < 0) {
-        // a tile number that no document uses
-    } else if (warp == kSoftmaxWarps) {
-        // ---------------- loads and products ----------------
+    if (warp == kSoftmaxWarps + 1) {
+        // ---------------- the work, one block's after another's, and its loads ----------------
         const uint32_t lead = lane == 0;
-        constexpr uint32_t id_s = idesc<T>(kTile, false), id_o = idesc<T>(DP, true);
-        const uint32_t qa = tc::smem_u32(q_tile);
-        int k_issued = min(kStages, n_tiles), v_issued = k_issued;
-        bool ok = n_tiles > 0;
-        auto score = [&](int j) {
-            const int st = j % kStages;
-            if (!wait.warp(&k_full[st], (uint32_t)(j / kStages) & 1u)) return false;
-            tc::fence_after_sync();
-            mma_kk<DP>(lead, tmem, qa, tc::smem_u32(k_tiles + st * kTileBytes), id_s);
-            tc::mma_commit(lead, &s_full);
+        if (lane == 0) {
+            prefetch_map(&f.q);
+            prefetch_map(&f.k);
+            prefetch_map(&f.v);
+        }
+        int block = blockIdx.x, item = 0, set = 1, group_in_set = -1, q_issued = 0, k_issued = 0, v_issued = 0;
+        uint32_t asked = 0;
+        bool ok = true, asking = false;
+        auto load_v = [&](int row, int hk) {
+            const int st = v_issued % kStages;
+            if (!wait.warp(&v_empty[st], ((uint32_t)(v_issued / kStages) & 1u) ^ 1u)) return false;
+            tc::mbar_arrive_expect_tx(lead, &v_full[st], kTileBytes);
+            for (int b = 0; b < kB; ++b)
+                tma_load(lead, v_tiles + st * kTileBytes + b * kBlockBytes, &f.v, 64 * b, hk, row, &v_full[st]);
+            ++v_issued;
             return true;
         };
-        if (ok) ok = wait.warp(&q_full, 0) && score(0);
-        for (int j = 0; ok && j < n_tiles; ++j) {
-            const int st = j % kStages;
-            // the scores are in registers: so their product is done and its K
-            // tile free
-            if (!(ok = wait.warp(&s_free, (uint32_t)j & 1u))) break;
-            if (j + kStages < n_tiles) {
-                load_k(w, j + kStages);
-                k_issued = j + kStages + 1;
+        while (ok && block >= 0) {
+            Work w;
+            w.group = block / f.numbers;
+            const int head0 = w.group * f.pack, hk = head0 / share;
+            const bool found = find_work<SPLIT>(f, block % f.numbers, w);
+            if (found && key_tiles<SPLIT>(w, a.causal, w.tile_hi - 1) == 0) {
+                // no query of these sees a key
+                const int first = w.tile_lo * kTile, last = min(w.nq, w.tile_hi * kTile);
+                if (SPLIT) {
+                    for (int r = lane; r < f.rows_per_doc; r += 32)
+                        f.part_ml[((int64_t)w.number * (a.heads / f.pack) + w.group) * f.rows_per_doc + r] =
+                            make_float2(-INFINITY, 0.f);
+                } else {
+                    for (int q = first + lane; q < last; q += 32)
+                        f.p.lse[(int64_t)head0 * a.q_tokens + w.q_row + q] = -INFINITY;
+                    for (int i = lane; i < (last - first) * (a.head_dim / 8); i += 32) {
+                        const int64_t row = w.q_row + first + i / (a.head_dim / 8);
+                        *reinterpret_cast<uint4 *>(static_cast<T *>(f.p.out) + (row * a.heads + head0) * a.head_dim +
+                                                   i % (a.head_dim / 8) * 8) = make_uint4(0, 0, 0, 0);
+                    }
+                }
+            } else if (found) {
+                const int slot = item % kSlots;
+                // the work before the last is done with its slot and its
+                // bias tables
+                if (item >= kSlots && !(ok = wait.warp(&work_empty[slot], (uint32_t)(item / kSlots - 1) & 1u))) break;
+                if (BIAS && w.group != group_in_set) {
+                    set ^= 1;
+                    group_in_set = w.group;
+                    for (int h = 0; h < f.pack; ++h)
+                        fill_bias<kCopies>(bias + set * bias_set + h * bias_floats(a.reach, kCopies), a, head0 + h, 1,
+                                           lane, 32);
+                }
+                w.table = set;
+                if (lane == 0) s_work[slot] = w;
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&work_full[slot]);
+                ++item;
+                int v_row = -1;           // the values of the last step are loaded after the keys of this one:
+                for (int tile = w.tile_hi - 1; ok && tile >= w.tile_lo; --tile) {   // their place is free later
+                    const int n = key_tiles<SPLIT>(w, a.causal, tile);
+                    for (int j = 0; j < n; ++j) {
+                        if (j == 0) {
+                            const int st = q_issued % kQStages;
+                            if (!(ok = wait.warp(&q_empty[st], ((uint32_t)(q_issued / kQStages) & 1u) ^ 1u))) break;
+                            tc::mbar_arrive_expect_tx(lead, &q_full[st],
+                                                      kB * 128u * (uint32_t)(f.pack * (kTile / f.pack)));
+                            for (int b = 0; b < kB; ++b)
+                                tma_load(lead, q_tiles + st * kTileBytes + b * kBlockBytes, &f.q, 64 * b, head0,
+                                         w.q_row + tile * kTile, &q_full[st]);
+                            ++q_issued;
+                        }
+                        const int st = k_issued % kStages, row = w.k_row + j * kTile;
+                        if (!(ok = wait.warp(&k_empty[st], ((uint32_t)(k_issued / kStages) & 1u) ^ 1u))) break;
+                        tc::mbar_arrive_expect_tx(lead, &k_full[st], kTileBytes);
+                        for (int b = 0; b < kB; ++b)
+                            tma_load(lead, k_tiles + st * kTileBytes + b * kBlockBytes, &f.k, 64 * b, hk, row, &k_full[st]);
+                        ++k_issued;
+                        if (kStages == 1) {
+                            if (!(ok = load_v(row, hk))) break;
+                        } else {
+                            if (v_row >= 0 && !(ok = load_v(v_row, hk))) break;
+                            v_row = row;
+                        }
+                    }
+                }
+                if (ok && kStages > 1) ok = load_v(v_row, hk);
+                if (!ok) break;
             }
-            if (kApart && j + 1 < n_tiles && !(ok = score(j + 1))) break;
-            if (!(ok = wait.warp(&v_full[st], (uint32_t)(j / kStages) & 1u))) break;
-            const int left = w.nk - (w.k_first + j * kTile);     // keys of the document from this tile on
-            if (left < kTile) clear_rows(v_tiles + st * kTileBytes, left, kB);
-            if (!(ok = wait.warp(&p_full, (uint32_t)j & 1u))) break;
-            tc::fence_after_sync();
-#pragma unroll
-            for (int k = 0; k < kTile / 16; ++k)
-                tc::mma_f16_ta(lead, tmem + kOCol, tmem + kPCol + (k / 4) * kPHalf + (k % 4) * 8,
-                               desc_mn_sw128(tc::smem_u32(v_tiles + st * kTileBytes) + k * 2048, kBlockBytes), id_o,
-                               j > 0 || k > 0);
-            tc::mma_commit(lead, &o_full);
-            if (!kApart && j + 1 < n_tiles && !(ok = score(j + 1))) break;
-            // P of this tile was written after the product before it was
-            // done, so with two stages that one's V tile is free; with one
-            // stage this product has to end first
-            if (kStages == 1 && j + 1 < n_tiles && !(ok = wait.warp(&o_full, (uint32_t)j & 1u))) break;
-            if (j + 1 >= kStages && j + 1 < n_tiles) {
-                load_v(w, j + 1);
-                v_issued = j + 2;
+            steal_block(lead, &s_answer, &steal_bar);
+            asking = true;
+            if (!(ok = wait.warp(&steal_bar, asked & 1u))) break;
+            ++asked;
+            asking = false;
+            block = stolen_block(&s_answer);
+            tc::fence_proxy_async_smem();     // read before the next answer is written
+            __syncwarp();
+        }
+        if (ok) {
+            const int slot = item % kSlots;
+            ok = item < kSlots || wait.warp(&work_empty[slot], (uint32_t)(item / kSlots - 1) & 1u);
+            if (lane == 0) {
+                s_work[slot].group = -1;
+                tc::mbar_arrive(&work_full[slot]);
             }
         }
-        // every product issued ends before the block frees its memory, and
-        // after an abort so does every copy (within the poll limit)
-        auto landed = [&](uint64_t *bar, uint32_t parity) {
-            for (uint32_t it = 0; it < kPolls; ++it)
-                if (tc::mbar_try_wait(bar, parity)) return;
-        };
-        tc::mma_commit(lead, &drained);
-        landed(&drained, 0);
-        if (!ok && n_tiles > 0) {
-            landed(&q_full, 0);
-            for (int j = max(0, k_issued - kStages); j < k_issued; ++j)
-                landed(&k_full[j % kStages], (uint32_t)(j / kStages) & 1u);
-            for (int j = max(0, v_issued - kStages); j < v_issued; ++j)
-                landed(&v_full[j % kStages], (uint32_t)(j / kStages) & 1u);
+        if (!ok) {
+            // after an abort: what is in flight lands before the block ends
+            auto landed = [&](uint64_t *bar, uint32_t parity) {
+                for (uint32_t it = 0; it < kPolls; ++it)
+                    if (tc::mbar_try_wait(bar, parity)) return;
+            };
+            if (asking) landed(&steal_bar, asked & 1u);
+            for (int i = max(0, q_issued - kQStages); i < q_issued; ++i)
+                landed(&q_full[i % kQStages], (uint32_t)(i / kQStages) & 1u);
+            for (int i = max(0, k_issued - kStages); i < k_issued; ++i)
+                landed(&k_full[i % kStages], (uint32_t)(i / kStages) & 1u);
+            for (int i = max(0, v_issued - kStages); i < v_issued; ++i)
+                landed(&v_full[i % kStages], (uint32_t)(i / kStages) & 1u);
         }
+        __syncwarp();
+    } else if (warp == kSoftmaxWarps) {
+        // ---------------- products ----------------
+        constexpr uint32_t id_o = idesc<T>(DP, true), id_s = idesc<T>(kTile, false);
+        const uint64_t q0 = desc_k(q_tiles), k0 = desc_k(k_tiles), v0 = desc_mn(v_tiles);
+        uint32_t step = 0, q_used = 0;
+        bool ok = true;
+        for (int item = 0; ok; ++item) {
+            const int slot = item % kSlots;
+            if (!(ok = wait.warp(&work_full[slot], (uint32_t)(item / kSlots) & 1u))) break;
+            const Work &w = s_work[slot];
+            if (uniform(w.group) < 0) break;
+            const int lo = uniform(w.tile_lo), keys = uniform(w.nk - w.k_first);
+            int tile = uniform(w.tile_hi) - 1, n = uniform(key_tiles<SPLIT>(w, a.causal, tile)), j = 0;
+            // the scores of step number `i`, the jj-th of nn of its tile
+            auto score = [&](uint32_t i, int jj, int nn) {
+                const uint32_t st = i % kStages, qs = q_used % kQStages;
+                if (jj == 0 && !wait.warp(&q_full[qs], (q_used / kQStages) & 1u)) return false;
+                if (!wait.warp(&k_full[st], (i / kStages) & 1u)) return false;
+                tc::fence_after_sync();
+                if (elected()) {
+                    mma_kk<DP>(tmem, q0 + qs * (kTileBytes >> 4), k0 + st * (kTileBytes >> 4), id_s);
+                    commit(&s_full);
+                    commit(&k_empty[st]);
+                    if (jj == nn - 1) commit(&q_empty[qs]);
+                }
+                __syncwarp();
+                if (jj == nn - 1) ++q_used;
+                return true;
+            };
+            ok = score(step, 0, n);
+            while (ok) {
+                // the step after this one, of the same work
+                int next_tile = tile, next_j = j + 1, next_n = n;
+                if (next_j == n) {
+                    next_j = 0;
+                    next_n = 0;
+                    if (--next_tile >= lo) next_n = uniform(key_tiles<SPLIT>(w, a.causal, next_tile));
+                }
+                const uint32_t st = step % kStages;
+                if (kApart && next_n > 0) {
+                    // this step's scores are in registers
+                    if (!(ok = wait.warp(&s_free, step & 1u))) break;
+                    if (!(ok = score(step + 1, next_j, next_n))) break;
+                }
+                if (!(ok = wait.warp(&v_full[st], (step / kStages) & 1u))) break;
+                const int left = keys - j * kTile;      // a document's last keys may be fewer than a tile
+                if (left < kTile) clear_rows(v_tiles + st * kTileBytes, left, kB);
+                if (!(ok = wait.warp(&p_full, step & 1u))) break;
+                tc::fence_after_sync();
+                if (elected()) {
+                    mma_halves<kPHalf>(tmem + kOCol, tmem + kPCol, v0 + st * (kTileBytes >> 4), id_o, j > 0);
+                    commit(&o_full);
+                    commit(&v_empty[st]);
+                }
+                __syncwarp();
+                if (!kApart && next_n > 0 && !(ok = score(step + 1, next_j, next_n))) break;
+                ++step;
+                tile = next_tile;
+                j = next_j;
+                n = next_n;
+                if (n == 0) break;
+            }
+            __syncwarp();
+            if (ok && lane == 0) tc::mbar_arrive(&work_empty[slot]);
+        }
+        // every product issued ends before the block frees its memory (waited
+        // for even after an abort, within the poll limit)
+        if (elected()) commit(&drained);
+        __syncwarp();
+        for (uint32_t it = 0; it < kPolls; ++it)
+            if (tc::mbar_try_wait(&drained, 0)) break;
         __syncwarp();
     } else {
         // ---------------- softmax and epilogue ----------------
         const int quarter = warp & 3, half = warp >> 2;
         const int r = quarter * 32 + lane;
-        const bool live = r < w.rows;
-        const int qi = w.query0 + (SPLIT ? r / f.pack : r);      // query of the document
-        const int head = head0 + (SPLIT ? r % f.pack : 0);
-        const int place = qi + w.shift;
-        // keys that this row sees, counted from this half's first column
-        const int seen = (live ? (a.causal ? min(w.nk, place + 1) : w.nk) - w.k_first : 0) - half * kHalf;
         const float c = a.scale * kLog2e;
         const uint32_t lane_base = tmem + ((uint32_t)(quarter * 32) << 16);
-        // the warp's places, for the distances that a chunk of keys can have
-        int place_lo = live ? place : INT32_MAX, place_hi = live ? place : INT32_MIN;
-        if (BIAS) {
-#pragma unroll
-            for (int o = 16; o; o >>= 1) {
-                place_lo = min(place_lo, __shfl_xor_sync(0xffffffffu, place_lo, o));
-                place_hi = max(place_hi, __shfl_xor_sync(0xffffffffu, place_hi, o));
-            }
-        }
-        const float *lut = bias + (SPLIT && live ? head - head0 : 0) * f.bias_stride + a.reach + kPad;
-        float m = -INFINITY, l = 0.f;
+        const uint32_t p_at = lane_base + kPCol + half * kPHalf;
+        uint32_t step = 0, meets = 0;                  // steps and meetings of the two halves so far
         bool ok = true;
-        for (int j = 0; j < n_tiles; ++j) {
-            if (!(ok = wait.warp(&s_full, (uint32_t)j & 1u))) break;
-            tc::fence_after_sync();
-            float x[2][32];
-            {
-                uint32_t raw[2][32];
-                tc::tmem_ld32_issue(lane_base + half * kHalf, raw[0]);
-                tc::tmem_ld32_issue(lane_base + half * kHalf + 32, raw[1]);
-                tc::tmem_ld_wait(raw[0]);
-                tc::tmem_ld_wait(raw[1]);
+#pragma unroll 1
+        for (int item = 0; ok; ++item) {
+            if (!(ok = wait.warp(&work_full[item % kSlots], (uint32_t)(item / kSlots) & 1u))) break;
+            const Work &w = s_work[item % kSlots];
+            if (w.group < 0) break;
+            const int head = w.group * f.pack + (SPLIT ? r % f.pack : 0);
+            const float *table =
+                bias + (BIAS ? w.table * bias_set + (SPLIT ? r % f.pack * bias_floats(a.reach, kCopies) : 0) : 0);
+#pragma unroll 1
+            for (int tile = w.tile_hi - 1; ok && tile >= w.tile_lo; --tile) {
+                const int n = key_tiles<SPLIT>(w, a.causal, tile);
+                const int qi = tile * kTile + (SPLIT ? r / f.pack : r);     // query of the document
+                const bool live = SPLIT ? r < f.rows_per_doc : qi < w.nq;
+                // a warp without a live row only keeps the others company
+                const bool idle = SPLIT ? quarter * 32 >= f.rows_per_doc : tile * kTile + quarter * 32 >= w.nq;
+                const int shift = w.nk - w.nq, place = qi + shift;
+                // keys that this row sees, counted from this half's first column
+                const int seen = (live ? (a.causal ? min(w.nk, place + 1) : w.nk) - w.k_first : 0) - half * kHalf;
+                float m = -INFINITY, l = 0.f;
+#pragma unroll 1
+                for (int j = 0; j < n; ++j, ++step) {
+                    if (!(ok = wait.warp(&s_full, step & 1u))) break;
+                    tc::fence_after_sync();
+                    if (idle) {
+                        tc::mbar_arrive(&s_free);
+                        if (step > 0 && !(ok = wait.warp(&o_full, (step - 1) & 1u))) break;
+                        tc::mbar_arrive(&p_full);
+                        continue;
+                    }
+                    float2 x[2][16];
+                    {
+                        uint32_t raw[2][32];
+                        tc::tmem_ld32_issue(lane_base + half * kHalf, raw[0]);
+                        tc::tmem_ld32_issue(lane_base + half * kHalf + 32, raw[1]);
+                        tc::tmem_ld_wait(raw[0]);
+                        tc::tmem_ld_wait(raw[1]);
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+                        for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) x[i][e] = __uint_as_float(raw[i][e]);
-            }
-            tc::fence_before_sync();
-            tc::mbar_arrive(&s_free);
-            if (BIAS) {
+                            for (int e = 0; e < 16; ++e)
+                                x[i][e] = make_float2(__uint_as_float(raw[i][2 * e]), __uint_as_float(raw[i][2 * e + 1]));
+                    }
+                    tc::fence_before_sync();
+                    tc::mbar_arrive(&s_free);
+                    // columns of the half that this row sees; that any row of
+                    // the warp does
+                    const int vis = seen - j * kTile;
+                    const bool all = __all_sync(0xffffffffu, vis >= kHalf);
+                    const int vis_any = all ? kHalf : __reduce_max_sync(0xffffffffu, vis);
+                    if (BIAS) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    // distances d0 - place + 0 .. 31
-                    const int d0 = w.k_first + j * kTile + half * kHalf + 32 * i;
-                    const bool after = d0 - place_hi >= a.reach, before = d0 + 31 - place_lo <= -a.reach;
-                    if (after || before) {
-                        const float b = lut[after ? a.reach : -a.reach];
+                        for (int i = 0; i < 2; ++i) {
+                            if (32 * i >= vis_any) continue;
+                            // distances d0 - place + 0 .. 31; the warp's places
+                            const int d0 = w.k_first + j * kTile + half * kHalf + 32 * i;
+                            const int place_lo = tile * kTile + (SPLIT ? quarter * 32 / f.pack : quarter * 32) + shift;
+                            const int place_hi =
+                                tile * kTile + (SPLIT ? (quarter * 32 + 31) / f.pack : quarter * 32 + 31) + shift;
+                            const bool after = d0 - place_hi >= a.reach, before = d0 + 31 - place_lo <= -a.reach;
+                            if (after || before) {
+                                const float b = table[bias_zero(a.reach) + (after ? a.reach : -a.reach)];
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) x[i][e] = fmaf(x[i][e], c, b);
+                                for (int e = 0; e < 16; ++e)
+                                    x[i][e] = fma2(x[i][e], make_float2(c, c), make_float2(b, b));
+                            } else if (SPLIT) {
+                                const float *b = table + bias_zero(a.reach) + d0 - place;
+#pragma unroll
+                                for (int e = 0; e < 16; ++e)
+                                    x[i][e] = fma2(x[i][e], make_float2(c, c), make_float2(b[2 * e], b[2 * e + 1]));
+                            } else {
+                                const float4 *b = bias_at(table, a.reach, d0 - place);
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) {
+                                    const float4 v = b[e];
+                                    x[i][2 * e] = fma2(x[i][2 * e], make_float2(c, c), make_float2(v.x, v.y));
+                                    x[i][2 * e + 1] = fma2(x[i][2 * e + 1], make_float2(c, c), make_float2(v.z, v.w));
+                                }
+                            }
+                        }
+                    }
+                    if (!all) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                if (32 * i + 2 * e >= vis) x[i][e].x = -INFINITY;
+                                if (32 * i + 2 * e + 1 >= vis) x[i][e].y = -INFINITY;
+                            }
+                    }
+                    float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) t4[e & 3] = fmax3f(t4[e & 3], x[i][e].x, x[i][e].y);
+                    float top = fmaxf(fmax3f(t4[0], t4[1], t4[2]), t4[3]);
+                    // the row's maximum over both halves (without a bias the
+                    // scale is not negative, so it can be applied after the
+                    // comparison)
+                    if (!BIAS) top *= c;
+                    s_top[meets & 1u][half][r] = top;
+                    tc::mbar_arrive(&pair_bar[quarter]);
+                    if (!(ok = wait.warp(&pair_bar[quarter], meets & 1u))) break;
+                    top = fmaxf(top, s_top[meets & 1u][half ^ 1][r]);
+                    ++meets;
+                    // the last step's product is done with P (and O) before
+                    // they are written
+                    if (step > 0 && !(ok = wait.warp(&o_full, (step - 1) & 1u))) break;
+                    tc::fence_after_sync();
+                    const bool raise = top > m + kRaise || m == -INFINITY;
+                    if (j == 0) {
+                        m = top;
+                    } else if (__any_sync(0xffffffffu, raise)) {
+                        const float old = m;
+                        if (raise) m = fmaxf(top, m);
+                        const float scale = raise && old != m ? exp2_approx(old - (m == -INFINITY ? 0.f : m)) : 1.f;
+                        l *= scale;
+#pragma unroll
+                        for (int i = 0; i < DP / 32; ++i) {
+                            uint32_t o[16];
+                            tmem_ld16(lane_base + kOCol + half * (DP / 2) + 16 * i, o);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * scale);
+                            tc::tmem_st16(lane_base + kOCol + half * (DP / 2) + 16 * i, o);
+                        }
+                    }
+                    const float sub = m == -INFINITY ? 0.f : m;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t pk[16];
+                        if (32 * i >= vis_any) {
+                            // no row of the warp sees these; the product may
+                            // still read them
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) pk[e] = 0u;
+                        } else {
+                            float2 s0 = make_float2(0.f, 0.f), s1 = s0;
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                float2 y = BIAS ? add2(x[i][e], make_float2(-sub, -sub))
+                                                : fma2(x[i][e], make_float2(c, c), make_float2(-sub, -sub));
+                                y.x = exp2_approx(y.x);
+                                y.y = exp2_approx(y.y);
+                                if (e & 1) s1 = add2(s1, y);
+                                else s0 = add2(s0, y);
+                                pk[e] = pack2<T>(y.x, y.y);
+                            }
+                            s0 = add2(s0, s1);
+                            l += s0.x + s0.y;
+                        }
+                        tc::tmem_st16(p_at + 16 * i, pk);
+                    }
+                    tc::tmem_st_wait();
+                    tc::fence_before_sync();
+                    tc::mbar_arrive(&p_full);
+                }
+                if (!ok) break;
+                if (idle) continue;
+                // the row's sum over both halves, and the last product
+                s_top[meets & 1u][half][r] = l;
+                tc::mbar_arrive(&pair_bar[quarter]);
+                if (!(ok = wait.warp(&pair_bar[quarter], meets & 1u))) break;
+                l += s_top[meets & 1u][half ^ 1][r];
+                ++meets;
+                if (n > 0 && !(ok = wait.warp(&o_full, (step - 1) & 1u))) break;
+                tc::fence_after_sync();
+                const int d = a.head_dim;
+                const bool none = n == 0 || l == 0.f;
+                const float inv = SPLIT ? 1.f : rcp_approx(l);
+                const int64_t at = ((int64_t)w.number * (a.heads / f.pack) + w.group) * f.rows_per_doc + r;   // split
+                const int64_t row = w.q_row + qi;                                                             // not split
+                if (live && half == 0) {
+                    if (SPLIT) f.part_ml[at] = make_float2(m, l);
+                    else f.p.lse[(int64_t)head * a.q_tokens + row] = none ? -INFINITY : (m + log2_approx(l)) * kLn2;
+                }
+#pragma unroll
+                for (int i = 0; i < DP / 64; ++i) {
+                    const int col = half * (DP / 2) + 32 * i;
+                    float o[32];
+                    tc::tmem_ld32(lane_base + kOCol + col, o);     // (whatever it holds where there was no product)
+                    if (!live) continue;
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = none ? 0.f : o[e] * inv;
+                    if (SPLIT) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4)
+                            if (col + e < d)
+                                *reinterpret_cast<float4 *>(f.part_o + at * d + col + e) =
+                                    make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
                     } else {
-                        const float *at = lut + (live ? d0 - place : 0);
+                        T *out = static_cast<T *>(f.p.out) + (row * a.heads + head) * d;
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) x[i][e] = fmaf(x[i][e], c, at[e]);
+                        for (int e = 0; e < 32; e += 8)
+                            if (col + e < d)
+                                *reinterpret_cast<uint4 *>(out + col + e) =
+                                    make_uint4(pack2<T>(o[e], o[e + 1]), pack2<T>(o[e + 2], o[e + 3]),
+                                               pack2<T>(o[e + 4], o[e + 5]), pack2<T>(o[e + 6], o[e + 7]));
                     }
                 }
+                tc::fence_before_sync();   // O is read before the next tile's first product
             }
-            const int vis = seen - j * kTile;                    // columns of the half that this row sees
-            if (!__all_sync(0xffffffffu, vis >= kHalf)) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if (32 * i + e >= vis) x[i][e] = -INFINITY;
-            }
-            // the row's maximum over both halves (without a bias the scale is
-            // not negative, so it can be applied after the comparison)
-            float top = fmaxf(max_of_32(x[0]), max_of_32(x[1]));
-            if (!BIAS) top *= c;
-            s_top[j & 1][half][r] = top;
-            tc::mbar_arrive(&pair_bar[quarter]);
-            if (!(ok = wait.warp(&pair_bar[quarter], (uint32_t)j & 1u))) break;
-            top = fmaxf(top, s_top[j & 1][half ^ 1][r]);
-            if (j > 0) {
-                // the last tile's product is done with P (and O) before they
-                // are written
-                if (!(ok = wait.warp(&o_full, (uint32_t)(j - 1) & 1u))) break;
-                tc::fence_after_sync();
-            }
-            const bool raise = top > m + kRaise || m == -INFINITY;
-            if (j == 0) {
-                m = top;
-            } else if (__any_sync(0xffffffffu, raise)) {
-                const float old = m;
-                if (raise) m = fmaxf(top, m);
-                const float scale = raise && old != m ? exp2_approx(old - (m == -INFINITY ? 0.f : m)) : 1.f;
-                l *= scale;
-#pragma unroll
-                for (int i = 0; i < DP / 32; ++i) {
-                    uint32_t o[16];
-                    tmem_ld16(lane_base + kOCol + half * (DP / 2) + 16 * i, o);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * scale);
-                    tc::tmem_st16(lane_base + kOCol + half * (DP / 2) + 16 * i, o);
-                }
-            }
-            const float sub = m == -INFINITY ? 0.f : m;
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                uint32_t pk[16];
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const float p0 = exp2_approx(BIAS ? x[i][2 * e] - sub : fmaf(x[i][2 * e], c, -sub));
-                    const float p1 = exp2_approx(BIAS ? x[i][2 * e + 1] - sub : fmaf(x[i][2 * e + 1], c, -sub));
-                    sum[2 * (e & 1)] += p0;
-                    sum[2 * (e & 1) + 1] += p1;
-                    pk[e] = pack2<T>(p0, p1);
-                }
-                tc::tmem_st16(lane_base + kPCol + half * kPHalf + 16 * i, pk);
-            }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-            tc::tmem_st_wait();
-            tc::fence_before_sync();
-            tc::mbar_arrive(&p_full);
-        }
-        // the row's sum over both halves
-        if (ok) {
-            s_top[n_tiles & 1][half][r] = l;
-            tc::mbar_arrive(&pair_bar[quarter]);
-            ok = wait.warp(&pair_bar[quarter], (uint32_t)n_tiles & 1u);
-            l += s_top[n_tiles & 1][half ^ 1][r];
-        }
-        if (ok && n_tiles > 0) ok = wait.warp(&o_full, (uint32_t)(n_tiles - 1) & 1u);
-        if (ok) {
-            tc::fence_after_sync();
-            const int d = a.head_dim;
-            const bool none = n_tiles == 0 || l == 0.f;
-            const float inv = SPLIT ? 1.f : 1.f / l;
-            const int64_t at = ((int64_t)t * groups + hg) * f.rows_per_doc + r;         // split
-            const int64_t row = w.q_row + r;                                            // not split
-            if (live && half == 0) {
-                if (SPLIT) f.part_ml[at] = make_float2(m, l);
-                else f.p.lse[(int64_t)head * a.q_tokens + row] = none ? -INFINITY : m * kLn2 + logf(l);
-            }
-#pragma unroll
-            for (int i = 0; i < DP / 64; ++i) {
-                const int col = half * (DP / 2) + 32 * i;
-                float o[32];
-                if (n_tiles > 0) tc::tmem_ld32(lane_base + kOCol + col, o);
-                if (!live) continue;
-#pragma unroll
-                for (int e = 0; e < 32; ++e) o[e] = none ? 0.f : o[e] * inv;
-                if (SPLIT) {
-#pragma unroll
-                    for (int e = 0; e < 32; e += 4)
-                        if (col + e < d)
-                            *reinterpret_cast<float4 *>(f.part_o + at * d + col + e) =
-                                make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-                } else {
-                    T *out = static_cast<T *>(f.p.out) + (row * a.heads + head) * d;
-#pragma unroll
-                    for (int e = 0; e < 32; e += 8)
-                        if (col + e < d)
-                            *reinterpret_cast<uint4 *>(out + col + e) =
-                                make_uint4(pack2<T>(o[e], o[e + 1]), pack2<T>(o[e + 2], o[e + 3]),
-                                           pack2<T>(o[e + 4], o[e + 5]), pack2<T>(o[e + 6], o[e + 7]));
-                }
-            }
+            __syncwarp();
+            if (ok && lane == 0) tc::mbar_arrive(&work_empty[item % kSlots]);
         }
     }
     tc::fence_before_sync();
@@ -469,19 +636,22 @@ __global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ Fwd
 // document and of a key head's heads fit one tile together.
 struct Shape {
     bool split;
-    int pack, chunk;
+    int pack, chunk, q_tiles, doc_tiles;
     int64_t blocks, chunks;
     size_t smem;
 };
 
-constexpr int kMaxBiasBytes = 24 * 1024;
+// bias tables of a block: what still lets two blocks share an SM
+constexpr int kMaxBiasBytes = 14 * 1024;
 
 Shape shape_of(const sieve_attention_args &a) {
     Shape s = {};
     const int dp = a.head_dim <= 64 ? 64 : 128, share = a.heads / a.kv_heads;
-    const int bias_bytes = a.num_buckets || a.scale < 0.f ? bias_entries(a.reach) * 4 : 0;
+    const bool packed = a.new_tokens > 0 && a.new_tokens <= kTile;
+    // two sets of tables
+    const int bias_bytes = a.num_buckets || a.scale < 0.f ? 2 * 4 * bias_floats(a.reach, packed ? 1 : 4) : 0;
     s.pack = 1;
-    if (a.new_tokens > 0 && a.new_tokens <= kTile) {
+    if (packed) {
         s.split = true;
         for (int p = 1; p <= share; ++p)
             if (share % p == 0 && p * a.new_tokens <= kTile && p * bias_bytes <= kMaxBiasBytes) s.pack = p;
@@ -490,12 +660,15 @@ Shape shape_of(const sieve_attention_args &a) {
         s.chunk = (int)(round_up(want < 2 * kTile ? 2 * kTile : want, kTile));
         s.chunks = doc_tiles(a.k_tokens, a.nseq, s.chunk);
         s.blocks = s.chunks * (a.heads / s.pack);
-    } else if (a.new_tokens > 0) {
-        s.blocks = a.nseq * ceil_div(a.new_tokens, kTile) * a.heads;
     } else {
-        s.blocks = doc_tiles(a.q_tokens, a.nseq, kTile) * a.heads;
+        // several tiles of queries to a block, where that leaves many blocks
+        for (s.q_tiles = 4;; s.q_tiles /= 2) {
+            s.doc_tiles = a.new_tokens > 0 ? (int)ceil_div(a.new_tokens, kTile * s.q_tiles) : 0;
+            s.blocks = (a.new_tokens > 0 ? a.nseq * s.doc_tiles : doc_tiles(a.q_tokens, a.nseq, kTile * s.q_tiles)) * a.heads;
+            if (s.q_tiles == 1 || s.blocks >= 16 * 152 * kBlocksPerSm) break;
+        }
     }
-    s.smem = 1024 + (size_t)(1 + 2 * stages(dp)) * (dp / 64) * kBlockBytes + (size_t)s.pack * bias_bytes;
+    s.smem = 1024 + (size_t)(3 * stages(dp)) * (dp / 64) * kBlockBytes + (size_t)s.pack * bias_bytes;
     return s;
 }
 
@@ -541,8 +714,9 @@ sieve_status launch_attention_forward(const AttentionArgs &p, void *ws, cudaStre
     f.pack = s.pack;
     f.rows_per_doc = a.new_tokens * s.pack;
     f.chunk = s.chunk;
-    f.doc_tiles = a.new_tokens > 0 ? (int)ceil_div(a.new_tokens, kTile) : 0;
-    f.bias_stride = bias_entries(a.reach);
+    f.doc_tiles = s.doc_tiles;
+    f.q_tiles = s.q_tiles;
+    f.numbers = (int)(s.blocks / (a.heads / s.pack));
     f.part_o = reinterpret_cast<float *>(static_cast<unsigned char *>(ws) + kCtlBytes);
     f.part_ml = reinterpret_cast<float2 *>(f.part_o + (s.split ? part_floats(a, s) * a.head_dim : 0));
     sieve_status rc = make_map(&f.q, a.dtype, a.q, a.head_dim, a.heads, a.q_tokens, a.q_token_stride,
