@@ -156,18 +156,19 @@ __device__ __forceinline__ float rcp_approx(float x) {    // relative error at m
 }
 
 // A bounded wait: gives up after the poll limit, or once another role of the
-// block has; the block then records SIEVE_ETIMEOUT and every role winds down.
+// block has; every role then winds down and the block records SIEVE_ETIMEOUT
+// at its end.  (Kept short: it is inlined at every wait, and the kernels'
+// instructions do not fit the first-level instruction caches.)
 struct Waiter {
     int *abort_flag;   // shared memory
-    int32_t *status;   // global
     __device__ __forceinline__ bool operator()(uint64_t *bar, uint32_t parity) const {
         if (tc::mbar_test_wait(bar, parity)) return true;
+#pragma unroll 1
         for (uint32_t it = 0; it < kPolls; ++it) {
             if (tc::mbar_try_wait(bar, parity)) return true;
-            if ((it & 255u) == 255u && *(volatile int *)abort_flag) return false;
+            if ((it & 255u) == 255u && *(volatile int *)abort_flag) break;
         }
-        atomicExch(abort_flag, 1);
-        atomicExch(status, SIEVE_ETIMEOUT);
+        *(volatile int *)abort_flag = 1;
         return false;
     }
     // the same for a whole warp in step
@@ -175,6 +176,12 @@ struct Waiter {
         return __all_sync(0xffffffffu, (*this)(bar, parity));
     }
 };
+// the copies or products in flight after an abort
+__device__ __forceinline__ void let_land(uint64_t *bar, uint32_t parity) {
+#pragma unroll 1
+    for (uint32_t it = 0; it < kPolls; ++it)
+        if (tc::mbar_try_wait(bar, parity)) return;
+}
 
 // Work stealing between the blocks of one grid: a running block asks for the
 // index of one that has not started and takes its place (the grid's hardware
@@ -238,7 +245,9 @@ __device__ __forceinline__ Doc doc_at(const sieve_attention_args &a, int s) {
 
 // Clear the rows [first, end) of a tile of `blocks` column blocks (a warp).
 __device__ __forceinline__ void clear_rows(unsigned char *tile, int first, int blocks, int end = kTile) {
+#pragma unroll 1
     for (int b = 0; b < blocks; ++b)
+#pragma unroll 1
         for (int c = first * 8 + (int)lane_id(); c < end * 8; c += 32)
             *reinterpret_cast<uint4 *>(tile + b * kBlockBytes + c * 16) = make_uint4(0, 0, 0, 0);
     tc::fence_proxy_async_smem();
@@ -278,6 +287,7 @@ template <int kCopies = 4>
 __device__ __forceinline__ void fill_bias(float *table, const sieve_attention_args &a, int head, int sign, int tid,
                                           int n) {
     const int stride = bias_stride(a.reach), zero = bias_zero(a.reach);
+#pragma unroll 1
     for (int i = tid; i < stride; i += n) {
         const float v = a.table ? scaled_bias(a, sign * (i - zero), head) : 0.f;
 #pragma unroll

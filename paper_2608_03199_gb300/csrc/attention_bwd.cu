@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dq(const __grid_constant
     __syncthreads();
     tc::fence_after_sync();
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
-    const Waiter wait{&s_abort, &f.p.ctl->status};
+    const Waiter wait{&s_abort};
 
     if (warp == kWarps) {
         // ---------------- loads ----------------
@@ -165,13 +165,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dq(const __grid_constant
         }
         if (!ok && n_tiles > 0) {
             // after an abort: the copies in flight land before the block ends
-            auto landed = [&](uint64_t *bar, uint32_t parity) {
-                for (uint32_t it = 0; it < kPolls; ++it)
-                    if (tc::mbar_try_wait(bar, parity)) return;
-            };
-            landed(&q_full, 0);
+            let_land(&q_full, 0);
             for (int j = max(0, issued - kStages); j < issued; ++j)
-                landed(&kv_full[j % kStages], (uint32_t)(j / kStages) & 1u);
+                let_land(&kv_full[j % kStages], (uint32_t)(j / kStages) & 1u);
         }
     } else if (warp == kWarps + 1) {
         // ---------------- products ----------------
@@ -229,8 +225,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dq(const __grid_constant
         // memory (waited for even after an abort, within the poll limit)
         if (elected()) commit(&done);
         __syncwarp();
-        for (uint32_t it = 0; it < kPolls; ++it)
-            if (tc::mbar_try_wait(&done, 0)) break;
+        let_land(&done, 0);
         __syncwarp();
     } else {
         // ---------------- P, dS and dQ ----------------
@@ -361,6 +356,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dq(const __grid_constant
     }
     tc::fence_before_sync();
     __syncthreads();
+    if (threadIdx.x == 0 && s_abort) atomicExch(&f.p.ctl->status, SIEVE_ETIMEOUT);
     if (warp == kWarps + 1) {
         tc::fence_after_sync();
         tc::tmem_dealloc(tmem, 512);
@@ -428,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dkv(const __grid_constan
     __syncthreads();
     tc::fence_after_sync();
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
-    const Waiter wait{&s_abort, &f.p.ctl->status};
+    const Waiter wait{&s_abort};
 
     if (warp == kWarps) {
         // ---------------- loads ----------------
@@ -462,13 +458,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dkv(const __grid_constan
         }
         if (!ok && n > 0) {
             // after an abort: the copies in flight land before the block ends
-            auto landed = [&](uint64_t *bar, uint32_t parity) {
-                for (uint32_t it = 0; it < kPolls; ++it)
-                    if (tc::mbar_try_wait(bar, parity)) return;
-            };
-            landed(&kv_full, 0);
+            let_land(&kv_full, 0);
             for (int i = max(0, issued - kStages); i < issued; ++i)
-                landed(&q_full[i % kStages], (uint32_t)(i / kStages) & 1u);
+                let_land(&q_full[i % kStages], (uint32_t)(i / kStages) & 1u);
         }
     } else if (warp == kWarps + 1) {
         // ---------------- products ----------------
@@ -530,8 +522,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dkv(const __grid_constan
         // its memory (waited for even after an abort, within the poll limit)
         if (elected()) commit(&done);
         __syncwarp();
-        for (uint32_t it = 0; it < kPolls; ++it)
-            if (tc::mbar_try_wait(&done, 0)) break;
+        let_land(&done, 0);
         __syncwarp();
     } else {
         // ---------------- P, dS, dK and dV ----------------
@@ -723,6 +714,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_dkv(const __grid_constan
     }
     tc::fence_before_sync();
     __syncthreads();
+    if (threadIdx.x == 0 && s_abort) atomicExch(&f.p.ctl->status, SIEVE_ETIMEOUT);
     if (warp == kWarps + 1) {
         tc::fence_after_sync();
         tc::tmem_dealloc(tmem, 512);

@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
     __syncthreads();
     tc::fence_after_sync();
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
-    const Waiter wait{&s_abort, &f.p.ctl->status};
+    const Waiter wait{&s_abort};
 
     if (warp == kSoftmaxWarps + 1) {
         // ---------------- the work, one block's after another's, and its loads ----------------
@@ -187,15 +187,6 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
         int block = blockIdx.x, item = 0, set = 1, group_in_set = -1, q_issued = 0, k_issued = 0, v_issued = 0;
         uint32_t asked = 0;
         bool ok = true, asking = false;
-        auto load_v = [&](int row, int hk) {
-            const int st = v_issued % kStages;
-            if (!wait.warp(&v_empty[st], ((uint32_t)(v_issued / kStages) & 1u) ^ 1u)) return false;
-            tc::mbar_arrive_expect_tx(lead, &v_full[st], kTileBytes);
-            for (int b = 0; b < kB; ++b)
-                tma_load(lead, v_tiles + st * kTileBytes + b * kBlockBytes, &f.v, 64 * b, hk, row, &v_full[st]);
-            ++v_issued;
-            return true;
-        };
         while (ok && block >= 0) {
             Work w;
             w.group = block / f.numbers;
@@ -234,10 +225,13 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(&work_full[slot]);
                 ++item;
-                int v_row = -1;           // the values of the last step are loaded after the keys of this one:
-                for (int tile = w.tile_hi - 1; ok && tile >= w.tile_lo; --tile) {   // their place is free later
-                    const int n = key_tiles<SPLIT>(w, a.causal, tile);
-                    for (int j = 0; j < n; ++j) {
+                // with two stages the values of a step are loaded after the
+                // keys of the next: their place is free later
+                int tile = w.tile_hi - 1, n = key_tiles<SPLIT>(w, a.causal, tile), j = 0, v_row = -1;
+#pragma unroll 1
+                while (true) {
+                    int row = -1;
+                    if (n > 0) {
                         if (j == 0) {
                             const int st = q_issued % kQStages;
                             if (!(ok = wait.warp(&q_empty[st], ((uint32_t)(q_issued / kQStages) & 1u) ^ 1u))) break;
@@ -248,21 +242,30 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
                                          w.q_row + tile * kTile, &q_full[st]);
                             ++q_issued;
                         }
-                        const int st = k_issued % kStages, row = w.k_row + j * kTile;
+                        const int st = k_issued % kStages;
+                        row = w.k_row + j * kTile;
                         if (!(ok = wait.warp(&k_empty[st], ((uint32_t)(k_issued / kStages) & 1u) ^ 1u))) break;
                         tc::mbar_arrive_expect_tx(lead, &k_full[st], kTileBytes);
                         for (int b = 0; b < kB; ++b)
                             tma_load(lead, k_tiles + st * kTileBytes + b * kBlockBytes, &f.k, 64 * b, hk, row, &k_full[st]);
                         ++k_issued;
-                        if (kStages == 1) {
-                            if (!(ok = load_v(row, hk))) break;
-                        } else {
-                            if (v_row >= 0 && !(ok = load_v(v_row, hk))) break;
-                            v_row = row;
+                        if (++j == n) {
+                            j = n = 0;
+                            if (--tile >= w.tile_lo) n = key_tiles<SPLIT>(w, a.causal, tile);
                         }
                     }
+                    if (kStages == 1) v_row = row;
+                    if (v_row >= 0) {
+                        const int st = v_issued % kStages;
+                        if (!(ok = wait.warp(&v_empty[st], ((uint32_t)(v_issued / kStages) & 1u) ^ 1u))) break;
+                        tc::mbar_arrive_expect_tx(lead, &v_full[st], kTileBytes);
+                        for (int b = 0; b < kB; ++b)
+                            tma_load(lead, v_tiles + st * kTileBytes + b * kBlockBytes, &f.v, 64 * b, hk, v_row, &v_full[st]);
+                        ++v_issued;
+                    }
+                    if (row < 0) break;
+                    v_row = row;
                 }
-                if (ok && kStages > 1) ok = load_v(v_row, hk);
                 if (!ok) break;
             }
             steal_block(lead, &s_answer, &steal_bar);
@@ -284,17 +287,13 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
         }
         if (!ok) {
             // after an abort: what is in flight lands before the block ends
-            auto landed = [&](uint64_t *bar, uint32_t parity) {
-                for (uint32_t it = 0; it < kPolls; ++it)
-                    if (tc::mbar_try_wait(bar, parity)) return;
-            };
-            if (asking) landed(&steal_bar, asked & 1u);
+            if (asking) let_land(&steal_bar, asked & 1u);
             for (int i = max(0, q_issued - kQStages); i < q_issued; ++i)
-                landed(&q_full[i % kQStages], (uint32_t)(i / kQStages) & 1u);
+                let_land(&q_full[i % kQStages], (uint32_t)(i / kQStages) & 1u);
             for (int i = max(0, k_issued - kStages); i < k_issued; ++i)
-                landed(&k_full[i % kStages], (uint32_t)(i / kStages) & 1u);
+                let_land(&k_full[i % kStages], (uint32_t)(i / kStages) & 1u);
             for (int i = max(0, v_issued - kStages); i < v_issued; ++i)
-                landed(&v_full[i % kStages], (uint32_t)(i / kStages) & 1u);
+                let_land(&v_full[i % kStages], (uint32_t)(i / kStages) & 1u);
         }
         __syncwarp();
     } else if (warp == kSoftmaxWarps) {
@@ -310,54 +309,56 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
             if (uniform(w.group) < 0) break;
             const int lo = uniform(w.tile_lo), keys = uniform(w.nk - w.k_first);
             int tile = uniform(w.tile_hi) - 1, n = uniform(key_tiles<SPLIT>(w, a.causal, tile)), j = 0;
-            // the scores of step number `i`, the jj-th of nn of its tile
-            auto score = [&](uint32_t i, int jj, int nn) {
-                const uint32_t st = i % kStages, qs = q_used % kQStages;
-                if (jj == 0 && !wait.warp(&q_full[qs], (q_used / kQStages) & 1u)) return false;
-                if (!wait.warp(&k_full[st], (i / kStages) & 1u)) return false;
-                tc::fence_after_sync();
-                if (elected()) {
-                    mma_kk<DP>(tmem, q0 + qs * (kTileBytes >> 4), k0 + st * (kTileBytes >> 4), id_s);
-                    commit(&s_full);
-                    commit(&k_empty[st]);
-                    if (jj == nn - 1) commit(&q_empty[qs]);
+            // (tile, j of n): the step whose scores are next; `key`: the
+            // first key of the one whose P is
+            int key = 0;
+            bool first = true;                          // no P yet
+#pragma unroll 1
+            while (true) {
+                const bool scored = n > 0;
+                const int next_key = j * kTile;
+                // with P apart from S the next scores come before this step's
+                // product with P (as soon as this step's are in registers)
+                for (int part = 0; part < 2; ++part) {
+                    if ((part == 0) == kApart) {
+                        if (!scored) continue;
+                        const uint32_t i = step + (first ? 0u : 1u), st = i % kStages, qs = q_used % kQStages;
+                        if (kApart && !first && !(ok = wait.warp(&s_free, step & 1u))) break;
+                        if (j == 0 && !(ok = wait.warp(&q_full[qs], (q_used / kQStages) & 1u))) break;
+                        if (!(ok = wait.warp(&k_full[st], (i / kStages) & 1u))) break;
+                        tc::fence_after_sync();
+                        if (elected()) {
+                            mma_kk<DP>(tmem, q0 + qs * (kTileBytes >> 4), k0 + st * (kTileBytes >> 4), id_s);
+                            commit(&s_full);
+                            commit(&k_empty[st]);
+                            if (j == n - 1) commit(&q_empty[qs]);
+                        }
+                        __syncwarp();
+                        if (++j == n) {
+                            ++q_used;
+                            j = n = 0;
+                            if (--tile >= lo) n = uniform(key_tiles<SPLIT>(w, a.causal, tile));
+                        }
+                    } else {
+                        if (first) continue;
+                        const uint32_t st = step % kStages;
+                        if (!(ok = wait.warp(&v_full[st], (step / kStages) & 1u))) break;
+                        if (keys - key < kTile) clear_rows(v_tiles + st * kTileBytes, keys - key, kB);
+                        if (!(ok = wait.warp(&p_full, step & 1u))) break;
+                        tc::fence_after_sync();
+                        if (elected()) {
+                            mma_halves<kPHalf>(tmem + kOCol, tmem + kPCol, v0 + st * (kTileBytes >> 4), id_o, key > 0);
+                            commit(&o_full);
+                            commit(&v_empty[st]);
+                        }
+                        __syncwarp();
+                    }
                 }
-                __syncwarp();
-                if (jj == nn - 1) ++q_used;
-                return true;
-            };
-            ok = score(step, 0, n);
-            while (ok) {
-                // the step after this one, of the same work
-                int next_tile = tile, next_j = j + 1, next_n = n;
-                if (next_j == n) {
-                    next_j = 0;
-                    next_n = 0;
-                    if (--next_tile >= lo) next_n = uniform(key_tiles<SPLIT>(w, a.causal, next_tile));
-                }
-                const uint32_t st = step % kStages;
-                if (kApart && next_n > 0) {
-                    // this step's scores are in registers
-                    if (!(ok = wait.warp(&s_free, step & 1u))) break;
-                    if (!(ok = score(step + 1, next_j, next_n))) break;
-                }
-                if (!(ok = wait.warp(&v_full[st], (step / kStages) & 1u))) break;
-                const int left = keys - j * kTile;      // a document's last keys may be fewer than a tile
-                if (left < kTile) clear_rows(v_tiles + st * kTileBytes, left, kB);
-                if (!(ok = wait.warp(&p_full, step & 1u))) break;
-                tc::fence_after_sync();
-                if (elected()) {
-                    mma_halves<kPHalf>(tmem + kOCol, tmem + kPCol, v0 + st * (kTileBytes >> 4), id_o, j > 0);
-                    commit(&o_full);
-                    commit(&v_empty[st]);
-                }
-                __syncwarp();
-                if (!kApart && next_n > 0 && !(ok = score(step + 1, next_j, next_n))) break;
-                ++step;
-                tile = next_tile;
-                j = next_j;
-                n = next_n;
-                if (n == 0) break;
+                if (!ok) break;
+                if (!first) ++step;
+                first = false;
+                if (!scored) break;
+                key = next_key;
             }
             __syncwarp();
             if (ok && lane == 0) tc::mbar_arrive(&work_empty[slot]);
@@ -366,8 +367,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
         // for even after an abort, within the poll limit)
         if (elected()) commit(&drained);
         __syncwarp();
-        for (uint32_t it = 0; it < kPolls; ++it)
-            if (tc::mbar_try_wait(&drained, 0)) break;
+        let_land(&drained, 0);
         __syncwarp();
     } else {
         // ---------------- softmax and epilogue ----------------
@@ -584,6 +584,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
     }
     tc::fence_before_sync();
     __syncthreads();
+    if (threadIdx.x == 0 && s_abort) atomicExch(&f.p.ctl->status, SIEVE_ETIMEOUT);
     if (warp == 0) {
         tc::fence_after_sync();
         tc::tmem_dealloc(tmem, kTmemCols);
@@ -594,13 +595,12 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
 template <typename T>
 __global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ FwdArgs f) {
     const sieve_attention_args &a = f.p.a;
-    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    if (w >= a.q_tokens * a.heads) return;
+    const unsigned w = blockIdx.x * 4 + (threadIdx.x >> 5);     // query and head
+    if (w >= (unsigned)a.q_tokens * a.heads) return;
     const int lane = lane_id(), d = a.head_dim, groups = a.heads / f.pack;
-    const int64_t row = w / a.heads;
-    const int head = (int)(w % a.heads), s = (int)(row / a.new_tokens), qi = (int)(row % a.new_tokens);
+    const int row = w / a.heads, head = w % a.heads, s = row / a.new_tokens, qi = row % a.new_tokens;
     const Doc doc = doc_at(a, s);
-    const int t0 = first_tile(a.k_offsets, s, (int)a.k_tokens, f.chunk), n = (int)ceil_div(doc.nk, f.chunk);
+    const int t0 = first_tile(a.k_offsets, s, (int)a.k_tokens, f.chunk), n = (doc.nk + f.chunk - 1) / f.chunk;
     const int r = qi * f.pack + head % f.pack;
     auto slot = [&](int i) { return ((int64_t)(t0 + i) * groups + head / f.pack) * f.rows_per_doc + r; };
     float top = -INFINITY;
@@ -628,7 +628,7 @@ __global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ Fwd
         uint2 o;
         o.x = pack2<T>(acc[0] * inv, acc[1] * inv);
         o.y = pack2<T>(acc[2] * inv, acc[3] * inv);
-        *reinterpret_cast<uint2 *>(static_cast<T *>(f.p.out) + w * d + 4 * lane) = o;
+        *reinterpret_cast<uint2 *>(static_cast<T *>(f.p.out) + (int64_t)w * d + 4 * lane) = o;
     }
 }
 
