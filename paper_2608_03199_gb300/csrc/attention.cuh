@@ -85,15 +85,16 @@ __device__ __forceinline__ void mma_kk(uint32_t d_tmem, uint64_t a, uint64_t b, 
         mma_ss(d_tmem, a + o, b + o, id, k > 0);
     }
 }
-// D (+)= A B with A (128 x 128, 16-bit pairs) in tensor memory, its two halves
-// of 64 columns `kHalfCols` 32-bit columns apart, and B a tile whose rows are
-// the contraction axis.
-template <uint32_t kHalfCols>
-__device__ __forceinline__ void mma_halves(uint32_t d_tmem, uint32_t a_tmem, uint64_t b, uint32_t id,
+// D (+)= A B with A (128 x 128, 16-bit pairs) in tensor memory, kept in groups
+// of kCols columns: a group's pairs at the start of the kStride 32-bit columns
+// of its own.  B a tile whose rows are the contraction axis.
+template <int kCols, int kStride>
+__device__ __forceinline__ void mma_groups(uint32_t d_tmem, uint32_t a_tmem, uint64_t b, uint32_t id,
                                            uint32_t accumulate) {
 #pragma unroll
     for (int k = 0; k < kTile / 16; ++k)
-        mma_ts(d_tmem, a_tmem + (k / 4) * kHalfCols + (k % 4) * 8, b + k * 128, id, k > 0 ? 1u : accumulate);
+        mma_ts(d_tmem, a_tmem + (16 * k / kCols) * kStride + (16 * k % kCols) / 2, b + k * 128, id,
+               k > 0 ? 1u : accumulate);
 }
 
 // a value that is the same in the whole warp, made so for the compiler too:
@@ -102,15 +103,15 @@ __device__ __forceinline__ void mma_halves(uint32_t d_tmem, uint32_t a_tmem, uin
 // cycles a step)
 __device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 
-__device__ __forceinline__ void tma_load(uint32_t lead, void *dst, const CUtensorMap *map, int c, int h, int t,
-                                         uint64_t *bar) {
+// one thread: a box of a map, and the bytes announced on `bar`
+__device__ __forceinline__ void tma_load(void *dst, const CUtensorMap *map, int c, int h, int t, uint64_t *bar) {
     asm volatile(
-        "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %6, 0;\n\t"
-        "@q cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
-        "[%0], [%1, {%2, %3, %4}], [%5];\n\t}" ::"r"(tc::smem_u32(dst)),
-        "l"(map), "r"(c), "r"(h), "r"(t), "r"(tc::smem_u32(bar)), "r"(lead)
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], "
+        "[%5];" ::"r"(tc::smem_u32(dst)),
+        "l"(map), "r"(c), "r"(h), "r"(t), "r"(tc::smem_u32(bar))
         : "memory");
 }
+__device__ __forceinline__ void expect(uint64_t *bar, uint32_t bytes) { tc::mbar_arrive_expect_tx(1u, bar, bytes); }
 __device__ __forceinline__ void prefetch_map(const CUtensorMap *map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
@@ -210,7 +211,38 @@ __device__ __forceinline__ int stolen_block(const uint4 *answer) {
     return x;
 }
 
+// The blocks of one grid, one after the other: this one's own, then what it
+// takes over from blocks that have not started.
+struct Blocks {
+    uint4 *answer;
+    uint64_t *bar;
+    uint32_t asked;
+    bool asking;
+    // the next block's index in `block`, or -1; false: the wait gave up
+    __device__ __forceinline__ bool next(const Waiter &wait, int &block) {
+        if (elected()) steal_block(1u, answer, bar);
+        __syncwarp();
+        asking = true;
+        if (!wait.warp(bar, asked & 1u)) return false;
+        ++asked;
+        asking = false;
+        block = stolen_block(answer);
+        tc::fence_proxy_async_smem();     // read before the next answer is written
+        __syncwarp();
+        return true;
+    }
+};
+
 // two fp32 operations in one instruction
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+        "mul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
     float2 d;
     asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"

@@ -20,10 +20,13 @@
 // and the table's gradient: dS summed along diagonals (equal distances), in
 // fp32, before any rounding.
 //
-// In both, warps 0-7 make P and dS (two warps to 32 lanes, 64 columns each),
-// warp 8 loads, warp 9 issues the products: while the threads turn S into P
+// In both, 16 warps (8 where shared memory has no room for 16 sets of sums by
+// distance) make P and dS, each for 32 lanes and its share of the columns; one
+// more loads, one more issues the products.  While the threads turn S into P
 // the tensor cores work on dP and the product before, and the other way
-// round.  A block takes all of tensor memory, so one runs per SM.
+// round.  A block takes all of tensor memory, so one runs per SM; when it is
+// done it takes over a block that has not started, whose loads and first
+// products run under its last sums and stores.
 #include <cstring>
 
 #include "attention.cuh"
@@ -32,10 +35,7 @@ namespace sieve {
 namespace enc {
 namespace {
 
-constexpr int kWarps = 8;
-constexpr int kCompute = kWarps * 32;
-constexpr int kThreads = kCompute + 64;
-constexpr int kHalf = kTile / 2;
+constexpr int kSlots = 2;      // the work in hand and the next
 constexpr int kScratch = 64;   // floats per warp for the diagonals of 32 x 32
 
 // k_attend_dkv rounds P to 16 bits.  A long document's probabilities are small
@@ -50,20 +50,23 @@ constexpr int kPShift = std::is_same_v<T, __half> ? 14 : 0;
 struct BwdArgs {
     AttentionArgs p;
     CUtensorMap q, k, v, dout;
-    float *stats;      // [q tile][head][2][128]: kPShift - lse in base 2, 2^-kPShift delta
+    float *stats;      // [q tile][head][2][128]: kPShift - lse in base 2, -2^-kPShift delta
     float *partial;    // [k tile][head][entries]: dS by distance
     int doc_tiles;     // new_tokens > 0: q tiles of a document
     int entries;       // bias_entries(reach)
+    int q_numbers, k_numbers;   // tile numbers; blocks run over them head by head
 };
 
-// tiles of the walked operand pair held at a time
-__host__ __device__ constexpr int stages(int dp) { return dp == 64 ? 3 : 2; }
+// Tiles held at a time: of the operand pair a block walks, and of the pair it
+// keeps (two: the next work's is loaded while this one's is in use).
+__host__ __device__ constexpr int walked(int) { return 2; }
+__host__ __device__ constexpr int kept(int dp) { return dp == 64 ? 2 : 1; }
 
 __device__ __forceinline__ int first_q_tile(const BwdArgs &f, int s) {
     return f.p.a.new_tokens > 0 ? s * f.doc_tiles : first_tile(f.p.a.q_offsets, s, (int)f.p.a.q_tokens, kTile);
 }
 
-// The eight compute warps meet: bounded like every wait, so a warp that gave
+// The threads that compute meet: bounded like every wait, so a warp that gave
 // up leaves none behind.
 struct Meeting {
     uint64_t *bar;
@@ -76,646 +79,849 @@ struct Meeting {
     }
 };
 
+// A warp's columns: kCols of the 128, read and written where they are.
+template <int kWarps>
+struct Columns {
+    static constexpr int kGroups = kWarps / 4, kCols = kTile / kGroups, kChunks = kCols / 32;
+};
+
+// One block's work.
+struct DqWork {
+    int head, q_row, row0, nq, k_row, nk, n, stats;   // head < 0: no more; n: key tiles
+};
+struct DkvWork {
+    int hk, k_row, key0, nk, q_row, nq, q_first, q_tiles, q_number, number;   // hk < 0: no more
+};
+
 template <typename T, int DP, bool BIAS>
-__global__ void __launch_bounds__(kThreads, 1) k_attend_dq(const __grid_constant__ BwdArgs f) {
-    constexpr int kB = DP / 64, kStages = stages(DP);
+__global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant__ BwdArgs f) {
+    constexpr int kWarps = 16, kCompute = kWarps * 32;
+    constexpr int kGroups = Columns<kWarps>::kGroups, kCols = Columns<kWarps>::kCols;
+    constexpr int kB = DP / 64, kWalked = walked(DP), kKept = kept(DP);
     constexpr uint32_t kTileBytes = kB * kBlockBytes;
     constexpr uint32_t kSCol = 0, kDpCol = 256, kDqCol = 384;   // S twice, dP (dS in its place), dQ
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t q_full, kv_full[kStages], kv_empty[kStages], s_full[2], s_free[2], dp_full,
-        ds_full, meet_bar, done;
+    __shared__ __align__(8) uint64_t q_full[kKept], q_empty[kKept], kv_full[kWalked], kv_empty[kWalked], s_full[2],
+        s_free[2], dp_full, ds_full, dq_full, meet_bar, done, work_full[kSlots], work_empty[kSlots], steal_bar;
+    __shared__ __align__(16) uint4 s_answer;
     __shared__ uint32_t tmem_slot;
     __shared__ int s_abort;
-    __shared__ float s_row[2][kTile];
+    __shared__ DqWork s_work[kSlots];
+    __shared__ float s_row[2][kGroups][kTile];
     const sieve_attention_args &a = f.p.a;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = lane_id();
-    if (blockIdx.x == 0 && threadIdx.x == 0) f.p.ctl->status = 0;
-
-    const int t = blockIdx.x / a.heads, head = blockIdx.x % a.heads, hk = head / (a.heads / a.kv_heads);
-    int s, tile;
-    if (a.new_tokens > 0) {
-        s = t / f.doc_tiles;
-        tile = t % f.doc_tiles;
-    } else {
-        s = find_doc(a.q_offsets, (int)a.nseq, (int)a.q_tokens, kTile, t);
-        tile = t - first_tile(a.q_offsets, s, (int)a.q_tokens, kTile);
-    }
-    const Doc doc = doc_at(a, s);
-    const int tiles = (int)ceil_div(doc.nq, kTile);
-    if (tile < 0 || tile >= tiles) return;
-    tile = tiles - 1 - tile;                           // the tiles that see most keys first
-    const int row0 = tile * kTile, rows = min(kTile, doc.nq - row0), shift = doc.nk - doc.nq;
-    const int k_end = a.causal ? min(doc.nk, row0 + rows + shift) : doc.nk;
-    const int n_tiles = k_end > 0 ? (k_end + kTile - 1) / kTile : 0;
-    float *stats = f.stats + ((int64_t)(first_q_tile(f, s) + tile) * a.heads + head) * 2 * kTile;
 
     unsigned char *base = reinterpret_cast<unsigned char *>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-    unsigned char *q_tile = base, *do_tile = base + kTileBytes, *kv = do_tile + kTileBytes;
-    float *bias = reinterpret_cast<float *>(kv + kStages * 2 * kTileBytes);
+    unsigned char *qd = base, *kv = qd + kKept * 2 * kTileBytes;      // pairs: Q and dO, K and V
+    float *bias = reinterpret_cast<float *>(kv + kWalked * 2 * kTileBytes);   // two heads' tables
+    const int bias_set = BIAS ? bias_floats(a.reach) : 0;
 
     if (threadIdx.x == 0) {
-        tc::mbar_init(&q_full, 1);
-        for (int i = 0; i < kStages; ++i) {
+        if (blockIdx.x == 0) f.p.ctl->status = 0;
+        for (int i = 0; i < kKept; ++i) {
+            tc::mbar_init(&q_full[i], 1);
+            tc::mbar_init(&q_empty[i], 1);
+        }
+        for (int i = 0; i < kWalked; ++i) {
             tc::mbar_init(&kv_full[i], 1);
             tc::mbar_init(&kv_empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
             tc::mbar_init(&s_full[i], 1);
             tc::mbar_init(&s_free[i], kCompute);
+            tc::mbar_init(&work_full[i], 1);
+            tc::mbar_init(&work_empty[i], kWarps + 1);
         }
         tc::mbar_init(&dp_full, 1);
         tc::mbar_init(&ds_full, kCompute);
+        tc::mbar_init(&dq_full, 1);
         tc::mbar_init(&meet_bar, kCompute);
         tc::mbar_init(&done, 1);
+        tc::mbar_init(&steal_bar, 1);
         s_abort = 0;
         tc::mbar_init_fence();
     }
-    if (warp == kWarps + 1) tc::tmem_alloc(&tmem_slot, 512);
-    if (BIAS)
-        fill_bias(bias, a, head, 1, threadIdx.x, kThreads);
+    if (warp == 0) tc::tmem_alloc(&tmem_slot, 512);
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
     const Waiter wait{&s_abort};
 
-    if (warp == kWarps) {
-        // ---------------- loads ----------------
-        const uint32_t lead = lane == 0;
-        bool ok = n_tiles > 0;
-        int issued = 0;
+    if (warp == kWarps + 1) {
+        // ---------------- the work, one block's after another's, and its loads ----------------
+        int block = blockIdx.x, item = 0, kv_issued = 0, head0 = -1, head1 = -1;
+        Blocks blocks{&s_answer, &steal_bar, 0, false};
+        bool ok = true;
+        while (ok && block >= 0) {
+            const int head = block / f.q_numbers, t = block % f.q_numbers, hk = head / (a.heads / a.kv_heads);
+            int s, tile;
+            if (a.new_tokens > 0) {
+                s = t / f.doc_tiles;
+                tile = t % f.doc_tiles;
+            } else {
+                s = find_doc(a.q_offsets, (int)a.nseq, (int)a.q_tokens, kTile, t);
+                tile = t - first_tile(a.q_offsets, s, (int)a.q_tokens, kTile);
+            }
+            const Doc doc = doc_at(a, s);
+            const int tiles = (doc.nq + kTile - 1) / kTile;
+            if (tile >= 0 && tile < tiles) {
+                tile = tiles - 1 - tile;               // the tiles that see most keys first
+                DqWork w;
+                w.head = head;
+                w.q_row = doc.q0;
+                w.row0 = tile * kTile;
+                w.nq = doc.nq;
+                w.k_row = doc.k0;
+                w.nk = doc.nk;
+                const int last = min(doc.nq, w.row0 + kTile);
+                const int end = a.causal ? min(doc.nk, last + doc.nk - doc.nq) : doc.nk;
+                w.n = end > 0 ? (end + kTile - 1) / kTile : 0;
+                w.stats = (first_q_tile(f, s) + tile) * a.heads + head;
+                if (w.n == 0) {
+                    // no query of these sees a key
+                    const int pieces = a.head_dim / 8;
+#pragma unroll 1
+                    for (int i = lane; i < (last - w.row0) * pieces; i += 32)
+                        *reinterpret_cast<uint4 *>(static_cast<T *>(f.p.dq) + (int64_t)(doc.q0 + w.row0 + i / pieces) * f.p.dq_ts +
+                                                   head * f.p.dq_hs + i % pieces * 8) = make_uint4(0, 0, 0, 0);
+                } else {
+                    const int slot = item % kSlots, qs = item % kKept;
+                    if (item >= kSlots && !(ok = wait.warp(&work_empty[slot], (uint32_t)(item / kSlots - 1) & 1u))) break;
+                    // a slot has its own bias table, done with when the slot is
+                    if (BIAS && head != (slot ? head1 : head0)) {
+                        fill_bias(bias + slot * bias_set, a, head, 1, lane, 32);
+                        (slot ? head1 : head0) = head;
+                    }
+                    if (lane == 0) s_work[slot] = w;
+                    __syncwarp();
+                    if (lane == 0) tc::mbar_arrive(&work_full[slot]);
+                    if (!(ok = wait.warp(&q_empty[qs], ((uint32_t)(item / kKept) & 1u) ^ 1u))) break;
+                    if (elected()) {
+                        expect(&q_full[qs], 2 * kTileBytes);
+                        for (int b = 0; b < kB; ++b) {
+                            tma_load(qd + qs * 2 * kTileBytes + b * kBlockBytes, &f.q, 64 * b, head, doc.q0 + w.row0, &q_full[qs]);
+                            tma_load(qd + (qs * 2 + 1) * kTileBytes + b * kBlockBytes, &f.dout, 64 * b, head, doc.q0 + w.row0,
+                                     &q_full[qs]);
+                        }
+                    }
+                    __syncwarp();
+                    ++item;
+#pragma unroll 1
+                    for (int j = 0; j < w.n; ++j, ++kv_issued) {
+                        const int st = kv_issued % kWalked;
+                        if (!(ok = wait.warp(&kv_empty[st], ((uint32_t)(kv_issued / kWalked) & 1u) ^ 1u))) break;
+                        if (elected()) {
+                            expect(&kv_full[st], 2 * kTileBytes);
+                            for (int b = 0; b < kB; ++b) {
+                                tma_load(kv + st * 2 * kTileBytes + b * kBlockBytes, &f.k, 64 * b, hk, doc.k0 + j * kTile, &kv_full[st]);
+                                tma_load(kv + (st * 2 + 1) * kTileBytes + b * kBlockBytes, &f.v, 64 * b, hk, doc.k0 + j * kTile,
+                                         &kv_full[st]);
+                            }
+                        }
+                        __syncwarp();
+                    }
+                    if (!ok) break;
+                }
+            }
+            ok = blocks.next(wait, block);
+        }
         if (ok) {
-            tc::mbar_arrive_expect_tx(lead, &q_full, 2 * kTileBytes);
-            for (int b = 0; b < kB; ++b) {
-                tma_load(lead, q_tile + b * kBlockBytes, &f.q, 64 * b, head, doc.q0 + row0, &q_full);
-                tma_load(lead, do_tile + b * kBlockBytes, &f.dout, 64 * b, head, doc.q0 + row0, &q_full);
+            const int slot = item % kSlots;
+            ok = item < kSlots || wait.warp(&work_empty[slot], (uint32_t)(item / kSlots - 1) & 1u);
+            if (lane == 0) {
+                s_work[slot].head = -1;
+                tc::mbar_arrive(&work_full[slot]);
             }
         }
-        for (int j = 0; ok && j < n_tiles; ++j) {
-            const int st = j % kStages;
-            if (!(ok = wait.warp(&kv_empty[st], ((uint32_t)(j / kStages) & 1u) ^ 1u))) break;
-            tc::mbar_arrive_expect_tx(lead, &kv_full[st], 2 * kTileBytes);
-            unsigned char *dst = kv + st * 2 * kTileBytes;
-            for (int b = 0; b < kB; ++b) {
-                tma_load(lead, dst + b * kBlockBytes, &f.k, 64 * b, hk, doc.k0 + j * kTile, &kv_full[st]);
-                tma_load(lead, dst + kTileBytes + b * kBlockBytes, &f.v, 64 * b, hk, doc.k0 + j * kTile, &kv_full[st]);
-            }
-            issued = j + 1;
+        if (!ok) {
+            // after an abort: what is in flight lands before the block ends
+            if (blocks.asking) let_land(&steal_bar, blocks.asked & 1u);
+            for (int i = max(0, item - kKept); i < item; ++i) let_land(&q_full[i % kKept], (uint32_t)(i / kKept) & 1u);
+            for (int i = max(0, kv_issued - kWalked); i < kv_issued; ++i)
+                let_land(&kv_full[i % kWalked], (uint32_t)(i / kWalked) & 1u);
         }
-        if (!ok && n_tiles > 0) {
-            // after an abort: the copies in flight land before the block ends
-            let_land(&q_full, 0);
-            for (int j = max(0, issued - kStages); j < issued; ++j)
-                let_land(&kv_full[j % kStages], (uint32_t)(j / kStages) & 1u);
-        }
-    } else if (warp == kWarps + 1) {
+        __syncwarp();
+    } else if (warp == kWarps) {
         // ---------------- products ----------------
         constexpr uint32_t id_s = idesc<T>(kTile, false), id_o = idesc<T>(DP, true);
-        const uint64_t qa = desc_k(q_tile), doa = desc_k(do_tile);
-        bool ok = n_tiles > 0;
-        auto k_of = [&](int j) { return kv + (j % kStages) * 2 * kTileBytes; };
-        auto loaded = [&](int j) {
-            if (!wait.warp(&kv_full[j % kStages], (uint32_t)(j / kStages) & 1u)) return false;
-            const int left = doc.nk - j * kTile;
-            if (left < kTile) {
-                clear_rows(k_of(j), left, kB);
-                clear_rows(k_of(j) + kTileBytes, left, kB);
+        constexpr uint32_t kPair = 2 * kTileBytes >> 4, kSecond = kTileBytes >> 4;   // in a descriptor's units
+        const uint64_t q0 = desc_k(qd), kk0 = desc_k(kv), km0 = desc_mn(kv);
+        uint32_t step = 0;
+        bool ok = true;
+        for (int item = 0; ok; ++item) {
+            const int slot = item % kSlots;
+            if (!(ok = wait.warp(&work_full[slot], (uint32_t)(item / kSlots) & 1u))) break;
+            if (uniform(s_work[slot].head) < 0) break;
+            const int n = uniform(s_work[slot].n), nk = uniform(s_work[slot].nk);
+            const uint64_t qa = q0 + item % kKept * kPair;
+            if (!(ok = wait.warp(&q_full[item % kKept], (uint32_t)(item / kKept) & 1u))) break;
+            // round j: the scores of step j + 1, dQ of step j, dP of step j + 1
+#pragma unroll 1
+            for (int j = -1; j < n; ++j) {
+                const bool more = j + 1 < n;
+                const uint32_t i = step + (j < 0 ? 0u : 1u), st = i % kWalked;
+                if (more) {
+                    if (!(ok = wait.warp(&kv_full[st], (i / kWalked) & 1u))) break;
+                    const int left = nk - (j + 1) * kTile;
+                    if (left < kTile) {
+                        // rows of another document: 0 x NaN in dS K, NaN in dP
+                        clear_rows(kv + st * 2 * kTileBytes, left, kB);
+                        clear_rows(kv + (st * 2 + 1) * kTileBytes, left, kB);
+                    }
+                    // the scores two steps back are in registers
+                    if (!(ok = wait.warp(&s_free[i & 1u], ((i >> 1) & 1u) ^ 1u))) break;
+                    tc::fence_after_sync();
+                    if (elected()) {
+                        mma_kk<DP>(tmem + kSCol + (i & 1u) * kTile, qa, kk0 + st * kPair, id_s);
+                        commit(&s_full[i & 1u]);
+                    }
+                    __syncwarp();
+                }
+                if (j >= 0) {
+                    if (!(ok = wait.warp(&ds_full, step & 1u))) break;
+                    tc::fence_after_sync();
+                    if (elected()) {
+                        mma_groups<kCols, kCols>(tmem + kDqCol, tmem + kDpCol, km0 + step % kWalked * kPair, id_o, j > 0);
+                        commit(&kv_empty[step % kWalked]);
+                        if (!more) commit(&dq_full);
+                    }
+                    __syncwarp();
+                    ++step;
+                }
+                if (more) {
+                    if (elected()) {
+                        mma_kk<DP>(tmem + kDpCol, qa + kSecond, kk0 + st * kPair + kSecond, id_s);
+                        commit(&dp_full);
+                        if (j + 2 == n) commit(&q_empty[item % kKept]);
+                    }
+                    __syncwarp();
+                }
             }
-            return true;
-        };
-        auto score = [&](int j) {
-            if (elected()) {
-                mma_kk<DP>(tmem + kSCol + (j & 1) * kTile, qa, desc_k(k_of(j)), id_s);
-                commit(&s_full[j & 1]);
-            }
-            __syncwarp();
-        };
-        auto dprob = [&](int j) {
-            if (elected()) {
-                mma_kk<DP>(tmem + kDpCol, doa, desc_k(k_of(j) + kTileBytes), id_s);
-                commit(&dp_full);
-            }
-            __syncwarp();
-        };
-        if (ok) ok = wait.warp(&q_full, 0) && loaded(0);
-        if (ok) {
-            tc::fence_after_sync();
-            score(0);
-            dprob(0);
+            if (ok && lane == 0) tc::mbar_arrive(&work_empty[slot]);
         }
-        for (int j = 0; ok && j < n_tiles; ++j) {
-            if (j + 1 < n_tiles) {
-                if (!(ok = loaded(j + 1))) break;
-                // the buffer's scores before (j - 1) are in registers
-                if (j > 0 && !(ok = wait.warp(&s_free[(j + 1) & 1], (uint32_t)((j - 1) / 2) & 1u))) break;
-                tc::fence_after_sync();
-                score(j + 1);
-            }
-            if (!(ok = wait.warp(&ds_full, (uint32_t)j & 1u))) break;
-            tc::fence_after_sync();
-            if (elected()) {
-                mma_halves<kHalf>(tmem + kDqCol, tmem + kDpCol, desc_mn(k_of(j)), id_o, j > 0);
-                commit(&kv_empty[j % kStages]);
-            }
-            __syncwarp();
-            if (j + 1 < n_tiles) dprob(j + 1);
-        }
-        // every product issued ends before the block reads dQ or frees its
-        // memory (waited for even after an abort, within the poll limit)
+        // every product issued ends before the block frees its memory (waited
+        // for even after an abort, within the poll limit)
         if (elected()) commit(&done);
         __syncwarp();
         let_land(&done, 0);
         __syncwarp();
     } else {
         // ---------------- P, dS and dQ ----------------
-        const int quarter = warp & 3, half = warp >> 2;
-        const int r = quarter * 32 + lane;
-        const bool live = r < rows;
-        const int place = row0 + r + shift;
-        const int seen = live ? (a.causal ? min(doc.nk, place + 1) : doc.nk) : 0;
-        const int64_t row = doc.q0 + row0 + r;
-        const int d = a.head_dim;
+        const int quarter = warp & 3, group = warp >> 2;
+        const int r = quarter * 32 + lane, d = a.head_dim;
         const float c = a.scale * kLog2e;
         const uint32_t lane_base = tmem + ((uint32_t)(quarter * 32) << 16);
-        // delta: each of a row's two threads adds one half of the products
-        float part = 0.f, nl = -INFINITY;
-        if (live) {
-            const T *o = static_cast<const T *>(f.p.out_in) + (row * a.heads + head) * d;
-            const T *g = static_cast<const T *>(f.p.dout) + (row * a.heads + head) * d;
-            for (int i = half * 8; i < d; i += 16) {
-                float x[8], y[8];
-                load_vec<T, 8>(o + i, x);
-                load_vec<T, 8>(g + i, y);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) part = fmaf(x[e], y[e], part);
-            }
-            const float lse = f.p.lse_in[(int64_t)head * a.q_tokens + row];
-            if (lse != -INFINITY) nl = -lse * kLog2e;
-        }
+        const uint32_t dp_at = lane_base + kDpCol + group * kCols;
         Meeting meet{&meet_bar, 0};
-        s_row[half][r] = part;
-        bool ok = meet(wait);
-        const float delta = live ? s_row[0][r] + s_row[1][r] : 0.f;
-        ok = ok && meet(wait);
-        int place_lo = live ? place : INT32_MAX, place_hi = live ? place : INT32_MIN;
-        if (BIAS) {
-            place_lo = row0 + quarter * 32 + shift;
-            place_hi = place_lo + 31;
-        }
-        const float bias_before = BIAS ? bias[bias_zero(a.reach) - a.reach] : 0.f;
-        const float bias_after = BIAS ? bias[bias_zero(a.reach) + a.reach] : 0.f;
-        float row_sum = 0.f;
-        for (int j = 0; ok && j < n_tiles; ++j) {
-            if (!(ok = wait.warp(&s_full[j & 1], (uint32_t)(j / 2) & 1u))) break;
-            tc::fence_after_sync();
-            float p[2][32];
-            const uint32_t s_at = lane_base + kSCol + (j & 1) * kTile + half * kHalf;
-            {
-                uint32_t raw[2][32];
-                tc::tmem_ld32_issue(s_at, raw[0]);
-                tc::tmem_ld32_issue(s_at + 32, raw[1]);
-                tc::tmem_ld_wait(raw[0]);
-                tc::tmem_ld_wait(raw[1]);
+        uint32_t step = 0;
+        bool ok = true;
+#pragma unroll 1
+        for (int item = 0; ok; ++item) {
+            const int slot = item % kSlots;
+            if (!(ok = wait.warp(&work_full[slot], (uint32_t)(item / kSlots) & 1u))) break;
+            const DqWork &w = s_work[slot];
+            if (w.head < 0) break;
+            const bool live = w.row0 + r < w.nq, idle = w.row0 + quarter * 32 >= w.nq;
+            const int place0 = w.row0 + quarter * 32 + w.nk - w.nq, place = place0 + lane;
+            const int seen = (live ? (a.causal ? min(w.nk, place + 1) : w.nk) : 0) - group * kCols;
+            const int64_t row = w.q_row + w.row0 + r;
+            const float *table = bias + slot * bias_set;
+            // delta: each of a row's threads adds a share of the products
+            float part = 0.f, nl = -INFINITY;
+            if (live) {
+                const T *o = static_cast<const T *>(f.p.out_in) + (row * a.heads + w.head) * d;
+                const T *g = static_cast<const T *>(f.p.dout) + (row * a.heads + w.head) * d;
+                const float lse = f.p.lse_in[(int64_t)w.head * a.q_tokens + row];
+                for (int i = group * 8; i < d; i += 8 * kGroups) {
+                    float x[8], y[8];
+                    load_vec<T, 8>(o + i, x);
+                    load_vec<T, 8>(g + i, y);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) part = fmaf(x[e], y[e], part);
+                }
+                if (lse != -INFINITY) nl = -lse * kLog2e;
+            }
+            s_row[0][group][r] = part;
+            if (!(ok = meet(wait))) break;
+            float delta = 0.f;
+#pragma unroll
+            for (int k = 0; k < kGroups; ++k) delta += s_row[0][k][r];
+            float2 sum2 = both(0.f);
+#pragma unroll 1
+            for (int j = 0; j < w.n; ++j, ++step) {
+                if (!(ok = wait.warp(&s_full[step & 1u], (step >> 1) & 1u))) break;
+                tc::fence_after_sync();
+                const int vis = seen - j * kTile;                    // columns of the group that this row sees
+                const bool all = __all_sync(0xffffffffu, vis >= kCols);
+                const bool none = idle || (!all && __reduce_max_sync(0xffffffffu, vis) <= 0);
+                uint32_t pk[kCols / 2];
+                float2 x[kCols / 2];
+                if (!none) {
+                    uint32_t raw[32];
+                    tc::tmem_ld32_issue(lane_base + kSCol + (step & 1u) * kTile + group * kCols, raw);
+                    tc::tmem_ld_wait(raw);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) x[e] = make_float2(__uint_as_float(raw[2 * e]), __uint_as_float(raw[2 * e + 1]));
+                }
                 tc::fence_before_sync();
-                tc::mbar_arrive(&s_free[j & 1]);
+                tc::mbar_arrive(&s_free[step & 1u]);
+                if (!none) {
+                    const int d0 = j * kTile + group * kCols;
+                    const bool after = d0 - place0 - 31 >= a.reach, before = d0 + 31 - place0 <= -a.reach;
+                    if (!BIAS || after || before) {
+                        const float b = nl + (BIAS ? table[bias_zero(a.reach) + (after ? a.reach : -a.reach)] : 0.f);
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int d0 = j * kTile + half * kHalf + 32 * i;
-                    if (!BIAS || d0 - place_hi >= a.reach || d0 + 31 - place_lo <= -a.reach) {
-                        const float b = nl + (!BIAS ? 0.f : d0 - place_hi >= a.reach ? bias_after : bias_before);
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) p[i][e] = exp2_approx(fmaf(__uint_as_float(raw[i][e]), c, b));
+                        for (int e = 0; e < 16; ++e) x[e] = fma2(x[e], both(c), both(b));
                     } else {
-                        const float4 *at = bias_at(bias, a.reach, d0 - place);
+                        const float4 *at = bias_at(table, a.reach, d0 - place);
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
                             const float4 b = at[e];
-                            p[i][4 * e + 0] = exp2_approx(fmaf(__uint_as_float(raw[i][4 * e + 0]), c, b.x + nl));
-                            p[i][4 * e + 1] = exp2_approx(fmaf(__uint_as_float(raw[i][4 * e + 1]), c, b.y + nl));
-                            p[i][4 * e + 2] = exp2_approx(fmaf(__uint_as_float(raw[i][4 * e + 2]), c, b.z + nl));
-                            p[i][4 * e + 3] = exp2_approx(fmaf(__uint_as_float(raw[i][4 * e + 3]), c, b.w + nl));
+                            x[2 * e] = fma2(x[2 * e], both(c), add2(make_float2(b.x, b.y), both(nl)));
+                            x[2 * e + 1] = fma2(x[2 * e + 1], both(c), add2(make_float2(b.z, b.w), both(nl)));
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        x[e].x = exp2_approx(x[e].x);
+                        x[e].y = exp2_approx(x[e].y);
+                    }
+                    if (!all) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            if (2 * e >= vis) x[e].x = 0.f;
+                            if (2 * e + 1 >= vis) x[e].y = 0.f;
                         }
                     }
                 }
-            }
-            const int vis = seen - j * kTile - half * kHalf;
-            if (!__all_sync(0xffffffffu, vis >= kHalf)) {
+                if (!(ok = wait.warp(&dp_full, step & 1u))) break;
+                tc::fence_after_sync();
+                if (!none) {
+                    float dp[32];
+                    tc::tmem_ld32(dp_at, dp);
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+                    for (int e = 0; e < 16; ++e) {
+                        x[e] = mul2(x[e], add2(make_float2(dp[2 * e], dp[2 * e + 1]), both(-delta)));
+                        if (BIAS) sum2 = add2(sum2, x[e]);
+                        pk[e] = pack2<T>(x[e].x, x[e].y);
+                    }
+                } else {
+                    // no row of the warp sees these; the product reads them
 #pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if (32 * i + e >= vis) p[i][e] = 0.f;
-            }
-            if (!(ok = wait.warp(&dp_full, (uint32_t)j & 1u))) break;
-            tc::fence_after_sync();
-            const uint32_t dp_at = lane_base + kDpCol + half * kHalf;
-            uint32_t w[32];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float dp[32];
-                tc::tmem_ld32(dp_at + 32 * i, dp);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const float x0 = p[i][2 * e] * (dp[2 * e] - delta), x1 = p[i][2 * e + 1] * (dp[2 * e + 1] - delta);
-                    if (BIAS) row_sum += x0 + x1;
-                    w[16 * i + e] = pack2<T>(x0, x1);
+                    for (int e = 0; e < 16; ++e) pk[e] = 0u;
                 }
+                tc::tmem_st16(dp_at, pk);
+                tc::tmem_st_wait();
+                if (BIAS && j == w.n - 1) s_row[1][group][r] = sum2.x + sum2.y;
+                tc::fence_before_sync();
+                tc::mbar_arrive(&ds_full);
             }
-            tmem_st32(dp_at, w);
-            tc::tmem_st_wait();
-            tc::fence_before_sync();
-            tc::mbar_arrive(&ds_full);
-        }
-        if (ok && n_tiles > 0) ok = wait.warp(&done, 0);
-        if (ok) {
+            if (!ok) break;
+            // (every thread's sum of dS arrived with its last dS)
+            if (!(ok = wait.warp(&ds_full, (step - 1) & 1u) && wait.warp(&dq_full, (uint32_t)item & 1u))) break;
             tc::fence_after_sync();
-            T *out = static_cast<T *>(f.p.dq) + row * f.p.dq_ts + head * f.p.dq_hs;
+            T *out = static_cast<T *>(f.p.dq) + row * f.p.dq_ts + w.head * f.p.dq_hs;
+            constexpr int kOut = DP / kGroups;       // 16 or 32 columns of dQ
 #pragma unroll
-            for (int i = 0; i < DP / 64; ++i) {
-                const int col = half * (DP / 2) + 32 * i;
-                float o[32];
-                tc::tmem_ld32(lane_base + kDqCol + col, o);
+            for (int i = 0; i < kOut / 16; ++i) {
+                const int col = group * kOut + 16 * i;
+                uint32_t o[16];
+                tmem_ld16(lane_base + kDqCol + col, o);
                 if (live)
 #pragma unroll
-                    for (int e = 0; e < 32; e += 8)
+                    for (int e = 0; e < 16; e += 8)
                         if (col + e < d) {
                             float v[8];
 #pragma unroll
-                            for (int u = 0; u < 8; ++u) v[u] = n_tiles > 0 && nl != -INFINITY ? o[e + u] * a.scale : 0.f;
-                            store_vec<T, 8>(out + col + e, v);
+                            for (int u = 0; u < 8; ++u) v[u] = nl != -INFINITY ? __uint_as_float(o[e + u]) * a.scale : 0.f;
+                            *reinterpret_cast<uint4 *>(out + col + e) =
+                                make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
                         }
             }
-            s_row[half][r] = row_sum;
-            if (meet(wait) && half == 0) {
+            tc::fence_before_sync();
+            if (group == 0) {
+                float *stats = f.stats + (int64_t)w.stats * 2 * kTile;
                 stats[r] = nl + (float)kPShift<T>;
-                stats[kTile + r] = (delta + (BIAS && nl != -INFINITY ? s_row[0][r] + s_row[1][r] : 0.f)) *
-                                   (1.f / (float)(1 << kPShift<T>));
+                if (BIAS && nl != -INFINITY)
+#pragma unroll
+                    for (int k = 0; k < kGroups; ++k) delta += s_row[1][k][r];
+                stats[kTile + r] = -delta * (1.f / (float)(1 << kPShift<T>));
             }
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&work_empty[slot]);
         }
     }
     tc::fence_before_sync();
     __syncthreads();
     if (threadIdx.x == 0 && s_abort) atomicExch(&f.p.ctl->status, SIEVE_ETIMEOUT);
-    if (warp == kWarps + 1) {
+    if (warp == 0) {
         tc::fence_after_sync();
         tc::tmem_dealloc(tmem, 512);
     }
 }
 
-template <typename T, int DP, bool BIAS>
-__global__ void __launch_bounds__(kThreads, 1) k_attend_dkv(const __grid_constant__ BwdArgs f) {
-    constexpr int kB = DP / 64, kStages = stages(DP);
+template <typename T, int DP, bool BIAS, int kWarps>
+__global__ void __launch_bounds__((kWarps + 2) * 32, 1) k_attend_dkv(const __grid_constant__ BwdArgs f) {
+    constexpr int kCompute = kWarps * 32;
+    constexpr int kGroups = Columns<kWarps>::kGroups, kCols = Columns<kWarps>::kCols, kChunks = Columns<kWarps>::kChunks;
+    constexpr int kB = DP / 64, kWalked = walked(DP), kKept = kept(DP);
     constexpr uint32_t kTileBytes = kB * kBlockBytes;
     constexpr uint32_t kSCol = 0, kDpCol = 128, kDvCol = 256, kDkCol = 384;   // P in S's place, dS in dP's
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(16) float s_stats[kStages][2][kTile];
-    __shared__ __align__(8) uint64_t kv_full, q_full[kStages], q_empty[kStages], s_full, p_full, dp_full, ds_full,
-        meet_bar, done;
+    __shared__ __align__(16) float s_stats[kWalked][2][kTile];
+    __shared__ __align__(8) uint64_t kv_full[kKept], kv_empty[kKept], q_full[kWalked], q_empty[kWalked], s_full, p_full,
+        dp_full, ds_full, acc_full, meet_bar, done, work_full[kSlots], work_empty[kSlots], steal_bar;
+    __shared__ __align__(16) uint4 s_answer;
     __shared__ uint32_t tmem_slot;
     __shared__ int s_abort;
+    __shared__ DkvWork s_work[kSlots];
     const sieve_attention_args &a = f.p.a;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = lane_id();
-
-    const int t = blockIdx.x / a.kv_heads, hk = blockIdx.x % a.kv_heads, share = a.heads / a.kv_heads;
-    const int s = find_doc(a.k_offsets, (int)a.nseq, (int)a.k_tokens, kTile, t);
-    const int tile = t - first_tile(a.k_offsets, s, (int)a.k_tokens, kTile);
-    const Doc doc = doc_at(a, s);
-    const int key0 = tile * kTile;
-    if (tile < 0 || key0 >= doc.nk) {
-        // a tile number that no document uses adds nothing to the table
-        for (int e = threadIdx.x; e < share * f.entries; e += kThreads)
-            f.partial[((int64_t)t * a.heads + hk * share) * f.entries + e] = 0.f;
-        return;
-    }
-    const int rows = min(kTile, doc.nk - key0), shift = doc.nk - doc.nq;
-    // the first tile of queries that sees any of these keys
-    const int q_first = a.causal ? max(0, key0 - shift) / kTile : 0;
-    const int q_tiles = max(0, (int)ceil_div(doc.nq, kTile) - q_first);
-    const int n = q_tiles * share;                     // steps: heads, queries inside
-    const int q_number = first_q_tile(f, s);
+    const int share = a.heads / a.kv_heads;
 
     unsigned char *base = reinterpret_cast<unsigned char *>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-    unsigned char *k_tile = base, *v_tile = base + kTileBytes, *qd = v_tile + kTileBytes;
-    float *bias = reinterpret_cast<float *>(qd + kStages * 2 * kTileBytes);
+    unsigned char *kv = base, *qd = kv + kKept * 2 * kTileBytes;      // pairs: K and V, Q and dO
+    float *bias = reinterpret_cast<float *>(qd + kWalked * 2 * kTileBytes);
     // the bias by minus the distance (columns run that way)
     constexpr int kCopies = DP == 64 ? 4 : 1;
     float *by_distance = bias + (BIAS ? bias_floats(a.reach, kCopies) : 0);   // [warps][entries]
-    float *scratch = by_distance + kWarps * f.entries;         // [warps][kScratch]
+    float *scratch = by_distance + kWarps * f.entries;                        // [warps][kScratch]
 
     if (threadIdx.x == 0) {
-        tc::mbar_init(&kv_full, 1);
-        for (int i = 0; i < kStages; ++i) {
+        if (blockIdx.x == 0 && a.q_tokens == 0) f.p.ctl->status = 0;      // (else k_attend_dq did)
+        for (int i = 0; i < kKept; ++i) {
+            tc::mbar_init(&kv_full[i], 1);
+            tc::mbar_init(&kv_empty[i], 1);
+        }
+        for (int i = 0; i < kWalked; ++i) {
             tc::mbar_init(&q_full[i], 1);
             tc::mbar_init(&q_empty[i], 1);
+        }
+        for (int i = 0; i < kSlots; ++i) {
+            tc::mbar_init(&work_full[i], 1);
+            tc::mbar_init(&work_empty[i], kWarps + 1);
         }
         tc::mbar_init(&s_full, 1);
         tc::mbar_init(&p_full, kCompute);
         tc::mbar_init(&dp_full, 1);
         tc::mbar_init(&ds_full, kCompute);
+        tc::mbar_init(&acc_full, 1);
         tc::mbar_init(&meet_bar, kCompute);
         tc::mbar_init(&done, 1);
+        tc::mbar_init(&steal_bar, 1);
         s_abort = 0;
         tc::mbar_init_fence();
     }
-    if (warp == kWarps + 1) tc::tmem_alloc(&tmem_slot, 512);
+    if (warp == 0) tc::tmem_alloc(&tmem_slot, 512);
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
     const Waiter wait{&s_abort};
 
-    if (warp == kWarps) {
-        // ---------------- loads ----------------
-        const uint32_t lead = lane == 0;
-        bool ok = n > 0;
-        int issued = 0;
+    if (warp == kWarps + 1) {
+        // ---------------- the work, one block's after another's, and its loads ----------------
+        int block = blockIdx.x, item = 0, q_issued = 0;
+        Blocks blocks{&s_answer, &steal_bar, 0, false};
+        bool ok = true;
+        while (ok && block >= 0) {
+            DkvWork w;
+            w.hk = block / f.k_numbers;
+            w.number = block % f.k_numbers;
+            const int s = find_doc(a.k_offsets, (int)a.nseq, (int)a.k_tokens, kTile, w.number);
+            const int tile = w.number - first_tile(a.k_offsets, s, (int)a.k_tokens, kTile);
+            const Doc doc = doc_at(a, s);
+            w.key0 = tile * kTile;
+            const bool used = tile >= 0 && w.key0 < doc.nk;
+            // the first tile of queries that sees any of these keys
+            const int shift = doc.nk - doc.nq;
+            w.q_first = a.causal ? max(0, w.key0 - shift) / kTile : 0;
+            w.q_tiles = used ? max(0, (doc.nq + kTile - 1) / kTile - w.q_first) : 0;
+            if (w.q_tiles == 0) {
+                // no query sees these keys, or no document uses the number:
+                // nothing for the table, and zeros for the keys
+#pragma unroll 1
+                for (int e = lane; e < share * f.entries; e += 32)
+                    f.partial[((int64_t)w.number * a.heads + w.hk * share) * f.entries + e] = 0.f;
+                const int pieces = a.head_dim / 8;
+#pragma unroll 1
+                for (int i = lane; used && i < min(kTile, doc.nk - w.key0) * pieces; i += 32) {
+                    const int64_t row = doc.k0 + w.key0 + i / pieces;
+                    *reinterpret_cast<uint4 *>(static_cast<T *>(f.p.dk) + row * f.p.dk_ts + w.hk * f.p.dk_hs + i % pieces * 8) =
+                        make_uint4(0, 0, 0, 0);
+                    *reinterpret_cast<uint4 *>(static_cast<T *>(f.p.dv) + row * f.p.dv_ts + w.hk * f.p.dv_hs + i % pieces * 8) =
+                        make_uint4(0, 0, 0, 0);
+                }
+            } else {
+                w.k_row = doc.k0;
+                w.nk = doc.nk;
+                w.q_row = doc.q0;
+                w.nq = doc.nq;
+                w.q_number = first_q_tile(f, s);
+                const int slot = item % kSlots, ks = item % kKept;
+                if (item >= kSlots && !(ok = wait.warp(&work_empty[slot], (uint32_t)(item / kSlots - 1) & 1u))) break;
+                if (lane == 0) {
+                    s_work[slot] = w;
+                    tc::mbar_arrive(&work_full[slot]);
+                }
+                if (!(ok = wait.warp(&kv_empty[ks], ((uint32_t)(item / kKept) & 1u) ^ 1u))) break;
+                if (elected()) {
+                    expect(&kv_full[ks], 2 * kTileBytes);
+                    for (int b = 0; b < kB; ++b) {
+                        tma_load(kv + ks * 2 * kTileBytes + b * kBlockBytes, &f.k, 64 * b, w.hk, doc.k0 + w.key0, &kv_full[ks]);
+                        tma_load(kv + (ks * 2 + 1) * kTileBytes + b * kBlockBytes, &f.v, 64 * b, w.hk, doc.k0 + w.key0,
+                                 &kv_full[ks]);
+                    }
+                }
+                __syncwarp();
+                ++item;
+                int head = w.hk * share, qt = w.q_first;
+#pragma unroll 1
+                for (int i = 0; i < w.q_tiles * share; ++i, ++q_issued) {
+                    const int st = q_issued % kWalked, row = doc.q0 + qt * kTile;
+                    if (!(ok = wait.warp(&q_empty[st], ((uint32_t)(q_issued / kWalked) & 1u) ^ 1u))) break;
+                    if (elected()) {
+                        expect(&q_full[st], 2 * kTileBytes + 2 * kTile * 4);
+                        for (int b = 0; b < kB; ++b) {
+                            tma_load(qd + st * 2 * kTileBytes + b * kBlockBytes, &f.q, 64 * b, head, row, &q_full[st]);
+                            tma_load(qd + (st * 2 + 1) * kTileBytes + b * kBlockBytes, &f.dout, 64 * b, head, row, &q_full[st]);
+                        }
+                        tc::bulk_g2s(1u, s_stats[st], f.stats + ((int64_t)(w.q_number + qt) * a.heads + head) * 2 * kTile,
+                                     2 * kTile * 4, &q_full[st]);
+                    }
+                    __syncwarp();
+                    if (++qt == w.q_first + w.q_tiles) {
+                        qt = w.q_first;
+                        ++head;
+                    }
+                }
+                if (!ok) break;
+            }
+            ok = blocks.next(wait, block);
+        }
         if (ok) {
-            tc::mbar_arrive_expect_tx(lead, &kv_full, 2 * kTileBytes);
-            for (int b = 0; b < kB; ++b) {
-                tma_load(lead, k_tile + b * kBlockBytes, &f.k, 64 * b, hk, doc.k0 + key0, &kv_full);
-                tma_load(lead, v_tile + b * kBlockBytes, &f.v, 64 * b, hk, doc.k0 + key0, &kv_full);
+            const int slot = item % kSlots;
+            ok = item < kSlots || wait.warp(&work_empty[slot], (uint32_t)(item / kSlots - 1) & 1u);
+            if (lane == 0) {
+                s_work[slot].hk = -1;
+                tc::mbar_arrive(&work_full[slot]);
             }
         }
-        int g = 0, qt = q_first;
-        for (int i = 0; ok && i < n; ++i) {
-            const int st = i % kStages, head = hk * share + g, row = doc.q0 + qt * kTile;
-            if (!(ok = wait.warp(&q_empty[st], ((uint32_t)(i / kStages) & 1u) ^ 1u))) break;
-            tc::mbar_arrive_expect_tx(lead, &q_full[st], 2 * kTileBytes + 2 * kTile * 4);
-            unsigned char *dst = qd + st * 2 * kTileBytes;
-            for (int b = 0; b < kB; ++b) {
-                tma_load(lead, dst + b * kBlockBytes, &f.q, 64 * b, head, row, &q_full[st]);
-                tma_load(lead, dst + kTileBytes + b * kBlockBytes, &f.dout, 64 * b, head, row, &q_full[st]);
-            }
-            tc::bulk_g2s(lead, s_stats[st], f.stats + ((int64_t)(q_number + qt) * a.heads + head) * 2 * kTile,
-                         2 * kTile * 4, &q_full[st]);
-            issued = i + 1;
-            if (++qt == q_first + q_tiles) {
-                qt = q_first;
-                ++g;
-            }
+        if (!ok) {
+            // after an abort: what is in flight lands before the block ends
+            if (blocks.asking) let_land(&steal_bar, blocks.asked & 1u);
+            for (int i = max(0, item - kKept); i < item; ++i) let_land(&kv_full[i % kKept], (uint32_t)(i / kKept) & 1u);
+            for (int i = max(0, q_issued - kWalked); i < q_issued; ++i)
+                let_land(&q_full[i % kWalked], (uint32_t)(i / kWalked) & 1u);
         }
-        if (!ok && n > 0) {
-            // after an abort: the copies in flight land before the block ends
-            let_land(&kv_full, 0);
-            for (int i = max(0, issued - kStages); i < issued; ++i)
-                let_land(&q_full[i % kStages], (uint32_t)(i / kStages) & 1u);
-        }
-    } else if (warp == kWarps + 1) {
+        __syncwarp();
+    } else if (warp == kWarps) {
         // ---------------- products ----------------
         constexpr uint32_t id_s = idesc<T>(kTile, false), id_o = idesc<T>(DP, true);
-        const uint64_t ka = desc_k(k_tile), va = desc_k(v_tile);
-        bool ok = n > 0;
-        auto q_of = [&](int i) { return qd + (i % kStages) * 2 * kTileBytes; };
-        int qt_loaded = q_first;
-        auto loaded = [&](int i) {
-            if (!wait.warp(&q_full[i % kStages], (uint32_t)(i / kStages) & 1u)) return false;
-            const int left = doc.nq - qt_loaded * kTile;
-            if (left < kTile) {
-                clear_rows(q_of(i), left, kB);
-                clear_rows(q_of(i) + kTileBytes, left, kB);
+        constexpr uint32_t kPair = 2 * kTileBytes >> 4, kSecond = kTileBytes >> 4;   // in a descriptor's units
+        const uint64_t k0 = desc_k(kv), qk0 = desc_k(qd), qm0 = desc_mn(qd);
+        uint32_t step = 0;
+        bool ok = true;
+        for (int item = 0; ok; ++item) {
+            const int slot = item % kSlots;
+            if (!(ok = wait.warp(&work_full[slot], (uint32_t)(item / kSlots) & 1u))) break;
+            const DkvWork &w = s_work[slot];
+            if (uniform(w.hk) < 0) break;
+            const int q_tiles = uniform(w.q_tiles), n = q_tiles * share;
+            const int left0 = uniform(w.nq - w.q_first * kTile);       // queries from the first tile on
+            const uint64_t ka = k0 + item % kKept * kPair;
+            if (!(ok = wait.warp(&kv_full[item % kKept], (uint32_t)(item / kKept) & 1u))) break;
+            int left = left0, qt = 0;
+            // round j: dV of step j, the scores of step j + 1, dK of step j,
+            // dP of step j + 1
+#pragma unroll 1
+            for (int j = -1; j < n; ++j) {
+                const bool more = j + 1 < n;
+                const uint32_t i = step + (j < 0 ? 0u : 1u), st = i % kWalked, now = step % kWalked;
+                if (j >= 0) {
+                    if (!(ok = wait.warp(&p_full, step & 1u))) break;
+                    tc::fence_after_sync();
+                    if (elected())
+                        mma_groups<kCols, kCols>(tmem + kDvCol, tmem + kSCol, qm0 + now * kPair + kSecond, id_o, j > 0);
+                    __syncwarp();
+                }
+                if (more) {
+                    if (!(ok = wait.warp(&q_full[st], (i / kWalked) & 1u))) break;
+                    if (left < kTile) {
+                        // rows of another document: their P and dS must be zeros
+                        clear_rows(qd + st * 2 * kTileBytes, left, kB);
+                        clear_rows(qd + (st * 2 + 1) * kTileBytes, left, kB);
+                    }
+                    left -= kTile;
+                    if (++qt == q_tiles) {
+                        qt = 0;
+                        left = left0;
+                    }
+                    tc::fence_after_sync();
+                    if (elected()) {
+                        mma_kk<DP>(tmem + kSCol, ka, qk0 + st * kPair, id_s);
+                        commit(&s_full);
+                    }
+                    __syncwarp();
+                }
+                if (j >= 0) {
+                    if (!(ok = wait.warp(&ds_full, step & 1u))) break;
+                    tc::fence_after_sync();
+                    if (elected()) {
+                        mma_groups<kCols, kCols>(tmem + kDkCol, tmem + kDpCol, qm0 + now * kPair, id_o, j > 0);
+                        commit(&q_empty[now]);
+                        if (!more) commit(&acc_full);
+                    }
+                    __syncwarp();
+                    ++step;
+                }
+                if (more) {
+                    if (elected()) {
+                        mma_kk<DP>(tmem + kDpCol, ka + kSecond, qk0 + st * kPair + kSecond, id_s);
+                        commit(&dp_full);
+                        if (j + 2 == n) commit(&kv_empty[item % kKept]);
+                    }
+                    __syncwarp();
+                }
             }
-            if (++qt_loaded == q_first + q_tiles) qt_loaded = q_first;
-            return true;
-        };
-        auto score = [&](int i) {
-            if (elected()) {
-                mma_kk<DP>(tmem + kSCol, ka, desc_k(q_of(i)), id_s);
-                commit(&s_full);
-            }
-            __syncwarp();
-        };
-        auto dprob = [&](int i) {
-            if (elected()) {
-                mma_kk<DP>(tmem + kDpCol, va, desc_k(q_of(i) + kTileBytes), id_s);
-                commit(&dp_full);
-            }
-            __syncwarp();
-        };
-        if (ok) ok = wait.warp(&kv_full, 0) && loaded(0);
-        if (ok) {
-            tc::fence_after_sync();
-            score(0);
-            dprob(0);
+            if (ok && lane == 0) tc::mbar_arrive(&work_empty[slot]);
         }
-        for (int i = 0; ok && i < n; ++i) {
-            if (!(ok = wait.warp(&p_full, (uint32_t)i & 1u))) break;
-            tc::fence_after_sync();
-            if (elected()) mma_halves<kHalf>(tmem + kDvCol, tmem + kSCol, desc_mn(q_of(i) + kTileBytes), id_o, i > 0);
-            __syncwarp();
-            if (i + 1 < n) {
-                if (!(ok = loaded(i + 1))) break;
-                tc::fence_after_sync();
-                score(i + 1);
-            }
-            if (!(ok = wait.warp(&ds_full, (uint32_t)i & 1u))) break;
-            tc::fence_after_sync();
-            if (elected()) {
-                mma_halves<kHalf>(tmem + kDkCol, tmem + kDpCol, desc_mn(q_of(i)), id_o, i > 0);
-                commit(&q_empty[i % kStages]);
-            }
-            __syncwarp();
-            if (i + 1 < n) dprob(i + 1);
-        }
-        // every product issued ends before the block reads dK and dV or frees
-        // its memory (waited for even after an abort, within the poll limit)
+        // every product issued ends before the block frees its memory (waited
+        // for even after an abort, within the poll limit)
         if (elected()) commit(&done);
         __syncwarp();
         let_land(&done, 0);
         __syncwarp();
     } else {
         // ---------------- P, dS, dK and dV ----------------
-        const int quarter = warp & 3, half = warp >> 2;
-        const int r = quarter * 32 + lane, key = key0 + r;
-        const bool live = r < rows;
-        const int d = a.head_dim;
+        const int quarter = warp & 3, group = warp >> 2;
+        const int r = quarter * 32 + lane, d = a.head_dim;
         const float c = a.scale * kLog2e;
         const uint32_t lane_base = tmem + ((uint32_t)(quarter * 32) << 16);
-        const int key_lo = key0 + quarter * 32;
         float *mine = by_distance + warp * f.entries, *line = scratch + warp * kScratch;
         const float not_first = lane == 0 ? 0.f : 1.f;
         constexpr float kDown = 1.f / (float)(1 << kPShift<T>);
-        float far_before = 0.f, far_after = 0.f;
         Meeting meet{&meet_bar, 0};
+        uint32_t step = 0;
+        int head_in_table = -1;
         bool ok = true;
-        int g = 0, qt = q_first;
-        for (int i = 0; i < n; ++i) {
-            const int head = hk * share + g, st = i % kStages;
-            if (BIAS && qt == q_first) {
-                // a new head: its bias, and its sums from zero
-                if (!(ok = meet(wait))) break;
-                fill_bias<kCopies>(bias, a, head, -1, threadIdx.x, kCompute);
-                for (int e = lane; e < f.entries; e += 32) mine[e] = 0.f;
-                far_before = far_after = 0.f;
-                if (!(ok = meet(wait))) break;
-            }
-            const int place0 = qt * kTile + half * kHalf + shift;      // place of the half's first query
-            if (!(ok = wait.warp(&q_full[st], (uint32_t)(i / kStages) & 1u))) break;   // the row statistics
-            if (!(ok = wait.warp(&s_full, (uint32_t)i & 1u))) break;
-            tc::fence_after_sync();
-            float p[2][32];
-            uint32_t w[32];
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                uint32_t raw[32];
-                tc::tmem_ld32_issue(lane_base + kSCol + half * kHalf + 32 * q, raw);
-                const float4 *nl = reinterpret_cast<const float4 *>(&s_stats[st][0][half * kHalf + 32 * q]);
-                const int lo = key_lo - (place0 + 32 * q) - 31, hi = key_lo + 31 - (place0 + 32 * q);
-                tc::tmem_ld_wait(raw);
-                if (!BIAS || lo >= a.reach || hi <= -a.reach) {
-                    const float b = !BIAS ? 0.f : bias[bias_zero(a.reach) + (lo >= a.reach ? -a.reach : a.reach)];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float4 x = nl[e];
-                        p[q][4 * e + 0] = exp2_approx(fmaf(__uint_as_float(raw[4 * e + 0]), c, x.x + b));
-                        p[q][4 * e + 1] = exp2_approx(fmaf(__uint_as_float(raw[4 * e + 1]), c, x.y + b));
-                        p[q][4 * e + 2] = exp2_approx(fmaf(__uint_as_float(raw[4 * e + 2]), c, x.z + b));
-                        p[q][4 * e + 3] = exp2_approx(fmaf(__uint_as_float(raw[4 * e + 3]), c, x.w + b));
+#pragma unroll 1
+        for (int item = 0; ok; ++item) {
+            const int slot = item % kSlots;
+            if (!(ok = wait.warp(&work_full[slot], (uint32_t)(item / kSlots) & 1u))) break;
+            const DkvWork &w = s_work[slot];
+            if (w.hk < 0) break;
+            const int key = w.key0 + r, key_lo = w.key0 + quarter * 32, shift = w.nk - w.nq;
+            const bool live = key < w.nk, idle = key_lo >= w.nk;
+#pragma unroll 1
+            for (int g = 0; ok && g < share; ++g) {
+                const int head = w.hk * share + g;
+                float far_before = 0.f, far_after = 0.f;
+                if (BIAS) {
+                    // sums from zero, and another head's bias
+                    if (head != head_in_table) {
+                        if (!(ok = meet(wait))) break;
+                        fill_bias<kCopies>(bias, a, head, -1, threadIdx.x, kCompute);
+                        head_in_table = head;
+                        if (!(ok = meet(wait))) break;
                     }
-                } else {
-                    const int first = place0 + 32 * q - key;
-                    const float4 *at = bias_at(bias, a.reach, first);
-                    const float *one = bias + bias_zero(a.reach) + first;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float4 x = nl[e];
-                        const float4 b = kCopies == 4 ? at[e] : make_float4(one[4 * e], one[4 * e + 1], one[4 * e + 2], one[4 * e + 3]);
-                        p[q][4 * e + 0] = exp2_approx(fmaf(__uint_as_float(raw[4 * e + 0]), c, x.x + b.x));
-                        p[q][4 * e + 1] = exp2_approx(fmaf(__uint_as_float(raw[4 * e + 1]), c, x.y + b.y));
-                        p[q][4 * e + 2] = exp2_approx(fmaf(__uint_as_float(raw[4 * e + 2]), c, x.z + b.z));
-                        p[q][4 * e + 3] = exp2_approx(fmaf(__uint_as_float(raw[4 * e + 3]), c, x.w + b.w));
-                    }
+                    for (int e = lane; e < f.entries; e += 32) mine[e] = 0.f;
+                    __syncwarp();
                 }
-            }
-            if (a.causal) {
-                const int from = key - place0;                        // columns before it do not see this key
-                if (!__all_sync(0xffffffffu, from <= 0)) {
+#pragma unroll 1
+                for (int qt = w.q_first; qt < w.q_first + w.q_tiles; ++qt, ++step) {
+                    const uint32_t st = step % kWalked;
+                    const int col0 = qt * kTile + group * kCols;              // the group's first query
+                    const int place0 = col0 + shift;
+                    // columns before `from` do not see this key, nor those
+                    // past the document's queries
+                    const int from = a.causal ? key - place0 : 0;
+                    if (!(ok = wait.warp(&q_full[st], (step / kWalked) & 1u))) break;   // the row statistics
+                    if (!(ok = wait.warp(&s_full, step & 1u))) break;
+                    tc::fence_after_sync();
+                    const bool none = idle || col0 >= w.nq || (a.causal && key_lo - place0 >= kCols);
+                    float2 p[kChunks][16];
+                    uint32_t pk[16];
 #pragma unroll
-                    for (int q = 0; q < 2; ++q)
+                    for (int q = 0; q < kChunks; ++q) {
+                        if (!none) {
+                            uint32_t raw[32];
+                            tc::tmem_ld32_issue(lane_base + kSCol + group * kCols + 32 * q, raw);
+                            const float4 *nl = reinterpret_cast<const float4 *>(&s_stats[st][0][group * kCols + 32 * q]);
+                            const int hi = key_lo + 31 - (place0 + 32 * q), lo = hi - 62;
+                            tc::tmem_ld_wait(raw);
+                            if (!BIAS || lo >= a.reach || hi <= -a.reach) {
+                                const float b =
+                                    !BIAS ? 0.f : bias[bias_zero(a.reach) + (lo >= a.reach ? -a.reach : a.reach)];
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (32 * q + e < from) p[q][e] = 0.f;
-                }
-            }
+                                for (int e = 0; e < 8; ++e) {
+                                    const float4 x = nl[e];
+                                    float2 x0 = make_float2(x.x, x.y), x1 = make_float2(x.z, x.w);
+                                    if (BIAS) {
+                                        x0 = add2(x0, both(b));
+                                        x1 = add2(x1, both(b));
+                                    }
+                                    p[q][2 * e] = fma2(make_float2(__uint_as_float(raw[4 * e]), __uint_as_float(raw[4 * e + 1])), both(c), x0);
+                                    p[q][2 * e + 1] = fma2(make_float2(__uint_as_float(raw[4 * e + 2]), __uint_as_float(raw[4 * e + 3])), both(c), x1);
+                                }
+                            } else {
+                                const int first = place0 + 32 * q - key;
+                                const float4 *at = bias_at(bias, a.reach, first);
+                                const float *one = bias + bias_zero(a.reach) + first;
 #pragma unroll
-            for (int q = 0; q < 2; ++q)
+                                for (int e = 0; e < 8; ++e) {
+                                    const float4 x = nl[e];
+                                    const float4 b = kCopies == 4 ? at[e] : make_float4(one[4 * e], one[4 * e + 1], one[4 * e + 2], one[4 * e + 3]);
+                                    p[q][2 * e] = fma2(make_float2(__uint_as_float(raw[4 * e]), __uint_as_float(raw[4 * e + 1])), both(c),
+                                                       add2(make_float2(x.x, x.y), make_float2(b.x, b.y)));
+                                    p[q][2 * e + 1] = fma2(make_float2(__uint_as_float(raw[4 * e + 2]), __uint_as_float(raw[4 * e + 3])), both(c),
+                                                           add2(make_float2(x.z, x.w), make_float2(b.z, b.w)));
+                                }
+                            }
 #pragma unroll
-                for (int e = 0; e < 16; ++e) w[16 * q + e] = pack2<T>(p[q][2 * e], p[q][2 * e + 1]);
-            tmem_st32(lane_base + kSCol + half * kHalf, w);
-            tc::tmem_st_wait();
-            tc::fence_before_sync();
-            tc::mbar_arrive(&p_full);
-
-            if (!(ok = wait.warp(&dp_full, (uint32_t)i & 1u))) break;
-            tc::fence_after_sync();
+                            for (int e = 0; e < 16; ++e) {
+                                p[q][e].x = exp2_approx(p[q][e].x);
+                                p[q][e].y = exp2_approx(p[q][e].y);
+                            }
+                            if (a.causal && !__all_sync(0xffffffffu, from <= 32 * q)) {
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                float dp[32];
-                tc::tmem_ld32(lane_base + kDpCol + half * kHalf + 32 * q, dp);
-                const float4 *dl = reinterpret_cast<const float4 *>(&s_stats[st][1][half * kHalf + 32 * q]);
+                                for (int e = 0; e < 16; ++e) {
+                                    if (32 * q + 2 * e < from) p[q][e].x = 0.f;
+                                    if (32 * q + 2 * e + 1 < from) p[q][e].y = 0.f;
+                                }
+                            }
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float4 x = dl[e];
-                    p[q][4 * e + 0] *= fmaf(dp[4 * e + 0], kDown, -x.x);
-                    p[q][4 * e + 1] *= fmaf(dp[4 * e + 1], kDown, -x.y);
-                    p[q][4 * e + 2] *= fmaf(dp[4 * e + 2], kDown, -x.z);
-                    p[q][4 * e + 3] *= fmaf(dp[4 * e + 3], kDown, -x.w);
-                }
+                            for (int e = 0; e < 16; ++e) pk[e] = pack2<T>(p[q][e].x, p[q][e].y);
+                        } else {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) w[16 * q + e] = pack2<T>(p[q][2 * e], p[q][2 * e + 1]);
-            }
-            tmem_st32(lane_base + kDpCol + half * kHalf, w);
-            tc::tmem_st_wait();
-            tc::fence_before_sync();
-            tc::mbar_arrive(&ds_full);
-
-            if (BIAS) {
-                // dS by distance, under the products.  A lane is a key, a step
-                // to the next query lowers its distance by one: a sum that
-                // moves up one lane with every step follows one distance, and
-                // leaves complete at lane 31.
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const int lo = key_lo - (place0 + 32 * q) - 31, hi = key_lo + 31 - (place0 + 32 * q);
-                    if (!live)   // rows past the document's keys add nothing
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) p[q][e] = 0.f;
-                    if (lo >= a.reach || hi <= -a.reach) {
-                        float x[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) x[e & 3] += p[q][e];
-                        (lo >= a.reach ? far_after : far_before) += (x[0] + x[1]) + (x[2] + x[3]);
-                    } else {
-                        float acc = 0.f;
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            if (e) acc = __shfl_up_sync(0xffffffffu, acc, 1);
-                            acc = e ? fmaf(acc, not_first, p[q][e]) : p[q][e];
-                            if (lane == 31) line[e] = acc;          // distance hi - e
+                            for (int e = 0; e < 16; ++e) pk[e] = 0u;
                         }
-                        if (lane < 31) line[62 - lane] = acc;       // lane's distance: hi - (62 - lane)
-                        __syncwarp();
-                        float *to = mine + a.reach + kPad + hi;
-                        to[-lane] += line[lane];
-                        if (lane < 31) to[-(lane + 32)] += line[lane + 32];
-                        __syncwarp();
+                        tc::tmem_st16(lane_base + kSCol + group * kCols + 16 * q, pk);
+                    }
+                    tc::tmem_st_wait();
+                    tc::fence_before_sync();
+                    tc::mbar_arrive(&p_full);
+
+                    if (!(ok = wait.warp(&dp_full, step & 1u))) break;
+                    tc::fence_after_sync();
+#pragma unroll
+                    for (int q = 0; q < kChunks; ++q) {
+                        if (!none) {
+                            float dp[32];
+                            tc::tmem_ld32(lane_base + kDpCol + group * kCols + 32 * q, dp);
+                            const float4 *dl = reinterpret_cast<const float4 *>(&s_stats[st][1][group * kCols + 32 * q]);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                const float4 x = dl[e];
+                                p[q][2 * e] = mul2(p[q][2 * e], fma2(make_float2(dp[4 * e], dp[4 * e + 1]), both(kDown), make_float2(x.x, x.y)));
+                                p[q][2 * e + 1] =
+                                    mul2(p[q][2 * e + 1], fma2(make_float2(dp[4 * e + 2], dp[4 * e + 3]), both(kDown), make_float2(x.z, x.w)));
+                            }
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) pk[e] = pack2<T>(p[q][e].x, p[q][e].y);
+                        }
+                        tc::tmem_st16(lane_base + kDpCol + group * kCols + 16 * q, pk);   // (zeros where none)
+                    }
+                    tc::tmem_st_wait();
+                    tc::fence_before_sync();
+                    tc::mbar_arrive(&ds_full);
+
+                    if (BIAS && !none) {
+                        // dS by distance, under the products.  A lane is a key,
+                        // a step to the next query lowers its distance by one: a
+                        // sum that moves up one lane with every step follows one
+                        // distance, and leaves complete at lane 31.
+#pragma unroll
+                        for (int q = 0; q < kChunks; ++q) {
+                            const int hi = key_lo + 31 - (place0 + 32 * q), lo = hi - 62;
+                            if (!live)   // rows past the document's keys add nothing
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) p[q][e] = both(0.f);
+                            if (lo >= a.reach || hi <= -a.reach) {
+                                float2 x0 = p[q][0], x1 = p[q][1];
+#pragma unroll
+                                for (int e = 2; e < 16; e += 2) {
+                                    x0 = add2(x0, p[q][e]);
+                                    x1 = add2(x1, p[q][e + 1]);
+                                }
+                                x0 = add2(x0, x1);
+                                (lo >= a.reach ? far_after : far_before) += x0.x + x0.y;
+                            } else {
+                                float acc = p[q][0].x;
+                                if (lane == 31) line[0] = acc;
+#pragma unroll
+                                for (int e = 1; e < 32; ++e) {
+                                    acc = __shfl_up_sync(0xffffffffu, acc, 1);
+                                    acc = fmaf(acc, not_first, e & 1 ? p[q][e / 2].y : p[q][e / 2].x);
+                                    if (lane == 31) line[e] = acc;          // distance hi - e
+                                }
+                                if (lane < 31) line[62 - lane] = acc;       // lane's distance: hi - (62 - lane)
+                                __syncwarp();
+                                float *to = mine + a.reach + kPad + hi;
+                                to[-lane] += line[lane];
+                                if (lane < 31) to[-(lane + 32)] += line[lane + 32];
+                                __syncwarp();
+                            }
+                        }
                     }
                 }
-                if (qt == q_first + q_tiles - 1) {
-                    // the head's last step: add the warps up, in order
+                if (BIAS && ok) {
+                    // the head's sums: the warps' added up, in order
                     const float before = warp_sum(far_before), after = warp_sum(far_after);
                     if (lane == 0) {
                         mine[kPad] += before;
                         mine[kPad + 2 * a.reach] += after;
                     }
                     if (!(ok = meet(wait))) break;
-                    float *out = f.partial + ((int64_t)t * a.heads + head) * f.entries;
+                    float *out = f.partial + ((int64_t)w.number * a.heads + head) * f.entries;
                     for (int e = threadIdx.x; e < f.entries; e += kCompute) {
                         float x = 0.f;
 #pragma unroll
                         for (int k = 0; k < kWarps; ++k) x += by_distance[k * f.entries + e];
                         out[e] = x;
                     }
+                    if (!(ok = meet(wait))) break;
                 }
             }
-            if (++qt == q_first + q_tiles) {
-                qt = q_first;
-                ++g;
-            }
-        }
-        if (BIAS && n == 0)   // no query sees these keys
-            for (int h = 0; h < share; ++h)
-                for (int e = threadIdx.x; e < f.entries; e += kCompute)
-                    f.partial[((int64_t)t * a.heads + hk * share + h) * f.entries + e] = 0.f;
-        if (ok && n > 0) ok = wait.warp(&done, 0);
-        if (ok) {
+            if (ok) ok = wait.warp(&acc_full, (uint32_t)item & 1u);
+            if (!ok) break;
             tc::fence_after_sync();
-            const int64_t row = doc.k0 + key;
-            // one half of the warps writes dV, the other dK
-            T *out = half ? static_cast<T *>(f.p.dk) + row * f.p.dk_ts + hk * f.p.dk_hs
-                          : static_cast<T *>(f.p.dv) + row * f.p.dv_ts + hk * f.p.dv_hs;
-            const float scale = half ? a.scale : kDown;
+            const int64_t row = w.k_row + key;
+            // the groups' shares: of dV first, then of dK
+            constexpr int kOut = 2 * DP / kGroups;
+            const bool is_k = group >= kGroups / 2;
+            const int col0 = group % (kGroups / 2) * kOut;
+            T *out = is_k ? static_cast<T *>(f.p.dk) + row * f.p.dk_ts + w.hk * f.p.dk_hs
+                          : static_cast<T *>(f.p.dv) + row * f.p.dv_ts + w.hk * f.p.dv_hs;
+            const float scale = is_k ? a.scale : kDown;
 #pragma unroll
-            for (int i = 0; i < DP / 32; ++i) {
-                float o[32];
-                tc::tmem_ld32(lane_base + (half ? kDkCol : kDvCol) + 32 * i, o);
+            for (int i = 0; i < kOut / 16; ++i) {
+                const int col = col0 + 16 * i;
+                uint32_t o[16];
+                tmem_ld16(lane_base + (is_k ? kDkCol : kDvCol) + col, o);
                 if (live)
 #pragma unroll
-                    for (int e = 0; e < 32; e += 8)
-                        if (32 * i + e < d) {
+                    for (int e = 0; e < 16; e += 8)
+                        if (col + e < d) {
                             float v[8];
 #pragma unroll
-                            for (int u = 0; u < 8; ++u) v[u] = n > 0 ? o[e + u] * scale : 0.f;
-                            store_vec<T, 8>(out + 32 * i + e, v);
+                            for (int u = 0; u < 8; ++u) v[u] = __uint_as_float(o[e + u]) * scale;
+                            *reinterpret_cast<uint4 *>(out + col + e) =
+                                make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
                         }
             }
+            tc::fence_before_sync();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&work_empty[slot]);
         }
     }
     tc::fence_before_sync();
     __syncthreads();
     if (threadIdx.x == 0 && s_abort) atomicExch(&f.p.ctl->status, SIEVE_ETIMEOUT);
-    if (warp == kWarps + 1) {
+    if (warp == 0) {
         tc::fence_after_sync();
         tc::tmem_dealloc(tmem, 512);
     }
@@ -777,24 +983,38 @@ Layout layout_of(const sieve_attention_args &a) {
     return l;
 }
 
+template <typename T, int DP, bool BIAS, int kWarps>
+cudaError_t run_dkv(const BwdArgs &f, int64_t blocks, size_t smem, cudaStream_t st) {
+    auto dkv = k_attend_dkv<T, DP, BIAS, kWarps>;
+    cudaError_t e = cudaFuncSetAttribute(dkv, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    dkv<<<(unsigned)blocks, (kWarps + 2) * 32, smem, st>>>(f);
+    return cudaGetLastError();
+}
+
+constexpr size_t kSharedLimit = 227 * 1024 - 4096;   // dynamic, beside the kernels' static part
+
 template <typename T, int DP, bool BIAS>
 cudaError_t run(const BwdArgs &f, const Layout &l, unsigned char *ws, cudaStream_t st) {
     const sieve_attention_args &a = f.p.a;
-    const size_t tiles = 1024 + (size_t)(2 + 2 * stages(DP)) * (DP / 64) * kBlockBytes;
+    const size_t tiles = 1024 + (size_t)2 * (walked(DP) + kept(DP)) * (DP / 64) * kBlockBytes;
     cudaError_t e;
     if (a.q_tokens > 0) {
         auto dq = k_attend_dq<T, DP, BIAS>;
-        const size_t smem = tiles + (BIAS ? (size_t)bias_floats(a.reach) * 4 : 0);
+        const size_t smem = tiles + (BIAS ? (size_t)2 * bias_floats(a.reach) * 4 : 0);
         if ((e = cudaFuncSetAttribute(dq, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
-        dq<<<(unsigned)(l.q_tiles * a.heads), kThreads, smem, st>>>(f);
+        dq<<<(unsigned)(l.q_tiles * a.heads), 18 * 32, smem, st>>>(f);
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
     }
     if (a.k_tokens > 0) {
-        auto dkv = k_attend_dkv<T, DP, BIAS>;
-        const size_t smem = tiles + (BIAS ? (size_t)(bias_floats(a.reach, DP == 64 ? 4 : 1) + f.entries * kWarps + kWarps * kScratch) * 4 : 0);
-        if ((e = cudaFuncSetAttribute(dkv, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
-        dkv<<<(unsigned)(l.k_tiles * a.kv_heads), kThreads, smem, st>>>(f);
-        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        // 16 warps where their sums by distance fit beside the tiles
+        auto smem = [&](int warps) {
+            return tiles + (BIAS ? (size_t)(bias_floats(a.reach, DP == 64 ? 4 : 1) + warps * (f.entries + kScratch)) * 4 : 0);
+        };
+        const int64_t blocks = l.k_tiles * a.kv_heads;
+        if (!BIAS || smem(16) <= kSharedLimit) e = run_dkv<T, DP, BIAS, 16>(f, blocks, smem(16), st);
+        else e = run_dkv<T, DP, BIAS, BIAS && DP == 128 ? 8 : 16>(f, blocks, smem(8), st);
+        if (e != cudaSuccess) return e;
     }
     if (BIAS) {
         if (a.k_tokens == 0 || a.q_tokens == 0)
@@ -829,6 +1049,8 @@ sieve_status launch_attention_backward(const AttentionArgs &p, void *ws, cudaStr
     f.partial = reinterpret_cast<float *>(w + l.partial);
     f.doc_tiles = a.new_tokens > 0 ? (int)ceil_div(a.new_tokens, kTile) : 0;
     f.entries = l.entries;
+    f.q_numbers = (int)l.q_tiles;
+    f.k_numbers = (int)l.k_tiles;
     sieve_status rc = SIEVE_OK;
     if (a.q_tokens > 0) {
         rc = make_map(&f.q, a.dtype, a.q, a.head_dim, a.heads, a.q_tokens, a.q_token_stride, a.q_head_stride, 1, kTile);

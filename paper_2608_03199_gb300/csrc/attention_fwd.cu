@@ -178,15 +178,14 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
 
     if (warp == kSoftmaxWarps + 1) {
         // ---------------- the work, one block's after another's, and its loads ----------------
-        const uint32_t lead = lane == 0;
         if (lane == 0) {
             prefetch_map(&f.q);
             prefetch_map(&f.k);
             prefetch_map(&f.v);
         }
         int block = blockIdx.x, item = 0, set = 1, group_in_set = -1, q_issued = 0, k_issued = 0, v_issued = 0;
-        uint32_t asked = 0;
-        bool ok = true, asking = false;
+        Blocks blocks{&s_answer, &steal_bar, 0, false};
+        bool ok = true;
         while (ok && block >= 0) {
             Work w;
             w.group = block / f.numbers;
@@ -235,19 +234,24 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
                         if (j == 0) {
                             const int st = q_issued % kQStages;
                             if (!(ok = wait.warp(&q_empty[st], ((uint32_t)(q_issued / kQStages) & 1u) ^ 1u))) break;
-                            tc::mbar_arrive_expect_tx(lead, &q_full[st],
-                                                      kB * 128u * (uint32_t)(f.pack * (kTile / f.pack)));
-                            for (int b = 0; b < kB; ++b)
-                                tma_load(lead, q_tiles + st * kTileBytes + b * kBlockBytes, &f.q, 64 * b, head0,
-                                         w.q_row + tile * kTile, &q_full[st]);
+                            if (elected()) {
+                                expect(&q_full[st], kB * 128u * (uint32_t)(f.pack * (kTile / f.pack)));
+                                for (int b = 0; b < kB; ++b)
+                                    tma_load(q_tiles + st * kTileBytes + b * kBlockBytes, &f.q, 64 * b, head0,
+                                             w.q_row + tile * kTile, &q_full[st]);
+                            }
+                            __syncwarp();
                             ++q_issued;
                         }
                         const int st = k_issued % kStages;
                         row = w.k_row + j * kTile;
                         if (!(ok = wait.warp(&k_empty[st], ((uint32_t)(k_issued / kStages) & 1u) ^ 1u))) break;
-                        tc::mbar_arrive_expect_tx(lead, &k_full[st], kTileBytes);
-                        for (int b = 0; b < kB; ++b)
-                            tma_load(lead, k_tiles + st * kTileBytes + b * kBlockBytes, &f.k, 64 * b, hk, row, &k_full[st]);
+                        if (elected()) {
+                            expect(&k_full[st], kTileBytes);
+                            for (int b = 0; b < kB; ++b)
+                                tma_load(k_tiles + st * kTileBytes + b * kBlockBytes, &f.k, 64 * b, hk, row, &k_full[st]);
+                        }
+                        __syncwarp();
                         ++k_issued;
                         if (++j == n) {
                             j = n = 0;
@@ -258,9 +262,12 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
                     if (v_row >= 0) {
                         const int st = v_issued % kStages;
                         if (!(ok = wait.warp(&v_empty[st], ((uint32_t)(v_issued / kStages) & 1u) ^ 1u))) break;
-                        tc::mbar_arrive_expect_tx(lead, &v_full[st], kTileBytes);
-                        for (int b = 0; b < kB; ++b)
-                            tma_load(lead, v_tiles + st * kTileBytes + b * kBlockBytes, &f.v, 64 * b, hk, v_row, &v_full[st]);
+                        if (elected()) {
+                            expect(&v_full[st], kTileBytes);
+                            for (int b = 0; b < kB; ++b)
+                                tma_load(v_tiles + st * kTileBytes + b * kBlockBytes, &f.v, 64 * b, hk, v_row, &v_full[st]);
+                        }
+                        __syncwarp();
                         ++v_issued;
                     }
                     if (row < 0) break;
@@ -268,14 +275,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
                 }
                 if (!ok) break;
             }
-            steal_block(lead, &s_answer, &steal_bar);
-            asking = true;
-            if (!(ok = wait.warp(&steal_bar, asked & 1u))) break;
-            ++asked;
-            asking = false;
-            block = stolen_block(&s_answer);
-            tc::fence_proxy_async_smem();     // read before the next answer is written
-            __syncwarp();
+            ok = blocks.next(wait, block);
         }
         if (ok) {
             const int slot = item % kSlots;
@@ -287,7 +287,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
         }
         if (!ok) {
             // after an abort: what is in flight lands before the block ends
-            if (asking) let_land(&steal_bar, asked & 1u);
+            if (blocks.asking) let_land(&steal_bar, blocks.asked & 1u);
             for (int i = max(0, q_issued - kQStages); i < q_issued; ++i)
                 let_land(&q_full[i % kQStages], (uint32_t)(i / kQStages) & 1u);
             for (int i = max(0, k_issued - kStages); i < k_issued; ++i)
@@ -347,7 +347,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
                         if (!(ok = wait.warp(&p_full, step & 1u))) break;
                         tc::fence_after_sync();
                         if (elected()) {
-                            mma_halves<kPHalf>(tmem + kOCol, tmem + kPCol, v0 + st * (kTileBytes >> 4), id_o, key > 0);
+                            mma_groups<kHalf, kPHalf>(tmem + kOCol, tmem + kPCol, v0 + st * (kTileBytes >> 4), id_o, key > 0);
                             commit(&o_full);
                             commit(&v_empty[st]);
                         }
