@@ -177,6 +177,12 @@ struct Waiter {
         return __all_sync(0xffffffffu, (*this)(bar, parity));
     }
 };
+// One arrival for a warp whose lanes are all done (an arrival of every lane is
+// as many serialised operations on the barrier).
+__device__ __forceinline__ void warp_arrive(uint64_t *bar) {
+    __syncwarp();
+    if (lane_id() == 0) tc::mbar_arrive(bar);
+}
 // the copies or products in flight after an abort
 __device__ __forceinline__ void let_land(uint64_t *bar, uint32_t parity) {
 #pragma unroll 1

@@ -36,7 +36,6 @@ namespace enc {
 namespace {
 
 constexpr int kSlots = 2;      // the work in hand and the next
-constexpr int kScratch = 64;   // floats per warp for the diagonals of 32 x 32
 
 // k_attend_dkv rounds P to 16 bits.  A long document's probabilities are small
 // and fp16 has no bits below 2^-24, so it takes 2^14 P there (P <= 1 up to the
@@ -72,7 +71,7 @@ struct Meeting {
     uint64_t *bar;
     uint32_t phase;
     __device__ __forceinline__ bool operator()(const Waiter &wait) {
-        tc::mbar_arrive(bar);
+        warp_arrive(bar);
         const bool ok = wait.warp(bar, phase);
         phase ^= 1u;
         return ok;
@@ -95,14 +94,14 @@ struct DkvWork {
 
 template <typename T, int DP, bool BIAS>
 __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant__ BwdArgs f) {
-    constexpr int kWarps = 16, kCompute = kWarps * 32;
+    constexpr int kWarps = 16;
     constexpr int kGroups = Columns<kWarps>::kGroups, kCols = Columns<kWarps>::kCols;
     constexpr int kB = DP / 64, kWalked = walked(DP), kKept = kept(DP);
     constexpr uint32_t kTileBytes = kB * kBlockBytes;
-    constexpr uint32_t kSCol = 0, kDpCol = 256, kDqCol = 384;   // S twice, dP (dS in its place), dQ
+    constexpr uint32_t kSCol = 0, kDpCol = 128, kDqCol = 384;   // S, dP twice (dS in its place), dQ
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t q_full[kKept], q_empty[kKept], kv_full[kWalked], kv_empty[kWalked], s_full[2],
-        s_free[2], dp_full, ds_full, dq_full, meet_bar, done, work_full[kSlots], work_empty[kSlots], steal_bar;
+    __shared__ __align__(8) uint64_t q_full[kKept], q_empty[kKept], kv_full[kWalked], kv_empty[kWalked], s_full, s_free,
+        dp_full[2], ds_full[2], dq_full, meet_bar, done, work_full[kSlots], work_empty[kSlots], steal_bar;
     __shared__ __align__(16) uint4 s_answer;
     __shared__ uint32_t tmem_slot;
     __shared__ int s_abort;
@@ -128,15 +127,15 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
             tc::mbar_init(&kv_empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
-            tc::mbar_init(&s_full[i], 1);
-            tc::mbar_init(&s_free[i], kCompute);
+            tc::mbar_init(&dp_full[i], 1);
+            tc::mbar_init(&ds_full[i], kWarps);
             tc::mbar_init(&work_full[i], 1);
             tc::mbar_init(&work_empty[i], kWarps + 1);
         }
-        tc::mbar_init(&dp_full, 1);
-        tc::mbar_init(&ds_full, kCompute);
+        tc::mbar_init(&s_full, 1);
+        tc::mbar_init(&s_free, kWarps);
         tc::mbar_init(&dq_full, 1);
-        tc::mbar_init(&meet_bar, kCompute);
+        tc::mbar_init(&meet_bar, kWarps);
         tc::mbar_init(&done, 1);
         tc::mbar_init(&steal_bar, 1);
         s_abort = 0;
@@ -257,12 +256,12 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
             const int n = uniform(s_work[slot].n), nk = uniform(s_work[slot].nk);
             const uint64_t qa = q0 + item % kKept * kPair;
             if (!(ok = wait.warp(&q_full[item % kKept], (uint32_t)(item / kKept) & 1u))) break;
-            // round j: the scores of step j + 1, dQ of step j, dP of step j + 1
+            // round j: the scores and dP of step j + 1 (under the threads'
+            // work on step j), dQ of step j
 #pragma unroll 1
             for (int j = -1; j < n; ++j) {
-                const bool more = j + 1 < n;
                 const uint32_t i = step + (j < 0 ? 0u : 1u), st = i % kWalked;
-                if (more) {
+                if (j + 1 < n) {
                     if (!(ok = wait.warp(&kv_full[st], (i / kWalked) & 1u))) break;
                     const int left = nk - (j + 1) * kTile;
                     if (left < kTile) {
@@ -270,33 +269,29 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
                         clear_rows(kv + st * 2 * kTileBytes, left, kB);
                         clear_rows(kv + (st * 2 + 1) * kTileBytes, left, kB);
                     }
-                    // the scores two steps back are in registers
-                    if (!(ok = wait.warp(&s_free[i & 1u], ((i >> 1) & 1u) ^ 1u))) break;
+                    // the scores of step j are in registers
+                    if (!(ok = wait.warp(&s_free, (i & 1u) ^ 1u))) break;
                     tc::fence_after_sync();
                     if (elected()) {
-                        mma_kk<DP>(tmem + kSCol + (i & 1u) * kTile, qa, kk0 + st * kPair, id_s);
-                        commit(&s_full[i & 1u]);
+                        mma_kk<DP>(tmem + kSCol, qa, kk0 + st * kPair, id_s);
+                        commit(&s_full);
+                        mma_kk<DP>(tmem + kDpCol + (i & 1u) * kTile, qa + kSecond, kk0 + st * kPair + kSecond, id_s);
+                        commit(&dp_full[i & 1u]);
+                        if (j + 2 == n) commit(&q_empty[item % kKept]);
                     }
                     __syncwarp();
                 }
                 if (j >= 0) {
-                    if (!(ok = wait.warp(&ds_full, step & 1u))) break;
+                    if (!(ok = wait.warp(&ds_full[step & 1u], (step >> 1) & 1u))) break;
                     tc::fence_after_sync();
                     if (elected()) {
-                        mma_groups<kCols, kCols>(tmem + kDqCol, tmem + kDpCol, km0 + step % kWalked * kPair, id_o, j > 0);
+                        mma_groups<kCols, kCols>(tmem + kDqCol, tmem + kDpCol + (step & 1u) * kTile,
+                                                 km0 + step % kWalked * kPair, id_o, j > 0);
                         commit(&kv_empty[step % kWalked]);
-                        if (!more) commit(&dq_full);
+                        if (j + 1 == n) commit(&dq_full);
                     }
                     __syncwarp();
                     ++step;
-                }
-                if (more) {
-                    if (elected()) {
-                        mma_kk<DP>(tmem + kDpCol, qa + kSecond, kk0 + st * kPair + kSecond, id_s);
-                        commit(&dp_full);
-                        if (j + 2 == n) commit(&q_empty[item % kKept]);
-                    }
-                    __syncwarp();
                 }
             }
             if (ok && lane == 0) tc::mbar_arrive(&work_empty[slot]);
@@ -313,7 +308,6 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
         const int r = quarter * 32 + lane, d = a.head_dim;
         const float c = a.scale * kLog2e;
         const uint32_t lane_base = tmem + ((uint32_t)(quarter * 32) << 16);
-        const uint32_t dp_at = lane_base + kDpCol + group * kCols;
         Meeting meet{&meet_bar, 0};
         uint32_t step = 0;
         bool ok = true;
@@ -351,7 +345,8 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
             float2 sum2 = both(0.f);
 #pragma unroll 1
             for (int j = 0; j < w.n; ++j, ++step) {
-                if (!(ok = wait.warp(&s_full[step & 1u], (step >> 1) & 1u))) break;
+                if (!(ok = wait.warp(&s_full, step & 1u))) break;
+                const uint32_t dp_at = lane_base + kDpCol + (step & 1u) * kTile + group * kCols;
                 tc::fence_after_sync();
                 const int vis = seen - j * kTile;                    // columns of the group that this row sees
                 const bool all = __all_sync(0xffffffffu, vis >= kCols);
@@ -360,13 +355,13 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
                 float2 x[kCols / 2];
                 if (!none) {
                     uint32_t raw[32];
-                    tc::tmem_ld32_issue(lane_base + kSCol + (step & 1u) * kTile + group * kCols, raw);
+                    tc::tmem_ld32_issue(lane_base + kSCol + group * kCols, raw);
                     tc::tmem_ld_wait(raw);
 #pragma unroll
                     for (int e = 0; e < 16; ++e) x[e] = make_float2(__uint_as_float(raw[2 * e]), __uint_as_float(raw[2 * e + 1]));
                 }
                 tc::fence_before_sync();
-                tc::mbar_arrive(&s_free[step & 1u]);
+                warp_arrive(&s_free);
                 if (!none) {
                     const int d0 = j * kTile + group * kCols;
                     const bool after = d0 - place0 - 31 >= a.reach, before = d0 + 31 - place0 <= -a.reach;
@@ -396,7 +391,7 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
                         }
                     }
                 }
-                if (!(ok = wait.warp(&dp_full, step & 1u))) break;
+                if (!(ok = wait.warp(&dp_full[step & 1u], (step >> 1) & 1u))) break;
                 tc::fence_after_sync();
                 if (!none) {
                     float dp[32];
@@ -416,11 +411,13 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
                 tc::tmem_st_wait();
                 if (BIAS && j == w.n - 1) s_row[1][group][r] = sum2.x + sum2.y;
                 tc::fence_before_sync();
-                tc::mbar_arrive(&ds_full);
+                // (a warp may be a step ahead of another here: the scores of the
+                // next step wait for all to have read this one's, not for dS)
+                warp_arrive(&ds_full[step & 1u]);
             }
             if (!ok) break;
             // (every thread's sum of dS arrived with its last dS)
-            if (!(ok = wait.warp(&ds_full, (step - 1) & 1u) && wait.warp(&dq_full, (uint32_t)item & 1u))) break;
+            if (!(ok = wait.warp(&ds_full[(step - 1) & 1u], ((step - 1) >> 1) & 1u) && wait.warp(&dq_full, (uint32_t)item & 1u))) break;
             tc::fence_after_sync();
             T *out = static_cast<T *>(f.p.dq) + row * f.p.dq_ts + w.head * f.p.dq_hs;
             constexpr int kOut = DP / kGroups;       // 16 or 32 columns of dQ
@@ -488,7 +485,6 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, 1) k_attend_dkv(const __gri
     // the bias by minus the distance (columns run that way)
     constexpr int kCopies = DP == 64 ? 4 : 1;
     float *by_distance = bias + (BIAS ? bias_floats(a.reach, kCopies) : 0);   // [warps][entries]
-    float *scratch = by_distance + kWarps * f.entries;                        // [warps][kScratch]
 
     if (threadIdx.x == 0) {
         if (blockIdx.x == 0 && a.q_tokens == 0) f.p.ctl->status = 0;      // (else k_attend_dq did)
@@ -505,11 +501,11 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, 1) k_attend_dkv(const __gri
             tc::mbar_init(&work_empty[i], kWarps + 1);
         }
         tc::mbar_init(&s_full, 1);
-        tc::mbar_init(&p_full, kCompute);
+        tc::mbar_init(&p_full, kWarps);
         tc::mbar_init(&dp_full, 1);
-        tc::mbar_init(&ds_full, kCompute);
+        tc::mbar_init(&ds_full, kWarps);
         tc::mbar_init(&acc_full, 1);
-        tc::mbar_init(&meet_bar, kCompute);
+        tc::mbar_init(&meet_bar, kWarps);
         tc::mbar_init(&done, 1);
         tc::mbar_init(&steal_bar, 1);
         s_abort = 0;
@@ -701,8 +697,7 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, 1) k_attend_dkv(const __gri
         const int r = quarter * 32 + lane, d = a.head_dim;
         const float c = a.scale * kLog2e;
         const uint32_t lane_base = tmem + ((uint32_t)(quarter * 32) << 16);
-        float *mine = by_distance + warp * f.entries, *line = scratch + warp * kScratch;
-        const float not_first = lane == 0 ? 0.f : 1.f;
+        float *mine = by_distance + warp * f.entries;
         constexpr float kDown = 1.f / (float)(1 << kPShift<T>);
         Meeting meet{&meet_bar, 0};
         uint32_t step = 0;
@@ -803,7 +798,7 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, 1) k_attend_dkv(const __gri
                     }
                     tc::tmem_st_wait();
                     tc::fence_before_sync();
-                    tc::mbar_arrive(&p_full);
+                    warp_arrive(&p_full);
 
                     if (!(ok = wait.warp(&dp_full, step & 1u))) break;
                     tc::fence_after_sync();
@@ -827,13 +822,16 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, 1) k_attend_dkv(const __gri
                     }
                     tc::tmem_st_wait();
                     tc::fence_before_sync();
-                    tc::mbar_arrive(&ds_full);
+                    warp_arrive(&ds_full);
 
                     if (BIAS && !none) {
                         // dS by distance, under the products.  A lane is a key,
-                        // a step to the next query lowers its distance by one: a
-                        // sum that moves up one lane with every step follows one
-                        // distance, and leaves complete at lane 31.
+                        // column e a query e further: with every column turned by
+                        // e lanes, lane l holds the elements of one distance, that
+                        // of key l and the first query, and where the turn wrapped
+                        // around those of the distance 32 less.  (One shuffle an
+                        // element; a sum handed from lane to lane and stored by
+                        // the last took 2.9K cycles a step instead.)
 #pragma unroll
                         for (int q = 0; q < kChunks; ++q) {
                             const int hi = key_lo + 31 - (place0 + 32 * q), lo = hi - 62;
@@ -850,19 +848,16 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, 1) k_attend_dkv(const __gri
                                 x0 = add2(x0, x1);
                                 (lo >= a.reach ? far_after : far_before) += x0.x + x0.y;
                             } else {
-                                float acc = p[q][0].x;
-                                if (lane == 31) line[0] = acc;
+                                float up = 0.f, down = 0.f;
 #pragma unroll
-                                for (int e = 1; e < 32; ++e) {
-                                    acc = __shfl_up_sync(0xffffffffu, acc, 1);
-                                    acc = fmaf(acc, not_first, e & 1 ? p[q][e / 2].y : p[q][e / 2].x);
-                                    if (lane == 31) line[e] = acc;          // distance hi - e
+                                for (int e = 0; e < 32; ++e) {
+                                    const float v = __shfl_sync(0xffffffffu, e & 1 ? p[q][e / 2].y : p[q][e / 2].x, lane + e);
+                                    if (lane + e < 32) up += v;
+                                    else down += v;
                                 }
-                                if (lane < 31) line[62 - lane] = acc;       // lane's distance: hi - (62 - lane)
-                                __syncwarp();
-                                float *to = mine + a.reach + kPad + hi;
-                                to[-lane] += line[lane];
-                                if (lane < 31) to[-(lane + 32)] += line[lane + 32];
+                                float *to = mine + a.reach + kPad + hi - 31 + lane;
+                                to[0] += up;
+                                if (lane > 0) to[-32] += down;
                                 __syncwarp();
                             }
                         }
@@ -1009,7 +1004,7 @@ cudaError_t run(const BwdArgs &f, const Layout &l, unsigned char *ws, cudaStream
     if (a.k_tokens > 0) {
         // 16 warps where their sums by distance fit beside the tiles
         auto smem = [&](int warps) {
-            return tiles + (BIAS ? (size_t)(bias_floats(a.reach, DP == 64 ? 4 : 1) + warps * (f.entries + kScratch)) * 4 : 0);
+            return tiles + (BIAS ? (size_t)(bias_floats(a.reach, DP == 64 ? 4 : 1) + warps * f.entries) * 4 : 0);
         };
         const int64_t blocks = l.k_tiles * a.kv_heads;
         if (!BIAS || smem(16) <= kSharedLimit) e = run_dkv<T, DP, BIAS, 16>(f, blocks, smem(16), st);

@@ -156,12 +156,12 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
             tc::mbar_init(&v_full[i], 1);
         }
         tc::mbar_init(&s_full, 1);
-        tc::mbar_init(&s_free, kSoftmax);
-        tc::mbar_init(&p_full, kSoftmax);
+        tc::mbar_init(&s_free, kSoftmaxWarps);
+        tc::mbar_init(&p_full, kSoftmaxWarps);
         tc::mbar_init(&o_full, 1);
         tc::mbar_init(&drained, 1);
         tc::mbar_init(&steal_bar, 1);
-        for (int i = 0; i < 4; ++i) tc::mbar_init(&pair_bar[i], 64);
+        for (int i = 0; i < 4; ++i) tc::mbar_init(&pair_bar[i], 2);
         for (int i = 0; i < kSlots; ++i) {
             tc::mbar_init(&work_full[i], 1);
             tc::mbar_init(&work_empty[i], kSoftmaxWarps + 1);
@@ -402,9 +402,9 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
                     if (!(ok = wait.warp(&s_full, step & 1u))) break;
                     tc::fence_after_sync();
                     if (idle) {
-                        tc::mbar_arrive(&s_free);
+                        warp_arrive(&s_free);
                         if (step > 0 && !(ok = wait.warp(&o_full, (step - 1) & 1u))) break;
-                        tc::mbar_arrive(&p_full);
+                        warp_arrive(&p_full);
                         continue;
                     }
                     float2 x[2][16];
@@ -421,7 +421,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
                                 x[i][e] = make_float2(__uint_as_float(raw[i][2 * e]), __uint_as_float(raw[i][2 * e + 1]));
                     }
                     tc::fence_before_sync();
-                    tc::mbar_arrive(&s_free);
+                    warp_arrive(&s_free);
                     // columns of the half that this row sees; that any row of
                     // the warp does
                     const int vis = seen - j * kTile;
@@ -478,7 +478,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
                     // comparison)
                     if (!BIAS) top *= c;
                     s_top[meets & 1u][half][r] = top;
-                    tc::mbar_arrive(&pair_bar[quarter]);
+                    warp_arrive(&pair_bar[quarter]);
                     if (!(ok = wait.warp(&pair_bar[quarter], meets & 1u))) break;
                     top = fmaxf(top, s_top[meets & 1u][half ^ 1][r]);
                     ++meets;
@@ -531,13 +531,13 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
                     }
                     tc::tmem_st_wait();
                     tc::fence_before_sync();
-                    tc::mbar_arrive(&p_full);
+                    warp_arrive(&p_full);
                 }
                 if (!ok) break;
                 if (idle) continue;
                 // the row's sum over both halves, and the last product
                 s_top[meets & 1u][half][r] = l;
-                tc::mbar_arrive(&pair_bar[quarter]);
+                warp_arrive(&pair_bar[quarter]);
                 if (!(ok = wait.warp(&pair_bar[quarter], meets & 1u))) break;
                 l += s_top[meets & 1u][half ^ 1][r];
                 ++meets;
