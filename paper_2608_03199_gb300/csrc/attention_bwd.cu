@@ -96,11 +96,13 @@ template <typename T, int DP, bool BIAS>
 __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant__ BwdArgs f) {
     constexpr int kWarps = 16;
     constexpr int kGroups = Columns<kWarps>::kGroups, kCols = Columns<kWarps>::kCols;
-    constexpr int kB = DP / 64, kWalked = walked(DP), kKept = kept(DP);
+    constexpr int kB = DP / 64, kKept = kept(DP);
+    // K of a step is used twice, last after the next step's scores; V once
+    constexpr int kKs = 3, kVs = DP == 64 ? 2 : 1;
     constexpr uint32_t kTileBytes = kB * kBlockBytes;
     constexpr uint32_t kSCol = 0, kDpCol = 128, kDqCol = 384;   // S, dP twice (dS in its place), dQ
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t q_full[kKept], q_empty[kKept], kv_full[kWalked], kv_empty[kWalked], s_full, s_free,
+    __shared__ __align__(8) uint64_t q_full[kKept], q_empty[kKept], k_full[kKs], k_empty[kKs], v_full[kVs], v_empty[kVs], s_full, s_free,
         dp_full[2], ds_full[2], dq_full, meet_bar, done, work_full[kSlots], work_empty[kSlots], steal_bar;
     __shared__ __align__(16) uint4 s_answer;
     __shared__ uint32_t tmem_slot;
@@ -112,8 +114,8 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
 
     unsigned char *base = reinterpret_cast<unsigned char *>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-    unsigned char *qd = base, *kv = qd + kKept * 2 * kTileBytes;      // pairs: Q and dO, K and V
-    float *bias = reinterpret_cast<float *>(kv + kWalked * 2 * kTileBytes);   // two heads' tables
+    unsigned char *qd = base, *k_tiles = qd + kKept * 2 * kTileBytes, *v_tiles = k_tiles + kKs * kTileBytes;   // qd: pairs
+    float *bias = reinterpret_cast<float *>(v_tiles + kVs * kTileBytes);      // two heads' tables
     const int bias_set = BIAS ? bias_floats(a.reach) : 0;
 
     if (threadIdx.x == 0) {
@@ -122,9 +124,13 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
             tc::mbar_init(&q_full[i], 1);
             tc::mbar_init(&q_empty[i], 1);
         }
-        for (int i = 0; i < kWalked; ++i) {
-            tc::mbar_init(&kv_full[i], 1);
-            tc::mbar_init(&kv_empty[i], 1);
+        for (int i = 0; i < kKs; ++i) {
+            tc::mbar_init(&k_full[i], 1);
+            tc::mbar_init(&k_empty[i], 1);
+        }
+        for (int i = 0; i < kVs; ++i) {
+            tc::mbar_init(&v_full[i], 1);
+            tc::mbar_init(&v_empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
             tc::mbar_init(&dp_full[i], 1);
@@ -150,7 +156,7 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
 
     if (warp == kWarps + 1) {
         // ---------------- the work, one block's after another's, and its loads ----------------
-        int block = blockIdx.x, item = 0, kv_issued = 0, head0 = -1, head1 = -1;
+        int block = blockIdx.x, item = 0, kv_issued = 0, k_issued = 0, head0 = -1, head1 = -1;
         Blocks blocks{&s_answer, &steal_bar, 0, false};
         bool ok = true;
         while (ok && block >= 0) {
@@ -209,15 +215,20 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
                     ++item;
 #pragma unroll 1
                     for (int j = 0; j < w.n; ++j, ++kv_issued) {
-                        const int st = kv_issued % kWalked;
-                        if (!(ok = wait.warp(&kv_empty[st], ((uint32_t)(kv_issued / kWalked) & 1u) ^ 1u))) break;
+                        const int ks = kv_issued % kKs, vs = kv_issued % kVs, row = doc.k0 + j * kTile;
+                        if (!(ok = wait.warp(&k_empty[ks], ((uint32_t)(kv_issued / kKs) & 1u) ^ 1u))) break;
                         if (elected()) {
-                            expect(&kv_full[st], 2 * kTileBytes);
-                            for (int b = 0; b < kB; ++b) {
-                                tma_load(kv + st * 2 * kTileBytes + b * kBlockBytes, &f.k, 64 * b, hk, doc.k0 + j * kTile, &kv_full[st]);
-                                tma_load(kv + (st * 2 + 1) * kTileBytes + b * kBlockBytes, &f.v, 64 * b, hk, doc.k0 + j * kTile,
-                                         &kv_full[st]);
-                            }
+                            expect(&k_full[ks], kTileBytes);
+                            for (int b = 0; b < kB; ++b)
+                                tma_load(k_tiles + ks * kTileBytes + b * kBlockBytes, &f.k, 64 * b, hk, row, &k_full[ks]);
+                        }
+                        __syncwarp();
+                        k_issued = kv_issued + 1;
+                        if (!(ok = wait.warp(&v_empty[vs], ((uint32_t)(kv_issued / kVs) & 1u) ^ 1u))) break;
+                        if (elected()) {
+                            expect(&v_full[vs], kTileBytes);
+                            for (int b = 0; b < kB; ++b)
+                                tma_load(v_tiles + vs * kTileBytes + b * kBlockBytes, &f.v, 64 * b, hk, row, &v_full[vs]);
                         }
                         __syncwarp();
                     }
@@ -238,15 +249,15 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
             // after an abort: what is in flight lands before the block ends
             if (blocks.asking) let_land(&steal_bar, blocks.asked & 1u);
             for (int i = max(0, item - kKept); i < item; ++i) let_land(&q_full[i % kKept], (uint32_t)(i / kKept) & 1u);
-            for (int i = max(0, kv_issued - kWalked); i < kv_issued; ++i)
-                let_land(&kv_full[i % kWalked], (uint32_t)(i / kWalked) & 1u);
+            for (int i = max(0, k_issued - kKs); i < k_issued; ++i) let_land(&k_full[i % kKs], (uint32_t)(i / kKs) & 1u);
+            for (int i = max(0, kv_issued - kVs); i < kv_issued; ++i) let_land(&v_full[i % kVs], (uint32_t)(i / kVs) & 1u);
         }
         __syncwarp();
     } else if (warp == kWarps) {
         // ---------------- products ----------------
         constexpr uint32_t id_s = idesc<T>(kTile, false), id_o = idesc<T>(DP, true);
-        constexpr uint32_t kPair = 2 * kTileBytes >> 4, kSecond = kTileBytes >> 4;   // in a descriptor's units
-        const uint64_t q0 = desc_k(qd), kk0 = desc_k(kv), km0 = desc_mn(kv);
+        constexpr uint32_t kPair = 2 * kTileBytes >> 4, kTileStep = kTileBytes >> 4;   // in a descriptor's units
+        const uint64_t q0 = desc_k(qd), kk0 = desc_k(k_tiles), km0 = desc_mn(k_tiles), v0 = desc_k(v_tiles);
         uint32_t step = 0;
         bool ok = true;
         for (int item = 0; ok; ++item) {
@@ -256,43 +267,49 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
             const int n = uniform(s_work[slot].n), nk = uniform(s_work[slot].nk);
             const uint64_t qa = q0 + item % kKept * kPair;
             if (!(ok = wait.warp(&q_full[item % kKept], (uint32_t)(item / kKept) & 1u))) break;
-            // round j: the scores and dP of step j + 1 (under the threads'
-            // work on step j), dQ of step j
+            // round j: the scores of step j + 1 as soon as those of step j are
+            // in registers; when dS of step j is there, dP of step j + 1, then
+            // dQ of step j
 #pragma unroll 1
             for (int j = -1; j < n; ++j) {
-                const uint32_t i = step + (j < 0 ? 0u : 1u), st = i % kWalked;
-                if (j + 1 < n) {
-                    if (!(ok = wait.warp(&kv_full[st], (i / kWalked) & 1u))) break;
-                    const int left = nk - (j + 1) * kTile;
-                    if (left < kTile) {
-                        // rows of another document: 0 x NaN in dS K, NaN in dP
-                        clear_rows(kv + st * 2 * kTileBytes, left, kB);
-                        clear_rows(kv + (st * 2 + 1) * kTileBytes, left, kB);
-                    }
-                    // the scores of step j are in registers
+                const uint32_t i = step + (j < 0 ? 0u : 1u), ks = i % kKs, vs = i % kVs;
+                const bool more = j + 1 < n;
+                const int left = nk - (j + 1) * kTile;
+                if (more) {
+                    if (!(ok = wait.warp(&k_full[ks], (i / kKs) & 1u))) break;
+                    // rows of another document: 0 x NaN in dS K
+                    if (left < kTile) clear_rows(k_tiles + ks * kTileBytes, left, kB);
                     if (!(ok = wait.warp(&s_free, (i & 1u) ^ 1u))) break;
                     tc::fence_after_sync();
                     if (elected()) {
-                        mma_kk<DP>(tmem + kSCol, qa, kk0 + st * kPair, id_s);
+                        mma_kk<DP>(tmem + kSCol, qa, kk0 + ks * kTileStep, id_s);
                         commit(&s_full);
-                        mma_kk<DP>(tmem + kDpCol + (i & 1u) * kTile, qa + kSecond, kk0 + st * kPair + kSecond, id_s);
+                    }
+                    __syncwarp();
+                }
+                if (j >= 0 && !(ok = wait.warp(&ds_full[step & 1u], (step >> 1) & 1u))) break;
+                if (more) {
+                    if (!(ok = wait.warp(&v_full[vs], (i / kVs) & 1u))) break;
+                    // and NaN in dP
+                    if (left < kTile) clear_rows(v_tiles + vs * kTileBytes, left, kB);
+                }
+                tc::fence_after_sync();
+                if (elected()) {
+                    if (more) {
+                        mma_kk<DP>(tmem + kDpCol + (i & 1u) * kTile, qa + kTileStep, v0 + vs * kTileStep, id_s);
                         commit(&dp_full[i & 1u]);
+                        commit(&v_empty[vs]);
                         if (j + 2 == n) commit(&q_empty[item % kKept]);
                     }
-                    __syncwarp();
-                }
-                if (j >= 0) {
-                    if (!(ok = wait.warp(&ds_full[step & 1u], (step >> 1) & 1u))) break;
-                    tc::fence_after_sync();
-                    if (elected()) {
+                    if (j >= 0) {
                         mma_groups<kCols, kCols>(tmem + kDqCol, tmem + kDpCol + (step & 1u) * kTile,
-                                                 km0 + step % kWalked * kPair, id_o, j > 0);
-                        commit(&kv_empty[step % kWalked]);
-                        if (j + 1 == n) commit(&dq_full);
+                                                 km0 + step % kKs * kTileStep, id_o, j > 0);
+                        commit(&k_empty[step % kKs]);
+                        if (!more) commit(&dq_full);
                     }
-                    __syncwarp();
-                    ++step;
                 }
+                __syncwarp();
+                if (j >= 0) ++step;
             }
             if (ok && lane == 0) tc::mbar_arrive(&work_empty[slot]);
         }
@@ -996,7 +1013,8 @@ cudaError_t run(const BwdArgs &f, const Layout &l, unsigned char *ws, cudaStream
     cudaError_t e;
     if (a.q_tokens > 0) {
         auto dq = k_attend_dq<T, DP, BIAS>;
-        const size_t smem = tiles + (BIAS ? (size_t)2 * bias_floats(a.reach) * 4 : 0);
+        const size_t smem = 1024 + (size_t)(2 * kept(DP) + 3 + (DP == 64 ? 2 : 1)) * (DP / 64) * kBlockBytes +
+                            (BIAS ? (size_t)2 * bias_floats(a.reach) * 4 : 0);
         if ((e = cudaFuncSetAttribute(dq, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
         dq<<<(unsigned)(l.q_tiles * a.heads), 18 * 32, smem, st>>>(f);
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
