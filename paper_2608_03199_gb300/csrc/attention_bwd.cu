@@ -8,7 +8,7 @@
 //   S = Q K^T, dP = dO V^T     a thread's lane is its query
 //   dS = P (dP - delta), rounded to 16 bits into tensor memory
 //   dQ += dS K
-// It starts with delta = dO . O of its rows; O was rounded, so with a table it
+// k_attend_delta gives it delta = dO . O.  O was rounded, so with a table it
 // also sums dS along every row: that sum would be zero with the exact delta
 // (the probabilities of a row add up to one), so delta plus the sum is the
 // exact one, and the second kernel takes that.
@@ -92,6 +92,52 @@ struct DkvWork {
     int hk, k_row, key0, nk, q_row, nq, q_first, q_tiles, q_number, number;   // hk < 0: no more
 };
 
+// delta = dO . O of every query, and -lse in base 2: a block per tile and head,
+// 8 or 16 lanes to a row.  (Inside k_attend_dq, with a row to a thread, the same
+// reads took 3K to 9K cycles of every block's time.)
+constexpr int kDeltaThreads = 256;
+template <typename T, int kLanes>
+__global__ void __launch_bounds__(kDeltaThreads) k_attend_delta(const __grid_constant__ BwdArgs f) {
+    const sieve_attention_args &a = f.p.a;
+    if (blockIdx.x == 0 && threadIdx.x == 0) f.p.ctl->status = 0;
+    const int t = blockIdx.x / a.heads, head = blockIdx.x % a.heads;
+    int s, tile;
+    if (a.new_tokens > 0) {
+        s = t / f.doc_tiles;
+        tile = t % f.doc_tiles;
+    } else {
+        s = find_doc(a.q_offsets, (int)a.nseq, (int)a.q_tokens, kTile, t);
+        tile = t - first_tile(a.q_offsets, s, (int)a.q_tokens, kTile);
+    }
+    const Doc doc = doc_at(a, s);
+    if (tile < 0 || tile * kTile >= doc.nq) return;
+    const int64_t row0 = doc.q0 + tile * kTile;
+    const int rows = min(kTile, doc.nq - tile * kTile);
+    float *stats = f.stats + ((int64_t)t * a.heads + head) * 2 * kTile;
+    const int piece = threadIdx.x % kLanes, d = a.head_dim;
+    const T *o = static_cast<const T *>(f.p.out_in) + (row0 * a.heads + head) * d + piece * 8;
+    const T *g = static_cast<const T *>(f.p.dout) + (row0 * a.heads + head) * d + piece * 8;
+    constexpr int kRows = kDeltaThreads / kLanes;
+#pragma unroll
+    for (int i = 0; i < kTile / kRows; ++i) {
+        const int r = i * kRows + threadIdx.x / kLanes;
+        float x[8], y[8], part = 0.f;
+        if (r < rows && piece * 8 < d) {
+            load_vec<T, 8>(o + (int64_t)r * a.heads * d, x);
+            load_vec<T, 8>(g + (int64_t)r * a.heads * d, y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) part = fmaf(x[e], y[e], part);
+        }
+#pragma unroll
+        for (int k = kLanes / 2; k; k >>= 1) part += __shfl_xor_sync(0xffffffffu, part, k);
+        if (piece == 0) {
+            const float lse = r < rows ? f.p.lse_in[(int64_t)head * a.q_tokens + row0 + r] : -INFINITY;
+            stats[r] = lse == -INFINITY ? -INFINITY : (float)kPShift<T> - lse * kLog2e;
+            stats[kTile + r] = -part * (1.f / (float)(1 << kPShift<T>));
+        }
+    }
+}
+
 template <typename T, int DP, bool BIAS>
 __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant__ BwdArgs f) {
     constexpr int kWarps = 16;
@@ -103,12 +149,13 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
     constexpr uint32_t kSCol = 0, kDpCol = 128, kDqCol = 384;   // S, dP twice (dS in its place), dQ
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t q_full[kKept], q_empty[kKept], k_full[kKs], k_empty[kKs], v_full[kVs], v_empty[kVs], s_full, s_free,
-        dp_full[2], ds_full[2], dq_full, meet_bar, done, work_full[kSlots], work_empty[kSlots], steal_bar;
+        dp_full[2], ds_full[2], dq_full, done, work_full[kSlots], work_empty[kSlots], steal_bar;
     __shared__ __align__(16) uint4 s_answer;
     __shared__ uint32_t tmem_slot;
     __shared__ int s_abort;
     __shared__ DqWork s_work[kSlots];
-    __shared__ float s_row[2][kGroups][kTile];
+    __shared__ float s_row[kGroups][kTile];
+    __shared__ __align__(16) float s_stats[kSlots][2][kTile];
     const sieve_attention_args &a = f.p.a;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = lane_id();
 
@@ -119,7 +166,6 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
     const int bias_set = BIAS ? bias_floats(a.reach) : 0;
 
     if (threadIdx.x == 0) {
-        if (blockIdx.x == 0) f.p.ctl->status = 0;
         for (int i = 0; i < kKept; ++i) {
             tc::mbar_init(&q_full[i], 1);
             tc::mbar_init(&q_empty[i], 1);
@@ -141,7 +187,6 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
         tc::mbar_init(&s_full, 1);
         tc::mbar_init(&s_free, kWarps);
         tc::mbar_init(&dq_full, 1);
-        tc::mbar_init(&meet_bar, kWarps);
         tc::mbar_init(&done, 1);
         tc::mbar_init(&steal_bar, 1);
         s_abort = 0;
@@ -204,7 +249,8 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
                     if (lane == 0) tc::mbar_arrive(&work_full[slot]);
                     if (!(ok = wait.warp(&q_empty[qs], ((uint32_t)(item / kKept) & 1u) ^ 1u))) break;
                     if (elected()) {
-                        expect(&q_full[qs], 2 * kTileBytes);
+                        expect(&q_full[qs], 2 * kTileBytes + 2 * kTile * 4);
+                        tc::bulk_g2s(1u, s_stats[slot], f.stats + (int64_t)w.stats * 2 * kTile, 2 * kTile * 4, &q_full[qs]);
                         for (int b = 0; b < kB; ++b) {
                             tma_load(qd + qs * 2 * kTileBytes + b * kBlockBytes, &f.q, 64 * b, head, doc.q0 + w.row0, &q_full[qs]);
                             tma_load(qd + (qs * 2 + 1) * kTileBytes + b * kBlockBytes, &f.dout, 64 * b, head, doc.q0 + w.row0,
@@ -325,7 +371,6 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
         const int r = quarter * 32 + lane, d = a.head_dim;
         const float c = a.scale * kLog2e;
         const uint32_t lane_base = tmem + ((uint32_t)(quarter * 32) << 16);
-        Meeting meet{&meet_bar, 0};
         uint32_t step = 0;
         bool ok = true;
 #pragma unroll 1
@@ -339,26 +384,9 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
             const int seen = (live ? (a.causal ? min(w.nk, place + 1) : w.nk) : 0) - group * kCols;
             const int64_t row = w.q_row + w.row0 + r;
             const float *table = bias + slot * bias_set;
-            // delta: each of a row's threads adds a share of the products
-            float part = 0.f, nl = -INFINITY;
-            if (live) {
-                const T *o = static_cast<const T *>(f.p.out_in) + (row * a.heads + w.head) * d;
-                const T *g = static_cast<const T *>(f.p.dout) + (row * a.heads + w.head) * d;
-                const float lse = f.p.lse_in[(int64_t)w.head * a.q_tokens + row];
-                for (int i = group * 8; i < d; i += 8 * kGroups) {
-                    float x[8], y[8];
-                    load_vec<T, 8>(o + i, x);
-                    load_vec<T, 8>(g + i, y);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) part = fmaf(x[e], y[e], part);
-                }
-                if (lse != -INFINITY) nl = -lse * kLog2e;
-            }
-            s_row[0][group][r] = part;
-            if (!(ok = meet(wait))) break;
-            float delta = 0.f;
-#pragma unroll
-            for (int k = 0; k < kGroups; ++k) delta += s_row[0][k][r];
+            if (!(ok = wait.warp(&q_full[item % kKept], (uint32_t)(item / kKept) & 1u))) break;   // the row statistics
+            const float nl = s_stats[slot][0][r] - (float)kPShift<T>;
+            const float minus_delta = s_stats[slot][1][r] * (float)(1 << kPShift<T>);
             float2 sum2 = both(0.f);
 #pragma unroll 1
             for (int j = 0; j < w.n; ++j, ++step) {
@@ -415,7 +443,7 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
                     tc::tmem_ld32(dp_at, dp);
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        x[e] = mul2(x[e], add2(make_float2(dp[2 * e], dp[2 * e + 1]), both(-delta)));
+                        x[e] = mul2(x[e], add2(make_float2(dp[2 * e], dp[2 * e + 1]), both(minus_delta)));
                         if (BIAS) sum2 = add2(sum2, x[e]);
                         pk[e] = pack2<T>(x[e].x, x[e].y);
                     }
@@ -426,7 +454,7 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
                 }
                 tc::tmem_st16(dp_at, pk);
                 tc::tmem_st_wait();
-                if (BIAS && j == w.n - 1) s_row[1][group][r] = sum2.x + sum2.y;
+                if (BIAS && j == w.n - 1) s_row[group][r] = sum2.x + sum2.y;
                 tc::fence_before_sync();
                 // (a warp may be a step ahead of another here: the scores of the
                 // next step wait for all to have read this one's, not for dS)
@@ -455,13 +483,12 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
                         }
             }
             tc::fence_before_sync();
-            if (group == 0) {
-                float *stats = f.stats + (int64_t)w.stats * 2 * kTile;
-                stats[r] = nl + (float)kPShift<T>;
-                if (BIAS && nl != -INFINITY)
+            if (BIAS && group == 0 && nl != -INFINITY) {
+                // the exact delta, for k_attend_dkv
+                float sum = 0.f;
 #pragma unroll
-                    for (int k = 0; k < kGroups; ++k) delta += s_row[1][k][r];
-                stats[kTile + r] = -delta * (1.f / (float)(1 << kPShift<T>));
+                for (int k = 0; k < kGroups; ++k) sum += s_row[k][r];
+                f.stats[(int64_t)w.stats * 2 * kTile + kTile + r] = (minus_delta - sum) * (1.f / (float)(1 << kPShift<T>));
             }
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&work_empty[slot]);
@@ -504,7 +531,7 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, 1) k_attend_dkv(const __gri
     float *by_distance = bias + (BIAS ? bias_floats(a.reach, kCopies) : 0);   // [warps][entries]
 
     if (threadIdx.x == 0) {
-        if (blockIdx.x == 0 && a.q_tokens == 0) f.p.ctl->status = 0;      // (else k_attend_dq did)
+        if (blockIdx.x == 0 && a.q_tokens == 0) f.p.ctl->status = 0;      // (else k_attend_delta did)
         for (int i = 0; i < kKept; ++i) {
             tc::mbar_init(&kv_full[i], 1);
             tc::mbar_init(&kv_empty[i], 1);
@@ -1012,6 +1039,8 @@ cudaError_t run(const BwdArgs &f, const Layout &l, unsigned char *ws, cudaStream
     const size_t tiles = 1024 + (size_t)2 * (walked(DP) + kept(DP)) * (DP / 64) * kBlockBytes;
     cudaError_t e;
     if (a.q_tokens > 0) {
+        k_attend_delta<T, DP / 8><<<(unsigned)(l.q_tiles * a.heads), kDeltaThreads, 0, st>>>(f);
+        if ((e = cudaGetLastError()) != cudaSuccess) return e;
         auto dq = k_attend_dq<T, DP, BIAS>;
         const size_t smem = 1024 + (size_t)(2 * kept(DP) + 3 + (DP == 64 ? 2 : 1)) * (DP / 64) * kBlockBytes +
                             (BIAS ? (size_t)2 * bias_floats(a.reach) * 4 : 0);

@@ -170,7 +170,7 @@ struct PoolArgs {
     int64_t stride, nseq;
     int tokens, width, dtype;
 };
-constexpr int kPoolTile = 128;   // tokens per block
+constexpr int kPoolTile = 256;   // tokens per block
 cudaError_t launch_pool_forward(const PoolArgs &a, cudaStream_t st);
 cudaError_t launch_pool_backward(const PoolArgs &a, cudaStream_t st);
 

@@ -1,35 +1,33 @@
 // norm.cu -- layer norm over the last axis, forward and backward.
+#include <type_traits>
+
 #include "encoder.cuh"
 
 namespace sieve {
 namespace enc {
 namespace {
 
-// Sum of a value over a group of TPR threads (a warp, or the whole block).
+// Sum of a value over the TPR threads of a block.
 template <int TPR>
-__device__ __forceinline__ float group_sum(float v, float *smem) {
+__device__ __forceinline__ float block_sum(float v, float *smem) {
     v = warp_sum(v);
-    if constexpr (TPR > 32) {
-        __syncthreads();
-        if (lane_id() == 0) smem[threadIdx.x >> 5] = v;
-        __syncthreads();
-        v = 0.f;
+    __syncthreads();
+    if (lane_id() == 0) smem[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = 0.f;
 #pragma unroll
-        for (int w = 0; w < TPR / 32; ++w) v += smem[w];
-    }
+    for (int w = 0; w < TPR / 32; ++w) v += smem[w];
     return v;
 }
 
-// One row per group of TPR threads, held in registers: NCH chunks of VEC
-// elements a thread, chunk c of thread i at (c * TPR + i) * VEC.
+// Rows wider than 1,024: one row per block of TPR threads, held in registers:
+// NCH chunks of VEC elements a thread, chunk c of thread i at (c * TPR + i) * VEC.
 template <typename T, typename W, int VEC, int TPR, int NCH>
-__global__ void __launch_bounds__(TPR > 128 ? TPR : 128)
+__global__ void __launch_bounds__(TPR)
     k_norm_forward(const NormArgs a) {
-    constexpr int kRows = TPR >= 128 ? 1 : 128 / TPR;
     __shared__ float smem[32];
-    const int i = threadIdx.x % TPR;
-    const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
-    if (TPR == 32 && row >= a.rows) return;
+    const int i = threadIdx.x;
+    const int64_t row = blockIdx.x;
     const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
     float v[NCH][VEC];
     float s = 0.f;
@@ -43,7 +41,7 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128)
 #pragma unroll
         for (int e = 0; e < VEC; ++e) s += v[c][e];
     }
-    const float mean = group_sum<TPR>(s, smem) / (float)a.width;
+    const float mean = block_sum<TPR>(s, smem) / (float)a.width;
     float q = 0.f;
 #pragma unroll
     for (int c = 0; c < NCH; ++c)
@@ -53,7 +51,7 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128)
                 v[c][e] -= mean;
                 q = fmaf(v[c][e], v[c][e], q);
             }
-    const float rstd = 1.f / sqrtf(group_sum<TPR>(q, smem) / (float)a.width + a.eps);
+    const float rstd = 1.f / sqrtf(block_sum<TPR>(q, smem) / (float)a.width + a.eps);
     T *y = static_cast<T *>(a.y) + row * a.y_stride;
     const W *w = static_cast<const W *>(a.weight), *b = static_cast<const W *>(a.bias);
 #pragma unroll
@@ -73,7 +71,7 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128)
     }
 }
 
-// Backward: a block of TPR threads walks its rows, R of them at a time, and
+// Its backward pass: a block of TPR threads walks its rows, R of them at a time, and
 // keeps the column sums of dweight and dbias of its columns in registers;
 // they go to partial[block][2][width] and k_norm_reduce adds the blocks up.
 template <typename T, typename W, int VEC, int TPR, int NCH, int R>
@@ -93,28 +91,35 @@ __global__ void __launch_bounds__(TPR)
     }
     const float inv_n = 1.f / (float)a.width;
     for (int64_t r0 = (int64_t)blockIdx.x * R; r0 < a.rows; r0 += (int64_t)gridDim.x * R) {
-        float g[R][NCH][VEC], xh[R][NCH][VEC], rs[R], s1[R], s2[R];
+        float g[R][NCH][VEC], xh[R][NCH][VEC], mu[R], rs[R], s1[R], s2[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int64_t row = r0 + r;
             const bool live = row < a.rows;
-            const float mu = live ? __ldg(a.mean_in + row) : 0.f;
-            rs[r] = live ? __ldg(a.rstd_in + row) : 0.f;
+            // (places past the row or the rows read its last piece: all loads
+            // go out before the first is used, with no branch between them)
+            const int64_t at = live ? row : a.rows - 1;
+            mu[r] = __ldg(a.mean_in + at);
+            rs[r] = live ? __ldg(a.rstd_in + at) : 0.f;
             s1[r] = s2[r] = 0.f;
 #pragma unroll
             for (int c = 0; c < NCH; ++c) {
-                const int col = (c * TPR + i) * VEC;
-                if (live && col < a.width) {
-                    load_vec<T, VEC>(dy + row * a.dy_stride + col, g[r][c]);
-                    load_vec<T, VEC>(x + row * a.x_stride + col, xh[r][c]);
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) xh[r][c][e] = (xh[r][c][e] - mu) * rs[r];
-                } else {
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) g[r][c][e] = xh[r][c][e] = 0.f;
-                }
+                const int col = min((c * TPR + i) * VEC, a.width - VEC);
+                load_vec<T, VEC>(dy + at * a.dy_stride + col, g[r][c]);
+                load_vec<T, VEC>(x + at * a.x_stride + col, xh[r][c]);
             }
         }
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int c = 0; c < NCH; ++c) {
+                const bool live = r0 + r < a.rows && (c * TPR + i) * VEC < a.width;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    g[r][c][e] = live ? g[r][c][e] : 0.f;
+                    xh[r][c][e] = live ? (xh[r][c][e] - mu[r]) * rs[r] : 0.f;
+                }
+            }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
 #pragma unroll
@@ -133,23 +138,21 @@ __global__ void __launch_bounds__(TPR)
             s1[r] = warp_sum(s1[r]);
             s2[r] = warp_sum(s2[r]);
         }
-        if constexpr (TPR > 32) {
-            __syncthreads();
-            if (lane_id() == 0)
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    smem[2 * r][i >> 5] = s1[r];
-                    smem[2 * r + 1][i >> 5] = s2[r];
-                }
-            __syncthreads();
+        __syncthreads();
+        if (lane_id() == 0)
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                s1[r] = s2[r] = 0.f;
+                smem[2 * r][i >> 5] = s1[r];
+                smem[2 * r + 1][i >> 5] = s2[r];
+            }
+        __syncthreads();
 #pragma unroll
-                for (int w = 0; w < TPR / 32; ++w) {
-                    s1[r] += smem[2 * r][w];
-                    s2[r] += smem[2 * r + 1][w];
-                }
+        for (int r = 0; r < R; ++r) {
+            s1[r] = s2[r] = 0.f;
+#pragma unroll
+            for (int w = 0; w < TPR / 32; ++w) {
+                s1[r] += smem[2 * r][w];
+                s2[r] += smem[2 * r + 1][w];
             }
         }
 #pragma unroll
@@ -178,6 +181,168 @@ __global__ void __launch_bounds__(TPR)
                 pb[col + e] = db[c][e];
             }
     }
+}
+
+// Rows up to 1,024 wide: a warp to a row, NCH chunks of VEC elements a lane,
+// chunk c of lane i at (c * 32 + i) * VEC.
+constexpr int kRowWarps = 8;
+
+template <typename T, int VEC>
+struct Raw {      // VEC elements as loaded
+    static_assert(VEC == 1 || VEC * sizeof(T) == 16, "");
+    uint4 v;
+    __device__ __forceinline__ void load(const T *p) {
+        if constexpr (VEC == 1) {
+            if constexpr (sizeof(T) == 4) v.x = *reinterpret_cast<const uint32_t *>(p);
+            else v.x = *reinterpret_cast<const uint16_t *>(p);
+        } else {
+            v = *reinterpret_cast<const uint4 *>(p);
+        }
+    }
+    __device__ __forceinline__ void get(float (&x)[VEC]) const {
+        const T *e = reinterpret_cast<const T *>(&v);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) x[i] = to_f32<T>(e[i]);
+    }
+};
+
+// Forward: one row a warp.  (A warp that walks rows with the weights in its
+// registers leaves too few warps to hide the loads: 2.5 times as long at 200K x
+// 1024; the weights come from the L1 cache instead.)
+template <typename T, typename W, int VEC, int NCH>
+__global__ void __launch_bounds__(kRowWarps * 32) k_norm_forward_rows(const NormArgs a) {
+    const int lane = lane_id();
+    const int64_t row = (int64_t)blockIdx.x * kRowWarps + (threadIdx.x >> 5);
+    if (row >= a.rows) return;
+    const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
+    float v[NCH][VEC], s = 0.f, q = 0.f;
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+        const int col = (c * 32 + lane) * VEC;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[c][e] = 0.f;
+        if (col < a.width) load_vec<T, VEC>(x + col, v[c]);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) s += v[c][e];
+    }
+    const float inv_n = 1.f / (float)a.width, mean = warp_sum(s) * inv_n;
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+        if ((c * 32 + lane) * VEC < a.width)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                v[c][e] -= mean;
+                q = fmaf(v[c][e], v[c][e], q);
+            }
+    const float rstd = 1.f / sqrtf(fmaf(warp_sum(q), inv_n, a.eps));
+    T *y = static_cast<T *>(a.y) + row * a.y_stride;
+    const W *w = static_cast<const W *>(a.weight), *b = static_cast<const W *>(a.bias);
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+        const int col = (c * 32 + lane) * VEC;
+        if (col >= a.width) continue;
+        float wv[VEC], bv[VEC];
+        load_vec<W, VEC>(w + col, wv);
+        if (b) load_vec<W, VEC>(b + col, bv);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[c][e] = fmaf(v[c][e] * rstd, wv[e], b ? bv[e] : 0.f);
+        store_vec<T, VEC>(y + col, v[c]);
+    }
+    if (a.mean && lane == 0) {
+        a.mean[row] = mean;
+        a.rstd[row] = rstd;
+    }
+}
+
+// Backward, moved 16 bytes at a time: a warp walks its rows, the next one's
+// elements on their way while it works on this one, and needs no other warp
+// until the end.
+template <typename T, typename W, int VEC, int NCH>
+__global__ void __launch_bounds__(kRowWarps * 32) k_norm_backward_rows(const NormArgs a) {
+    __shared__ float part[kRowWarps][32 * VEC];
+    const int lane = lane_id(), warp = threadIdx.x >> 5;
+    const int64_t step = (int64_t)gridDim.x * kRowWarps;
+    int64_t row = (int64_t)blockIdx.x * kRowWarps + warp;
+    const T *dy = static_cast<const T *>(a.dy), *x = static_cast<const T *>(a.x);
+    T *dx = static_cast<T *>(a.dx);
+    float wv[NCH][VEC], dw[NCH][VEC], db[NCH][VEC], mu = 0.f, rs = 0.f;
+    Raw<T, VEC> ny[NCH], nx[NCH];
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+        const int col = (c * 32 + lane) * VEC;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) dw[c][e] = db[c][e] = 0.f;
+        if (col < a.width) {
+            load_vec<W, VEC>(static_cast<const W *>(a.weight) + col, wv[c]);
+            if (row < a.rows) {
+                ny[c].load(dy + row * a.dy_stride + col);
+                nx[c].load(x + row * a.x_stride + col);
+            }
+        }
+    }
+    if (row < a.rows) {
+        mu = __ldg(a.mean_in + row);
+        rs = __ldg(a.rstd_in + row);
+    }
+    const float inv_n = 1.f / (float)a.width;
+    for (; row < a.rows; row += step) {
+        const bool more = row + step < a.rows;
+        const float r = rs, m = mu;
+        float g[NCH][VEC], u[NCH][VEC], s1 = 0.f, s2 = 0.f;
+        if (more) {
+            mu = __ldg(a.mean_in + row + step);
+            rs = __ldg(a.rstd_in + row + step);
+        }
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) {
+            const int col = (c * 32 + lane) * VEC;
+            if (col >= a.width) continue;
+            ny[c].get(g[c]);
+            nx[c].get(u[c]);
+            if (more) {
+                ny[c].load(dy + (row + step) * a.dy_stride + col);
+                nx[c].load(x + (row + step) * a.x_stride + col);
+            }
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const float d = g[c][e];
+                u[c][e] = (u[c][e] - m) * r;
+                dw[c][e] = fmaf(d, u[c][e], dw[c][e]);
+                db[c][e] += d;
+                g[c][e] = d * wv[c][e];
+                s1 += g[c][e];
+                s2 = fmaf(g[c][e], u[c][e], s2);
+            }
+        }
+        const float m1 = warp_sum(s1) * inv_n, m2 = warp_sum(s2) * inv_n;
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) {
+            const int col = (c * 32 + lane) * VEC;
+            if (col >= a.width) continue;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) g[c][e] = r * (g[c][e] - m1 - u[c][e] * m2);
+            store_vec<T, VEC>(dx + row * a.dx_stride + col, g[c]);
+        }
+    }
+    // the block's warps added up, in order
+    float *out = a.partial + (int64_t)blockIdx.x * 2 * a.width;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) {
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) part[warp][lane * VEC + e] = k ? db[c][e] : dw[c][e];
+            __syncthreads();
+            for (int i = threadIdx.x; i < 32 * VEC; i += kRowWarps * 32) {
+                const int col = c * 32 * VEC + i;
+                if (col >= a.width) continue;
+                float t = 0.f;
+#pragma unroll
+                for (int w = 0; w < kRowWarps; ++w) t += part[w][i];
+                out[k * a.width + col] = t;
+            }
+        }
 }
 
 // dweight and dbias: the sum over blocks of their partial sums.  32 columns
@@ -218,24 +383,58 @@ bool wide(const NormArgs &a) {
 
 template <typename T, typename W, int VEC, int TPR, int NCH>
 cudaError_t forward_as(const NormArgs &a, cudaStream_t st) {
-    constexpr int rows = TPR >= 128 ? 1 : 128 / TPR;
-    k_norm_forward<T, W, VEC, TPR, NCH>
-        <<<(unsigned)ceil_div(a.rows, rows), TPR > 128 ? TPR : 128, 0, st>>>(a);
+    k_norm_forward<T, W, VEC, TPR, NCH><<<(unsigned)a.rows, TPR, 0, st>>>(a);
     return cudaGetLastError();
+}
+
+constexpr int kMaxBlocks = 152 * 4;
+constexpr int kRowsWidth = 1024;   // widest row of the row-walking kernels
+
+template <typename T, typename W, int VEC, int NCH>
+cudaError_t forward_rows(const NormArgs &a, cudaStream_t st) {
+    k_norm_forward_rows<T, W, VEC, NCH><<<(unsigned)ceil_div(a.rows, kRowWarps), kRowWarps * 32, 0, st>>>(a);
+    return cudaGetLastError();
+}
+template <typename T, typename W, int VEC, int NCH>
+cudaError_t backward_rows(const NormArgs &a, int blocks, cudaStream_t st) {
+    k_norm_backward_rows<T, W, VEC, NCH><<<blocks, kRowWarps * 32, 0, st>>>(a);
+    return cudaGetLastError();
+}
+// chunks of a lane, rounded up to an instantiated number
+template <int VEC, typename F>
+cudaError_t by_chunks(int width, F f) {
+    const int n = (int)ceil_div(width, 32 * VEC);
+    if constexpr (VEC == 8) {
+        if (n <= 1) return f(std::integral_constant<int, 1>{});
+        if (n == 2) return f(std::integral_constant<int, 2>{});
+        if (n == 3) return f(std::integral_constant<int, 3>{});
+        return f(std::integral_constant<int, 4>{});
+    } else {
+        static_assert(VEC == 4, "");
+        if (n <= 2) return f(std::integral_constant<int, 2>{});
+        if (n <= 4) return f(std::integral_constant<int, 4>{});
+        if (n <= 6) return f(std::integral_constant<int, 6>{});
+        return f(std::integral_constant<int, 8>{});
+    }
 }
 
 template <typename T, typename W>
 cudaError_t forward(const NormArgs &a, cudaStream_t st) {
     constexpr int V = 16 / sizeof(T);
+    if (a.width <= kRowsWidth) {
+        if (wide<T, W>(a))
+            return by_chunks<V>(a.width, [&](auto n) { return forward_rows<T, W, V, decltype(n)::value>(a, st); });
+        // (element by element, 32 a lane: 44 us at 20K x 1001, against 35 with
+        // 8 a thread in blocks)
+        if (a.width <= 128) return forward_rows<T, W, 1, 4>(a, st);
+        if (a.width <= 384) return forward_rows<T, W, 1, 12>(a, st);
+        return forward_as<T, W, 1, 128, 8>(a, st);
+    }
     if (wide<T, W>(a)) {
         const int chunks = a.width / V;
-        if (chunks <= 32) return forward_as<T, W, V, 32, 1>(a, st);
-        if (chunks <= 64) return forward_as<T, W, V, 32, 2>(a, st);
-        if (chunks <= 128) return forward_as<T, W, V, 32, 4>(a, st);
         if (chunks <= 512) return forward_as<T, W, V, 128, 4>(a, st);
         return forward_as<T, W, V, 512, V == 8 ? 4 : 8>(a, st);
     }
-    if (a.width <= 256) return forward_as<T, W, 1, 32, 8>(a, st);
     if (a.width <= 2048) return forward_as<T, W, 1, 128, 16>(a, st);
     return forward_as<T, W, 1, 512, 32>(a, st);
 }
@@ -246,11 +445,11 @@ cudaError_t backward_as(const NormArgs &a, int blocks, cudaStream_t st) {
     return cudaGetLastError();
 }
 
-constexpr int kMaxBlocks = 152 * 4;
-
+// Blocks of either backward kernel: enough for the SMs, and few partial sums
+// where there are few rows.
 int backward_blocks(int64_t rows, int width) {
-    (void)width;
-    return (int)(rows < kMaxBlocks ? rows : kMaxBlocks);
+    const int64_t n = width <= kRowsWidth ? ceil_div(rows, kRowWarps) : rows;
+    return (int)(n < kMaxBlocks ? n : kMaxBlocks);
 }
 
 template <typename T, typename W>
@@ -259,17 +458,17 @@ cudaError_t backward(const NormArgs &a, cudaStream_t st) {
     const int blocks = backward_blocks(a.rows, a.width);
     cudaError_t e = cudaSuccess;
     if (blocks > 0) {
-        if (wide<T, W>(a)) {
+        if (a.width <= kRowsWidth && wide<T, W>(a)) {
+            e = by_chunks<V>(a.width, [&](auto n) { return backward_rows<T, W, V, decltype(n)::value>(a, blocks, st); });
+        } else if (wide<T, W>(a)) {
             const int chunks = a.width / V;
-            if (chunks <= 32) e = backward_as<T, W, V, 32, 1, 4>(a, blocks, st);
-            else if (chunks <= 64) e = backward_as<T, W, V, 64, 1, 4>(a, blocks, st);
-            else if (chunks <= 128) e = backward_as<T, W, V, 128, 1, 4>(a, blocks, st);
-            else if (chunks <= 256) e = backward_as<T, W, V, 256, 1, 2>(a, blocks, st);
+            if (chunks <= 256) e = backward_as<T, W, V, 256, 1, 2>(a, blocks, st);
             else if (chunks <= 512) e = backward_as<T, W, V, 512, 1, 2>(a, blocks, st);
             else e = backward_as<T, W, V, 512, V == 8 ? 4 : 8, 1>(a, blocks, st);
         } else {
             if (a.width <= 128) e = backward_as<T, W, 1, 32, 4, 4>(a, blocks, st);
-            else if (a.width <= 1024) e = backward_as<T, W, 1, 128, 8, 2>(a, blocks, st);
+            else if (a.width <= 512) e = backward_as<T, W, 1, 128, 4, 4>(a, blocks, st);
+            else if (a.width <= 1024) e = backward_as<T, W, 1, 256, 4, 4>(a, blocks, st);
             else if (a.width <= 4096) e = backward_as<T, W, 1, 512, 8, 1>(a, blocks, st);
             else e = backward_as<T, W, 1, 1024, 16, 1>(a, blocks, st);
         }

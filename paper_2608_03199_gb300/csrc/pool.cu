@@ -5,7 +5,8 @@ namespace sieve {
 namespace enc {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;        // of the kernels that move tokens
+constexpr int kFinishThreads = 256;
 
 // Column sums of one tile of kPoolTile tokens of one document.  The block's
 // threads are `cols` column chunks of VEC elements by kThreads / cols strands
@@ -48,6 +49,7 @@ __global__ void __launch_bounds__(kThreads) k_pool_partial(const PoolArgs a, int
     }
 }
 
+template <int kThreads>
 __device__ __forceinline__ float block_sum(float v, float *smem) {
     v = warp_sum(v);
     __syncthreads();
@@ -60,8 +62,8 @@ __device__ __forceinline__ float block_sum(float v, float *smem) {
 }
 
 // A document's tiles added in order, its mean, norm and unit row.
-__global__ void __launch_bounds__(kThreads) k_pool_finish(const PoolArgs a) {
-    __shared__ float smem[kThreads / 32];
+__global__ void __launch_bounds__(kFinishThreads) k_pool_finish(const PoolArgs a) {
+    __shared__ float smem[kFinishThreads / 32];
     const int s = blockIdx.x;
     int first, len;
     doc_range(a.offsets, s, a.tokens, first, len);
@@ -69,16 +71,16 @@ __global__ void __launch_bounds__(kThreads) k_pool_finish(const PoolArgs a) {
     const float inv = len > 0 ? 1.f / (float)len : 0.f;
     float *row = a.rows + (int64_t)s * a.width;
     float q = 0.f;
-    for (int c = threadIdx.x; c < a.width; c += kThreads) {
+    for (int c = threadIdx.x; c < a.width; c += kFinishThreads) {
         float v = 0.f;
         for (int t = 0; t < tiles; ++t) v += a.partial[(int64_t)(t0 + t) * a.width + c];
         v *= inv;
         row[c] = v;
         q = fmaf(v, v, q);
     }
-    const float norm = sqrtf(block_sum(q, smem));
+    const float norm = sqrtf(block_sum<kFinishThreads>(q, smem));
     const float scale = norm > 0.f ? 1.f / norm : 0.f;
-    for (int c = threadIdx.x; c < a.width; c += kThreads) row[c] = norm != 0.f ? row[c] * scale : 0.f;
+    for (int c = threadIdx.x; c < a.width; c += kFinishThreads) row[c] = norm != 0.f ? row[c] * scale : 0.f;
     if (threadIdx.x == 0) a.norms[s] = norm;
 }
 
@@ -96,7 +98,7 @@ __global__ void __launch_bounds__(kThreads) k_pool_backward(const PoolArgs a) {
     const float *g = a.drows + (int64_t)s * a.width, *u = a.rows_in + (int64_t)s * a.width;
     float d = 0.f;
     for (int c = threadIdx.x; c < a.width; c += kThreads) d = fmaf(g[c], u[c], d);
-    d = block_sum(d, smem);
+    d = block_sum<kThreads>(d, smem);
     const float norm = a.norms_in[s];
     const float scale = norm != 0.f ? 1.f / norm / (float)len : 0.f;
     T *out = static_cast<T *>(a.dh) + (int64_t)(first + r0) * a.stride;
@@ -130,7 +132,7 @@ cudaError_t forward(const PoolArgs &a, cudaStream_t st) {
         cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
     }
-    k_pool_finish<<<(unsigned)a.nseq, kThreads, 0, st>>>(a);
+    k_pool_finish<<<(unsigned)a.nseq, kFinishThreads, 0, st>>>(a);
     return cudaGetLastError();
 }
 

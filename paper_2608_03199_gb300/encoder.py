@@ -65,7 +65,7 @@ def _on(device, stream, inputs):
     """Allocations inside belong to ``stream``; ``inputs`` allocated on
     another stream are kept until ``stream`` has passed the call."""
     with torch.cuda.device(device), torch.cuda.stream(stream):
-        yield C.c_void_p(stream.cuda_stream)
+        yield stream.cuda_stream
         for t in inputs:
             if t is not None:
                 t.record_stream(stream)
@@ -74,7 +74,7 @@ def _on(device, stream, inputs):
 @contextlib.contextmanager
 def _on_device(device):
     with torch.cuda.device(device):
-        yield C.c_void_p(torch.cuda.current_stream(device).cuda_stream)
+        yield torch.cuda.current_stream(device).cuda_stream
 
 
 class _Current:
@@ -95,9 +95,10 @@ class _Current:
 def _launch(device, stream, *inputs):
     if stream is not None:
         return _on(device, stream, inputs)
-    if device.index != torch.cuda.current_device():
+    index = device.index
+    if index != torch._C._cuda_getDevice():
         return _on_device(device)
-    return _Current(C.c_void_p(torch.cuda.current_stream(device).cuda_stream))
+    return _Current(torch._C._cuda_getCurrentRawStream(index))
 
 
 def _need(t, name, dtypes, ndim, device=None):
@@ -113,20 +114,27 @@ def _need(t, name, dtypes, ndim, device=None):
 
 
 def _rows(t, name, dtypes, device=None, shape=None):
-    """A matrix whose rows are contiguous (their stride is free); a
-    contiguous tensor of more dims counts as the matrix of its last axis."""
+    """(rows, width, row stride) of a matrix whose rows are contiguous (their
+    stride is free); a contiguous tensor of more dims counts as the matrix of
+    its last axis."""
     _need(t, name, dtypes, None, device)
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{name} must have shape {tuple(shape)}, has {tuple(t.shape)}")
-    if t.dim() != 2:
-        if t.dim() < 1 or not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous or a matrix")
-        t = t.view(-1, t.shape[-1])
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    size = t.shape
+    if shape is not None and size != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, has {tuple(size)}")
+    if len(size) < 1:
+        raise ValueError(f"{name} must be contiguous or a matrix")
+    width = size[-1]
+    if t.is_contiguous():
+        rows = size[0] if len(size) == 2 else t.numel() // width if width else 0
+        return rows, width, width
+    if len(size) != 2:
+        raise ValueError(f"{name} must be contiguous or a matrix")
+    rows, (across, along) = size[0], t.stride()
+    if width > 1 and along != 1:
         raise ValueError(f"{name}: the elements of a row must be contiguous")
-    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+    if rows > 1 and across < width:
         raise ValueError(f"{name}: rows must not overlap")
-    return t, max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+    return rows, width, across if rows > 1 else width
 
 
 def _vector(t, name, dtypes, n, device):
@@ -162,21 +170,23 @@ def layer_norm(x, weight, bias=None, eps=1e-5, out=None, stream=None):
     of more dims.  ``weight`` / ``bias``: [width] of x's type or fp32.
     Returns (y, mean, rstd); mean and rstd ([rows] fp32) are what
     :func:`layer_norm_backward` needs."""
-    x2, xs = _rows(x, "x", _FLOATS)
-    dev = x.device
-    rows, width = x2.shape
-    _vector(weight, "weight", (x.dtype, torch.float32), width, dev)
+    rows, width, xs = _rows(x, "x", _FLOATS)
+    dev, kind = x.device, x.dtype
+    _vector(weight, "weight", (kind, torch.float32), width, dev)
     if bias is not None:
         _vector(bias, "bias", (weight.dtype,), width, dev)
     with _launch(dev, stream, x, weight, bias, out) as s:
         if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=dev)
-        y2, ys = _rows(out, "out", (x.dtype,), dev, x.shape)
-        mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=dev).unbind(0)
-        _sieve._check(_sieve.lib().sieve_layer_norm(
-            x2.data_ptr(), xs, weight.data_ptr(), None if bias is None else bias.data_ptr(), rows, width,
-            DTYPES[x.dtype], DTYPES[weight.dtype], eps, y2.data_ptr(), ys, mean.data_ptr(), rstd.data_ptr(), s),
-            "sieve_layer_norm")
+            out, ys = torch.empty(x.shape, dtype=kind, device=dev), width
+        else:
+            ys = _rows(out, "out", (kind,), dev, x.shape)[2]
+        mean = torch.empty(rows, dtype=torch.float32, device=dev)
+        rstd = torch.empty(rows, dtype=torch.float32, device=dev)
+        rc = _sieve.lib().sieve_layer_norm(
+            x.data_ptr(), xs, weight.data_ptr(), None if bias is None else bias.data_ptr(), rows, width,
+            DTYPES[kind], DTYPES[weight.dtype], eps, out.data_ptr(), ys, mean.data_ptr(), rstd.data_ptr(), s)
+        if rc:
+            _sieve._check(rc, "sieve_layer_norm")
     return out, mean, rstd
 
 
@@ -184,10 +194,9 @@ def layer_norm_backward(dy, x, weight, mean, rstd, need_dbias=True, out=None, wo
     """Gradients of :func:`layer_norm`: (dx, dweight, dbias), dbias None
     without ``need_dbias`` (sieve_layer_norm_backward).  ``mean`` and ``rstd``
     are the forward call's; ``out`` receives dx and may be ``dy``."""
-    x2, xs = _rows(x, "x", _FLOATS)
+    rows, width, xs = _rows(x, "x", _FLOATS)
     dev = x.device
-    rows, width = x2.shape
-    dy2, dys = _rows(dy, "dy", (x.dtype,), dev, x.shape)
+    dys = _rows(dy, "dy", (x.dtype,), dev, x.shape)[2]
     _vector(weight, "weight", (x.dtype, torch.float32), width, dev)
     _vector(mean, "mean", (torch.float32,), rows, dev)
     _vector(rstd, "rstd", (torch.float32,), rows, dev)
@@ -198,13 +207,13 @@ def layer_norm_backward(dy, x, weight, mean, rstd, need_dbias=True, out=None, wo
     with _launch(dev, stream, dy, x, weight, mean, rstd, out) as s:
         if out is None:
             out = torch.empty(x.shape, dtype=x.dtype, device=dev)
-        dx2, dxs = _rows(out, "out", (x.dtype,), dev, x.shape)
+        dxs = _rows(out, "out", (x.dtype,), dev, x.shape)[2]
         dw = torch.empty(width, dtype=weight.dtype, device=dev)
         db = torch.empty(width, dtype=weight.dtype, device=dev) if need_dbias else None
         ws = _scratch(workspace, n.value, dev)
         _sieve._check(lib.sieve_layer_norm_backward(
-            dy2.data_ptr(), dys, x2.data_ptr(), xs, weight.data_ptr(), mean.data_ptr(), rstd.data_ptr(), rows,
-            width, DTYPES[x.dtype], DTYPES[weight.dtype], dx2.data_ptr(), dxs, dw.data_ptr(),
+            dy.data_ptr(), dys, x.data_ptr(), xs, weight.data_ptr(), mean.data_ptr(), rstd.data_ptr(), rows,
+            width, DTYPES[x.dtype], DTYPES[weight.dtype], out.data_ptr(), dxs, dw.data_ptr(),
             None if db is None else db.data_ptr(), ws.data_ptr(), ws.numel(), s), "sieve_layer_norm_backward")
     return out, dw, db
 
@@ -252,66 +261,69 @@ def _heads(t, name, dtypes, device, ndim=3):
 
 
 def _strides(t):
-    # an axis of one element has no stride that matters
-    ts = t.stride(-3) if t.shape[-3] > 1 else t.shape[-2] * t.shape[-1]
-    hs = t.stride(-2) if t.shape[-2] > 1 else t.shape[-1]
-    return ts, hs
+    """Token and head strides; an axis of one element has none that matters."""
+    *_, tokens, heads, dim = t.shape
+    *_, ts, hs, _ = t.stride()
+    return ts if tokens > 1 else heads * dim, hs if heads > 1 else dim
+
+
+def _new_strides(t):
+    """The same of [nseq][new][heads][dim], whose tokens must be evenly spaced."""
+    nseq, new, heads, dim = t.shape
+    across, ts, hs, _ = t.stride()
+    if nseq > 1 and new > 1 and across != new * ts:
+        raise ValueError("new tokens must be evenly spaced")
+    return across if new == 1 and nseq > 1 else ts if new > 1 else heads * dim, hs if heads > 1 else dim
 
 
 def _attention_args(q, k, v, offsets, q_offsets, table, buckets, causal, scale):
     _need(q, "q", _HALVES, None)
-    dev = q.device
-    if q.dim() not in (3, 4):
+    dev, kind = q.device, (q.dtype,)
+    ndim = q.dim()
+    if ndim != 3 and ndim != 4:
         raise ValueError("q must be [tokens][heads][dim] or [nseq][new][heads][dim]")
-    _heads(q, "q", _HALVES, dev, q.dim())
-    _heads(k, "k", (q.dtype,), dev)
-    _heads(v, "v", (q.dtype,), dev)
+    _heads(q, "q", kind, None, ndim)
+    _heads(k, "k", kind, dev)
+    _heads(v, "v", kind, dev)
     _offsets(offsets, "offsets", dev)
     nseq = offsets.shape[0] - 1
-    if k.shape != v.shape or k.shape[2] != q.shape[-1] or q.shape[-2] % max(k.shape[1], 1):
+    heads, dim = q.shape[-2:]
+    k_tokens, kv_heads, k_dim = k.shape
+    if v.shape != k.shape or k_dim != dim or heads % max(kv_heads, 1):
         raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not fit together")
-    a = AttentionArgsC()
-    if q.dim() == 4:
+    new, q_off = 0, None
+    if ndim == 4:
         if q_offsets is not None:
             raise ValueError("q of [nseq][new][heads][dim] has no q_offsets")
-        if q.shape[0] != nseq or q.shape[1] < 1 or (nseq > 1 and q.stride(0) != q.shape[1] * q.stride(1)):
-            raise ValueError("q must hold the same number of new tokens for every document, evenly spaced")
-        a.new_tokens = q.shape[1]
-        a.q_tokens = nseq * q.shape[1]
-        if q.shape[1] > 1 or nseq < 2:
-            a.q_token_stride, a.q_head_stride = _strides(q)
-        else:
-            a.q_token_stride, a.q_head_stride = q.stride(0), _strides(q)[1]
+        new = q.shape[1]
+        if q.shape[0] != nseq or new < 1:
+            raise ValueError("q must hold the same number of new tokens, at least one, for every document")
+        q_tokens = nseq * new
+        q_ts, q_hs = _new_strides(q)
     else:
-        a.q_tokens = q.shape[0]
-        a.q_token_stride, a.q_head_stride = _strides(q)
+        q_tokens = q.shape[0]
+        q_ts, q_hs = _strides(q)
         if q_offsets is not None:
-            a.q_offsets = _offsets(q_offsets, "q_offsets", dev, nseq + 1).data_ptr()
-        elif q.shape[0] != k.shape[0]:
+            q_off = _offsets(q_offsets, "q_offsets", dev, nseq + 1).data_ptr()
+        elif q_tokens != k_tokens:
             raise ValueError("q and k hold different numbers of tokens: pass q_offsets")
-    a.dtype = DTYPES[q.dtype]
-    a.heads, a.kv_heads, a.head_dim = q.shape[-2], k.shape[1], q.shape[-1]
-    a.nseq, a.k_tokens = nseq, k.shape[0]
-    a.causal = 1 if causal else 0
-    a.scale = a.head_dim ** -0.5 if scale is None else scale
-    a.k_offsets = offsets.data_ptr()
-    a.q, a.k, a.v = q.data_ptr(), k.data_ptr(), v.data_ptr()
-    a.k_token_stride, a.k_head_stride = _strides(k)
-    a.v_token_stride, a.v_head_stride = _strides(v)
     if (table is None) != (buckets is None):
         raise ValueError("table and buckets go together")
+    bias = (0, 0, None, None)
     if table is not None:
         _need(table, "table", (torch.float32,), 2, dev)
         _need(buckets, "buckets", (torch.int32,), 1, dev)
-        if table.shape[1] != a.heads or not table.is_contiguous():
-            raise ValueError(f"table must be contiguous [num_buckets][{a.heads}]")
+        if table.shape[1] != heads or not table.is_contiguous():
+            raise ValueError(f"table must be contiguous [num_buckets][{heads}]")
         if buckets.shape[0] % 2 != 1 or not buckets.is_contiguous():
             raise ValueError("buckets must be contiguous [2 reach + 1]")
         if table.shape[0] < 1:
             raise ValueError("table has no bucket")
-        a.num_buckets, a.reach = table.shape[0], buckets.shape[0] // 2
-        a.table, a.bucket_map = table.data_ptr(), buckets.data_ptr()
-    return a
+        bias = (table.shape[0], buckets.shape[0] // 2, table.data_ptr(), buckets.data_ptr())
+    return AttentionArgsC(DTYPES[q.dtype], heads, kv_heads, dim, nseq, q_tokens, k_tokens, new, 1 if causal else 0,
+                          dim ** -0.5 if scale is None and dim else scale or 0.0, bias[0], bias[1], 0, q_off,
+                          offsets.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), q_ts, q_hs, *_strides(k),
+                          *_strides(v), bias[2], bias[3])
 
 
 def attention(q, k, v, offsets, q_offsets=None, table=None, buckets=None, causal=False, scale=None, out=None,
@@ -337,7 +349,10 @@ def attention(q, k, v, offsets, q_offsets=None, table=None, buckets=None, causal
     dev = q.device
     lib = _sieve.lib()
     n = _size()
-    _sieve._check(lib.sieve_attention_workspace_size(C.byref(a), C.byref(n)), "sieve_attention_workspace_size")
+    ref = C.byref(a)
+    rc = lib.sieve_attention_workspace_size(ref, C.byref(n))
+    if rc:
+        _sieve._check(rc, "sieve_attention_workspace_size")
     with _launch(dev, stream, q, k, v, offsets, q_offsets, table, buckets, out) as s:
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=dev)
@@ -345,8 +360,9 @@ def attention(q, k, v, offsets, q_offsets=None, table=None, buckets=None, causal
             raise ValueError("out must be contiguous, of q's shape and type")
         lse = torch.empty((a.heads, a.q_tokens), dtype=torch.float32, device=dev)
         ws = _scratch(workspace, n.value, dev)
-        _sieve._check(lib.sieve_attention(C.byref(a), out.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel(), s),
-                      "sieve_attention")
+        rc = lib.sieve_attention(ref, out.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel(), s)
+        if rc:
+            _sieve._check(rc, "sieve_attention")
         if check and a.q_tokens:
             _sieve._check(encoder_status(ws, s), "sieve_attention (device status)")
     return out, lse
@@ -384,13 +400,7 @@ def attention_backward(dout, q, k, v, out, lse, offsets, q_offsets=None, table=N
             _heads(g, name, (q.dtype,), dev, t.dim())
             if g.shape != t.shape:
                 raise ValueError(f"{name} must have shape {tuple(t.shape)}")
-            if g.dim() == 4:
-                if g.shape[0] > 1 and g.stride(0) != g.shape[1] * g.stride(1):
-                    raise ValueError(f"{name}: tokens must be evenly spaced")
-                ts, hs = _strides(g)
-                strides += [g.stride(0) if g.shape[1] == 1 and g.shape[0] > 1 else ts, hs]
-            else:
-                strides += _strides(g)
+            strides += _new_strides(g) if g.dim() == 4 else _strides(g)
         dtable = None if table is None else torch.empty(table.shape, dtype=torch.float32, device=dev)
         ws = _scratch(workspace, n.value, dev)
         _sieve._check(lib.sieve_attention_backward(
@@ -406,7 +416,7 @@ def encoder_status(ws, stream) -> int:
     """The device status word of the last attention call that used the
     workspace tensor ``ws`` (sieve_encoder_status; synchronizes the stream)."""
     v = _i32(0)
-    handle = stream if isinstance(stream, C.c_void_p) else _sieve._stream(stream)
+    handle = stream if isinstance(stream, int) else _sieve._stream(stream)
     buf = ws.buf if isinstance(ws, _sieve.Workspace) else ws
     _sieve._check(_sieve.lib().sieve_encoder_status(buf.data_ptr(), buf.numel(), C.byref(v), handle),
                   "sieve_encoder_status")
@@ -420,12 +430,11 @@ def unit_pool(h, offsets, out=None, workspace=None, stream=None):
     :func:`search` takes (sieve_unit_pool).  Returns (rows [nseq][width],
     norms [nseq], the means' lengths); a document without tokens, or whose
     mean is zero, gets zeros."""
-    h2, hs = _rows(h, "h", _FLOATS)
+    tokens, width, hs = _rows(h, "h", _FLOATS)
     if h.dim() != 2:
         raise ValueError("h must be [tokens][width]")
     dev = h.device
     _offsets(offsets, "offsets", dev)
-    tokens, width = h2.shape
     nseq = offsets.shape[0] - 1
     lib = _sieve.lib()
     n = _size()
@@ -439,7 +448,7 @@ def unit_pool(h, offsets, out=None, workspace=None, stream=None):
             raise ValueError("out must be a contiguous float32 [nseq][width] tensor")
         norms = torch.empty(nseq, dtype=torch.float32, device=dev)
         ws = _scratch(workspace, n.value, dev)
-        _sieve._check(lib.sieve_unit_pool(h2.data_ptr(), hs, offsets.data_ptr(), tokens, nseq, width,
+        _sieve._check(lib.sieve_unit_pool(h.data_ptr(), hs, offsets.data_ptr(), tokens, nseq, width,
                                           DTYPES[h.dtype], out.data_ptr(), norms.data_ptr(), ws.data_ptr(),
                                           ws.numel(), s), "sieve_unit_pool")
     return out, norms
@@ -463,8 +472,8 @@ def unit_pool_backward(drows, rows, norms, offsets, tokens, dtype=torch.float32,
         drows = drows.contiguous()
         if out is None:
             out = torch.empty((tokens, width), dtype=dtype, device=dev)
-        dh, hs = _rows(out, "out", (dtype,), dev, torch.Size((tokens, width)))
+        hs = _rows(out, "out", (dtype,), dev, torch.Size((tokens, width)))[2]
         _sieve._check(_sieve.lib().sieve_unit_pool_backward(
             drows.data_ptr(), rows.data_ptr(), norms.data_ptr(), offsets.data_ptr(), tokens, nseq, width,
-            DTYPES[dtype], dh.data_ptr(), hs, s), "sieve_unit_pool_backward")
+            DTYPES[dtype], out.data_ptr(), hs, s), "sieve_unit_pool_backward")
     return out
