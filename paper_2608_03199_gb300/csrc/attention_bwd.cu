@@ -20,9 +20,8 @@
 // and the table's gradient: dS summed along diagonals (equal distances), in
 // fp32, before any rounding.
 //
-// In both, 16 warps (8 where shared memory has no room for 16 sets of sums by
-// distance) make P and dS, each for 32 lanes and its share of the columns; one
-// more loads, one more issues the products.  While the threads turn S into P
+// In both, 16 warps make P and dS, each for 32 lanes and 32 columns; one more
+// loads, one more issues the products.  While the threads turn S into P
 // the tensor cores work on dP and the product before, and the other way
 // round.  A block takes all of tensor memory, so one runs per SM; when it is
 // done it takes over a block that has not started, whose loads and first
@@ -503,10 +502,17 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
     }
 }
 
-template <typename T, int DP, bool BIAS, int kWarps>
-__global__ void __launch_bounds__((kWarps + 2) * 32, 1) k_attend_dkv(const __grid_constant__ BwdArgs f) {
-    constexpr int kCompute = kWarps * 32;
+// Sets of sums by distance: one for each group of columns and for its even and
+// its odd quarters of keys.  In one step two quarters of a set are 64 keys
+// apart and their 63 distances do not meet; the next step's sums wait for all
+// warps to be done with this one's (its P does), so an entry has one order.
+constexpr int kSums = 8;
+
+template <typename T, int DP, bool BIAS>
+__global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant__ BwdArgs f) {
+    constexpr int kWarps = 16, kCompute = kWarps * 32;
     constexpr int kGroups = Columns<kWarps>::kGroups, kCols = Columns<kWarps>::kCols, kChunks = Columns<kWarps>::kChunks;
+    static_assert(kSums == 2 * kGroups, "");
     constexpr int kB = DP / 64, kWalked = walked(DP), kKept = kept(DP);
     constexpr uint32_t kTileBytes = kB * kBlockBytes;
     constexpr uint32_t kSCol = 0, kDpCol = 128, kDvCol = 256, kDkCol = 384;   // P in S's place, dS in dP's
@@ -518,6 +524,7 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, 1) k_attend_dkv(const __gri
     __shared__ uint32_t tmem_slot;
     __shared__ int s_abort;
     __shared__ DkvWork s_work[kSlots];
+    __shared__ float s_far[kWarps][2];
     const sieve_attention_args &a = f.p.a;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = lane_id();
     const int share = a.heads / a.kv_heads;
@@ -528,7 +535,7 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, 1) k_attend_dkv(const __gri
     float *bias = reinterpret_cast<float *>(qd + kWalked * 2 * kTileBytes);
     // the bias by minus the distance (columns run that way)
     constexpr int kCopies = DP == 64 ? 4 : 1;
-    float *by_distance = bias + (BIAS ? bias_floats(a.reach, kCopies) : 0);   // [warps][entries]
+    float *by_distance = bias + (BIAS ? bias_floats(a.reach, kCopies) : 0);   // [kSums][entries]
 
     if (threadIdx.x == 0) {
         if (blockIdx.x == 0 && a.q_tokens == 0) f.p.ctl->status = 0;      // (else k_attend_delta did)
@@ -741,7 +748,8 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, 1) k_attend_dkv(const __gri
         const int r = quarter * 32 + lane, d = a.head_dim;
         const float c = a.scale * kLog2e;
         const uint32_t lane_base = tmem + ((uint32_t)(quarter * 32) << 16);
-        float *mine = by_distance + warp * f.entries;
+        // the group's sums of even or of odd quarters (see kSums)
+        float *mine = by_distance + (2 * group + (quarter & 1)) * f.entries;
         constexpr float kDown = 1.f / (float)(1 << kPShift<T>);
         Meeting meet{&meet_bar, 0};
         uint32_t step = 0;
@@ -760,15 +768,15 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, 1) k_attend_dkv(const __gri
                 const int head = w.hk * share + g;
                 float far_before = 0.f, far_after = 0.f;
                 if (BIAS) {
-                    // sums from zero, and another head's bias
+                    // another head's bias (the last head's was last read before
+                    // the warps met)
                     if (head != head_in_table) {
-                        if (!(ok = meet(wait))) break;
                         fill_bias<kCopies>(bias, a, head, -1, threadIdx.x, kCompute);
+                        if (head_in_table < 0)
+                            for (int e = threadIdx.x; e < kSums * f.entries; e += kCompute) by_distance[e] = 0.f;
                         head_in_table = head;
                         if (!(ok = meet(wait))) break;
                     }
-                    for (int e = lane; e < f.entries; e += 32) mine[e] = 0.f;
-                    __syncwarp();
                 }
 #pragma unroll 1
                 for (int qt = w.q_first; qt < w.q_first + w.q_tiles; ++qt, ++step) {
@@ -911,15 +919,22 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, 1) k_attend_dkv(const __gri
                     // the head's sums: the warps' added up, in order
                     const float before = warp_sum(far_before), after = warp_sum(far_after);
                     if (lane == 0) {
-                        mine[kPad] += before;
-                        mine[kPad + 2 * a.reach] += after;
+                        s_far[warp][0] = before;
+                        s_far[warp][1] = after;
                     }
                     if (!(ok = meet(wait))) break;
                     float *out = f.partial + ((int64_t)w.number * a.heads + head) * f.entries;
                     for (int e = threadIdx.x; e < f.entries; e += kCompute) {
                         float x = 0.f;
 #pragma unroll
-                        for (int k = 0; k < kWarps; ++k) x += by_distance[k * f.entries + e];
+                        for (int k = 0; k < kSums; ++k) {
+                            x += by_distance[k * f.entries + e];
+                            by_distance[k * f.entries + e] = 0.f;      // for the next head
+                        }
+                        if (e == kPad)
+                            for (int k = 0; k < kWarps; ++k) x += s_far[k][0];
+                        if (e == kPad + 2 * a.reach)
+                            for (int k = 0; k < kWarps; ++k) x += s_far[k][1];
                         out[e] = x;
                     }
                     if (!(ok = meet(wait))) break;
@@ -1022,17 +1037,6 @@ Layout layout_of(const sieve_attention_args &a) {
     return l;
 }
 
-template <typename T, int DP, bool BIAS, int kWarps>
-cudaError_t run_dkv(const BwdArgs &f, int64_t blocks, size_t smem, cudaStream_t st) {
-    auto dkv = k_attend_dkv<T, DP, BIAS, kWarps>;
-    cudaError_t e = cudaFuncSetAttribute(dkv, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-    dkv<<<(unsigned)blocks, (kWarps + 2) * 32, smem, st>>>(f);
-    return cudaGetLastError();
-}
-
-constexpr size_t kSharedLimit = 227 * 1024 - 4096;   // dynamic, beside the kernels' static part
-
 template <typename T, int DP, bool BIAS>
 cudaError_t run(const BwdArgs &f, const Layout &l, unsigned char *ws, cudaStream_t st) {
     const sieve_attention_args &a = f.p.a;
@@ -1049,14 +1053,12 @@ cudaError_t run(const BwdArgs &f, const Layout &l, unsigned char *ws, cudaStream
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
     }
     if (a.k_tokens > 0) {
-        // 16 warps where their sums by distance fit beside the tiles
-        auto smem = [&](int warps) {
-            return tiles + (BIAS ? (size_t)(bias_floats(a.reach, DP == 64 ? 4 : 1) + warps * f.entries) * 4 : 0);
-        };
-        const int64_t blocks = l.k_tiles * a.kv_heads;
-        if (!BIAS || smem(16) <= kSharedLimit) e = run_dkv<T, DP, BIAS, 16>(f, blocks, smem(16), st);
-        else e = run_dkv<T, DP, BIAS, BIAS && DP == 128 ? 8 : 16>(f, blocks, smem(8), st);
-        if (e != cudaSuccess) return e;
+        auto dkv = k_attend_dkv<T, DP, BIAS>;
+        const size_t smem =
+            tiles + (BIAS ? (size_t)(bias_floats(a.reach, DP == 64 ? 4 : 1) + kSums * f.entries) * 4 : 0);
+        if ((e = cudaFuncSetAttribute(dkv, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
+        dkv<<<(unsigned)(l.k_tiles * a.kv_heads), 18 * 32, smem, st>>>(f);
+        if ((e = cudaGetLastError()) != cudaSuccess) return e;
     }
     if (BIAS) {
         if (a.k_tokens == 0 || a.q_tokens == 0)

@@ -37,12 +37,14 @@ constexpr int kSoftmax = kSoftmaxWarps * 32;
 constexpr int kThreads = kSoftmax + 64;
 constexpr int kSlots = 2;     // the work in hand and the next
 constexpr int kHalf = kTile / 2;
-constexpr int kBlocksPerSm = 2;
 constexpr uint32_t kTmemCols = 256;
+constexpr int kBlocksPerSm = 2;
 constexpr float kRaise = 8.f;
 // Tiles of K and of V held at a time.  With one, the next K loads under the
 // softmax of this one and the next V under the scores of the next: that is
 // enough, and at 128 columns it lets two blocks share an SM.
+// (Over chunks of keys too: one block with three tiles of K and two of V took
+// half as long again as two blocks with one each.)
 __host__ __device__ constexpr int stages(int dp) { return dp == 64 ? 2 : 1; }
 
 // One block's work: some tiles of queries of one document, each against the
@@ -151,8 +153,8 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
         }
         for (int i = 0; i < kStages; ++i) {
             tc::mbar_init(&k_empty[i], 1);
-            tc::mbar_init(&v_empty[i], 1);
             tc::mbar_init(&k_full[i], 1);
+            tc::mbar_init(&v_empty[i], 1);
             tc::mbar_init(&v_full[i], 1);
         }
         tc::mbar_init(&s_full, 1);
@@ -458,20 +460,20 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
                             }
                         }
                     }
-                    if (!all) {
+                    float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                        for (int i = 0; i < 2; ++i)
+                    for (int i = 0; i < 2; ++i) {
+                        if (32 * i >= vis_any) continue;
+                        if (!all && !__all_sync(0xffffffffu, vis >= 32 * i + 32)) {
 #pragma unroll
                             for (int e = 0; e < 16; ++e) {
                                 if (32 * i + 2 * e >= vis) x[i][e].x = -INFINITY;
                                 if (32 * i + 2 * e + 1 >= vis) x[i][e].y = -INFINITY;
                             }
-                    }
-                    float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
+                        }
 #pragma unroll
                         for (int e = 0; e < 16; ++e) t4[e & 3] = fmax3f(t4[e & 3], x[i][e].x, x[i][e].y);
+                    }
                     float top = fmaxf(fmax3f(t4[0], t4[1], t4[2]), t4[3]);
                     // the row's maximum over both halves (without a bias the
                     // scale is not negative, so it can be applied after the
