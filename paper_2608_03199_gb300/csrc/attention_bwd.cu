@@ -35,6 +35,7 @@ namespace enc {
 namespace {
 
 constexpr int kSlots = 2;      // the work in hand and the next
+constexpr int kShort = 16;     // steps of work that is short
 
 // k_attend_dkv rounds P to 16 bits.  A long document's probabilities are small
 // and fp16 has no bits below 2^-24, so it takes 2^14 P there (P <= 1 up to the
@@ -203,21 +204,27 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
         int block = blockIdx.x, item = 0, kv_issued = 0, k_issued = 0, head0 = -1, head1 = -1;
         Blocks blocks{&s_answer, &steal_bar, 0, false};
         bool ok = true;
-        while (ok && block >= 0) {
-            const int head = block / f.q_numbers, t = block % f.q_numbers, hk = head / (a.heads / a.kv_heads);
-            int s, tile;
-            if (a.new_tokens > 0) {
-                s = t / f.doc_tiles;
-                tile = t % f.doc_tiles;
-            } else {
-                s = find_doc(a.q_offsets, (int)a.nseq, (int)a.q_tokens, kTile, t);
-                tile = t - first_tile(a.q_offsets, s, (int)a.q_tokens, kTile);
-            }
-            const Doc doc = doc_at(a, s);
-            const int tiles = (doc.nq + kTile - 1) / kTile;
-            if (tile >= 0 && tile < tiles) {
+        // the next work that has steps (head < 0: none is left); false: a wait
+        // gave up
+        auto fetch = [&](DqWork &w, bool own) {
+            while (true) {
+                if (!own && !blocks.next(wait, block)) return false;
+                own = false;
+                w.head = -1;
+                if (block < 0) return true;
+                const int head = block / f.q_numbers, t = block % f.q_numbers;
+                int s, tile;
+                if (a.new_tokens > 0) {
+                    s = t / f.doc_tiles;
+                    tile = t % f.doc_tiles;
+                } else {
+                    s = find_doc(a.q_offsets, (int)a.nseq, (int)a.q_tokens, kTile, t);
+                    tile = t - first_tile(a.q_offsets, s, (int)a.q_tokens, kTile);
+                }
+                const Doc doc = doc_at(a, s);
+                const int tiles = (doc.nq + kTile - 1) / kTile;
+                if (tile < 0 || tile >= tiles) continue;
                 tile = tiles - 1 - tile;               // the tiles that see most keys first
-                DqWork w;
                 w.head = head;
                 w.q_row = doc.q0;
                 w.row0 = tile * kTile;
@@ -228,59 +235,68 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
                 const int end = a.causal ? min(doc.nk, last + doc.nk - doc.nq) : doc.nk;
                 w.n = end > 0 ? (end + kTile - 1) / kTile : 0;
                 w.stats = (first_q_tile(f, s) + tile) * a.heads + head;
-                if (w.n == 0) {
-                    // no query of these sees a key
-                    const int pieces = a.head_dim / 8;
+                if (w.n > 0) return true;
+                // no query of these sees a key
+                const int pieces = a.head_dim / 8;
 #pragma unroll 1
-                    for (int i = lane; i < (last - w.row0) * pieces; i += 32)
-                        *reinterpret_cast<uint4 *>(static_cast<T *>(f.p.dq) + (int64_t)(doc.q0 + w.row0 + i / pieces) * f.p.dq_ts +
-                                                   head * f.p.dq_hs + i % pieces * 8) = make_uint4(0, 0, 0, 0);
-                } else {
-                    const int slot = item % kSlots, qs = item % kKept;
-                    if (item >= kSlots && !(ok = wait.warp(&work_empty[slot], (uint32_t)(item / kSlots - 1) & 1u))) break;
-                    // a slot has its own bias table, done with when the slot is
-                    if (BIAS && head != (slot ? head1 : head0)) {
-                        fill_bias(bias + slot * bias_set, a, head, 1, lane, 32);
-                        (slot ? head1 : head0) = head;
-                    }
-                    if (lane == 0) s_work[slot] = w;
-                    __syncwarp();
-                    if (lane == 0) tc::mbar_arrive(&work_full[slot]);
-                    if (!(ok = wait.warp(&q_empty[qs], ((uint32_t)(item / kKept) & 1u) ^ 1u))) break;
-                    if (elected()) {
-                        expect(&q_full[qs], 2 * kTileBytes + 2 * kTile * 4);
-                        tc::bulk_g2s(1u, s_stats[slot], f.stats + (int64_t)w.stats * 2 * kTile, 2 * kTile * 4, &q_full[qs]);
-                        for (int b = 0; b < kB; ++b) {
-                            tma_load(qd + qs * 2 * kTileBytes + b * kBlockBytes, &f.q, 64 * b, head, doc.q0 + w.row0, &q_full[qs]);
-                            tma_load(qd + (qs * 2 + 1) * kTileBytes + b * kBlockBytes, &f.dout, 64 * b, head, doc.q0 + w.row0,
-                                     &q_full[qs]);
-                        }
-                    }
-                    __syncwarp();
-                    ++item;
-#pragma unroll 1
-                    for (int j = 0; j < w.n; ++j, ++kv_issued) {
-                        const int ks = kv_issued % kKs, vs = kv_issued % kVs, row = doc.k0 + j * kTile;
-                        if (!(ok = wait.warp(&k_empty[ks], ((uint32_t)(kv_issued / kKs) & 1u) ^ 1u))) break;
-                        if (elected()) {
-                            expect(&k_full[ks], kTileBytes);
-                            for (int b = 0; b < kB; ++b)
-                                tma_load(k_tiles + ks * kTileBytes + b * kBlockBytes, &f.k, 64 * b, hk, row, &k_full[ks]);
-                        }
-                        __syncwarp();
-                        k_issued = kv_issued + 1;
-                        if (!(ok = wait.warp(&v_empty[vs], ((uint32_t)(kv_issued / kVs) & 1u) ^ 1u))) break;
-                        if (elected()) {
-                            expect(&v_full[vs], kTileBytes);
-                            for (int b = 0; b < kB; ++b)
-                                tma_load(v_tiles + vs * kTileBytes + b * kBlockBytes, &f.v, 64 * b, hk, row, &v_full[vs]);
-                        }
-                        __syncwarp();
-                    }
-                    if (!ok) break;
+                for (int i = lane; i < (last - w.row0) * pieces; i += 32)
+                    *reinterpret_cast<uint4 *>(static_cast<T *>(f.p.dq) + (int64_t)(doc.q0 + w.row0 + i / pieces) * f.p.dq_ts +
+                                               head * f.p.dq_hs + i % pieces * 8) = make_uint4(0, 0, 0, 0);
+            }
+        };
+        DqWork w;
+        ok = fetch(w, true);
+        while (ok && w.head >= 0) {
+            const int slot = item % kSlots, qs = item % kKept, head = w.head, hk = head / (a.heads / a.kv_heads);
+            if (item >= kSlots && !(ok = wait.warp(&work_empty[slot], (uint32_t)(item / kSlots - 1) & 1u))) break;
+            // a slot has its own bias table, done with when the slot is
+            if (BIAS && head != (slot ? head1 : head0)) {
+                fill_bias(bias + slot * bias_set, a, head, 1, lane, 32);
+                (slot ? head1 : head0) = head;
+            }
+            if (lane == 0) s_work[slot] = w;
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&work_full[slot]);
+            if (!(ok = wait.warp(&q_empty[qs], ((uint32_t)(item / kKept) & 1u) ^ 1u))) break;
+            if (elected()) {
+                expect(&q_full[qs], 2 * kTileBytes + 2 * kTile * 4);
+                tc::bulk_g2s(1u, s_stats[slot], f.stats + (int64_t)w.stats * 2 * kTile, 2 * kTile * 4, &q_full[qs]);
+                for (int b = 0; b < kB; ++b) {
+                    tma_load(qd + qs * 2 * kTileBytes + b * kBlockBytes, &f.q, 64 * b, head, w.q_row + w.row0, &q_full[qs]);
+                    tma_load(qd + (qs * 2 + 1) * kTileBytes + b * kBlockBytes, &f.dout, 64 * b, head, w.q_row + w.row0,
+                             &q_full[qs]);
                 }
             }
-            ok = blocks.next(wait, block);
+            __syncwarp();
+            ++item;
+            // The next work is looked for (a few thousand cycles) while the
+            // first steps of this one run.  Not so early for long work: others
+            // may be done sooner.
+            DqWork then;
+            const int when = w.n <= kShort ? min(w.n, 2) : w.n;
+#pragma unroll 1
+            for (int j = 0; j < w.n; ++j) {
+                const int ks = kv_issued % kKs, vs = kv_issued % kVs, row = w.k_row + j * kTile;
+                if (!(ok = wait.warp(&k_empty[ks], ((uint32_t)(kv_issued / kKs) & 1u) ^ 1u))) break;
+                if (elected()) {
+                    expect(&k_full[ks], kTileBytes);
+                    for (int b = 0; b < kB; ++b)
+                        tma_load(k_tiles + ks * kTileBytes + b * kBlockBytes, &f.k, 64 * b, hk, row, &k_full[ks]);
+                }
+                __syncwarp();
+                k_issued = kv_issued + 1;
+                if (!(ok = wait.warp(&v_empty[vs], ((uint32_t)(kv_issued / kVs) & 1u) ^ 1u))) break;
+                if (elected()) {
+                    expect(&v_full[vs], kTileBytes);
+                    for (int b = 0; b < kB; ++b)
+                        tma_load(v_tiles + vs * kTileBytes + b * kBlockBytes, &f.v, 64 * b, hk, row, &v_full[vs]);
+                }
+                __syncwarp();
+                ++kv_issued;
+                if (j + 1 == when && !(ok = fetch(then, false))) break;
+            }
+            if (!ok) break;
+            w = then;
         }
         if (ok) {
             const int slot = item % kSlots;
@@ -574,80 +590,95 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
         int block = blockIdx.x, item = 0, q_issued = 0;
         Blocks blocks{&s_answer, &steal_bar, 0, false};
         bool ok = true;
-        while (ok && block >= 0) {
-            DkvWork w;
-            w.hk = block / f.k_numbers;
-            w.number = block % f.k_numbers;
-            const int s = find_doc(a.k_offsets, (int)a.nseq, (int)a.k_tokens, kTile, w.number);
-            const int tile = w.number - first_tile(a.k_offsets, s, (int)a.k_tokens, kTile);
-            const Doc doc = doc_at(a, s);
-            w.key0 = tile * kTile;
-            const bool used = tile >= 0 && w.key0 < doc.nk;
-            // the first tile of queries that sees any of these keys
-            const int shift = doc.nk - doc.nq;
-            w.q_first = a.causal ? max(0, w.key0 - shift) / kTile : 0;
-            w.q_tiles = used ? max(0, (doc.nq + kTile - 1) / kTile - w.q_first) : 0;
-            if (w.q_tiles == 0) {
+        // the next work that has steps (hk < 0: none is left); false: a wait
+        // gave up
+        auto fetch = [&](DkvWork &w, bool own) {
+            while (true) {
+                if (!own && !blocks.next(wait, block)) return false;
+                own = false;
+                w.hk = -1;
+                if (block < 0) return true;
+                const int hk = block / f.k_numbers;
+                w.number = block % f.k_numbers;
+                const int s = find_doc(a.k_offsets, (int)a.nseq, (int)a.k_tokens, kTile, w.number);
+                const int tile = w.number - first_tile(a.k_offsets, s, (int)a.k_tokens, kTile);
+                const Doc doc = doc_at(a, s);
+                w.key0 = tile * kTile;
+                const bool used = tile >= 0 && w.key0 < doc.nk;
+                // the first tile of queries that sees any of these keys
+                w.q_first = a.causal ? max(0, w.key0 - (doc.nk - doc.nq)) / kTile : 0;
+                w.q_tiles = used ? max(0, (doc.nq + kTile - 1) / kTile - w.q_first) : 0;
+                if (w.q_tiles > 0) {
+                    w.hk = hk;
+                    w.k_row = doc.k0;
+                    w.nk = doc.nk;
+                    w.q_row = doc.q0;
+                    w.nq = doc.nq;
+                    w.q_number = first_q_tile(f, s);
+                    return true;
+                }
                 // no query sees these keys, or no document uses the number:
                 // nothing for the table, and zeros for the keys
 #pragma unroll 1
                 for (int e = lane; e < share * f.entries; e += 32)
-                    f.partial[((int64_t)w.number * a.heads + w.hk * share) * f.entries + e] = 0.f;
+                    f.partial[((int64_t)w.number * a.heads + hk * share) * f.entries + e] = 0.f;
                 const int pieces = a.head_dim / 8;
 #pragma unroll 1
                 for (int i = lane; used && i < min(kTile, doc.nk - w.key0) * pieces; i += 32) {
                     const int64_t row = doc.k0 + w.key0 + i / pieces;
-                    *reinterpret_cast<uint4 *>(static_cast<T *>(f.p.dk) + row * f.p.dk_ts + w.hk * f.p.dk_hs + i % pieces * 8) =
+                    *reinterpret_cast<uint4 *>(static_cast<T *>(f.p.dk) + row * f.p.dk_ts + hk * f.p.dk_hs + i % pieces * 8) =
                         make_uint4(0, 0, 0, 0);
-                    *reinterpret_cast<uint4 *>(static_cast<T *>(f.p.dv) + row * f.p.dv_ts + w.hk * f.p.dv_hs + i % pieces * 8) =
+                    *reinterpret_cast<uint4 *>(static_cast<T *>(f.p.dv) + row * f.p.dv_ts + hk * f.p.dv_hs + i % pieces * 8) =
                         make_uint4(0, 0, 0, 0);
                 }
-            } else {
-                w.k_row = doc.k0;
-                w.nk = doc.nk;
-                w.q_row = doc.q0;
-                w.nq = doc.nq;
-                w.q_number = first_q_tile(f, s);
-                const int slot = item % kSlots, ks = item % kKept;
-                if (item >= kSlots && !(ok = wait.warp(&work_empty[slot], (uint32_t)(item / kSlots - 1) & 1u))) break;
-                if (lane == 0) {
-                    s_work[slot] = w;
-                    tc::mbar_arrive(&work_full[slot]);
+            }
+        };
+        DkvWork w;
+        ok = fetch(w, true);
+        while (ok && w.hk >= 0) {
+            const int slot = item % kSlots, ks = item % kKept;
+            if (item >= kSlots && !(ok = wait.warp(&work_empty[slot], (uint32_t)(item / kSlots - 1) & 1u))) break;
+            if (lane == 0) {
+                s_work[slot] = w;
+                tc::mbar_arrive(&work_full[slot]);
+            }
+            if (!(ok = wait.warp(&kv_empty[ks], ((uint32_t)(item / kKept) & 1u) ^ 1u))) break;
+            if (elected()) {
+                expect(&kv_full[ks], 2 * kTileBytes);
+                for (int b = 0; b < kB; ++b) {
+                    tma_load(kv + ks * 2 * kTileBytes + b * kBlockBytes, &f.k, 64 * b, w.hk, w.k_row + w.key0, &kv_full[ks]);
+                    tma_load(kv + (ks * 2 + 1) * kTileBytes + b * kBlockBytes, &f.v, 64 * b, w.hk, w.k_row + w.key0, &kv_full[ks]);
                 }
-                if (!(ok = wait.warp(&kv_empty[ks], ((uint32_t)(item / kKept) & 1u) ^ 1u))) break;
+            }
+            __syncwarp();
+            ++item;
+            // (the next work is looked for as in k_attend_dq)
+            DkvWork then;
+            const int n = w.q_tiles * share, when = n <= kShort ? min(n, 2) : n;
+            int head = w.hk * share, qt = w.q_first;
+#pragma unroll 1
+            for (int i = 0; i < n; ++i) {
+                const int st = q_issued % kWalked, row = w.q_row + qt * kTile;
+                if (!(ok = wait.warp(&q_empty[st], ((uint32_t)(q_issued / kWalked) & 1u) ^ 1u))) break;
                 if (elected()) {
-                    expect(&kv_full[ks], 2 * kTileBytes);
+                    expect(&q_full[st], 2 * kTileBytes + 2 * kTile * 4);
                     for (int b = 0; b < kB; ++b) {
-                        tma_load(kv + ks * 2 * kTileBytes + b * kBlockBytes, &f.k, 64 * b, w.hk, doc.k0 + w.key0, &kv_full[ks]);
-                        tma_load(kv + (ks * 2 + 1) * kTileBytes + b * kBlockBytes, &f.v, 64 * b, w.hk, doc.k0 + w.key0,
-                                 &kv_full[ks]);
+                        tma_load(qd + st * 2 * kTileBytes + b * kBlockBytes, &f.q, 64 * b, head, row, &q_full[st]);
+                        tma_load(qd + (st * 2 + 1) * kTileBytes + b * kBlockBytes, &f.dout, 64 * b, head, row, &q_full[st]);
                     }
+                    tc::bulk_g2s(1u, s_stats[st], f.stats + ((int64_t)(w.q_number + qt) * a.heads + head) * 2 * kTile,
+                                 2 * kTile * 4, &q_full[st]);
                 }
                 __syncwarp();
-                ++item;
-                int head = w.hk * share, qt = w.q_first;
-#pragma unroll 1
-                for (int i = 0; i < w.q_tiles * share; ++i, ++q_issued) {
-                    const int st = q_issued % kWalked, row = doc.q0 + qt * kTile;
-                    if (!(ok = wait.warp(&q_empty[st], ((uint32_t)(q_issued / kWalked) & 1u) ^ 1u))) break;
-                    if (elected()) {
-                        expect(&q_full[st], 2 * kTileBytes + 2 * kTile * 4);
-                        for (int b = 0; b < kB; ++b) {
-                            tma_load(qd + st * 2 * kTileBytes + b * kBlockBytes, &f.q, 64 * b, head, row, &q_full[st]);
-                            tma_load(qd + (st * 2 + 1) * kTileBytes + b * kBlockBytes, &f.dout, 64 * b, head, row, &q_full[st]);
-                        }
-                        tc::bulk_g2s(1u, s_stats[st], f.stats + ((int64_t)(w.q_number + qt) * a.heads + head) * 2 * kTile,
-                                     2 * kTile * 4, &q_full[st]);
-                    }
-                    __syncwarp();
-                    if (++qt == w.q_first + w.q_tiles) {
-                        qt = w.q_first;
-                        ++head;
-                    }
+                ++q_issued;
+                if (++qt == w.q_first + w.q_tiles) {
+                    qt = w.q_first;
+                    ++head;
                 }
-                if (!ok) break;
+                if (i + 1 == when && !(ok = fetch(then, false))) break;
             }
-            ok = blocks.next(wait, block);
+            if (!ok) break;
+            w = then;
         }
         if (ok) {
             const int slot = item % kSlots;
