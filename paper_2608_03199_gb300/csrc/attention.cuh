@@ -98,9 +98,7 @@ __device__ __forceinline__ void mma_groups(uint32_t d_tmem, uint32_t a_tmem, uin
 }
 
 // a value that is the same in the whole warp, made so for the compiler too:
-// control flow and operands that depend on it stay in uniform registers (a
-// product issued from others first moves every operand there; measured 2-3K
-// cycles a step)
+// control flow that depends on it does not diverge
 __device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 
 // one thread: a box of a map, and the bytes announced on `bar`
@@ -301,8 +299,7 @@ __device__ __forceinline__ void clear_rows(unsigned char *tile, int first, int b
 // A thread needs 32 consecutive entries, from a start that falls by one from
 // lane to lane.  So the table is kept four times, copy s shifted by s entries:
 // whatever its start, a lane reads it from one of them in aligned vectors of
-// four (8 shared-memory instructions for 32 entries; measured 1.5K cycles a
-// tile with single reads).  Copies lie 8 banks apart, and zero distance sits
+// four: 8 shared-memory instructions for 32 entries.  Copies lie 8 banks apart, and zero distance sits
 // at an index of 3 mod 4: then the 8 lanes of a phase, whose tiles start at
 // multiples of four, hit 32 different banks.
 constexpr int kPad = 64;

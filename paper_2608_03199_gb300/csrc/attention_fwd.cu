@@ -47,11 +47,11 @@ constexpr float kRaise = 8.f;
 // half as long again as two blocks with one each.)
 __host__ __device__ constexpr int stages(int dp) { return dp == 64 ? 2 : 1; }
 
-// One block's work: some tiles of queries of one document, each against the
-// document's keys (or a chunk of them).
+// One block's work: a tile of queries of one document against the document's
+// keys (or a chunk of them).
 struct Work {
-    int q_row, nq, tile_lo, tile_hi;   // first row of q, queries; tiles, walked from hi - 1 down
-    int k_row, k_first, k_end, nk;     // first row and key of the chunk, its end, the document's keys
+    int q_row, nq, query0;             // first row of q, queries, the tile's first query
+    int k_row, k_first, nk, n;         // first row and key of the chunk, the document's keys; key tiles
     int group, number;                 // heads, tile or chunk number; group < 0: no more work
     int table;                         // which bias table
 };
@@ -62,8 +62,7 @@ struct FwdArgs {
     int pack;            // heads of one key head in a tile (1: a tile is 128 queries of one head)
     int rows_per_doc;    // split: new_tokens * pack
     int chunk;           // split: keys per block
-    int doc_tiles;       // new_tokens > 0, not split: blocks of a document
-    int q_tiles;         // not split: tiles of queries per block
+    int doc_tiles;       // new_tokens > 0, not split: tiles of a document
     int numbers;         // tile or chunk numbers; blocks run over them head by head
     float *part_o;       // split: [chunk number][head groups][rows][head_dim]
     float2 *part_ml;     // split: [chunk number][head groups][rows]: maximum (base 2), sum
@@ -74,46 +73,40 @@ template <bool SPLIT>
 __device__ __forceinline__ bool find_work(const FwdArgs &f, int t, Work &w) {
     const sieve_attention_args &a = f.p.a;
     Doc doc;
+    int k_end, last;                                   // of the tile's queries, the one that sees most
     if (SPLIT) {
         const int s = find_doc(a.k_offsets, (int)a.nseq, (int)a.k_tokens, f.chunk, t);
         doc = doc_at(a, s);
         w.k_first = (t - first_tile(a.k_offsets, s, (int)a.k_tokens, f.chunk)) * f.chunk;
         if (w.k_first < 0 || w.k_first >= doc.nk) return false;
-        w.k_end = min(doc.nk, w.k_first + f.chunk);
-        w.tile_lo = 0;
-        w.tile_hi = 1;
+        k_end = min(doc.nk, w.k_first + f.chunk);
+        w.query0 = 0;
+        last = doc.nq;
     } else {
-        int s, group;
+        int s, tile;
         if (a.new_tokens > 0) {
             s = t / f.doc_tiles;
-            group = t % f.doc_tiles;
+            tile = t % f.doc_tiles;
         } else {
-            const int step = kTile * f.q_tiles;
-            s = find_doc(a.q_offsets, (int)a.nseq, (int)a.q_tokens, step, t);
-            group = t - first_tile(a.q_offsets, s, (int)a.q_tokens, step);
+            s = find_doc(a.q_offsets, (int)a.nseq, (int)a.q_tokens, kTile, t);
+            tile = t - first_tile(a.q_offsets, s, (int)a.q_tokens, kTile);
         }
         doc = doc_at(a, s);
-        const int tiles = (int)ceil_div(doc.nq, kTile);
-        w.tile_hi = tiles - group * f.q_tiles;         // the tiles that see most keys first
-        if (group < 0 || w.tile_hi <= 0) return false;
-        w.tile_lo = max(0, w.tile_hi - f.q_tiles);
+        const int tiles = (doc.nq + kTile - 1) / kTile;
+        if (tile < 0 || tile >= tiles) return false;
+        w.query0 = (tiles - 1 - tile) * kTile;         // the tiles that see most keys first
         w.k_first = 0;
-        w.k_end = doc.nk;
+        k_end = doc.nk;
+        last = min(doc.nq, w.query0 + kTile);
     }
+    if (a.causal) k_end = min(k_end, last + doc.nk - doc.nq);
+    w.n = k_end > w.k_first ? (k_end - w.k_first + kTile - 1) / kTile : 0;
     w.number = t;
     w.q_row = doc.q0;
     w.nq = doc.nq;
     w.k_row = doc.k0 + w.k_first;
     w.nk = doc.nk;
     return true;
-}
-
-// key tiles of a tile of queries
-template <bool SPLIT>
-__device__ __forceinline__ int key_tiles(const Work &w, int causal, int tile) {
-    int end = w.k_end;
-    if (causal) end = min(end, (SPLIT ? w.nq : min(w.nq, (tile + 1) * kTile)) + w.nk - w.nq);
-    return end > w.k_first ? (end - w.k_first + kTile - 1) / kTile : 0;
 }
 
 template <typename T, int DP, bool BIAS, bool SPLIT>
@@ -193,9 +186,9 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
             w.group = block / f.numbers;
             const int head0 = w.group * f.pack, hk = head0 / share;
             const bool found = find_work<SPLIT>(f, block % f.numbers, w);
-            if (found && key_tiles<SPLIT>(w, a.causal, w.tile_hi - 1) == 0) {
+            if (found && w.n == 0) {
                 // no query of these sees a key
-                const int first = w.tile_lo * kTile, last = min(w.nq, w.tile_hi * kTile);
+                const int first = w.query0, last = min(w.nq, w.query0 + kTile);
                 if (SPLIT) {
                     for (int r = lane; r < f.rows_per_doc; r += 32)
                         f.part_ml[((int64_t)w.number * (a.heads / f.pack) + w.group) * f.rows_per_doc + r] =
@@ -226,54 +219,45 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(&work_full[slot]);
                 ++item;
+                const int qs = q_issued % kQStages;
+                if (!(ok = wait.warp(&q_empty[qs], ((uint32_t)(q_issued / kQStages) & 1u) ^ 1u))) break;
+                if (elected()) {
+                    expect(&q_full[qs], kB * 128u * (uint32_t)(f.pack * (kTile / f.pack)));
+                    for (int b = 0; b < kB; ++b)
+                        tma_load(q_tiles + qs * kTileBytes + b * kBlockBytes, &f.q, 64 * b, head0, w.q_row + w.query0,
+                                 &q_full[qs]);
+                }
+                __syncwarp();
+                ++q_issued;
                 // with two stages the values of a step are loaded after the
                 // keys of the next: their place is free later
-                int tile = w.tile_hi - 1, n = key_tiles<SPLIT>(w, a.causal, tile), j = 0, v_row = -1;
+                constexpr int kBehind = kStages - 1;
 #pragma unroll 1
-                while (true) {
-                    int row = -1;
-                    if (n > 0) {
-                        if (j == 0) {
-                            const int st = q_issued % kQStages;
-                            if (!(ok = wait.warp(&q_empty[st], ((uint32_t)(q_issued / kQStages) & 1u) ^ 1u))) break;
-                            if (elected()) {
-                                expect(&q_full[st], kB * 128u * (uint32_t)(f.pack * (kTile / f.pack)));
-                                for (int b = 0; b < kB; ++b)
-                                    tma_load(q_tiles + st * kTileBytes + b * kBlockBytes, &f.q, 64 * b, head0,
-                                             w.q_row + tile * kTile, &q_full[st]);
-                            }
-                            __syncwarp();
-                            ++q_issued;
-                        }
+                for (int j = 0; j < w.n + kBehind; ++j) {
+                    if (j < w.n) {
                         const int st = k_issued % kStages;
-                        row = w.k_row + j * kTile;
                         if (!(ok = wait.warp(&k_empty[st], ((uint32_t)(k_issued / kStages) & 1u) ^ 1u))) break;
                         if (elected()) {
                             expect(&k_full[st], kTileBytes);
                             for (int b = 0; b < kB; ++b)
-                                tma_load(k_tiles + st * kTileBytes + b * kBlockBytes, &f.k, 64 * b, hk, row, &k_full[st]);
+                                tma_load(k_tiles + st * kTileBytes + b * kBlockBytes, &f.k, 64 * b, hk, w.k_row + j * kTile,
+                                         &k_full[st]);
                         }
                         __syncwarp();
                         ++k_issued;
-                        if (++j == n) {
-                            j = n = 0;
-                            if (--tile >= w.tile_lo) n = key_tiles<SPLIT>(w, a.causal, tile);
-                        }
                     }
-                    if (kStages == 1) v_row = row;
-                    if (v_row >= 0) {
+                    if (j >= kBehind) {
                         const int st = v_issued % kStages;
                         if (!(ok = wait.warp(&v_empty[st], ((uint32_t)(v_issued / kStages) & 1u) ^ 1u))) break;
                         if (elected()) {
                             expect(&v_full[st], kTileBytes);
                             for (int b = 0; b < kB; ++b)
-                                tma_load(v_tiles + st * kTileBytes + b * kBlockBytes, &f.v, 64 * b, hk, v_row, &v_full[st]);
+                                tma_load(v_tiles + st * kTileBytes + b * kBlockBytes, &f.v, 64 * b, hk,
+                                         w.k_row + (j - kBehind) * kTile, &v_full[st]);
                         }
                         __syncwarp();
                         ++v_issued;
                     }
-                    if (row < 0) break;
-                    v_row = row;
                 }
                 if (!ok) break;
             }
@@ -302,67 +286,53 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
         // ---------------- products ----------------
         constexpr uint32_t id_o = idesc<T>(DP, true), id_s = idesc<T>(kTile, false);
         const uint64_t q0 = desc_k(q_tiles), k0 = desc_k(k_tiles), v0 = desc_mn(v_tiles);
-        uint32_t step = 0, q_used = 0;
+        uint32_t step = 0;
         bool ok = true;
         for (int item = 0; ok; ++item) {
             const int slot = item % kSlots;
             if (!(ok = wait.warp(&work_full[slot], (uint32_t)(item / kSlots) & 1u))) break;
             const Work &w = s_work[slot];
             if (uniform(w.group) < 0) break;
-            const int lo = uniform(w.tile_lo), keys = uniform(w.nk - w.k_first);
-            int tile = uniform(w.tile_hi) - 1, n = uniform(key_tiles<SPLIT>(w, a.causal, tile)), j = 0;
-            // (tile, j of n): the step whose scores are next; `key`: the
-            // first key of the one whose P is
-            int key = 0;
-            bool first = true;                          // no P yet
+            const int n = uniform(w.n), keys = uniform(w.nk - w.k_first), qs = item % kQStages;
+            if (!(ok = wait.warp(&q_full[qs], (uint32_t)(item / kQStages) & 1u))) break;
+            // round j: the scores of step j + 1 and the product with P of step
+            // j.  With P apart from S the scores come first (as soon as those
+            // of step j are in registers), else P has their place until its
+            // product.
 #pragma unroll 1
-            while (true) {
-                const bool scored = n > 0;
-                const int next_key = j * kTile;
-                // with P apart from S the next scores come before this step's
-                // product with P (as soon as this step's are in registers)
+            for (int j = -1; ok && j < n; ++j) {
                 for (int part = 0; part < 2; ++part) {
                     if ((part == 0) == kApart) {
-                        if (!scored) continue;
-                        const uint32_t i = step + (first ? 0u : 1u), st = i % kStages, qs = q_used % kQStages;
-                        if (kApart && !first && !(ok = wait.warp(&s_free, step & 1u))) break;
-                        if (j == 0 && !(ok = wait.warp(&q_full[qs], (q_used / kQStages) & 1u))) break;
+                        if (j + 1 == n) continue;
+                        const uint32_t i = step + (j < 0 ? 0u : 1u), st = i % kStages;
+                        if (kApart && j >= 0 && !(ok = wait.warp(&s_free, step & 1u))) break;
                         if (!(ok = wait.warp(&k_full[st], (i / kStages) & 1u))) break;
                         tc::fence_after_sync();
                         if (elected()) {
                             mma_kk<DP>(tmem, q0 + qs * (kTileBytes >> 4), k0 + st * (kTileBytes >> 4), id_s);
                             commit(&s_full);
                             commit(&k_empty[st]);
-                            if (j == n - 1) commit(&q_empty[qs]);
+                            if (j + 2 == n) commit(&q_empty[qs]);
                         }
                         __syncwarp();
-                        if (++j == n) {
-                            ++q_used;
-                            j = n = 0;
-                            if (--tile >= lo) n = uniform(key_tiles<SPLIT>(w, a.causal, tile));
-                        }
                     } else {
-                        if (first) continue;
+                        if (j < 0) continue;
                         const uint32_t st = step % kStages;
                         if (!(ok = wait.warp(&v_full[st], (step / kStages) & 1u))) break;
-                        if (keys - key < kTile) clear_rows(v_tiles + st * kTileBytes, keys - key, kB);
+                        // rows of another document: 0 x NaN
+                        if (keys - j * kTile < kTile) clear_rows(v_tiles + st * kTileBytes, keys - j * kTile, kB);
                         if (!(ok = wait.warp(&p_full, step & 1u))) break;
                         tc::fence_after_sync();
                         if (elected()) {
-                            mma_groups<kHalf, kPHalf>(tmem + kOCol, tmem + kPCol, v0 + st * (kTileBytes >> 4), id_o, key > 0);
+                            mma_groups<kHalf, kPHalf>(tmem + kOCol, tmem + kPCol, v0 + st * (kTileBytes >> 4), id_o, j > 0);
                             commit(&o_full);
                             commit(&v_empty[st]);
                         }
                         __syncwarp();
                     }
                 }
-                if (!ok) break;
-                if (!first) ++step;
-                first = false;
-                if (!scored) break;
-                key = next_key;
+                if (j >= 0) ++step;
             }
-            __syncwarp();
             if (ok && lane == 0) tc::mbar_arrive(&work_empty[slot]);
         }
         // every product issued ends before the block frees its memory (waited
@@ -388,165 +358,162 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
             const int head = w.group * f.pack + (SPLIT ? r % f.pack : 0);
             const float *table =
                 bias + (BIAS ? w.table * bias_set + (SPLIT ? r % f.pack * bias_floats(a.reach, kCopies) : 0) : 0);
+            const int n = w.n, qi = w.query0 + (SPLIT ? r / f.pack : r);     // query of the document
+            const bool live = SPLIT ? r < f.rows_per_doc : qi < w.nq;
+            // a warp without a live row only keeps the others company
+            const bool idle = SPLIT ? quarter * 32 >= f.rows_per_doc : w.query0 + quarter * 32 >= w.nq;
+            const int shift = w.nk - w.nq, place = qi + shift;
+            // keys that this row sees, counted from this half's first column
+            const int seen = (live ? (a.causal ? min(w.nk, place + 1) : w.nk) - w.k_first : 0) - half * kHalf;
+            float m = -INFINITY, l = 0.f;
 #pragma unroll 1
-            for (int tile = w.tile_hi - 1; ok && tile >= w.tile_lo; --tile) {
-                const int n = key_tiles<SPLIT>(w, a.causal, tile);
-                const int qi = tile * kTile + (SPLIT ? r / f.pack : r);     // query of the document
-                const bool live = SPLIT ? r < f.rows_per_doc : qi < w.nq;
-                // a warp without a live row only keeps the others company
-                const bool idle = SPLIT ? quarter * 32 >= f.rows_per_doc : tile * kTile + quarter * 32 >= w.nq;
-                const int shift = w.nk - w.nq, place = qi + shift;
-                // keys that this row sees, counted from this half's first column
-                const int seen = (live ? (a.causal ? min(w.nk, place + 1) : w.nk) - w.k_first : 0) - half * kHalf;
-                float m = -INFINITY, l = 0.f;
-#pragma unroll 1
-                for (int j = 0; j < n; ++j, ++step) {
-                    if (!(ok = wait.warp(&s_full, step & 1u))) break;
-                    tc::fence_after_sync();
-                    if (idle) {
-                        warp_arrive(&s_free);
-                        if (step > 0 && !(ok = wait.warp(&o_full, (step - 1) & 1u))) break;
-                        warp_arrive(&p_full);
-                        continue;
-                    }
-                    float2 x[2][16];
-                    {
-                        uint32_t raw[2][32];
-                        tc::tmem_ld32_issue(lane_base + half * kHalf, raw[0]);
-                        tc::tmem_ld32_issue(lane_base + half * kHalf + 32, raw[1]);
-                        tc::tmem_ld_wait(raw[0]);
-                        tc::tmem_ld_wait(raw[1]);
-#pragma unroll
-                        for (int i = 0; i < 2; ++i)
-#pragma unroll
-                            for (int e = 0; e < 16; ++e)
-                                x[i][e] = make_float2(__uint_as_float(raw[i][2 * e]), __uint_as_float(raw[i][2 * e + 1]));
-                    }
-                    tc::fence_before_sync();
+            for (int j = 0; j < n; ++j, ++step) {
+                if (!(ok = wait.warp(&s_full, step & 1u))) break;
+                tc::fence_after_sync();
+                if (idle) {
                     warp_arrive(&s_free);
-                    // columns of the half that this row sees; that any row of
-                    // the warp does
-                    const int vis = seen - j * kTile;
-                    const bool all = __all_sync(0xffffffffu, vis >= kHalf);
-                    const int vis_any = all ? kHalf : __reduce_max_sync(0xffffffffu, vis);
-                    if (BIAS) {
+                    if (step > 0 && !(ok = wait.warp(&o_full, (step - 1) & 1u))) break;
+                    warp_arrive(&p_full);
+                    continue;
+                }
+                float2 x[2][16];
+                {
+                    uint32_t raw[2][32];
+                    tc::tmem_ld32_issue(lane_base + half * kHalf, raw[0]);
+                    tc::tmem_ld32_issue(lane_base + half * kHalf + 32, raw[1]);
+                    tc::tmem_ld_wait(raw[0]);
+                    tc::tmem_ld_wait(raw[1]);
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            if (32 * i >= vis_any) continue;
-                            // distances d0 - place + 0 .. 31; the warp's places
-                            const int d0 = w.k_first + j * kTile + half * kHalf + 32 * i;
-                            const int place_lo = tile * kTile + (SPLIT ? quarter * 32 / f.pack : quarter * 32) + shift;
-                            const int place_hi =
-                                tile * kTile + (SPLIT ? (quarter * 32 + 31) / f.pack : quarter * 32 + 31) + shift;
-                            const bool after = d0 - place_hi >= a.reach, before = d0 + 31 - place_lo <= -a.reach;
-                            if (after || before) {
-                                const float b = table[bias_zero(a.reach) + (after ? a.reach : -a.reach)];
+                    for (int i = 0; i < 2; ++i)
 #pragma unroll
-                                for (int e = 0; e < 16; ++e)
-                                    x[i][e] = fma2(x[i][e], make_float2(c, c), make_float2(b, b));
-                            } else if (SPLIT) {
-                                const float *b = table + bias_zero(a.reach) + d0 - place;
-#pragma unroll
-                                for (int e = 0; e < 16; ++e)
-                                    x[i][e] = fma2(x[i][e], make_float2(c, c), make_float2(b[2 * e], b[2 * e + 1]));
-                            } else {
-                                const float4 *b = bias_at(table, a.reach, d0 - place);
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) {
-                                    const float4 v = b[e];
-                                    x[i][2 * e] = fma2(x[i][2 * e], make_float2(c, c), make_float2(v.x, v.y));
-                                    x[i][2 * e + 1] = fma2(x[i][2 * e + 1], make_float2(c, c), make_float2(v.z, v.w));
-                                }
-                            }
-                        }
-                    }
-                    float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                        for (int e = 0; e < 16; ++e)
+                            x[i][e] = make_float2(__uint_as_float(raw[i][2 * e]), __uint_as_float(raw[i][2 * e + 1]));
+                }
+                tc::fence_before_sync();
+                warp_arrive(&s_free);
+                // columns of the half that this row sees; that any row of
+                // the warp does
+                const int vis = seen - j * kTile;
+                const bool all = __all_sync(0xffffffffu, vis >= kHalf);
+                const int vis_any = all ? kHalf : __reduce_max_sync(0xffffffffu, vis);
+                if (BIAS) {
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         if (32 * i >= vis_any) continue;
-                        if (!all && !__all_sync(0xffffffffu, vis >= 32 * i + 32)) {
+                        // distances d0 - place + 0 .. 31; the warp's places
+                        const int d0 = w.k_first + j * kTile + half * kHalf + 32 * i;
+                        const int place_lo = w.query0 + (SPLIT ? quarter * 32 / f.pack : quarter * 32) + shift;
+                        const int place_hi =
+                            w.query0 + (SPLIT ? (quarter * 32 + 31) / f.pack : quarter * 32 + 31) + shift;
+                        const bool after = d0 - place_hi >= a.reach, before = d0 + 31 - place_lo <= -a.reach;
+                        if (after || before) {
+                            const float b = table[bias_zero(a.reach) + (after ? a.reach : -a.reach)];
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                if (32 * i + 2 * e >= vis) x[i][e].x = -INFINITY;
-                                if (32 * i + 2 * e + 1 >= vis) x[i][e].y = -INFINITY;
-                            }
-                        }
+                            for (int e = 0; e < 16; ++e)
+                                x[i][e] = fma2(x[i][e], make_float2(c, c), make_float2(b, b));
+                        } else if (SPLIT) {
+                            const float *b = table + bias_zero(a.reach) + d0 - place;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) t4[e & 3] = fmax3f(t4[e & 3], x[i][e].x, x[i][e].y);
-                    }
-                    float top = fmaxf(fmax3f(t4[0], t4[1], t4[2]), t4[3]);
-                    // the row's maximum over both halves (without a bias the
-                    // scale is not negative, so it can be applied after the
-                    // comparison)
-                    if (!BIAS) top *= c;
-                    s_top[meets & 1u][half][r] = top;
-                    warp_arrive(&pair_bar[quarter]);
-                    if (!(ok = wait.warp(&pair_bar[quarter], meets & 1u))) break;
-                    top = fmaxf(top, s_top[meets & 1u][half ^ 1][r]);
-                    ++meets;
-                    // the last step's product is done with P (and O) before
-                    // they are written
-                    if (step > 0 && !(ok = wait.warp(&o_full, (step - 1) & 1u))) break;
-                    tc::fence_after_sync();
-                    const bool raise = top > m + kRaise || m == -INFINITY;
-                    if (j == 0) {
-                        m = top;
-                    } else if (__any_sync(0xffffffffu, raise)) {
-                        const float old = m;
-                        if (raise) m = fmaxf(top, m);
-                        const float scale = raise && old != m ? exp2_approx(old - (m == -INFINITY ? 0.f : m)) : 1.f;
-                        l *= scale;
-#pragma unroll
-                        for (int i = 0; i < DP / 32; ++i) {
-                            uint32_t o[16];
-                            tmem_ld16(lane_base + kOCol + half * (DP / 2) + 16 * i, o);
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * scale);
-                            tc::tmem_st16(lane_base + kOCol + half * (DP / 2) + 16 * i, o);
-                        }
-                    }
-                    const float sub = m == -INFINITY ? 0.f : m;
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        uint32_t pk[16];
-                        if (32 * i >= vis_any) {
-                            // no row of the warp sees these; the product may
-                            // still read them
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) pk[e] = 0u;
+                            for (int e = 0; e < 16; ++e)
+                                x[i][e] = fma2(x[i][e], make_float2(c, c), make_float2(b[2 * e], b[2 * e + 1]));
                         } else {
-                            float2 s0 = make_float2(0.f, 0.f), s1 = s0;
+                            const float4 *b = bias_at(table, a.reach, d0 - place);
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                float2 y = BIAS ? add2(x[i][e], make_float2(-sub, -sub))
-                                                : fma2(x[i][e], make_float2(c, c), make_float2(-sub, -sub));
-                                y.x = exp2_approx(y.x);
-                                y.y = exp2_approx(y.y);
-                                if (e & 1) s1 = add2(s1, y);
-                                else s0 = add2(s0, y);
-                                pk[e] = pack2<T>(y.x, y.y);
+                            for (int e = 0; e < 8; ++e) {
+                                const float4 v = b[e];
+                                x[i][2 * e] = fma2(x[i][2 * e], make_float2(c, c), make_float2(v.x, v.y));
+                                x[i][2 * e + 1] = fma2(x[i][2 * e + 1], make_float2(c, c), make_float2(v.z, v.w));
                             }
-                            s0 = add2(s0, s1);
-                            l += s0.x + s0.y;
                         }
-                        tc::tmem_st16(p_at + 16 * i, pk);
                     }
-                    tc::tmem_st_wait();
-                    tc::fence_before_sync();
-                    warp_arrive(&p_full);
                 }
-                if (!ok) break;
-                if (idle) continue;
+                float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if (32 * i >= vis_any) continue;
+                    if (!all && !__all_sync(0xffffffffu, vis >= 32 * i + 32)) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            if (32 * i + 2 * e >= vis) x[i][e].x = -INFINITY;
+                            if (32 * i + 2 * e + 1 >= vis) x[i][e].y = -INFINITY;
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) t4[e & 3] = fmax3f(t4[e & 3], x[i][e].x, x[i][e].y);
+                }
+                float top = fmaxf(fmax3f(t4[0], t4[1], t4[2]), t4[3]);
+                // the row's maximum over both halves (without a bias the
+                // scale is not negative, so it can be applied after the
+                // comparison)
+                if (!BIAS) top *= c;
+                s_top[meets & 1u][half][r] = top;
+                warp_arrive(&pair_bar[quarter]);
+                if (!(ok = wait.warp(&pair_bar[quarter], meets & 1u))) break;
+                top = fmaxf(top, s_top[meets & 1u][half ^ 1][r]);
+                ++meets;
+                // the last step's product is done with P (and O) before
+                // they are written
+                if (step > 0 && !(ok = wait.warp(&o_full, (step - 1) & 1u))) break;
+                tc::fence_after_sync();
+                const bool raise = top > m + kRaise || m == -INFINITY;
+                if (j == 0) {
+                    m = top;
+                } else if (__any_sync(0xffffffffu, raise)) {
+                    const float old = m;
+                    if (raise) m = fmaxf(top, m);
+                    const float scale = raise && old != m ? exp2_approx(old - (m == -INFINITY ? 0.f : m)) : 1.f;
+                    l *= scale;
+#pragma unroll
+                    for (int i = 0; i < DP / 32; ++i) {
+                        uint32_t o[16];
+                        tmem_ld16(lane_base + kOCol + half * (DP / 2) + 16 * i, o);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * scale);
+                        tc::tmem_st16(lane_base + kOCol + half * (DP / 2) + 16 * i, o);
+                    }
+                }
+                const float sub = m == -INFINITY ? 0.f : m;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    uint32_t pk[16];
+                    if (32 * i >= vis_any) {
+                        // no row of the warp sees these; the product may
+                        // still read them
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) pk[e] = 0u;
+                    } else {
+                        float2 s0 = make_float2(0.f, 0.f), s1 = s0;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            float2 y = BIAS ? add2(x[i][e], make_float2(-sub, -sub))
+                                            : fma2(x[i][e], make_float2(c, c), make_float2(-sub, -sub));
+                            y.x = exp2_approx(y.x);
+                            y.y = exp2_approx(y.y);
+                            if (e & 1) s1 = add2(s1, y);
+                            else s0 = add2(s0, y);
+                            pk[e] = pack2<T>(y.x, y.y);
+                        }
+                        s0 = add2(s0, s1);
+                        l += s0.x + s0.y;
+                    }
+                    tc::tmem_st16(p_at + 16 * i, pk);
+                }
+                tc::tmem_st_wait();
+                tc::fence_before_sync();
+                warp_arrive(&p_full);
+            }
+            if (!ok) break;
+            if (!idle) {
                 // the row's sum over both halves, and the last product
                 s_top[meets & 1u][half][r] = l;
                 warp_arrive(&pair_bar[quarter]);
                 if (!(ok = wait.warp(&pair_bar[quarter], meets & 1u))) break;
                 l += s_top[meets & 1u][half ^ 1][r];
                 ++meets;
-                if (n > 0 && !(ok = wait.warp(&o_full, (step - 1) & 1u))) break;
+                if (!(ok = wait.warp(&o_full, (step - 1) & 1u))) break;
                 tc::fence_after_sync();
                 const int d = a.head_dim;
-                const bool none = n == 0 || l == 0.f;
+                const bool none = l == 0.f;
                 const float inv = SPLIT ? 1.f : rcp_approx(l);
                 const int64_t at = ((int64_t)w.number * (a.heads / f.pack) + w.group) * f.rows_per_doc + r;   // split
                 const int64_t row = w.q_row + qi;                                                             // not split
@@ -558,7 +525,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
                 for (int i = 0; i < DP / 64; ++i) {
                     const int col = half * (DP / 2) + 32 * i;
                     float o[32];
-                    tc::tmem_ld32(lane_base + kOCol + col, o);     // (whatever it holds where there was no product)
+                    tc::tmem_ld32(lane_base + kOCol + col, o);  
                     if (!live) continue;
 #pragma unroll
                     for (int e = 0; e < 32; ++e) o[e] = none ? 0.f : o[e] * inv;
@@ -611,18 +578,19 @@ __global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ Fwd
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     const float base = top == -INFINITY ? 0.f : top;
     float l = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
     for (int i = 0; i < n; ++i) {
         const int64_t at = slot(i);
         const float2 ml = f.part_ml[at];
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (4 * lane < d) o = *reinterpret_cast<const float4 *>(f.part_o + at * d + 4 * lane);
         const float e = exp2_approx(ml.x - base);
         l = fmaf(ml.y, e, l);
-        if (4 * lane < d && ml.y != 0.f) {
-            const float4 o = *reinterpret_cast<const float4 *>(f.part_o + at * d + 4 * lane);
-            acc[0] = fmaf(o.x, e, acc[0]);
-            acc[1] = fmaf(o.y, e, acc[1]);
-            acc[2] = fmaf(o.z, e, acc[2]);
-            acc[3] = fmaf(o.w, e, acc[3]);
-        }
+        if (ml.y == 0.f) continue;                 // (a chunk without visible keys has no sums)
+        acc[0] = fmaf(o.x, e, acc[0]);
+        acc[1] = fmaf(o.y, e, acc[1]);
+        acc[2] = fmaf(o.z, e, acc[2]);
+        acc[3] = fmaf(o.w, e, acc[3]);
     }
     if (lane == 0) f.p.lse[(int64_t)head * a.q_tokens + row] = l == 0.f ? -INFINITY : top * kLn2 + logf(l);
     if (4 * lane < d) {
@@ -638,7 +606,7 @@ __global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ Fwd
 // document and of a key head's heads fit one tile together.
 struct Shape {
     bool split;
-    int pack, chunk, q_tiles, doc_tiles;
+    int pack, chunk, doc_tiles;
     int64_t blocks, chunks;
     size_t smem;
 };
@@ -663,12 +631,11 @@ Shape shape_of(const sieve_attention_args &a) {
         s.chunks = doc_tiles(a.k_tokens, a.nseq, s.chunk);
         s.blocks = s.chunks * (a.heads / s.pack);
     } else {
-        // several tiles of queries to a block, where that leaves many blocks
-        for (s.q_tiles = 4;; s.q_tiles /= 2) {
-            s.doc_tiles = a.new_tokens > 0 ? (int)ceil_div(a.new_tokens, kTile * s.q_tiles) : 0;
-            s.blocks = (a.new_tokens > 0 ? a.nseq * s.doc_tiles : doc_tiles(a.q_tokens, a.nseq, kTile * s.q_tiles)) * a.heads;
-            if (s.q_tiles == 1 || s.blocks >= 16 * 152 * kBlocksPerSm) break;
-        }
+        // A block's work is one tile of queries.  (Up to four of a document
+        // took 393 us where this takes 383, on 512 documents of 0 to 512
+        // tokens and 12 heads of 64: the work is shared out less evenly.)
+        s.doc_tiles = a.new_tokens > 0 ? (int)ceil_div(a.new_tokens, kTile) : 0;
+        s.blocks = (a.new_tokens > 0 ? a.nseq * s.doc_tiles : doc_tiles(a.q_tokens, a.nseq, kTile)) * a.heads;
     }
     s.smem = 1024 + (size_t)(3 * stages(dp)) * (dp / 64) * kBlockBytes + (size_t)s.pack * bias_bytes;
     return s;
@@ -717,7 +684,6 @@ sieve_status launch_attention_forward(const AttentionArgs &p, void *ws, cudaStre
     f.rows_per_doc = a.new_tokens * s.pack;
     f.chunk = s.chunk;
     f.doc_tiles = s.doc_tiles;
-    f.q_tiles = s.q_tiles;
     f.numbers = (int)(s.blocks / (a.heads / s.pack));
     f.part_o = reinterpret_cast<float *>(static_cast<unsigned char *>(ws) + kCtlBytes);
     f.part_ml = reinterpret_cast<float2 *>(f.part_o + (s.split ? part_floats(a, s) * a.head_dim : 0));

@@ -449,7 +449,9 @@ cudaError_t backward_as(const NormArgs &a, int blocks, cudaStream_t st) {
 // where there are few rows.
 int backward_blocks(int64_t rows, int width) {
     const int64_t n = width <= kRowsWidth ? ceil_div(rows, kRowWarps) : rows;
-    return (int)(n < kMaxBlocks ? n : kMaxBlocks);
+    // (rows of 513 to 1,024: two blocks fit an SM)
+    const int64_t most = width > 512 && width <= kRowsWidth ? kMaxBlocks / 2 : kMaxBlocks;
+    return (int)(n < most ? n : most);
 }
 
 template <typename T, typename W>
