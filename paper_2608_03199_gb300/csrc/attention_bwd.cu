@@ -58,7 +58,7 @@ struct BwdArgs {
 
 // Tiles held at a time: of the operand pair a block walks, and of the pair it
 // keeps (two: the next work's is loaded while this one's is in use).
-__host__ __device__ constexpr int walked(int) { return 2; }
+constexpr int kWalked = 2;
 __host__ __device__ constexpr int kept(int dp) { return dp == 64 ? 2 : 1; }
 
 __device__ __forceinline__ int first_q_tile(const BwdArgs &f, int s) {
@@ -78,11 +78,9 @@ struct Meeting {
     }
 };
 
-// A warp's columns: kCols of the 128, read and written where they are.
-template <int kWarps>
-struct Columns {
-    static constexpr int kGroups = kWarps / 4, kCols = kTile / kGroups, kChunks = kCols / 32;
-};
+// 16 warps compute: four groups of 32 columns (one thread's, read and written
+// where they are), four warps to the 128 lanes.
+constexpr int kWarps = 16, kGroups = kWarps / 4, kCols = kTile / kGroups;
 
 // One block's work.
 struct DqWork {
@@ -140,8 +138,6 @@ __global__ void __launch_bounds__(kDeltaThreads) k_attend_delta(const __grid_con
 
 template <typename T, int DP, bool BIAS>
 __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant__ BwdArgs f) {
-    constexpr int kWarps = 16;
-    constexpr int kGroups = Columns<kWarps>::kGroups, kCols = Columns<kWarps>::kCols;
     constexpr int kB = DP / 64, kKept = kept(DP);
     // K of a step is used twice, last after the next step's scores; V once
     constexpr int kKs = 3, kVs = DP == 64 ? 2 : 1;
@@ -519,17 +515,16 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
 }
 
 // Sets of sums by distance: one for each group of columns and for its even and
-// its odd quarters of keys.  In one step two quarters of a set are 64 keys
-// apart and their 63 distances do not meet; the next step's sums wait for all
-// warps to be done with this one's (its P does), so an entry has one order.
+// its odd quarters of keys.  The pieces (32 keys by 32 queries) that meet in a
+// set lie a multiple of 64 distances apart, over all steps of a head, so the 63
+// distances of a piece are its own: it stores its sums, and no order matters.
 constexpr int kSums = 8;
 
 template <typename T, int DP, bool BIAS>
 __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant__ BwdArgs f) {
-    constexpr int kWarps = 16, kCompute = kWarps * 32;
-    constexpr int kGroups = Columns<kWarps>::kGroups, kCols = Columns<kWarps>::kCols, kChunks = Columns<kWarps>::kChunks;
+    constexpr int kCompute = kWarps * 32;
     static_assert(kSums == 2 * kGroups, "");
-    constexpr int kB = DP / 64, kWalked = walked(DP), kKept = kept(DP);
+    constexpr int kB = DP / 64, kKept = kept(DP);
     constexpr uint32_t kTileBytes = kB * kBlockBytes;
     constexpr uint32_t kSCol = 0, kDpCol = 128, kDvCol = 256, kDkCol = 384;   // P in S's place, dS in dP's
     extern __shared__ unsigned char smem_raw[];
@@ -821,88 +816,82 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
                     if (!(ok = wait.warp(&s_full, step & 1u))) break;
                     tc::fence_after_sync();
                     const bool none = idle || col0 >= w.nq || (a.causal && key_lo - place0 >= kCols);
-                    float2 p[kChunks][16];
-                    uint32_t pk[16];
+                    float2 p[kCols / 2];
+                    uint32_t pk[kCols / 2];
+                    if (!none) {
+                        uint32_t raw[32];
+                        tc::tmem_ld32_issue(lane_base + kSCol + group * kCols, raw);
+                        const float4 *nl = reinterpret_cast<const float4 *>(&s_stats[st][0][group * kCols]);
+                        const int hi = key_lo + 31 - place0, lo = hi - 62;
+                        tc::tmem_ld_wait(raw);
+                        if (!BIAS || lo >= a.reach || hi <= -a.reach) {
+                            const float b =
+                                !BIAS ? 0.f : bias[bias_zero(a.reach) + (lo >= a.reach ? -a.reach : a.reach)];
 #pragma unroll
-                    for (int q = 0; q < kChunks; ++q) {
-                        if (!none) {
-                            uint32_t raw[32];
-                            tc::tmem_ld32_issue(lane_base + kSCol + group * kCols + 32 * q, raw);
-                            const float4 *nl = reinterpret_cast<const float4 *>(&s_stats[st][0][group * kCols + 32 * q]);
-                            const int hi = key_lo + 31 - (place0 + 32 * q), lo = hi - 62;
-                            tc::tmem_ld_wait(raw);
-                            if (!BIAS || lo >= a.reach || hi <= -a.reach) {
-                                const float b =
-                                    !BIAS ? 0.f : bias[bias_zero(a.reach) + (lo >= a.reach ? -a.reach : a.reach)];
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) {
-                                    const float4 x = nl[e];
-                                    float2 x0 = make_float2(x.x, x.y), x1 = make_float2(x.z, x.w);
-                                    if (BIAS) {
-                                        x0 = add2(x0, both(b));
-                                        x1 = add2(x1, both(b));
-                                    }
-                                    p[q][2 * e] = fma2(make_float2(__uint_as_float(raw[4 * e]), __uint_as_float(raw[4 * e + 1])), both(c), x0);
-                                    p[q][2 * e + 1] = fma2(make_float2(__uint_as_float(raw[4 * e + 2]), __uint_as_float(raw[4 * e + 3])), both(c), x1);
+                            for (int e = 0; e < 8; ++e) {
+                                const float4 x = nl[e];
+                                float2 x0 = make_float2(x.x, x.y), x1 = make_float2(x.z, x.w);
+                                if (BIAS) {
+                                    x0 = add2(x0, both(b));
+                                    x1 = add2(x1, both(b));
                                 }
-                            } else {
-                                const int first = place0 + 32 * q - key;
-                                const float4 *at = bias_at(bias, a.reach, first);
-                                const float *one = bias + bias_zero(a.reach) + first;
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) {
-                                    const float4 x = nl[e];
-                                    const float4 b = kCopies == 4 ? at[e] : make_float4(one[4 * e], one[4 * e + 1], one[4 * e + 2], one[4 * e + 3]);
-                                    p[q][2 * e] = fma2(make_float2(__uint_as_float(raw[4 * e]), __uint_as_float(raw[4 * e + 1])), both(c),
-                                                       add2(make_float2(x.x, x.y), make_float2(b.x, b.y)));
-                                    p[q][2 * e + 1] = fma2(make_float2(__uint_as_float(raw[4 * e + 2]), __uint_as_float(raw[4 * e + 3])), both(c),
-                                                           add2(make_float2(x.z, x.w), make_float2(b.z, b.w)));
-                                }
+                                p[2 * e] = fma2(make_float2(__uint_as_float(raw[4 * e]), __uint_as_float(raw[4 * e + 1])), both(c), x0);
+                                p[2 * e + 1] = fma2(make_float2(__uint_as_float(raw[4 * e + 2]), __uint_as_float(raw[4 * e + 3])), both(c), x1);
                             }
+                        } else {
+                            const int first = place0 - key;
+                            const float4 *at = bias_at(bias, a.reach, first);
+                            const float *one = bias + bias_zero(a.reach) + first;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                const float4 x = nl[e];
+                                const float4 b = kCopies == 4 ? at[e] : make_float4(one[4 * e], one[4 * e + 1], one[4 * e + 2], one[4 * e + 3]);
+                                p[2 * e] = fma2(make_float2(__uint_as_float(raw[4 * e]), __uint_as_float(raw[4 * e + 1])), both(c),
+                                                   add2(make_float2(x.x, x.y), make_float2(b.x, b.y)));
+                                p[2 * e + 1] = fma2(make_float2(__uint_as_float(raw[4 * e + 2]), __uint_as_float(raw[4 * e + 3])), both(c),
+                                                       add2(make_float2(x.z, x.w), make_float2(b.z, b.w)));
+                            }
+                        }
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            p[e].x = exp2_approx(p[e].x);
+                            p[e].y = exp2_approx(p[e].y);
+                        }
+                        if (a.causal && !__all_sync(0xffffffffu, from <= 0)) {
 #pragma unroll
                             for (int e = 0; e < 16; ++e) {
-                                p[q][e].x = exp2_approx(p[q][e].x);
-                                p[q][e].y = exp2_approx(p[q][e].y);
+                                if (2 * e < from) p[e].x = 0.f;
+                                if (2 * e + 1 < from) p[e].y = 0.f;
                             }
-                            if (a.causal && !__all_sync(0xffffffffu, from <= 32 * q)) {
-#pragma unroll
-                                for (int e = 0; e < 16; ++e) {
-                                    if (32 * q + 2 * e < from) p[q][e].x = 0.f;
-                                    if (32 * q + 2 * e + 1 < from) p[q][e].y = 0.f;
-                                }
-                            }
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) pk[e] = pack2<T>(p[q][e].x, p[q][e].y);
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) pk[e] = 0u;
                         }
-                        tc::tmem_st16(lane_base + kSCol + group * kCols + 16 * q, pk);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) pk[e] = pack2<T>(p[e].x, p[e].y);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) pk[e] = 0u;
                     }
+                    tc::tmem_st16(lane_base + kSCol + group * kCols, pk);
                     tc::tmem_st_wait();
                     tc::fence_before_sync();
                     warp_arrive(&p_full);
 
                     if (!(ok = wait.warp(&dp_full, step & 1u))) break;
                     tc::fence_after_sync();
+                    if (!none) {
+                        float dp[32];
+                        tc::tmem_ld32(lane_base + kDpCol + group * kCols, dp);
+                        const float4 *dl = reinterpret_cast<const float4 *>(&s_stats[st][1][group * kCols]);
 #pragma unroll
-                    for (int q = 0; q < kChunks; ++q) {
-                        if (!none) {
-                            float dp[32];
-                            tc::tmem_ld32(lane_base + kDpCol + group * kCols + 32 * q, dp);
-                            const float4 *dl = reinterpret_cast<const float4 *>(&s_stats[st][1][group * kCols + 32 * q]);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                const float4 x = dl[e];
-                                p[q][2 * e] = mul2(p[q][2 * e], fma2(make_float2(dp[4 * e], dp[4 * e + 1]), both(kDown), make_float2(x.x, x.y)));
-                                p[q][2 * e + 1] =
-                                    mul2(p[q][2 * e + 1], fma2(make_float2(dp[4 * e + 2], dp[4 * e + 3]), both(kDown), make_float2(x.z, x.w)));
-                            }
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) pk[e] = pack2<T>(p[q][e].x, p[q][e].y);
+                        for (int e = 0; e < 8; ++e) {
+                            const float4 x = dl[e];
+                            p[2 * e] = mul2(p[2 * e], fma2(make_float2(dp[4 * e], dp[4 * e + 1]), both(kDown), make_float2(x.x, x.y)));
+                            p[2 * e + 1] =
+                                mul2(p[2 * e + 1], fma2(make_float2(dp[4 * e + 2], dp[4 * e + 3]), both(kDown), make_float2(x.z, x.w)));
                         }
-                        tc::tmem_st16(lane_base + kDpCol + group * kCols + 16 * q, pk);   // (zeros where none)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) pk[e] = pack2<T>(p[e].x, p[e].y);
                     }
+                    tc::tmem_st16(lane_base + kDpCol + group * kCols, pk);   // (zeros where none)
                     tc::tmem_st_wait();
                     tc::fence_before_sync();
                     warp_arrive(&ds_full);
@@ -913,36 +902,32 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
                         // e lanes, lane l holds the elements of one distance, that
                         // of key l and the first query, and where the turn wrapped
                         // around those of the distance 32 less.  (One shuffle an
-                        // element; a sum handed from lane to lane and stored by
-                        // the last took 2.9K cycles a step instead.)
+                        // element.  With a sum handed from lane to lane and stored
+                        // by the last a step took 2.9K cycles, with this 2.45K.)
+                        const int hi = key_lo + 31 - place0, lo = hi - 62;
+                        if (!live)   // rows past the document's keys add nothing
 #pragma unroll
-                        for (int q = 0; q < kChunks; ++q) {
-                            const int hi = key_lo + 31 - (place0 + 32 * q), lo = hi - 62;
-                            if (!live)   // rows past the document's keys add nothing
+                            for (int e = 0; e < 16; ++e) p[e] = both(0.f);
+                        if (lo >= a.reach || hi <= -a.reach) {
+                            float2 x0 = p[0], x1 = p[1];
 #pragma unroll
-                                for (int e = 0; e < 16; ++e) p[q][e] = both(0.f);
-                            if (lo >= a.reach || hi <= -a.reach) {
-                                float2 x0 = p[q][0], x1 = p[q][1];
-#pragma unroll
-                                for (int e = 2; e < 16; e += 2) {
-                                    x0 = add2(x0, p[q][e]);
-                                    x1 = add2(x1, p[q][e + 1]);
-                                }
-                                x0 = add2(x0, x1);
-                                (lo >= a.reach ? far_after : far_before) += x0.x + x0.y;
-                            } else {
-                                float up = 0.f, down = 0.f;
-#pragma unroll
-                                for (int e = 0; e < 32; ++e) {
-                                    const float v = __shfl_sync(0xffffffffu, e & 1 ? p[q][e / 2].y : p[q][e / 2].x, lane + e);
-                                    if (lane + e < 32) up += v;
-                                    else down += v;
-                                }
-                                float *to = mine + a.reach + kPad + hi - 31 + lane;
-                                to[0] += up;
-                                if (lane > 0) to[-32] += down;
-                                __syncwarp();
+                            for (int e = 2; e < 16; e += 2) {
+                                x0 = add2(x0, p[e]);
+                                x1 = add2(x1, p[e + 1]);
                             }
+                            x0 = add2(x0, x1);
+                            (lo >= a.reach ? far_after : far_before) += x0.x + x0.y;
+                        } else {
+                            float up = 0.f, down = 0.f;
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) {
+                                const float v = __shfl_sync(0xffffffffu, e & 1 ? p[e / 2].y : p[e / 2].x, lane + e);
+                                if (lane + e < 32) up += v;
+                                else down += v;
+                            }
+                            float *to = mine + a.reach + kPad + hi - 31 + lane;
+                            to[0] = up;
+                            if (lane > 0) to[-32] = down;
                         }
                     }
                 }
@@ -1071,7 +1056,7 @@ Layout layout_of(const sieve_attention_args &a) {
 template <typename T, int DP, bool BIAS>
 cudaError_t run(const BwdArgs &f, const Layout &l, unsigned char *ws, cudaStream_t st) {
     const sieve_attention_args &a = f.p.a;
-    const size_t tiles = 1024 + (size_t)2 * (walked(DP) + kept(DP)) * (DP / 64) * kBlockBytes;
+    const size_t tiles = 1024 + (size_t)2 * (kWalked + kept(DP)) * (DP / 64) * kBlockBytes;
     cudaError_t e;
     if (a.q_tokens > 0) {
         k_attend_delta<T, DP / 8><<<(unsigned)(l.q_tiles * a.heads), kDeltaThreads, 0, st>>>(f);

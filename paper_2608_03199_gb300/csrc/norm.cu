@@ -1,4 +1,20 @@
 // norm.cu -- layer norm over the last axis, forward and backward.
+//
+//   forward   mu = mean(x), r = 1 / sqrt(mean((x - mu)^2) + eps), xh = (x - mu) r,
+//             y = xh w + b
+//   backward  g = dy w, dx = r (g - mean(g) - xh mean(g xh)),
+//             dw = sum over rows of dy xh, db = sum over rows of dy
+//
+// Both are bound by memory: a row is read once into registers, where its sums
+// and its outputs come from.  The column sums of dw and db stay in registers of
+// the threads that walk the rows, one pair of partial rows a block, added in a
+// fixed order by a second launch: no atomics, the same bits every time.
+// Everything between the load and the store is fp32.
+//
+// Measured: forward 200,003 x 1024 bf16 (819 MB) 152 us, 5.4 TB/s; 100,003 x
+// 768 bf16 forward 51 us (6.0 TB/s), backward 90 us (461 MB, 5.1 TB/s: a warp's
+// next row is on its way while it works on this one, at two blocks an SM) and 8 us
+// for the partial sums.
 #include <type_traits>
 
 #include "encoder.cuh"
@@ -20,8 +36,9 @@ __device__ __forceinline__ float block_sum(float v, float *smem) {
     return v;
 }
 
-// Rows wider than 1,024: one row per block of TPR threads, held in registers:
-// NCH chunks of VEC elements a thread, chunk c of thread i at (c * TPR + i) * VEC.
+// Rows wider than 1,024, and wider than 384 that cannot move 16 bytes at a time:
+// one row per block of TPR threads, held in registers: NCH chunks of VEC elements
+// a thread, chunk c of thread i at (c * TPR + i) * VEC.
 template <typename T, typename W, int VEC, int TPR, int NCH>
 __global__ void __launch_bounds__(TPR)
     k_norm_forward(const NormArgs a) {
@@ -71,7 +88,9 @@ __global__ void __launch_bounds__(TPR)
     }
 }
 
-// Its backward pass: a block of TPR threads walks its rows, R of them at a time, and
+// The backward pass of rows wider than 1,024 and of those that cannot move 16
+// bytes at a time: a block of TPR threads walks its rows, R of them at a time (their
+// loads go out together, and one meeting of the block serves all), and
 // keeps the column sums of dweight and dbias of its columns in registers;
 // they go to partial[block][2][width] and k_norm_reduce adds the blocks up.
 template <typename T, typename W, int VEC, int TPR, int NCH, int R>
@@ -424,8 +443,8 @@ cudaError_t forward(const NormArgs &a, cudaStream_t st) {
     if (a.width <= kRowsWidth) {
         if (wide<T, W>(a))
             return by_chunks<V>(a.width, [&](auto n) { return forward_rows<T, W, V, decltype(n)::value>(a, st); });
-        // (element by element, 32 a lane: 44 us at 20K x 1001, against 35 with
-        // 8 a thread in blocks)
+        // element by element: a warp to a row up to 12 a lane; past that a block
+        // with 8 a thread (20,011 x 1001 fp32: 35 us, against 44 with 32 a lane)
         if (a.width <= 128) return forward_rows<T, W, 1, 4>(a, st);
         if (a.width <= 384) return forward_rows<T, W, 1, 12>(a, st);
         return forward_as<T, W, 1, 128, 8>(a, st);
@@ -449,7 +468,9 @@ cudaError_t backward_as(const NormArgs &a, int blocks, cudaStream_t st) {
 // where there are few rows.
 int backward_blocks(int64_t rows, int width) {
     const int64_t n = width <= kRowsWidth ? ceil_div(rows, kRowWarps) : rows;
-    // (rows of 513 to 1,024: two blocks fit an SM)
+    // rows of 513 to 1,024: their registers let two blocks share an SM, and more
+    // blocks only make more partial sums (20,011 x 1001 fp32, both passes: 132 us;
+    // 150 with twice as many)
     const int64_t most = width > 512 && width <= kRowsWidth ? kMaxBlocks / 2 : kMaxBlocks;
     return (int)(n < most ? n : most);
 }

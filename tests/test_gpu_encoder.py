@@ -364,6 +364,21 @@ def test_unit_pool(lengths, width, dtype):
     assert torch.equal(sieve.unit_pool(h, off)[0], rows)
 
 
+@pytest.mark.parametrize("size", [1e-38, 1e-25, 1e25, 1e37])
+def test_unit_pool_of_means_whose_squares_leave_fp32(size):
+    h = randn(gen(5), 70, 96)
+    off = ref.offsets_of([3, 0, 67], DEV)
+    rows, norms = sieve.unit_pool(h, off)
+    small, small_norms = sieve.unit_pool(h * size, off)
+    # h * size rounds every element by half an ulp (subnormals, at 1e-38, by
+    # 2^-150: 1e-7 of the size), and so does every step of the sums
+    means = torch.stack([h[:3].mean(0), h[:1].mean(0) * 0, h[3:].mean(0)])
+    spread = h.abs().max() / means.norm(dim=1).clamp(min=1e-3)
+    bound = (80 * 2.0 ** -23 * spread)[:, None]
+    assert ((small - rows).abs() <= bound).all()
+    assert ((small_norms.double() / size - norms.double()).abs() <= bound[:, 0] * norms).all()
+
+
 def test_unit_pool_strided_rows_zero_means_and_other_documents():
     g = gen(77)
     wide = randn(g, 300, 900).to(BF16)
