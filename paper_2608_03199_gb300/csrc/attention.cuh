@@ -264,6 +264,45 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
     return d;
 }
 
+// A warp's rows to memory.  A thread holds N chunks (16 bytes) of its own row;
+// turned among N neighbouring lanes, lane i of them holds chunk i of each of
+// their rows, and one store of the warp writes 32 / N rows' N chunks side by
+// side.  (Stored thread by thread, 16 bytes to each of 32 rows, 128 rows of dK
+// and dV took 3.8K cycles of a block.)
+template <int N>
+__device__ __forceinline__ void turn_rows(uint4 (&c)[N]) {
+#pragma unroll
+    for (int b = 1; b < N; b <<= 1) {
+        const bool up = lane_id() & b;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (i & b) continue;
+            uint32_t *x = reinterpret_cast<uint32_t *>(&c[i]), *y = reinterpret_cast<uint32_t *>(&c[i | b]);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? x[w] : y[w], b);
+                if (up) x[w] = got;
+                else y[w] = got;
+            }
+        }
+    }
+}
+// `out`: the warp's first row, at this thread's first column; `rows` of the 32
+// rows exist, `cols` columns from there on.
+template <typename T, int N>
+__device__ __forceinline__ void store_rows(T *out, int64_t stride, int rows, int cols, uint4 (&c)[N]) {
+    turn_rows(c);
+    const int at = (int)lane_id() % N, first = (int)lane_id() - at;
+    if (8 * at >= cols) return;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (first + i < rows) *reinterpret_cast<uint4 *>(out + (first + i) * stride + 8 * at) = c[i];
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack8(const float *v) {
+    return make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+}
+
 struct Doc {
     int q0, nq, k0, nk;   // first rows and lengths
 };

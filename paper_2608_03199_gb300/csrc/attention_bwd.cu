@@ -475,23 +475,22 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
             // (every thread's sum of dS arrived with its last dS)
             if (!(ok = wait.warp(&ds_full[(step - 1) & 1u], ((step - 1) >> 1) & 1u) && wait.warp(&dq_full, (uint32_t)item & 1u))) break;
             tc::fence_after_sync();
-            T *out = static_cast<T *>(f.p.dq) + row * f.p.dq_ts + w.head * f.p.dq_hs;
-            constexpr int kOut = DP / kGroups;       // 16 or 32 columns of dQ
+            if (!idle) {
+                constexpr int kOut = DP / kGroups;       // 16 or 32 columns of dQ
+                const int col = group * kOut;
+                uint4 c[kOut / 8];
 #pragma unroll
-            for (int i = 0; i < kOut / 16; ++i) {
-                const int col = group * kOut + 16 * i;
-                uint32_t o[16];
-                tmem_ld16(lane_base + kDqCol + col, o);
-                if (live)
+                for (int i = 0; i < kOut / 16; ++i) {
+                    uint32_t o[16];
+                    tmem_ld16(lane_base + kDqCol + col + 16 * i, o);
+                    float v[16];
 #pragma unroll
-                    for (int e = 0; e < 16; e += 8)
-                        if (col + e < d) {
-                            float v[8];
-#pragma unroll
-                            for (int u = 0; u < 8; ++u) v[u] = nl != -INFINITY ? __uint_as_float(o[e + u]) * a.scale : 0.f;
-                            *reinterpret_cast<uint4 *>(out + col + e) =
-                                make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
-                        }
+                    for (int e = 0; e < 16; ++e) v[e] = nl != -INFINITY ? __uint_as_float(o[e]) * a.scale : 0.f;
+                    c[2 * i] = pack8<T>(v);
+                    c[2 * i + 1] = pack8<T>(v + 8);
+                }
+                store_rows(static_cast<T *>(f.p.dq) + (row - lane) * f.p.dq_ts + w.head * f.p.dq_hs + col, f.p.dq_ts,
+                           w.nq - w.row0 - quarter * 32, d - col, c);
             }
             tc::fence_before_sync();
             if (BIAS && group == 0 && nl != -INFINITY) {
@@ -959,29 +958,24 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
             if (ok) ok = wait.warp(&acc_full, (uint32_t)item & 1u);
             if (!ok) break;
             tc::fence_after_sync();
-            const int64_t row = w.k_row + key;
+            const int64_t row = w.k_row + key_lo;
             // the groups' shares: of dV first, then of dK
             constexpr int kOut = 2 * DP / kGroups;
             const bool is_k = group >= kGroups / 2;
             const int col0 = group % (kGroups / 2) * kOut;
-            T *out = is_k ? static_cast<T *>(f.p.dk) + row * f.p.dk_ts + w.hk * f.p.dk_hs
-                          : static_cast<T *>(f.p.dv) + row * f.p.dv_ts + w.hk * f.p.dv_hs;
+            const int64_t stride = is_k ? f.p.dk_ts : f.p.dv_ts;
+            T *out = is_k ? static_cast<T *>(f.p.dk) + row * stride + w.hk * f.p.dk_hs
+                          : static_cast<T *>(f.p.dv) + row * stride + w.hk * f.p.dv_hs;
             const float scale = is_k ? a.scale : kDown;
 #pragma unroll
-            for (int i = 0; i < kOut / 16; ++i) {
-                const int col = col0 + 16 * i;
-                uint32_t o[16];
-                tmem_ld16(lane_base + (is_k ? kDkCol : kDvCol) + col, o);
-                if (live)
+            for (int i = 0; i < kOut / 32 && !idle; ++i) {
+                const int col = col0 + 32 * i;
+                float v[32];
+                tc::tmem_ld32(lane_base + (is_k ? kDkCol : kDvCol) + col, v);
 #pragma unroll
-                    for (int e = 0; e < 16; e += 8)
-                        if (col + e < d) {
-                            float v[8];
-#pragma unroll
-                            for (int u = 0; u < 8; ++u) v[u] = __uint_as_float(o[e + u]) * scale;
-                            *reinterpret_cast<uint4 *>(out + col + e) =
-                                make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
-                        }
+                for (int e = 0; e < 32; ++e) v[e] *= scale;
+                uint4 c[4] = {pack8<T>(v), pack8<T>(v + 8), pack8<T>(v + 16), pack8<T>(v + 24)};
+                store_rows(out + col, stride, w.nk - key_lo, d - col, c);
             }
             tc::fence_before_sync();
             __syncwarp();

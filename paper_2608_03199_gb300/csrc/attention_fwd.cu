@@ -525,24 +525,19 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
                 for (int i = 0; i < DP / 64; ++i) {
                     const int col = half * (DP / 2) + 32 * i;
                     float o[32];
-                    tc::tmem_ld32(lane_base + kOCol + col, o);  
-                    if (!live) continue;
+                    tc::tmem_ld32(lane_base + kOCol + col, o);
 #pragma unroll
                     for (int e = 0; e < 32; ++e) o[e] = none ? 0.f : o[e] * inv;
                     if (SPLIT) {
 #pragma unroll
                         for (int e = 0; e < 32; e += 4)
-                            if (col + e < d)
+                            if (live && col + e < d)
                                 *reinterpret_cast<float4 *>(f.part_o + at * d + col + e) =
                                     make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
                     } else {
-                        T *out = static_cast<T *>(f.p.out) + (row * a.heads + head) * d;
-#pragma unroll
-                        for (int e = 0; e < 32; e += 8)
-                            if (col + e < d)
-                                *reinterpret_cast<uint4 *>(out + col + e) =
-                                    make_uint4(pack2<T>(o[e], o[e + 1]), pack2<T>(o[e + 2], o[e + 3]),
-                                               pack2<T>(o[e + 4], o[e + 5]), pack2<T>(o[e + 6], o[e + 7]));
+                        uint4 p[4] = {pack8<T>(o), pack8<T>(o + 8), pack8<T>(o + 16), pack8<T>(o + 24)};
+                        store_rows(static_cast<T *>(f.p.out) + ((row - lane) * a.heads + head) * d + col,
+                                   (int64_t)a.heads * d, w.nq - qi + lane, d - col, p);
                     }
                 }
                 tc::fence_before_sync();   // O is read before the next tile's first product
