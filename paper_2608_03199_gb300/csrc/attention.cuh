@@ -222,11 +222,16 @@ struct Blocks {
     uint64_t *bar;
     uint32_t asked;
     bool asking;
-    // the next block's index in `block`, or -1; false: the wait gave up
-    __device__ __forceinline__ bool next(const Waiter &wait, int &block) {
+    // ask ahead (the answer is taken by next()): where the block at hand is
+    // short, else another may have been free for the next one sooner
+    __device__ __forceinline__ void ask() {
         if (elected()) steal_block(1u, answer, bar);
         __syncwarp();
         asking = true;
+    }
+    // the next block's index in `block`, or -1; false: the wait gave up
+    __device__ __forceinline__ bool next(const Waiter &wait, int &block) {
+        if (!asking) ask();
         if (!wait.warp(bar, asked & 1u)) return false;
         ++asked;
         asking = false;
@@ -306,17 +311,66 @@ __device__ __forceinline__ uint4 pack8(const float *v) {
 struct Doc {
     int q0, nq, k0, nk;   // first rows and lengths
 };
-__device__ __forceinline__ Doc doc_at(const sieve_attention_args &a, int s) {
-    Doc d;
-    doc_range(a.k_offsets, s, (int)a.k_tokens, d.k0, d.nk);
+// the queries of document s, where its keys are known (most often they are the
+// same rows)
+__device__ __forceinline__ void queries_of(const sieve_attention_args &a, int s, Doc &d) {
     if (a.new_tokens > 0) {
         d.q0 = s * a.new_tokens;
         d.nq = a.new_tokens;
+    } else if (a.q_offsets == a.k_offsets && a.q_tokens == a.k_tokens) {
+        d.q0 = d.k0;
+        d.nq = d.nk;
     } else {
         doc_range(a.q_offsets, s, (int)a.q_tokens, d.q0, d.nq);
     }
+}
+// and the other way round
+__device__ __forceinline__ void keys_of(const sieve_attention_args &a, int s, Doc &d) {
+    if (a.q_offsets == a.k_offsets && a.q_tokens == a.k_tokens) {
+        d.k0 = d.q0;
+        d.nk = d.nq;
+    } else {
+        doc_range(a.k_offsets, s, (int)a.k_tokens, d.k0, d.nk);
+    }
+}
+__device__ __forceinline__ Doc doc_at(const sieve_attention_args &a, int s) {
+    Doc d;
+    doc_range(a.k_offsets, s, (int)a.k_tokens, d.k0, d.nk);
+    queries_of(a, s, d);
     return d;
 }
+
+// The documents of rising tile numbers, for one warp (see find_doc): it keeps
+// where every 32nd of 1,024 documents starts, so that most numbers take one
+// dependent load, which brings the document's rows as well.  (A search from
+// nothing and the rows after it are five, and a block's finder took 5K to 8K
+// cycles for its next work.)
+struct DocFinder {
+    const int32_t *off;
+    int nseq, tokens;
+    int base, start;         // start: first number of document base + 32 * lane
+    __device__ __forceinline__ DocFinder(const int32_t *offsets, int64_t n, int64_t t)
+        : off(offsets), nseq((int)n), tokens((int)t), base(0), start(0x7fffffff) {}
+    // number t: its document, the document's first row and length, which of the
+    // document's tiles
+    __device__ __forceinline__ void operator()(int t, int &doc, int &row, int &len, int &tile) {
+        const int lane = lane_id();
+        if (t < __shfl_sync(0xffffffffu, start, 0) || t >= __shfl_sync(0xffffffffu, start, 31)) {
+            base = find_doc(off, nseq, tokens, kTile, t);
+            start = base + 32 * lane < nseq ? first_tile(off, base + 32 * lane, tokens, kTile) : 0x7fffffff;
+        }
+        // (max(): broken offsets find something in range)
+        const int from = base + 32 * max(31 - __clz((int)__ballot_sync(0xffffffffu, start <= t)), 0), d = from + lane;
+        const int a = min(max(__ldg(off + min(d, nseq)), 0), tokens);
+        const int b = min(max(__ldg(off + min(d + 1, nseq)), 0), tokens);
+        const int first = a / kTile + d;
+        const int k = max(31 - __clz((int)__ballot_sync(0xffffffffu, d < nseq && first <= t)), 0);
+        doc = from + k;
+        row = __shfl_sync(0xffffffffu, a, k);
+        len = max(__shfl_sync(0xffffffffu, b, k) - row, 0);
+        tile = t - __shfl_sync(0xffffffffu, first, k);
+    }
+};
 
 // Clear the rows [first, end) of a tile of `blocks` column blocks (a warp).
 __device__ __forceinline__ void clear_rows(unsigned char *tile, int first, int blocks, int end = kTile) {

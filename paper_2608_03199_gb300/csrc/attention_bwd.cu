@@ -61,10 +61,6 @@ struct BwdArgs {
 constexpr int kWalked = 2;
 __host__ __device__ constexpr int kept(int dp) { return dp == 64 ? 2 : 1; }
 
-__device__ __forceinline__ int first_q_tile(const BwdArgs &f, int s) {
-    return f.p.a.new_tokens > 0 ? s * f.doc_tiles : first_tile(f.p.a.q_offsets, s, (int)f.p.a.q_tokens, kTile);
-}
-
 // The threads that compute meet: bounded like every wait, so a warp that gave
 // up leaves none behind.
 struct Meeting {
@@ -202,6 +198,7 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
         bool ok = true;
         // the next work that has steps (head < 0: none is left); false: a wait
         // gave up
+        DocFinder find(a.q_offsets, a.nseq, a.q_tokens);
         auto fetch = [&](DqWork &w, bool own) {
             while (true) {
                 if (!own && !blocks.next(wait, block)) return false;
@@ -210,16 +207,18 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
                 if (block < 0) return true;
                 const int head = block / f.q_numbers, t = block % f.q_numbers;
                 int s, tile;
+                Doc doc;
                 if (a.new_tokens > 0) {
                     s = t / f.doc_tiles;
                     tile = t % f.doc_tiles;
+                    doc = doc_at(a, s);
                 } else {
-                    s = find_doc(a.q_offsets, (int)a.nseq, (int)a.q_tokens, kTile, t);
-                    tile = t - first_tile(a.q_offsets, s, (int)a.q_tokens, kTile);
+                    find(t, s, doc.q0, doc.nq, tile);
+                    keys_of(a, s, doc);
                 }
-                const Doc doc = doc_at(a, s);
                 const int tiles = (doc.nq + kTile - 1) / kTile;
                 if (tile < 0 || tile >= tiles) continue;
+                const int number0 = t - tile;          // the document's first
                 tile = tiles - 1 - tile;               // the tiles that see most keys first
                 w.head = head;
                 w.q_row = doc.q0;
@@ -230,8 +229,11 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
                 const int last = min(doc.nq, w.row0 + kTile);
                 const int end = a.causal ? min(doc.nk, last + doc.nk - doc.nq) : doc.nk;
                 w.n = end > 0 ? (end + kTile - 1) / kTile : 0;
-                w.stats = (first_q_tile(f, s) + tile) * a.heads + head;
-                if (w.n > 0) return true;
+                w.stats = (number0 + tile) * a.heads + head;
+                if (w.n > 0) {
+                    if (w.n <= kShort) blocks.ask();
+                    return true;
+                }
                 // no query of these sees a key
                 const int pieces = a.head_dim / 8;
 #pragma unroll 1
@@ -265,9 +267,8 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
             }
             __syncwarp();
             ++item;
-            // The next work is looked for (a few thousand cycles) while the
-            // first steps of this one run.  Not so early for long work: others
-            // may be done sooner.
+            // The next work is looked for while the first steps of this one
+            // run.  Not so early for long work: others may be done sooner.
             DqWork then;
             const int when = w.n <= kShort ? min(w.n, 2) : w.n;
 #pragma unroll 1
@@ -586,6 +587,7 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
         bool ok = true;
         // the next work that has steps (hk < 0: none is left); false: a wait
         // gave up
+        DocFinder find(a.k_offsets, a.nseq, a.k_tokens);
         auto fetch = [&](DkvWork &w, bool own) {
             while (true) {
                 if (!own && !blocks.next(wait, block)) return false;
@@ -594,9 +596,10 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
                 if (block < 0) return true;
                 const int hk = block / f.k_numbers;
                 w.number = block % f.k_numbers;
-                const int s = find_doc(a.k_offsets, (int)a.nseq, (int)a.k_tokens, kTile, w.number);
-                const int tile = w.number - first_tile(a.k_offsets, s, (int)a.k_tokens, kTile);
-                const Doc doc = doc_at(a, s);
+                int s, tile;
+                Doc doc;
+                find(w.number, s, doc.k0, doc.nk, tile);
+                queries_of(a, s, doc);
                 w.key0 = tile * kTile;
                 const bool used = tile >= 0 && w.key0 < doc.nk;
                 // the first tile of queries that sees any of these keys
@@ -608,7 +611,8 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
                     w.nk = doc.nk;
                     w.q_row = doc.q0;
                     w.nq = doc.nq;
-                    w.q_number = first_q_tile(f, s);
+                    w.q_number = a.new_tokens > 0 ? s * f.doc_tiles : doc.q0 / kTile + s;
+                    if (w.q_tiles * share <= kShort) blocks.ask();
                     return true;
                 }
                 // no query sees these keys, or no document uses the number:

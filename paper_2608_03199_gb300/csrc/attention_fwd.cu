@@ -36,6 +36,7 @@ constexpr int kSoftmaxWarps = 8;
 constexpr int kSoftmax = kSoftmaxWarps * 32;
 constexpr int kThreads = kSoftmax + 64;
 constexpr int kSlots = 2;     // the work in hand and the next
+constexpr int kShort = 16;    // key tiles of work that is short
 constexpr int kHalf = kTile / 2;
 constexpr uint32_t kTmemCols = 256;
 constexpr int kBlocksPerSm = 2;
@@ -70,7 +71,7 @@ struct FwdArgs {
 
 // False where the block's number is one that no document uses.
 template <bool SPLIT>
-__device__ __forceinline__ bool find_work(const FwdArgs &f, int t, Work &w) {
+__device__ __forceinline__ bool find_work(const FwdArgs &f, DocFinder &find, int t, Work &w) {
     const sieve_attention_args &a = f.p.a;
     Doc doc;
     int k_end, last;                                   // of the tile's queries, the one that sees most
@@ -87,11 +88,11 @@ __device__ __forceinline__ bool find_work(const FwdArgs &f, int t, Work &w) {
         if (a.new_tokens > 0) {
             s = t / f.doc_tiles;
             tile = t % f.doc_tiles;
+            doc = doc_at(a, s);
         } else {
-            s = find_doc(a.q_offsets, (int)a.nseq, (int)a.q_tokens, kTile, t);
-            tile = t - first_tile(a.q_offsets, s, (int)a.q_tokens, kTile);
+            find(t, s, doc.q0, doc.nq, tile);
+            keys_of(a, s, doc);
         }
-        doc = doc_at(a, s);
         const int tiles = (doc.nq + kTile - 1) / kTile;
         if (tile < 0 || tile >= tiles) return false;
         w.query0 = (tiles - 1 - tile) * kTile;         // the tiles that see most keys first
@@ -180,12 +181,13 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
         }
         int block = blockIdx.x, item = 0, set = 1, group_in_set = -1, q_issued = 0, k_issued = 0, v_issued = 0;
         Blocks blocks{&s_answer, &steal_bar, 0, false};
+        DocFinder find(a.q_offsets, a.nseq, a.q_tokens);
         bool ok = true;
         while (ok && block >= 0) {
             Work w;
             w.group = block / f.numbers;
             const int head0 = w.group * f.pack, hk = head0 / share;
-            const bool found = find_work<SPLIT>(f, block % f.numbers, w);
+            const bool found = find_work<SPLIT>(f, find, block % f.numbers, w);
             if (found && w.n == 0) {
                 // no query of these sees a key
                 const int first = w.query0, last = min(w.nq, w.query0 + kTile);
@@ -219,6 +221,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(&work_full[slot]);
                 ++item;
+                if (!SPLIT && w.n <= kShort) blocks.ask();
                 const int qs = q_issued % kQStages;
                 if (!(ok = wait.warp(&q_empty[qs], ((uint32_t)(q_issued / kQStages) & 1u) ^ 1u))) break;
                 if (elected()) {
