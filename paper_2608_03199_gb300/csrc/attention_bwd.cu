@@ -518,13 +518,16 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
 // its odd quarters of keys.  The pieces (32 keys by 32 queries) that meet in a
 // set lie a multiple of 64 distances apart, over all steps of a head, so the 63
 // distances of a piece are its own: it stores its sums, and no order matters.
+// Where there is room the sets are there twice, and the next head's are another
+// than the ones being added up.
 constexpr int kSums = 8;
+__host__ __device__ constexpr int sum_sets(int dp) { return dp == 64 ? 2 : 1; }
 
 template <typename T, int DP, bool BIAS>
 __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant__ BwdArgs f) {
     constexpr int kCompute = kWarps * 32;
     static_assert(kSums == 2 * kGroups, "");
-    constexpr int kB = DP / 64, kKept = kept(DP);
+    constexpr int kB = DP / 64, kKept = kept(DP), kSumSets = sum_sets(DP);
     constexpr uint32_t kTileBytes = kB * kBlockBytes;
     constexpr uint32_t kSCol = 0, kDpCol = 128, kDvCol = 256, kDkCol = 384;   // P in S's place, dS in dP's
     extern __shared__ unsigned char smem_raw[];
@@ -535,7 +538,7 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
     __shared__ uint32_t tmem_slot;
     __shared__ int s_abort;
     __shared__ DkvWork s_work[kSlots];
-    __shared__ float s_far[kWarps][2];
+    __shared__ float s_far[kSumSets][kWarps][2];
     const sieve_attention_args &a = f.p.a;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = lane_id();
     const int share = a.heads / a.kv_heads;
@@ -546,7 +549,7 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
     float *bias = reinterpret_cast<float *>(qd + kWalked * 2 * kTileBytes);
     // the bias by minus the distance (columns run that way)
     constexpr int kCopies = DP == 64 ? 4 : 1;
-    float *by_distance = bias + (BIAS ? bias_floats(a.reach, kCopies) : 0);   // [kSums][entries]
+    float *by_distance = bias + (BIAS ? bias_floats(a.reach, kCopies) : 0);   // [kSumSets][kSums][entries]
 
     if (threadIdx.x == 0) {
         if (blockIdx.x == 0 && a.q_tokens == 0) f.p.ctl->status = 0;      // (else k_attend_delta did)
@@ -779,6 +782,8 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
         const uint32_t lane_base = tmem + ((uint32_t)(quarter * 32) << 16);
         // the group's sums of even or of odd quarters (see kSums)
         float *mine = by_distance + (2 * group + (quarter & 1)) * f.entries;
+        const int set_size = kSums * f.entries;
+        int set = 0;
         constexpr float kDown = 1.f / (float)(1 << kPShift<T>);
         Meeting meet{&meet_bar, 0};
         uint32_t step = 0;
@@ -802,7 +807,7 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
                     if (head != head_in_table) {
                         fill_bias<kCopies>(bias, a, head, -1, threadIdx.x, kCompute);
                         if (head_in_table < 0)
-                            for (int e = threadIdx.x; e < kSums * f.entries; e += kCompute) by_distance[e] = 0.f;
+                            for (int e = threadIdx.x; e < kSumSets * set_size; e += kCompute) by_distance[e] = 0.f;
                         head_in_table = head;
                         if (!(ok = meet(wait))) break;
                     }
@@ -928,7 +933,7 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
                                 if (lane + e < 32) up += v;
                                 else down += v;
                             }
-                            float *to = mine + a.reach + kPad + hi - 31 + lane;
+                            float *to = mine + set * set_size + a.reach + kPad + hi - 31 + lane;
                             to[0] = up;
                             if (lane > 0) to[-32] = down;
                         }
@@ -938,25 +943,28 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
                     // the head's sums: the warps' added up, in order
                     const float before = warp_sum(far_before), after = warp_sum(far_after);
                     if (lane == 0) {
-                        s_far[warp][0] = before;
-                        s_far[warp][1] = after;
+                        s_far[set][warp][0] = before;
+                        s_far[set][warp][1] = after;
                     }
                     if (!(ok = meet(wait))) break;
                     float *out = f.partial + ((int64_t)w.number * a.heads + head) * f.entries;
+                    float *sums = by_distance + set * set_size;
                     for (int e = threadIdx.x; e < f.entries; e += kCompute) {
                         float x = 0.f;
 #pragma unroll
                         for (int k = 0; k < kSums; ++k) {
-                            x += by_distance[k * f.entries + e];
-                            by_distance[k * f.entries + e] = 0.f;      // for the next head
+                            x += sums[k * f.entries + e];
+                            sums[k * f.entries + e] = 0.f;      // for a later head
                         }
                         if (e == kPad)
-                            for (int k = 0; k < kWarps; ++k) x += s_far[k][0];
+                            for (int k = 0; k < kWarps; ++k) x += s_far[set][k][0];
                         if (e == kPad + 2 * a.reach)
-                            for (int k = 0; k < kWarps; ++k) x += s_far[k][1];
+                            for (int k = 0; k < kWarps; ++k) x += s_far[set][k][1];
                         out[e] = x;
                     }
-                    if (!(ok = meet(wait))) break;
+                    // (with two sets the next meeting keeps the order)
+                    if (kSumSets == 1 && !(ok = meet(wait))) break;
+                    set ^= kSumSets - 1;
                 }
             }
             if (ok) ok = wait.warp(&acc_full, (uint32_t)item & 1u);
@@ -1069,7 +1077,7 @@ cudaError_t run(const BwdArgs &f, const Layout &l, unsigned char *ws, cudaStream
     if (a.k_tokens > 0) {
         auto dkv = k_attend_dkv<T, DP, BIAS>;
         const size_t smem =
-            tiles + (BIAS ? (size_t)(bias_floats(a.reach, DP == 64 ? 4 : 1) + kSums * f.entries) * 4 : 0);
+            tiles + (BIAS ? (size_t)(bias_floats(a.reach, DP == 64 ? 4 : 1) + sum_sets(DP) * kSums * f.entries) * 4 : 0);
         if ((e = cudaFuncSetAttribute(dkv, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
         dkv<<<(unsigned)(l.k_tiles * a.kv_heads), 18 * 32, smem, st>>>(f);
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
