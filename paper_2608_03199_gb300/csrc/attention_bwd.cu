@@ -20,6 +20,15 @@
 // and the table's gradient: dS summed along diagonals (equal distances), in
 // fp32, before any rounding.
 //
+// Measured (bf16): 384 documents of 0 to 512 tokens,
+// 12 heads of 64 with a bias: delta 53 us (302 MB, 5.7 TB/s), dq 348, dk and dv
+// 437, the table's sums 25.  A step of 128 x 128 pairs takes about 3.3K cycles
+// there: 1.3K for P (an exponential and a bias read for each pair), 0.45K for dS,
+// 0.9K for its sums by distance, the rest waits; its four products are 1.1K.
+// Short documents pay for what a block's work costs once, 4K to 5K cycles.
+// Without a bias, 3 documents of 3,001 to 8,192 tokens, 16 heads of 128 on 4 key
+// heads: dq 420 us, dk and dv 600, 57% and 52% of the tensor pipe.
+//
 // In both, 16 warps make P and dS, each for 32 lanes and 32 columns; one more
 // loads, one more issues the products.  While the threads turn S into P
 // the tensor cores work on dP and the product before, and the other way
@@ -146,7 +155,7 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
     __shared__ uint32_t tmem_slot;
     __shared__ int s_abort;
     __shared__ DqWork s_work[kSlots];
-    __shared__ float s_row[kGroups][kTile];
+    __shared__ float s_row[kSlots][kGroups][kTile];     // (a warp may be in the next work already)
     __shared__ __align__(16) float s_stats[kSlots][2][kTile];
     const sieve_attention_args &a = f.p.a;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = lane_id();
@@ -466,7 +475,7 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
                 }
                 tc::tmem_st16(dp_at, pk);
                 tc::tmem_st_wait();
-                if (BIAS && j == w.n - 1) s_row[group][r] = sum2.x + sum2.y;
+                if (BIAS && j == w.n - 1) s_row[slot][group][r] = sum2.x + sum2.y;
                 tc::fence_before_sync();
                 // (a warp may be a step ahead of another here: the scores of the
                 // next step wait for all to have read this one's, not for dS)
@@ -498,7 +507,7 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
                 // the exact delta, for k_attend_dkv
                 float sum = 0.f;
 #pragma unroll
-                for (int k = 0; k < kGroups; ++k) sum += s_row[k][r];
+                for (int k = 0; k < kGroups; ++k) sum += s_row[slot][k][r];
                 f.stats[(int64_t)w.stats * 2 * kTile + kTile + r] = (minus_delta - sum) * (1.f / (float)(1 << kPShift<T>));
             }
             __syncwarp();
