@@ -22,7 +22,7 @@
 // the steps on documents of a few tiles.)
 //
 // Measured (bf16): 4 documents of 6,001 to 8,192 tokens, causal, 16 heads of 128
-// on 4 key heads: 702 us, 1.14 PFLOP/s, bound by the softmax between two products
+// on 4 key heads: 707 us, 1.13 PFLOP/s, bound by the softmax between two products
 // (two blocks an SM hide most of it).  512 documents of 0 to 512 tokens, 12 heads
 // of 64 with a bias: 365 us; the products are a sixth of that, the rest is the
 // softmax (an exponential and a bias read for each pair) and, for documents of a

@@ -93,9 +93,11 @@ __global__ void __launch_bounds__(TPR)
 // loads go out together, and one meeting of the block serves all), and
 // keeps the column sums of dweight and dbias of its columns in registers;
 // they go to partial[block][2][width] and k_norm_reduce adds the blocks up.
+// (Registers for three blocks of 256 an SM: 20,011 x 1001 fp32, both passes, 99 us
+// with two rows at a time and the next two on their way; 115 with four and one
+// block an SM; 132 with four and none on their way.)
 template <typename T, typename W, int VEC, int TPR, int NCH, int R>
-__global__ void __launch_bounds__(TPR)
-    k_norm_backward(const NormArgs a) {
+__global__ void __launch_bounds__(TPR, TPR <= 256 ? 768 / TPR : 1) k_norm_backward(const NormArgs a) {
     __shared__ float smem[2 * R][TPR / 32];
     const int i = threadIdx.x;
     const T *dy = static_cast<const T *>(a.dy), *x = static_cast<const T *>(a.x);
@@ -109,8 +111,11 @@ __global__ void __launch_bounds__(TPR)
         for (int e = 0; e < VEC; ++e) dw[c][e] = db[c][e] = 0.f;
     }
     const float inv_n = 1.f / (float)a.width;
-    for (int64_t r0 = (int64_t)blockIdx.x * R; r0 < a.rows; r0 += (int64_t)gridDim.x * R) {
-        float g[R][NCH][VEC], xh[R][NCH][VEC], mu[R], rs[R], s1[R], s2[R];
+    // Element by element the next rows are on their way while these are worked
+    // on (wider pieces leave no registers for it).
+    constexpr bool kAhead = VEC == 1 && TPR <= 256;
+    using Rows = float[R][NCH][VEC];
+    auto load = [&](int64_t r0, Rows &g, Rows &xh, float (&mu)[R], float (&rs)[R]) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int64_t row = r0 + r;
@@ -120,7 +125,6 @@ __global__ void __launch_bounds__(TPR)
             const int64_t at = live ? row : a.rows - 1;
             mu[r] = __ldg(a.mean_in + at);
             rs[r] = live ? __ldg(a.rstd_in + at) : 0.f;
-            s1[r] = s2[r] = 0.f;
 #pragma unroll
             for (int c = 0; c < NCH; ++c) {
                 const int col = min((c * TPR + i) * VEC, a.width - VEC);
@@ -128,6 +132,33 @@ __global__ void __launch_bounds__(TPR)
                 load_vec<T, VEC>(x + at * a.x_stride + col, xh[r][c]);
             }
         }
+    };
+    const int64_t first = (int64_t)blockIdx.x * R, step = (int64_t)gridDim.x * R;
+    Rows next_g, next_x;
+    float next_mu[R], next_rs[R];
+    if (kAhead) load(first, next_g, next_x, next_mu, next_rs);
+    for (int64_t r0 = first; r0 < a.rows; r0 += step) {
+        Rows g, xh;
+        float mu[R], rs[R], s1[R], s2[R];
+        if (kAhead) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                mu[r] = next_mu[r];
+                rs[r] = next_rs[r];
+#pragma unroll
+                for (int c = 0; c < NCH; ++c)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        g[r][c][e] = next_g[r][c][e];
+                        xh[r][c][e] = next_x[r][c][e];
+                    }
+            }
+            if (r0 + step < a.rows) load(r0 + step, next_g, next_x, next_mu, next_rs);
+        } else {
+            load(r0, g, xh, mu, rs);
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) s1[r] = s2[r] = 0.f;
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -469,8 +500,8 @@ cudaError_t backward_as(const NormArgs &a, int blocks, cudaStream_t st) {
 int backward_blocks(int64_t rows, int width) {
     const int64_t n = width <= kRowsWidth ? ceil_div(rows, kRowWarps) : rows;
     // rows of 513 to 1,024: their registers let two blocks share an SM, and more
-    // blocks only make more partial sums (20,011 x 1001 fp32, both passes: 132 us;
-    // 150 with twice as many)
+    // blocks only make more partial sums (100,003 x 768 bf16, both passes: 157 us;
+    // 162 with twice as many)
     const int64_t most = width > 512 && width <= kRowsWidth ? kMaxBlocks / 2 : kMaxBlocks;
     return (int)(n < most ? n : most);
 }
@@ -489,9 +520,9 @@ cudaError_t backward(const NormArgs &a, cudaStream_t st) {
             else if (chunks <= 512) e = backward_as<T, W, V, 512, 1, 2>(a, blocks, st);
             else e = backward_as<T, W, V, 512, V == 8 ? 4 : 8, 1>(a, blocks, st);
         } else {
-            if (a.width <= 128) e = backward_as<T, W, 1, 32, 4, 4>(a, blocks, st);
-            else if (a.width <= 512) e = backward_as<T, W, 1, 128, 4, 4>(a, blocks, st);
-            else if (a.width <= 1024) e = backward_as<T, W, 1, 256, 4, 4>(a, blocks, st);
+            if (a.width <= 128) e = backward_as<T, W, 1, 32, 4, 2>(a, blocks, st);
+            else if (a.width <= 512) e = backward_as<T, W, 1, 128, 4, 2>(a, blocks, st);
+            else if (a.width <= 1024) e = backward_as<T, W, 1, 256, 4, 2>(a, blocks, st);
             else if (a.width <= 4096) e = backward_as<T, W, 1, 512, 8, 1>(a, blocks, st);
             else e = backward_as<T, W, 1, 1024, 16, 1>(a, blocks, st);
         }
