@@ -182,6 +182,16 @@ def test_attention_of_new_tokens(new, heads, kv_heads, dim, dtype, buckets):
             ref.assert_within(got, want[name], bound[name], name)
 
 
+@pytest.mark.parametrize("same,causal", [(True, False), (False, True)])
+def test_attention_of_thousands_of_documents(same, causal):
+    """More documents than a block keeps in view at a time, with long runs of
+    empty ones, and heads that make every block start over."""
+    klen = [i * 7 % 5 for i in range(1100)] + [0] * 1200 + [130] + [0] * 70 + [1, 2, 3] * 100 + [0] * 40
+    qlen = klen if same else klen[::-1]
+    q, k, v, dout, table, bmap = attention_inputs(11, qlen, klen, 3, 3, 16, BF16, 16, 20, causal)
+    check_attention(q, k, v, dout, qlen, klen, table, bmap, causal)
+
+
 def test_attention_of_one_new_token_over_one_long_document():
     klen = [40_001]
     q, k, v, _, table, bmap = attention_inputs(9, [1], klen, 4, 1, 128, BF16, 32, 128, True)
