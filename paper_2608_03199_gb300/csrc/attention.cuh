@@ -13,7 +13,7 @@
 // anything.  Scores of such keys are replaced before they are used; where such
 // rows are the contraction axis their probabilities are exact zeros, but
 // 0 x NaN is NaN, so the warp that issues the products first clears those
-// rows of the tile (at most once per block and operand, in its idle time).
+// rows of the tile (the last of a document, in its idle time).
 #pragma once
 
 #include <cuda.h>
@@ -32,10 +32,6 @@ constexpr uint32_t kPolls = 1u << 24;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-// Operand descriptors with 128-byte swizzle.  K-major: as in tcgen05.cuh.
-// MN-major: the 64-element blocks of the M or N axis lie kBlockBytes apart
-// (leading offset), groups of 8 rows of the contraction axis 1024 bytes apart.
-
 // Instruction descriptor of kind::f16, fp32 accumulation, M = 128: both
 // operands fp16 (format 0) or bf16 (format 1), B K-major or MN-major (bit 16).
 template <typename T>
@@ -53,6 +49,9 @@ __device__ __forceinline__ bool elected() {
     asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(p));
     return p != 0;
 }
+// Operand descriptors with 128-byte swizzle.  K-major: as in tcgen05.cuh.
+// MN-major: the 64-element blocks of the M or N axis lie kBlockBytes apart
+// (leading offset), groups of 8 rows of the contraction axis 1024 bytes apart.
 __device__ __forceinline__ uint64_t desc_k(const void *tile) {      // K-major
     return tc::desc_k_sw128(tc::smem_u32(tile));
 }
