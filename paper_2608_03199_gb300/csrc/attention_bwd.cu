@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
     constexpr uint32_t kSCol = 0, kDpCol = 128, kDqCol = 384;   // S, dP twice (dS in its place), dQ
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t q_full[kKept], q_empty[kKept], k_full[kKs], k_empty[kKs], v_full[kVs], v_empty[kVs], s_full, s_free,
-        dp_full[2], ds_full[2], dq_full, done, work_full[kSlots], work_empty[kSlots], steal_bar;
+        dp_full[2], ds_full[2], dq_full, done, work_full[kSlots], work_empty[kSlots], stat_full[kSlots], steal_bar;
     __shared__ __align__(16) uint4 s_answer;
     __shared__ uint32_t tmem_slot;
     __shared__ int s_abort;
@@ -184,6 +184,7 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
             tc::mbar_init(&ds_full[i], kWarps);
             tc::mbar_init(&work_full[i], 1);
             tc::mbar_init(&work_empty[i], kWarps + 1);
+            tc::mbar_init(&stat_full[i], 1);
         }
         tc::mbar_init(&s_full, 1);
         tc::mbar_init(&s_free, kWarps);
@@ -202,7 +203,7 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
 
     if (warp == kWarps + 1) {
         // ---------------- the work, one block's after another's, and its loads ----------------
-        int block = blockIdx.x, item = 0, kv_issued = 0, k_issued = 0, head0 = -1, head1 = -1;
+        int block = blockIdx.x, item = 0, stats_issued = 0, kv_issued = 0, k_issued = 0, head0 = -1, head1 = -1;
         Blocks blocks{&s_answer, &steal_bar, 0, false};
         bool ok = true;
         // the next work that has steps (head < 0: none is left); false: a wait
@@ -264,10 +265,20 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
             if (lane == 0) s_work[slot] = w;
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&work_full[slot]);
+            // The row statistics complete on a barrier of their slot: every warp
+            // has read them, and so passed it, before the slot is free again.
+            // (q_full is no barrier for those warps: with one pair held the
+            // products alone let the next pair in, and a warp that had not
+            // looked yet would find its phase gone.)
+            if (elected()) {
+                expect(&stat_full[slot], 2 * kTile * 4);
+                tc::bulk_g2s(1u, s_stats[slot], f.stats + (int64_t)w.stats * 2 * kTile, 2 * kTile * 4, &stat_full[slot]);
+            }
+            __syncwarp();
+            ++stats_issued;
             if (!(ok = wait.warp(&q_empty[qs], ((uint32_t)(item / kKept) & 1u) ^ 1u))) break;
             if (elected()) {
-                expect(&q_full[qs], 2 * kTileBytes + 2 * kTile * 4);
-                tc::bulk_g2s(1u, s_stats[slot], f.stats + (int64_t)w.stats * 2 * kTile, 2 * kTile * 4, &q_full[qs]);
+                expect(&q_full[qs], 2 * kTileBytes);
                 for (int b = 0; b < kB; ++b) {
                     tma_load(qd + qs * 2 * kTileBytes + b * kBlockBytes, &f.q, 64 * b, head, w.q_row + w.row0, &q_full[qs]);
                     tma_load(qd + (qs * 2 + 1) * kTileBytes + b * kBlockBytes, &f.dout, 64 * b, head, w.q_row + w.row0,
@@ -315,6 +326,8 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
         if (!ok) {
             // after an abort: what is in flight lands before the block ends
             if (blocks.asking) let_land(&steal_bar, blocks.asked & 1u);
+            for (int i = max(0, stats_issued - kSlots); i < stats_issued; ++i)
+                let_land(&stat_full[i % kSlots], (uint32_t)(i / kSlots) & 1u);
             for (int i = max(0, item - kKept); i < item; ++i) let_land(&q_full[i % kKept], (uint32_t)(i / kKept) & 1u);
             for (int i = max(0, k_issued - kKs); i < k_issued; ++i) let_land(&k_full[i % kKs], (uint32_t)(i / kKs) & 1u);
             for (int i = max(0, kv_issued - kVs); i < kv_issued; ++i) let_land(&v_full[i % kVs], (uint32_t)(i / kVs) & 1u);
@@ -405,7 +418,7 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
             const int seen = (live ? (a.causal ? min(w.nk, place + 1) : w.nk) : 0) - group * kCols;
             const int64_t row = w.q_row + w.row0 + r;
             const float *table = bias + slot * bias_set;
-            if (!(ok = wait.warp(&q_full[item % kKept], (uint32_t)(item / kKept) & 1u))) break;   // the row statistics
+            if (!(ok = wait.warp(&stat_full[slot], (uint32_t)(item / kSlots) & 1u))) break;
             const float nl = s_stats[slot][0][r] - (float)kPShift<T>;
             const float minus_delta = s_stats[slot][1][r] * (float)(1 << kPShift<T>);
             float2 sum2 = both(0.f);
