@@ -67,8 +67,12 @@ sieve_status check_attention(const sieve_attention_args *a, bool pointers) {
     return SIEVE_OK;
 }
 
+// The arguments as the kernels take them, for sizes and launches alike: the
+// queries' documents filled in, no reach (which nothing has checked) without a
+// table.
 sieve_attention_args resolved(const sieve_attention_args *a) {
     sieve_attention_args r = *a;
+    if (!r.num_buckets) r.reach = 0;
     if (r.new_tokens == 0 && !r.q_offsets) r.q_offsets = r.k_offsets;
     return r;
 }
@@ -157,7 +161,7 @@ sieve_status sieve_attention_workspace_size(const sieve_attention_args *a, size_
     if (!bytes) return SIEVE_EINVAL;
     sieve_status rc = check_attention(a, false);
     if (rc != SIEVE_OK) return rc;
-    *bytes = attention_workspace_bytes(*a);
+    *bytes = attention_workspace_bytes(resolved(a));
     return SIEVE_OK;
 }
 
@@ -166,7 +170,7 @@ sieve_status sieve_attention(const sieve_attention_args *a, void *out, float *ls
     sieve_status rc = check_attention(a, true);
     if (rc != SIEVE_OK) return rc;
     if (a->q_tokens > 0 && (!out || !lse || !aligned_to(out, 16))) return SIEVE_EINVAL;
-    if ((rc = check_workspace(ws, ws_bytes, attention_workspace_bytes(*a))) != SIEVE_OK) return rc;
+    if ((rc = check_workspace(ws, ws_bytes, attention_workspace_bytes(resolved(a)))) != SIEVE_OK) return rc;
     if ((rc = check_current_device()) != SIEVE_OK) return rc;
     if (a->q_tokens == 0) return SIEVE_OK;
     AttentionArgs p = {};
@@ -180,7 +184,7 @@ sieve_status sieve_attention_backward_workspace_size(const sieve_attention_args 
     if (!bytes) return SIEVE_EINVAL;
     sieve_status rc = check_attention(a, false);
     if (rc != SIEVE_OK) return rc;
-    *bytes = attention_backward_workspace_bytes(*a);
+    *bytes = attention_backward_workspace_bytes(resolved(a));
     return SIEVE_OK;
 }
 
@@ -198,7 +202,7 @@ sieve_status sieve_attention_backward(const sieve_attention_args *a, const void 
         return SIEVE_EINVAL;
     if (a->k_tokens > 0 && (!dk || !dv || !aligned_to(dk, 16) || !aligned_to(dv, 16))) return SIEVE_EINVAL;
     if (a->table && !dtable) return SIEVE_EINVAL;
-    if ((rc = check_workspace(ws, ws_bytes, attention_backward_workspace_bytes(*a))) != SIEVE_OK) return rc;
+    if ((rc = check_workspace(ws, ws_bytes, attention_backward_workspace_bytes(resolved(a)))) != SIEVE_OK) return rc;
     if ((rc = check_current_device()) != SIEVE_OK) return rc;
     AttentionArgs p = {};
     p.a = resolved(a);

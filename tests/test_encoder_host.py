@@ -149,3 +149,17 @@ def test_reference_agrees_with_autograd():
     res, _ = ref.unit_pool(h.detach(), [3, 4], dr)
     assert torch.allclose(res["rows"], u.detach(), rtol=1e-10)
     assert torch.allclose(res["dh"], torch.autograd.grad(u, h, dr)[0], rtol=1e-9, atol=1e-12)
+
+
+@pytest.mark.parametrize("reach", [-5, 7, 256, 1 << 30])
+def test_reach_counts_for_nothing_without_a_table(reach):
+    """Without a table the reach is not looked at: a call with a negative
+    scale (which runs as if with a bias of zero) is sized and laid out the same
+    whatever it holds."""
+    many = dict(heads=8, kv_heads=1, nseq=4, new_tokens=1, q_tokens=4, k_tokens=1_000_000, scale=-0.5)
+    sizes = []
+    for r in (0, reach):
+        n = C.c_size_t()
+        assert sieve.lib().sieve_attention_workspace_size(C.byref(args(**many, reach=r)), C.byref(n)) == 0
+        sizes.append(n.value)
+    assert sizes[0] == sizes[1]
