@@ -184,8 +184,10 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
         // ---------------- the work, one block's after another's, and its loads ----------------
         if (lane == 0) {
             prefetch_map(&f.q);
-            prefetch_map(&f.k);
-            prefetch_map(&f.v);
+            if (a.k_tokens > 0) {     // (else there are no maps)
+                prefetch_map(&f.k);
+                prefetch_map(&f.v);
+            }
         }
         int block = blockIdx.x, item = 0, set = 1, group_in_set = -1, q_issued = 0, k_issued = 0, v_issued = 0;
         Blocks blocks{&s_answer, &steal_bar, 0, false};

@@ -18,3 +18,22 @@ def test_attention_of_many_documents_of_one_tile(dim, dtype, buckets, causal):
     n = [1 + i * 37 % 128 for i in range(700)]
     q, k, v, dout, table, bmap = attention_inputs(21 + dim, n, n, 4, 2, dim, dtype, buckets, 64, causal)
     check_attention(q, k, v, dout, n, n, table, bmap, causal)
+
+
+@pytest.mark.parametrize("new", [0, 1, 3])
+@pytest.mark.parametrize("buckets", [0, 32])
+def test_attention_over_no_keys_at_all(new, buckets):
+    """Queries of documents that hold no key yet: zeros, -inf, zero gradients."""
+    qlen, klen = [new or 130] * 3, [0, 0, 0]
+    q, k, v, dout, table, bmap = attention_inputs(31, qlen, klen, 4, 2, 64, BF16, buckets, 64, True)
+    off = ref.offsets_of(klen, DEV)
+    kw = dict(table=table, buckets=bmap, causal=True, check=True)
+    if new:
+        q, dout = q.view(3, new, 4, 64), dout.view(3, new, 4, 64)
+    else:
+        kw["q_offsets"] = ref.offsets_of(qlen, DEV)
+    out, lse = sieve.attention(q, k, v, off, **kw)
+    assert not out.any() and torch.isneginf(lse).all()
+    dq, dk, dv, dtable = sieve.attention_backward(dout, q, k, v, out, lse, off, **kw)
+    assert not dq.any() and dk.shape == k.shape and dv.shape == v.shape
+    assert dtable is None or not dtable.any()
