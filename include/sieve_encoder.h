@@ -13,7 +13,8 @@
  * buffer the caller's, scratch from the caller's workspace (256-byte
  * aligned, sized by the *_workspace_size call), nothing allocated, nothing
  * printed, no abort; calls are asynchronous on `stream` and return
- * SIEVE_EINVAL before any device work for an argument they refuse.  The same
+ * SIEVE_EINVAL before any device work for an argument they refuse, a pointer
+ * that is not aligned to its elements among them.  The same
  * call on the same inputs gives the same bits: no sum depends on the order in
  * which blocks run.
  *

@@ -16,6 +16,9 @@ namespace {
     } while (0)
 
 bool aligned_to(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+// fp32 and int32 arrays that are read or written element by element
+template <typename... P>
+bool aligned4(const P *...p) { return (aligned_to(p, 4) && ...); }
 
 size_t type_bytes(int dtype) { return dtype == SIEVE_F32 ? 4 : 2; }
 bool is_type(int dtype) { return dtype == SIEVE_F32 || dtype == SIEVE_F16 || dtype == SIEVE_BF16; }
@@ -58,6 +61,7 @@ sieve_status check_attention(const sieve_attention_args *a, bool pointers) {
     if (!pointers) return SIEVE_OK;
     if (biased ? (!a->table || !a->bucket_map) : (a->table || a->bucket_map)) return SIEVE_EINVAL;
     if (a->nseq > 0 && !a->k_offsets) return SIEVE_EINVAL;
+    if (!aligned4(a->q_offsets, a->k_offsets, a->table, a->bucket_map)) return SIEVE_EINVAL;
     const int64_t strides[6] = {a->q_token_stride, a->q_head_stride, a->k_token_stride,
                                 a->k_head_stride,  a->v_token_stride, a->v_head_stride};
     for (int64_t s : strides)
@@ -90,7 +94,7 @@ sieve_status sieve_layer_norm(const void *x, int64_t x_stride, const void *weigh
     if (bad_rows(x, x_stride, rows, width, dtype) || bad_rows(y, y_stride, rows, width, dtype)) return SIEVE_EINVAL;
     if (!weight || !aligned_to(weight, type_bytes(weight_dtype)) || !aligned_to(bias, type_bytes(weight_dtype)))
         return SIEVE_EINVAL;
-    if (!mean != !rstd) return SIEVE_EINVAL;
+    if (!mean != !rstd || !aligned4(mean, rstd)) return SIEVE_EINVAL;
     if ((rc = check_current_device()) != SIEVE_OK) return rc;
     if (rows == 0) return SIEVE_OK;
     NormArgs a = {};
@@ -133,7 +137,7 @@ sieve_status sieve_layer_norm_backward(const void *dy, int64_t dy_stride, const 
     if (!weight || !dweight || !aligned_to(weight, ws_type) || !aligned_to(dweight, ws_type) ||
         !aligned_to(dbias, ws_type))
         return SIEVE_EINVAL;
-    if (rows > 0 && (!mean || !rstd)) return SIEVE_EINVAL;
+    if ((rows > 0 && (!mean || !rstd)) || !aligned4(mean, rstd)) return SIEVE_EINVAL;
     if ((rc = check_workspace(ws, ws_bytes, norm_backward_workspace_bytes(rows, width))) != SIEVE_OK) return rc;
     if ((rc = check_current_device()) != SIEVE_OK) return rc;
     NormArgs a = {};
@@ -169,7 +173,7 @@ sieve_status sieve_attention(const sieve_attention_args *a, void *out, float *ls
                              void *stream) {
     sieve_status rc = check_attention(a, true);
     if (rc != SIEVE_OK) return rc;
-    if (a->q_tokens > 0 && (!out || !lse || !aligned_to(out, 16))) return SIEVE_EINVAL;
+    if (a->q_tokens > 0 && (!out || !lse || !aligned_to(out, 16) || !aligned4(lse))) return SIEVE_EINVAL;
     if ((rc = check_workspace(ws, ws_bytes, attention_workspace_bytes(resolved(a)))) != SIEVE_OK) return rc;
     if ((rc = check_current_device()) != SIEVE_OK) return rc;
     if (a->q_tokens == 0) return SIEVE_OK;
@@ -198,10 +202,10 @@ sieve_status sieve_attention_backward(const sieve_attention_args *a, const void 
     for (int i = 0; i < 6; ++i)
         if (grad_strides[i] < 0 || grad_strides[i] % 8) return SIEVE_EINVAL;
     if (a->q_tokens > 0 && (!dout || !out || !lse || !dq || !aligned_to(dout, 16) || !aligned_to(out, 16) ||
-                            !aligned_to(dq, 16)))
+                            !aligned_to(dq, 16) || !aligned4(lse)))
         return SIEVE_EINVAL;
     if (a->k_tokens > 0 && (!dk || !dv || !aligned_to(dk, 16) || !aligned_to(dv, 16))) return SIEVE_EINVAL;
-    if (a->table && !dtable) return SIEVE_EINVAL;
+    if ((a->table && !dtable) || !aligned4(dtable)) return SIEVE_EINVAL;
     if ((rc = check_workspace(ws, ws_bytes, attention_backward_workspace_bytes(resolved(a)))) != SIEVE_OK) return rc;
     if ((rc = check_current_device()) != SIEVE_OK) return rc;
     AttentionArgs p = {};
@@ -240,12 +244,12 @@ sieve_status sieve_unit_pool_workspace_size(int64_t tokens, int64_t nseq, int32_
 }
 
 static sieve_status check_pool(const int32_t *offsets, int64_t tokens, int64_t nseq, int32_t width, int32_t dtype,
-                               const void *tok, int64_t stride, const void *r, const void *n) {
+                               const void *tok, int64_t stride, const float *r, const float *n) {
     size_t need;
     sieve_status rc = sieve_unit_pool_workspace_size(tokens, nseq, width, &need);
     if (rc != SIEVE_OK) return rc;
     if (!is_type(dtype) || (nseq == 0 && tokens > 0)) return SIEVE_EINVAL;
-    if (nseq > 0 && (!offsets || !r || !n)) return SIEVE_EINVAL;
+    if ((nseq > 0 && (!offsets || !r || !n)) || !aligned4(offsets, r, n)) return SIEVE_EINVAL;
     return bad_rows(tok, stride, tokens, width, dtype) ? SIEVE_EINVAL : SIEVE_OK;
 }
 
@@ -279,7 +283,7 @@ sieve_status sieve_unit_pool_backward(const float *drows, const float *rows, con
                                       int32_t dtype, void *dh, int64_t dh_stride, void *stream) {
     sieve_status rc = check_pool(offsets, tokens, nseq, width, dtype, dh, dh_stride, rows, norms);
     if (rc != SIEVE_OK) return rc;
-    if (nseq > 0 && !drows) return SIEVE_EINVAL;
+    if ((nseq > 0 && !drows) || !aligned4(drows)) return SIEVE_EINVAL;
     if ((rc = check_current_device()) != SIEVE_OK) return rc;
     if (nseq == 0 || tokens == 0) return SIEVE_OK;
     PoolArgs a = {};

@@ -163,3 +163,25 @@ def test_reach_counts_for_nothing_without_a_table(reach):
         assert sieve.lib().sieve_attention_workspace_size(C.byref(args(**many, reach=r)), C.byref(n)) == 0
         sizes.append(n.value)
     assert sizes[0] == sizes[1]
+
+
+def test_unaligned_pointers_are_refused_without_gpu():
+    """Every pointer that a kernel reads or writes element by element lies at
+    a multiple of its element's size, or the call refuses it."""
+    lib, p, odd, big = sieve.lib(), C.c_void_p(256), C.c_void_p(258), 1 << 40
+    biased = dict(num_buckets=8, reach=4, table=256, bucket_map=256)
+    strides = (C.c_int64 * 6)(256, 64, 128, 64, 128, 64)
+    for bad in (dict(k_offsets=258), dict(q_offsets=258), dict(biased, table=258), dict(biased, bucket_map=258)):
+        assert lib.sieve_attention(C.byref(args(**bad)), p, p, p, big, None) == -1, bad
+        assert lib.sieve_attention_backward(C.byref(args(**bad)), p, p, p, p, p, p, strides, p, p, big, None) == -1, bad
+    assert lib.sieve_attention(C.byref(args()), p, odd, p, big, None) == -1
+    assert lib.sieve_attention_backward(C.byref(args()), p, p, odd, p, p, p, strides, None, p, big, None) == -1
+    assert lib.sieve_attention_backward(C.byref(args(**biased)), p, p, p, p, p, p, strides, odd, p, big, None) == -1
+    for m, r in ((odd, p), (p, odd)):
+        assert lib.sieve_layer_norm(p, 64, p, p, 3, 64, 0, 0, 1e-5, p, 64, m, r, None) == -1
+        assert lib.sieve_layer_norm_backward(p, 64, p, 64, p, m, r, 3, 64, 0, 0, p, 64, p, p, p, big, None) == -1
+    for at in range(3):
+        x = [odd if i == at else p for i in range(3)]
+        assert lib.sieve_unit_pool(p, 64, x[0], 1000, 7, 64, 0, x[1], x[2], p, big, None) == -1, at
+        assert lib.sieve_unit_pool_backward(p, x[1], x[2], x[0], 1000, 7, 64, 0, p, 64, None) == -1, at
+    assert lib.sieve_unit_pool_backward(odd, p, p, p, 1000, 7, 64, 0, p, 64, None) == -1
