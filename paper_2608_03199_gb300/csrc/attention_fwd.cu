@@ -32,6 +32,7 @@
 // Where every document has a few new queries against many keys, a block takes
 // the rows of all heads that share a key head (up to 128) over one chunk of
 // the keys, and k_attend_join adds the chunks up.
+#include <cfloat>
 #include <cstring>
 
 #include "attention.cuh"
@@ -456,7 +457,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
                 }
                 float top = fmaxf(fmax3f(t4[0], t4[1], t4[2]), t4[3]);
                 // the row's maximum over both halves (without a bias the
-                // scale is not negative, so it can be applied after the
+                // scale is above zero, so it can be applied after the
                 // comparison)
                 if (!BIAS) top *= c;
                 s_top[meets & 1u][half][r] = top;
@@ -619,6 +620,12 @@ struct Shape {
     size_t smem;
 };
 
+// Whether a call runs the kernels with a bias, if of zero.  Those compare and
+// hide finished scores; the others compare raw ones, hide them with -inf and
+// apply the scale after that, which takes a scale above zero (a negative one
+// turns the order around, and -inf times zero is NaN).
+bool runs_biased(const sieve_attention_args &a) { return a.num_buckets || !(a.scale > FLT_MIN); }
+
 // bias tables of a block: what still lets two blocks share an SM
 constexpr int kMaxBiasBytes = 14 * 1024;
 
@@ -627,7 +634,7 @@ Shape shape_of(const sieve_attention_args &a) {
     const int dp = a.head_dim <= 64 ? 64 : 128, share = a.heads / a.kv_heads;
     const bool packed = a.new_tokens > 0 && a.new_tokens <= kTile;
     // two sets of tables
-    const int bias_bytes = a.num_buckets || a.scale < 0.f ? 2 * 4 * bias_floats(a.reach, packed ? 1 : 4) : 0;
+    const int bias_bytes = runs_biased(a) ? 2 * 4 * bias_floats(a.reach, packed ? 1 : 4) : 0;
     s.pack = 1;
     if (packed) {
         s.split = true;
@@ -666,9 +673,7 @@ cudaError_t run(const FwdArgs &f, const Shape &s, cudaStream_t st) {
 
 template <typename T, int DP>
 cudaError_t by_shape(const FwdArgs &f, const Shape &s, cudaStream_t st) {
-    // a negative scale turns the order of the raw scores around: the biased
-    // form, which compares finished scores, takes it (with a bias of zero)
-    const bool biased = f.p.a.num_buckets || f.p.a.scale < 0.f;
+    const bool biased = runs_biased(f.p.a);
     if (s.split) return biased ? run<T, DP, true, true>(f, s, st) : run<T, DP, false, true>(f, s, st);
     return biased ? run<T, DP, true, false>(f, s, st) : run<T, DP, false, false>(f, s, st);
 }

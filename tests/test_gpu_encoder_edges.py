@@ -5,7 +5,7 @@ import torch
 
 import encoder_reference as ref
 import paper_2608_03199_gb300 as sieve
-from test_gpu_encoder import BF16, DEV, FP16, FP32, attention_inputs, check_attention, gen, randn  # noqa: F401
+from test_gpu_encoder import BF16, DEV, FP16, attention_inputs, check_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +37,36 @@ def test_attention_over_no_keys_at_all(new, buckets):
     dq, dk, dv, dtable = sieve.attention_backward(dout, q, k, v, out, lse, off, **kw)
     assert not dq.any() and dk.shape == k.shape and dv.shape == v.shape
     assert dtable is None or not dtable.any()
+
+
+SCALES = [0.0, -0.0, 1e-42, -0.3]
+
+
+@pytest.mark.parametrize("scale", SCALES)
+@pytest.mark.parametrize("dim,dtype,buckets,causal", [(64, BF16, 0, False), (64, FP16, 0, True), (128, BF16, 0, True), (40, BF16, 32, False)])
+def test_attention_takes_any_finite_scale(dim, dtype, buckets, causal, scale):
+    """Zero (a mean over the keys seen), less than a normal number, negative:
+    with and without a table, documents that end inside a tile."""
+    qlen, klen = ([200, 0, 33, 128, 5], [200, 0, 33, 128, 5]) if dim != 128 else ([200, 7, 33, 130, 5], [129, 0, 300, 128, 3])
+    q, k, v, dout, table, bmap = attention_inputs(41, qlen, klen, 4, 2, dim, dtype, buckets, 64, causal)
+    check_attention(q, k, v, dout, qlen, klen, table, bmap, causal, scale)
+
+
+def check_new_tokens(new, klen, heads, kv_heads, dim, dtype, buckets, causal, scale=None, seed=0):
+    """Forward and backward of `new` tokens for each document."""
+    qlen = [new] * len(klen)
+    q, k, v, dout, table, bmap = attention_inputs(seed + new, qlen, klen, heads, kv_heads, dim, dtype, buckets, 64, causal)
+    off, shape = ref.offsets_of(klen, DEV), (len(klen), new, heads, dim)
+    kw = dict(table=table, buckets=bmap, causal=causal, scale=scale, check=True)
+    out, lse = sieve.attention(q.view(shape), k, v, off, **kw)
+    grads = sieve.attention_backward(dout.view(shape), q.view(shape), k, v, out, lse, off, **kw)
+    want, bound = ref.attention(q, k, v, qlen, klen, table, bmap, causal, scale, dout)
+    for name, got in zip(("out", "lse", "dq", "dk", "dv", "dtable"), (out, lse, *grads)):
+        if got is not None:
+            ref.assert_within(got.reshape(want[name].shape), want[name], bound[name], name)
+
+
+@pytest.mark.parametrize("scale", SCALES)
+@pytest.mark.parametrize("buckets,causal", [(0, True), (0, False), (32, True)])
+def test_attention_of_new_tokens_takes_any_finite_scale(buckets, causal, scale):
+    check_new_tokens(3, [700, 0, 1, 2, 129, 640], 6, 2, 64, BF16, buckets, causal, scale)
