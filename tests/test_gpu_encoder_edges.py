@@ -5,7 +5,7 @@ import torch
 
 import encoder_reference as ref
 import paper_2608_03199_gb300 as sieve
-from test_gpu_encoder import BF16, DEV, FP16, attention_inputs, check_attention
+from test_gpu_encoder import BF16, DEV, FP16, attention_inputs, check_attention, gen, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -70,3 +70,56 @@ def check_new_tokens(new, klen, heads, kv_heads, dim, dtype, buckets, causal, sc
 @pytest.mark.parametrize("buckets,causal", [(0, True), (0, False), (32, True)])
 def test_attention_of_new_tokens_takes_any_finite_scale(buckets, causal, scale):
     check_new_tokens(3, [700, 0, 1, 2, 129, 640], 6, 2, 64, BF16, buckets, causal, scale)
+
+
+@pytest.mark.parametrize("new", [128, 129, 300])
+@pytest.mark.parametrize("heads,kv_heads,dim,dtype,buckets,causal", [(4, 2, 64, BF16, 32, True), (3, 1, 128, FP16, 0, True),
+                                                                     (2, 2, 72, BF16, 16, False)])
+def test_attention_of_many_new_tokens(new, heads, kv_heads, dim, dtype, buckets, causal):
+    """A tile of new tokens for each document, one more, and several tiles,
+    over fewer and over more kept tokens."""
+    check_new_tokens(new, [500, 0, 1, 128, 299, 130], heads, kv_heads, dim, dtype, buckets, causal)
+
+
+@pytest.mark.parametrize("left", [0, 8, 3])
+def test_layer_norm_in_place_leaves_the_columns_beside_it(left):
+    """y over x and dx over dy inside a wider matrix: the columns on both sides stay."""
+    g = gen(left)
+    wide, wide_dy = randn(g, 50, 800).to(BF16), randn(g, 50, 800).to(BF16)
+    kept, kept_dy = wide.clone(), wide_dy.clone()
+    part = slice(left, left + 512)
+    w = randn(g, 512).to(BF16)
+    want, bound = ref.layer_norm(kept[:, part], w, None, 1e-6, kept_dy[:, part])
+    y, mean, rstd = sieve.layer_norm(wide[:, part], w, eps=1e-6, out=wide[:, part])
+    ref.assert_within(y, want["y"], bound["y"], "y")
+    dx, dw, _ = sieve.layer_norm_backward(wide_dy[:, part], kept[:, part], w, mean, rstd, out=wide_dy[:, part])
+    ref.assert_within(dx, want["dx"], bound["dx"], "dx")
+    for now, before in ((wide, kept), (wide_dy, kept_dy)):
+        assert torch.equal(now[:, :left], before[:, :left]) and torch.equal(now[:, left + 512:], before[:, left + 512:])
+
+
+def test_every_call_on_another_stream_and_with_a_kept_workspace():
+    """Bit for bit what the current stream and scratch of their own give."""
+    g = gen(81)
+    n = [300, 0, 90]
+    off = ref.offsets_of(n, DEV)
+    q, k, v, dout, table, bmap = attention_inputs(82, n, n, 4, 2, 64, BF16, 32, 64, True)
+    h, w, drows = randn(g, sum(n), 256), randn(g, 256), randn(g, 3, 256)
+
+    def calls(**kw):
+        plain = {key: x for key, x in kw.items() if key != "workspace"}
+        y, mean, rstd = sieve.layer_norm(h, w, **plain)
+        dx, dw, db = sieve.layer_norm_backward(y, h, w, mean, rstd, **kw)
+        out, lse = sieve.attention(q, k, v, off, table=table, buckets=bmap, causal=True, check=True, **kw)
+        grads = sieve.attention_backward(dout, q, k, v, out, lse, off, table=table, buckets=bmap, causal=True, check=True, **kw)
+        rows, norms = sieve.unit_pool(h, off, **kw)
+        dh = sieve.unit_pool_backward(drows, rows, norms, off, h.shape[0], **plain)
+        return (y, mean, rstd, dx, dw, db, out, lse, *grads, rows, norms, dh)
+
+    want = calls()
+    torch.cuda.synchronize()
+    s, ws = torch.cuda.Stream(), sieve.Workspace()
+    for _ in range(3):
+        for got in (calls(stream=s), calls(workspace=ws), calls(stream=s, workspace=sieve.Workspace())):
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
