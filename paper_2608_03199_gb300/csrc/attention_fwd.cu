@@ -738,11 +738,23 @@ sieve_status make_map(CUtensorMap *map, int dtype, const void *base, int head_di
     const cuuint64_t strides[2] = {(cuuint64_t)(heads > 1 ? head_stride : head_dim) * 2,
                                    (cuuint64_t)(tokens > 1 ? token_stride : (int64_t)heads * head_dim) * 2};
     const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_tokens}, step[3] = {1, 1, 1};
-    const CUresult r = encode(
-        map, dtype == SIEVE_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
-        const_cast<void *>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? SIEVE_OK : SIEVE_EINVAL;
+    auto make = [&] {
+        return encode(map, dtype == SIEVE_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+                      const_cast<void *>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    };
+    CUresult r = make();
+    if (r == CUDA_ERROR_INVALID_CONTEXT || r == CUDA_ERROR_NOT_INITIALIZED) {
+        // The driver's functions want a current context, and a host thread has
+        // none before its first call of the runtime that needs one.
+        int dev;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e == cudaSuccess) e = cudaSetDevice(dev);
+        if (e != cudaSuccess) return record_cuda_error(e);
+        r = make();
+    }
+    if (r == CUDA_SUCCESS) return SIEVE_OK;
+    return r == CUDA_ERROR_INVALID_VALUE ? SIEVE_EINVAL : record_cuda_error(static_cast<cudaError_t>(r));
 }
 
 }  // namespace enc

@@ -1,10 +1,14 @@
 """Arguments of the encoder operators at the edges of what they take, on the
 GPU against their definitions in 64 bits (encoder_reference)."""
+import ctypes as C
+import threading
+
 import pytest
 import torch
 
 import encoder_reference as ref
 import paper_2608_03199_gb300 as sieve
+from paper_2608_03199_gb300.encoder import AttentionArgsC
 from test_gpu_encoder import BF16, DEV, FP16, attention_inputs, check_attention, gen, randn
 
 pytestmark = pytest.mark.gpu
@@ -123,3 +127,22 @@ def test_every_call_on_another_stream_and_with_a_kept_workspace():
         for got in (calls(stream=s), calls(workspace=ws), calls(stream=s, workspace=sieve.Workspace())):
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_attention_from_a_new_host_thread():
+    """A thread that has made no CUDA call yet has no current context."""
+    n = [60, 5]
+    q, k, v, dout, table, bmap = attention_inputs(72, n, n, 2, 1, 64, BF16, 32, 64, False)
+    off, s = ref.offsets_of(n, DEV), torch.cuda.current_stream().cuda_stream
+    want = sieve.attention(q, k, v, off, table=table, buckets=bmap)
+    out, lse = torch.empty_like(q), torch.empty_like(want[1])
+    ws = torch.empty(1 << 16, dtype=torch.uint8, device=DEV)
+    a = AttentionArgsC(2, 2, 1, 64, 2, 65, 65, 0, 0, 0.125, 32, 64, 0, None, off.data_ptr(), q.data_ptr(), k.data_ptr(),
+                       v.data_ptr(), 128, 64, 64, 64, 64, 64, table.data_ptr(), bmap.data_ptr())
+    rc = []
+    t = threading.Thread(target=lambda: rc.append(sieve.lib().sieve_attention(
+        C.byref(a), out.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel(), s)))
+    t.start()
+    t.join()
+    assert rc == [0]
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
