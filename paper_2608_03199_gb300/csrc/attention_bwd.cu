@@ -1081,27 +1081,37 @@ Layout layout_of(const sieve_attention_args &a) {
     return l;
 }
 
+template <int DP, bool BIAS>
+size_t dq_smem(int reach) {
+    return 1024 + (size_t)(2 * kept(DP) + 3 + (DP == 64 ? 2 : 1)) * (DP / 64) * kBlockBytes +
+           (BIAS ? (size_t)2 * bias_floats(reach) * 4 : 0);
+}
+template <int DP, bool BIAS>
+size_t dkv_smem(int reach) {
+    return 1024 + (size_t)2 * (kWalked + kept(DP)) * (DP / 64) * kBlockBytes +
+           (BIAS ? (size_t)(bias_floats(reach, DP == 64 ? 4 : 1) + sum_sets(DP) * kSums * bias_entries(reach)) * 4 : 0);
+}
+
 template <typename T, int DP, bool BIAS>
 cudaError_t run(const BwdArgs &f, const Layout &l, unsigned char *ws, cudaStream_t st) {
     const sieve_attention_args &a = f.p.a;
-    const size_t tiles = 1024 + (size_t)2 * (kWalked + kept(DP)) * (DP / 64) * kBlockBytes;
+    // (the kernels' limits are the process', so they are the most that any
+    // call asks for: another host thread may launch at any moment)
+    constexpr auto kLimit = cudaFuncAttributeMaxDynamicSharedMemorySize;
+    constexpr int kMost = SIEVE_ATTENTION_MAX_REACH;
     cudaError_t e;
     if (a.q_tokens > 0) {
         k_attend_delta<T, DP / 8><<<(unsigned)(l.q_tiles * a.heads), kDeltaThreads, 0, st>>>(f);
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
         auto dq = k_attend_dq<T, DP, BIAS>;
-        const size_t smem = 1024 + (size_t)(2 * kept(DP) + 3 + (DP == 64 ? 2 : 1)) * (DP / 64) * kBlockBytes +
-                            (BIAS ? (size_t)2 * bias_floats(a.reach) * 4 : 0);
-        if ((e = cudaFuncSetAttribute(dq, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
-        dq<<<(unsigned)(l.q_tiles * a.heads), 18 * 32, smem, st>>>(f);
+        if ((e = cudaFuncSetAttribute(dq, kLimit, (int)dq_smem<DP, BIAS>(kMost))) != cudaSuccess) return e;
+        dq<<<(unsigned)(l.q_tiles * a.heads), 18 * 32, dq_smem<DP, BIAS>(a.reach), st>>>(f);
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
     }
     if (a.k_tokens > 0) {
         auto dkv = k_attend_dkv<T, DP, BIAS>;
-        const size_t smem =
-            tiles + (BIAS ? (size_t)(bias_floats(a.reach, DP == 64 ? 4 : 1) + sum_sets(DP) * kSums * f.entries) * 4 : 0);
-        if ((e = cudaFuncSetAttribute(dkv, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
-        dkv<<<(unsigned)(l.k_tiles * a.kv_heads), 18 * 32, smem, st>>>(f);
+        if ((e = cudaFuncSetAttribute(dkv, kLimit, (int)dkv_smem<DP, BIAS>(kMost))) != cudaSuccess) return e;
+        dkv<<<(unsigned)(l.k_tiles * a.kv_heads), 18 * 32, dkv_smem<DP, BIAS>(a.reach), st>>>(f);
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
     }
     if (BIAS) {

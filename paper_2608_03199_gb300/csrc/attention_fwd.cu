@@ -629,12 +629,23 @@ bool runs_biased(const sieve_attention_args &a) { return a.num_buckets || !(a.sc
 // bias tables of a block: what still lets two blocks share an SM
 constexpr int kMaxBiasBytes = 14 * 1024;
 
+// two sets of one head's tables
+int bias_bytes_of(int reach, bool packed) { return 2 * 4 * bias_floats(reach, packed ? 1 : 4); }
+size_t smem_bytes(int dp, int bias_bytes) {
+    return 1024 + (size_t)(3 * stages(dp)) * (dp / 64) * kBlockBytes + (size_t)bias_bytes;
+}
+// The most that any call asks of an instance.
+template <int DP, bool BIAS, bool SPLIT>
+size_t most_smem() {
+    const int one = BIAS ? bias_bytes_of(SIEVE_ATTENTION_MAX_REACH, SPLIT) : 0;
+    return smem_bytes(DP, BIAS && SPLIT && one < kMaxBiasBytes ? kMaxBiasBytes : one);
+}
+
 Shape shape_of(const sieve_attention_args &a) {
     Shape s = {};
     const int dp = a.head_dim <= 64 ? 64 : 128, share = a.heads / a.kv_heads;
     const bool packed = a.new_tokens > 0 && a.new_tokens <= kTile;
-    // two sets of tables
-    const int bias_bytes = runs_biased(a) ? 2 * 4 * bias_floats(a.reach, packed ? 1 : 4) : 0;
+    const int bias_bytes = runs_biased(a) ? bias_bytes_of(a.reach, packed) : 0;
     s.pack = 1;
     if (packed) {
         s.split = true;
@@ -652,7 +663,7 @@ Shape shape_of(const sieve_attention_args &a) {
         s.doc_tiles = a.new_tokens > 0 ? (int)ceil_div(a.new_tokens, kTile) : 0;
         s.blocks = (a.new_tokens > 0 ? a.nseq * s.doc_tiles : doc_tiles(a.q_tokens, a.nseq, kTile)) * a.heads;
     }
-    s.smem = 1024 + (size_t)(3 * stages(dp)) * (dp / 64) * kBlockBytes + (size_t)s.pack * bias_bytes;
+    s.smem = smem_bytes(dp, s.pack * bias_bytes);
     return s;
 }
 
@@ -663,7 +674,10 @@ size_t part_floats(const sieve_attention_args &a, const Shape &s) {
 template <typename T, int DP, bool BIAS, bool SPLIT>
 cudaError_t run(const FwdArgs &f, const Shape &s, cudaStream_t st) {
     auto kernel = k_attend<T, DP, BIAS, SPLIT>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem);
+    // The limit is the process', the same whatever this call needs: another
+    // host thread may launch between this line and the launch.
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         (int)most_smem<DP, BIAS, SPLIT>());
     if (e != cudaSuccess) return e;
     kernel<<<(unsigned)s.blocks, kThreads, s.smem, st>>>(f);
     if ((e = cudaGetLastError()) != cudaSuccess || !SPLIT) return e;

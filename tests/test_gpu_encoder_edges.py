@@ -146,3 +146,41 @@ def test_attention_from_a_new_host_thread():
     t.join()
     assert rc == [0]
     assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
+def test_host_threads_with_tables_of_different_reach():
+    """A kernel's shared-memory limit belongs to the process: calls with small
+    tables must not lower it under a launch with large ones."""
+    n, lib, strides = [150, 40], sieve.lib(), (C.c_int64 * 6)(128, 64, 64, 64, 64, 64)
+    jobs = []
+    for reach in (64, 256, 8, 200):
+        q, k, v, dout, table, bmap = attention_inputs(71, n, n, 2, 1, 64, BF16, 16, reach, False)
+        off, s = ref.offsets_of(n, DEV), torch.cuda.Stream()
+        out, lse = sieve.attention(q, k, v, off, table=table, buckets=bmap)
+        got = [torch.zeros_like(t) for t in (out, lse, q, k, v, table)]
+        want = (out, lse, *sieve.attention_backward(dout, q, k, v, out, lse, off, table=table, buckets=bmap))
+        ws = torch.empty(1 << 20, dtype=torch.uint8, device=DEV)
+        a = AttentionArgsC(2, 2, 1, 64, 2, 190, 190, 0, 0, 0.125, 16, reach, 0, None, off.data_ptr(), q.data_ptr(), k.data_ptr(),
+                           v.data_ptr(), 128, 64, 64, 64, 64, 64, table.data_ptr(), bmap.data_ptr())
+        jobs.append((a, [t.data_ptr() for t in got], dout.data_ptr(), ws, s, got, want, (q, k, v, table, bmap, off, dout)))
+    torch.cuda.synchronize()
+    codes = []
+
+    def work(a, p, dout, ws, s, *kept):
+        for _ in range(1500):
+            rc = lib.sieve_attention(C.byref(a), p[0], p[1], ws.data_ptr(), ws.numel(), s.cuda_stream)
+            rc = rc or lib.sieve_attention_backward(C.byref(a), dout, p[0], p[1], p[2], p[3], p[4], strides, p[5],
+                                                    ws.data_ptr(), ws.numel(), s.cuda_stream)
+            if rc:
+                codes.append((rc, lib.sieve_last_cuda_error()))
+                return
+
+    threads = [threading.Thread(target=work, args=j) for j in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not codes, codes
+    for *_, got, want, _ in jobs:
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
