@@ -737,23 +737,28 @@ sieve_status make_map(CUtensorMap *map, int dtype, const void *base, int head_di
     using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
                                 const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-    static Encode encode = nullptr;   // the driver's function; the same whoever finds it first
-    if (!encode) {
-        void *fn = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        const cudaError_t e =
-            cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found);
-        if (e != cudaSuccess) return record_cuda_error(e);
-        if (found != cudaDriverEntryPointSuccess || !fn) return SIEVE_EUNSUPPORTED;
-        encode = reinterpret_cast<Encode>(fn);
-    }
+    // the driver's function, found once (the first caller's thread looks, the
+    // others wait for it)
+    struct Found {
+        Encode fn = nullptr;
+        cudaError_t error;
+        Found() {
+            void *p = nullptr;
+            cudaDriverEntryPointQueryResult how = cudaDriverEntryPointSymbolNotFound;
+            error = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &how);
+            if (error == cudaSuccess && how == cudaDriverEntryPointSuccess) fn = reinterpret_cast<Encode>(p);
+        }
+    };
+    static const Found found;
+    if (found.error != cudaSuccess) return record_cuda_error(found.error);
+    if (!found.fn) return SIEVE_EUNSUPPORTED;
     const cuuint64_t dims[3] = {(cuuint64_t)head_dim, (cuuint64_t)heads, (cuuint64_t)tokens};
     // an axis of one element has no stride that matters
     const cuuint64_t strides[2] = {(cuuint64_t)(heads > 1 ? head_stride : head_dim) * 2,
                                    (cuuint64_t)(tokens > 1 ? token_stride : (int64_t)heads * head_dim) * 2};
     const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_tokens}, step[3] = {1, 1, 1};
     auto make = [&] {
-        return encode(map, dtype == SIEVE_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+        return found.fn(map, dtype == SIEVE_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
                       const_cast<void *>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
                       CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     };
