@@ -103,7 +103,10 @@ sieve_status sieve_layer_norm_backward(const void *dy, int64_t dy_stride, const 
  *            the distance clamped to [-reach, reach]; entries outside
  *            [0, num_buckets) are clamped
  * The score of a query and a key it sees is s = scale q.k + table[bucket][h];
- * a score of -inf (a bias of -inf) hides the key.
+ * a score of -inf (a bias of -inf) hides the key.  Finite biases beyond
+ * +-2.35e38 count as the type's largest or lowest.  Scores are fp32: beside a
+ * bias of 1e9 the product vanishes, and keys of equal bias share their weight
+ * evenly.
  *   out      device [q_tokens][heads][head_dim] of dtype, contiguous:
  *            sum of softmax(s) v
  *   lse      device [heads][q_tokens] fp32: log of the sum of exp(s)

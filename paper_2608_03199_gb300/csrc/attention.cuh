@@ -386,7 +386,8 @@ __device__ __forceinline__ void clear_rows(unsigned char *tile, int first, int b
 // -reach - kPad .. reach + kPad: 32 rows by 32 columns that hold any distance
 // inside (-reach, reach) hold none outside this range, so their lookups need
 // no clamp.  Finite values stay finite: the type's lowest must not become
-// -inf, which hides a key.
+// -inf, which hides a key.  Beyond 2.35e38, where log2(e) leaves the type, they
+// count as its lowest or largest.
 //
 // A thread needs 32 consecutive entries, from a start that falls by one from
 // lane to lane.  So the table is kept four times, copy s shifted by s entries:

@@ -58,7 +58,7 @@ constexpr int kPShift = std::is_same_v<T, __half> ? 14 : 0;
 struct BwdArgs {
     AttentionArgs p;
     CUtensorMap q, k, v, dout;
-    float *stats;      // [q tile][head][2][128]: kPShift - lse in base 2, -2^-kPShift delta
+    float *stats;      // [q tile][head][stat_rows][128], see there
     float *partial;    // [k tile][head][entries]: dS by distance
     int doc_tiles;     // new_tokens > 0: q tiles of a document
     int entries;       // bias_entries(reach)
@@ -69,6 +69,16 @@ struct BwdArgs {
 // keeps (two: the next work's is loaded while this one's is in use).
 constexpr int kWalked = 2;
 __host__ __device__ constexpr int kept(int dp) { return dp == 64 ? 2 : 1; }
+
+// Row statistics, 128 to a row: kPShift - lse in base 2; -2^-kPShift delta.  With
+// a table two more, where the tile has a far query (see far_statistics): minus
+// its largest score in base 2 and kPShift - log2 of the sum of the 2^(score -
+// largest), zeros for the others.  A far query's first one is minus zero: its
+// mark, which changes no sum.  The kernels hold the first two rows of a tile; the
+// others are read where they lie.
+constexpr int kStats = 2;
+__host__ __device__ constexpr int stat_rows(bool bias) { return bias ? 4 : kStats; }
+__device__ __forceinline__ bool is_far(float stat) { return __float_as_uint(stat) == 0x80000000u; }
 
 // The threads that compute meet: bounded like every wait, so a warp that gave
 // up leaves none behind.
@@ -95,12 +105,63 @@ struct DkvWork {
     int hk, k_row, key0, nk, q_row, nq, q_first, q_tiles, q_number, number;   // hk < 0: no more
 };
 
+// A query all of whose keys have huge biases is far: beside 1e6 an lse in 32 bits
+// leaves P off by a percent, beside 1e9 the log of the sum is lost in it and P of
+// n keys would be 1 each, not 1 / n.  So its largest score and its sum are made
+// anew, each for itself, from scores that are rounded as the forward pass rounds
+// them; P = 2^((score - largest) - log2 sum) is exact at any size.  This takes a
+// warp a pass over the query's keys without the tensor cores, and biases that a
+// model learns stay far below the limit.
+constexpr float kFar = 256.f;      // of an lse (off by 2^-17 there) and of a bias in base 2
+template <typename T>
+__device__ __noinline__ bool far_statistics(const sieve_attention_args &a, const Doc &doc, int head, int qi, float &top,
+                                            float &log2_sum) {
+    const int lane = lane_id(), d = a.head_dim, place = qi + doc.nk - doc.nq;
+    const int seen = a.causal ? min(doc.nk, place + 1) : doc.nk;
+    // the largest bias of the keys seen: not huge, and the size is the scores' own
+    const int lo = min(max(-place, -a.reach), a.reach), hi = min(max(seen - 1 - place, -a.reach), a.reach);
+    float most = -INFINITY;
+    for (int i = lo + lane; i <= hi; i += 32) most = fmaxf(most, scaled_bias(a, i, head));
+#pragma unroll
+    for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+    if (seen <= 0 || !(fabsf(most) > kFar) || isinf(most)) return false;
+    const T *q = static_cast<const T *>(a.q) + (int64_t)(doc.q0 + qi) * a.q_token_stride + head * a.q_head_stride;
+    const T *k = static_cast<const T *>(a.k) + head / (a.heads / a.kv_heads) * a.k_head_stride;
+    const float c = a.scale * kLog2e;
+    float m = -INFINITY, l = 0.f;
+    for (int j = lane; j < seen; j += 32) {
+        const T *kj = k + (int64_t)(doc.k0 + j) * a.k_token_stride;
+        float dot = 0.f;
+        for (int i = 0; i < d; i += 8) {
+            float x[8], y[8];
+            load_vec<T, 8>(q + i, x);
+            load_vec<T, 8>(kj + i, y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dot = fmaf(x[e], y[e], dot);
+        }
+        const float x = fmaf(dot, c, scaled_bias(a, j - place, head));
+        if (x == -INFINITY) continue;
+        if (x > m) {
+            l = fmaf(l, exp2f(m - x), 1.f);
+            m = x;
+        } else {
+            l += exp2f(x - m);
+        }
+    }
+    top = m;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    l = warp_sum(m == -INFINITY ? l : l * exp2f(m - top));
+    log2_sum = log2f(l);
+    return true;
+}
+
 // delta = dO . O of every query, and -lse in base 2: a block per tile and head,
 // 8 or 16 lanes to a row.  (Inside k_attend_dq, with a row to a thread, the same
 // reads took 3K to 9K cycles of every block's time.)
 constexpr int kDeltaThreads = 256;
-template <typename T, int kLanes>
-__global__ void __launch_bounds__(kDeltaThreads) k_attend_delta(const __grid_constant__ BwdArgs f) {
+template <typename T, int kLanes, bool BIAS>
+__global__ void __launch_bounds__(kDeltaThreads, 8) k_attend_delta(const __grid_constant__ BwdArgs f) {
     const sieve_attention_args &a = f.p.a;
     if (blockIdx.x == 0 && threadIdx.x == 0) f.p.ctl->status = 0;
     const int t = blockIdx.x / a.heads, head = blockIdx.x % a.heads;
@@ -116,11 +177,12 @@ __global__ void __launch_bounds__(kDeltaThreads) k_attend_delta(const __grid_con
     if (tile < 0 || tile * kTile >= doc.nq) return;
     const int64_t row0 = doc.q0 + tile * kTile;
     const int rows = min(kTile, doc.nq - tile * kTile);
-    float *stats = f.stats + ((int64_t)t * a.heads + head) * 2 * kTile;
+    float *stats = f.stats + ((int64_t)t * a.heads + head) * stat_rows(BIAS) * kTile;
     const int piece = threadIdx.x % kLanes, d = a.head_dim;
     const T *o = static_cast<const T *>(f.p.out_in) + (row0 * a.heads + head) * d + piece * 8;
     const T *g = static_cast<const T *>(f.p.dout) + (row0 * a.heads + head) * d + piece * 8;
     constexpr int kRows = kDeltaThreads / kLanes;
+    uint32_t may_be_far = 0;      // of this thread's rows, one bit each
 #pragma unroll
     for (int i = 0; i < kTile / kRows; ++i) {
         const int r = i * kRows + threadIdx.x / kLanes;
@@ -135,8 +197,27 @@ __global__ void __launch_bounds__(kDeltaThreads) k_attend_delta(const __grid_con
         for (int k = kLanes / 2; k; k >>= 1) part += __shfl_xor_sync(0xffffffffu, part, k);
         if (piece == 0) {
             const float lse = r < rows ? f.p.lse_in[(int64_t)head * a.q_tokens + row0 + r] : -INFINITY;
-            stats[r] = lse == -INFINITY ? -INFINITY : (float)kPShift<T> - lse * kLog2e;
+            stats[r] = lse == -INFINITY ? -INFINITY : (float)kPShift<T> - lse * kLog2e + 0.f;   // (no minus zero)
             stats[kTile + r] = -part * (1.f / (float)(1 << kPShift<T>));
+            if (BIAS && fabsf(lse) > kFar && !isinf(lse)) may_be_far |= 1u << i;
+        }
+    }
+    if (!BIAS || !__syncthreads_or(may_be_far)) return;
+    stats[2 * kTile + threadIdx.x] = 0.f;
+    static_assert(kDeltaThreads == 2 * kTile, "");
+    __syncthreads();
+#pragma unroll 1
+    for (int n = 0; n < kTile / kRows * (32 / kLanes); ++n) {
+        const int i = n / (32 / kLanes), from = n % (32 / kLanes) * kLanes;       // row of the warp, its first lane
+        const int r = i * kRows + ((int)threadIdx.x / 32 * 32 + from) / kLanes;
+        float top, log2_sum;
+        if (!(__shfl_sync(0xffffffffu, may_be_far, from) >> i & 1u) ||
+            !far_statistics<T>(a, doc, head, tile * kTile + r, top, log2_sum))
+            continue;
+        if (lane_id() == (uint32_t)from) {
+            stats[r] = -0.f;
+            stats[2 * kTile + r] = -top;
+            stats[3 * kTile + r] = (float)kPShift<T> - log2_sum;
         }
     }
 }
@@ -156,7 +237,7 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
     __shared__ int s_abort;
     __shared__ DqWork s_work[kSlots];
     __shared__ float s_row[kSlots][kGroups][kTile];     // (a warp may be in the next work already)
-    __shared__ __align__(16) float s_stats[kSlots][2][kTile];
+    __shared__ __align__(16) float s_stats[kSlots][kStats][kTile];
     const sieve_attention_args &a = f.p.a;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = lane_id();
 
@@ -271,8 +352,9 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
             // products alone let the next pair in, and a warp that had not
             // looked yet would find its phase gone.)
             if (elected()) {
-                expect(&stat_full[slot], 2 * kTile * 4);
-                tc::bulk_g2s(1u, s_stats[slot], f.stats + (int64_t)w.stats * 2 * kTile, 2 * kTile * 4, &stat_full[slot]);
+                expect(&stat_full[slot], kStats * kTile * 4);
+                tc::bulk_g2s(1u, s_stats[slot], f.stats + (int64_t)w.stats * stat_rows(BIAS) * kTile, kStats * kTile * 4,
+                             &stat_full[slot]);
             }
             __syncwarp();
             ++stats_issued;
@@ -419,7 +501,9 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
             const int64_t row = w.q_row + w.row0 + r;
             const float *table = bias + slot * bias_set;
             if (!(ok = wait.warp(&stat_full[slot], (uint32_t)(item / kSlots) & 1u))) break;
-            const float nl = s_stats[slot][0][r] - (float)kPShift<T>;
+            const bool far = BIAS && is_far(s_stats[slot][0][r]), any_far = BIAS && __any_sync(0xffffffffu, far);
+            const float nl = far ? 0.f : s_stats[slot][0][r] - (float)kPShift<T>;
+            float *const stats = f.stats + (int64_t)w.stats * stat_rows(BIAS) * kTile + r;    // this row's
             const float minus_delta = s_stats[slot][1][r] * (float)(1 << kPShift<T>);
             float2 sum2 = both(0.f);
 #pragma unroll 1
@@ -456,6 +540,12 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
                             x[2 * e] = fma2(x[2 * e], both(c), add2(make_float2(b.x, b.y), both(nl)));
                             x[2 * e + 1] = fma2(x[2 * e + 1], both(c), add2(make_float2(b.z, b.w), both(nl)));
                         }
+                    }
+                    if (any_far) {
+                        const float top = far ? stats[2 * kTile] : 0.f;
+                        const float rest = far ? stats[3 * kTile] - (float)kPShift<T> : 0.f;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) x[e] = add2(add2(x[e], both(top)), both(rest));
                     }
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
@@ -521,7 +611,7 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
                 float sum = 0.f;
 #pragma unroll
                 for (int k = 0; k < kGroups; ++k) sum += s_row[slot][k][r];
-                f.stats[(int64_t)w.stats * 2 * kTile + kTile + r] = (minus_delta - sum) * (1.f / (float)(1 << kPShift<T>));
+                stats[kTile] = (minus_delta - sum) * (1.f / (float)(1 << kPShift<T>));
             }
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&work_empty[slot]);
@@ -553,7 +643,7 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
     constexpr uint32_t kTileBytes = kB * kBlockBytes;
     constexpr uint32_t kSCol = 0, kDpCol = 128, kDvCol = 256, kDkCol = 384;   // P in S's place, dS in dP's
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(16) float s_stats[kWalked][2][kTile];
+    __shared__ __align__(16) float s_stats[kWalked][kStats][kTile];
     __shared__ __align__(8) uint64_t kv_full[kKept], kv_empty[kKept], q_full[kWalked], q_empty[kWalked], s_full, p_full,
         dp_full, ds_full, acc_full, meet_bar, done, work_full[kSlots], work_empty[kSlots], steal_bar;
     __shared__ __align__(16) uint4 s_answer;
@@ -684,13 +774,13 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
                 const int st = q_issued % kWalked, row = w.q_row + qt * kTile;
                 if (!(ok = wait.warp(&q_empty[st], ((uint32_t)(q_issued / kWalked) & 1u) ^ 1u))) break;
                 if (elected()) {
-                    expect(&q_full[st], 2 * kTileBytes + 2 * kTile * 4);
+                    expect(&q_full[st], 2 * kTileBytes + kStats * kTile * 4);
                     for (int b = 0; b < kB; ++b) {
                         tma_load(qd + st * 2 * kTileBytes + b * kBlockBytes, &f.q, 64 * b, head, row, &q_full[st]);
                         tma_load(qd + (st * 2 + 1) * kTileBytes + b * kBlockBytes, &f.dout, 64 * b, head, row, &q_full[st]);
                     }
-                    tc::bulk_g2s(1u, s_stats[st], f.stats + ((int64_t)(w.q_number + qt) * a.heads + head) * 2 * kTile,
-                                 2 * kTile * 4, &q_full[st]);
+                    tc::bulk_g2s(1u, s_stats[st], f.stats + ((int64_t)(w.q_number + qt) * a.heads + head) * stat_rows(BIAS) * kTile,
+                                 kStats * kTile * 4, &q_full[st]);
                 }
                 __syncwarp();
                 ++q_issued;
@@ -853,6 +943,8 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
                         tc::tmem_ld32_issue(lane_base + kSCol + group * kCols, raw);
                         const float4 *nl = reinterpret_cast<const float4 *>(&s_stats[st][0][group * kCols]);
                         const int hi = key_lo + 31 - place0, lo = hi - 62;
+                        const bool any_far =
+                            BIAS && __any_sync(0xffffffffu, is_far(s_stats[st][0][group * kCols + lane]));
                         tc::tmem_ld_wait(raw);
                         if (!BIAS || lo >= a.reach || hi <= -a.reach) {
                             const float b =
@@ -880,6 +972,16 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
                                                    add2(make_float2(x.x, x.y), make_float2(b.x, b.y)));
                                 p[2 * e + 1] = fma2(make_float2(__uint_as_float(raw[4 * e + 2]), __uint_as_float(raw[4 * e + 3])), both(c),
                                                        add2(make_float2(x.z, x.w), make_float2(b.z, b.w)));
+                            }
+                        }
+                        if (any_far) {
+                            const float *top = f.stats + 2 * kTile + group * kCols + lane +
+                                               ((int64_t)(w.q_number + qt) * a.heads + head) * stat_rows(BIAS) * kTile;
+                            const float t = top[0], u = top[kTile];
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                p[e].x = (p[e].x + __shfl_sync(0xffffffffu, t, 2 * e)) + __shfl_sync(0xffffffffu, u, 2 * e);
+                                p[e].y = (p[e].y + __shfl_sync(0xffffffffu, t, 2 * e + 1)) + __shfl_sync(0xffffffffu, u, 2 * e + 1);
                             }
                         }
 #pragma unroll
@@ -1075,7 +1177,7 @@ Layout layout_of(const sieve_attention_args &a) {
     l.entries = a.num_buckets ? bias_entries(a.reach) : 0;
     l.splits = (int)(l.k_tiles < 16 * 64 ? ceil_div(l.k_tiles, 16) : 64);
     l.stats = kCtlBytes;
-    l.partial = l.stats + (size_t)l.q_tiles * a.heads * 2 * kTile * sizeof(float);
+    l.partial = l.stats + (size_t)l.q_tiles * a.heads * stat_rows(a.num_buckets) * kTile * sizeof(float);
     l.split_sums = l.partial + (size_t)round_up(l.k_tiles * a.heads * l.entries * (int64_t)sizeof(float), 256);
     l.total = l.split_sums + (size_t)round_up((int64_t)a.heads * l.splits * l.entries * (int64_t)sizeof(float), 256);
     return l;
@@ -1101,7 +1203,7 @@ cudaError_t run(const BwdArgs &f, const Layout &l, unsigned char *ws, cudaStream
     constexpr int kMost = SIEVE_ATTENTION_MAX_REACH;
     cudaError_t e;
     if (a.q_tokens > 0) {
-        k_attend_delta<T, DP / 8><<<(unsigned)(l.q_tiles * a.heads), kDeltaThreads, 0, st>>>(f);
+        k_attend_delta<T, DP / 8, BIAS><<<(unsigned)(l.q_tiles * a.heads), kDeltaThreads, 0, st>>>(f);
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
         auto dq = k_attend_dq<T, DP, BIAS>;
         if ((e = cudaFuncSetAttribute(dq, kLimit, (int)dq_smem<DP, BIAS>(kMost))) != cudaSuccess) return e;

@@ -78,6 +78,13 @@ struct FwdArgs {
     float2 *part_ml;     // split: [chunk number][head groups][rows]: maximum (base 2), sum
 };
 
+// The log of a row's sum from its maximum in base 2 and its sum.  A bias at the
+// end of the type's range stands there in base 2 as well (see scaled_bias), and
+// so does its row's lse.
+__device__ __forceinline__ float lse_of(float m, float l) {
+    return fabsf(m) == FLT_MAX ? m : (m + log2_approx(l)) * kLn2;
+}
+
 // False where the block's number is one that no document uses.
 template <bool SPLIT>
 __device__ __forceinline__ bool find_work(const FwdArgs &f, DocFinder &find, int t, Work &w) {
@@ -533,7 +540,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
                 const int64_t row = w.q_row + qi;                                                             // not split
                 if (live && half == 0) {
                     if (SPLIT) f.part_ml[at] = make_float2(m, l);
-                    else f.p.lse[(int64_t)head * a.q_tokens + row] = none ? -INFINITY : (m + log2_approx(l)) * kLn2;
+                    else f.p.lse[(int64_t)head * a.q_tokens + row] = none ? -INFINITY : lse_of(m, l);
                 }
 #pragma unroll
                 for (int i = 0; i < DP / 64; ++i) {
@@ -601,7 +608,7 @@ __global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ Fwd
         acc[2] = fmaf(o.z, e, acc[2]);
         acc[3] = fmaf(o.w, e, acc[3]);
     }
-    if (lane == 0) f.p.lse[(int64_t)head * a.q_tokens + row] = l == 0.f ? -INFINITY : top * kLn2 + logf(l);
+    if (lane == 0) f.p.lse[(int64_t)head * a.q_tokens + row] = l == 0.f ? -INFINITY : fabsf(top) == FLT_MAX ? top : top * kLn2 + logf(l);
     if (4 * lane < d) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
         uint2 o;

@@ -9,7 +9,7 @@ import torch
 import encoder_reference as ref
 import paper_2608_03199_gb300 as sieve
 from paper_2608_03199_gb300.encoder import AttentionArgsC
-from test_gpu_encoder import BF16, DEV, FP16, attention_inputs, check_attention, gen, randn
+from test_gpu_encoder import BF16, DEV, FP16, FP32, attention_inputs, check_attention, gen, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -184,3 +184,56 @@ def test_host_threads_with_tables_of_different_reach():
     assert not codes, codes
     for *_, got, want, _ in jobs:
         assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+LOWEST = torch.finfo(FP32).min
+
+
+@pytest.mark.parametrize("value", [LOWEST, -LOWEST, -1e30, 1e30])
+@pytest.mark.parametrize("dim,dtype,causal", [(64, BF16, False), (64, FP16, True), (128, FP16, False), (96, BF16, True)])
+def test_biases_beside_which_scores_vanish(dim, dtype, causal, value):
+    """Biases so large that adding the score changes nothing, in 64 bits
+    either: the keys that carry the row's largest share its weight evenly, and
+    the gradients follow.  One head all of that value; one where it stands at
+    the near buckets alone, so that some rows see nothing else; one without."""
+    n = [200, 1, 0, 2, 130]
+    q, k, v, dout, table, bmap = attention_inputs(51, n, n, 3, 3, dim, dtype, 32, 64, causal)
+    table[:, 0] = value
+    table[bmap[64 - 2:64 + 3].long().unique(), 1] = value
+    out, lse, dq, dk, dv, dtable = check_attention(q, k, v, dout, n, n, table, bmap, causal)
+    assert lse[:2].isfinite().logical_or(lse[:2] == -torch.inf).all()
+    off = ref.offsets_of(n, DEV)
+    again = sieve.attention_backward(dout, q, k, v, out, lse, off, table=table, buckets=bmap, causal=causal)
+    assert all(torch.equal(a, b) for a, b in zip(again, (dq, dk, dv, dtable)))
+
+
+@pytest.mark.parametrize("value", [LOWEST, -1e30])
+def test_new_tokens_with_biases_beside_which_scores_vanish(value):
+    klen = [300, 0, 1, 129]
+    qlen = [3] * 4
+    q, k, v, dout, table, bmap = attention_inputs(52, qlen, klen, 4, 2, 64, BF16, 32, 64, True)
+    table[:, 1] = value
+    off, kw = ref.offsets_of(klen, DEV), dict(table=table, buckets=bmap, causal=True, check=True)
+    out, lse = sieve.attention(q.view(4, 3, 4, 64), k, v, off, **kw)
+    grads = sieve.attention_backward(dout.view(4, 3, 4, 64), q.view(4, 3, 4, 64), k, v, out, lse, off, **kw)
+    want, bound = ref.attention(q, k, v, qlen, klen, table, bmap, True, None, dout)
+    for name, got in zip(("out", "lse", "dq", "dk", "dv", "dtable"), (out, lse, *grads)):
+        ref.assert_within(got.reshape(want[name].shape), want[name], bound[name], name)
+
+
+@pytest.mark.parametrize("value", [-3e4, -1e6, -1e9, -1e30, LOWEST, 1e6, 1e9])
+def test_probabilities_of_a_row_add_up_to_one_under_any_bias(value):
+    """With dout = 1 every column of dv adds up to the number of queries.  In
+    fp16 P is off by 2^-11, dv by as much again; a score that rounds to another
+    fp32 neighbour in the two passes moves single P, not their sum's 2^-10."""
+    n = [200, 130]
+    q, k, v, dout, table, bmap = attention_inputs(53, n, n, 2, 1, 64, FP16, 32, 64, False)
+    table += value if value > LOWEST / 2 else 0
+    if value <= LOWEST / 2:
+        table[:] = value
+    off, kw = ref.offsets_of(n, DEV), dict(table=table, buckets=bmap, check=True)
+    out, lse = sieve.attention(q, k, v, off, **kw)
+    dv = sieve.attention_backward(torch.ones_like(dout), q, k, v, out, lse, off, **kw)[2]
+    for a, b in ((0, 200), (200, 330)):
+        total = dv[a:b].double().sum(0) / (2 * (b - a))        # two heads share the key head
+        assert ((total - 1).abs() <= 2 * ref.U[FP16] + 2.0 ** -10).all(), float(total.mean())
