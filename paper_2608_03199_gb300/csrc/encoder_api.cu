@@ -81,6 +81,12 @@ sieve_attention_args resolved(const sieve_attention_args *a) {
     return r;
 }
 
+// The status word of a call that launches no kernel to write it.
+sieve_status nothing_to_do(void *ws, cudaStream_t st) {
+    ENC_CUDA(cudaMemsetAsync(ws, 0, sizeof(EncCtl), st));
+    return SIEVE_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -176,7 +182,7 @@ sieve_status sieve_attention(const sieve_attention_args *a, void *out, float *ls
     if (a->q_tokens > 0 && (!out || !lse || !aligned_to(out, 16) || !aligned4(lse))) return SIEVE_EINVAL;
     if ((rc = check_workspace(ws, ws_bytes, attention_workspace_bytes(resolved(a)))) != SIEVE_OK) return rc;
     if ((rc = check_current_device()) != SIEVE_OK) return rc;
-    if (a->q_tokens == 0) return SIEVE_OK;
+    if (a->q_tokens == 0) return nothing_to_do(ws, static_cast<cudaStream_t>(stream));
     AttentionArgs p = {};
     p.a = resolved(a);
     p.out = out;
@@ -208,6 +214,8 @@ sieve_status sieve_attention_backward(const sieve_attention_args *a, const void 
     if ((a->table && !dtable) || !aligned4(dtable)) return SIEVE_EINVAL;
     if ((rc = check_workspace(ws, ws_bytes, attention_backward_workspace_bytes(resolved(a)))) != SIEVE_OK) return rc;
     if ((rc = check_current_device()) != SIEVE_OK) return rc;
+    if (a->q_tokens == 0 && a->k_tokens == 0)
+        if ((rc = nothing_to_do(ws, static_cast<cudaStream_t>(stream))) != SIEVE_OK) return rc;
     AttentionArgs p = {};
     p.a = resolved(a);
     p.dout = dout;

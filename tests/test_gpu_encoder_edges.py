@@ -237,3 +237,21 @@ def test_probabilities_of_a_row_add_up_to_one_under_any_bias(value):
     for a, b in ((0, 200), (200, 330)):
         total = dv[a:b].double().sum(0) / (2 * (b - a))        # two heads share the key head
         assert ((total - 1).abs() <= 2 * ref.U[FP16] + 2.0 ** -10).all(), float(total.mean())
+
+
+def test_status_of_a_call_without_work():
+    """A call that launches nothing leaves the status word of a call that went well."""
+    lib, off = sieve.lib(), torch.zeros(3, dtype=torch.int32, device=DEV)
+    t = torch.zeros(64, dtype=BF16, device=DEV)
+    a = AttentionArgsC(dtype=2, heads=1, kv_heads=1, head_dim=64, nseq=2, scale=1.0, k_offsets=off.data_ptr(), q=t.data_ptr(),
+                       k=t.data_ptr(), v=t.data_ptr(), q_token_stride=64, q_head_stride=64, k_token_stride=64,
+                       k_head_stride=64, v_token_stride=64, v_head_stride=64)
+    stream = torch.cuda.current_stream().cuda_stream
+    strides = (C.c_int64 * 6)(*[64] * 6)
+    p = t.data_ptr()
+    for call in (lambda ws: lib.sieve_attention(C.byref(a), p, p, ws.data_ptr(), ws.numel(), stream),
+                 lambda ws: lib.sieve_attention_backward(C.byref(a), p, p, p, p, p, p, strides, None, ws.data_ptr(),
+                                                         ws.numel(), stream)):
+        ws = torch.full((1 << 16,), 0xFF, dtype=torch.uint8, device=DEV)
+        assert call(ws) == 0
+        assert sieve.encoder_status(ws, stream) == 0
