@@ -141,7 +141,9 @@ __global__ void __launch_bounds__(kThreads) k_pool_backward(const PoolArgs a) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
             const int col = c * VEC + e;
-            v[e] = norm != 0.f ? (g[col] - d * u[col]) * scale : 0.f;
+            // (a norm below 2^-128 has no reciprocal; 0 times infinity is NaN)
+            const float x = g[col] - d * u[col];
+            v[e] = norm == 0.f ? 0.f : isinf(scale) ? x / norm / (float)len : x * scale;
         }
         for (int r = strand; r < n; r += strands) store_vec<T, VEC>(out + (int64_t)r * a.stride + c * VEC, v);
     }

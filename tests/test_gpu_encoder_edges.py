@@ -255,3 +255,18 @@ def test_status_of_a_call_without_work():
         ws = torch.full((1 << 16,), 0xFF, dtype=torch.uint8, device=DEV)
         assert call(ws) == 0
         assert sieve.encoder_status(ws, stream) == 0
+
+
+def test_unit_pool_gradient_of_the_smallest_means():
+    """A mean below 2^-128 has no reciprocal in fp32; a document whose rows
+    get no gradient has none all the same, and others what fp32 can hold."""
+    h = torch.zeros(4, 96, device=DEV)
+    h[:, 0] = 1e-39
+    off = ref.offsets_of([3, 1], DEV)
+    rows, norms = sieve.unit_pool(h, off)
+    drows = torch.zeros(2, 96, device=DEV)
+    drows[1, 1] = 0.125
+    dh = sieve.unit_pool_backward(drows, rows, norms, off, 4)
+    want = torch.zeros(4, 96, device=DEV, dtype=torch.float64)
+    want[3, 1] = 0.125 / norms[1].double()
+    ref.assert_within(dh, want, 2.0 ** -21 * want, "dh")
