@@ -46,20 +46,31 @@ namespace {
 constexpr int kSlots = 2;      // the work in hand and the next
 constexpr int kShort = 16;     // steps of work that is short
 
-// k_attend_dkv rounds P to 16 bits.  A long document's probabilities are small
-// and fp16 has no bits below 2^-24, so it takes 2^14 P there (P <= 1 up to the
-// rounding of lse), and dV is scaled back; dS = 2^14 P (2^-14 dP - 2^-14
-// delta) costs no operation more.  dS itself stays as it is: its size is the
-// caller's, and a factor could overflow what would not (fp16 gradients want a
-// scaled loss).
+// fp16 has no bits below 2^-24, and a long document's P and dS are small.  So
+// k_attend_dkv takes 2^14 P (P <= 1 up to the rounding of lse) and scales dV
+// back, and both kernels round dS times a power of two that its row (dq) or
+// document (dk) cannot overflow with, and scale dQ and dK back.  The bound:
+// |dS| <= |dP| + |delta| <= 2 |dout| |v| for the row's dout and the document's
+// longest v (O is a mean of v), so the power is 2^14 over the next one above it.
+// (Unscaled, dout of 1e-2 on 12,288 tokens left dq and dk off by 1.6e-3 of their
+// norm, of 1e-3 by 1.6e-2; rounding the results alone takes 2.1e-4 and 1.1e-3.)
 template <typename T>
 constexpr int kPShift = std::is_same_v<T, __half> ? 14 : 0;
+template <typename T>
+constexpr bool kScaled = std::is_same_v<T, __half>;
+__device__ __forceinline__ float power_for(float bound) {
+    if (!(bound > 0.f) || isinf(bound)) return 1.f;
+    const int e = (__float_as_int(bound) >> 23) - 126;      // bound < 2^e
+    return __int_as_float((127 + min(14 - e, 100)) << 23);
+}
 
 struct BwdArgs {
     AttentionArgs p;
     CUtensorMap q, k, v, dout;
     float *stats;      // [q tile][head][stat_rows][128], see there
     float *partial;    // [k tile][head][entries]: dS by distance
+    float *values;     // fp16: [k tile][key head]: the length of the longest v
+    float *bounds;     // fp16: [q tile][head]: the largest bound of a row's dS
     int doc_tiles;     // new_tokens > 0: q tiles of a document
     int entries;       // bias_entries(reach)
     int q_numbers, k_numbers;   // tile numbers; blocks run over them head by head
@@ -70,14 +81,15 @@ struct BwdArgs {
 constexpr int kWalked = 2;
 __host__ __device__ constexpr int kept(int dp) { return dp == 64 ? 2 : 1; }
 
-// Row statistics, 128 to a row: kPShift - lse in base 2; -2^-kPShift delta.  With
-// a table two more, where the tile has a far query (see far_statistics): minus
-// its largest score in base 2 and kPShift - log2 of the sum of the 2^(score -
-// largest), zeros for the others.  A far query's first one is minus zero: its
-// mark, which changes no sum.  The kernels hold the first two rows of a tile; the
-// others are read where they lie.
-constexpr int kStats = 2;
-__host__ __device__ constexpr int stat_rows(bool bias) { return bias ? 4 : kStats; }
+// Row statistics, 128 to a row: kPShift - lse in base 2; -2^-kPShift delta; in
+// fp16 the power of two of its dS.  With a table two more, where the tile has a
+// far query (see far_statistics): minus its largest score in base 2 and kPShift -
+// log2 of the sum of the 2^(score - largest), zeros for the others.  A far query's
+// first one is minus zero: its mark, which changes no sum.  The kernels hold the
+// rows up to those two, which are read where they lie.
+constexpr int kStats = 2;                                               // what k_attend_dkv holds
+__host__ __device__ constexpr int held(bool scaled) { return kStats + (scaled ? 1 : 0); }   // k_attend_dq
+__host__ __device__ constexpr int stat_rows(bool scaled, bool bias) { return held(scaled) + (bias ? 2 : 0); }
 __device__ __forceinline__ bool is_far(float stat) { return __float_as_uint(stat) == 0x80000000u; }
 
 // The threads that compute meet: bounded like every wait, so a warp that gave
@@ -103,6 +115,7 @@ struct DqWork {
 };
 struct DkvWork {
     int hk, k_row, key0, nk, q_row, nq, q_first, q_tiles, q_number, number;   // hk < 0: no more
+    float power;                                                              // of dS
 };
 
 // A query all of whose keys have huge biases is far: beside 1e6 an lse in 32 bits
@@ -156,12 +169,48 @@ __device__ __noinline__ bool far_statistics(const sieve_attention_args &a, const
     return true;
 }
 
+// fp16: the length of the longest v of every tile of keys and key head.
+constexpr int kDeltaThreads = 256;
+template <typename T, int kLanes>
+__global__ void __launch_bounds__(kDeltaThreads) k_attend_values(const __grid_constant__ BwdArgs f) {
+    const sieve_attention_args &a = f.p.a;
+    __shared__ float s_most[kDeltaThreads / 32];
+    const int t = blockIdx.x / a.kv_heads, head = blockIdx.x % a.kv_heads;
+    const int s = find_doc(a.k_offsets, (int)a.nseq, (int)a.k_tokens, kTile, t);
+    int first, len;
+    doc_range(a.k_offsets, s, (int)a.k_tokens, first, len);
+    const int r0 = (t - first_tile(a.k_offsets, s, (int)a.k_tokens, kTile)) * kTile;
+    if (r0 < 0 || r0 >= len) return;
+    const int rows = min(kTile, len - r0), piece = threadIdx.x % kLanes;
+    const T *v = static_cast<const T *>(a.v) + (int64_t)(first + r0) * a.v_token_stride + head * a.v_head_stride + piece * 8;
+    constexpr int kRows = kDeltaThreads / kLanes;
+    float most = 0.f;
+#pragma unroll
+    for (int i = 0; i < kTile / kRows; ++i) {
+        const int r = i * kRows + threadIdx.x / kLanes;
+        float x[8], sum = 0.f;
+        if (r < rows && piece * 8 < a.head_dim) {
+            load_vec<T, 8>(v + (int64_t)r * a.v_token_stride, x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
+        }
+#pragma unroll
+        for (int k = kLanes / 2; k; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+        most = fmaxf(most, sum);
+    }
+    most = warp_max(most);
+    if (lane_id() == 0) s_most[threadIdx.x >> 5] = most;
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+    most = warp_max(threadIdx.x < kDeltaThreads / 32 ? s_most[threadIdx.x] : 0.f);
+    if (threadIdx.x == 0) f.values[(int64_t)t * a.kv_heads + head] = sqrtf(most);
+}
+
 // delta = dO . O of every query, and -lse in base 2: a block per tile and head,
 // 8 or 16 lanes to a row.  (Inside k_attend_dq, with a row to a thread, the same
 // reads took 3K to 9K cycles of every block's time.)
-constexpr int kDeltaThreads = 256;
 template <typename T, int kLanes, bool BIAS>
-__global__ void __launch_bounds__(kDeltaThreads, 8) k_attend_delta(const __grid_constant__ BwdArgs f) {
+__global__ void __launch_bounds__(kDeltaThreads, kScaled<T> ? 6 : 8) k_attend_delta(const __grid_constant__ BwdArgs f) {
     const sieve_attention_args &a = f.p.a;
     if (blockIdx.x == 0 && threadIdx.x == 0) f.p.ctl->status = 0;
     const int t = blockIdx.x / a.heads, head = blockIdx.x % a.heads;
@@ -177,24 +226,38 @@ __global__ void __launch_bounds__(kDeltaThreads, 8) k_attend_delta(const __grid_
     if (tile < 0 || tile * kTile >= doc.nq) return;
     const int64_t row0 = doc.q0 + tile * kTile;
     const int rows = min(kTile, doc.nq - tile * kTile);
-    float *stats = f.stats + ((int64_t)t * a.heads + head) * stat_rows(BIAS) * kTile;
+    constexpr int kHeld = held(kScaled<T>);
+    float *stats = f.stats + ((int64_t)t * a.heads + head) * stat_rows(kScaled<T>, BIAS) * kTile;
     const int piece = threadIdx.x % kLanes, d = a.head_dim;
     const T *o = static_cast<const T *>(f.p.out_in) + (row0 * a.heads + head) * d + piece * 8;
     const T *g = static_cast<const T *>(f.p.dout) + (row0 * a.heads + head) * d + piece * 8;
     constexpr int kRows = kDeltaThreads / kLanes;
     uint32_t may_be_far = 0;      // of this thread's rows, one bit each
+    // the document's longest v: its first tiles' are asked for here, and looked at
+    // once the rows are in hand
+    const int k_tiles = (doc.nk + kTile - 1) / kTile, lane = lane_id();
+    const float *values = f.values + (int64_t)(doc.k0 / kTile + s) * a.kv_heads + head / (a.heads / a.kv_heads);
+    float longest = kScaled<T> && lane < k_tiles ? values[(int64_t)lane * a.kv_heads] : 0.f, most = 0.f;
+    float square[kScaled<T> ? kTile / kRows : 1];
 #pragma unroll
     for (int i = 0; i < kTile / kRows; ++i) {
         const int r = i * kRows + threadIdx.x / kLanes;
-        float x[8], y[8], part = 0.f;
+        float x[8], y[8], part = 0.f, sum = 0.f;
         if (r < rows && piece * 8 < d) {
             load_vec<T, 8>(o + (int64_t)r * a.heads * d, x);
             load_vec<T, 8>(g + (int64_t)r * a.heads * d, y);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) part = fmaf(x[e], y[e], part);
+            for (int e = 0; e < 8; ++e) {
+                part = fmaf(x[e], y[e], part);
+                if (kScaled<T>) sum = fmaf(y[e], y[e], sum);
+            }
         }
 #pragma unroll
-        for (int k = kLanes / 2; k; k >>= 1) part += __shfl_xor_sync(0xffffffffu, part, k);
+        for (int k = kLanes / 2; k; k >>= 1) {
+            part += __shfl_xor_sync(0xffffffffu, part, k);
+            if (kScaled<T>) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+        }
+        if (kScaled<T>) square[i] = sum;
         if (piece == 0) {
             const float lse = r < rows ? f.p.lse_in[(int64_t)head * a.q_tokens + row0 + r] : -INFINITY;
             stats[r] = lse == -INFINITY ? -INFINITY : (float)kPShift<T> - lse * kLog2e + 0.f;   // (no minus zero)
@@ -202,8 +265,27 @@ __global__ void __launch_bounds__(kDeltaThreads, 8) k_attend_delta(const __grid_
             if (BIAS && fabsf(lse) > kFar && !isinf(lse)) may_be_far |= 1u << i;
         }
     }
+    if constexpr (kScaled<T>) {
+        __shared__ float s_most[kDeltaThreads / 32];
+        for (int i = lane + 32; i < k_tiles; i += 32) longest = fmaxf(longest, values[(int64_t)i * a.kv_heads]);
+        longest = 2.f * warp_max(longest);
+#pragma unroll
+        for (int i = 0; i < kTile / kRows; ++i) {
+            const float bound = sqrtf(square[i]) * longest;
+            most = fmaxf(most, bound);
+            if (piece == 0) stats[2 * kTile + i * kRows + threadIdx.x / kLanes] = power_for(bound);
+        }
+        most = warp_max(most);
+        if (lane_id() == 0) s_most[threadIdx.x >> 5] = most;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+#pragma unroll
+            for (int k = 1; k < kDeltaThreads / 32; ++k) most = fmaxf(most, s_most[k]);
+            f.bounds[(int64_t)t * a.heads + head] = most;
+        }
+    }
     if (!BIAS || !__syncthreads_or(may_be_far)) return;
-    stats[2 * kTile + threadIdx.x] = 0.f;
+    stats[kHeld * kTile + threadIdx.x] = 0.f;
     static_assert(kDeltaThreads == 2 * kTile, "");
     __syncthreads();
 #pragma unroll 1
@@ -216,8 +298,8 @@ __global__ void __launch_bounds__(kDeltaThreads, 8) k_attend_delta(const __grid_
             continue;
         if (lane_id() == (uint32_t)from) {
             stats[r] = -0.f;
-            stats[2 * kTile + r] = -top;
-            stats[3 * kTile + r] = (float)kPShift<T> - log2_sum;
+            stats[kHeld * kTile + r] = -top;
+            stats[(kHeld + 1) * kTile + r] = (float)kPShift<T> - log2_sum;
         }
     }
 }
@@ -237,7 +319,8 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
     __shared__ int s_abort;
     __shared__ DqWork s_work[kSlots];
     __shared__ float s_row[kSlots][kGroups][kTile];     // (a warp may be in the next work already)
-    __shared__ __align__(16) float s_stats[kSlots][kStats][kTile];
+    constexpr int kHeld = held(kScaled<T>), kStatRows = stat_rows(kScaled<T>, BIAS);
+    __shared__ __align__(16) float s_stats[kSlots][kHeld][kTile];
     const sieve_attention_args &a = f.p.a;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = lane_id();
 
@@ -352,8 +435,8 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
             // products alone let the next pair in, and a warp that had not
             // looked yet would find its phase gone.)
             if (elected()) {
-                expect(&stat_full[slot], kStats * kTile * 4);
-                tc::bulk_g2s(1u, s_stats[slot], f.stats + (int64_t)w.stats * stat_rows(BIAS) * kTile, kStats * kTile * 4,
+                expect(&stat_full[slot], kHeld * kTile * 4);
+                tc::bulk_g2s(1u, s_stats[slot], f.stats + (int64_t)w.stats * kStatRows * kTile, kHeld * kTile * 4,
                              &stat_full[slot]);
             }
             __syncwarp();
@@ -503,7 +586,8 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
             if (!(ok = wait.warp(&stat_full[slot], (uint32_t)(item / kSlots) & 1u))) break;
             const bool far = BIAS && is_far(s_stats[slot][0][r]), any_far = BIAS && __any_sync(0xffffffffu, far);
             const float nl = far ? 0.f : s_stats[slot][0][r] - (float)kPShift<T>;
-            float *const stats = f.stats + (int64_t)w.stats * stat_rows(BIAS) * kTile + r;    // this row's
+            float *const stats = f.stats + (int64_t)w.stats * kStatRows * kTile + r;    // this row's
+            const float power = kScaled<T> ? s_stats[slot][kHeld - 1][r] : 1.f;
             const float minus_delta = s_stats[slot][1][r] * (float)(1 << kPShift<T>);
             float2 sum2 = both(0.f);
 #pragma unroll 1
@@ -542,8 +626,8 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
                         }
                     }
                     if (any_far) {
-                        const float top = far ? stats[2 * kTile] : 0.f;
-                        const float rest = far ? stats[3 * kTile] - (float)kPShift<T> : 0.f;
+                        const float top = far ? stats[kHeld * kTile] : 0.f;
+                        const float rest = far ? stats[(kHeld + 1) * kTile] - (float)kPShift<T> : 0.f;
 #pragma unroll
                         for (int e = 0; e < 16; ++e) x[e] = add2(add2(x[e], both(top)), both(rest));
                     }
@@ -569,7 +653,8 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
                     for (int e = 0; e < 16; ++e) {
                         x[e] = mul2(x[e], add2(make_float2(dp[2 * e], dp[2 * e + 1]), both(minus_delta)));
                         if (BIAS) sum2 = add2(sum2, x[e]);
-                        pk[e] = pack2<T>(x[e].x, x[e].y);
+                        const float2 y = kScaled<T> ? mul2(x[e], both(power)) : x[e];
+                        pk[e] = pack2<T>(y.x, y.y);
                     }
                 } else {
                     // no row of the warp sees these; the product reads them
@@ -592,13 +677,14 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dq(const __grid_constant_
                 constexpr int kOut = DP / kGroups;       // 16 or 32 columns of dQ
                 const int col = group * kOut;
                 uint4 c[kOut / 8];
+                const float back = kScaled<T> ? a.scale / power : a.scale;
 #pragma unroll
                 for (int i = 0; i < kOut / 16; ++i) {
                     uint32_t o[16];
                     tmem_ld16(lane_base + kDqCol + col + 16 * i, o);
                     float v[16];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) v[e] = nl != -INFINITY ? __uint_as_float(o[e]) * a.scale : 0.f;
+                    for (int e = 0; e < 16; ++e) v[e] = nl != -INFINITY ? __uint_as_float(o[e]) * back : 0.f;
                     c[2 * i] = pack8<T>(v);
                     c[2 * i + 1] = pack8<T>(v + 8);
                 }
@@ -643,6 +729,7 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
     constexpr uint32_t kTileBytes = kB * kBlockBytes;
     constexpr uint32_t kSCol = 0, kDpCol = 128, kDvCol = 256, kDkCol = 384;   // P in S's place, dS in dP's
     extern __shared__ unsigned char smem_raw[];
+    constexpr int kStatRows = stat_rows(kScaled<T>, BIAS);
     __shared__ __align__(16) float s_stats[kWalked][kStats][kTile];
     __shared__ __align__(8) uint64_t kv_full[kKept], kv_empty[kKept], q_full[kWalked], q_empty[kWalked], s_full, p_full,
         dp_full, ds_full, acc_full, meet_bar, done, work_full[kSlots], work_empty[kSlots], steal_bar;
@@ -727,6 +814,13 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
                     w.q_row = doc.q0;
                     w.nq = doc.nq;
                     w.q_number = a.new_tokens > 0 ? s * f.doc_tiles : doc.q0 / kTile + s;
+                    if (kScaled<T>) {
+                        float most = 0.f;
+                        for (int i = lane; i < w.q_tiles * share; i += 32)
+                            most = fmaxf(most, f.bounds[(int64_t)(w.q_number + w.q_first + i / share) * a.heads + hk * share +
+                                                        i % share]);
+                        w.power = power_for(warp_max(most));
+                    }
                     if (w.q_tiles * share <= kShort) blocks.ask();
                     return true;
                 }
@@ -779,7 +873,7 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
                         tma_load(qd + st * 2 * kTileBytes + b * kBlockBytes, &f.q, 64 * b, head, row, &q_full[st]);
                         tma_load(qd + (st * 2 + 1) * kTileBytes + b * kBlockBytes, &f.dout, 64 * b, head, row, &q_full[st]);
                     }
-                    tc::bulk_g2s(1u, s_stats[st], f.stats + ((int64_t)(w.q_number + qt) * a.heads + head) * stat_rows(BIAS) * kTile,
+                    tc::bulk_g2s(1u, s_stats[st], f.stats + ((int64_t)(w.q_number + qt) * a.heads + head) * kStatRows * kTile,
                                  kStats * kTile * 4, &q_full[st]);
                 }
                 __syncwarp();
@@ -975,8 +1069,8 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
                             }
                         }
                         if (any_far) {
-                            const float *top = f.stats + 2 * kTile + group * kCols + lane +
-                                               ((int64_t)(w.q_number + qt) * a.heads + head) * stat_rows(BIAS) * kTile;
+                            const float *top = f.stats + held(kScaled<T>) * kTile + group * kCols + lane +
+                                               ((int64_t)(w.q_number + qt) * a.heads + head) * kStatRows * kTile;
                             const float t = top[0], u = top[kTile];
 #pragma unroll
                             for (int e = 0; e < 16; ++e) {
@@ -1021,7 +1115,10 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
                                 mul2(p[2 * e + 1], fma2(make_float2(dp[4 * e + 2], dp[4 * e + 3]), both(kDown), make_float2(x.z, x.w)));
                         }
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) pk[e] = pack2<T>(p[e].x, p[e].y);
+                        for (int e = 0; e < 16; ++e) {
+                            const float2 y = kScaled<T> ? mul2(p[e], both(w.power)) : p[e];
+                            pk[e] = pack2<T>(y.x, y.y);
+                        }
                     }
                     tc::tmem_st16(lane_base + kDpCol + group * kCols, pk);   // (zeros where none)
                     tc::tmem_st_wait();
@@ -1102,7 +1199,7 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
             const int64_t stride = is_k ? f.p.dk_ts : f.p.dv_ts;
             T *out = is_k ? static_cast<T *>(f.p.dk) + row * stride + w.hk * f.p.dk_hs
                           : static_cast<T *>(f.p.dv) + row * stride + w.hk * f.p.dv_hs;
-            const float scale = is_k ? a.scale : kDown;
+            const float scale = !is_k ? kDown : kScaled<T> ? a.scale / w.power : a.scale;
 #pragma unroll
             for (int i = 0; i < kOut / 32 && !idle; ++i) {
                 const int col = col0 + 32 * i;
@@ -1168,7 +1265,7 @@ __global__ void __launch_bounds__(kReduceThreads) k_attend_buckets(const __grid_
 struct Layout {
     int64_t q_tiles, k_tiles;
     int entries, splits;
-    size_t stats, partial, split_sums, total;   // byte offsets
+    size_t stats, values, bounds, partial, split_sums, total;   // byte offsets
 };
 Layout layout_of(const sieve_attention_args &a) {
     Layout l = {};
@@ -1177,9 +1274,13 @@ Layout layout_of(const sieve_attention_args &a) {
     l.entries = a.num_buckets ? bias_entries(a.reach) : 0;
     l.splits = (int)(l.k_tiles < 16 * 64 ? ceil_div(l.k_tiles, 16) : 64);
     l.stats = kCtlBytes;
-    l.partial = l.stats + (size_t)l.q_tiles * a.heads * stat_rows(a.num_buckets) * kTile * sizeof(float);
-    l.split_sums = l.partial + (size_t)round_up(l.k_tiles * a.heads * l.entries * (int64_t)sizeof(float), 256);
-    l.total = l.split_sums + (size_t)round_up((int64_t)a.heads * l.splits * l.entries * (int64_t)sizeof(float), 256);
+    const bool scaled = a.dtype == SIEVE_F16;
+    auto floats = [](int64_t n) { return (size_t)round_up(n * (int64_t)sizeof(float), 256); };
+    l.values = l.stats + floats(l.q_tiles * a.heads * stat_rows(scaled, a.num_buckets) * kTile);
+    l.bounds = l.values + (scaled ? floats(l.k_tiles * a.kv_heads) : 0);
+    l.partial = l.bounds + (scaled ? floats(l.q_tiles * a.heads) : 0);
+    l.split_sums = l.partial + floats(l.k_tiles * a.heads * l.entries);
+    l.total = l.split_sums + floats((int64_t)a.heads * l.splits * l.entries);
     return l;
 }
 
@@ -1203,6 +1304,11 @@ cudaError_t run(const BwdArgs &f, const Layout &l, unsigned char *ws, cudaStream
     constexpr int kMost = SIEVE_ATTENTION_MAX_REACH;
     cudaError_t e;
     if (a.q_tokens > 0) {
+        if constexpr (kScaled<T>)
+            if (a.k_tokens > 0) {
+                k_attend_values<T, DP / 8><<<(unsigned)(l.k_tiles * a.kv_heads), kDeltaThreads, 0, st>>>(f);
+                if ((e = cudaGetLastError()) != cudaSuccess) return e;
+            }
         k_attend_delta<T, DP / 8, BIAS><<<(unsigned)(l.q_tiles * a.heads), kDeltaThreads, 0, st>>>(f);
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
         auto dq = k_attend_dq<T, DP, BIAS>;
@@ -1247,6 +1353,8 @@ sieve_status launch_attention_backward(const AttentionArgs &p, void *ws, cudaStr
     f.p.ctl = static_cast<EncCtl *>(ws);
     f.stats = reinterpret_cast<float *>(w + l.stats);
     f.partial = reinterpret_cast<float *>(w + l.partial);
+    f.values = reinterpret_cast<float *>(w + l.values);
+    f.bounds = reinterpret_cast<float *>(w + l.bounds);
     f.doc_tiles = a.new_tokens > 0 ? (int)ceil_div(a.new_tokens, kTile) : 0;
     f.entries = l.entries;
     f.q_numbers = (int)l.q_tiles;

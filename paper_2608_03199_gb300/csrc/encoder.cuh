@@ -98,6 +98,12 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
+
 // The rows of document s among `tokens` packed rows, clamped into the array.
 __device__ __forceinline__ void doc_range(const int32_t *__restrict__ off, int s, int tokens, int &first,
                                           int &len) {

@@ -43,14 +43,14 @@ def test_attention_over_no_keys_at_all(new, buckets):
     assert dtable is None or not dtable.any()
 
 
-SCALES = [0.0, -0.0, 1e-42, -0.3]
+SCALES = [0.0, -0.0, 1e-42, -0.3, 1.0]
 
 
 @pytest.mark.parametrize("scale", SCALES)
 @pytest.mark.parametrize("dim,dtype,buckets,causal", [(64, BF16, 0, False), (64, FP16, 0, True), (128, BF16, 0, True), (40, BF16, 32, False)])
 def test_attention_takes_any_finite_scale(dim, dtype, buckets, causal, scale):
-    """Zero (a mean over the keys seen), less than a normal number, negative:
-    with and without a table, documents that end inside a tile."""
+    """Zero (a mean over the keys seen), less than a normal number, negative,
+    and one: with and without a table, documents that end inside a tile."""
     qlen, klen = ([200, 0, 33, 128, 5], [200, 0, 33, 128, 5]) if dim != 128 else ([200, 7, 33, 130, 5], [129, 0, 300, 128, 3])
     q, k, v, dout, table, bmap = attention_inputs(41, qlen, klen, 4, 2, dim, dtype, buckets, 64, causal)
     check_attention(q, k, v, dout, qlen, klen, table, bmap, causal, scale)
@@ -270,3 +270,21 @@ def test_unit_pool_gradient_of_the_smallest_means():
     want = torch.zeros(4, 96, device=DEV, dtype=torch.float64)
     want[3, 1] = 0.125 / norms[1].double()
     ref.assert_within(dh, want, 2.0 ** -21 * want, "dh")
+
+
+@pytest.mark.parametrize("size", [1e-5, 1e-4, 1.0])
+@pytest.mark.parametrize("dim,buckets,causal", [(64, 0, False), (64, 32, True), (128, 0, True), (128, 32, False)])
+def test_fp16_gradients_of_long_documents(dim, buckets, causal, size):
+    """The probabilities of thousands of keys are small, and dS smaller by
+    dout: in fp16 it must not round among the subnormals."""
+    n = [2000, 3, 150]
+    q, k, v, dout, table, bmap = attention_inputs(91, n, n, 2, 1, dim, FP16, buckets, 64, causal)
+    dout[1000:1500] = 0         # rows without a gradient beside rows with one
+    check_attention(q, k, v, dout * size, n, n, table, bmap, causal)
+
+
+def test_fp16_gradients_whose_ds_leaves_the_type():
+    """dS past 65,504 with dq and dk far below it."""
+    n = [2] * 60 + [3] * 40 + [5, 40]
+    q, k, v, dout, *_ = attention_inputs(92, n, n, 4, 2, 64, FP16, 0, 0, False)
+    check_attention(q * 0.01, k * 0.01, v * 30, dout * 600, n, n)
