@@ -10,7 +10,9 @@
 //   O += P V       tcgen05, P from tensor memory
 // The maximum that P is taken against is raised only when a row's grows by
 // more than 2^8 (its sum uses the same one, so the result is the same softmax;
-// P stays below 2^8, exact in scale): then the thread rescales its row of O.
+// P stays below 2^8, exact in scale): then the thread rescales its row of O.  In
+// fp16 P is taken 2^7 times as large, sum and all: it stays below 2^15, and small
+// weights keep their bits down to 2^-21 of the largest.
 //
 // Warps 0-7 make P (two warps to the 32 lanes of a quarter, 64 columns each,
 // so that a row's scores stay in registers); warp 8 loads and issues the
@@ -50,6 +52,8 @@ constexpr int kHalf = kTile / 2;
 constexpr uint32_t kTmemCols = 256;
 constexpr int kBlocksPerSm = 2;
 constexpr float kRaise = 8.f;
+template <typename T>
+constexpr float kUp = std::is_same_v<T, __half> ? 7.f : 0.f;
 // Tiles of K and of V held at a time.  With one, the next K loads under the
 // softmax of this one and the next V under the scores of the next: that is
 // enough, and at 128 columns it lets two blocks share an SM.
@@ -493,7 +497,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
                         tc::tmem_st16(lane_base + kOCol + half * (DP / 2) + 16 * i, o);
                     }
                 }
-                const float sub = m == -INFINITY ? 0.f : m;
+                const float sub = m == -INFINITY ? 0.f : m - kUp<T>;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     uint32_t pk[16];
@@ -539,8 +543,8 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) k_attend(const __grid_
                 const int64_t at = ((int64_t)w.number * (a.heads / f.pack) + w.group) * f.rows_per_doc + r;   // split
                 const int64_t row = w.q_row + qi;                                                             // not split
                 if (live && half == 0) {
-                    if (SPLIT) f.part_ml[at] = make_float2(m, l);
-                    else f.p.lse[(int64_t)head * a.q_tokens + row] = none ? -INFINITY : lse_of(m, l);
+                    if (SPLIT) f.part_ml[at] = make_float2(m - kUp<T>, l);
+                    else f.p.lse[(int64_t)head * a.q_tokens + row] = none ? -INFINITY : lse_of(m - kUp<T>, l);
                 }
 #pragma unroll
                 for (int i = 0; i < DP / 64; ++i) {

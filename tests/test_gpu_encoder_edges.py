@@ -288,3 +288,17 @@ def test_fp16_gradients_whose_ds_leaves_the_type():
     n = [2] * 60 + [3] * 40 + [5, 40]
     q, k, v, dout, *_ = attention_inputs(92, n, n, 4, 2, 64, FP16, 0, 0, False)
     check_attention(q * 0.01, k * 0.01, v * 30, dout * 600, n, n)
+
+
+def test_fp16_weights_far_below_the_largest():
+    """The key at a query's own place carries nearly all of its row, every
+    other 2^-20 of that: their weights must not round among fp16's subnormals
+    (the early queries meet the large one first)."""
+    n = 3000
+    table = torch.zeros(4, 1, device=DEV)
+    table[1] = 14.0                                             # no distance
+    bmap = torch.tensor([0, 1, 0], dtype=torch.int32, device=DEV)
+    v = 0.5 + randn(gen(95), n, 1, 64).abs()
+    v[:100] = 0                                                 # rows made of the small weights alone
+    q = torch.zeros(n, 1, 64, dtype=FP16, device=DEV)
+    check_attention(q, q, v.to(FP16), None, [n], [n], table, bmap, backward=False)
