@@ -84,7 +84,8 @@ sieve_status sieve_layer_norm_backward(const void *dy, int64_t dy_stride, const 
  *   q        device [q_tokens][heads][head_dim] of `dtype` (SIEVE_F16 or
  *            SIEVE_BF16); k, v device [k_tokens][kv_heads][head_dim].  Tokens
  *            and heads lie `*_token_stride` and `*_head_stride` elements
- *            apart (multiples of 8; base pointers 16-byte aligned), elements
+ *            apart (multiples of 8, at least head_dim where the axis has more
+ *            than one; base pointers 16-byte aligned), elements
  *            of a head contiguous, so they may be parts of one projection.
  *   heads    a multiple of kv_heads: query head h reads key head
  *            h / (heads / kv_heads)
@@ -139,8 +140,8 @@ sieve_status sieve_attention(const sieve_attention_args *a, void *out, float *ls
  *   dout     device [q_tokens][heads][head_dim] of dtype, contiguous
  *   out, lse what sieve_attention wrote for the same arguments
  *   dq, dk, dv  device out, of dtype; tokens and heads `grad_strides` apart
- *            (token and head stride of dq, dk, dv in turn, elements, multiples
- *            of 8; bases 16-byte aligned)
+ *            (token and head stride of dq, dk, dv in turn, with the same rules;
+ *            bases 16-byte aligned)
  *   dtable   device [num_buckets][heads] fp32 out; required with a table
  * Every row of every document is written, with zeros where nothing reaches it. */
 sieve_status sieve_attention_backward_workspace_size(const sieve_attention_args *a, size_t *bytes);

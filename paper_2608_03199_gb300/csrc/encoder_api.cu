@@ -38,6 +38,10 @@ sieve_status check_workspace(const void *ws, size_t have, size_t need) {
     return SIEVE_OK;
 }
 
+// Whether the heads of an axis of `n` would overlap.  (A tensor map wants every
+// stride to clear the axes below it.)
+bool overlapping(int64_t n, int64_t stride, int32_t head_dim) { return n > 1 && stride < head_dim; }
+
 sieve_status check_attention(const sieve_attention_args *a, bool pointers) {
     if (!a) return SIEVE_EINVAL;
     if (a->dtype != SIEVE_F16 && a->dtype != SIEVE_BF16) return SIEVE_EINVAL;
@@ -66,6 +70,9 @@ sieve_status check_attention(const sieve_attention_args *a, bool pointers) {
                                 a->k_head_stride,  a->v_token_stride, a->v_head_stride};
     for (int64_t s : strides)
         if (s < 0 || s % 8 || s >= (int64_t)1 << 38) return SIEVE_EINVAL;
+    const int64_t counts[6] = {a->q_tokens, a->heads, a->k_tokens, a->kv_heads, a->k_tokens, a->kv_heads};
+    for (int i = 0; i < 6; ++i)
+        if (overlapping(counts[i], strides[i], a->head_dim)) return SIEVE_EINVAL;
     if (a->q_tokens > 0 && (!a->q || !aligned_to(a->q, 16))) return SIEVE_EINVAL;
     if (a->k_tokens > 0 && (!a->k || !a->v || !aligned_to(a->k, 16) || !aligned_to(a->v, 16))) return SIEVE_EINVAL;
     return SIEVE_OK;
@@ -205,8 +212,10 @@ sieve_status sieve_attention_backward(const sieve_attention_args *a, const void 
     sieve_status rc = check_attention(a, true);
     if (rc != SIEVE_OK) return rc;
     if (!grad_strides) return SIEVE_EINVAL;
+    const int64_t counts[6] = {a->q_tokens, a->heads, a->k_tokens, a->kv_heads, a->k_tokens, a->kv_heads};
     for (int i = 0; i < 6; ++i)
-        if (grad_strides[i] < 0 || grad_strides[i] % 8) return SIEVE_EINVAL;
+        if (grad_strides[i] < 0 || grad_strides[i] % 8 || overlapping(counts[i], grad_strides[i], a->head_dim))
+            return SIEVE_EINVAL;
     if (a->q_tokens > 0 && (!dout || !out || !lse || !dq || !aligned_to(dout, 16) || !aligned_to(out, 16) ||
                             !aligned_to(dq, 16) || !aligned4(lse)))
         return SIEVE_EINVAL;

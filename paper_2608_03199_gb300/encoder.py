@@ -264,7 +264,13 @@ def _strides(t):
     """Token and head strides; an axis of one element has none that matters."""
     *_, tokens, heads, dim = t.shape
     *_, ts, hs, _ = t.stride()
-    return ts if tokens > 1 else heads * dim, hs if heads > 1 else dim
+    return _apart(ts if tokens > 1 else heads * dim, hs if heads > 1 else dim, dim)
+
+
+def _apart(ts, hs, dim):
+    if ts < dim or hs < dim:
+        raise ValueError("tokens and heads must not overlap: an expanded tensor has to be made contiguous")
+    return ts, hs
 
 
 def _new_strides(t):
@@ -273,7 +279,7 @@ def _new_strides(t):
     across, ts, hs, _ = t.stride()
     if nseq > 1 and new > 1 and across != new * ts:
         raise ValueError("new tokens must be evenly spaced")
-    return across if new == 1 and nseq > 1 else ts if new > 1 else heads * dim, hs if heads > 1 else dim
+    return _apart(across if new == 1 and nseq > 1 else ts if new > 1 else heads * dim, hs if heads > 1 else dim, dim)
 
 
 def _attention_args(q, k, v, offsets, q_offsets, table, buckets, causal, scale):

@@ -185,3 +185,28 @@ def test_unaligned_pointers_are_refused_without_gpu():
         assert lib.sieve_unit_pool(p, 64, x[0], 1000, 7, 64, 0, x[1], x[2], p, big, None) == -1, at
         assert lib.sieve_unit_pool_backward(p, x[1], x[2], x[0], 1000, 7, 64, 0, p, 64, None) == -1, at
     assert lib.sieve_unit_pool_backward(odd, p, p, p, 1000, 7, 64, 0, p, 64, None) == -1
+
+
+@pytest.mark.parametrize("name", ["q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride", "v_token_stride",
+                                  "v_head_stride"])
+@pytest.mark.parametrize("stride", [0, 56])
+def test_overlapping_heads_are_refused_without_gpu(name, stride):
+    """A stride of zero (an expanded tensor) or below the head's length, where
+    the axis has more than one element; where it has one, any."""
+    p, big, fields = C.c_void_p(256), 1 << 40, ["q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride",
+                                                "v_token_stride", "v_head_stride"]
+    lib = sieve.lib()
+    assert lib.sieve_attention(C.byref(args(**{name: stride})), p, p, p, big, None) == -1
+    strides = [256, 64, 128, 64, 128, 64]
+    strides[fields.index(name)] = stride
+    assert lib.sieve_attention_backward(C.byref(args()), p, p, p, p, p, p, (C.c_int64 * 6)(*strides), p, p, big, None) == -1
+    single = args(**{name: stride}, heads=1, kv_heads=1, nseq=1, q_tokens=1, k_tokens=1)
+    assert lib.sieve_attention(C.byref(single), p, p, p, 0, None) == -3          # only the workspace is wrong
+
+
+def test_binding_names_expanded_tensors():
+    t = torch.empty(5, 1, 64).expand(5, 3, 64)
+    for call in (lambda: sieve.encoder._strides(t), lambda: sieve.encoder._new_strides(torch.empty(1, 1, 3, 64).expand(4, 1, 3, 64))):
+        with pytest.raises(ValueError, match="contiguous"):
+            call()
+    assert sieve.encoder._strides(torch.empty(1, 3, 64)[:, :1]) == (64, 64)
