@@ -302,3 +302,19 @@ def test_fp16_weights_far_below_the_largest():
     v[:100] = 0                                                 # rows made of the small weights alone
     q = torch.zeros(n, 1, 64, dtype=FP16, device=DEV)
     check_attention(q, q, v.to(FP16), None, [n], [n], table, bmap, backward=False)
+
+
+@pytest.mark.parametrize("new", [0, 1])
+def test_lse_of_even_weights_is_the_logarithm_of_their_number(new):
+    """With q = 0 a row's sum is the number of its keys, exactly, so lse is off
+    by the logarithm's own ulp, its conversion from base 2 and one rounding."""
+    klen = [1, 2, 3, 5, 100, 1000, 3001, 7777, 20_000]
+    qlen = [new] * len(klen) if new else [min(b, 5) for b in klen]
+    k = randn(gen(61), sum(klen), 1, 64).to(BF16)
+    off = ref.offsets_of(klen, DEV)
+    if new:
+        lse = sieve.attention(k.new_zeros(len(klen), 1, 1, 64), k, k, off)[1]
+    else:
+        lse = sieve.attention(k.new_zeros(sum(qlen), 1, 64), k, k, off, q_offsets=ref.offsets_of(qlen, DEV))[1]
+    want = torch.tensor([b for a, b in zip(qlen, klen) for _ in range(a)], device=DEV).double().log()[None]
+    ref.assert_within(lse, want, 2.0 ** -22 * want, "lse")
