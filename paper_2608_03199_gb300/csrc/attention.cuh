@@ -142,7 +142,9 @@ __device__ __forceinline__ float exp2_approx(float x) {
     return y;
 }
 
-__device__ __forceinline__ float log2_approx(float x) {   // absolute error at most 2^-22
+// absolute error at most 2^-22 for x within (0.5, 2), relative elsewhere: the sum of
+// 2^20 keys leaves an lse off by 2^-18 at most, and P of the backward pass by as much
+__device__ __forceinline__ float log2_approx(float x) {
     float y;
     asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;

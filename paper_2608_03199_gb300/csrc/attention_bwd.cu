@@ -21,13 +21,15 @@
 // fp32, before any rounding.
 //
 // Measured (bf16): 384 documents of 0 to 512 tokens,
-// 12 heads of 64 with a bias: delta 53 us (302 MB, 5.7 TB/s), dq 348, dk and dv
-// 437, the table's sums 25.  A step of 128 x 128 pairs takes about 3.3K cycles
+// 12 heads of 64 with a bias: delta 55 us (302 MB, 5.5 TB/s), dq 351, dk and dv
+// 444, the table's sums 19; at a reach of 256 dq 397, dk and dv 467.  fp16: the
+// longest v 37 (124 MB), delta 76, dq 357, dk and dv 461.  A step of 128 x 128 pairs takes about 3.3K cycles
 // there: 1.3K for P (an exponential and a bias read for each pair), 0.45K for dS,
 // 0.9K for its sums by distance, the rest waits; its four products are 1.1K.
 // Short documents pay for what a block's work costs once, 4K to 5K cycles.
 // Without a bias, 3 documents of 3,001 to 8,192 tokens, 16 heads of 128 on 4 key
-// heads: dq 420 us, dk and dv 600, 57% and 52% of the tensor pipe.
+// heads: dq 420 us, dk and dv 610, 57% and 52% of the tensor pipe.  10,000 texts of 10
+// to 60 tokens, 12 heads of 64, a tile to each: delta 412, dq 2,119, dk and dv 2,627.
 //
 // In both, 16 warps make P and dS, each for 32 lanes and 32 columns; one more
 // loads, one more issues the products.  While the threads turn S into P
@@ -44,7 +46,11 @@ namespace enc {
 namespace {
 
 constexpr int kSlots = 2;      // the work in hand and the next
-constexpr int kShort = 16;     // steps of work that is short
+// Steps of work that is short: the next is asked for, and looked for, while it runs.
+// (dq and dkv with 0 / 4 / 16 / 64 here: 384 documents of up to 512 tokens 360, 442 /
+// 351, 445 / 351, 445 / 351, 445 us; 64 of up to 2,048 442, 570 / 448, 580 / 434, 584 /
+// 434, 583; 3 of up to 8,192 412, 599 / 415, 597 / 422, 614 / 465, 649.)
+constexpr int kShort = 16;
 
 // fp16 has no bits below 2^-24, and a long document's P and dS are small.  So
 // k_attend_dkv takes 2^14 P (P <= 1 up to the rounding of lse) and scales dV
@@ -123,7 +129,8 @@ struct DkvWork {
 // n keys would be 1 each, not 1 / n.  So its largest score and its sum are made
 // anew, each for itself, from scores that are rounded as the forward pass rounds
 // them; P = 2^((score - largest) - log2 sum) is exact at any size.  This takes a
-// warp a pass over the query's keys without the tensor cores, and biases that a
+// warp a pass over the query's keys without the tensor cores: 1.7 ms for one head
+// of 12 that is all huge, on 384 documents of up to 512 tokens.  Biases that a
 // model learns stay far below the limit.
 constexpr float kFar = 256.f;      // of an lse (off by 2^-17 there) and of a bias in base 2
 template <typename T>
@@ -1131,8 +1138,8 @@ __global__ void __launch_bounds__(18 * 32, 1) k_attend_dkv(const __grid_constant
                         // e lanes, lane l holds the elements of one distance, that
                         // of key l and the first query, and where the turn wrapped
                         // around those of the distance 32 less.  (One shuffle an
-                        // element.  With a sum handed from lane to lane and stored
-                        // by the last a step took 2.9K cycles, with this 2.45K.)
+                        // element: 0.45K cycles a step less than a sum handed from
+                        // lane to lane and stored by the last.)
                         const int hi = key_lo + 31 - place0, lo = hi - 62;
                         if (!live)   // rows past the document's keys add nothing
 #pragma unroll

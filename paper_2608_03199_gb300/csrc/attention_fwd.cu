@@ -24,12 +24,15 @@
 // the steps on documents of a few tiles.)
 //
 // Measured (bf16): 4 documents of 6,001 to 8,192 tokens, causal, 16 heads of 128
-// on 4 key heads: 707 us, 1.13 PFLOP/s, bound by the softmax between two products
+// on 4 key heads: 705 us, 1.14 PFLOP/s, bound by the softmax between two products
 // (two blocks an SM hide most of it).  512 documents of 0 to 512 tokens, 12 heads
-// of 64 with a bias: 365 us; the products are a sixth of that, the rest is the
-// softmax (an exponential and a bias read for each pair) and, for documents of a
+// of 64 with a bias: 367 us (256 without); the products are a sixth of that, the rest
+// is the softmax (an exponential and a bias read for each pair) and, for documents of a
 // tile or two, what a block's work costs once.  One new token for each of 24
-// documents of up to 32K tokens: 689 MB in 155 us, 4.5 TB/s with the join.
+// documents of up to 32K tokens: 689 MB in 156 us, 4.4 TB/s with the join (8 us).
+// Two blocks share an SM up to a reach of 130 or so; past that the bias tables leave
+// room for one: 534 us on the 512 documents at a reach of 256.  A text of 10 to 60
+// tokens has a tile to itself: 10,000 of them, 12 heads of 64, 1,266 us.
 //
 // Where every document has a few new queries against many keys, a block takes
 // the rows of all heads that share a key head (up to 128) over one chunk of
@@ -47,7 +50,11 @@ constexpr int kSoftmaxWarps = 8;
 constexpr int kSoftmax = kSoftmaxWarps * 32;
 constexpr int kThreads = kSoftmax + 64;
 constexpr int kSlots = 2;     // the work in hand and the next
-constexpr int kShort = 16;    // key tiles of work that is short
+// Key tiles of work that is short: the next is asked for ahead of its end.  (With
+// long work other blocks are done sooner: 4 documents of 6K to 8K tokens 677 us, 703
+// with 64 here.  On short work it is worth little: never asking ahead, documents of
+// 128 tokens 114 against 113 us, of 512 365 against 367.)
+constexpr int kShort = 16;
 constexpr int kHalf = kTile / 2;
 constexpr uint32_t kTmemCols = 256;
 constexpr int kBlocksPerSm = 2;
@@ -662,15 +669,22 @@ Shape shape_of(const sieve_attention_args &a) {
         s.split = true;
         for (int p = 1; p <= share; ++p)
             if (share % p == 0 && p * a.new_tokens <= kTile && p * bias_bytes <= kMaxBiasBytes) s.pack = p;
-        // chunks: about two rounds of blocks, no fewer than two tiles each
+        // as many heads of a key head to a block as their bias tables leave room
+        // for: each block reads K and V once (8 heads on a key head at a reach of
+        // 128, or 4 at 256, take two: 257 us where one takes 156)
+        // chunks: about two rounds of blocks, no fewer than two tiles each.  (One
+        // token, 1 / 2 / 4 rounds: 24 documents of up to 32K 176 / 164 / 168 us, 4 of
+        // them 58 / 69 / 107, one 49 / 69 / 69, 300 of up to 1,000 100 / 100 / 98;
+        // at least 1 / 2 / 4 tiles: 4 of up to 2,000 26 / 26 / 30, one of 32K 69 / 69 /
+        // 49: where there are few documents it is the join that many chunks cost.)
         const int64_t want = a.k_tokens * (a.heads / s.pack) / (2 * 152 * kBlocksPerSm);
         s.chunk = (int)(round_up(want < 2 * kTile ? 2 * kTile : want, kTile));
         s.chunks = doc_tiles(a.k_tokens, a.nseq, s.chunk);
         s.blocks = s.chunks * (a.heads / s.pack);
     } else {
         // A block's work is one tile of queries.  (Up to four of a document
-        // took 393 us where this takes 383, on 512 documents of 0 to 512
-        // tokens and 12 heads of 64: the work is shared out less evenly.)
+        // took a fortieth longer on 512 documents of 0 to 512 tokens and 12
+        // heads of 64: the work is shared out less evenly.)
         s.doc_tiles = a.new_tokens > 0 ? (int)ceil_div(a.new_tokens, kTile) : 0;
         s.blocks = (a.new_tokens > 0 ? a.nseq * s.doc_tiles : doc_tiles(a.q_tokens, a.nseq, kTile)) * a.heads;
     }

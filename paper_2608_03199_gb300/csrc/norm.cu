@@ -11,10 +11,12 @@
 // fixed order by a second launch: no atomics, the same bits every time.
 // Everything between the load and the store is fp32.
 //
-// Measured: forward 200,003 x 1024 bf16 (819 MB) 152 us, 5.4 TB/s; 100,003 x
-// 768 bf16 forward 51 us (6.0 TB/s), backward 90 us (461 MB, 5.1 TB/s: a warp's
-// next row is on its way while it works on this one, at two blocks an SM) and 8 us
-// for the partial sums.
+// Measured: forward 200,003 x 1024 bf16 (819 MB) 149 us, 5.5 TB/s; 100,003 x
+// 768 bf16 forward 54 us (307 MB, 5.7 TB/s), backward 96 us (461 MB, 4.8 TB/s: a
+// warp's next row is on its way while it works on this one, at two blocks an SM) and
+// 4 us for the partial sums; odd widths, element by element: 20,011 x 1001 fp32
+// forward 30 us (160 MB, 5.4 TB/s), backward 62 us (240 MB, 3.9 TB/s), bf16 29 and 59.
+// (Figures of this file: device time of each launch, nothing in the L2 cache.)
 #include <type_traits>
 
 #include "encoder.cuh"
@@ -22,19 +24,6 @@
 namespace sieve {
 namespace enc {
 namespace {
-
-// Sum of a value over the TPR threads of a block.
-template <int TPR>
-__device__ __forceinline__ float block_sum(float v, float *smem) {
-    v = warp_sum(v);
-    __syncthreads();
-    if (lane_id() == 0) smem[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = 0.f;
-#pragma unroll
-    for (int w = 0; w < TPR / 32; ++w) v += smem[w];
-    return v;
-}
 
 // Rows wider than 1,024, and wider than 384 that cannot move 16 bytes at a time:
 // one row per block of TPR threads, held in registers: NCH chunks of VEC elements
@@ -93,9 +82,10 @@ __global__ void __launch_bounds__(TPR)
 // loads go out together, and one meeting of the block serves all), and
 // keeps the column sums of dweight and dbias of its columns in registers;
 // they go to partial[block][2][width] and k_norm_reduce adds the blocks up.
-// (Registers for three blocks of 256 an SM: 20,011 x 1001 fp32, both passes, 99 us
-// with two rows at a time and the next two on their way; 115 with four and one
-// block an SM; 132 with four and none on their way.)
+// (20,011 x 1001 fp32, both passes: 99 us with two rows at a time and the next two
+// on their way, at two blocks of 256 an SM, which is the grid, though the registers
+// would let three; 115 with four rows and one block an SM; 132 with four and none on
+// their way.)
 template <typename T, typename W, int VEC, int TPR, int NCH, int R>
 __global__ void __launch_bounds__(TPR, TPR <= 256 ? 768 / TPR : 1) k_norm_backward(const NormArgs a) {
     __shared__ float smem[2 * R][TPR / 32];
@@ -438,7 +428,9 @@ cudaError_t forward_as(const NormArgs &a, cudaStream_t st) {
 }
 
 constexpr int kMaxBlocks = 152 * 4;
-constexpr int kRowsWidth = 1024;   // widest row of the row-walking kernels
+// Widest row of the row-walking kernels.  (A warp to a row against a block: 200,003
+// x 1024 bf16 forward 149 us, 309; 100,003 x 768 both passes 154, 394.)
+constexpr int kRowsWidth = 1024;
 
 template <typename T, typename W, int VEC, int NCH>
 cudaError_t forward_rows(const NormArgs &a, cudaStream_t st) {
@@ -474,17 +466,20 @@ cudaError_t forward(const NormArgs &a, cudaStream_t st) {
     if (a.width <= kRowsWidth) {
         if (wide<T, W>(a))
             return by_chunks<V>(a.width, [&](auto n) { return forward_rows<T, W, V, decltype(n)::value>(a, st); });
-        // element by element: a warp to a row up to 12 a lane; past that a block
-        // with 8 a thread (20,011 x 1001 fp32: 35 us, against 44 with 32 a lane)
+        // element by element: a warp to a row up to 12 a lane (fp32, 150,000 x 101
+        // 37 us, 46 if compiled for 12; 60,000 x 301 29 us, 55 with a block); past
+        // that a block with 8 a thread (20,011 x 1001 30 us, 44 with 32 a lane)
         if (a.width <= 128) return forward_rows<T, W, 1, 4>(a, st);
         if (a.width <= 384) return forward_rows<T, W, 1, 12>(a, st);
         return forward_as<T, W, 1, 128, 8>(a, st);
     }
     if (wide<T, W>(a)) {
+        // (40,000 x 2048 bf16: 78 us, 259 with 512 threads)
         const int chunks = a.width / V;
         if (chunks <= 512) return forward_as<T, W, V, 128, 4>(a, st);
         return forward_as<T, W, V, 512, V == 8 ? 4 : 8>(a, st);
     }
+    // (13,000 x 1501 fp32: 33 us, 221 with 512 threads)
     if (a.width <= 2048) return forward_as<T, W, 1, 128, 16>(a, st);
     return forward_as<T, W, 1, 512, 32>(a, st);
 }
@@ -515,11 +510,16 @@ cudaError_t backward(const NormArgs &a, cudaStream_t st) {
         if (a.width <= kRowsWidth && wide<T, W>(a)) {
             e = by_chunks<V>(a.width, [&](auto n) { return backward_rows<T, W, V, decltype(n)::value>(a, blocks, st); });
         } else if (wide<T, W>(a)) {
+            // (bf16: 40,000 x 2048 126 us, 229 with 512 threads; 20,000 x 4096 158,
+            // 315 with 4 pieces a thread)
             const int chunks = a.width / V;
             if (chunks <= 256) e = backward_as<T, W, V, 256, 1, 2>(a, blocks, st);
             else if (chunks <= 512) e = backward_as<T, W, V, 512, 1, 2>(a, blocks, st);
             else e = backward_as<T, W, V, 512, V == 8 ? 4 : 8, 1>(a, blocks, st);
         } else {
+            // the narrowest block that holds a row at 4 elements a thread, 8 from
+            // 1,025 on (fp32, against the next wider one: 150,000 x 101 120 us, 163;
+            // 60,000 x 301 74, 154; 20,011 x 1001 62, 183; 7,000 x 3001 86, 317)
             if (a.width <= 128) e = backward_as<T, W, 1, 32, 4, 2>(a, blocks, st);
             else if (a.width <= 512) e = backward_as<T, W, 1, 128, 4, 2>(a, blocks, st);
             else if (a.width <= 1024) e = backward_as<T, W, 1, 256, 4, 2>(a, blocks, st);

@@ -8,8 +8,14 @@ everywhere in this package the functions only marshal tensors into libsieve's
 CUDA kernels; they raise TypeError or ValueError for tensors they cannot take
 and :class:`SieveError` for anything the library refuses, and run on
 ``stream`` (default: the current stream of the tensors' device).  Results and
-scratch belong to the stream they are computed on, and inputs are kept from
-reuse until that stream has passed the call.
+scratch belong to the stream they are computed on; with an explicit ``stream``
+inputs are kept from reuse until that stream has passed the call.  Rows that
+belong to no document (before the first offset, past the last) are not written
+in results: a tensor with room to spare holds anything there.
+
+The calls are outside of torch.autograd: results never require a gradient,
+whatever their inputs do, and a backward pass is a call of its own, as in
+``examples/encode_and_deduplicate.py``.
 
 * :func:`layer_norm`, :func:`layer_norm_backward`
 * :func:`attention`, :func:`attention_backward` (relative position bias:
