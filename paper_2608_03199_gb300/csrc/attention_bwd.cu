@@ -21,7 +21,7 @@
 // fp32, before any rounding.
 //
 // Measured (bf16): 384 documents of 0 to 512 tokens,
-// 12 heads of 64 with a bias: delta 55 us (302 MB, 5.5 TB/s), dq 351, dk and dv
+// 12 heads of 64 with a bias: delta 55 us (249 MB, 4.5 TB/s), dq 351, dk and dv
 // 444, the table's sums 19; at a reach of 256 dq 397, dk and dv 467.  fp16: the
 // longest v 37 (124 MB), delta 76, dq 357, dk and dv 461.  A step of 128 x 128 pairs takes about 3.3K cycles
 // there: 1.3K for P (an exponential and a bias read for each pair), 0.45K for dS,
