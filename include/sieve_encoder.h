@@ -5,9 +5,11 @@
  *
  * The search of sieve.h starts from one unit-norm fp32 row per document.
  * These calls are the parts of a text encoder that are not plain matrix
- * products: layer norm, attention with a learned relative position bias, and
- * the pooling of a document's tokens into its unit row.  The paper takes the
- * rows as given, so it has no counterpart.
+ * products: token embedding, layer norm, attention with a learned relative
+ * position bias, the residual step between two blocks, the pooling of a
+ * document's tokens into its unit row, and the cross entropy that an encoder
+ * is trained with.  The paper takes the rows as given, so it has no
+ * counterpart.
  *
  * Conventions are sieve.h's: device pointers of the current device, every
  * buffer the caller's, scratch from the caller's workspace (256-byte
@@ -40,11 +42,21 @@ extern "C" {
 #define SIEVE_F32 0
 #define SIEVE_F16 1
 #define SIEVE_BF16 2
+/* types of token ids and targets */
+#define SIEVE_I32 3
+#define SIEVE_I64 4
 
 #define SIEVE_NORM_MAX_WIDTH 16384
 #define SIEVE_ATTENTION_MAX_DIM 128
 #define SIEVE_ATTENTION_MAX_BUCKETS 64
 #define SIEVE_ATTENTION_MAX_REACH 256
+#define SIEVE_EMBED_MAX_WIDTH 16384
+#define SIEVE_EMBED_MAX_TOKENS (1 << 30)
+#define SIEVE_EMBED_MAX_VOCAB (1 << 26)
+#define SIEVE_RESIDUAL_NORM_MAX_WIDTH 8192
+#define SIEVE_CROSS_ENTROPY_MAX_WIDTH 16384
+#define SIEVE_CROSS_ENTROPY_MAX_ROWS (1 << 24)
+#define SIEVE_CROSS_ENTROPY_MAX_CLASSES (1 << 24)
 
 /* Layer norm of every row of x:
  *   mu = mean(x), r = 1 / sqrt(mean((x - mu)^2) + eps), y = (x - mu) r w + b
@@ -150,8 +162,8 @@ sieve_status sieve_attention_backward(const sieve_attention_args *a, const void 
                                       void *dv, const int64_t grad_strides[6], float *dtable,
                                       void *ws, size_t ws_bytes, void *stream);
 
-/* The status word that the last sieve_attention or sieve_attention_backward
- * enqueued with workspace ws left there: 0, or SIEVE_ETIMEOUT where a bounded
+/* The status word that the last sieve_attention, sieve_cross_entropy or
+ * backward pass of theirs enqueued with workspace ws left there: 0, or SIEVE_ETIMEOUT where a bounded
  * wait inside a kernel gave up (its outputs are then undefined).  Copies the
  * word to *status (host) on `stream` and synchronizes `stream`. */
 sieve_status sieve_encoder_status(const void *ws, size_t ws_bytes, int32_t *status, void *stream);
@@ -177,6 +189,161 @@ sieve_status sieve_unit_pool_backward(const float *drows, const float *rows, con
                                       const int32_t *offsets, int64_t tokens, int64_t nseq,
                                       int32_t width, int32_t dtype, void *dh, int64_t dh_stride,
                                       void *stream);
+
+/* Token embedding: out[t] = scale table[ids[t]], rounded once.  An id outside
+ * [0, vocab) has no row: zeros, and no gradient.
+ *   ids    device [tokens], contiguous, of `id_type` (SIEVE_I32 or SIEVE_I64)
+ *   table  device [vocab][width] of `table_dtype`, rows table_stride apart
+ *          (>= width)
+ *   out    device [tokens][width] of `dtype`, rows out_stride apart
+ * Any of the three types for table and out.  width 1..SIEVE_EMBED_MAX_WIDTH,
+ * tokens up to SIEVE_EMBED_MAX_TOKENS, vocab 1..SIEVE_EMBED_MAX_VOCAB; scale
+ * finite.  tokens = 0 does nothing. */
+sieve_status sieve_embed(const void *ids, int32_t id_type, int64_t tokens, const void *table,
+                         int64_t table_stride, int64_t vocab, int32_t width, int32_t table_dtype,
+                         float scale, void *out, int64_t out_stride, int32_t dtype, void *stream);
+
+/* The gradient of its table: dtable[v] = scale * sum of dout[t] over the
+ * tokens t with ids[t] = v, in fp32 and in an order that depends on the ids
+ * alone (the tokens are sorted by id first, equal ids in the tokens' order).
+ *   dout     device [tokens][width] of `dtype`, rows dout_stride apart
+ *   dtable   device [vocab][width] of `table_dtype`, rows dtable_stride apart.
+ *            accumulate = 0: every row is written, with zeros where no token
+ *            has its id; 1: the sums are added to what is there and rows
+ *            without a token stay as they are (a tied table's second gradient)
+ */
+sieve_status sieve_embed_backward_workspace_size(int64_t tokens, int64_t vocab, int32_t width,
+                                                 size_t *bytes);
+sieve_status sieve_embed_backward(const void *dout, int64_t dout_stride, const void *ids,
+                                  int32_t id_type, int64_t tokens, int64_t vocab, int32_t width,
+                                  int32_t dtype, float scale, void *dtable, int64_t dtable_stride,
+                                  int32_t table_dtype, int32_t accumulate, void *ws,
+                                  size_t ws_bytes, void *stream);
+
+/* The residual step between two blocks of an encoder: the block's output y is
+ * normed (post), gated and added to the scaled stream h, and the sum is normed
+ * (pre) for the next block, in one pass:
+ *   u = N(y; post_weight, post_bias), or y without post_weight
+ *   stream = alpha h + gate u
+ *   x = N(stream; weight, bias), from the sum before it is rounded
+ * where N(v; w, b) = (v - mu) r w + b, mu = mean(v) and r = 1 / sqrt(mean((v -
+ * mu)^2) + eps), or with rms = 1 mu = 0.
+ *   h, y, stream, x  device [rows][width] of `dtype`, rows `*_stride` apart
+ *            (>= width); stream may be h, x may be y
+ *   weight, bias, post_weight, post_bias  device [width] of `weight_dtype`
+ *            (dtype, or SIEVE_F32), nullable; a bias goes with its weight, and
+ *            one of the weights is there.  Without weight there is no x.
+ *   gate     gate_kind SIEVE_GATE_NONE: 1; _COLUMN: device [width] of
+ *            weight_dtype; _ROW: device [rows][width] of dtype, gate_stride apart
+ *   stats    device [4][rows] fp32: mu and r of the post norm, mu and r of the
+ *            pre norm (0 and 1 where there is none): what the backward pass needs
+ * width 1..SIEVE_RESIDUAL_NORM_MAX_WIDTH, eps >= 0 and finite, alpha finite. */
+#define SIEVE_GATE_NONE 0
+#define SIEVE_GATE_COLUMN 1
+#define SIEVE_GATE_ROW 2
+typedef struct {
+    int64_t rows;
+    int32_t width, dtype, weight_dtype, rms, gate_kind;
+    float alpha, eps;
+    int32_t reserved0;
+    const void *h, *y, *gate;
+    int64_t h_stride, y_stride, gate_stride;
+    const void *weight, *bias, *post_weight, *post_bias;
+} sieve_residual_norm_args;
+
+sieve_status sieve_residual_norm(const sieve_residual_norm_args *a, void *stream_out,
+                                 int64_t stream_stride, void *x, int64_t x_stride, float *stats,
+                                 void *stream);
+
+/* Its backward pass, from the gradients of both results (the sum is made again
+ * from h and y, so it is not rounded here either):
+ *   G = dstream + dN(dx; stream),  dh = alpha G,  dy = dN(gate G; y) or gate G,
+ *   dgate = G u (summed over rows for a column gate),  and the weights'
+ *   gradients summed over rows
+ * with dN(d; v) = r (d w - mean(d w) - vh mean(d w vh)), vh = (v - mu) r, the
+ * mean of d w left out with rms = 1.
+ *   dstream  device [rows][width] of dtype, nullable where there is a weight
+ *   dx       the same, required where there is a weight, else NULL
+ *   dh, dy   device out, of dtype; dh may be dstream, dy may be dx
+ *   dweight, dbias, dpost_weight, dpost_bias  device [width] of weight_dtype
+ *            out, where the weight of that name is there
+ *   dgate    like gate, out
+ * The sums over rows are fp32, in an order that depends on the sizes alone;
+ * rows = 0 writes zeros to them. */
+typedef struct {
+    const void *dstream, *dx;
+    int64_t dstream_stride, dx_stride;
+    const float *stats;
+    void *dh, *dy, *dgate;
+    int64_t dh_stride, dy_stride, dgate_stride;
+    void *dweight, *dbias, *dpost_weight, *dpost_bias;
+} sieve_residual_norm_grads;
+
+sieve_status sieve_residual_norm_backward_workspace_size(int64_t rows, int32_t width, size_t *bytes);
+sieve_status sieve_residual_norm_backward(const sieve_residual_norm_args *a,
+                                          const sieve_residual_norm_grads *g, void *ws,
+                                          size_t ws_bytes, void *stream);
+
+/* Softmax cross entropy of rows against a table of classes, without keeping
+ * the scores:
+ *   z[r][v] = scale h[r].weight[v] + bias[v]
+ *   lse[r] = log of the sum over v of exp(z[r][v]),
+ *   loss[r] = lse[r] - z[r][targets[r]]
+ * (as log1p of the other classes' sum against the target's, so that a small
+ * loss keeps its digits).  A target outside [0, classes) means none: the row's
+ * loss and lse are 0 and it gets and gives no gradient, whatever h holds there.
+ * The rows with a target are found on the device and only they cost time.
+ *   h        device [rows][width] of `dtype` (SIEVE_F16 or SIEVE_BF16), rows
+ *            h_stride apart
+ *   weight   device [classes][width] of dtype, rows weight_stride apart.
+ *            width and strides are multiples of 8, bases 16-byte aligned.
+ *   bias     device [classes] fp32, nullable; -inf hides a class
+ *   targets  device [rows], contiguous, of `target_type`
+ * A hidden target's loss is +inf.  Where every class is hidden lse is -inf.
+ * width 8..SIEVE_CROSS_ENTROPY_MAX_WIDTH, up to SIEVE_CROSS_ENTROPY_MAX_ROWS
+ * rows and 1..SIEVE_CROSS_ENTROPY_MAX_CLASSES classes, scale finite. */
+typedef struct {
+    int64_t rows, classes;
+    int32_t width, dtype, target_type;
+    float scale;
+    const void *h, *weight;
+    int64_t h_stride, weight_stride;
+    const float *bias;
+    const void *targets;
+} sieve_cross_entropy_args;
+
+sieve_status sieve_cross_entropy_workspace_size(const sieve_cross_entropy_args *a, size_t *bytes);
+sieve_status sieve_cross_entropy(const sieve_cross_entropy_args *a, float *loss, float *lse,
+                                 void *ws, size_t ws_bytes, void *stream);
+
+/* Its backward pass, for the gradient dloss of every row's loss: with
+ * q = exp(z - lse) - [v = target] (exactly expm1(-loss) at the target),
+ *   dh[r] = dloss[r] scale sum over v of q weight[v],
+ *   dweight[v] = scale sum over r of dloss[r] q h[r],
+ *   dbias[v] = sum over r of dloss[r] q.
+ * The scores are made anew in pieces of the classes; q is rounded once to
+ * dtype on its way into both products, and where the rows' dloss differ, so is
+ * dloss h over its largest.
+ *   dloss    device [rows] fp32;  loss, lse what sieve_cross_entropy wrote
+ *   dh       device [rows][width] of dtype out, rows dh_stride apart; nullable
+ *   dweight  device [classes][width] of `dweight_dtype` (dtype or SIEVE_F32)
+ *            out, rows dweight_stride apart; nullable.  accumulate = 1
+ *            (SIEVE_F32 alone) adds to what is there.
+ *   dbias    device [classes] fp32 out, nullable; without a bias there is none
+ * Strides are multiples of 8, bases of dh and dweight 16-byte aligned. */
+typedef struct {
+    const float *dloss, *loss, *lse;
+    void *dh, *dweight;
+    int64_t dh_stride, dweight_stride;
+    int32_t dweight_dtype, accumulate;
+    float *dbias;
+} sieve_cross_entropy_grads;
+
+sieve_status sieve_cross_entropy_backward_workspace_size(const sieve_cross_entropy_args *a,
+                                                         size_t *bytes);
+sieve_status sieve_cross_entropy_backward(const sieve_cross_entropy_args *a,
+                                          const sieve_cross_entropy_grads *g, void *ws,
+                                          size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -17,6 +17,9 @@ Entry points (same names as the C ABI):
 * :func:`layer_norm`, :func:`attention`, :func:`unit_pool` and their
   ``*_backward`` -- the encoder operators that make the rows
   (:mod:`paper_2608_03199_gb300.encoder`)
+* :func:`embed`, :func:`residual_norm`, :func:`cross_entropy` and their
+  ``*_backward`` -- the operators around an encoder's blocks
+  (:mod:`paper_2608_03199_gb300.blocks`)
 """
 from __future__ import annotations
 
@@ -707,4 +710,9 @@ from . import encoder as _encoder  # noqa: E402  (uses this module's helpers)
 from .encoder import (attention, attention_backward, encoder_status, layer_norm,  # noqa: E402,F401
                       layer_norm_backward, relative_buckets, unit_pool, unit_pool_backward)
 
+from . import blocks as _blocks  # noqa: E402
+from .blocks import (cross_entropy, cross_entropy_backward, embed, embed_backward,  # noqa: E402,F401
+                     residual_norm, residual_norm_backward)
+
 _SIGNATURES.update(_encoder.SIGNATURES)
+_SIGNATURES.update(_blocks.SIGNATURES)

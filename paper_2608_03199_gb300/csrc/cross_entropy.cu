@@ -1,0 +1,937 @@
+// cross_entropy.cu -- softmax cross entropy of rows against a table of classes,
+// without keeping the scores, and its backward pass.
+//
+//   z = scale h W^T + b,  lse = log sum exp z,  loss = lse - z_t
+//   q = exp(z - lse) - [v = t]
+//   dh = dloss scale q W,  dW = scale (dloss q)^T h,  db = sum dloss q
+//
+// Four products of 2 rows classes width operations each: z in the forward pass;
+// z again, dh and dW in the backward pass.  All run in one kernel,
+// k_xent<MODE>: tiles of 128 x 256, operands loaded by TMA into a ring of
+// stages, tcgen05 products into one of two accumulators in tensor memory while
+// eight warps work on the other.
+//   MODE 0  z tiles to a running maximum and sum per row; the target's score
+//           is kept apart, so that loss = log1p(sum of the others against it)
+//   MODE 1  z tiles to q, rounded to 16 bits, in a pool of panels
+//   MODE 2  dh and dW from the pool
+// The backward pass takes as many classes at a time as the pool holds (MODE 1,
+// then MODE 2); dh is added up over these pieces in fp32.
+//
+// Rows without a target are left out: k_xent_rows makes the list of the others
+// (and a copy of their h, unless every row has a target), and everything after it
+// runs over that list, whose length only the device knows.
+//
+// The pool: panel j holds 64 classes of all listed rows, [rows padded to 128]
+// [64], so its address needs no stride that depends on the list.  As operand of
+// dh a panel is K-major, as operand of dW MN-major.
+//
+// dloss differs from row to row.  dh takes it at the end, in fp32.  dW needs it
+// in the product: where all rows have the same one it is a factor at the end,
+// else h times dloss over the largest is rounded to 16 bits as an operand of its own.
+// In fp16 q is taken 2^14 times as large, so that small probabilities keep
+// their bits.
+#include <cfloat>
+#include <cstring>
+
+#include "attention.cuh"
+#include "blocks.cuh"
+#include "tensor_map.cuh"
+
+namespace sieve {
+namespace enc {
+namespace {
+
+constexpr int kM = 128, kN = 256, kK = 64;            // a tile, and the contraction of a stage
+constexpr int kBox = 64;                              // rows of a box of 128 bytes
+constexpr uint32_t kBoxBytes = kBox * 128;
+constexpr int kABoxes = kM / kBox, kBBoxes = kN / kBox;
+constexpr uint32_t kStageBytes = (kABoxes + kBBoxes) * kBoxBytes;
+constexpr int kEpiWarps = 8;
+constexpr int kThreads = (kEpiWarps + 2) * 32;
+constexpr uint32_t kOutBytes = 32 * 128;              // a warp's rows on their way out
+__host__ __device__ constexpr int stages(int mode) { return mode == 1 ? 3 : 4; }
+__host__ __device__ constexpr uint32_t smem_bytes(int mode) {
+    return 1024 + stages(mode) * kStageBytes + (mode == 0 ? 0 : kEpiWarps * kOutBytes);
+}
+constexpr uint32_t kTmemCols = 512;
+constexpr int kGrid = 152;                            // one block an SM
+constexpr int kMaxGroup = 16;                         // tiles of classes whose statistics one block keeps
+constexpr int kRowTile = 256;                         // rows of a block of k_xent_rows
+constexpr int64_t kPoolBytes = (int64_t)1 << 30;
+
+struct Ctl {
+    int32_t status;
+    int n;               // rows with a target
+    int all;             // every row has one
+    int same;            // all of them have the same dloss
+    float factor;        // that dloss, or the largest magnitude
+};
+
+struct XentArgs {
+    CUtensorMap h, hc, hs, w, pool_in, pool_out, acc, dw;
+    Ctl *ctl;
+    const int *target;                    // of the list
+    const float *lse, *loss, *dloss;      // of the list
+    const float *bias;
+    float *hit;                           // [rows] the target's score
+    float2 *part;                         // [parts][rows of the list, padded] maximum and sum
+    float *colsum;                        // [32 rows][classes]
+    int64_t pool_rows;
+    int rows, classes, width;
+    float scale, c;                       // c = scale log2(e)
+    int want_dh, want_dw, want_db, dw_f32, accumulate;
+};
+
+template <typename T>
+constexpr float kUp = std::is_same_v<T, __half> ? 16384.f : 1.f;
+
+// classes of a piece, and how the forward pass groups its tiles
+__host__ __device__ inline int64_t padded(int64_t n) { return (n < 1 ? 1 : n) + kM - 1 - ((n < 1 ? 1 : n) - 1) % kM; }
+__host__ __device__ inline int piece_classes(int64_t n, int classes, int64_t pool_rows) {
+    const int64_t most = pool_rows / padded(n) / (kN / kK) * kN;
+    const int64_t pieces = (classes + most - 1) / most, each = (classes + pieces - 1) / pieces;
+    return (int)((each + kN - 1) / kN * kN);
+}
+__host__ __device__ inline int group_tiles(int64_t n, int classes) {
+    const int64_t tiles = padded(n) / kM * ((classes + kN - 1) / kN), g = tiles / (8 * kGrid);
+    return (int)(g < 1 ? 1 : g > kMaxGroup ? kMaxGroup : g);
+}
+
+// ---------------------------------------------------------------------------
+// The rows with a target.
+struct RowArgs {
+    const void *targets, *h;
+    const float *dloss, *loss, *lse;      // backward
+    float *loss_out, *lse_out;            // forward: zeros where there is no target
+    void *dh;                             // backward: the same
+    int64_t h_stride, dh_stride;
+    int rows, classes, width, target_type;
+    Ctl *ctl;
+    int *count;                           // [blocks]
+    uint32_t *top, *low;                  // [blocks] largest dloss, and its lowest, as ordered keys
+    int *row, *target;
+    float *dloss_c, *loss_c, *lse_c;
+    void *hc, *hs;
+};
+
+// whole numbers in the order of the floats
+__device__ __forceinline__ uint32_t ordered(float v) {
+    const uint32_t b = __float_as_uint(v);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float unordered(uint32_t k) {
+    return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
+}
+
+__global__ void __launch_bounds__(kRowTile) k_xent_count(const RowArgs a) {
+    __shared__ uint32_t top[kRowTile / 32], low[kRowTile / 32];
+    const int64_t r = (int64_t)blockIdx.x * kRowTile + threadIdx.x;
+    const bool live = r < a.rows && id_at(a.targets, a.target_type, r, a.classes) >= 0;
+    const int n = __syncthreads_count(live);
+    if (threadIdx.x == 0) a.count[blockIdx.x] = n;
+    if (!a.dloss) return;
+    const uint32_t k = live ? ordered(a.dloss[r]) : 0;
+    const uint32_t t = __reduce_max_sync(0xffffffffu, k), l = __reduce_min_sync(0xffffffffu, live ? k : 0xffffffffu);
+    if (lane_id() == 0) {
+        top[threadIdx.x >> 5] = t;
+        low[threadIdx.x >> 5] = l;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        uint32_t t2 = 0, l2 = 0xffffffffu;
+        for (int w = 0; w < kRowTile / 32; ++w) {
+            t2 = max(t2, top[w]);
+            l2 = min(l2, low[w]);
+        }
+        a.top[blockIdx.x] = t2;
+        a.low[blockIdx.x] = l2;
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kRowTile) k_xent_rows(const RowArgs a) {
+    constexpr int kWarps = kRowTile / 32;
+    __shared__ int s_before[kWarps], s_all[kWarps], s_rank[kWarps], s_list[kRowTile];
+    __shared__ uint32_t s_top[kWarps], s_low[kWarps];
+    const int tid = threadIdx.x, lane = lane_id(), warp = tid >> 5;
+    int before = 0, all = 0;
+    uint32_t top = 0, low = 0xffffffffu;
+#pragma unroll 4
+    for (int b = tid; b < (int)gridDim.x; b += kRowTile) {
+        const int c = a.count[b];
+        all += c;
+        if (b < (int)blockIdx.x) before += c;
+        if (a.dloss) {
+            top = max(top, a.top[b]);
+            low = min(low, a.low[b]);
+        }
+    }
+    before = __reduce_add_sync(0xffffffffu, before);
+    all = __reduce_add_sync(0xffffffffu, all);
+    top = __reduce_max_sync(0xffffffffu, top);
+    low = __reduce_min_sync(0xffffffffu, low);
+    const int64_t r = (int64_t)blockIdx.x * kRowTile + tid;
+    const int t = r < a.rows ? id_at(a.targets, a.target_type, r, a.classes) : -1;
+    const unsigned live = __ballot_sync(0xffffffffu, t >= 0);
+    if (lane == 0) {
+        s_before[warp] = before;
+        s_all[warp] = all;
+        s_top[warp] = top;
+        s_low[warp] = low;
+        s_rank[warp] = __popc(live);
+    }
+    __syncthreads();
+    before = all = 0;
+    top = 0;
+    low = 0xffffffffu;
+    int rank = 0, here = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        before += s_before[w];
+        all += s_all[w];
+        top = max(top, s_top[w]);
+        low = min(low, s_low[w]);
+        if (w < warp) rank += s_rank[w];
+        here += s_rank[w];
+    }
+    rank += __popc(live & ((1u << lane) - 1));
+    const bool every = all == a.rows, same = top == low;
+    const float hi = unordered(top), lo = unordered(low);
+    const float factor = same ? hi : fmaxf(fabsf(hi), fabsf(lo));
+    if (blockIdx.x == 0 && tid == 0) {
+        a.ctl->status = 0;
+        a.ctl->n = all;
+        a.ctl->all = every;
+        a.ctl->same = !a.dloss || same;
+        a.ctl->factor = a.dloss && all > 0 ? factor : 0.f;
+    }
+    if (t >= 0) {
+        const int at = before + rank;
+        s_list[rank] = tid;
+        a.row[at] = (int)r;
+        a.target[at] = t;
+        if (a.dloss) {
+            a.dloss_c[at] = a.dloss[r];
+            a.loss_c[at] = a.loss[r];
+            a.lse_c[at] = a.lse[r];
+        }
+    } else if (r < a.rows && a.loss_out) {
+        a.loss_out[r] = 0.f;
+        a.lse_out[r] = 0.f;
+    }
+    __syncthreads();
+    const T *h = static_cast<const T *>(a.h);
+    const int chunks = a.width / 8;
+    const bool scaled = a.dloss && a.hs && !same;
+    if (!every || scaled) {
+        T *hc = static_cast<T *>(a.hc), *hs = static_cast<T *>(a.hs);
+        for (int i = warp; i < here; i += kWarps) {
+            const int64_t from = (int64_t)blockIdx.x * kRowTile + s_list[i], to = before + i;
+            const float f = scaled ? a.dloss[from] / factor : 0.f;
+#pragma unroll 4
+            for (int c = lane; c < chunks; c += 32) {
+                const uint4 raw = __ldg(reinterpret_cast<const uint4 *>(h + from * a.h_stride) + c);
+                if (!every) reinterpret_cast<uint4 *>(hc + to * a.width)[c] = raw;
+                if (scaled) {
+                    const T *x = reinterpret_cast<const T *>(&raw);
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = f * to_f32<T>(x[e]);
+                    reinterpret_cast<uint4 *>(hs + to * a.width)[c] = pack8<T>(v);
+                }
+            }
+        }
+        // the last tile's places past the list: zeros
+        if (blockIdx.x == 0) {
+            const int last = (int)min(padded(all), (int64_t)a.rows);
+            for (int i = all + warp; i < last; i += kWarps)
+                for (int c = lane; c < chunks; c += 32) {
+                    if (!every) reinterpret_cast<uint4 *>(hc + (int64_t)i * a.width)[c] = make_uint4(0, 0, 0, 0);
+                    if (scaled) reinterpret_cast<uint4 *>(hs + (int64_t)i * a.width)[c] = make_uint4(0, 0, 0, 0);
+                }
+        }
+    }
+    if (a.dh && here < kRowTile)
+        for (int i = warp; i < kRowTile; i += kWarps) {
+            const int64_t row = (int64_t)blockIdx.x * kRowTile + i;
+            if (row >= a.rows || id_at(a.targets, a.target_type, row, a.classes) >= 0) continue;
+            for (int c = lane; c < chunks; c += 32)
+                reinterpret_cast<uint4 *>(static_cast<T *>(a.dh) + row * a.dh_stride)[c] = make_uint4(0, 0, 0, 0);
+        }
+}
+
+// ---------------------------------------------------------------------------
+// Instruction descriptor: fp32 accumulation, M = 128, both operands T, K- or MN-major.
+template <typename T>
+__device__ __forceinline__ uint32_t product(int N, bool a_mn, bool b_mn) {
+    return idesc<T>(N, b_mn) | (a_mn ? 1u << 15 : 0u);
+}
+// MN-major operand of boxes of 64 columns by 64 rows of the contraction axis
+__device__ __forceinline__ uint64_t desc_boxes(const void *tile) {
+    return (tc::desc_k_sw128(tc::smem_u32(tile)) & ~((uint64_t)0x3FFF << 16)) | (uint64_t)(kBoxBytes >> 4) << 16;
+}
+
+__device__ __forceinline__ void load_box(void *dst, const CUtensorMap *map, int x, int y, uint64_t *bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], "
+        "[%4];" ::"r"(tc::smem_u32(dst)),
+        "l"(map), "r"(x), "r"(y), "r"(tc::smem_u32(bar))
+        : "memory");
+}
+__device__ __forceinline__ void store_box(const CUtensorMap *map, int x, int y, const void *src) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x),
+                 "r"(y), "r"(tc::smem_u32(src))
+                 : "memory");
+}
+__device__ __forceinline__ void add_box(const CUtensorMap *map, int x, int y, const void *src) {
+    asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map),
+                 "r"(x), "r"(y), "r"(tc::smem_u32(src))
+                 : "memory");
+}
+__device__ __forceinline__ void stores_issued() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
+// One tile's work.
+struct Tile {
+    int m0, n0;          // first row and column of the result
+    int n_boxes;         // of 64 columns
+    int blocks;          // stages of the contraction axis
+    bool dw;             // MODE 2: dW, else dh
+};
+
+// The tiles of a launch, in order: what every role walks.
+template <int MODE>
+struct Walk {
+    int n, mp, row_tiles, class_tiles, group, groups;
+    int v0, v1;                                      // classes of the piece
+    int dh_tiles, d_tiles, dw_rows, total, width;
+    __device__ __forceinline__ Walk(const XentArgs &a, int piece) {
+        n = a.ctl->n;
+        mp = (int)padded(n);
+        width = a.width;
+        row_tiles = (n + kM - 1) / kM;
+        d_tiles = (a.width + kN - 1) / kN;
+        v0 = 0;
+        v1 = a.classes;
+        if (MODE != 0) {
+            const int each = piece_classes(n, a.classes, a.pool_rows);
+            v0 = (int)min((int64_t)piece * each, (int64_t)a.classes);
+            v1 = (int)min((int64_t)v0 + each, (int64_t)a.classes);
+        }
+        class_tiles = (v1 - v0 + kN - 1) / kN;
+        group = MODE == 0 ? group_tiles(n, a.classes) : 1;
+        groups = (class_tiles + group - 1) / group;
+        dh_tiles = a.want_dh && v1 > v0 ? row_tiles * d_tiles : 0;
+        dw_rows = a.want_dw ? (v1 - v0 + kM - 1) / kM : 0;
+        total = MODE == 2 ? dh_tiles + dw_rows * d_tiles : row_tiles * groups;
+    }
+    // tiles of item i
+    __device__ __forceinline__ int tiles(int i) const {
+        return MODE == 0 ? min(group, class_tiles - i / row_tiles * group) : 1;
+    }
+    __device__ __forceinline__ Tile tile(int i, int k) const {
+        Tile t;
+        if (MODE != 2) {
+            t.m0 = i % row_tiles * kM;
+            t.n0 = v0 + (i / row_tiles * group + k) * kN;
+            t.n_boxes = kBBoxes;
+            t.blocks = (width + kK - 1) / kK;
+            t.dw = false;
+            return t;
+        }
+        t.dw = i >= dh_tiles;
+        if (t.dw) i -= dh_tiles;
+        const int across = t.dw ? dw_rows : row_tiles;
+        t.m0 = i % across * kM;
+        t.n0 = i / across * kN;
+        t.n_boxes = min(kBBoxes, (width - t.n0 + kBox - 1) / kBox);
+        t.blocks = t.dw ? (n + kK - 1) / kK : (v1 - v0 + kK - 1) / kK;
+        return t;
+    }
+};
+
+template <typename T, int MODE, bool BIAS>
+__global__ void __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ XentArgs a, int piece) {
+    constexpr int kStages = stages(MODE);
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t full[kStages], empty[kStages], d_full[2], d_empty[2], drained;
+    __shared__ uint32_t tmem_slot;
+    __shared__ int s_abort;
+    __shared__ __align__(16) float s_bias[kEpiWarps][BIAS ? kN / 2 : 4];
+    const Walk<MODE> walk(a, piece);
+    if (walk.total == 0) return;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = lane_id();
+    unsigned char *base = reinterpret_cast<unsigned char *>(
+        (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            tc::mbar_init(&full[s], 1);
+            tc::mbar_init(&empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            tc::mbar_init(&d_full[b], 1);
+            tc::mbar_init(&d_empty[b], kEpiWarps);
+        }
+        tc::mbar_init(&drained, 1);
+        s_abort = 0;
+        tc::mbar_init_fence();
+    }
+    if (warp == 0) tc::tmem_alloc(&tmem_slot, kTmemCols);
+    tc::fence_before_sync();
+    __syncthreads();
+    tc::fence_after_sync();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
+    const Waiter wait{&s_abort};
+    const bool all = a.ctl->all, same = a.ctl->same;
+
+    if (warp == kEpiWarps) {
+        // ---------------- loads ----------------
+        const CUtensorMap *rows = MODE == 2 && !same ? &a.hs : all ? &a.h : &a.hc;
+        int s = 0;
+        bool ok = true;
+        for (int i = blockIdx.x; ok && i < walk.total; i += gridDim.x)
+            for (int k = 0, nk = walk.tiles(i); ok && k < nk; ++k) {
+                const Tile t = walk.tile(i, k);
+#pragma unroll 1
+                for (int b = 0; b < t.blocks; ++b, ++s) {
+                    const int st = s % kStages;
+                    if (!(ok = wait.warp(&empty[st], ((uint32_t)(s / kStages) & 1u) ^ 1u))) break;
+                    if (elected()) {
+                        unsigned char *pa = base + st * kStageBytes, *pb = pa + kABoxes * kBoxBytes;
+                        expect(&full[st], (kABoxes + t.n_boxes) * kBoxBytes);
+#pragma unroll
+                        for (int j = 0; j < kABoxes; ++j) {
+                            void *dst = pa + j * kBoxBytes;
+                            if (MODE != 2) load_box(dst, rows, b * kK, t.m0 + j * kBox, &full[st]);
+                            else if (t.dw) load_box(dst, &a.pool_in, 0, (t.m0 / kBox + j) * walk.mp + b * kK, &full[st]);
+                            else load_box(dst, &a.pool_in, 0, b * walk.mp + t.m0 + j * kBox, &full[st]);
+                        }
+                        for (int j = 0; j < t.n_boxes; ++j) {
+                            void *dst = pb + j * kBoxBytes;
+                            if (MODE != 2) load_box(dst, &a.w, b * kK, t.n0 + j * kBox, &full[st]);
+                            else if (t.dw) load_box(dst, rows, t.n0 + j * kBox, b * kK, &full[st]);
+                            else load_box(dst, &a.w, t.n0 + j * kBox, walk.v0 + b * kK, &full[st]);
+                        }
+                    }
+                    __syncwarp();
+                }
+            }
+        if (!ok)      // after an abort: what is in flight lands before the block ends
+            for (int j = max(0, s - kStages); j < s; ++j) let_land(&full[j % kStages], (uint32_t)(j / kStages) & 1u);
+        __syncwarp();
+    } else if (warp == kEpiWarps + 1) {
+        // ---------------- products ----------------
+        int s = 0, c = 0;
+        bool ok = true;
+        for (int i = blockIdx.x; ok && i < walk.total; i += gridDim.x)
+            for (int k = 0, nk = walk.tiles(i); ok && k < nk; ++k, ++c) {
+                const Tile t = walk.tile(i, k);
+                const int buf = c & 1;
+                if (!(ok = wait.warp(&d_empty[buf], ((uint32_t)(c >> 1) & 1u) ^ 1u))) break;
+                const bool a_mn = MODE == 2 && t.dw, b_mn = MODE == 2;
+                const uint32_t id = product<T>(t.n_boxes * kBox, a_mn, b_mn), d = tmem + buf * kN;
+                const uint64_t step_a = a_mn ? 128 : 2, step_b = b_mn ? 128 : 2;
+#pragma unroll 1
+                for (int b = 0; b < t.blocks; ++b, ++s) {
+                    const int st = s % kStages;
+                    if (!(ok = wait.warp(&full[st], (uint32_t)(s / kStages) & 1u))) break;
+                    tc::fence_after_sync();
+                    if (elected()) {
+                        const unsigned char *pa = base + st * kStageBytes, *pb = pa + kABoxes * kBoxBytes;
+                        const uint64_t da = a_mn ? desc_boxes(pa) : desc_k(pa), db = b_mn ? desc_boxes(pb) : desc_k(pb);
+#pragma unroll
+                        for (int x = 0; x < kK / 16; ++x)
+                            mma_ss(d, da + x * step_a, db + x * step_b, id, b > 0 || x > 0);
+                        commit(&empty[st]);
+                    }
+                    __syncwarp();
+                }
+                if (!ok) break;
+                if (elected()) commit(&d_full[buf]);
+                __syncwarp();
+            }
+        // every product issued ends before the block frees its memory
+        if (elected()) commit(&drained);
+        __syncwarp();
+        let_land(&drained, 0);
+        __syncwarp();
+    } else {
+        // ---------------- what becomes of a tile ----------------
+        const int quarter = warp & 3, half = warp >> 2, r = quarter * 32 + lane;
+        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+        unsigned char *out = base + kStages * kStageBytes + warp * kOutBytes;
+        const float factor = MODE == 2 ? a.ctl->factor * a.scale / kUp<T> : 0.f;
+        int c = 0;
+        bool ok = true;
+        for (int i = blockIdx.x; ok && i < walk.total; i += gridDim.x) {
+            float top = -INFINITY, sum = 0.f, lse = 0.f, dloss = 0.f;
+            int target = -1, row = 0;
+            bool live = false;
+            if (MODE != 2) {
+                row = walk.tile(i, 0).m0 + r;
+                live = row < walk.n;
+                if (live) target = a.target[row];
+                if (MODE == 1 && live) {
+                    lse = a.lse[row];
+                    if (lse == -INFINITY) lse = INFINITY;       // every class hidden: no probabilities
+                    if (!BIAS) lse *= kLog2e;
+                    dloss = a.dloss[row];
+                }
+            }
+            for (int k = 0, nk = walk.tiles(i); ok && k < nk; ++k, ++c) {
+                const Tile t = walk.tile(i, k);
+                const int buf = c & 1;
+                // this warp's columns of the tile
+                const int col = t.n0 + half * (kN / 2);
+                if (MODE != 2 && BIAS) {
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < kN / 2; j += 32)
+                        s_bias[warp][j + lane] = col + j + lane < a.classes ? __ldg(a.bias + col + j + lane) : -INFINITY;
+                    __syncwarp();
+                }
+                if (!(ok = wait.warp(&d_full[buf], (uint32_t)(c >> 1) & 1u))) break;
+                tc::fence_after_sync();
+                const uint32_t d = lanes + buf * kN + half * (kN / 2);
+                if constexpr (MODE == 0) {
+#pragma unroll 1
+                    for (int j = 0; j < kN / 2; j += 32) {
+                        float x[32];
+                        tc::tmem_ld32(d + j, x);
+                        if constexpr (BIAS) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) x[e] = fmaf(x[e], a.scale, s_bias[warp][j + e]);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) x[e] *= a.c;
+                            const int left = a.classes - col - j;
+                            if (left < 32)
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) x[e] = e < left ? x[e] : -INFINITY;
+                        }
+                        const int at = target - col - j;
+                        if (__any_sync(0xffffffffu, at >= 0 && at < 32)) {
+                            float hit = 0.f;
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (e == at) {
+                                    hit = x[e];
+                                    x[e] = -INFINITY;
+                                }
+                            if (at >= 0 && at < 32) a.hit[row] = hit;
+                        }
+                        const float high = fmaxf(top, max_of_32(x)), from = high == -INFINITY ? 0.f : high;
+                        constexpr float unit = BIAS ? kLog2e : 1.f;
+                        float s0 = sum * exp2_approx((top - from) * unit), s1 = 0.f, s2 = 0.f, s3 = 0.f;
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4) {
+                            s0 += exp2_approx((x[e] - from) * unit);
+                            s1 += exp2_approx((x[e + 1] - from) * unit);
+                            s2 += exp2_approx((x[e + 2] - from) * unit);
+                            s3 += exp2_approx((x[e + 3] - from) * unit);
+                        }
+                        sum = (s0 + s1) + (s2 + s3);
+                        top = high;
+                    }
+                } else if constexpr (MODE == 1) {
+#pragma unroll 1
+                    for (int j = 0; j < kN / 2; j += 64) {
+                        uint32_t packed[32];
+#pragma unroll
+                        for (int jj = 0; jj < 64; jj += 32) {
+                            float x[32];
+                            tc::tmem_ld32(d + j + jj, x);
+                            const int first = col + j + jj;
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                x[e] = BIAS ? exp2_approx((fmaf(x[e], a.scale, s_bias[warp][j + jj + e]) - lse) * kLog2e)
+                                            : exp2_approx(fmaf(x[e], a.c, -lse));
+                            const int at = target - first;
+                            if (__any_sync(0xffffffffu, at >= 0 && at < 32)) {
+                                const float q = at >= 0 && at < 32 ? expm1f(-a.loss[row]) : 0.f;
+#pragma unroll
+                                for (int e = 0; e < 32; ++e)
+                                    if (e == at) x[e] = q;
+                            }
+                            // nothing past the list or the classes
+                            const int left = live ? a.classes - first : 0;
+                            if (__any_sync(0xffffffffu, left < 32))
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) x[e] = e < left ? x[e] : 0.f;
+#pragma unroll
+                            for (int e = 0; e < 32; e += 2)
+                                packed[(jj + e) / 2] = pack2<T>(x[e] * kUp<T>, x[e + 1] * kUp<T>);
+                            if (BIAS && a.want_db) {
+                                // the columns' sums over the warp's rows: lane e ends with column e
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) x[e] = live ? x[e] * dloss : 0.f;
+#pragma unroll
+                                for (int w = 16; w; w >>= 1) {
+                                    const bool up = lane & w;
+#pragma unroll
+                                    for (int e = 0; e < w; ++e) {
+                                        const float keep = up ? x[e + w] : x[e], give = up ? x[e] : x[e + w];
+                                        x[e] = keep + __shfl_xor_sync(0xffffffffu, give, w);
+                                    }
+                                }
+                                if (first + lane < a.classes)
+                                    a.colsum[((int64_t)t.m0 / 32 + quarter) * a.classes + first + lane] = x[0];
+                            }
+                        }
+                        stores_read();
+                        __syncwarp();
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            *reinterpret_cast<uint4 *>(out + lane * 128 + ((e ^ (lane & 7)) << 4)) =
+                                make_uint4(packed[4 * e], packed[4 * e + 1], packed[4 * e + 2], packed[4 * e + 3]);
+                        tc::fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) {
+                            store_box(&a.pool_out, 0, (col + j - walk.v0) / kK * walk.mp + t.m0 + quarter * 32, out);
+                            stores_issued();
+                        }
+                    }
+                } else {
+                    const int columns = t.n_boxes * kBox;        // of the tile that exist
+                    const int r0 = (t.dw ? walk.v0 : 0) + t.m0 + quarter * 32;
+                    const bool some = t.dw ? r0 < walk.v1 : true;
+                    const bool wide = !t.dw || a.dw_f32;         // fp32 results: 32 columns to a box, else 64
+                    const bool adds = t.dw ? a.accumulate : piece > 0;
+                    const float f = t.dw ? factor : 1.f;
+                    // (dh: past the list's rows of the last tile nothing is read again)
+#pragma unroll 1
+                    for (int j = 0; j < kN / 2 && half * (kN / 2) + j < columns; j += 64) {
+                        float x[2][32];
+                        if (t.blocks > 0) {
+                            tc::tmem_ld32(d + j, x[0]);
+                            tc::tmem_ld32(d + j + 32, x[1]);
+                        }
+#pragma unroll
+                        for (int b = 0; b < 2; ++b)
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) x[b][e] = t.blocks > 0 ? x[b][e] * f : 0.f;
+                        const int x0 = t.n0 + half * (kN / 2) + j;
+                        const CUtensorMap *map = t.dw ? &a.dw : &a.acc;
+                        if (wide) {
+#pragma unroll
+                            for (int b = 0; b < 2; ++b) {
+                                stores_read();
+                                __syncwarp();
+#pragma unroll
+                                for (int e = 0; e < 8; ++e)
+                                    *reinterpret_cast<float4 *>(out + lane * 128 + ((e ^ (lane & 7)) << 4)) =
+                                        make_float4(x[b][4 * e], x[b][4 * e + 1], x[b][4 * e + 2], x[b][4 * e + 3]);
+                                tc::fence_proxy_async_smem();
+                                __syncwarp();
+                                if (lane == 0 && some && x0 + 32 * b < a.width) {
+                                    if (adds) add_box(map, x0 + 32 * b, r0, out);
+                                    else store_box(map, x0 + 32 * b, r0, out);
+                                    stores_issued();
+                                }
+                            }
+                        } else {
+                            stores_read();
+                            __syncwarp();
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                *reinterpret_cast<uint4 *>(out + lane * 128 + ((e ^ (lane & 7)) << 4)) =
+                                    pack8<T>(&x[e / 4][8 * (e % 4)]);
+                            tc::fence_proxy_async_smem();
+                            __syncwarp();
+                            if (lane == 0 && some) {
+                                store_box(map, x0, r0, out);
+                                stores_issued();
+                            }
+                        }
+                    }
+                }
+                tc::fence_before_sync();
+                warp_arrive(&d_empty[buf]);
+            }
+            if (MODE == 0 && ok && live)
+                a.part[(int64_t)(i / walk.row_tiles * 2 + half) * walk.mp + row] = make_float2(top, sum);
+        }
+        stores_done();
+    }
+    tc::fence_before_sync();
+    __syncthreads();
+    if (warp == 0) {
+        tc::fence_after_sync();
+        tc::tmem_dealloc(tmem, kTmemCols);
+    }
+    if (threadIdx.x == 0 && s_abort) atomicExch(&a.ctl->status, SIEVE_ETIMEOUT);
+}
+
+// ---------------------------------------------------------------------------
+// The parts of a row's statistics added up: 32 rows by 16 strands of parts.
+struct JoinArgs {
+    const Ctl *ctl;
+    const int *row;
+    const float *hit;
+    const float2 *part;
+    int classes, biased;
+    float *loss, *lse;
+};
+constexpr int kStrands = 16;
+
+__global__ void __launch_bounds__(32 * kStrands) k_xent_join(const JoinArgs a) {
+    __shared__ float2 s_part[kStrands][32];
+    const int lane = lane_id(), strand = threadIdx.x >> 5;
+    const int n = a.ctl->n;
+    const int group = group_tiles(n, a.classes), tiles = (a.classes + kN - 1) / kN;
+    const int parts = (tiles + group - 1) / group * 2;
+    const int64_t stride = padded(n);
+    const float unit = a.biased ? kLog2e : 1.f;
+    for (int64_t i0 = (int64_t)blockIdx.x * 32; i0 < n; i0 += (int64_t)gridDim.x * 32) {
+        const int64_t i = i0 + lane;
+        float m = -INFINITY, s = 0.f;
+        auto merge = [&](float2 p) {
+            const float high = fmaxf(m, p.x), from = high == -INFINITY ? 0.f : high;
+            s = s * exp2_approx((m - from) * unit) + p.y * exp2_approx((p.x - from) * unit);
+            m = high;
+        };
+        if (i < n)
+#pragma unroll 4
+            for (int p = strand; p < parts; p += kStrands) merge(a.part[p * stride + i]);
+        __syncthreads();
+        s_part[strand][lane] = make_float2(m, s);
+        __syncthreads();
+        if (strand > 0 || i >= n) continue;
+        m = -INFINITY;
+        s = 0.f;
+        for (int k = 0; k < kStrands; ++k) merge(s_part[k][lane]);
+        // the others' sum s 2^m and the target's score, in base 2 (a bias: in base e)
+        const float hit = a.hit[i], d = (m - hit) * unit;
+        const float ln = a.biased ? 1.f : kLn2;               // to natural units
+        float loss, lse;
+        if (hit == -INFINITY) {                               // a hidden target
+            loss = INFINITY;
+            lse = m == -INFINITY ? -INFINITY : m * ln + logf(s);
+        } else if (m <= hit) {
+            loss = log1pf(s * exp2f(d));
+            lse = hit * ln + loss;
+        } else {
+            const float more = logf(s + exp2f(-d));
+            loss = (m - hit) * ln + more;
+            lse = m * ln + more;
+        }
+        if (isnan(s) || isnan(hit)) loss = lse = NAN;
+        const int64_t r = a.row[i];
+        a.loss[r] = loss;
+        a.lse[r] = lse;
+    }
+}
+
+// dh from its fp32 sums: the list's rows to their places.
+template <typename T>
+__global__ void __launch_bounds__(256) k_xent_dh(const Ctl *ctl, const int *row, const float *dloss, const float *acc, int width,
+                                                 float scale, T *dh, int64_t stride) {
+    const int chunks = width / 8;
+    const int64_t total = (int64_t)ctl->n * chunks;
+    for (int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x; w < total; w += (int64_t)gridDim.x * 256) {
+        const int64_t i = w / chunks;
+        const int c = (int)(w - i * chunks);
+        const float f = dloss[i] * scale / kUp<T>;
+        const float4 *x = reinterpret_cast<const float4 *>(acc + i * width) + 2 * c;
+        const float4 p = __ldcs(x), q = __ldcs(x + 1);
+        const float v[8] = {p.x * f, p.y * f, p.z * f, p.w * f, q.x * f, q.y * f, q.z * f, q.w * f};
+        reinterpret_cast<uint4 *>(dh + row[i] * stride)[c] = pack8<T>(v);
+    }
+}
+
+// dbias from the column sums of every 32 rows: 32 columns by 8 strands.
+__global__ void __launch_bounds__(256) k_xent_db(const Ctl *ctl, const float *colsum, int classes, float *db) {
+    __shared__ float part[8][32];
+    const int lane = lane_id(), strand = threadIdx.x >> 5, v = blockIdx.x * 32 + lane;
+    const int sums = (ctl->n + kM - 1) / kM * (kM / 32);
+    float s = 0.f;
+    if (v < classes)
+#pragma unroll 4
+        for (int t = strand; t < sums; t += 8) s += colsum[(int64_t)t * classes + v];
+    part[strand][lane] = s;
+    __syncthreads();
+    if (strand || v >= classes) return;
+    for (int k = 1; k < 8; ++k) s += part[k][lane];
+    db[v] = s;
+}
+
+// ---------------------------------------------------------------------------
+struct Layout {
+    size_t count, top, low, row, target, dloss, loss, lse, hc, hs, hit, part, pool, acc, colsum, bytes;
+    int64_t pool_rows;
+};
+Layout layout(const sieve_cross_entropy_args &a, bool backward) {
+    Layout l = {};
+    size_t at = kCtlBytes;
+    auto take = [&](int64_t bytes) {
+        const size_t here = at;
+        at += (size_t)round_up(bytes, 1024);
+        return here;
+    };
+    const int64_t n = a.rows, np = padded(n), blocks = ceil_div(n, kRowTile);
+    l.count = take(blocks * 4);
+    l.row = take(n * 4);
+    l.target = take(n * 4);
+    l.hc = take(n * a.width * 2);
+    if (!backward) {
+        const int64_t row_tiles = np / kM, class_tiles = ceil_div(a.classes, kN);
+        // (group_tiles: up to 16 tiles a part, and no fewer than 8 parts a block before that)
+        const int64_t whole = ceil_div(row_tiles * class_tiles, kMaxGroup), parts = (whole > 16 * kGrid ? whole : 16 * kGrid) + row_tiles;
+        l.hit = take(n * 4);
+        l.part = take((parts < row_tiles * class_tiles ? parts : row_tiles * class_tiles) * 2 * kM * 8);
+    } else {
+        l.top = take(blocks * 4);
+        l.low = take(blocks * 4);
+        l.dloss = take(n * 4);
+        l.loss = take(n * 4);
+        l.lse = take(n * 4);
+        l.hs = take(n * a.width * 2);
+        const int64_t needed = np * (round_up(a.classes, kN) / kK), least = np * (kN / kK), most = kPoolBytes / 128;
+        l.pool_rows = needed < most ? needed : least > most ? least : most;
+        l.pool = take(l.pool_rows * 128);
+        l.acc = take(np * a.width * 4);
+        if (a.bias) l.colsum = take(np / 32 * a.classes * 4);
+    }
+    l.bytes = at;
+    return l;
+}
+
+template <typename T, int MODE, bool BIAS>
+cudaError_t run(const XentArgs &a, int piece, cudaStream_t st) {
+    auto kernel = k_xent<T, MODE, BIAS>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(MODE));
+    if (e != cudaSuccess) return e;
+    kernel<<<kGrid, kThreads, smem_bytes(MODE), st>>>(a, piece);
+    return cudaGetLastError();
+}
+
+struct Call {
+    XentArgs x;
+    RowArgs r;
+    unsigned blocks;
+};
+sieve_status prepare(Call &c, const sieve_cross_entropy_args &a, const Layout &l, unsigned char *ws) {
+    std::memset(&c, 0, sizeof c);
+    XentArgs &x = c.x;
+    x.ctl = reinterpret_cast<Ctl *>(ws);
+    x.target = reinterpret_cast<int *>(ws + l.target);
+    x.bias = a.bias;
+    x.rows = (int)a.rows;
+    x.classes = (int)a.classes;
+    x.width = a.width;
+    x.scale = a.scale;
+    x.c = a.scale * kLog2e;
+    RowArgs &r = c.r;
+    r.targets = a.targets;
+    r.h = a.h;
+    r.h_stride = a.h_stride;
+    r.rows = x.rows;
+    r.classes = x.classes;
+    r.width = a.width;
+    r.target_type = a.target_type;
+    r.ctl = x.ctl;
+    r.count = reinterpret_cast<int *>(ws + l.count);
+    r.row = reinterpret_cast<int *>(ws + l.row);
+    r.target = reinterpret_cast<int *>(ws + l.target);
+    r.hc = ws + l.hc;
+    c.blocks = (unsigned)ceil_div(a.rows, kRowTile);
+    sieve_status rc = make_matrix_map(&x.h, a.dtype, a.h, a.rows, a.width, a.h_stride, kBox);
+    if (rc == SIEVE_OK) rc = make_matrix_map(&x.hc, a.dtype, ws + l.hc, a.rows, a.width, a.width, kBox);
+    if (rc == SIEVE_OK) rc = make_matrix_map(&x.w, a.dtype, a.weight, a.classes, a.width, a.weight_stride, kBox);
+    return rc;
+}
+
+template <typename T>
+cudaError_t forward(const Call &c, const JoinArgs &j, cudaStream_t st) {
+    k_xent_count<<<c.blocks, kRowTile, 0, st>>>(c.r);
+    k_xent_rows<T><<<c.blocks, kRowTile, 0, st>>>(c.r);
+    cudaError_t e = c.x.bias ? run<T, 0, true>(c.x, 0, st) : run<T, 0, false>(c.x, 0, st);
+    if (e != cudaSuccess) return e;
+    const int64_t blocks = ceil_div(c.x.rows, 32);
+    k_xent_join<<<(unsigned)(blocks < 4096 ? blocks : 4096), 32 * kStrands, 0, st>>>(j);
+    return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t backward(const Call &c, const sieve_cross_entropy_grads &g, const float *acc, int pieces, cudaStream_t st) {
+    k_xent_count<<<c.blocks, kRowTile, 0, st>>>(c.r);
+    k_xent_rows<T><<<c.blocks, kRowTile, 0, st>>>(c.r);
+    for (int p = 0; p < pieces; ++p) {
+        cudaError_t e = c.x.bias ? run<T, 1, true>(c.x, p, st) : run<T, 1, false>(c.x, p, st);
+        if (e == cudaSuccess && (g.dh || g.dweight)) e = run<T, 2, false>(c.x, p, st);
+        if (e != cudaSuccess) return e;
+    }
+    if (g.dh)
+        k_xent_dh<T><<<kGrid * 8, 256, 0, st>>>(c.x.ctl, c.r.row, c.x.dloss, acc, c.x.width, c.x.scale, static_cast<T *>(g.dh),
+                                               g.dh_stride);
+    if (g.dbias)
+        k_xent_db<<<(unsigned)ceil_div(c.x.classes, 32), 256, 0, st>>>(c.x.ctl, c.x.colsum, c.x.classes, g.dbias);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+size_t cross_entropy_workspace_bytes(const sieve_cross_entropy_args &a) { return layout(a, false).bytes; }
+size_t cross_entropy_backward_workspace_bytes(const sieve_cross_entropy_args &a) { return layout(a, true).bytes; }
+
+sieve_status launch_cross_entropy(const sieve_cross_entropy_args &a, float *loss, float *lse, void *ws,
+                                  cudaStream_t st) {
+    unsigned char *base = static_cast<unsigned char *>(ws);
+    const Layout l = layout(a, false);
+    Call c;
+    const sieve_status rc = prepare(c, a, l, base);
+    if (rc != SIEVE_OK) return rc;
+    c.x.hit = reinterpret_cast<float *>(base + l.hit);
+    c.x.part = reinterpret_cast<float2 *>(base + l.part);
+    c.r.loss_out = loss;
+    c.r.lse_out = lse;
+    const JoinArgs j = {c.x.ctl, c.r.row, c.x.hit, c.x.part, c.x.classes, a.bias != nullptr, loss, lse};
+    const cudaError_t e = a.dtype == SIEVE_F16 ? forward<__half>(c, j, st) : forward<__nv_bfloat16>(c, j, st);
+    return e == cudaSuccess ? SIEVE_OK : record_cuda_error(e);
+}
+
+sieve_status launch_cross_entropy_backward(const sieve_cross_entropy_args &a, const sieve_cross_entropy_grads &g,
+                                           void *ws, cudaStream_t st) {
+    unsigned char *base = static_cast<unsigned char *>(ws);
+    const Layout l = layout(a, true);
+    Call c;
+    sieve_status rc = prepare(c, a, l, base);
+    if (rc != SIEVE_OK) return rc;
+    c.x.lse = reinterpret_cast<float *>(base + l.lse);
+    c.x.loss = reinterpret_cast<float *>(base + l.loss);
+    c.x.dloss = reinterpret_cast<float *>(base + l.dloss);
+    c.x.colsum = reinterpret_cast<float *>(base + l.colsum);
+    c.x.pool_rows = l.pool_rows;
+    c.x.want_dh = g.dh != nullptr;
+    c.x.want_dw = g.dweight != nullptr;
+    c.x.want_db = g.dbias != nullptr;
+    c.x.dw_f32 = g.dweight_dtype == SIEVE_F32;
+    c.x.accumulate = g.accumulate;
+    c.r.dloss = g.dloss;
+    c.r.loss = g.loss;
+    c.r.lse = g.lse;
+    c.r.dh = g.dh;
+    c.r.dh_stride = g.dh_stride;
+    c.r.top = reinterpret_cast<uint32_t *>(base + l.top);
+    c.r.low = reinterpret_cast<uint32_t *>(base + l.low);
+    c.r.dloss_c = reinterpret_cast<float *>(base + l.dloss);
+    c.r.loss_c = reinterpret_cast<float *>(base + l.loss);
+    c.r.lse_c = reinterpret_cast<float *>(base + l.lse);
+    c.r.hs = base + l.hs;
+    rc = make_matrix_map(&c.x.hs, a.dtype, base + l.hs, a.rows, a.width, a.width, kBox);
+    if (rc == SIEVE_OK) rc = make_matrix_map(&c.x.pool_in, a.dtype, base + l.pool, l.pool_rows, kK, kK, kBox);
+    if (rc == SIEVE_OK) rc = make_matrix_map(&c.x.pool_out, a.dtype, base + l.pool, l.pool_rows, kK, kK, 32);
+    if (rc == SIEVE_OK) rc = make_matrix_map(&c.x.acc, SIEVE_F32, base + l.acc, padded(a.rows), a.width, a.width, 32);
+    if (rc == SIEVE_OK && g.dweight)
+        rc = make_matrix_map(&c.x.dw, g.dweight_dtype, g.dweight, a.classes, a.width, g.dweight_stride, 32);
+    if (rc != SIEVE_OK) return rc;
+    const int each = piece_classes(a.rows, c.x.classes, l.pool_rows), pieces = (int)ceil_div(a.classes, each);
+    const float *acc = reinterpret_cast<const float *>(base + l.acc);
+    const cudaError_t e = a.dtype == SIEVE_F16 ? backward<__half>(c, g, acc, pieces, st)
+                                               : backward<__nv_bfloat16>(c, g, acc, pieces, st);
+    return e == cudaSuccess ? SIEVE_OK : record_cuda_error(e);
+}
+
+}  // namespace enc
+}  // namespace sieve

@@ -1,0 +1,531 @@
+// embed.cu -- token embedding and the gradient of its table.
+//
+//   forward   out[t] = scale table[id_t]; zeros for an id outside the table
+//   backward  dtable[v] = scale * sum of dout[t] over the tokens with id_t = v
+//
+// Both are bound by memory.  The backward pass sorts the tokens by id (stable,
+// so the sums have a fixed order), then walks the sorted list in pieces of
+// kPiece tokens: a warp adds up the rows of one piece in registers and writes
+// every id that lies wholly inside it.  An id that goes on into other pieces
+// (a frequent word, the mask token) leaves one partial row a piece, which
+// k_embed_join adds up in order.  So the work is even whatever the ids are.
+// Rows that no token has are found by the blocks that write their zeros.
+#include "blocks.cuh"
+
+namespace sieve {
+namespace enc {
+namespace {
+
+constexpr int kThreads = 256;
+
+// VEC consecutive elements as loaded, 16 bytes at a time
+template <typename T, int VEC>
+struct Chunk {
+    static constexpr int kWords = VEC * sizeof(T) >= 16 ? VEC * sizeof(T) / 16 : 1;
+    static_assert(VEC == 1 || VEC * sizeof(T) % 16 == 0, "");
+    uint4 w[kWords];
+    __device__ __forceinline__ void load(const T *p) {
+        if constexpr (VEC == 1) {
+            if constexpr (sizeof(T) == 4) w[0].x = __ldg(reinterpret_cast<const unsigned int *>(p));
+            else w[0].x = __ldg(reinterpret_cast<const unsigned short *>(p));
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) w[i] = __ldg(reinterpret_cast<const uint4 *>(p) + i);
+        }
+    }
+    __device__ __forceinline__ float get(int e) const {
+        return to_f32<T>(reinterpret_cast<const T *>(w)[e]);
+    }
+};
+template <typename T, int VEC>
+__device__ __forceinline__ void put(T *p, const float (&v)[VEC]) {
+    if constexpr (VEC == 1) {
+        *p = from_f32<T>(v[0]);
+    } else {
+        uint4 w[VEC * sizeof(T) / 16];
+        T *e = reinterpret_cast<T *>(w);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) e[i] = from_f32<T>(v[i]);
+#pragma unroll
+        for (int i = 0; i < (int)(VEC * sizeof(T) / 16); ++i) reinterpret_cast<uint4 *>(p)[i] = w[i];
+    }
+}
+
+// A block takes `tokens_per_block` tokens; thread l takes chunks l, l + 256, ...
+// of theirs, kAhead of them at a time.
+template <typename T, typename O, int VEC>
+__global__ void __launch_bounds__(kThreads) k_embed(const EmbedArgs a, int tokens_per_block, int chunks) {
+    constexpr int kAhead = 4;
+    const int64_t first = (int64_t)blockIdx.x * tokens_per_block;
+    const int here = (int)min((int64_t)tokens_per_block, a.tokens - first);
+    const int total = here * chunks;
+    const T *table = static_cast<const T *>(a.table);
+    O *out = static_cast<O *>(a.out);
+    for (int l0 = threadIdx.x; l0 < total; l0 += kThreads * kAhead) {
+        int tok[kAhead], col[kAhead], id[kAhead];
+        Chunk<T, VEC> x[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int l = l0 + u * kThreads;
+            tok[u] = l / chunks;
+            col[u] = (l - tok[u] * chunks) * VEC;
+            id[u] = l < total ? id_at(a.ids, a.id_type, first + tok[u], a.vocab) : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (id[u] >= 0) x[u].load(table + id[u] * a.table_stride + col[u]);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (l0 + u * kThreads >= total) break;
+            float v[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) v[e] = id[u] >= 0 ? a.scale * x[u].get(e) : 0.f;
+            put<O, VEC>(out + (first + tok[u]) * a.out_stride + col[u], v);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// The sort: passes over digits of up to 9 bits, the lowest first.  The list is
+// cut into `tiles` pieces of `per` tokens; k_sort_count counts every tile's
+// digits, and k_sort_scatter finds from all counts where each of its digits
+// starts and places its tokens in order.
+constexpr int kSortThreads = 512;
+constexpr int kSortItems = 4;
+constexpr int kSortStep = kSortThreads * kSortItems;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kMaxDigits = 512;
+constexpr int kMaxSortTiles = 304;     // two for each SM
+
+struct Sort {
+    int tokens, per, tiles, vocab;
+    int shift, bits;                   // this pass' digit
+    const int32_t *key_in, *val_in;    // nullptr in the first pass: the ids themselves
+    int32_t *key_out, *val_out;
+    int32_t *count;                    // [tiles][1 << bits]
+    int32_t *joins;                    // number of ids to join, zeroed by the first pass
+    const void *ids;
+    int id_type;
+};
+
+// The token's key: its id, or vocab where it has none.
+__device__ __forceinline__ int sort_key(const Sort &s, int i) {
+    if (s.key_in) return s.key_in[i];
+    const int id = id_at(s.ids, s.id_type, i, s.vocab);
+    return id < 0 ? s.vocab : id;
+}
+
+__global__ void __launch_bounds__(kSortThreads) k_sort_count(const Sort s) {
+    __shared__ int bins[kMaxDigits];
+    const int n = 1 << s.bits;
+    if (blockIdx.x == 0 && threadIdx.x == 0 && !s.key_in) *s.joins = 0;
+    for (int i = threadIdx.x; i < n; i += kSortThreads) bins[i] = 0;
+    __syncthreads();
+    const int first = blockIdx.x * s.per, last = min(first + s.per, s.tokens);
+#pragma unroll 4
+    for (int i = first + threadIdx.x; i < last; i += kSortThreads)
+        atomicAdd(&bins[(sort_key(s, i) >> s.shift) & (n - 1)], 1);
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += kSortThreads) s.count[blockIdx.x * n + i] = bins[i];
+}
+
+__global__ void __launch_bounds__(kSortThreads) k_sort_scatter(const Sort s) {
+    __shared__ int start[kMaxDigits];              // where the tile's next token of a digit goes
+    __shared__ int of_warp[kSortWarps][kMaxDigits];
+    __shared__ int sums[kSortWarps];
+    const int n = 1 << s.bits, tid = threadIdx.x, lane = lane_id(), warp = tid >> 5;
+    // digit tid: tokens of it in all tiles, and in the tiles before this one
+    int all = 0, before = 0;
+    if (tid < n) {
+#pragma unroll 8
+        for (int t = 0; t < s.tiles; ++t) {
+            const int c = s.count[t * n + tid];
+            all += c;
+            before += t < (int)blockIdx.x ? c : 0;
+        }
+    }
+    int scan = all;                                // exclusive sum over the digits
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, scan, o);
+        if (lane >= o) scan += up;
+    }
+    if (lane == 31) sums[warp] = scan;
+    __syncthreads();
+    int base = scan - all + before;
+    for (int w = 0; w < warp; ++w) base += sums[w];
+    if (tid < n) start[tid] = base;
+    const int first = blockIdx.x * s.per, last = min(first + s.per, s.tokens);
+    for (int at = first; at < last; at += kSortStep) {
+        for (int i = lane; i < n; i += 32) of_warp[warp][i] = 0;
+        __syncwarp();
+        int key[kSortItems], val[kSortItems], rank[kSortItems];
+        const int mine = at + warp * 32 * kSortItems + lane;
+#pragma unroll
+        for (int k = 0; k < kSortItems; ++k) {
+            const int i = mine + k * 32;
+            key[k] = i < last ? sort_key(s, i) : -1;
+            val[k] = i < last && s.key_in ? s.val_in[i] : i;
+        }
+        // the warp's tokens in order: how many of the same digit came before
+#pragma unroll
+        for (int k = 0; k < kSortItems; ++k) {
+            const bool live = mine + k * 32 < last;
+            const int d = live ? (key[k] >> s.shift) & (n - 1) : n;
+            const unsigned same = __match_any_sync(0xffffffffu, d);
+            if (live) rank[k] = of_warp[warp][d] + __popc(same & ((1u << lane) - 1));
+            __syncwarp();
+            if (live && lane == 31 - __clz((int)same)) of_warp[warp][d] += __popc(same);
+            __syncwarp();
+        }
+        __syncthreads();
+        // each warp's first place of a digit
+        if (tid < n) {
+            int p = start[tid];
+#pragma unroll
+            for (int w = 0; w < kSortWarps; ++w) {
+                const int c = of_warp[w][tid];
+                of_warp[w][tid] = p;
+                p += c;
+            }
+            start[tid] = p;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kSortItems; ++k)
+            if (mine + k * 32 < last) {
+                const int to = of_warp[warp][(key[k] >> s.shift) & (n - 1)] + rank[k];
+                s.key_out[to] = key[k];
+                s.val_out[to] = val[k];
+            }
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------------------
+constexpr int kPiece = 64;              // sorted tokens of a warp
+constexpr int kPieceWarps = 4;
+constexpr int kColumns = 256;           // columns of a warp: 8 a lane
+constexpr int kZeroRows = 32;           // table rows of a block that looks for empty ones
+
+struct Sums {
+    EmbedArgs a;
+    const int32_t *key, *val;           // sorted
+    float *partial;                     // [pieces][2][width]: of an id that came from the piece before, of one that goes on
+    int32_t *joins, *join_list;         // pieces where an id starts that goes on
+    int pieces, slices, sum_blocks;
+};
+
+// Places of a lane's 8 columns in a slice: together with VEC > 1, else 32 apart.
+template <int VEC>
+__device__ __forceinline__ int column(int lane, int e) {
+    return VEC == 1 ? e * 32 + lane : (e / VEC * 32 + lane) * VEC + e % VEC;
+}
+template <typename T, int VEC>
+struct Row {                            // 8 columns of a row
+    Chunk<T, VEC> c[8 / VEC];
+    __device__ __forceinline__ void load(const T *p, int lane, int left) {
+#pragma unroll
+        for (int i = 0; i < 8 / VEC; ++i)
+            if (column<VEC>(lane, i * VEC) < left) c[i].load(p + column<VEC>(lane, i * VEC));
+    }
+    __device__ __forceinline__ float get(int e) const { return c[e / VEC].get(e % VEC); }
+};
+// the finished sums of a table row
+template <typename G, int VEC>
+__device__ __forceinline__ void finish(const EmbedArgs &a, int id, int col0, int lane, const float (&sum)[8]) {
+    G *to = static_cast<G *>(a.dtable) + id * a.dtable_stride + col0;
+    const int left = a.width - col0;
+#pragma unroll
+    for (int i = 0; i < 8 / VEC; ++i) {
+        const int col = column<VEC>(lane, i * VEC);
+        if (col >= left) continue;
+        float v[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            v[e] = a.scale * sum[i * VEC + e];
+            if (a.accumulate) v[e] += to_f32<G>(to[col + e]);
+        }
+        put<G, VEC>(to + col, v);
+    }
+}
+
+// first place in the sorted keys whose key is at least v (a whole warp)
+__device__ __forceinline__ int lower_bound(const int32_t *key, int n, int v) {
+    int lo = 0, hi = n;                 // the answer is in [lo, hi]
+    while (hi > lo) {
+        const int step = (hi - lo + 31) / 32;
+        const int i = lo + ((int)lane_id() + 1) * step - 1;
+        // lanes whose stretch of `step` keys lies wholly below v
+        const int below = __popc(__ballot_sync(0xffffffffu, i < hi && key[min(i, n - 1)] < v));
+        const int from = lo + below * step;
+        hi = min(hi, from + step - 1);
+        lo = min(from, hi);
+        if (step == 1) break;
+    }
+    return lo;
+}
+
+template <typename T, typename G, int VEC>
+__global__ void __launch_bounds__(kPieceWarps * 32) k_embed_sums(const Sums s) {
+    const EmbedArgs &a = s.a;
+    const int lane = lane_id(), warp = threadIdx.x >> 5;
+    if ((int)blockIdx.x >= s.sum_blocks) {
+        // ---- the zeros of rows that no token has
+        __shared__ int range[2];
+        __shared__ int has[kZeroRows];
+        const int v0 = ((int)blockIdx.x - s.sum_blocks) * kZeroRows, v1 = min(v0 + kZeroRows, a.vocab);
+        if (threadIdx.x < kZeroRows) has[threadIdx.x] = 0;
+        if (warp < 2) {
+            const int p = lower_bound(s.key, a.tokens, warp ? v1 : v0);
+            if (lane == 0) range[warp] = p;
+        }
+        __syncthreads();
+#pragma unroll 4
+        for (int i = range[0] + threadIdx.x; i < range[1]; i += kPieceWarps * 32) has[s.key[i] - v0] = 1;
+        __syncthreads();
+        float zero[VEC] = {};
+        for (int v = v0 + warp; v < v1; v += kPieceWarps)
+            if (!has[v - v0])
+                for (int col = lane * VEC; col < a.width; col += 32 * VEC)
+                    put<G, VEC>(static_cast<G *>(a.dtable) + v * a.dtable_stride + col, zero);
+        return;
+    }
+    const int64_t work = (int64_t)blockIdx.x * kPieceWarps + warp;
+    const int piece = (int)(work / s.slices), col0 = (int)(work % s.slices) * kColumns;
+    if (piece >= s.pieces) return;
+    const int p0 = piece * kPiece, count = min(kPiece, a.tokens - p0), left = a.width - col0;
+    int keys[2], vals[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int i = min(p0 + h * 32 + lane, a.tokens - 1);
+        keys[h] = s.key[i];
+        vals[h] = s.val[i];
+    }
+    const int prev = p0 > 0 ? s.key[p0 - 1] : -1, next = p0 + count < a.tokens ? s.key[p0 + count] : a.vocab;
+    const T *dout = static_cast<const T *>(a.dout) + col0;
+    constexpr int kAhead = 8;
+    float sum[8] = {};
+    int cur = __shfl_sync(0xffffffffu, keys[0], 0);
+    // a whole id is written at once; what reaches into other pieces is kept
+    auto flush = [&](int key, bool from_before, bool goes_on) {
+        if (key >= a.vocab) return;
+        if (!from_before && !goes_on) {
+            finish<G, VEC>(a, key, col0, lane, sum);
+            return;
+        }
+        float *to = s.partial + ((int64_t)piece * 2 + (from_before ? 0 : 1)) * a.width + col0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (column<VEC>(lane, e) < left) to[column<VEC>(lane, e)] = sum[e];
+        if (!from_before && col0 == 0 && lane == 0) s.join_list[atomicAdd(s.joins, 1)] = piece;
+    };
+    bool whole = true;                  // no id has ended in this piece yet
+    for (int j0 = 0; j0 < count; j0 += kAhead) {
+        Row<T, VEC> x[kAhead];
+        int key[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int j = j0 + u;
+            key[u] = __shfl_sync(0xffffffffu, j < 32 ? keys[0] : keys[1], j & 31);
+            const int t = __shfl_sync(0xffffffffu, j < 32 ? vals[0] : vals[1], j & 31);
+            if (j >= count) key[u] = -1;
+            else if (key[u] < a.vocab) x[u].load(dout + t * a.dout_stride, lane, left);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (key[u] < 0) break;
+            if (key[u] != cur) {
+                flush(cur, whole && cur == prev, false);
+                whole = false;
+                cur = key[u];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+            }
+            if (cur < a.vocab)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (column<VEC>(lane, e) < left) sum[e] += x[u].get(e);
+        }
+    }
+    flush(cur, whole && cur == prev, cur == next);
+}
+
+// The ids that several pieces share: the partial row of the piece where the id
+// starts, then of those that it goes through, by 16 strands of pieces added in order.
+constexpr int kStrands = 16;
+constexpr int kJoinBlocks = 152 * 2;
+template <typename G>
+__global__ void __launch_bounds__(kStrands * 32) k_embed_join(const Sums s) {
+    __shared__ float part[kStrands][kColumns];
+    __shared__ int shared_end;
+    const EmbedArgs &a = s.a;
+    const int lane = lane_id(), strand = threadIdx.x >> 5;
+    const int64_t total = (int64_t)*s.joins * s.slices;
+    for (int64_t w = blockIdx.x; w < total; w += gridDim.x) {
+        const int piece = s.join_list[w / s.slices], col0 = (int)(w % s.slices) * kColumns, left = a.width - col0;
+        const int id = s.key[piece * kPiece + kPiece - 1];
+        __syncthreads();
+        if (strand == 0) {
+            const int end = lower_bound(s.key, a.tokens, id + 1);   // past the id's last token
+            if (lane == 0) shared_end = end;
+        }
+        __syncthreads();
+        const int n = (shared_end - 1) / kPiece - piece;      // pieces that it goes on into
+        const int each = (n + kStrands - 1) / kStrands;
+        const int from = piece + 1 + strand * each, to = min(from + each, piece + 1 + n);
+        float sum[8] = {};
+#pragma unroll 4
+        for (int p = from; p < to; ++p) {
+            const float *x = s.partial + (int64_t)p * 2 * a.width + col0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e * 32 + lane < left) sum[e] += __ldcg(x + e * 32 + lane);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) part[strand][e * 32 + lane] = sum[e];
+        __syncthreads();
+        const int col = threadIdx.x;
+        if (col < kColumns && col < left) {
+            float v = __ldcg(s.partial + ((int64_t)piece * 2 + 1) * a.width + col0 + col);
+#pragma unroll
+            for (int k = 0; k < kStrands; ++k) v += part[k][col];
+            G *to_row = static_cast<G *>(a.dtable) + id * a.dtable_stride + col0 + col;
+            v *= a.scale;
+            if (a.accumulate) v += to_f32<G>(*to_row);
+            *to_row = from_f32<G>(v);
+        }
+    }
+}
+
+bool aligned(const void *p, size_t m) { return reinterpret_cast<uintptr_t>(p) % m == 0; }
+// whether rows can be moved VEC elements (16 bytes or more) at a time
+bool wide_rows(const void *p, int64_t stride, int width, int vec, size_t size) {
+    return width % vec == 0 && stride * size % 16 == 0 && aligned(p, 16);
+}
+
+int key_bits(int64_t vocab) {            // of the numbers 0 .. vocab
+    int b = 1;
+    while (((int64_t)1 << b) <= vocab) ++b;
+    return b;
+}
+struct SortShape {
+    int passes, bits, per, tiles;
+};
+SortShape sort_shape(int64_t tokens, int64_t vocab) {
+    SortShape s;
+    const int all = key_bits(vocab);
+    s.passes = (all + 8) / 9;
+    s.bits = (all + s.passes - 1) / s.passes;
+    const int64_t most = ceil_div(tokens, kMaxSortTiles);
+    s.per = (int)round_up(most < 1 ? 1 : most, kSortStep);
+    s.tiles = (int)ceil_div(tokens, s.per);
+    return s;
+}
+// [tokens] keys and places twice, counts, [pieces] joins, their number, partial rows
+struct Layout {
+    size_t key[2], val[2], count, list, joins, partial, bytes;
+};
+Layout layout(int64_t tokens, int64_t vocab, int width) {
+    const SortShape s = sort_shape(tokens, vocab);
+    const int64_t pieces = ceil_div(tokens, kPiece);
+    Layout l;
+    size_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const size_t here = at;
+        at += (size_t)round_up(bytes, 256);
+        return here;
+    };
+    for (int i = 0; i < 2; ++i) {
+        l.key[i] = take(tokens * 4);
+        l.val[i] = take(tokens * 4);
+    }
+    l.count = take((int64_t)s.tiles * (1 << s.bits) * 4);
+    l.list = take(pieces * 4);
+    l.joins = take(4);
+    l.partial = take(pieces * 2 * width * 4);
+    l.bytes = at;
+    return l;
+}
+
+}  // namespace
+
+cudaError_t launch_embed(const EmbedArgs &a, cudaStream_t st) {
+    return with_type(a.table_dtype, [&](auto t) {
+        using T = typename decltype(t)::type;
+        return with_type(a.dtype, [&](auto o) {
+            using O = typename decltype(o)::type;
+            constexpr int V = sizeof(T) == 4 && sizeof(O) == 4 ? 4 : 8;
+            const bool wide = wide_rows(a.table, a.table_stride, a.width, V, sizeof(T)) &&
+                              wide_rows(a.out, a.out_stride, a.width, V, sizeof(O));
+            const int chunks = wide ? a.width / V : a.width;
+            const int per = chunks >= 1024 ? 1 : 1024 / chunks;
+            const unsigned blocks = (unsigned)ceil_div(a.tokens, per);
+            if (wide) k_embed<T, O, V><<<blocks, kThreads, 0, st>>>(a, per, chunks);
+            else k_embed<T, O, 1><<<blocks, kThreads, 0, st>>>(a, per, chunks);
+            return cudaGetLastError();
+        });
+    });
+}
+
+cudaError_t launch_embed_backward(const EmbedArgs &a, void *ws, cudaStream_t st) {
+    unsigned char *base = static_cast<unsigned char *>(ws);
+    const Layout l = layout(a.tokens, a.vocab, a.width);
+    const SortShape shape = sort_shape(a.tokens, a.vocab);
+    auto ints = [&](size_t at) { return reinterpret_cast<int32_t *>(base + at); };
+    Sort s = {};
+    s.tokens = a.tokens;
+    s.per = shape.per;
+    s.tiles = shape.tiles;
+    s.vocab = a.vocab;
+    s.bits = shape.bits;
+    s.count = ints(l.count);
+    s.joins = ints(l.joins);
+    s.ids = a.ids;
+    s.id_type = a.id_type;
+    for (int pass = 0; pass < shape.passes && a.tokens > 0; ++pass) {
+        s.shift = pass * shape.bits;
+        s.key_in = pass ? ints(l.key[(pass + 1) & 1]) : nullptr;
+        s.val_in = pass ? ints(l.val[(pass + 1) & 1]) : nullptr;
+        s.key_out = ints(l.key[pass & 1]);
+        s.val_out = ints(l.val[pass & 1]);
+        k_sort_count<<<s.tiles, kSortThreads, 0, st>>>(s);
+        k_sort_scatter<<<s.tiles, kSortThreads, 0, st>>>(s);
+    }
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    Sums u = {};
+    u.a = a;
+    u.key = ints(l.key[(shape.passes - 1) & 1]);
+    u.val = ints(l.val[(shape.passes - 1) & 1]);
+    u.partial = reinterpret_cast<float *>(base + l.partial);
+    u.joins = s.joins;
+    u.join_list = ints(l.list);
+    u.pieces = (int)ceil_div(a.tokens, kPiece);
+    u.slices = (int)ceil_div(a.width, kColumns);
+    u.sum_blocks = (int)ceil_div((int64_t)u.pieces * u.slices, kPieceWarps);
+    const int64_t zero_blocks = a.accumulate ? 0 : ceil_div(a.vocab, kZeroRows);
+    const unsigned blocks = (unsigned)(u.sum_blocks + zero_blocks);
+    if (!blocks) return cudaSuccess;
+    return with_type(a.dtype, [&](auto t) {
+        using T = typename decltype(t)::type;
+        return with_type(a.table_dtype, [&](auto g) {
+            using G = typename decltype(g)::type;
+            constexpr int V = sizeof(T) == 4 && sizeof(G) == 4 ? 4 : 8;
+            if (wide_rows(a.dout, a.dout_stride, a.width, V, sizeof(T)) &&
+                wide_rows(a.dtable, a.dtable_stride, a.width, V, sizeof(G)))
+                k_embed_sums<T, G, V><<<blocks, kPieceWarps * 32, 0, st>>>(u);
+            else
+                k_embed_sums<T, G, 1><<<blocks, kPieceWarps * 32, 0, st>>>(u);
+            if (a.tokens > kPiece) k_embed_join<G><<<kJoinBlocks, kStrands * 32, 0, st>>>(u);
+            return cudaGetLastError();
+        });
+    });
+}
+
+size_t embed_backward_workspace_bytes(int64_t tokens, int64_t vocab, int width) {
+    return layout(tokens, vocab, width).bytes;
+}
+
+}  // namespace enc
+}  // namespace sieve

@@ -1,0 +1,530 @@
+// residual_norm.cu -- the residual step between two blocks of an encoder,
+// forward and backward:
+//
+//   forward   u = N1(y), stream = alpha h + gate u, x = N2(stream)
+//   backward  G = dstream + dN2(dx), dh = alpha G, dgate = G u,
+//             dy = dN1(gate G), and the sums over rows for the weights
+//
+// N(v) = (v - mu) r w + b with r = 1 / sqrt(mean((v - mu)^2) + eps), mu = mean(v)
+// or 0 (rms); dN(d) = r (g - mean(g) - vh mean(g vh)) with g = d w, vh = (v - mu) r
+// and mean(g) left out with rms.  Either norm may be absent.
+//
+// Both are bound by memory: a row is read once into registers and everything
+// comes from there, in fp32, rounded once.  The backward pass makes the stream
+// again from h and y, so it costs no other read than the stream would and the
+// rounding of the stored stream does not enter.
+//
+// The sums over rows stay in registers of the threads that walk the rows, four
+// of them for a column: A = dx xh2, B = dx, C = d uh, D = d, where uh is the
+// normed y (y itself without a post norm) and d the gradient G, times the gate
+// where every row has its own.  All weights' gradients follow from these after
+// the rows: a column gate w is a common factor, dpost_weight = w C, dpost_bias = w D,
+// dgate = post_weight C + post_bias D.
+#include <type_traits>
+
+#include "blocks.cuh"
+
+namespace sieve {
+namespace enc {
+namespace {
+
+template <typename T, int VEC>
+struct Piece {      // VEC elements as loaded
+    static_assert(VEC == 1 || VEC * sizeof(T) == 16, "");
+    uint4 v;
+    __device__ __forceinline__ void load(const T *p) {
+        if constexpr (VEC == 1) {
+            if constexpr (sizeof(T) == 4) v.x = *reinterpret_cast<const uint32_t *>(p);
+            else v.x = *reinterpret_cast<const uint16_t *>(p);
+        } else {
+            v = *reinterpret_cast<const uint4 *>(p);
+        }
+    }
+    __device__ __forceinline__ void clear() { v = make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ float get(int i) const { return to_f32<T>(reinterpret_cast<const T *>(&v)[i]); }
+};
+
+// sum over the TPR threads of a row: a warp, or the block
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float *smem) {
+    if constexpr (TPR == 32) return warp_sum(v);
+    else return block_sum<TPR>(v, smem);
+}
+
+// Forward.  A row per warp (TPR = 32, eight rows a block) or per block of TPR
+// threads; chunk c of thread i at (c * TPR + i) * VEC.
+template <typename T, typename W, int VEC, int TPR, int NCH>
+__global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) k_residual_norm(const ResidualNormArgs p) {
+    constexpr int kRows = TPR == 32 ? 8 : 1;
+    __shared__ float smem[32];
+    const sieve_residual_norm_args &a = p.a;
+    const int i = TPR == 32 ? lane_id() : threadIdx.x;
+    const int64_t row = (int64_t)blockIdx.x * kRows + (TPR == 32 ? threadIdx.x >> 5 : 0);
+    if (row >= a.rows) return;
+    const T *h = static_cast<const T *>(a.h) + row * a.h_stride, *y = static_cast<const T *>(a.y) + row * a.y_stride;
+    const T *gate_row = static_cast<const T *>(a.gate) + row * a.gate_stride;
+    const W *gate = static_cast<const W *>(a.gate);
+    const W *w1 = static_cast<const W *>(a.post_weight), *b1 = static_cast<const W *>(a.post_bias);
+    const W *w2 = static_cast<const W *>(a.weight), *b2 = static_cast<const W *>(a.bias);
+    const int width = a.width;
+    const float inv_n = 1.f / (float)width;
+    Piece<T, VEC> hp[NCH];
+    float v[NCH][VEC], s = 0.f;
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+        const int col = (c * TPR + i) * VEC;
+        Piece<T, VEC> yp;
+        yp.clear();
+        if (col < width) {
+            yp.load(y + col);
+            hp[c].load(h + col);
+        }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            v[c][e] = yp.get(e);
+            s += v[c][e];
+        }
+    }
+    // mean and factor of v, which is centred; places past the row stay zero
+    auto normed = [&](float sum, float &mean, float &r) {
+        mean = a.rms ? 0.f : row_sum<TPR>(sum, smem) * inv_n;
+        float q = 0.f;
+#pragma unroll
+        for (int c = 0; c < NCH; ++c)
+            if ((c * TPR + i) * VEC < width)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    v[c][e] -= mean;
+                    q = fmaf(v[c][e], v[c][e], q);
+                }
+        r = 1.f / sqrtf(fmaf(row_sum<TPR>(q, smem), inv_n, a.eps));
+    };
+    float mean1 = 0.f, r1 = 1.f, mean2 = 0.f, r2 = 1.f;
+    if (w1) normed(s, mean1, r1);
+    s = 0.f;
+    T *out = static_cast<T *>(p.stream) + row * p.stream_stride;
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+        const int col = (c * TPR + i) * VEC;
+        if (col >= width) continue;
+        if (w1) {
+            float w[VEC], b[VEC];
+            load_vec<W, VEC>(w1 + col, w);
+            if (b1) load_vec<W, VEC>(b1 + col, b);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) v[c][e] = fmaf(v[c][e] * r1, w[e], b1 ? b[e] : 0.f);
+        }
+        if (a.gate_kind != SIEVE_GATE_NONE) {
+            float g[VEC];
+            if (a.gate_kind == SIEVE_GATE_ROW) load_vec<T, VEC>(gate_row + col, g);
+            else load_vec<W, VEC>(gate + col, g);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) v[c][e] *= g[e];
+        }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            v[c][e] = fmaf(a.alpha, hp[c].get(e), v[c][e]);
+            s += v[c][e];
+        }
+        store_vec<T, VEC>(out + col, v[c]);
+    }
+    if (w2) {
+        normed(s, mean2, r2);
+        T *x = static_cast<T *>(p.x) + row * p.x_stride;
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) {
+            const int col = (c * TPR + i) * VEC;
+            if (col >= width) continue;
+            float w[VEC], b[VEC];
+            load_vec<W, VEC>(w2 + col, w);
+            if (b2) load_vec<W, VEC>(b2 + col, b);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) v[c][e] = fmaf(v[c][e] * r2, w[e], b2 ? b[e] : 0.f);
+            store_vec<T, VEC>(x + col, v[c]);
+        }
+    }
+    if (p.stats && i == 0) {
+        p.stats[row] = mean1;
+        p.stats[a.rows + row] = r1;
+        p.stats[2 * a.rows + row] = mean2;
+        p.stats[3 * a.rows + row] = r2;
+    }
+}
+
+// Backward.  The TPR threads of a row (a warp, four rows a block; or a block)
+// walk rows, and keep the four sums of their columns in registers, or in
+// shared memory (kShared) where a thread holds too much; at the end they go to
+// partial[group][4][width] and k_residual_reduce adds the groups up.
+constexpr int kWarpRows = 4;
+__host__ __device__ constexpr int groups_of(int tpr) { return tpr == 32 ? kWarpRows : 1; }
+
+template <typename T, typename W, int VEC, int TPR, int NCH, bool kShared>
+__global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR) k_residual_norm_backward(const ResidualNormArgs p) {
+    extern __shared__ float acc[];                 // kShared: [4][width]
+    __shared__ float2 meet[2][32];
+    const sieve_residual_norm_args &a = p.a;
+    const sieve_residual_norm_grads &g = p.g;
+    const int i = TPR == 32 ? lane_id() : threadIdx.x;
+    const int64_t group = (int64_t)blockIdx.x * groups_of(TPR) + (TPR == 32 ? threadIdx.x >> 5 : 0);
+    const int64_t step = (int64_t)gridDim.x * groups_of(TPR);
+    const T *h = static_cast<const T *>(a.h), *y = static_cast<const T *>(a.y);
+    const T *dstream = static_cast<const T *>(g.dstream), *dx = static_cast<const T *>(g.dx);
+    const T *gate_rows = a.gate_kind == SIEVE_GATE_ROW ? static_cast<const T *>(a.gate) : nullptr;
+    const W *gate = a.gate_kind == SIEVE_GATE_COLUMN ? static_cast<const W *>(a.gate) : nullptr;
+    const W *w1 = static_cast<const W *>(a.post_weight), *b1 = static_cast<const W *>(a.post_bias);
+    const W *w2 = static_cast<const W *>(a.weight);
+    const int width = a.width;
+    const float inv_n = 1.f / (float)width, centre = a.rms ? 0.f : inv_n;
+    float sum[kShared ? 1 : 4][NCH][VEC];
+    if constexpr (kShared) {
+        for (int c = i; c < 4 * width; c += TPR) acc[c] = 0.f;
+        __syncthreads();
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int c = 0; c < NCH; ++c)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) sum[k][c][e] = 0.f;
+    }
+    auto add = [&](int k, int c, int e, float v) {
+        if constexpr (kShared) acc[k * width + (c * TPR + i) * VEC + e] += v;
+        else sum[k][c][e] += v;
+    };
+    // two sums over the row's threads at once
+    int turn = 0;
+    auto both_sums = [&](float &s, float &t) {
+        s = warp_sum(s);
+        t = warp_sum(t);
+        if constexpr (TPR > 32) {
+            if (lane_id() == 0) meet[turn][threadIdx.x >> 5] = make_float2(s, t);
+            __syncthreads();
+            s = t = 0.f;
+#pragma unroll
+            for (int w = 0; w < TPR / 32; ++w) {
+                s += meet[turn][w].x;
+                t += meet[turn][w].y;
+            }
+            turn ^= 1;      // the next meeting's barrier lies between these reads and the next writes here
+        }
+    };
+    // a row's elements, on their way while the row before is worked on
+    Piece<T, VEC> nh[NCH], ny[NCH], ns[NCH], nx[NCH];
+    float n_stats[4] = {};
+    auto load = [&](int64_t row) {
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) {
+            const int col = (c * TPR + i) * VEC;
+            nh[c].clear();
+            ny[c].clear();
+            ns[c].clear();
+            nx[c].clear();
+            if (col >= width) continue;
+            ny[c].load(y + row * a.y_stride + col);
+            if (dstream) ns[c].load(dstream + row * g.dstream_stride + col);
+            if (w2) {
+                nh[c].load(h + row * a.h_stride + col);
+                nx[c].load(dx + row * g.dx_stride + col);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) n_stats[k] = __ldg(g.stats + k * a.rows + row);
+    };
+    if (group < a.rows) load(group);
+    for (int64_t row = group; row < a.rows; row += step) {
+        float uh[NCH][VEC], sh[NCH][VEC], d2[NCH][VEC], G[NCH][VEC];
+        float s1 = 0.f, s2 = 0.f;
+        const float mu1 = n_stats[0], r1 = n_stats[1], mu2 = n_stats[2], r2 = n_stats[3];
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) {
+            const int col = (c * TPR + i) * VEC;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                uh[c][e] = (ny[c].get(e) - mu1) * r1;
+                G[c][e] = ns[c].get(e);
+                sh[c][e] = nh[c].get(e);
+                d2[c][e] = nx[c].get(e);
+            }
+            if (!w2 || col >= width) continue;
+            // the stream again, then the gradient through its norm
+            float u[VEC], t[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) u[e] = uh[c][e];
+            if (w1) {
+                load_vec<W, VEC>(w1 + col, t);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) u[e] *= t[e];
+                if (b1) {
+                    load_vec<W, VEC>(b1 + col, t);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) u[e] += t[e];
+                }
+            }
+            if (gate || gate_rows) {
+                if (gate) load_vec<W, VEC>(gate + col, t);
+                else load_vec<T, VEC>(gate_rows + row * a.gate_stride + col, t);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) u[e] *= t[e];
+            }
+            load_vec<W, VEC>(w2 + col, t);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                sh[c][e] = (fmaf(a.alpha, sh[c][e], u[e]) - mu2) * r2;
+                add(0, c, e, d2[c][e] * sh[c][e]);
+                add(1, c, e, d2[c][e]);
+                d2[c][e] *= t[e];
+                s1 += d2[c][e];
+                s2 = fmaf(d2[c][e], sh[c][e], s2);
+            }
+        }
+        if (row + step < a.rows) load(row + step);
+        if (w2) {
+            both_sums(s1, s2);
+            const float m1 = s1 * centre, m2 = s2 * inv_n;
+#pragma unroll
+            for (int c = 0; c < NCH; ++c)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) G[c][e] += r2 * (d2[c][e] - m1 - sh[c][e] * m2);
+        }
+        T *dh = static_cast<T *>(g.dh) + row * g.dh_stride, *dy = static_cast<T *>(g.dy) + row * g.dy_stride;
+        s1 = s2 = 0.f;
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) {
+            const int col = (c * TPR + i) * VEC;
+            if (col >= width) continue;
+            float t[VEC], w[VEC];
+            if (w1) load_vec<W, VEC>(w1 + col, w);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) t[e] = a.alpha * G[c][e];
+            store_vec<T, VEC>(dh + col, t);
+            if (gate_rows) {
+                float b[VEC], gr[VEC];
+                if (b1) load_vec<W, VEC>(b1 + col, b);
+                load_vec<T, VEC>(gate_rows + row * a.gate_stride + col, gr);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    t[e] = G[c][e] * (w1 ? fmaf(uh[c][e], w[e], b1 ? b[e] : 0.f) : uh[c][e]);
+                    G[c][e] *= gr[e];
+                }
+                store_vec<T, VEC>(static_cast<T *>(g.dgate) + row * g.dgate_stride + col, t);
+            }
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                add(2, c, e, G[c][e] * uh[c][e]);
+                add(3, c, e, G[c][e]);
+            }
+            if (gate) {
+                load_vec<W, VEC>(gate + col, t);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) G[c][e] *= t[e];
+            }
+            if (w1) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    G[c][e] *= w[e];
+                    s1 += G[c][e];
+                    s2 = fmaf(G[c][e], uh[c][e], s2);
+                }
+            } else {
+                store_vec<T, VEC>(dy + col, G[c]);
+            }
+        }
+        if (w1) {
+            both_sums(s1, s2);
+            const float m1 = s1 * centre, m2 = s2 * inv_n;
+#pragma unroll
+            for (int c = 0; c < NCH; ++c) {
+                const int col = (c * TPR + i) * VEC;
+                if (col >= width) continue;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) G[c][e] = r1 * (G[c][e] - m1 - uh[c][e] * m2);
+                store_vec<T, VEC>(dy + col, G[c]);
+            }
+        }
+    }
+    float *out = p.partial + group * 4 * width;
+    if constexpr (kShared) {
+        __syncthreads();
+        for (int c = i; c < 4 * width; c += TPR) out[c] = acc[c];
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int c = 0; c < NCH; ++c)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const int col = (c * TPR + i) * VEC + e;
+                    if (col < width) out[k * width + col] = sum[k][c][e];
+                }
+    }
+}
+
+// The weights' gradients from the groups' sums: 32 columns by 32 strands of
+// groups; each strand adds its groups in order, the strands in order after that.
+// blockIdx.y: the pre norm's, or the post norm's and the gate's.
+template <typename W>
+__global__ void __launch_bounds__(1024) k_residual_reduce(const ResidualNormArgs p, int groups) {
+    __shared__ float part[2][32][33];
+    const sieve_residual_norm_args &a = p.a;
+    const int lane = threadIdx.x & 31, strand = threadIdx.x >> 5;
+    const int col = blockIdx.x * 32 + lane;
+    const float *in = p.partial + (int64_t)blockIdx.y * 2 * a.width;
+    float s = 0.f, t = 0.f;
+    if (col < a.width)
+#pragma unroll 4
+        for (int b = strand; b < groups; b += 32) {
+            s += in[(int64_t)b * 4 * a.width + col];
+            t += in[(int64_t)b * 4 * a.width + a.width + col];
+        }
+    part[0][strand][lane] = s;
+    part[1][strand][lane] = t;
+    __syncthreads();
+    if (strand > 0 || col >= a.width) return;
+    s = t = 0.f;
+#pragma unroll
+    for (int k = 0; k < 32; ++k) {
+        s += part[0][k][lane];
+        t += part[1][k][lane];
+    }
+    auto put = [&](void *to, float v) {
+        if (to) static_cast<W *>(to)[col] = from_f32<W>(v);
+    };
+    if (blockIdx.y == 0) {
+        put(p.g.dweight, s);
+        put(p.g.dbias, t);
+        return;
+    }
+    const float gate = a.gate_kind == SIEVE_GATE_COLUMN ? to_f32<W>(static_cast<const W *>(a.gate)[col]) : 1.f;
+    const float w = a.post_weight ? to_f32<W>(static_cast<const W *>(a.post_weight)[col]) : 1.f;
+    const float b = a.post_bias ? to_f32<W>(static_cast<const W *>(a.post_bias)[col]) : 0.f;
+    put(p.g.dpost_weight, gate * s);
+    put(p.g.dpost_bias, gate * t);
+    if (a.gate_kind == SIEVE_GATE_COLUMN) put(p.g.dgate, fmaf(w, s, b * t));
+}
+
+bool aligned(const void *p, size_t m) { return reinterpret_cast<uintptr_t>(p) % m == 0; }
+// Whether everything can be moved 16 bytes of a row at a time (weights of
+// another type move the same number of elements).
+template <typename T>
+bool wide(const ResidualNormArgs &p) {
+    constexpr int v = 16 / sizeof(T);
+    const sieve_residual_norm_args &a = p.a;
+    auto rows = [&](const void *q, int64_t stride) { return !q || (stride % v == 0 && aligned(q, 16)); };
+    if (a.width % v) return false;
+    for (const void *w : {a.weight, a.bias, a.post_weight, a.post_bias,
+                          a.gate_kind == SIEVE_GATE_COLUMN ? a.gate : nullptr})
+        if (!aligned(w, 16)) return false;
+    const bool row_gate = a.gate_kind == SIEVE_GATE_ROW;
+    return rows(a.h, a.h_stride) && rows(a.y, a.y_stride) && rows(row_gate ? a.gate : nullptr, a.gate_stride) &&
+           rows(p.stream, p.stream_stride) && rows(p.x, p.x_stride) && rows(p.g.dstream, p.g.dstream_stride) &&
+           rows(p.g.dx, p.g.dx_stride) && rows(p.g.dh, p.g.dh_stride) && rows(p.g.dy, p.g.dy_stride) &&
+           rows(row_gate ? p.g.dgate : nullptr, p.g.dgate_stride);
+}
+
+template <typename T, typename W, int VEC, int TPR, int NCH>
+cudaError_t forward_as(const ResidualNormArgs &p, cudaStream_t st) {
+    constexpr int kRows = TPR == 32 ? 8 : 1;
+    k_residual_norm<T, W, VEC, TPR, NCH><<<(unsigned)ceil_div(p.a.rows, kRows), TPR == 32 ? 256 : TPR, 0, st>>>(p);
+    return cudaGetLastError();
+}
+
+template <typename T, typename W>
+cudaError_t forward(const ResidualNormArgs &p, cudaStream_t st) {
+    constexpr int V = 16 / sizeof(T);
+    const int width = p.a.width;
+    if (wide<T>(p)) {
+        if (width <= 256) return forward_as<T, W, V, 32, 8 / V>(p, st);
+        if (width <= 512) return forward_as<T, W, V, 32, 16 / V>(p, st);
+        if (width <= 768) return forward_as<T, W, V, 32, 24 / V>(p, st);
+        if (width <= 1024) return forward_as<T, W, V, 32, 32 / V>(p, st);
+        if (width <= 2048) return forward_as<T, W, V, 128, 16 / V>(p, st);
+        if (width <= 4096) return forward_as<T, W, V, 256, 16 / V>(p, st);
+        return forward_as<T, W, V, 512, 16 / V>(p, st);
+    }
+    if (width <= 128) return forward_as<T, W, 1, 32, 4>(p, st);
+    if (width <= 384) return forward_as<T, W, 1, 32, 12>(p, st);
+    if (width <= 1024) return forward_as<T, W, 1, 128, 8>(p, st);
+    if (width <= 2048) return forward_as<T, W, 1, 256, 8>(p, st);
+    return forward_as<T, W, 1, 512, 16>(p, st);
+}
+
+// Threads of a row in the backward pass: 8 elements each, up to 1024 of them.
+int backward_threads(int width) {
+    if (width <= 256) return 32;
+    if (width <= 512) return 64;
+    if (width <= 768) return 96;
+    if (width <= 1024) return 128;
+    if (width <= 2048) return 256;
+    return width <= 4096 ? 512 : 1024;
+}
+// Blocks: as many as an SM holds, and few partial sums where there are few rows.
+int backward_blocks(int64_t rows, int width) {
+    const int tpr = backward_threads(width);
+    const int64_t n = ceil_div(rows, groups_of(tpr)), most = 152 * (tpr <= 128 ? 4 : tpr <= 512 ? 512 / tpr : 1);
+    return (int)(n < most ? n : most);
+}
+
+template <typename T, typename W, int VEC, int TPR>
+cudaError_t backward_as(const ResidualNormArgs &p, int blocks, cudaStream_t st) {
+    constexpr bool kShared = TPR == 1024;
+    auto kernel = k_residual_norm_backward<T, W, VEC, TPR, 8 / VEC, kShared>;
+    size_t smem = 0;
+    if (kShared) {
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             4 * SIEVE_RESIDUAL_NORM_MAX_WIDTH * (int)sizeof(float));
+        if (e != cudaSuccess) return e;
+        smem = (size_t)4 * p.a.width * sizeof(float);
+    }
+    kernel<<<blocks, TPR == 32 ? 32 * kWarpRows : TPR, smem, st>>>(p);
+    return cudaGetLastError();
+}
+
+template <typename T, typename W, int VEC>
+cudaError_t backward_by_width(const ResidualNormArgs &p, int blocks, cudaStream_t st) {
+    switch (backward_threads(p.a.width)) {
+        case 32: return backward_as<T, W, VEC, 32>(p, blocks, st);
+        case 64: return backward_as<T, W, VEC, 64>(p, blocks, st);
+        case 96: return backward_as<T, W, VEC, 96>(p, blocks, st);
+        case 128: return backward_as<T, W, VEC, 128>(p, blocks, st);
+        case 256: return backward_as<T, W, VEC, 256>(p, blocks, st);
+        case 512: return backward_as<T, W, VEC, 512>(p, blocks, st);
+        default: return backward_as<T, W, VEC, 1024>(p, blocks, st);
+    }
+}
+
+template <typename T, typename W>
+cudaError_t backward(const ResidualNormArgs &p, cudaStream_t st) {
+    const int blocks = backward_blocks(p.a.rows, p.a.width), groups = blocks * groups_of(backward_threads(p.a.width));
+    if (blocks > 0) {
+        const cudaError_t e = wide<T>(p) ? backward_by_width<T, W, 16 / sizeof(T)>(p, blocks, st)
+                                         : backward_by_width<T, W, 1>(p, blocks, st);
+        if (e != cudaSuccess) return e;
+    }
+    k_residual_reduce<W><<<dim3((unsigned)ceil_div(p.a.width, 32), 2), 1024, 0, st>>>(p, groups);
+    return cudaGetLastError();
+}
+
+template <typename F>
+cudaError_t by_type(int dtype, int wtype, F f) {
+    if (dtype == SIEVE_F32) return f(float{}, float{});
+    if (dtype == SIEVE_F16) return wtype == SIEVE_F32 ? f(__half{}, float{}) : f(__half{}, __half{});
+    return wtype == SIEVE_F32 ? f(__nv_bfloat16{}, float{}) : f(__nv_bfloat16{}, __nv_bfloat16{});
+}
+
+}  // namespace
+
+cudaError_t launch_residual_norm(const ResidualNormArgs &p, cudaStream_t st) {
+    return by_type(p.a.dtype, p.a.weight_dtype,
+                   [&](auto t, auto w) { return forward<decltype(t), decltype(w)>(p, st); });
+}
+cudaError_t launch_residual_norm_backward(const ResidualNormArgs &p, cudaStream_t st) {
+    return by_type(p.a.dtype, p.a.weight_dtype,
+                   [&](auto t, auto w) { return backward<decltype(t), decltype(w)>(p, st); });
+}
+size_t residual_norm_backward_workspace_bytes(int64_t rows, int width) {
+    const int64_t groups = (int64_t)backward_blocks(rows, width) * groups_of(backward_threads(width));
+    return (size_t)round_up(groups * 4 * width * (int64_t)sizeof(float) + 256, 256);
+}
+
+}  // namespace enc
+}  // namespace sieve
