@@ -321,9 +321,9 @@ sieve_status sieve_cross_entropy(const sieve_cross_entropy_args *a, float *loss,
  *   dh[r] = dloss[r] scale sum over v of q weight[v],
  *   dweight[v] = scale sum over r of dloss[r] q h[r],
  *   dbias[v] = sum over r of dloss[r] q.
- * The scores are made anew in pieces of the classes; q is rounded once to
- * dtype on its way into both products, and where the rows' dloss differ, so is
- * dloss h over its largest.
+ * The scores are made anew in pieces of the classes; q (times the mantissa of
+ * dloss, where the rows' dloss differ) is rounded once to dtype on its way into
+ * both products.
  *   dloss    device [rows] fp32;  loss, lse what sieve_cross_entropy wrote
  *   dh       device [rows][width] of dtype out, rows dh_stride apart; nullable
  *   dweight  device [classes][width] of `dweight_dtype` (dtype or SIEVE_F32)

@@ -25,11 +25,22 @@
 // [64], so its address needs no stride that depends on the list.  As operand of
 // dh a panel is K-major, as operand of dW MN-major.
 //
-// dloss differs from row to row.  dh takes it at the end, in fp32.  dW needs it
-// in the product: where all rows have the same one it is a factor at the end,
-// else h times dloss over the largest is rounded to 16 bits as an operand of its own.
-// In fp16 q is taken 2^14 times as large, so that small probabilities keep
-// their bits.
+// dloss differs from row to row, and dW needs it in the product.  Where all
+// rows have the same one it is a factor at the end.  Else it is taken apart, m 2^e:
+// q is rounded times m, h gets an exact 2^e (over the largest) in a copy of its own,
+// and so does dh at the end; nothing is rounded twice.  In fp16 q is taken 2^14
+// times as large, so that small probabilities keep their bits.
+//
+// The tensor cores cut a sum off at every step of 16 products instead of
+// rounding it, which leaves a score of 2,048 products off by a few 1e-6 of itself, all to
+// one side.  So a contraction runs in chunks (256 products of a score, 4,096 of
+// a gradient) whose sums are added up in registers.
+//
+// A row's q add up to zero, its rounded q to some e.  Where the likely classes
+// are much alike (rows of the same topic), q W is a difference of large numbers
+// and e times what they have in common would show in dh.  So MODE 1 adds
+// up what it rounded, and dh gets -e times the target's row of W at the end: a
+// rounding error then counts with its class' distance from the target.
 #include <cfloat>
 #include <cstring>
 
@@ -47,6 +58,7 @@ constexpr uint32_t kBoxBytes = kBox * 128;
 constexpr int kABoxes = kM / kBox, kBBoxes = kN / kBox;
 constexpr uint32_t kStageBytes = (kABoxes + kBBoxes) * kBoxBytes;
 constexpr int kEpiWarps = 8;
+__host__ __device__ constexpr int chunk_blocks(int mode) { return mode == 2 ? 64 : 4; }
 constexpr int kThreads = (kEpiWarps + 2) * 32;
 constexpr uint32_t kOutBytes = 32 * 128;              // a warp's rows on their way out
 __host__ __device__ constexpr int stages(int mode) { return mode == 1 ? 3 : 4; }
@@ -56,6 +68,7 @@ __host__ __device__ constexpr uint32_t smem_bytes(int mode) {
 constexpr uint32_t kTmemCols = 512;
 constexpr int kGrid = 152;                            // one block an SM
 constexpr int kMaxGroup = 16;                         // tiles of classes whose statistics one block keeps
+constexpr int kMaxSlabs = 16;
 constexpr int kRowTile = 256;                         // rows of a block of k_xent_rows
 constexpr int64_t kPoolBytes = (int64_t)1 << 30;
 
@@ -64,18 +77,19 @@ struct Ctl {
     int n;               // rows with a target
     int all;             // every row has one
     int same;            // all of them have the same dloss
-    float factor;        // that dloss, or the largest magnitude
+    float factor;        // that dloss, or the power of two above the largest magnitude
 };
 
 struct XentArgs {
     CUtensorMap h, hc, hs, w, pool_in, pool_out, acc, dw;
     Ctl *ctl;
     const int *target;                    // of the list
-    const float *lse, *loss, *dloss;      // of the list
+    const float *lse, *loss, *dloss, *part_of;   // of the list (part_of: m, or 1)
     const float *bias;
     float *hit;                           // [rows] the target's score
     float2 *part;                         // [parts][rows of the list, padded] maximum and sum
     float *colsum;                        // [32 rows][classes]
+    float *rest;                          // [halves of class tiles][rows of the list, padded] sums of rounded q
     int64_t pool_rows;
     int rows, classes, width;
     float scale, c;                       // c = scale log2(e)
@@ -84,6 +98,13 @@ struct XentArgs {
 
 template <typename T>
 constexpr float kUp = std::is_same_v<T, __half> ? 16384.f : 1.f;
+
+// two rounded values of a packed pair, added to a sum
+template <typename T>
+__device__ __forceinline__ float2 add_pair(float2 sum, uint32_t pair) {
+    if constexpr (std::is_same_v<T, __half>) return add2(sum, __half22float2(*reinterpret_cast<const __half2 *>(&pair)));
+    else return add2(sum, make_float2(__uint_as_float(pair << 16), __uint_as_float(pair & 0xffff0000u)));
+}
 
 // classes of a piece, and how the forward pass groups its tiles
 __host__ __device__ inline int64_t padded(int64_t n) { return (n < 1 ? 1 : n) + kM - 1 - ((n < 1 ? 1 : n) - 1) % kM; }
@@ -95,6 +116,16 @@ __host__ __device__ inline int piece_classes(int64_t n, int classes, int64_t poo
 __host__ __device__ inline int group_tiles(int64_t n, int classes) {
     const int64_t tiles = padded(n) / kM * ((classes + kN - 1) / kN), g = tiles / (8 * kGrid);
     return (int)(g < 1 ? 1 : g > kMaxGroup ? kMaxGroup : g);
+}
+
+// dh has few tiles and a long contraction: it is cut into `slabs`, each with
+// sums of its own, so that no block works longer on one than half of an SM's share
+// of the launch.
+__host__ __device__ inline int dh_slabs(int64_t n, int classes, int width, int64_t pool_rows, bool dw) {
+    const int64_t blocks = piece_classes(n, classes, pool_rows) / kK, across = (width + kN - 1) / kN;
+    const int64_t tiles = padded(n) / kM * across, others = dw ? blocks / 2 * across * ((n + kK - 1) / kK) : 0;
+    const int64_t share = (tiles * blocks + others) / kGrid / 2 + 1, slabs = (blocks + share - 1) / share;
+    return (int)(slabs < kMaxSlabs ? slabs : kMaxSlabs);
 }
 
 // ---------------------------------------------------------------------------
@@ -110,7 +141,7 @@ struct RowArgs {
     int *count;                           // [blocks]
     uint32_t *top, *low;                  // [blocks] largest dloss, and its lowest, as ordered keys
     int *row, *target;
-    float *dloss_c, *loss_c, *lse_c;
+    float *dloss_c, *loss_c, *lse_c, *part_c, *whole_c;   // part_c whole_c = dloss
     void *hc, *hs;
 };
 
@@ -197,13 +228,23 @@ __global__ void __launch_bounds__(kRowTile) k_xent_rows(const RowArgs a) {
     rank += __popc(live & ((1u << lane) - 1));
     const bool every = all == a.rows, same = top == low;
     const float hi = unordered(top), lo = unordered(low);
-    const float factor = same ? hi : fmaxf(fabsf(hi), fabsf(lo));
+    // m 2^e of a dloss; a zero, or one that is not finite, stays whole, and so does
+    // its h
+    const float largest = fmaxf(fabsf(hi), fabsf(lo));
+    int e_top = 0;
+    if (isfinite(largest)) frexpf(largest, &e_top);
+    auto apart = [&](float v, int &e) {
+        const float m = frexpf(v, &e);
+        if (v != 0.f && isfinite(v)) return m;
+        e = e_top;
+        return v;
+    };
     if (blockIdx.x == 0 && tid == 0) {
         a.ctl->status = 0;
         a.ctl->n = all;
         a.ctl->all = every;
         a.ctl->same = !a.dloss || same;
-        a.ctl->factor = a.dloss && all > 0 ? factor : 0.f;
+        a.ctl->factor = a.dloss && all > 0 ? (same ? hi : ldexpf(1.f, e_top)) : 0.f;
     }
     if (t >= 0) {
         const int at = before + rank;
@@ -211,7 +252,12 @@ __global__ void __launch_bounds__(kRowTile) k_xent_rows(const RowArgs a) {
         a.row[at] = (int)r;
         a.target[at] = t;
         if (a.dloss) {
-            a.dloss_c[at] = a.dloss[r];
+            const float v = a.dloss[r];
+            int e;
+            const float m = apart(v, e);
+            a.dloss_c[at] = v;
+            a.part_c[at] = same ? 1.f : m;
+            a.whole_c[at] = same ? v : ldexpf(1.f, e);
             a.loss_c[at] = a.loss[r];
             a.lse_c[at] = a.lse[r];
         }
@@ -227,7 +273,9 @@ __global__ void __launch_bounds__(kRowTile) k_xent_rows(const RowArgs a) {
         T *hc = static_cast<T *>(a.hc), *hs = static_cast<T *>(a.hs);
         for (int i = warp; i < here; i += kWarps) {
             const int64_t from = (int64_t)blockIdx.x * kRowTile + s_list[i], to = before + i;
-            const float f = scaled ? a.dloss[from] / factor : 0.f;
+            int e_row = e_top;
+            if (scaled) apart(a.dloss[from], e_row);
+            const float f = ldexpf(1.f, e_row - e_top);
 #pragma unroll 4
             for (int c = lane; c < chunks; c += 32) {
                 const uint4 raw = __ldg(reinterpret_cast<const uint4 *>(h + from * a.h_stride) + c);
@@ -296,7 +344,8 @@ __device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait
 struct Tile {
     int m0, n0;          // first row and column of the result
     int n_boxes;         // of 64 columns
-    int blocks;          // stages of the contraction axis
+    int first, blocks;   // stages of the contraction axis
+    int slab;            // MODE 2, dh: which sums
     bool dw;             // MODE 2: dW, else dh
 };
 
@@ -305,7 +354,7 @@ template <int MODE>
 struct Walk {
     int n, mp, row_tiles, class_tiles, group, groups;
     int v0, v1;                                      // classes of the piece
-    int dh_tiles, d_tiles, dw_rows, total, width;
+    int dh_tiles, d_tiles, dw_rows, total, width, slabs, slab_blocks;
     __device__ __forceinline__ Walk(const XentArgs &a, int piece) {
         n = a.ctl->n;
         mp = (int)padded(n);
@@ -322,7 +371,12 @@ struct Walk {
         class_tiles = (v1 - v0 + kN - 1) / kN;
         group = MODE == 0 ? group_tiles(n, a.classes) : 1;
         groups = (class_tiles + group - 1) / group;
-        dh_tiles = a.want_dh && v1 > v0 ? row_tiles * d_tiles : 0;
+        slabs = slab_blocks = 1;
+        if (MODE == 2) {
+            slabs = dh_slabs(n, a.classes, a.width, a.pool_rows, a.want_dw);
+            slab_blocks = (piece_classes(n, a.classes, a.pool_rows) / kK + slabs - 1) / slabs;
+        }
+        dh_tiles = a.want_dh && v1 > v0 ? row_tiles * d_tiles * slabs : 0;
         dw_rows = a.want_dw ? (v1 - v0 + kM - 1) / kM : 0;
         total = MODE == 2 ? dh_tiles + dw_rows * d_tiles : row_tiles * groups;
     }
@@ -336,6 +390,7 @@ struct Walk {
             t.m0 = i % row_tiles * kM;
             t.n0 = v0 + (i / row_tiles * group + k) * kN;
             t.n_boxes = kBBoxes;
+            t.first = t.slab = 0;
             t.blocks = (width + kK - 1) / kK;
             t.dw = false;
             return t;
@@ -344,16 +399,19 @@ struct Walk {
         if (t.dw) i -= dh_tiles;
         const int across = t.dw ? dw_rows : row_tiles;
         t.m0 = i % across * kM;
-        t.n0 = i / across * kN;
+        i /= across;
+        t.n0 = i % d_tiles * kN;
+        t.slab = i / d_tiles;
         t.n_boxes = min(kBBoxes, (width - t.n0 + kBox - 1) / kBox);
-        t.blocks = t.dw ? (n + kK - 1) / kK : (v1 - v0 + kK - 1) / kK;
+        t.first = t.slab * slab_blocks;
+        t.blocks = t.dw ? (n + kK - 1) / kK : max(0, min(slab_blocks, (v1 - v0 + kK - 1) / kK - t.first));
         return t;
     }
 };
 
 template <typename T, int MODE, bool BIAS>
 __global__ void __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ XentArgs a, int piece) {
-    constexpr int kStages = stages(MODE);
+    constexpr int kStages = stages(MODE), kChunk = chunk_blocks(MODE);
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t full[kStages], empty[kStages], d_full[2], d_empty[2], drained;
     __shared__ uint32_t tmem_slot;
@@ -405,13 +463,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ Xe
                             void *dst = pa + j * kBoxBytes;
                             if (MODE != 2) load_box(dst, rows, b * kK, t.m0 + j * kBox, &full[st]);
                             else if (t.dw) load_box(dst, &a.pool_in, 0, (t.m0 / kBox + j) * walk.mp + b * kK, &full[st]);
-                            else load_box(dst, &a.pool_in, 0, b * walk.mp + t.m0 + j * kBox, &full[st]);
+                            else load_box(dst, &a.pool_in, 0, (t.first + b) * walk.mp + t.m0 + j * kBox, &full[st]);
                         }
                         for (int j = 0; j < t.n_boxes; ++j) {
                             void *dst = pb + j * kBoxBytes;
                             if (MODE != 2) load_box(dst, &a.w, b * kK, t.n0 + j * kBox, &full[st]);
                             else if (t.dw) load_box(dst, rows, t.n0 + j * kBox, b * kK, &full[st]);
-                            else load_box(dst, &a.w, t.n0 + j * kBox, walk.v0 + b * kK, &full[st]);
+                            else load_box(dst, &a.w, t.n0 + j * kBox, walk.v0 + (t.first + b) * kK, &full[st]);
                         }
                     }
                     __syncwarp();
@@ -425,15 +483,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ Xe
         int s = 0, c = 0;
         bool ok = true;
         for (int i = blockIdx.x; ok && i < walk.total; i += gridDim.x)
-            for (int k = 0, nk = walk.tiles(i); ok && k < nk; ++k, ++c) {
+            for (int k = 0, nk = walk.tiles(i); ok && k < nk; ++k) {
                 const Tile t = walk.tile(i, k);
-                const int buf = c & 1;
-                if (!(ok = wait.warp(&d_empty[buf], ((uint32_t)(c >> 1) & 1u) ^ 1u))) break;
                 const bool a_mn = MODE == 2 && t.dw, b_mn = MODE == 2;
-                const uint32_t id = product<T>(t.n_boxes * kBox, a_mn, b_mn), d = tmem + buf * kN;
+                const uint32_t id = product<T>(t.n_boxes * kBox, a_mn, b_mn);
                 const uint64_t step_a = a_mn ? 128 : 2, step_b = b_mn ? 128 : 2;
 #pragma unroll 1
                 for (int b = 0; b < t.blocks; ++b, ++s) {
+                    const int buf = c & 1;
+                    const uint32_t d = tmem + buf * kN;
+                    if (b % kChunk == 0 && !(ok = wait.warp(&d_empty[buf], ((uint32_t)(c >> 1) & 1u) ^ 1u))) break;
                     const int st = s % kStages;
                     if (!(ok = wait.warp(&full[st], (uint32_t)(s / kStages) & 1u))) break;
                     tc::fence_after_sync();
@@ -442,14 +501,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ Xe
                         const uint64_t da = a_mn ? desc_boxes(pa) : desc_k(pa), db = b_mn ? desc_boxes(pb) : desc_k(pb);
 #pragma unroll
                         for (int x = 0; x < kK / 16; ++x)
-                            mma_ss(d, da + x * step_a, db + x * step_b, id, b > 0 || x > 0);
+                            mma_ss(d, da + x * step_a, db + x * step_b, id, b % kChunk > 0 || x > 0);
                         commit(&empty[st]);
+                        if (b % kChunk == kChunk - 1 || b + 1 == t.blocks) commit(&d_full[buf]);
                     }
                     __syncwarp();
+                    if (b % kChunk == kChunk - 1 || b + 1 == t.blocks) ++c;
                 }
-                if (!ok) break;
-                if (elected()) commit(&d_full[buf]);
-                __syncwarp();
             }
         // every product issued ends before the block frees its memory
         if (elected()) commit(&drained);
@@ -465,7 +523,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ Xe
         int c = 0;
         bool ok = true;
         for (int i = blockIdx.x; ok && i < walk.total; i += gridDim.x) {
-            float top = -INFINITY, sum = 0.f, lse = 0.f, dloss = 0.f;
+            float top = -INFINITY, sum = 0.f, lse = 0.f, dloss = 0.f, part = 0.f;
             int target = -1, row = 0;
             bool live = false;
             if (MODE != 2) {
@@ -477,11 +535,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ Xe
                     if (lse == -INFINITY) lse = INFINITY;       // every class hidden: no probabilities
                     if (!BIAS) lse *= kLog2e;
                     dloss = a.dloss[row];
+                    part = a.part_of[row] * kUp<T>;
                 }
             }
-            for (int k = 0, nk = walk.tiles(i); ok && k < nk; ++k, ++c) {
+            for (int k = 0, nk = walk.tiles(i); ok && k < nk; ++k) {
                 const Tile t = walk.tile(i, k);
-                const int buf = c & 1;
                 // this warp's columns of the tile
                 const int col = t.n0 + half * (kN / 2);
                 if (MODE != 2 && BIAS) {
@@ -491,14 +549,40 @@ __global__ void __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ Xe
                         s_bias[warp][j + lane] = col + j + lane < a.classes ? __ldg(a.bias + col + j + lane) : -INFINITY;
                     __syncwarp();
                 }
-                if (!(ok = wait.warp(&d_full[buf], (uint32_t)(c >> 1) & 1u))) break;
-                tc::fence_after_sync();
-                const uint32_t d = lanes + buf * kN + half * (kN / 2);
-                if constexpr (MODE == 0) {
+                // The tile's sums: its chunks added up, each released as soon as it is
+                // in registers, so that the next tile's products run under what follows.
+                float2 acc[kN / 4];
+#pragma unroll
+                for (int e = 0; e < kN / 4; ++e) acc[e] = make_float2(0.f, 0.f);
 #pragma unroll 1
+                for (int b = 0; b < t.blocks; b += kChunk, ++c) {
+                    if (!(ok = wait.warp(&d_full[c & 1], (uint32_t)(c >> 1) & 1u))) break;
+                    tc::fence_after_sync();
+                    const uint32_t from = lanes + (c & 1) * kN + half * (kN / 2);
+#pragma unroll
                     for (int j = 0; j < kN / 2; j += 32) {
                         float x[32];
-                        tc::tmem_ld32(d + j, x);
+                        tc::tmem_ld32(from + j, x);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            acc[j / 2 + e] = add2(make_float2(x[2 * e], x[2 * e + 1]), acc[j / 2 + e]);
+                    }
+                    tc::fence_before_sync();
+                    warp_arrive(&d_empty[c & 1]);
+                }
+                if (!ok) break;
+                auto take = [&](int j, float (&x)[32]) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        x[2 * e] = acc[j / 2 + e].x;
+                        x[2 * e + 1] = acc[j / 2 + e].y;
+                    }
+                };
+                if constexpr (MODE == 0) {
+#pragma unroll
+                    for (int j = 0; j < kN / 2; j += 32) {
+                        float x[32];
+                        take(j, x);
                         if constexpr (BIAS) {
 #pragma unroll
                             for (int e = 0; e < 32; ++e) x[e] = fmaf(x[e], a.scale, s_bias[warp][j + e]);
@@ -535,13 +619,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ Xe
                         top = high;
                     }
                 } else if constexpr (MODE == 1) {
-#pragma unroll 1
+                    float2 rest[2] = {};
+#pragma unroll
                     for (int j = 0; j < kN / 2; j += 64) {
                         uint32_t packed[32];
 #pragma unroll
                         for (int jj = 0; jj < 64; jj += 32) {
                             float x[32];
-                            tc::tmem_ld32(d + j + jj, x);
+                            take(j + jj, x);
                             const int first = col + j + jj;
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
@@ -561,7 +646,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ Xe
                                 for (int e = 0; e < 32; ++e) x[e] = e < left ? x[e] : 0.f;
 #pragma unroll
                             for (int e = 0; e < 32; e += 2)
-                                packed[(jj + e) / 2] = pack2<T>(x[e] * kUp<T>, x[e + 1] * kUp<T>);
+                                packed[(jj + e) / 2] = pack2<T>(x[e] * part, x[e + 1] * part);
+#pragma unroll
+                            for (int e = 0; e < 32; e += 2)
+                                rest[e / 2 % 2] = add_pair<T>(rest[e / 2 % 2], packed[(jj + e) / 2]);
                             if (BIAS && a.want_db) {
                                 // the columns' sums over the warp's rows: lane e ends with column e
 #pragma unroll
@@ -592,36 +680,34 @@ __global__ void __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ Xe
                             stores_issued();
                         }
                     }
+                    if (live) a.rest[(int64_t)(t.n0 / kN * 2 + half) * walk.mp + row] = (rest[0].x + rest[0].y) + (rest[1].x + rest[1].y);
                 } else {
                     const int columns = t.n_boxes * kBox;        // of the tile that exist
-                    const int r0 = (t.dw ? walk.v0 : 0) + t.m0 + quarter * 32;
+                    const int r0 = (t.dw ? walk.v0 : t.slab * walk.mp) + t.m0 + quarter * 32;
                     const bool some = t.dw ? r0 < walk.v1 : true;
                     const bool wide = !t.dw || a.dw_f32;         // fp32 results: 32 columns to a box, else 64
                     const bool adds = t.dw ? a.accumulate : piece > 0;
                     const float f = t.dw ? factor : 1.f;
                     // (dh: past the list's rows of the last tile nothing is read again)
-#pragma unroll 1
-                    for (int j = 0; j < kN / 2 && half * (kN / 2) + j < columns; j += 64) {
-                        float x[2][32];
-                        if (t.blocks > 0) {
-                            tc::tmem_ld32(d + j, x[0]);
-                            tc::tmem_ld32(d + j + 32, x[1]);
-                        }
 #pragma unroll
-                        for (int b = 0; b < 2; ++b)
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) x[b][e] = t.blocks > 0 ? x[b][e] * f : 0.f;
+                    for (int j = 0; j < kN / 2; j += 64) {
+                        if (half * (kN / 2) + j >= columns) break;
                         const int x0 = t.n0 + half * (kN / 2) + j;
                         const CUtensorMap *map = t.dw ? &a.dw : &a.acc;
-                        if (wide) {
+                        uint32_t packed[32];
 #pragma unroll
-                            for (int b = 0; b < 2; ++b) {
+                        for (int b = 0; b < 2; ++b) {
+                            float x[32];
+                            take(j + 32 * b, x);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) x[e] *= f;
+                            if (wide) {
                                 stores_read();
                                 __syncwarp();
 #pragma unroll
                                 for (int e = 0; e < 8; ++e)
                                     *reinterpret_cast<float4 *>(out + lane * 128 + ((e ^ (lane & 7)) << 4)) =
-                                        make_float4(x[b][4 * e], x[b][4 * e + 1], x[b][4 * e + 2], x[b][4 * e + 3]);
+                                        make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
                                 tc::fence_proxy_async_smem();
                                 __syncwarp();
                                 if (lane == 0 && some && x0 + 32 * b < a.width) {
@@ -629,14 +715,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ Xe
                                     else store_box(map, x0 + 32 * b, r0, out);
                                     stores_issued();
                                 }
+                            } else {
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) packed[16 * b + e] = pack2<T>(x[2 * e], x[2 * e + 1]);
                             }
-                        } else {
+                        }
+                        if (!wide) {
                             stores_read();
                             __syncwarp();
 #pragma unroll
                             for (int e = 0; e < 8; ++e)
                                 *reinterpret_cast<uint4 *>(out + lane * 128 + ((e ^ (lane & 7)) << 4)) =
-                                    pack8<T>(&x[e / 4][8 * (e % 4)]);
+                                    make_uint4(packed[4 * e], packed[4 * e + 1], packed[4 * e + 2], packed[4 * e + 3]);
                             tc::fence_proxy_async_smem();
                             __syncwarp();
                             if (lane == 0 && some) {
@@ -646,8 +736,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ Xe
                         }
                     }
                 }
-                tc::fence_before_sync();
-                warp_arrive(&d_empty[buf]);
             }
             if (MODE == 0 && ok && live)
                 a.part[(int64_t)(i / walk.row_tiles * 2 + half) * walk.mp + row] = make_float2(top, sum);
@@ -723,20 +811,57 @@ __global__ void __launch_bounds__(32 * kStrands) k_xent_join(const JoinArgs a) {
     }
 }
 
-// dh from its fp32 sums: the list's rows to their places.
+// dh from its slabs' sums: the list's rows to their places, 32 to a block, with
+// what the rounded q of a row add up to taken off the target's.
+struct DhArgs {
+    const Ctl *ctl;
+    const int *row, *target;
+    const float *whole, *acc, *rest;
+    const void *weight;
+    void *dh;
+    int64_t weight_stride, dh_stride, pool_rows;
+    int classes, width, want_dw;
+    float scale;
+};
 template <typename T>
-__global__ void __launch_bounds__(256) k_xent_dh(const Ctl *ctl, const int *row, const float *dloss, const float *acc, int width,
-                                                 float scale, T *dh, int64_t stride) {
-    const int chunks = width / 8;
-    const int64_t total = (int64_t)ctl->n * chunks;
-    for (int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x; w < total; w += (int64_t)gridDim.x * 256) {
-        const int64_t i = w / chunks;
-        const int c = (int)(w - i * chunks);
-        const float f = dloss[i] * scale / kUp<T>;
-        const float4 *x = reinterpret_cast<const float4 *>(acc + i * width) + 2 * c;
-        const float4 p = __ldcs(x), q = __ldcs(x + 1);
-        const float v[8] = {p.x * f, p.y * f, p.z * f, p.w * f, q.x * f, q.y * f, q.z * f, q.w * f};
-        reinterpret_cast<uint4 *>(dh + row[i] * stride)[c] = pack8<T>(v);
+__global__ void __launch_bounds__(32 * kStrands) k_xent_dh(const DhArgs a) {
+    __shared__ float s_rest[kStrands][32];
+    const int lane = lane_id(), strand = threadIdx.x >> 5, n = a.ctl->n, chunks = a.width / 8;
+    const int64_t mp = padded(n);
+    const int parts = (a.classes + kN - 1) / kN * 2;
+    const int slabs = dh_slabs(n, a.classes, a.width, a.pool_rows, a.want_dw);
+    for (int64_t i0 = (int64_t)blockIdx.x * 32; i0 < n; i0 += (int64_t)gridDim.x * 32) {
+        float sum = 0.f;
+        if (i0 + lane < n)
+#pragma unroll 8
+            for (int p = strand; p < parts; p += kStrands) sum += a.rest[p * mp + i0 + lane];
+        __syncthreads();
+        s_rest[strand][lane] = sum;
+        __syncthreads();
+        for (int k = strand; k < 32 && i0 + k < n; k += kStrands) {
+            const int64_t i = i0 + k;
+            float rest = 0.f;
+            for (int p = 0; p < kStrands; ++p) rest -= s_rest[p][k];
+            const float f = a.whole[i] * a.scale / kUp<T>;
+            const T *w = static_cast<const T *>(a.weight) + a.target[i] * a.weight_stride;
+            T *out = static_cast<T *>(a.dh) + a.row[i] * a.dh_stride;
+            for (int c = lane; c < chunks; c += 32) {
+                float v[8];
+                load_vec<T, 8>(w + 8 * c, v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] *= rest;
+                for (int s = 0; s < slabs; ++s) {
+                    const float4 *x = reinterpret_cast<const float4 *>(a.acc + (s * mp + i) * a.width) + 2 * c;
+                    const float4 p = __ldcs(x), q = __ldcs(x + 1);
+                    const float y[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] += y[e];
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] *= f;
+                reinterpret_cast<uint4 *>(out)[c] = pack8<T>(v);
+            }
+        }
     }
 }
 
@@ -758,8 +883,8 @@ __global__ void __launch_bounds__(256) k_xent_db(const Ctl *ctl, const float *co
 
 // ---------------------------------------------------------------------------
 struct Layout {
-    size_t count, top, low, row, target, dloss, loss, lse, hc, hs, hit, part, pool, acc, colsum, bytes;
-    int64_t pool_rows;
+    size_t count, top, low, row, target, dloss, loss, lse, hc, hs, hit, part, part_of, whole, pool, acc, rest, colsum, bytes;
+    int64_t pool_rows, acc_rows;
 };
 Layout layout(const sieve_cross_entropy_args &a, bool backward) {
     Layout l = {};
@@ -786,11 +911,18 @@ Layout layout(const sieve_cross_entropy_args &a, bool backward) {
         l.dloss = take(n * 4);
         l.loss = take(n * 4);
         l.lse = take(n * 4);
+        l.part_of = take(n * 4);
+        l.whole = take(n * 4);
         l.hs = take(n * a.width * 2);
         const int64_t needed = np * (round_up(a.classes, kN) / kK), least = np * (kN / kK), most = kPoolBytes / 128;
         l.pool_rows = needed < most ? needed : least > most ? least : most;
         l.pool = take(l.pool_rows * 128);
-        l.acc = take(np * a.width * 4);
+        // (dh_slabs: tiles times slabs stay below two shares for each SM, or there is one slab)
+        const int64_t across = ceil_div(a.width, kN), some = 2 * kGrid / across + 1;
+        const int64_t most_slabs = np / kM * kMaxSlabs < np / kM + some ? np / kM * kMaxSlabs : np / kM + some;
+        l.acc_rows = most_slabs * kM;
+        l.acc = take(l.acc_rows * a.width * 4);
+        l.rest = take(ceil_div(a.classes, kN) * 2 * np * 4);
         if (a.bias) l.colsum = take(np / 32 * a.classes * 4);
     }
     l.bytes = at;
@@ -854,7 +986,7 @@ cudaError_t forward(const Call &c, const JoinArgs &j, cudaStream_t st) {
 }
 
 template <typename T>
-cudaError_t backward(const Call &c, const sieve_cross_entropy_grads &g, const float *acc, int pieces, cudaStream_t st) {
+cudaError_t backward(const Call &c, const sieve_cross_entropy_grads &g, const DhArgs &d, int pieces, cudaStream_t st) {
     k_xent_count<<<c.blocks, kRowTile, 0, st>>>(c.r);
     k_xent_rows<T><<<c.blocks, kRowTile, 0, st>>>(c.r);
     for (int p = 0; p < pieces; ++p) {
@@ -862,9 +994,10 @@ cudaError_t backward(const Call &c, const sieve_cross_entropy_grads &g, const fl
         if (e == cudaSuccess && (g.dh || g.dweight)) e = run<T, 2, false>(c.x, p, st);
         if (e != cudaSuccess) return e;
     }
-    if (g.dh)
-        k_xent_dh<T><<<kGrid * 8, 256, 0, st>>>(c.x.ctl, c.r.row, c.x.dloss, acc, c.x.width, c.x.scale, static_cast<T *>(g.dh),
-                                               g.dh_stride);
+    if (g.dh) {
+        const int64_t blocks = ceil_div(c.x.rows, 32);
+        k_xent_dh<T><<<(unsigned)(blocks < 4096 ? blocks : 4096), 32 * kStrands, 0, st>>>(d);
+    }
     if (g.dbias)
         k_xent_db<<<(unsigned)ceil_div(c.x.classes, 32), 256, 0, st>>>(c.x.ctl, c.x.colsum, c.x.classes, g.dbias);
     return cudaGetLastError();
@@ -902,6 +1035,7 @@ sieve_status launch_cross_entropy_backward(const sieve_cross_entropy_args &a, co
     c.x.loss = reinterpret_cast<float *>(base + l.loss);
     c.x.dloss = reinterpret_cast<float *>(base + l.dloss);
     c.x.colsum = reinterpret_cast<float *>(base + l.colsum);
+    c.x.rest = reinterpret_cast<float *>(base + l.rest);
     c.x.pool_rows = l.pool_rows;
     c.x.want_dh = g.dh != nullptr;
     c.x.want_dw = g.dweight != nullptr;
@@ -918,18 +1052,22 @@ sieve_status launch_cross_entropy_backward(const sieve_cross_entropy_args &a, co
     c.r.dloss_c = reinterpret_cast<float *>(base + l.dloss);
     c.r.loss_c = reinterpret_cast<float *>(base + l.loss);
     c.r.lse_c = reinterpret_cast<float *>(base + l.lse);
+    c.r.part_c = reinterpret_cast<float *>(base + l.part_of);
+    c.r.whole_c = reinterpret_cast<float *>(base + l.whole);
+    c.x.part_of = c.r.part_c;
     c.r.hs = base + l.hs;
     rc = make_matrix_map(&c.x.hs, a.dtype, base + l.hs, a.rows, a.width, a.width, kBox);
     if (rc == SIEVE_OK) rc = make_matrix_map(&c.x.pool_in, a.dtype, base + l.pool, l.pool_rows, kK, kK, kBox);
     if (rc == SIEVE_OK) rc = make_matrix_map(&c.x.pool_out, a.dtype, base + l.pool, l.pool_rows, kK, kK, 32);
-    if (rc == SIEVE_OK) rc = make_matrix_map(&c.x.acc, SIEVE_F32, base + l.acc, padded(a.rows), a.width, a.width, 32);
+    if (rc == SIEVE_OK) rc = make_matrix_map(&c.x.acc, SIEVE_F32, base + l.acc, l.acc_rows, a.width, a.width, 32);
     if (rc == SIEVE_OK && g.dweight)
         rc = make_matrix_map(&c.x.dw, g.dweight_dtype, g.dweight, a.classes, a.width, g.dweight_stride, 32);
     if (rc != SIEVE_OK) return rc;
     const int each = piece_classes(a.rows, c.x.classes, l.pool_rows), pieces = (int)ceil_div(a.classes, each);
-    const float *acc = reinterpret_cast<const float *>(base + l.acc);
-    const cudaError_t e = a.dtype == SIEVE_F16 ? backward<__half>(c, g, acc, pieces, st)
-                                               : backward<__nv_bfloat16>(c, g, acc, pieces, st);
+    const DhArgs d = {c.x.ctl, c.r.row, c.x.target, c.r.whole_c, reinterpret_cast<const float *>(base + l.acc), c.x.rest, a.weight,
+                      g.dh, a.weight_stride, g.dh_stride, l.pool_rows, c.x.classes, a.width, c.x.want_dw, a.scale};
+    const cudaError_t e = a.dtype == SIEVE_F16 ? backward<__half>(c, g, d, pieces, st)
+                                               : backward<__nv_bfloat16>(c, g, d, pieces, st);
     return e == cudaSuccess ? SIEVE_OK : record_cuda_error(e);
 }
 
