@@ -7,9 +7,10 @@
 //
 // Four products of 2 rows classes width operations each: z in the forward pass;
 // z again, dh and dW in the backward pass.  All run in one kernel,
-// k_xent<MODE>: tiles of 128 x 256, operands loaded by TMA into a ring of
-// stages, tcgen05 products into one of two accumulators in tensor memory while
-// eight warps work on the other.
+// k_xent<MODE>: tiles of 256 x 256 of a pair of blocks on two SMs (each loads half
+// of both operands by TMA into a ring of stages and keeps 128 rows of the result in
+// tensor memory), tcgen05 products into one of two accumulators while eight warps
+// of each block work on the other.
 //   MODE 0  z tiles to a running maximum and sum per row; the target's score
 //           is kept apart, so that loss = log1p(sum of the others against it)
 //   MODE 1  z tiles to q, rounded to 16 bits, in a pool of panels
@@ -52,21 +53,23 @@ namespace sieve {
 namespace enc {
 namespace {
 
-constexpr int kM = 128, kN = 256, kK = 64;            // a tile, and the contraction of a stage
+constexpr int kM = 256, kN = 256, kK = 64;            // a pair's tile, and the contraction of a stage
+constexpr int kHalf = kM / 2;                         // rows of a block, and its columns of the second operand
 constexpr int kBox = 64;                              // rows of a box of 128 bytes
 constexpr uint32_t kBoxBytes = kBox * 128;
-constexpr int kABoxes = kM / kBox, kBBoxes = kN / kBox;
-constexpr uint32_t kStageBytes = (kABoxes + kBBoxes) * kBoxBytes;
+constexpr int kBoxes = kHalf / kBox;                  // of an operand in a block
+constexpr uint32_t kStageBytes = 2 * kBoxes * kBoxBytes;
 constexpr int kEpiWarps = 8;
 __host__ __device__ constexpr int chunk_blocks(int mode) { return mode == 2 ? 64 : 4; }
 constexpr int kThreads = (kEpiWarps + 2) * 32;
 constexpr uint32_t kOutBytes = 32 * 128;              // a warp's rows on their way out
-__host__ __device__ constexpr int stages(int mode) { return mode == 1 ? 3 : 4; }
+__host__ __device__ constexpr int stages(int mode) { return mode == 1 ? 4 : 6; }
+__host__ __device__ constexpr int outs(int mode) { return mode == 0 ? 0 : mode == 1 ? 2 : 1; }   // buffers of a warp
 __host__ __device__ constexpr uint32_t smem_bytes(int mode) {
-    return 1024 + stages(mode) * kStageBytes + (mode == 0 ? 0 : kEpiWarps * kOutBytes);
+    return 1024 + stages(mode) * kStageBytes + outs(mode) * kEpiWarps * kOutBytes;
 }
 constexpr uint32_t kTmemCols = 512;
-constexpr int kGrid = 152;                            // one block an SM
+constexpr int kGrid = 152, kPairs = kGrid / 2;        // one block an SM
 constexpr int kMaxGroup = 16;                         // tiles of classes whose statistics one block keeps
 constexpr int kMaxSlabs = 16;
 constexpr int kRowTile = 256;                         // rows of a block of k_xent_rows
@@ -114,17 +117,17 @@ __host__ __device__ inline int piece_classes(int64_t n, int classes, int64_t poo
     return (int)((each + kN - 1) / kN * kN);
 }
 __host__ __device__ inline int group_tiles(int64_t n, int classes) {
-    const int64_t tiles = padded(n) / kM * ((classes + kN - 1) / kN), g = tiles / (8 * kGrid);
+    const int64_t tiles = padded(n) / kM * ((classes + kN - 1) / kN), g = tiles / (8 * kPairs);
     return (int)(g < 1 ? 1 : g > kMaxGroup ? kMaxGroup : g);
 }
 
 // dh has few tiles and a long contraction: it is cut into `slabs`, each with
-// sums of its own, so that no block works longer on one than half of an SM's share
-// of the launch.
+// sums of its own, so that no pair works longer on one than half of its share of
+// the launch.
 __host__ __device__ inline int dh_slabs(int64_t n, int classes, int width, int64_t pool_rows, bool dw) {
     const int64_t blocks = piece_classes(n, classes, pool_rows) / kK, across = (width + kN - 1) / kN;
-    const int64_t tiles = padded(n) / kM * across, others = dw ? blocks / 2 * across * ((n + kK - 1) / kK) : 0;
-    const int64_t share = (tiles * blocks + others) / kGrid / 2 + 1, slabs = (blocks + share - 1) / share;
+    const int64_t tiles = padded(n) / kM * across, others = dw ? blocks / (kM / kK) * across * ((n + kK - 1) / kK) : 0;
+    const int64_t share = (tiles * blocks + others) / kPairs / 2 + 1, slabs = (blocks + share - 1) / share;
     return (int)(slabs < kMaxSlabs ? slabs : kMaxSlabs);
 }
 
@@ -309,21 +312,65 @@ __global__ void __launch_bounds__(kRowTile) k_xent_rows(const RowArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Instruction descriptor: fp32 accumulation, M = 128, both operands T, K- or MN-major.
+// Instruction descriptor: fp32 accumulation, M = 256 over the pair, both operands
+// T (fp16 is format 0, bf16 1), K- or MN-major.
 template <typename T>
 __device__ __forceinline__ uint32_t product(int N, bool a_mn, bool b_mn) {
-    return idesc<T>(N, b_mn) | (a_mn ? 1u << 15 : 0u);
+    const uint32_t f = std::is_same_v<T, __half> ? 0u : 1u;
+    return (1u << 4) | (f << 7) | (f << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
+           ((uint32_t)(N >> 3) << 17) | ((uint32_t)(kM >> 4) << 24);
+}
+// The instructions of a pair of blocks.  The first of the two issues the products;
+// loads of both complete on its barriers, and its commits arrive on both blocks'.
+__device__ __forceinline__ uint32_t pair_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t at_first(const void *p) {    // the same place in the first block's shared memory
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(tc::smem_u32(p)));
+    return a;
+}
+__device__ __forceinline__ void pair_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void pair_mma(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(a), "l"(b), "r"(id), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void pair_commit(uint64_t *bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+                     tc::smem_u32(bar)),
+                 "h"((uint16_t)3)
+                 : "memory");
+}
+__device__ __forceinline__ void pair_alloc(uint32_t *slot, uint32_t cols) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(slot)), "r"(cols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void pair_dealloc(uint32_t tmem, uint32_t cols) {
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
+}
+// one arrival of a warp whose lanes are all done, at a place in either block
+__device__ __forceinline__ void warp_arrive_at(uint32_t bar) {
+    __syncwarp();
+    if (lane_id() == 0) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 // MN-major operand of boxes of 64 columns by 64 rows of the contraction axis
 __device__ __forceinline__ uint64_t desc_boxes(const void *tile) {
     return (tc::desc_k_sw128(tc::smem_u32(tile)) & ~((uint64_t)0x3FFF << 16)) | (uint64_t)(kBoxBytes >> 4) << 16;
 }
 
-__device__ __forceinline__ void load_box(void *dst, const CUtensorMap *map, int x, int y, uint64_t *bar) {
+__device__ __forceinline__ void load_box(void *dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
     asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], "
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], "
         "[%4];" ::"r"(tc::smem_u32(dst)),
-        "l"(map), "r"(x), "r"(y), "r"(tc::smem_u32(bar))
+        "l"(map), "r"(x), "r"(y), "r"(bar)
         : "memory");
 }
 __device__ __forceinline__ void store_box(const CUtensorMap *map, int x, int y, const void *src) {
@@ -338,12 +385,13 @@ __device__ __forceinline__ void add_box(const CUtensorMap *map, int x, int y, co
 }
 __device__ __forceinline__ void stores_issued() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void one_store_read() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
 __device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 // One tile's work.
 struct Tile {
     int m0, n0;          // first row and column of the result
-    int n_boxes;         // of 64 columns
+    int n_boxes;         // of 64 columns, in each block
     int first, blocks;   // stages of the contraction axis
     int slab;            // MODE 2, dh: which sums
     bool dw;             // MODE 2: dW, else dh
@@ -389,7 +437,7 @@ struct Walk {
         if (MODE != 2) {
             t.m0 = i % row_tiles * kM;
             t.n0 = v0 + (i / row_tiles * group + k) * kN;
-            t.n_boxes = kBBoxes;
+            t.n_boxes = kBoxes;
             t.first = t.slab = 0;
             t.blocks = (width + kK - 1) / kK;
             t.dw = false;
@@ -402,7 +450,7 @@ struct Walk {
         i /= across;
         t.n0 = i % d_tiles * kN;
         t.slab = i / d_tiles;
-        t.n_boxes = min(kBBoxes, (width - t.n0 + kBox - 1) / kBox);
+        t.n_boxes = width - t.n0 > kN / 2 ? kBoxes : kBoxes / 2;
         t.first = t.slab * slab_blocks;
         t.blocks = t.dw ? (n + kK - 1) / kK : max(0, min(slab_blocks, (v1 - v0 + kK - 1) / kK - t.first));
         return t;
@@ -410,7 +458,7 @@ struct Walk {
 };
 
 template <typename T, int MODE, bool BIAS>
-__global__ void __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ XentArgs a, int piece) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ XentArgs a, int piece) {
     constexpr int kStages = stages(MODE), kChunk = chunk_blocks(MODE);
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t full[kStages], empty[kStages], d_full[2], d_empty[2], drained;
@@ -429,16 +477,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ Xe
         }
         for (int b = 0; b < 2; ++b) {
             tc::mbar_init(&d_full[b], 1);
-            tc::mbar_init(&d_empty[b], kEpiWarps);
+            tc::mbar_init(&d_empty[b], 2 * kEpiWarps);
         }
         tc::mbar_init(&drained, 1);
         s_abort = 0;
         tc::mbar_init_fence();
     }
-    if (warp == 0) tc::tmem_alloc(&tmem_slot, kTmemCols);
+    __syncwarp();
+    if (warp == 0) pair_alloc(&tmem_slot, kTmemCols);
     tc::fence_before_sync();
     __syncthreads();
+    pair_sync();
     tc::fence_after_sync();
+    const int rank = (int)pair_rank(), pair = blockIdx.x / 2, pairs = gridDim.x / 2;
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
     const Waiter wait{&s_abort};
     const bool all = a.ctl->all, same = a.ctl->same;
@@ -448,7 +499,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ Xe
         const CUtensorMap *rows = MODE == 2 && !same ? &a.hs : all ? &a.h : &a.hc;
         int s = 0;
         bool ok = true;
-        for (int i = blockIdx.x; ok && i < walk.total; i += gridDim.x)
+        for (int i = pair; ok && i < walk.total; i += pairs)
             for (int k = 0, nk = walk.tiles(i); ok && k < nk; ++k) {
                 const Tile t = walk.tile(i, k);
 #pragma unroll 1
@@ -456,37 +507,39 @@ __global__ void __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ Xe
                     const int st = s % kStages;
                     if (!(ok = wait.warp(&empty[st], ((uint32_t)(s / kStages) & 1u) ^ 1u))) break;
                     if (elected()) {
-                        unsigned char *pa = base + st * kStageBytes, *pb = pa + kABoxes * kBoxBytes;
-                        expect(&full[st], (kABoxes + t.n_boxes) * kBoxBytes);
+                        unsigned char *pa = base + st * kStageBytes, *pb = pa + kBoxes * kBoxBytes;
+                        const uint32_t bar = at_first(&full[st]);
+                        if (rank == 0) expect(&full[st], 2 * (kBoxes + t.n_boxes) * kBoxBytes);
+                        const int m = t.m0 + rank * kHalf, n = t.n0 + rank * t.n_boxes * kBox;
 #pragma unroll
-                        for (int j = 0; j < kABoxes; ++j) {
+                        for (int j = 0; j < kBoxes; ++j) {
                             void *dst = pa + j * kBoxBytes;
-                            if (MODE != 2) load_box(dst, rows, b * kK, t.m0 + j * kBox, &full[st]);
-                            else if (t.dw) load_box(dst, &a.pool_in, 0, (t.m0 / kBox + j) * walk.mp + b * kK, &full[st]);
-                            else load_box(dst, &a.pool_in, 0, (t.first + b) * walk.mp + t.m0 + j * kBox, &full[st]);
+                            if (MODE != 2) load_box(dst, rows, b * kK, m + j * kBox, bar);
+                            else if (t.dw) load_box(dst, &a.pool_in, 0, (m / kBox + j) * walk.mp + b * kK, bar);
+                            else load_box(dst, &a.pool_in, 0, (t.first + b) * walk.mp + m + j * kBox, bar);
                         }
                         for (int j = 0; j < t.n_boxes; ++j) {
                             void *dst = pb + j * kBoxBytes;
-                            if (MODE != 2) load_box(dst, &a.w, b * kK, t.n0 + j * kBox, &full[st]);
-                            else if (t.dw) load_box(dst, rows, t.n0 + j * kBox, b * kK, &full[st]);
-                            else load_box(dst, &a.w, t.n0 + j * kBox, walk.v0 + (t.first + b) * kK, &full[st]);
+                            if (MODE != 2) load_box(dst, &a.w, b * kK, n + j * kBox, bar);
+                            else if (t.dw) load_box(dst, rows, n + j * kBox, b * kK, bar);
+                            else load_box(dst, &a.w, n + j * kBox, walk.v0 + (t.first + b) * kK, bar);
                         }
                     }
                     __syncwarp();
                 }
             }
-        if (!ok)      // after an abort: what is in flight lands before the block ends
+        if (!ok && rank == 0)      // after an abort: what is in flight (of both) lands before the blocks end
             for (int j = max(0, s - kStages); j < s; ++j) let_land(&full[j % kStages], (uint32_t)(j / kStages) & 1u);
         __syncwarp();
     } else if (warp == kEpiWarps + 1) {
         // ---------------- products ----------------
         int s = 0, c = 0;
         bool ok = true;
-        for (int i = blockIdx.x; ok && i < walk.total; i += gridDim.x)
+        for (int i = pair; rank == 0 && ok && i < walk.total; i += pairs)
             for (int k = 0, nk = walk.tiles(i); ok && k < nk; ++k) {
                 const Tile t = walk.tile(i, k);
                 const bool a_mn = MODE == 2 && t.dw, b_mn = MODE == 2;
-                const uint32_t id = product<T>(t.n_boxes * kBox, a_mn, b_mn);
+                const uint32_t id = product<T>(2 * t.n_boxes * kBox, a_mn, b_mn);
                 const uint64_t step_a = a_mn ? 128 : 2, step_b = b_mn ? 128 : 2;
 #pragma unroll 1
                 for (int b = 0; b < t.blocks; ++b, ++s) {
@@ -497,32 +550,34 @@ __global__ void __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ Xe
                     if (!(ok = wait.warp(&full[st], (uint32_t)(s / kStages) & 1u))) break;
                     tc::fence_after_sync();
                     if (elected()) {
-                        const unsigned char *pa = base + st * kStageBytes, *pb = pa + kABoxes * kBoxBytes;
+                        const unsigned char *pa = base + st * kStageBytes, *pb = pa + kBoxes * kBoxBytes;
                         const uint64_t da = a_mn ? desc_boxes(pa) : desc_k(pa), db = b_mn ? desc_boxes(pb) : desc_k(pb);
 #pragma unroll
                         for (int x = 0; x < kK / 16; ++x)
-                            mma_ss(d, da + x * step_a, db + x * step_b, id, b % kChunk > 0 || x > 0);
-                        commit(&empty[st]);
-                        if (b % kChunk == kChunk - 1 || b + 1 == t.blocks) commit(&d_full[buf]);
+                            pair_mma(d, da + x * step_a, db + x * step_b, id, b % kChunk > 0 || x > 0);
+                        pair_commit(&empty[st]);
+                        if (b % kChunk == kChunk - 1 || b + 1 == t.blocks) pair_commit(&d_full[buf]);
                     }
                     __syncwarp();
                     if (b % kChunk == kChunk - 1 || b + 1 == t.blocks) ++c;
                 }
             }
         // every product issued ends before the block frees its memory
-        if (elected()) commit(&drained);
+        if (rank == 0 && elected()) pair_commit(&drained);
         __syncwarp();
         let_land(&drained, 0);
         __syncwarp();
     } else {
         // ---------------- what becomes of a tile ----------------
-        const int quarter = warp & 3, half = warp >> 2, r = quarter * 32 + lane;
+        const int quarter = warp & 3, half = warp >> 2, r_warp = rank * kHalf + quarter * 32, r = r_warp + lane;
+        const uint32_t released = at_first(&d_empty[0]);
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
-        unsigned char *out = base + kStages * kStageBytes + warp * kOutBytes;
+        unsigned char *const outs_at = base + kStages * kStageBytes + warp * outs(MODE) * kOutBytes;
+        unsigned char *out = outs_at;
         const float factor = MODE == 2 ? a.ctl->factor * a.scale / kUp<T> : 0.f;
         int c = 0;
         bool ok = true;
-        for (int i = blockIdx.x; ok && i < walk.total; i += gridDim.x) {
+        for (int i = pair; ok && i < walk.total; i += pairs) {
             float top = -INFINITY, sum = 0.f, lse = 0.f, dloss = 0.f, part = 0.f;
             int target = -1, row = 0;
             bool live = false;
@@ -568,7 +623,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ Xe
                             acc[j / 2 + e] = add2(make_float2(x[2 * e], x[2 * e + 1]), acc[j / 2 + e]);
                     }
                     tc::fence_before_sync();
-                    warp_arrive(&d_empty[c & 1]);
+                    warp_arrive_at(released + (c & 1) * 8);
                 }
                 if (!ok) break;
                 auto take = [&](int j, float (&x)[32]) {
@@ -664,10 +719,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ Xe
                                     }
                                 }
                                 if (first + lane < a.classes)
-                                    a.colsum[((int64_t)t.m0 / 32 + quarter) * a.classes + first + lane] = x[0];
+                                    a.colsum[(int64_t)((t.m0 + r_warp) / 32) * a.classes + first + lane] = x[0];
                             }
                         }
-                        stores_read();
+                        out = outs_at + j / 64 * kOutBytes;
+                        one_store_read();      // the one from this buffer, but not the last
                         __syncwarp();
 #pragma unroll
                         for (int e = 0; e < 8; ++e)
@@ -676,14 +732,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ Xe
                         tc::fence_proxy_async_smem();
                         __syncwarp();
                         if (lane == 0) {
-                            store_box(&a.pool_out, 0, (col + j - walk.v0) / kK * walk.mp + t.m0 + quarter * 32, out);
+                            store_box(&a.pool_out, 0, (col + j - walk.v0) / kK * walk.mp + t.m0 + r_warp, out);
                             stores_issued();
                         }
                     }
                     if (live) a.rest[(int64_t)(t.n0 / kN * 2 + half) * walk.mp + row] = (rest[0].x + rest[0].y) + (rest[1].x + rest[1].y);
                 } else {
-                    const int columns = t.n_boxes * kBox;        // of the tile that exist
-                    const int r0 = (t.dw ? walk.v0 : t.slab * walk.mp) + t.m0 + quarter * 32;
+                    const int columns = 2 * t.n_boxes * kBox;    // of the tile that exist
+                    const int r0 = (t.dw ? walk.v0 : t.slab * walk.mp) + t.m0 + r_warp;
                     const bool some = t.dw ? r0 < walk.v1 : true;
                     const bool wide = !t.dw || a.dw_f32;         // fp32 results: 32 columns to a box, else 64
                     const bool adds = t.dw ? a.accumulate : piece > 0;
@@ -729,7 +785,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ Xe
                                     make_uint4(packed[4 * e], packed[4 * e + 1], packed[4 * e + 2], packed[4 * e + 3]);
                             tc::fence_proxy_async_smem();
                             __syncwarp();
-                            if (lane == 0 && some) {
+                            if (lane == 0 && some && x0 < a.width) {
                                 store_box(map, x0, r0, out);
                                 stores_issued();
                             }
@@ -744,10 +800,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ Xe
     }
     tc::fence_before_sync();
     __syncthreads();
-    if (warp == 0) {
-        tc::fence_after_sync();
-        tc::tmem_dealloc(tmem, kTmemCols);
-    }
+    pair_sync();          // neither leaves while the other's copies, products or arrivals may reach it
+    tc::fence_after_sync();
+    if (warp == 0) pair_dealloc(tmem, kTmemCols);
     if (threadIdx.x == 0 && s_abort) atomicExch(&a.ctl->status, SIEVE_ETIMEOUT);
 }
 
@@ -901,8 +956,8 @@ Layout layout(const sieve_cross_entropy_args &a, bool backward) {
     l.hc = take(n * a.width * 2);
     if (!backward) {
         const int64_t row_tiles = np / kM, class_tiles = ceil_div(a.classes, kN);
-        // (group_tiles: up to 16 tiles a part, and no fewer than 8 parts a block before that)
-        const int64_t whole = ceil_div(row_tiles * class_tiles, kMaxGroup), parts = (whole > 16 * kGrid ? whole : 16 * kGrid) + row_tiles;
+        // (group_tiles: up to 16 tiles a part, and no fewer than 8 parts a pair before that)
+        const int64_t whole = ceil_div(row_tiles * class_tiles, kMaxGroup), parts = (whole > 16 * kPairs ? whole : 16 * kPairs) + row_tiles;
         l.hit = take(n * 4);
         l.part = take((parts < row_tiles * class_tiles ? parts : row_tiles * class_tiles) * 2 * kM * 8);
     } else {
@@ -917,8 +972,8 @@ Layout layout(const sieve_cross_entropy_args &a, bool backward) {
         const int64_t needed = np * (round_up(a.classes, kN) / kK), least = np * (kN / kK), most = kPoolBytes / 128;
         l.pool_rows = needed < most ? needed : least > most ? least : most;
         l.pool = take(l.pool_rows * 128);
-        // (dh_slabs: tiles times slabs stay below two shares for each SM, or there is one slab)
-        const int64_t across = ceil_div(a.width, kN), some = 2 * kGrid / across + 1;
+        // (dh_slabs: tiles times slabs stay below two shares for each pair, or there is one slab)
+        const int64_t across = ceil_div(a.width, kN), some = 2 * kPairs / across + 1;
         const int64_t most_slabs = np / kM * kMaxSlabs < np / kM + some ? np / kM * kMaxSlabs : np / kM + some;
         l.acc_rows = most_slabs * kM;
         l.acc = take(l.acc_rows * a.width * 4);
