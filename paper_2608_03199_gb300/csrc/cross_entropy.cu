@@ -356,10 +356,13 @@ __device__ __forceinline__ void pair_alloc(uint32_t *slot, uint32_t cols) {
 __device__ __forceinline__ void pair_dealloc(uint32_t tmem, uint32_t cols) {
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
 }
-// one arrival of a warp whose lanes are all done, at a place in either block
+// One arrival of a warp whose lanes are all done, at a place in either block.  What
+// it hands over is tensor memory, which the tcgen05 fences order; a release to
+// the cluster would wait for every store of the warp besides (4,099 x 32,800 x 256
+// forward: 75 us with it).
 __device__ __forceinline__ void warp_arrive_at(uint32_t bar) {
     __syncwarp();
-    if (lane_id() == 0) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    if (lane_id() == 0) asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 // MN-major operand of boxes of 64 columns by 64 rows of the contraction axis
 __device__ __forceinline__ uint64_t desc_boxes(const void *tile) {
@@ -606,21 +609,34 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                 }
                 // The tile's sums: its chunks added up, each released as soon as it is
                 // in registers, so that the next tile's products run under what follows.
-                float2 acc[kN / 4];
+                uint32_t acc[kN / 64][32];
 #pragma unroll
-                for (int e = 0; e < kN / 4; ++e) acc[e] = make_float2(0.f, 0.f);
+                for (int j = 0; j < kN / 64; ++j)
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) acc[j][e] = 0u;
 #pragma unroll 1
                 for (int b = 0; b < t.blocks; b += kChunk, ++c) {
                     if (!(ok = wait.warp(&d_full[c & 1], (uint32_t)(c >> 1) & 1u))) break;
                     tc::fence_after_sync();
                     const uint32_t from = lanes + (c & 1) * kN + half * (kN / 2);
+                    if (MODE == 0 && b == 0) {        // (in the others it costs registers that they lack)
 #pragma unroll
-                    for (int j = 0; j < kN / 2; j += 32) {
-                        float x[32];
-                        tc::tmem_ld32(from + j, x);
+                        for (int j = 0; j < kN / 64; ++j) tc::tmem_ld32_issue(from + 32 * j, acc[j]);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            acc[j / 2 + e] = add2(make_float2(x[2 * e], x[2 * e + 1]), acc[j / 2 + e]);
+                        for (int j = 0; j < kN / 64; ++j) tc::tmem_ld_wait(acc[j]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < kN / 64; ++j) {
+                            float x[32];
+                            tc::tmem_ld32(from + 32 * j, x);
+#pragma unroll
+                            for (int e = 0; e < 32; e += 2) {
+                                const float2 v = add2(make_float2(x[e], x[e + 1]),
+                                                      make_float2(__uint_as_float(acc[j][e]), __uint_as_float(acc[j][e + 1])));
+                                acc[j][e] = __float_as_uint(v.x);
+                                acc[j][e + 1] = __float_as_uint(v.y);
+                            }
+                        }
                     }
                     tc::fence_before_sync();
                     warp_arrive_at(released + (c & 1) * 8);
@@ -628,10 +644,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                 if (!ok) break;
                 auto take = [&](int j, float (&x)[32]) {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        x[2 * e] = acc[j / 2 + e].x;
-                        x[2 * e + 1] = acc[j / 2 + e].y;
-                    }
+                    for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(acc[j / 32][e]);
                 };
                 if constexpr (MODE == 0) {
 #pragma unroll
