@@ -61,7 +61,11 @@ constexpr int kBoxes = kHalf / kBox;                  // of an operand in a bloc
 constexpr uint32_t kStageBytes = 2 * kBoxes * kBoxBytes;
 constexpr int kEpiWarps = 8;
 __host__ __device__ constexpr int chunk_blocks(int mode) { return mode == 2 ? 64 : 4; }
-constexpr int kThreads = (kEpiWarps + 2) * 32;
+// Registers: 384 threads start with 168 each, 64,512 in all.  The eight warps that
+// hold a tile's sums take 232, the four others (two of them idle) keep 40.
+constexpr int kThreads = (kEpiWarps + 4) * 32;
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 232;"); }
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 40;"); }
 constexpr uint32_t kOutBytes = 32 * 128;              // a warp's rows on their way out
 __host__ __device__ constexpr int stages(int mode) { return mode == 1 ? 4 : 6; }
 __host__ __device__ constexpr int outs(int mode) { return mode == 0 ? 0 : mode == 1 ? 2 : 1; }   // buffers of a warp
@@ -87,7 +91,7 @@ struct XentArgs {
     CUtensorMap h, hc, hs, w, pool_in, pool_out, acc, dw;
     Ctl *ctl;
     const int *target;                    // of the list
-    const float *lse, *loss, *dloss, *part_of;   // of the list (part_of: m, or 1)
+    const float *lse, *at_target, *dloss, *part_of;   // of the list (q at the target; m, or 1)
     const float *bias;
     float *hit;                           // [rows] the target's score
     float2 *part;                         // [parts][rows of the list, padded] maximum and sum
@@ -102,11 +106,18 @@ struct XentArgs {
 template <typename T>
 constexpr float kUp = std::is_same_v<T, __half> ? 16384.f : 1.f;
 
-// two rounded values of a packed pair, added to a sum
+// two rounded values of a packed pair, added to two sums
 template <typename T>
 __device__ __forceinline__ float2 add_pair(float2 sum, uint32_t pair) {
-    if constexpr (std::is_same_v<T, __half>) return add2(sum, __half22float2(*reinterpret_cast<const __half2 *>(&pair)));
-    else return add2(sum, make_float2(__uint_as_float(pair << 16), __uint_as_float(pair & 0xffff0000u)));
+    if constexpr (std::is_same_v<T, __half>)
+        asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tadd.f32.f16 %0, lo, %0;\n\tadd.f32.f16 %1, hi, %1;\n\t}"
+            : "+f"(sum.x), "+f"(sum.y)
+            : "r"(pair));
+    else
+        asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tadd.f32.bf16 %0, lo, %0;\n\tadd.f32.bf16 %1, hi, %1;\n\t}"
+            : "+f"(sum.x), "+f"(sum.y)
+            : "r"(pair));
+    return sum;
 }
 
 // classes of a piece, and how the forward pass groups its tiles
@@ -144,7 +155,7 @@ struct RowArgs {
     int *count;                           // [blocks]
     uint32_t *top, *low;                  // [blocks] largest dloss, and its lowest, as ordered keys
     int *row, *target;
-    float *dloss_c, *loss_c, *lse_c, *part_c, *whole_c;   // part_c whole_c = dloss
+    float *dloss_c, *at_target_c, *lse_c, *part_c, *whole_c;   // part_c whole_c = dloss
     void *hc, *hs;
 };
 
@@ -261,7 +272,7 @@ __global__ void __launch_bounds__(kRowTile) k_xent_rows(const RowArgs a) {
             a.dloss_c[at] = v;
             a.part_c[at] = same ? 1.f : m;
             a.whole_c[at] = same ? v : ldexpf(1.f, e);
-            a.loss_c[at] = a.loss[r];
+            a.at_target_c[at] = expm1f(-a.loss[r]);
             a.lse_c[at] = a.lse[r];
         }
     } else if (r < a.rows && a.loss_out) {
@@ -391,6 +402,12 @@ __device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait
 __device__ __forceinline__ void one_store_read() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
 __device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
+__device__ __forceinline__ float2 get(const float *p) { return make_float2(p[0], p[1]); }
+__device__ __forceinline__ void put(float *p, float2 v) {
+    p[0] = v.x;
+    p[1] = v.y;
+}
+
 // One tile's work.
 struct Tile {
     int m0, n0;          // first row and column of the result
@@ -499,6 +516,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
 
     if (warp == kEpiWarps) {
         // ---------------- loads ----------------
+        fewer_registers();
         const CUtensorMap *rows = MODE == 2 && !same ? &a.hs : all ? &a.h : &a.hc;
         int s = 0;
         bool ok = true;
@@ -536,6 +554,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
         __syncwarp();
     } else if (warp == kEpiWarps + 1) {
         // ---------------- products ----------------
+        fewer_registers();
         int s = 0, c = 0;
         bool ok = true;
         for (int i = pair; rank == 0 && ok && i < walk.total; i += pairs)
@@ -570,8 +589,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
         __syncwarp();
         let_land(&drained, 0);
         __syncwarp();
+    } else if (warp > kEpiWarps) {
+        fewer_registers();
     } else {
         // ---------------- what becomes of a tile ----------------
+        more_registers();
         const int quarter = warp & 3, half = warp >> 2, r_warp = rank * kHalf + quarter * 32, r = r_warp + lane;
         const uint32_t released = at_first(&d_empty[0]);
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
@@ -581,7 +603,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
         int c = 0;
         bool ok = true;
         for (int i = pair; ok && i < walk.total; i += pairs) {
-            float top = -INFINITY, sum = 0.f, lse = 0.f, dloss = 0.f, part = 0.f;
+            float top = -INFINITY, sum = 0.f, lse = INFINITY, dloss = 0.f, part = 0.f, q_target = 0.f;
             int target = -1, row = 0;
             bool live = false;
             if (MODE != 2) {
@@ -590,10 +612,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                 if (live) target = a.target[row];
                 if (MODE == 1 && live) {
                     lse = a.lse[row];
-                    if (lse == -INFINITY) lse = INFINITY;       // every class hidden: no probabilities
+                    if (lse == -INFINITY) lse = INFINITY;       // every class hidden: no probabilities either
                     if (!BIAS) lse *= kLog2e;
                     dloss = a.dloss[row];
                     part = a.part_of[row] * kUp<T>;
+                    q_target = a.at_target[row];
                 }
             }
             for (int k = 0, nk = walk.tiles(i); ok && k < nk; ++k) {
@@ -610,16 +633,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                 // The tile's sums: its chunks added up, each released as soon as it is
                 // in registers, so that the next tile's products run under what follows.
                 uint32_t acc[kN / 64][32];
-#pragma unroll
-                for (int j = 0; j < kN / 64; ++j)
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) acc[j][e] = 0u;
-#pragma unroll 1
-                for (int b = 0; b < t.blocks; b += kChunk, ++c) {
-                    if (!(ok = wait.warp(&d_full[c & 1], (uint32_t)(c >> 1) & 1u))) break;
+                auto chunk = [&](bool first) {
+                    if (!(ok = wait.warp(&d_full[c & 1], (uint32_t)(c >> 1) & 1u))) return;
                     tc::fence_after_sync();
                     const uint32_t from = lanes + (c & 1) * kN + half * (kN / 2);
-                    if (MODE == 0 && b == 0) {        // (in the others it costs registers that they lack)
+                    if (first) {
 #pragma unroll
                         for (int j = 0; j < kN / 64; ++j) tc::tmem_ld32_issue(from + 32 * j, acc[j]);
 #pragma unroll
@@ -631,8 +649,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                             tc::tmem_ld32(from + 32 * j, x);
 #pragma unroll
                             for (int e = 0; e < 32; e += 2) {
-                                const float2 v = add2(make_float2(x[e], x[e + 1]),
-                                                      make_float2(__uint_as_float(acc[j][e]), __uint_as_float(acc[j][e + 1])));
+                                const float2 v = add2(get(x + e), make_float2(__uint_as_float(acc[j][e]), __uint_as_float(acc[j][e + 1])));
                                 acc[j][e] = __float_as_uint(v.x);
                                 acc[j][e + 1] = __float_as_uint(v.y);
                             }
@@ -640,108 +657,152 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                     }
                     tc::fence_before_sync();
                     warp_arrive_at(released + (c & 1) * 8);
+                    ++c;
+                };
+                if (MODE != 2) {
+                    chunk(true);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kN / 64; ++j)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) acc[j][e] = 0u;
                 }
+#pragma unroll 1
+                for (int b = MODE != 2 ? kChunk : 0; ok && b < t.blocks; b += kChunk) chunk(false);
                 if (!ok) break;
                 auto take = [&](int j, float (&x)[32]) {
 #pragma unroll
                     for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(acc[j / 32][e]);
                 };
+                const float *bias = s_bias[warp];
+                // whether a row's target is among these columns, or the classes end there
+                // (rows past the list: lse = inf, so their probabilities are zero)
+                const int at0 = target >= 0 ? target - col : -1, left0 = a.classes - col;
+                const bool hits = MODE == 0 && __any_sync(0xffffffffu, at0 >= 0 && at0 < kN / 2);
+                const bool ends = MODE != 2 && left0 < kN / 2;
                 if constexpr (MODE == 0) {
 #pragma unroll
                     for (int j = 0; j < kN / 2; j += 32) {
                         float x[32];
                         take(j, x);
-                        if constexpr (BIAS) {
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) x[e] = fmaf(x[e], a.scale, s_bias[warp][j + e]);
-                        } else {
+                        for (int e = 0; e < 32; e += 2)
+                            put(x + e, BIAS ? fma2(get(x + e), both(a.scale), get(bias + j + e)) : mul2(get(x + e), both(a.c)));
+                        if (!BIAS && ends)
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) x[e] *= a.c;
-                            const int left = a.classes - col - j;
-                            if (left < 32)
-#pragma unroll
-                                for (int e = 0; e < 32; ++e) x[e] = e < left ? x[e] : -INFINITY;
-                        }
-                        const int at = target - col - j;
-                        if (__any_sync(0xffffffffu, at >= 0 && at < 32)) {
+                            for (int e = 0; e < 32; ++e) x[e] = j + e < left0 ? x[e] : -INFINITY;
+                        const bool here = at0 >= j && at0 < j + 32;
+                        if (hits && __any_sync(0xffffffffu, here)) {
                             float hit = 0.f;
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
-                                if (e == at) {
+                                if (j + e == at0) {
                                     hit = x[e];
                                     x[e] = -INFINITY;
                                 }
-                            if (at >= 0 && at < 32) a.hit[row] = hit;
+                            if (here) a.hit[row] = hit;
                         }
                         const float high = fmaxf(top, max_of_32(x)), from = high == -INFINITY ? 0.f : high;
                         constexpr float unit = BIAS ? kLog2e : 1.f;
-                        float s0 = sum * exp2_approx((top - from) * unit), s1 = 0.f, s2 = 0.f, s3 = 0.f;
+                        float2 s0 = make_float2(sum * exp2_approx((top - from) * unit), 0.f), s1 = make_float2(0.f, 0.f);
 #pragma unroll
                         for (int e = 0; e < 32; e += 4) {
-                            s0 += exp2_approx((x[e] - from) * unit);
-                            s1 += exp2_approx((x[e + 1] - from) * unit);
-                            s2 += exp2_approx((x[e + 2] - from) * unit);
-                            s3 += exp2_approx((x[e + 3] - from) * unit);
+                            float2 u = add2(get(x + e), both(-from)), v = add2(get(x + e + 2), both(-from));
+                            if (BIAS) {
+                                u = mul2(u, both(unit));
+                                v = mul2(v, both(unit));
+                            }
+                            s0 = add2(s0, make_float2(exp2_approx(u.x), exp2_approx(u.y)));
+                            s1 = add2(s1, make_float2(exp2_approx(v.x), exp2_approx(v.y)));
                         }
-                        sum = (s0 + s1) + (s2 + s3);
+                        s0 = add2(s0, s1);
+                        sum = s0.x + s0.y;
                         top = high;
                     }
                 } else if constexpr (MODE == 1) {
-                    float2 rest[2] = {};
+                    float2 rest = make_float2(0.f, 0.f);
 #pragma unroll
                     for (int j = 0; j < kN / 2; j += 64) {
                         uint32_t packed[32];
-#pragma unroll
-                        for (int jj = 0; jj < 64; jj += 32) {
-                            float x[32];
-                            take(j + jj, x);
-                            const int first = col + j + jj;
-#pragma unroll
-                            for (int e = 0; e < 32; ++e)
-                                x[e] = BIAS ? exp2_approx((fmaf(x[e], a.scale, s_bias[warp][j + jj + e]) - lse) * kLog2e)
-                                            : exp2_approx(fmaf(x[e], a.c, -lse));
-                            const int at = target - first;
-                            if (__any_sync(0xffffffffu, at >= 0 && at < 32)) {
-                                const float q = at >= 0 && at < 32 ? expm1f(-a.loss[row]) : 0.f;
-#pragma unroll
-                                for (int e = 0; e < 32; ++e)
-                                    if (e == at) x[e] = q;
-                            }
-                            // nothing past the list or the classes
-                            const int left = live ? a.classes - first : 0;
-                            if (__any_sync(0xffffffffu, left < 32))
-#pragma unroll
-                                for (int e = 0; e < 32; ++e) x[e] = e < left ? x[e] : 0.f;
-#pragma unroll
-                            for (int e = 0; e < 32; e += 2)
-                                packed[(jj + e) / 2] = pack2<T>(x[e] * part, x[e + 1] * part);
-#pragma unroll
-                            for (int e = 0; e < 32; e += 2)
-                                rest[e / 2 % 2] = add_pair<T>(rest[e / 2 % 2], packed[(jj + e) / 2]);
-                            if (BIAS && a.want_db) {
-                                // the columns' sums over the warp's rows: lane e ends with column e
-#pragma unroll
-                                for (int e = 0; e < 32; ++e) x[e] = live ? x[e] * dloss : 0.f;
-#pragma unroll
-                                for (int w = 16; w; w >>= 1) {
-                                    const bool up = lane & w;
-#pragma unroll
-                                    for (int e = 0; e < w; ++e) {
-                                        const float keep = up ? x[e + w] : x[e], give = up ? x[e] : x[e + w];
-                                        x[e] = keep + __shfl_xor_sync(0xffffffffu, give, w);
-                                    }
-                                }
-                                if (first + lane < a.classes)
-                                    a.colsum[(int64_t)((t.m0 + r_warp) / 32) * a.classes + first + lane] = x[0];
-                            }
-                        }
+                        float2 some = make_float2(0.f, 0.f);      // of these columns
                         out = outs_at + j / 64 * kOutBytes;
                         one_store_read();      // the one from this buffer, but not the last
                         __syncwarp();
 #pragma unroll
+                        for (int jj = 0; jj < 64; jj += 32) {
+                            float x[32];
+                            take(j + jj, x);
+#pragma unroll
+                            for (int e = 0; e < 32; e += 2) {
+                                float2 u;
+                                if (BIAS)
+                                    u = mul2(add2(fma2(get(x + e), both(a.scale), get(bias + j + jj + e)), both(-lse)), both(kLog2e));
+                                else
+                                    u = fma2(get(x + e), both(a.c), both(-lse));
+                                x[e] = exp2_approx(u.x);
+                                x[e + 1] = exp2_approx(u.y);
+                            }
+                            if (!BIAS && ends)      // (a bias ends in -inf)
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) x[e] = j + jj + e < left0 ? x[e] : 0.f;
+#pragma unroll
+                            for (int e = 0; e < 32; e += 2) {
+                                const float2 q = mul2(get(x + e), both(part));
+                                packed[(jj + e) / 2] = pack2<T>(q.x, q.y);
+                                some = add_pair<T>(some, packed[(jj + e) / 2]);
+                            }
+                            if (BIAS && a.want_db) {
+                                // The columns' sums over the warp's rows, turned in the buffer that
+                                // the packed values leave from later: a lane takes four columns of eight
+                                // rows.  (In registers alone, 31 shuffles and twice as many selects.)
+                                const float2 d = both(live ? dloss : 0.f);
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) {
+                                    const float2 u = mul2(get(x + 4 * e), d), v = mul2(get(x + 4 * e + 2), d);
+                                    *reinterpret_cast<float4 *>(out + lane * 128 + ((e ^ (lane & 7)) << 4)) = make_float4(u.x, u.y, v.x, v.y);
+                                }
+                                if (at0 >= j + jj && at0 < j + jj + 32) {
+                                    const int e = at0 - j - jj;
+                                    *reinterpret_cast<float *>(out + lane * 128 + (((e >> 2) ^ (lane & 7)) << 4) + (e & 3) * 4) =
+                                        q_target * dloss;
+                                }
+                                __syncwarp();
+                                float2 u = make_float2(0.f, 0.f), v = u;
+#pragma unroll
+                                for (int k = 0; k < 8; ++k) {
+                                    const float4 f = *reinterpret_cast<const float4 *>(out + ((lane & 24) + k) * 128 + (((lane & 7) ^ k) << 4));
+                                    u = add2(u, make_float2(f.x, f.y));
+                                    v = add2(v, make_float2(f.z, f.w));
+                                }
+#pragma unroll
+                                for (int w = 8; w <= 16; w <<= 1) {
+                                    u = add2(u, make_float2(__shfl_xor_sync(0xffffffffu, u.x, w), __shfl_xor_sync(0xffffffffu, u.y, w)));
+                                    v = add2(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, w), __shfl_xor_sync(0xffffffffu, v.y, w)));
+                                }
+                                const int at = col + j + jj + 4 * (lane & 7) + (lane >> 3);
+                                const float mine = lane & 16 ? (lane & 8 ? v.y : v.x) : (lane & 8 ? u.y : u.x);
+                                if (at < a.classes) a.colsum[(int64_t)((t.m0 + r_warp) / 32) * a.classes + at] = mine;
+                                __syncwarp();
+                            }
+                        }
+#pragma unroll
                         for (int e = 0; e < 8; ++e)
                             *reinterpret_cast<uint4 *>(out + lane * 128 + ((e ^ (lane & 7)) << 4)) =
                                 make_uint4(packed[4 * e], packed[4 * e + 1], packed[4 * e + 2], packed[4 * e + 3]);
+                        // The target's goes to its place here: nearly every tile has some row's, and
+                        // a choice at every element of it cost half as long again.  Such a
+                        // row is added up anew: p near 1 must not leave its rounding in the sum.
+                        if (at0 >= j && at0 < j + 64) {
+                            const int e = at0 - j;
+                            reinterpret_cast<T *>(out + lane * 128 + (((e >> 3) ^ (lane & 7)) << 4))[e & 7] = from_f32<T>(q_target * part);
+                            some = make_float2(0.f, 0.f);
+#pragma unroll 1
+                            for (int c8 = 0; c8 < 8; ++c8) {
+                                const uint4 v = *reinterpret_cast<const uint4 *>(out + lane * 128 + (c8 << 4));
+                                some = add_pair<T>(add_pair<T>(add_pair<T>(add_pair<T>(some, v.x), v.y), v.z), v.w);
+                            }
+                        }
+                        rest = add2(rest, some);
                         tc::fence_proxy_async_smem();
                         __syncwarp();
                         if (lane == 0) {
@@ -749,7 +810,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                             stores_issued();
                         }
                     }
-                    if (live) a.rest[(int64_t)(t.n0 / kN * 2 + half) * walk.mp + row] = (rest[0].x + rest[0].y) + (rest[1].x + rest[1].y);
+                    if (live) a.rest[(int64_t)(t.n0 / kN * 2 + half) * walk.mp + row] = rest.x + rest.y;
                 } else {
                     const int columns = 2 * t.n_boxes * kBox;    // of the tile that exist
                     const int r0 = (t.dw ? walk.v0 : t.slab * walk.mp) + t.m0 + r_warp;
@@ -951,7 +1012,7 @@ __global__ void __launch_bounds__(256) k_xent_db(const Ctl *ctl, const float *co
 
 // ---------------------------------------------------------------------------
 struct Layout {
-    size_t count, top, low, row, target, dloss, loss, lse, hc, hs, hit, part, part_of, whole, pool, acc, rest, colsum, bytes;
+    size_t count, top, low, row, target, dloss, at_target, lse, hc, hs, hit, part, part_of, whole, pool, acc, rest, colsum, bytes;
     int64_t pool_rows, acc_rows;
 };
 Layout layout(const sieve_cross_entropy_args &a, bool backward) {
@@ -977,7 +1038,7 @@ Layout layout(const sieve_cross_entropy_args &a, bool backward) {
         l.top = take(blocks * 4);
         l.low = take(blocks * 4);
         l.dloss = take(n * 4);
-        l.loss = take(n * 4);
+        l.at_target = take(n * 4);
         l.lse = take(n * 4);
         l.part_of = take(n * 4);
         l.whole = take(n * 4);
@@ -1100,7 +1161,7 @@ sieve_status launch_cross_entropy_backward(const sieve_cross_entropy_args &a, co
     sieve_status rc = prepare(c, a, l, base);
     if (rc != SIEVE_OK) return rc;
     c.x.lse = reinterpret_cast<float *>(base + l.lse);
-    c.x.loss = reinterpret_cast<float *>(base + l.loss);
+    c.x.at_target = reinterpret_cast<float *>(base + l.at_target);
     c.x.dloss = reinterpret_cast<float *>(base + l.dloss);
     c.x.colsum = reinterpret_cast<float *>(base + l.colsum);
     c.x.rest = reinterpret_cast<float *>(base + l.rest);
@@ -1118,7 +1179,7 @@ sieve_status launch_cross_entropy_backward(const sieve_cross_entropy_args &a, co
     c.r.top = reinterpret_cast<uint32_t *>(base + l.top);
     c.r.low = reinterpret_cast<uint32_t *>(base + l.low);
     c.r.dloss_c = reinterpret_cast<float *>(base + l.dloss);
-    c.r.loss_c = reinterpret_cast<float *>(base + l.loss);
+    c.r.at_target_c = reinterpret_cast<float *>(base + l.at_target);
     c.r.lse_c = reinterpret_cast<float *>(base + l.lse);
     c.r.part_c = reinterpret_cast<float *>(base + l.part_of);
     c.r.whole_c = reinterpret_cast<float *>(base + l.whole);
