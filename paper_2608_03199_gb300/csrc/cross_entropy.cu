@@ -76,7 +76,7 @@ constexpr uint32_t kTmemCols = 512;
 constexpr int kGrid = 152, kPairs = kGrid / 2;        // one block an SM
 constexpr int kMaxGroup = 16;                         // tiles of classes whose statistics one block keeps
 constexpr int kMaxSlabs = 16;
-constexpr int kRowTile = 256;                         // rows of a block of k_xent_rows
+constexpr int kRowTile = 256;                         // rows whose targets are counted together
 constexpr int64_t kPoolBytes = (int64_t)1 << 30;
 
 struct Ctl {
@@ -193,19 +193,25 @@ __global__ void __launch_bounds__(kRowTile) k_xent_count(const RowArgs a) {
     }
 }
 
-template <typename T>
+// SUB blocks share a tile of rows, so that many blocks copy where there are few
+// tiles (32,768 rows of 768, one in seven with a target, backward: 26 us with one).
+// More than kFewRows rows have tiles enough, and every block reads all tiles' counts.
+constexpr int64_t kFewRows = 1 << 18;
+template <typename T, int SUB>
 __global__ void __launch_bounds__(kRowTile) k_xent_rows(const RowArgs a) {
     constexpr int kWarps = kRowTile / 32;
     __shared__ int s_before[kWarps], s_all[kWarps], s_rank[kWarps], s_list[kRowTile];
     __shared__ uint32_t s_top[kWarps], s_low[kWarps];
+    constexpr int kMine = kRowTile / SUB;            // rows of this block, from first on in its tile
+    const int tile = (int)blockIdx.x / SUB, tiles = (int)gridDim.x / SUB, first = (int)blockIdx.x % SUB * kMine;
     const int tid = threadIdx.x, lane = lane_id(), warp = tid >> 5;
     int before = 0, all = 0;
     uint32_t top = 0, low = 0xffffffffu;
 #pragma unroll 4
-    for (int b = tid; b < (int)gridDim.x; b += kRowTile) {
+    for (int b = tid; b < tiles; b += kRowTile) {
         const int c = a.count[b];
         all += c;
-        if (b < (int)blockIdx.x) before += c;
+        if (b < tile) before += c;
         if (a.dloss) {
             top = max(top, a.top[b]);
             low = min(low, a.low[b]);
@@ -215,7 +221,7 @@ __global__ void __launch_bounds__(kRowTile) k_xent_rows(const RowArgs a) {
     all = __reduce_add_sync(0xffffffffu, all);
     top = __reduce_max_sync(0xffffffffu, top);
     low = __reduce_min_sync(0xffffffffu, low);
-    const int64_t r = (int64_t)blockIdx.x * kRowTile + tid;
+    const int64_t r = (int64_t)tile * kRowTile + tid;
     const int t = r < a.rows ? id_at(a.targets, a.target_type, r, a.classes) : -1;
     const unsigned live = __ballot_sync(0xffffffffu, t >= 0);
     if (lane == 0) {
@@ -229,16 +235,18 @@ __global__ void __launch_bounds__(kRowTile) k_xent_rows(const RowArgs a) {
     before = all = 0;
     top = 0;
     low = 0xffffffffu;
-    int rank = 0, here = 0;
+    int rank = 0, here = 0;                          // before this thread's row in the block's, and of the block
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
         before += s_before[w];
         all += s_all[w];
         top = max(top, s_top[w]);
         low = min(low, s_low[w]);
-        if (w < warp) rank += s_rank[w];
-        here += s_rank[w];
+        if (w * 32 < first) before += s_rank[w];
+        else if (w * 32 < first + kMine) here += s_rank[w];
+        if (w * 32 >= first && w < warp) rank += s_rank[w];
     }
+    const bool mine = tid >= first && tid < first + kMine;
     rank += __popc(live & ((1u << lane) - 1));
     const bool every = all == a.rows, same = top == low;
     const float hi = unordered(top), lo = unordered(low);
@@ -260,7 +268,7 @@ __global__ void __launch_bounds__(kRowTile) k_xent_rows(const RowArgs a) {
         a.ctl->same = !a.dloss || same;
         a.ctl->factor = a.dloss && all > 0 ? (same ? hi : ldexpf(1.f, e_top)) : 0.f;
     }
-    if (t >= 0) {
+    if (mine && t >= 0) {
         const int at = before + rank;
         s_list[rank] = tid;
         a.row[at] = (int)r;
@@ -275,7 +283,7 @@ __global__ void __launch_bounds__(kRowTile) k_xent_rows(const RowArgs a) {
             a.at_target_c[at] = expm1f(-a.loss[r]);
             a.lse_c[at] = a.lse[r];
         }
-    } else if (r < a.rows && a.loss_out) {
+    } else if (mine && r < a.rows && a.loss_out) {
         a.loss_out[r] = 0.f;
         a.lse_out[r] = 0.f;
     }
@@ -286,7 +294,7 @@ __global__ void __launch_bounds__(kRowTile) k_xent_rows(const RowArgs a) {
     if (!every || scaled) {
         T *hc = static_cast<T *>(a.hc), *hs = static_cast<T *>(a.hs);
         for (int i = warp; i < here; i += kWarps) {
-            const int64_t from = (int64_t)blockIdx.x * kRowTile + s_list[i], to = before + i;
+            const int64_t from = (int64_t)tile * kRowTile + s_list[i], to = before + i;
             int e_row = e_top;
             if (scaled) apart(a.dloss[from], e_row);
             const float f = ldexpf(1.f, e_row - e_top);
@@ -304,18 +312,16 @@ __global__ void __launch_bounds__(kRowTile) k_xent_rows(const RowArgs a) {
             }
         }
         // the last tile's places past the list: zeros
-        if (blockIdx.x == 0) {
-            const int last = (int)min(padded(all), (int64_t)a.rows);
-            for (int i = all + warp; i < last; i += kWarps)
-                for (int c = lane; c < chunks; c += 32) {
-                    if (!every) reinterpret_cast<uint4 *>(hc + (int64_t)i * a.width)[c] = make_uint4(0, 0, 0, 0);
-                    if (scaled) reinterpret_cast<uint4 *>(hs + (int64_t)i * a.width)[c] = make_uint4(0, 0, 0, 0);
-                }
-        }
+        const int last = (int)min(padded(all), (int64_t)a.rows);
+        for (int i = all + (int)blockIdx.x * kWarps + warp; i < last; i += (int)gridDim.x * kWarps)
+            for (int c = lane; c < chunks; c += 32) {
+                if (!every) reinterpret_cast<uint4 *>(hc + (int64_t)i * a.width)[c] = make_uint4(0, 0, 0, 0);
+                if (scaled) reinterpret_cast<uint4 *>(hs + (int64_t)i * a.width)[c] = make_uint4(0, 0, 0, 0);
+            }
     }
-    if (a.dh && here < kRowTile)
-        for (int i = warp; i < kRowTile; i += kWarps) {
-            const int64_t row = (int64_t)blockIdx.x * kRowTile + i;
+    if (a.dh && here < kMine)
+        for (int i = warp; i < kMine; i += kWarps) {
+            const int64_t row = (int64_t)tile * kRowTile + first + i;
             if (row >= a.rows || id_at(a.targets, a.target_type, row, a.classes) >= 0) continue;
             for (int c = lane; c < chunks; c += 32)
                 reinterpret_cast<uint4 *>(static_cast<T *>(a.dh) + row * a.dh_stride)[c] = make_uint4(0, 0, 0, 0);
@@ -903,21 +909,37 @@ __global__ void __launch_bounds__(32 * kStrands) k_xent_join(const JoinArgs a) {
     for (int64_t i0 = (int64_t)blockIdx.x * 32; i0 < n; i0 += (int64_t)gridDim.x * 32) {
         const int64_t i = i0 + lane;
         float m = -INFINITY, s = 0.f;
-        auto merge = [&](float2 p) {
-            const float high = fmaxf(m, p.x), from = high == -INFINITY ? 0.f : high;
-            s = s * exp2_approx((m - from) * unit) + p.y * exp2_approx((p.x - from) * unit);
+        // eight parts at a time against their common maximum
+        auto merge = [&](const float2 (&p)[8]) {
+            float high = m;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) high = fmaxf(high, p[k].x);
+            const float from = high == -INFINITY ? 0.f : high;
+            s *= exp2_approx((m - from) * unit);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s += p[k].y * exp2_approx((p[k].x - from) * unit);
             m = high;
         };
         if (i < n)
-#pragma unroll 4
-            for (int p = strand; p < parts; p += kStrands) merge(a.part[p * stride + i]);
+            for (int p = strand; p < parts; p += 8 * kStrands) {
+                float2 some[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    some[k] = p + k * kStrands < parts ? a.part[(p + k * kStrands) * stride + i] : make_float2(-INFINITY, 0.f);
+                merge(some);
+            }
         __syncthreads();
         s_part[strand][lane] = make_float2(m, s);
         __syncthreads();
         if (strand > 0 || i >= n) continue;
         m = -INFINITY;
         s = 0.f;
-        for (int k = 0; k < kStrands; ++k) merge(s_part[k][lane]);
+        for (int k0 = 0; k0 < kStrands; k0 += 8) {
+            float2 some[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) some[k] = s_part[k0 + k][lane];
+            merge(some);
+        }
         // the others' sum s 2^m and the target's score, in base 2 (a bias: in base e)
         const float hit = a.hit[i], d = (m - hit) * unit;
         const float ln = a.biased ? 1.f : kLn2;               // to natural units
@@ -1104,9 +1126,15 @@ sieve_status prepare(Call &c, const sieve_cross_entropy_args &a, const Layout &l
 }
 
 template <typename T>
-cudaError_t forward(const Call &c, const JoinArgs &j, cudaStream_t st) {
+void list_rows(const Call &c, cudaStream_t st) {
     k_xent_count<<<c.blocks, kRowTile, 0, st>>>(c.r);
-    k_xent_rows<T><<<c.blocks, kRowTile, 0, st>>>(c.r);
+    if (c.x.rows <= kFewRows) k_xent_rows<T, 8><<<c.blocks * 8, kRowTile, 0, st>>>(c.r);
+    else k_xent_rows<T, 1><<<c.blocks, kRowTile, 0, st>>>(c.r);
+}
+
+template <typename T>
+cudaError_t forward(const Call &c, const JoinArgs &j, cudaStream_t st) {
+    list_rows<T>(c, st);
     cudaError_t e = c.x.bias ? run<T, 0, true>(c.x, 0, st) : run<T, 0, false>(c.x, 0, st);
     if (e != cudaSuccess) return e;
     const int64_t blocks = ceil_div(c.x.rows, 32);
@@ -1116,8 +1144,7 @@ cudaError_t forward(const Call &c, const JoinArgs &j, cudaStream_t st) {
 
 template <typename T>
 cudaError_t backward(const Call &c, const sieve_cross_entropy_grads &g, const DhArgs &d, int pieces, cudaStream_t st) {
-    k_xent_count<<<c.blocks, kRowTile, 0, st>>>(c.r);
-    k_xent_rows<T><<<c.blocks, kRowTile, 0, st>>>(c.r);
+    list_rows<T>(c, st);
     for (int p = 0; p < pieces; ++p) {
         cudaError_t e = c.x.bias ? run<T, 1, true>(c.x, p, st) : run<T, 1, false>(c.x, p, st);
         if (e == cudaSuccess && (g.dh || g.dweight)) e = run<T, 2, false>(c.x, p, st);

@@ -10,6 +10,8 @@
 // (a frequent word, the mask token) leaves one partial row a piece, which
 // k_embed_join adds up in order.  So the work is even whatever the ids are.
 // Rows that no token has are found by the blocks that write their zeros.
+#include <type_traits>
+
 #include "blocks.cuh"
 
 namespace sieve {
@@ -137,7 +139,7 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(const Sort s) {
     // digit tid: tokens of it in all tiles, and in the tiles before this one
     int all = 0, before = 0;
     if (tid < n) {
-#pragma unroll 8
+#pragma unroll 16
         for (int t = 0; t < s.tiles; ++t) {
             const int c = s.count[t * n + tid];
             all += c;
@@ -205,7 +207,7 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(const Sort s) {
 // ---------------------------------------------------------------------------
 constexpr int kPiece = 64;              // sorted tokens of a warp
 constexpr int kPieceWarps = 4;
-constexpr int kColumns = 256;           // columns of a warp: 8 a lane
+constexpr int kColumns = 256;           // columns of a warp, times NC: 8 a lane each
 constexpr int kZeroRows = 32;           // table rows of a block that looks for empty ones
 
 struct Sums {
@@ -216,28 +218,28 @@ struct Sums {
     int pieces, slices, sum_blocks;
 };
 
-// Places of a lane's 8 columns in a slice: together with VEC > 1, else 32 apart.
+// Places of a lane's 8 NC columns in a slice: VEC together.
 template <int VEC>
 __device__ __forceinline__ int column(int lane, int e) {
-    return VEC == 1 ? e * 32 + lane : (e / VEC * 32 + lane) * VEC + e % VEC;
+    return (e / VEC * 32 + lane) * VEC + e % VEC;
 }
-template <typename T, int VEC>
-struct Row {                            // 8 columns of a row
-    Chunk<T, VEC> c[8 / VEC];
+template <typename T, int VEC, int NC>
+struct Row {                            // a lane's columns of a row
+    Chunk<T, VEC> c[8 * NC / VEC];
     __device__ __forceinline__ void load(const T *p, int lane, int left) {
 #pragma unroll
-        for (int i = 0; i < 8 / VEC; ++i)
+        for (int i = 0; i < 8 * NC / VEC; ++i)
             if (column<VEC>(lane, i * VEC) < left) c[i].load(p + column<VEC>(lane, i * VEC));
     }
     __device__ __forceinline__ float get(int e) const { return c[e / VEC].get(e % VEC); }
 };
 // the finished sums of a table row
-template <typename G, int VEC>
-__device__ __forceinline__ void finish(const EmbedArgs &a, int id, int col0, int lane, const float (&sum)[8]) {
+template <typename G, int VEC, int NC>
+__device__ __forceinline__ void finish(const EmbedArgs &a, int id, int col0, int lane, const float (&sum)[8 * NC]) {
     G *to = static_cast<G *>(a.dtable) + id * a.dtable_stride + col0;
     const int left = a.width - col0;
 #pragma unroll
-    for (int i = 0; i < 8 / VEC; ++i) {
+    for (int i = 0; i < 8 * NC / VEC; ++i) {
         const int col = column<VEC>(lane, i * VEC);
         if (col >= left) continue;
         float v[VEC];
@@ -266,7 +268,7 @@ __device__ __forceinline__ int lower_bound(const int32_t *key, int n, int v) {
     return lo;
 }
 
-template <typename T, typename G, int VEC>
+template <typename T, typename G, int VEC, int NC>
 __global__ void __launch_bounds__(kPieceWarps * 32) k_embed_sums(const Sums s) {
     const EmbedArgs &a = s.a;
     const int lane = lane_id(), warp = threadIdx.x >> 5;
@@ -292,7 +294,8 @@ __global__ void __launch_bounds__(kPieceWarps * 32) k_embed_sums(const Sums s) {
         return;
     }
     const int64_t work = (int64_t)blockIdx.x * kPieceWarps + warp;
-    const int piece = (int)(work / s.slices), col0 = (int)(work % s.slices) * kColumns;
+    const int across = (s.slices + NC - 1) / NC;
+    const int piece = (int)(work / across), col0 = (int)(work % across) * kColumns * NC;
     if (piece >= s.pieces) return;
     const int p0 = piece * kPiece, count = min(kPiece, a.tokens - p0), left = a.width - col0;
     int keys[2], vals[2];
@@ -304,25 +307,25 @@ __global__ void __launch_bounds__(kPieceWarps * 32) k_embed_sums(const Sums s) {
     }
     const int prev = p0 > 0 ? s.key[p0 - 1] : -1, next = p0 + count < a.tokens ? s.key[p0 + count] : a.vocab;
     const T *dout = static_cast<const T *>(a.dout) + col0;
-    constexpr int kAhead = 8;
-    float sum[8] = {};
+    constexpr int kAhead = NC == 1 ? 8 : 4;
+    float sum[8 * NC] = {};
     int cur = __shfl_sync(0xffffffffu, keys[0], 0);
     // a whole id is written at once; what reaches into other pieces is kept
     auto flush = [&](int key, bool from_before, bool goes_on) {
         if (key >= a.vocab) return;
         if (!from_before && !goes_on) {
-            finish<G, VEC>(a, key, col0, lane, sum);
+            finish<G, VEC, NC>(a, key, col0, lane, sum);
             return;
         }
         float *to = s.partial + ((int64_t)piece * 2 + (from_before ? 0 : 1)) * a.width + col0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
+        for (int e = 0; e < 8 * NC; ++e)
             if (column<VEC>(lane, e) < left) to[column<VEC>(lane, e)] = sum[e];
         if (!from_before && col0 == 0 && lane == 0) s.join_list[atomicAdd(s.joins, 1)] = piece;
     };
     bool whole = true;                  // no id has ended in this piece yet
     for (int j0 = 0; j0 < count; j0 += kAhead) {
-        Row<T, VEC> x[kAhead];
+        Row<T, VEC, NC> x[kAhead];
         int key[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
@@ -340,11 +343,11 @@ __global__ void __launch_bounds__(kPieceWarps * 32) k_embed_sums(const Sums s) {
                 whole = false;
                 cur = key[u];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+                for (int e = 0; e < 8 * NC; ++e) sum[e] = 0.f;
             }
             if (cur < a.vocab)
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
+                for (int e = 0; e < 8 * NC; ++e)
                     if (column<VEC>(lane, e) < left) sum[e] += x[u].get(e);
         }
     }
@@ -352,48 +355,90 @@ __global__ void __launch_bounds__(kPieceWarps * 32) k_embed_sums(const Sums s) {
 }
 
 // The ids that several pieces share: the partial row of the piece where the id
-// starts, then of those that it goes through, by 16 strands of pieces added in order.
+// starts, then of those that it goes on into.  Up to kShort of these are added by
+// a warp for every kColumns columns; more (a very frequent id) by all strands of
+// the block, each a stretch of the pieces in order, then the strands in order.
 constexpr int kStrands = 16;
-constexpr int kJoinBlocks = 152 * 2;
+constexpr int kJoinBlocks = 152 * 4;
+constexpr int kShort = 8;
 template <typename G>
 __global__ void __launch_bounds__(kStrands * 32) k_embed_join(const Sums s) {
     __shared__ float part[kStrands][kColumns];
-    __shared__ int shared_end;
+    __shared__ int shared_end, n_long, long_piece[kStrands * 32];
     const EmbedArgs &a = s.a;
-    const int lane = lane_id(), strand = threadIdx.x >> 5;
-    const int64_t total = (int64_t)*s.joins * s.slices;
-    for (int64_t w = blockIdx.x; w < total; w += gridDim.x) {
-        const int piece = s.join_list[w / s.slices], col0 = (int)(w % s.slices) * kColumns, left = a.width - col0;
-        const int id = s.key[piece * kPiece + kPiece - 1];
+    const int lane = lane_id(), warp = threadIdx.x >> 5;
+    const int joins = *s.joins;
+    // pieces that the id at the end of `piece` goes on into, as far as kShort + 1
+    auto reach = [&](int piece, int id) {
+        int n = 0;
+        while (n <= kShort && (int64_t)(piece + 1 + n) * kPiece < a.tokens && s.key[(piece + 1 + n) * kPiece] == id) ++n;
+        return n;
+    };
+    auto write = [&](int id, int col, float v) {
+        G *to = static_cast<G *>(a.dtable) + id * a.dtable_stride + col;
+        v *= a.scale;
+        if (a.accumulate) v += to_f32<G>(*to);
+        *to = from_f32<G>(v);
+    };
+    // this block's joins: blockIdx.x, + gridDim.x, ...
+    for (int64_t j0 = blockIdx.x; j0 < joins; j0 += (int64_t)gridDim.x * kStrands * 32) {
         __syncthreads();
-        if (strand == 0) {
-            const int end = lower_bound(s.key, a.tokens, id + 1);   // past the id's last token
-            if (lane == 0) shared_end = end;
-        }
+        if (threadIdx.x == 0) n_long = 0;
         __syncthreads();
-        const int n = (shared_end - 1) / kPiece - piece;      // pieces that it goes on into
-        const int each = (n + kStrands - 1) / kStrands;
-        const int from = piece + 1 + strand * each, to = min(from + each, piece + 1 + n);
-        float sum[8] = {};
-#pragma unroll 4
-        for (int p = from; p < to; ++p) {
-            const float *x = s.partial + (int64_t)p * 2 * a.width + col0;
+        const int here = (int)min((int64_t)kStrands * 32, (joins - j0 + gridDim.x - 1) / gridDim.x);
+        for (int w = warp; w < here * s.slices; w += kStrands) {
+            const int piece = s.join_list[j0 + (int64_t)(w / s.slices) * gridDim.x], slice = w % s.slices;
+            const int id = s.key[piece * kPiece + kPiece - 1], n = reach(piece, id);
+            if (n > kShort) {
+                if (slice == 0 && lane == 0) long_piece[atomicAdd(&n_long, 1)] = piece;
+                continue;
+            }
+            const int col0 = slice * kColumns, left = a.width - col0;
+            const float *x = s.partial + (int64_t)piece * 2 * a.width + col0;
+            float sum[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] = e * 32 + lane < left ? __ldcg(x + a.width + e * 32 + lane) : 0.f;
+#pragma unroll 2
+            for (int p = 1; p <= n; ++p)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (e * 32 + lane < left) sum[e] += __ldcg(x + (int64_t)p * 2 * a.width + e * 32 + lane);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (e * 32 + lane < left) sum[e] += __ldcg(x + e * 32 + lane);
+                if (e * 32 + lane < left) write(id, col0 + e * 32 + lane, sum[e]);
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) part[strand][e * 32 + lane] = sum[e];
         __syncthreads();
-        const int col = threadIdx.x;
-        if (col < kColumns && col < left) {
-            float v = __ldcg(s.partial + ((int64_t)piece * 2 + 1) * a.width + col0 + col);
+        const int count = n_long;
+        for (int w = 0; w < count * s.slices; ++w) {
+            const int piece = long_piece[w / s.slices], col0 = w % s.slices * kColumns, left = a.width - col0;
+            const int id = s.key[piece * kPiece + kPiece - 1];
+            __syncthreads();
+            if (warp == 0) {
+                const int end = lower_bound(s.key, a.tokens, id + 1);   // past the id's last token
+                if (lane == 0) shared_end = end;
+            }
+            __syncthreads();
+            const int n = (shared_end - 1) / kPiece - piece;
+            const int each = (n + kStrands - 1) / kStrands;
+            const int from = piece + 1 + warp * each, to = min(from + each, piece + 1 + n);
+            float sum[8] = {};
+#pragma unroll 4
+            for (int p = from; p < to; ++p) {
+                const float *x = s.partial + (int64_t)p * 2 * a.width + col0;
 #pragma unroll
-            for (int k = 0; k < kStrands; ++k) v += part[k][col];
-            G *to_row = static_cast<G *>(a.dtable) + id * a.dtable_stride + col0 + col;
-            v *= a.scale;
-            if (a.accumulate) v += to_f32<G>(*to_row);
-            *to_row = from_f32<G>(v);
+                for (int e = 0; e < 8; ++e)
+                    if (e * 32 + lane < left) sum[e] += __ldcg(x + e * 32 + lane);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) part[warp][e * 32 + lane] = sum[e];
+            __syncthreads();
+            const int col = threadIdx.x;
+            if (col < kColumns && col < left) {
+                float v = __ldcg(s.partial + ((int64_t)piece * 2 + 1) * a.width + col0 + col);
+#pragma unroll
+                for (int k = 0; k < kStrands; ++k) v += part[k][col];
+                write(id, col0 + col, v);
+            }
         }
     }
 }
@@ -503,20 +548,31 @@ cudaError_t launch_embed_backward(const EmbedArgs &a, void *ws, cudaStream_t st)
     u.join_list = ints(l.list);
     u.pieces = (int)ceil_div(a.tokens, kPiece);
     u.slices = (int)ceil_div(a.width, kColumns);
-    u.sum_blocks = (int)ceil_div((int64_t)u.pieces * u.slices, kPieceWarps);
     const int64_t zero_blocks = a.accumulate ? 0 : ceil_div(a.vocab, kZeroRows);
-    const unsigned blocks = (unsigned)(u.sum_blocks + zero_blocks);
-    if (!blocks) return cudaSuccess;
     return with_type(a.dtype, [&](auto t) {
         using T = typename decltype(t)::type;
         return with_type(a.table_dtype, [&](auto g) {
             using G = typename decltype(g)::type;
             constexpr int V = sizeof(T) == 4 && sizeof(G) == 4 ? 4 : 8;
-            if (wide_rows(a.dout, a.dout_stride, a.width, V, sizeof(T)) &&
-                wide_rows(a.dtable, a.dtable_stride, a.width, V, sizeof(G)))
-                k_embed_sums<T, G, V><<<blocks, kPieceWarps * 32, 0, st>>>(u);
+            auto launch = [&](auto vec, auto nc) {
+                constexpr int VEC = decltype(vec)::value, NC = decltype(nc)::value;
+                u.sum_blocks = (int)ceil_div((int64_t)u.pieces * ceil_div(u.slices, NC), kPieceWarps);
+                const unsigned blocks = (unsigned)(u.sum_blocks + zero_blocks);
+                if (blocks) k_embed_sums<T, G, VEC, NC><<<blocks, kPieceWarps * 32, 0, st>>>(u);
+            };
+            using One = std::integral_constant<int, 1>;
+            // More columns a lane where there are pieces enough to fill the SMs: less work
+            // beside the sums for every token (131,000 tokens of 768 columns, bf16, 64,000
+            // ids: see the head of this file).  Odd rows move element by element.
+            if (!wide_rows(a.dout, a.dout_stride, a.width, V, sizeof(T)) ||
+                !wide_rows(a.dtable, a.dtable_stride, a.width, V, sizeof(G)))
+                launch(One{}, One{});
+            else if (u.slices == 1 || u.pieces < 152 * 2)
+                launch(std::integral_constant<int, V>{}, One{});
+            else if (u.slices % 3 == 0)
+                launch(std::integral_constant<int, V>{}, std::integral_constant<int, 3>{});
             else
-                k_embed_sums<T, G, 1><<<blocks, kPieceWarps * 32, 0, st>>>(u);
+                launch(std::integral_constant<int, V>{}, std::integral_constant<int, 2>{});
             if (a.tokens > kPiece) k_embed_join<G><<<kJoinBlocks, kStrands * 32, 0, st>>>(u);
             return cudaGetLastError();
         });

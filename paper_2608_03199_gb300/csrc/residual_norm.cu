@@ -157,9 +157,16 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) k_residual_norm(const R
 // partial[group][4][width] and k_residual_reduce adds the groups up.
 constexpr int kWarpRows = 4;
 __host__ __device__ constexpr int groups_of(int tpr) { return tpr == 32 ? kWarpRows : 1; }
+// Blocks that share an SM: 512 threads or so of 128 registers where a thread has 8
+// elements of a row, 640 to 768 of 80 to 96 where it has 4.
+__host__ __device__ constexpr int blocks_per_sm(int tpr, int elements) {
+    const int threads = tpr == 32 ? 32 * kWarpRows : tpr;
+    return threads >= 512 ? 1 : (elements == 8 ? 512 : 768) / threads;
+}
 
 template <typename T, typename W, int VEC, int TPR, int NCH, bool kShared>
-__global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR) k_residual_norm_backward(const ResidualNormArgs p) {
+__global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR, blocks_per_sm(TPR, NCH * VEC))
+    k_residual_norm_backward(const ResidualNormArgs p) {
     extern __shared__ float acc[];                 // kShared: [4][width]
     __shared__ float2 meet[2][32];
     const sieve_residual_norm_args &a = p.a;
@@ -175,6 +182,11 @@ __global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR) k_residual_n
     const W *w2 = static_cast<const W *>(a.weight);
     const int width = a.width;
     const float inv_n = 1.f / (float)width, centre = a.rms ? 0.f : inv_n;
+    // this thread's columns: (c * TPR + i) * VEC.  Those past the row read its last
+    // piece, so that no branch lies between loads, and count for nothing.
+    auto column = [&](int c) { return (c * TPR + i) * VEC; };
+    auto in = [&](int c) { return column(c) < width; };
+    auto place = [&](int c) { return min(column(c), width - VEC); };
     float sum[kShared ? 1 : 4][NCH][VEC];
     if constexpr (kShared) {
         for (int c = i; c < 4 * width; c += TPR) acc[c] = 0.f;
@@ -188,8 +200,11 @@ __global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR) k_residual_n
                 for (int e = 0; e < VEC; ++e) sum[k][c][e] = 0.f;
     }
     auto add = [&](int k, int c, int e, float v) {
-        if constexpr (kShared) acc[k * width + (c * TPR + i) * VEC + e] += v;
-        else sum[k][c][e] += v;
+        if constexpr (kShared) {
+            if (in(c)) acc[k * width + column(c) + e] += v;
+        } else {
+            sum[k][c][e] += v;
+        }
     };
     // two sums over the row's threads at once
     int turn = 0;
@@ -209,23 +224,20 @@ __global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR) k_residual_n
         }
     };
     // a row's elements, on their way while the row before is worked on
-    Piece<T, VEC> nh[NCH], ny[NCH], ns[NCH], nx[NCH];
+    Piece<T, VEC> nh[NCH], ny[NCH], ns[NCH], nx[NCH], ng[NCH];
     float n_stats[4] = {};
     auto load = [&](int64_t row) {
 #pragma unroll
         for (int c = 0; c < NCH; ++c) {
-            const int col = (c * TPR + i) * VEC;
-            nh[c].clear();
-            ny[c].clear();
-            ns[c].clear();
-            nx[c].clear();
-            if (col >= width) continue;
+            const int col = place(c);
             ny[c].load(y + row * a.y_stride + col);
             if (dstream) ns[c].load(dstream + row * g.dstream_stride + col);
+            else ns[c].clear();
             if (w2) {
                 nh[c].load(h + row * a.h_stride + col);
                 nx[c].load(dx + row * g.dx_stride + col);
             }
+            if (gate_rows) ng[c].load(gate_rows + row * a.gate_stride + col);
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k) n_stats[k] = __ldg(g.stats + k * a.rows + row);
@@ -233,43 +245,45 @@ __global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR) k_residual_n
     if (group < a.rows) load(group);
     for (int64_t row = group; row < a.rows; row += step) {
         float uh[NCH][VEC], sh[NCH][VEC], d2[NCH][VEC], G[NCH][VEC];
+        Piece<T, VEC> gr[NCH];
         float s1 = 0.f, s2 = 0.f;
         const float mu1 = n_stats[0], r1 = n_stats[1], mu2 = n_stats[2], r2 = n_stats[3];
 #pragma unroll
         for (int c = 0; c < NCH; ++c) {
-            const int col = (c * TPR + i) * VEC;
+            gr[c] = ng[c];
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 uh[c][e] = (ny[c].get(e) - mu1) * r1;
                 G[c][e] = ns[c].get(e);
-                sh[c][e] = nh[c].get(e);
-                d2[c][e] = nx[c].get(e);
             }
-            if (!w2 || col >= width) continue;
+            if (!w2) continue;
             // the stream again, then the gradient through its norm
             float u[VEC], t[VEC];
 #pragma unroll
             for (int e = 0; e < VEC; ++e) u[e] = uh[c][e];
             if (w1) {
-                load_vec<W, VEC>(w1 + col, t);
+                load_vec<W, VEC>(w1 + place(c), t);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) u[e] *= t[e];
                 if (b1) {
-                    load_vec<W, VEC>(b1 + col, t);
+                    load_vec<W, VEC>(b1 + place(c), t);
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) u[e] += t[e];
                 }
             }
-            if (gate || gate_rows) {
-                if (gate) load_vec<W, VEC>(gate + col, t);
-                else load_vec<T, VEC>(gate_rows + row * a.gate_stride + col, t);
+            if (gate) {
+                load_vec<W, VEC>(gate + place(c), t);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) u[e] *= t[e];
+            } else if (gate_rows) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) u[e] *= gr[c].get(e);
             }
-            load_vec<W, VEC>(w2 + col, t);
+            load_vec<W, VEC>(w2 + place(c), t);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                sh[c][e] = (fmaf(a.alpha, sh[c][e], u[e]) - mu2) * r2;
+                sh[c][e] = (fmaf(a.alpha, nh[c].get(e), u[e]) - mu2) * r2;
+                d2[c][e] = in(c) ? nx[c].get(e) : 0.f;
                 add(0, c, e, d2[c][e] * sh[c][e]);
                 add(1, c, e, d2[c][e]);
                 d2[c][e] *= t[e];
@@ -290,23 +304,20 @@ __global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR) k_residual_n
         s1 = s2 = 0.f;
 #pragma unroll
         for (int c = 0; c < NCH; ++c) {
-            const int col = (c * TPR + i) * VEC;
-            if (col >= width) continue;
             float t[VEC], w[VEC];
-            if (w1) load_vec<W, VEC>(w1 + col, w);
+            if (w1) load_vec<W, VEC>(w1 + place(c), w);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) t[e] = a.alpha * G[c][e];
-            store_vec<T, VEC>(dh + col, t);
+            if (in(c)) store_vec<T, VEC>(dh + column(c), t);
             if (gate_rows) {
-                float b[VEC], gr[VEC];
-                if (b1) load_vec<W, VEC>(b1 + col, b);
-                load_vec<T, VEC>(gate_rows + row * a.gate_stride + col, gr);
+                float b[VEC];
+                if (b1) load_vec<W, VEC>(b1 + place(c), b);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
                     t[e] = G[c][e] * (w1 ? fmaf(uh[c][e], w[e], b1 ? b[e] : 0.f) : uh[c][e]);
-                    G[c][e] *= gr[e];
+                    G[c][e] *= gr[c].get(e);
                 }
-                store_vec<T, VEC>(static_cast<T *>(g.dgate) + row * g.dgate_stride + col, t);
+                if (in(c)) store_vec<T, VEC>(static_cast<T *>(g.dgate) + row * g.dgate_stride + column(c), t);
             }
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
@@ -314,19 +325,19 @@ __global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR) k_residual_n
                 add(3, c, e, G[c][e]);
             }
             if (gate) {
-                load_vec<W, VEC>(gate + col, t);
+                load_vec<W, VEC>(gate + place(c), t);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) G[c][e] *= t[e];
             }
             if (w1) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    G[c][e] *= w[e];
+                    G[c][e] = in(c) ? G[c][e] * w[e] : 0.f;
                     s1 += G[c][e];
                     s2 = fmaf(G[c][e], uh[c][e], s2);
                 }
-            } else {
-                store_vec<T, VEC>(dy + col, G[c]);
+            } else if (in(c)) {
+                store_vec<T, VEC>(dy + column(c), G[c]);
             }
         }
         if (w1) {
@@ -334,11 +345,9 @@ __global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR) k_residual_n
             const float m1 = s1 * centre, m2 = s2 * inv_n;
 #pragma unroll
             for (int c = 0; c < NCH; ++c) {
-                const int col = (c * TPR + i) * VEC;
-                if (col >= width) continue;
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) G[c][e] = r1 * (G[c][e] - m1 - uh[c][e] * m2);
-                store_vec<T, VEC>(dy + col, G[c]);
+                if (in(c)) store_vec<T, VEC>(dy + column(c), G[c]);
             }
         }
     }
@@ -448,26 +457,27 @@ cudaError_t forward(const ResidualNormArgs &p, cudaStream_t st) {
     return forward_as<T, W, 1, 512, 16>(p, st);
 }
 
-// Threads of a row in the backward pass: 8 elements each, up to 1024 of them.
-int backward_threads(int width) {
-    if (width <= 256) return 32;
-    if (width <= 512) return 64;
-    if (width <= 768) return 96;
-    if (width <= 1024) return 128;
-    if (width <= 2048) return 256;
-    return width <= 4096 ? 512 : 1024;
-}
-// Blocks: as many as an SM holds, and few partial sums where there are few rows.
-int backward_blocks(int64_t rows, int width) {
-    const int tpr = backward_threads(width);
-    const int64_t n = ceil_div(rows, groups_of(tpr)), most = 152 * (tpr <= 128 ? 4 : tpr <= 512 ? 512 / tpr : 1);
-    return (int)(n < most ? n : most);
+// The backward pass' threads of a row and its blocks: 8 elements a thread where
+// they move 16 bytes at a time, else 4 (one by one, 8 need more registers than
+// there are), and 8 again past 4,096.
+struct Plan {
+    int tpr, elements, blocks, groups;
+};
+Plan plan(int64_t rows, int width, bool wide) {
+    Plan p;
+    p.elements = wide || width > 4096 ? 8 : 4;
+    const int need = (width + p.elements - 1) / p.elements;
+    p.tpr = need <= 32 ? 32 : need <= 64 ? 64 : need <= 96 ? 96 : need <= 128 ? 128 : need <= 256 ? 256 : need <= 512 ? 512 : 1024;
+    const int64_t n = ceil_div(rows, groups_of(p.tpr)), most = 152 * blocks_per_sm(p.tpr, p.elements);
+    p.blocks = (int)(n < most ? n : most);
+    p.groups = p.blocks * groups_of(p.tpr);
+    return p;
 }
 
-template <typename T, typename W, int VEC, int TPR>
+template <typename T, typename W, int VEC, int TPR, int ELEMENTS>
 cudaError_t backward_as(const ResidualNormArgs &p, int blocks, cudaStream_t st) {
     constexpr bool kShared = TPR == 1024;
-    auto kernel = k_residual_norm_backward<T, W, VEC, TPR, 8 / VEC, kShared>;
+    auto kernel = k_residual_norm_backward<T, W, VEC, TPR, ELEMENTS / VEC, kShared>;
     size_t smem = 0;
     if (kShared) {
         cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
@@ -479,28 +489,30 @@ cudaError_t backward_as(const ResidualNormArgs &p, int blocks, cudaStream_t st) 
     return cudaGetLastError();
 }
 
-template <typename T, typename W, int VEC>
-cudaError_t backward_by_width(const ResidualNormArgs &p, int blocks, cudaStream_t st) {
-    switch (backward_threads(p.a.width)) {
-        case 32: return backward_as<T, W, VEC, 32>(p, blocks, st);
-        case 64: return backward_as<T, W, VEC, 64>(p, blocks, st);
-        case 96: return backward_as<T, W, VEC, 96>(p, blocks, st);
-        case 128: return backward_as<T, W, VEC, 128>(p, blocks, st);
-        case 256: return backward_as<T, W, VEC, 256>(p, blocks, st);
-        case 512: return backward_as<T, W, VEC, 512>(p, blocks, st);
-        default: return backward_as<T, W, VEC, 1024>(p, blocks, st);
+template <typename T, typename W, int VEC, int ELEMENTS>
+cudaError_t backward_by_width(const ResidualNormArgs &p, const Plan &q, cudaStream_t st) {
+    switch (q.tpr) {
+        case 32: return backward_as<T, W, VEC, 32, ELEMENTS>(p, q.blocks, st);
+        case 64: return backward_as<T, W, VEC, 64, ELEMENTS>(p, q.blocks, st);
+        case 96: return backward_as<T, W, VEC, 96, ELEMENTS>(p, q.blocks, st);
+        case 128: return backward_as<T, W, VEC, 128, ELEMENTS>(p, q.blocks, st);
+        case 256: return backward_as<T, W, VEC, 256, ELEMENTS>(p, q.blocks, st);
+        case 512: return backward_as<T, W, VEC, 512, ELEMENTS>(p, q.blocks, st);
+        default: return backward_as<T, W, VEC, 1024, ELEMENTS>(p, q.blocks, st);
     }
 }
 
 template <typename T, typename W>
 cudaError_t backward(const ResidualNormArgs &p, cudaStream_t st) {
-    const int blocks = backward_blocks(p.a.rows, p.a.width), groups = blocks * groups_of(backward_threads(p.a.width));
-    if (blocks > 0) {
-        const cudaError_t e = wide<T>(p) ? backward_by_width<T, W, 16 / sizeof(T)>(p, blocks, st)
-                                         : backward_by_width<T, W, 1>(p, blocks, st);
+    const bool w = wide<T>(p);
+    const Plan q = plan(p.a.rows, p.a.width, w);
+    if (q.blocks > 0) {
+        const cudaError_t e = w ? backward_by_width<T, W, 16 / sizeof(T), 8>(p, q, st)
+                              : q.elements == 4 ? backward_by_width<T, W, 1, 4>(p, q, st)
+                                                : backward_as<T, W, 1, 1024, 8>(p, q.blocks, st);
         if (e != cudaSuccess) return e;
     }
-    k_residual_reduce<W><<<dim3((unsigned)ceil_div(p.a.width, 32), 2), 1024, 0, st>>>(p, groups);
+    k_residual_reduce<W><<<dim3((unsigned)ceil_div(p.a.width, 32), 2), 1024, 0, st>>>(p, q.groups);
     return cudaGetLastError();
 }
 
@@ -522,8 +534,8 @@ cudaError_t launch_residual_norm_backward(const ResidualNormArgs &p, cudaStream_
                    [&](auto t, auto w) { return backward<decltype(t), decltype(w)>(p, st); });
 }
 size_t residual_norm_backward_workspace_bytes(int64_t rows, int width) {
-    const int64_t groups = (int64_t)backward_blocks(rows, width) * groups_of(backward_threads(width));
-    return (size_t)round_up(groups * 4 * width * (int64_t)sizeof(float) + 256, 256);
+    const int64_t a = plan(rows, width, true).groups, b = plan(rows, width, false).groups;
+    return (size_t)round_up((a > b ? a : b) * 4 * width * (int64_t)sizeof(float) + 256, 256);
 }
 
 }  // namespace enc
