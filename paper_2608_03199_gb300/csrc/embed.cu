@@ -357,89 +357,104 @@ __global__ void __launch_bounds__(kPieceWarps * 32) k_embed_sums(const Sums s) {
 // The ids that several pieces share: the partial row of the piece where the id
 // starts, then of those that it goes on into.  Up to kShort of these are added by
 // a warp for every kColumns columns; more (a very frequent id) by all strands of
-// the block, each a stretch of the pieces in order, then the strands in order.
+// a block, each a stretch of the pieces in order, then the strands in order.
 constexpr int kStrands = 16;
+constexpr int kJoinThreads = kStrands * 32;
 constexpr int kJoinBlocks = 152 * 4;
 constexpr int kShort = 8;
 template <typename G>
-__global__ void __launch_bounds__(kStrands * 32) k_embed_join(const Sums s) {
+__global__ void __launch_bounds__(kJoinThreads) k_embed_join(const Sums s) {
     __shared__ float part[kStrands][kColumns];
-    __shared__ int shared_end, n_long, long_piece[kStrands * 32];
+    __shared__ int shared_end, found[kStrands], long_piece[kJoinThreads];
     const EmbedArgs &a = s.a;
     const int lane = lane_id(), warp = threadIdx.x >> 5;
     const int joins = *s.joins;
-    // pieces that the id at the end of `piece` goes on into, as far as kShort + 1
-    auto reach = [&](int piece, int id) {
-        int n = 0;
-        while (n <= kShort && (int64_t)(piece + 1 + n) * kPiece < a.tokens && s.key[(piece + 1 + n) * kPiece] == id) ++n;
-        return n;
-    };
     auto write = [&](int id, int col, float v) {
         G *to = static_cast<G *>(a.dtable) + id * a.dtable_stride + col;
         v *= a.scale;
         if (a.accumulate) v += to_f32<G>(*to);
         *to = from_f32<G>(v);
     };
-    // this block's joins: blockIdx.x, + gridDim.x, ...
-    for (int64_t j0 = blockIdx.x; j0 < joins; j0 += (int64_t)gridDim.x * kStrands * 32) {
+    // whether the id at the end of `piece` goes on into piece + n
+    auto reaches = [&](int piece, int id, int n) {
+        const int64_t p = (int64_t)(piece + n) * kPiece;
+        return p < a.tokens && s.key[p] == id;
+    };
+    // the short ones: a warp for each and kColumns columns
+    for (int64_t w = (int64_t)blockIdx.x * kStrands + warp; w < (int64_t)joins * s.slices; w += (int64_t)gridDim.x * kStrands) {
+        const int piece = s.join_list[w / s.slices], col0 = (int)(w % s.slices) * kColumns, left = a.width - col0;
+        const int id = s.key[piece * kPiece + kPiece - 1];
+        const int n = __popc(__ballot_sync(0xffffffffu, lane <= kShort && reaches(piece, id, 1 + lane)));
+        if (n > kShort) continue;
+        const float *x = s.partial + (int64_t)piece * 2 * a.width + col0;
+        float sum[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] = x[a.width + min(e * 32 + lane, left - 1)];
+#pragma unroll 4
+        for (int p = 1; p <= n; ++p)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] += x[(int64_t)p * 2 * a.width + min(e * 32 + lane, left - 1)];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e * 32 + lane < left) write(id, col0 + e * 32 + lane, sum[e]);
+    }
+    // the long ones, by their number in the list: every block finds all of them and takes its share
+    int64_t before = 0;
+    for (int j0 = 0; j0 < joins; j0 += kJoinThreads) {
+        const int j = j0 + (int)threadIdx.x, piece = j < joins ? s.join_list[j] : -1;
+        const bool is_long = piece >= 0 && reaches(piece, s.key[piece * kPiece + kPiece - 1], 1 + kShort);
+        const unsigned votes = __ballot_sync(0xffffffffu, is_long);
         __syncthreads();
-        if (threadIdx.x == 0) n_long = 0;
+        if (lane == 0) found[warp] = __popc(votes);
         __syncthreads();
-        const int here = (int)min((int64_t)kStrands * 32, (joins - j0 + gridDim.x - 1) / gridDim.x);
-        for (int w = warp; w < here * s.slices; w += kStrands) {
-            const int piece = s.join_list[j0 + (int64_t)(w / s.slices) * gridDim.x], slice = w % s.slices;
-            const int id = s.key[piece * kPiece + kPiece - 1], n = reach(piece, id);
-            if (n > kShort) {
-                if (slice == 0 && lane == 0) long_piece[atomicAdd(&n_long, 1)] = piece;
-                continue;
-            }
-            const int col0 = slice * kColumns, left = a.width - col0;
-            const float *x = s.partial + (int64_t)piece * 2 * a.width + col0;
-            float sum[8];
+        int rank = __popc(votes & ((1u << lane) - 1)), count = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum[e] = e * 32 + lane < left ? __ldcg(x + a.width + e * 32 + lane) : 0.f;
-#pragma unroll 2
-            for (int p = 1; p <= n; ++p)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (e * 32 + lane < left) sum[e] += __ldcg(x + (int64_t)p * 2 * a.width + e * 32 + lane);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (e * 32 + lane < left) write(id, col0 + e * 32 + lane, sum[e]);
+        for (int w = 0; w < kStrands; ++w) {
+            rank += w < warp ? found[w] : 0;
+            count += found[w];
         }
+        if (is_long) long_piece[rank] = piece;
         __syncthreads();
-        const int count = n_long;
-        for (int w = 0; w < count * s.slices; ++w) {
-            const int piece = long_piece[w / s.slices], col0 = w % s.slices * kColumns, left = a.width - col0;
-            const int id = s.key[piece * kPiece + kPiece - 1];
+        const int64_t first = before * s.slices, last = (before + count) * s.slices;
+        before += count;
+        for (int64_t w = first + (blockIdx.x + gridDim.x - first % gridDim.x) % gridDim.x; w < last; w += gridDim.x) {
+            const int start = long_piece[(w - first) / s.slices], col0 = (int)((w - first) % s.slices) * kColumns;
+            const int id = s.key[start * kPiece + kPiece - 1], left = a.width - col0;
             __syncthreads();
             if (warp == 0) {
                 const int end = lower_bound(s.key, a.tokens, id + 1);   // past the id's last token
                 if (lane == 0) shared_end = end;
             }
             __syncthreads();
-            const int n = (shared_end - 1) / kPiece - piece;
+            const int n = (shared_end - 1) / kPiece - start;
             const int each = (n + kStrands - 1) / kStrands;
-            const int from = piece + 1 + warp * each, to = min(from + each, piece + 1 + n);
+            const int from = start + 1 + warp * each, to = min(from + each, start + 1 + n);
             float sum[8] = {};
-#pragma unroll 4
-            for (int p = from; p < to; ++p) {
-                const float *x = s.partial + (int64_t)p * 2 * a.width + col0;
+            // (eight pieces' loads go out together: places past the row read its last element)
+            for (int p = from; p < to; p += 8) {
+                float v[8][8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (e * 32 + lane < left) sum[e] += __ldcg(x + e * 32 + lane);
+                for (int k = 0; k < 8; ++k)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        v[k][e] = s.partial[(int64_t)min(p + k, to - 1) * 2 * a.width + col0 + min(e * 32 + lane, left - 1)];
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum[e] += p + k < to ? v[k][e] : 0.f;
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) part[warp][e * 32 + lane] = sum[e];
             __syncthreads();
             const int col = threadIdx.x;
             if (col < kColumns && col < left) {
-                float v = __ldcg(s.partial + ((int64_t)piece * 2 + 1) * a.width + col0 + col);
+                float v = s.partial[((int64_t)start * 2 + 1) * a.width + col0 + col];
 #pragma unroll
                 for (int k = 0; k < kStrands; ++k) v += part[k][col];
                 write(id, col0 + col, v);
             }
         }
+        __syncthreads();
     }
 }
 

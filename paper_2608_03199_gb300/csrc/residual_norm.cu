@@ -52,9 +52,12 @@ __device__ __forceinline__ float row_sum(float v, float *smem) {
 }
 
 // Forward.  A row per warp (TPR = 32, eight rows a block) or per block of TPR
-// threads; chunk c of thread i at (c * TPR + i) * VEC.
+// threads; chunk c of thread i at (c * TPR + i) * VEC.  Up to 24 elements a lane fit
+// 64 registers, so that four blocks share an SM (100,003 x 768 bf16: 113 us, 126 with
+// three); 32 do not (200,003 x 1024: 269 us, 315 with spills).
 template <typename T, typename W, int VEC, int TPR, int NCH>
-__global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) k_residual_norm(const ResidualNormArgs p) {
+__global__ void __launch_bounds__(TPR == 32 ? 256 : TPR, TPR == 32 ? (NCH * VEC <= 24 ? 4 : 3) : 1024 / TPR)
+    k_residual_norm(const ResidualNormArgs p) {
     constexpr int kRows = TPR == 32 ? 8 : 1;
     __shared__ float smem[32];
     const sieve_residual_norm_args &a = p.a;
@@ -157,8 +160,9 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) k_residual_norm(const R
 // partial[group][4][width] and k_residual_reduce adds the groups up.
 constexpr int kWarpRows = 4;
 __host__ __device__ constexpr int groups_of(int tpr) { return tpr == 32 ? kWarpRows : 1; }
-// Blocks that share an SM: 512 threads or so of 128 registers where a thread has 8
-// elements of a row, 640 to 768 of 80 to 96 where it has 4.
+// Blocks that share an SM: 512 threads of 128 registers where a thread has 8
+// elements of a row (576 of 112 spill: 100,003 x 768 bf16 236 -> 333 us), 768 of 80
+// where it has 4.
 __host__ __device__ constexpr int blocks_per_sm(int tpr, int elements) {
     const int threads = tpr == 32 ? 32 * kWarpRows : tpr;
     return threads >= 512 ? 1 : (elements == 8 ? 512 : 768) / threads;
@@ -244,7 +248,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR, blocks_per_s
     };
     if (group < a.rows) load(group);
     for (int64_t row = group; row < a.rows; row += step) {
-        float uh[NCH][VEC], sh[NCH][VEC], d2[NCH][VEC], G[NCH][VEC];
+        float uh[NCH][VEC], sh[NCH][VEC], G[NCH][VEC];
         Piece<T, VEC> gr[NCH];
         float s1 = 0.f, s2 = 0.f;
         const float mu1 = n_stats[0], r1 = n_stats[1], mu2 = n_stats[2], r2 = n_stats[3];
@@ -283,22 +287,23 @@ __global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR, blocks_per_s
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 sh[c][e] = (fmaf(a.alpha, nh[c].get(e), u[e]) - mu2) * r2;
-                d2[c][e] = in(c) ? nx[c].get(e) : 0.f;
-                add(0, c, e, d2[c][e] * sh[c][e]);
-                add(1, c, e, d2[c][e]);
-                d2[c][e] *= t[e];
-                s1 += d2[c][e];
-                s2 = fmaf(d2[c][e], sh[c][e], s2);
+                float d = in(c) ? nx[c].get(e) : 0.f;
+                add(0, c, e, d * sh[c][e]);
+                add(1, c, e, d);
+                d *= t[e];
+                s1 += d;
+                s2 = fmaf(d, sh[c][e], s2);
+                G[c][e] = fmaf(r2, d, G[c][e]);
             }
         }
         if (row + step < a.rows) load(row + step);
         if (w2) {
             both_sums(s1, s2);
-            const float m1 = s1 * centre, m2 = s2 * inv_n;
+            const float m1 = r2 * s1 * centre, m2 = r2 * s2 * inv_n;
 #pragma unroll
             for (int c = 0; c < NCH; ++c)
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) G[c][e] += r2 * (d2[c][e] - m1 - sh[c][e] * m2);
+                for (int e = 0; e < VEC; ++e) G[c][e] -= fmaf(sh[c][e], m2, m1);
         }
         T *dh = static_cast<T *>(g.dh) + row * g.dh_stride, *dy = static_cast<T *>(g.dy) + row * g.dy_stride;
         s1 = s2 = 0.f;
