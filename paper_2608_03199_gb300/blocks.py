@@ -22,7 +22,6 @@ import paper_2608_03199_gb300 as _sieve
 from .encoder import (DTYPES, _FLOATS, _HALVES, _launch, _need, _rows, _scratch, _vector, encoder_status)
 
 ID_TYPES = {torch.int32: 3, torch.int64: 4}
-GATES = {"none": 0, "column": 1, "row": 2}
 
 
 class ResidualNormArgsC(C.Structure):
@@ -161,20 +160,28 @@ def _residual_args(h, y, weight, bias, post_weight, post_bias, gate, alpha, rms,
     ys = _rows(y, "y", (kind,), dev, h.shape)[2]
     if weight is None and post_weight is None:
         raise ValueError("at least one of weight and post_weight is needed")
-    wtype = (weight if weight is not None else post_weight).dtype
-    for w, b, name in ((weight, bias, "weight"), (post_weight, post_bias, "post_weight")):
-        if w is not None:
-            _vector(w, name, (kind, torch.float32) if wtype in (kind, torch.float32) else (kind,), width, dev)
-            _need(w, name, (wtype,), 1, dev)
-        if b is not None:
-            if w is None:
-                raise ValueError(f"a bias goes with its weight: {name} is missing")
-            _vector(b, name.replace("weight", "bias"), (wtype,), width, dev)
+    first = weight if weight is not None else post_weight
+    wtype = first.dtype if isinstance(first, torch.Tensor) else None
+    if wtype is not kind and wtype is not torch.float32:
+        _need(first, "weight" if weight is not None else "post_weight", (kind, torch.float32), 1, dev)
+    types = (wtype,)
+    if weight is not None:
+        _vector(weight, "weight", types, width, dev)
+    if bias is not None:
+        if weight is None:
+            raise ValueError("a bias goes with its weight: weight is missing")
+        _vector(bias, "bias", types, width, dev)
+    if post_weight is not None:
+        _vector(post_weight, "post_weight", types, width, dev)
+    if post_bias is not None:
+        if post_weight is None:
+            raise ValueError("a bias goes with its weight: post_weight is missing")
+        _vector(post_bias, "post_bias", types, width, dev)
     gate_kind, gs = 0, 0
     if gate is not None:
-        if gate.dim() == 1 and h.dim() > 1:
+        if isinstance(gate, torch.Tensor) and gate.dim() == 1 and h.dim() > 1:
             gate_kind = 1
-            _vector(gate, "gate", (wtype,), width, dev)
+            _vector(gate, "gate", types, width, dev)
         else:
             gate_kind = 2
             gs = _rows(gate, "gate", (kind,), dev, h.shape)[2]

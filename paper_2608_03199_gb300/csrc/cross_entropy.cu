@@ -61,9 +61,9 @@ constexpr int kBoxes = kHalf / kBox;                  // of an operand in a bloc
 constexpr uint32_t kStageBytes = 2 * kBoxes * kBoxBytes;
 constexpr int kEpiWarps = 8;
 __host__ __device__ constexpr int chunk_blocks(int mode) { return mode == 2 ? 64 : 4; }
-// Registers: 384 threads start with 168 each, 64,512 in all.  The eight warps that
+// Registers: 384 threads start with kRegisters each, 64,512 in all.  The eight warps that
 // hold a tile's sums take 232, the four others (two of them idle) keep 40.
-constexpr int kThreads = (kEpiWarps + 4) * 32;
+constexpr int kThreads = (kEpiWarps + 4) * 32, kRegisters = 168;
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 232;"); }
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 40;"); }
 constexpr uint32_t kOutBytes = 32 * 128;              // a warp's rows on their way out
@@ -84,7 +84,7 @@ struct Ctl {
     int n;               // rows with a target
     int all;             // every row has one
     int same;            // all of them have the same dloss
-    float factor;        // that dloss, or the power of two above the largest magnitude
+    float factor;        // that dloss, or the power of two below the largest magnitude
 };
 
 struct XentArgs {
@@ -250,14 +250,16 @@ __global__ void __launch_bounds__(kRowTile) k_xent_rows(const RowArgs a) {
     rank += __popc(live & ((1u << lane) - 1));
     const bool every = all == a.rows, same = top == low;
     const float hi = unordered(top), lo = unordered(low);
-    // m 2^e of a dloss; a zero, or one that is not finite, stays whole, and so does
-    // its h
+    // m 2^e of a dloss, m from 1 to 2 (so that 2^e is finite); a zero, or one that is
+    // not finite, stays whole, and so does its h
     const float largest = fmaxf(fabsf(hi), fabsf(lo));
-    int e_top = 0;
+    int e_top = 1;
     if (isfinite(largest)) frexpf(largest, &e_top);
+    --e_top;
     auto apart = [&](float v, int &e) {
         const float m = frexpf(v, &e);
-        if (v != 0.f && isfinite(v)) return m;
+        --e;
+        if (v != 0.f && isfinite(v)) return 2.f * m;
         e = e_top;
         return v;
     };
@@ -1083,6 +1085,12 @@ Layout layout(const sieve_cross_entropy_args &a, bool backward) {
 template <typename T, int MODE, bool BIAS>
 cudaError_t run(const XentArgs &a, int piece, cudaStream_t st) {
     auto kernel = k_xent<T, MODE, BIAS>;
+    // The warps trade registers among each other, which takes all that kRegisters says.
+    static const int registers = [&] {
+        cudaFuncAttributes f;
+        return cudaFuncGetAttributes(&f, kernel) == cudaSuccess ? f.numRegs : -1;
+    }();
+    if (registers != kRegisters) return cudaErrorInvalidDeviceFunction;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(MODE));
     if (e != cudaSuccess) return e;
     kernel<<<kGrid, kThreads, smem_bytes(MODE), st>>>(a, piece);

@@ -53,37 +53,28 @@ __device__ __forceinline__ void put(T *p, const float (&v)[VEC]) {
     }
 }
 
-// A block takes `tokens_per_block` tokens; thread l takes chunks l, l + 256, ...
-// of theirs, kAhead of them at a time.
+// A block takes `tokens_per_block` tokens and its threads chunk after chunk of
+// theirs, one at a time: many warps hide the two loads that depend on each other
+// better than few with more of them in hand (200,003 tokens of 1024 columns, fp32 to
+// bf16: 98 us, 125 with four chunks ahead, 169 with eight).
 template <typename T, typename O, int VEC>
 __global__ void __launch_bounds__(kThreads) k_embed(const EmbedArgs a, int tokens_per_block, int chunks) {
-    constexpr int kAhead = 4;
     const int64_t first = (int64_t)blockIdx.x * tokens_per_block;
-    const int here = (int)min((int64_t)tokens_per_block, a.tokens - first);
-    const int total = here * chunks;
+    const int total = (int)min((int64_t)tokens_per_block, a.tokens - first) * chunks;
     const T *table = static_cast<const T *>(a.table);
     O *out = static_cast<O *>(a.out);
-    for (int l0 = threadIdx.x; l0 < total; l0 += kThreads * kAhead) {
-        int tok[kAhead], col[kAhead], id[kAhead];
-        Chunk<T, VEC> x[kAhead];
+#pragma unroll 1
+    for (int l = threadIdx.x; l < total; l += kThreads) {
+        const int token = l / chunks, col = (l - token * chunks) * VEC;
+        const int id = id_at(a.ids, a.id_type, first + token, a.vocab);
+        float v[VEC] = {};
+        if (id >= 0) {
+            Chunk<T, VEC> x;
+            x.load(table + id * a.table_stride + col);
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int l = l0 + u * kThreads;
-            tok[u] = l / chunks;
-            col[u] = (l - tok[u] * chunks) * VEC;
-            id[u] = l < total ? id_at(a.ids, a.id_type, first + tok[u], a.vocab) : -1;
+            for (int e = 0; e < VEC; ++e) v[e] = a.scale * x.get(e);
         }
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (id[u] >= 0) x[u].load(table + id[u] * a.table_stride + col[u]);
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (l0 + u * kThreads >= total) break;
-            float v[VEC];
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) v[e] = id[u] >= 0 ? a.scale * x[u].get(e) : 0.f;
-            put<O, VEC>(out + (first + tok[u]) * a.out_stride + col[u], v);
-        }
+        put<O, VEC>(out + (first + token) * a.out_stride + col, v);
     }
 }
 

@@ -25,6 +25,7 @@ EMBED = [
     (1, 1, 1, FP32, FP32, I64), (1, 7, 8, BF16, BF16, I32), (23, 50_000, 768, BF16, BF16, I64), (64, 5, 40, FP16, FP16, I32),
     (65, 5, 40, FP32, BF16, I64), (700, 511, 96, FP32, FP16, I32), (700, 512, 301, FP32, FP32, I64), (2049, 513, 257, BF16, FP32, I32),
     (5000, 3, 1000, FP16, BF16, I64), (9001, 100_003, 64, FP32, FP32, I64), (40_000, 262_144, 48, BF16, BF16, I32),
+    (40_000, 3_000, 768, FP32, BF16, I64), (30_011, 1_000, 512, BF16, BF16, I32), (21_000, 5_000, 1_280, FP16, FP32, I64),
     (3, 20, 16_384, FP32, BF16, I32), (130, 9, 16_383, BF16, BF16, I64), (20_000, 1, 8, FP32, BF16, I64), (640_001, 300, 24, FP32, BF16, I32),
 ]
 
@@ -351,6 +352,71 @@ def test_cross_entropy_small_losses_keep_their_digits():
     want = torch.log1p(torch.exp(-x) + torch.exp(-2 * x))
     assert ((loss.double() - want).abs() <= 2.0 ** -18 * want).all()
     check_loss(h, weight, t, None, 1.0, torch.ones(n, device=DEV))
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+def test_cross_entropy_takes_any_dloss(dtype):
+    """Magnitudes from the type's largest to subnormal ones, zeros and both
+    signs, in one call; rows whose dloss is far below the largest keep their dh."""
+    g = gen(14)
+    h, weight, t, b = loss_inputs(g, 640, 300, 64, dtype, 0.9, True, spread=0.5)
+    exponents = torch.randint(-18, 4, (640,), generator=g, device=DEV)
+    for up in (0, 80 if dtype == BF16 else 0, -100 if dtype == BF16 else 0):
+        dloss = torch.where(torch.arange(640, device=DEV) % 5 == 0, 0.0, randn(g, 640)) * torch.exp2((exponents + up).float())
+        check_loss(h, weight, t, b, 1.0, dloss)
+    # the type's ends at once; dweight is off the type, dh is not (rows of bf16 reach as far as fp32)
+    if dtype == BF16:
+        dloss = torch.full((640,), 1e-42, device=DEV)
+        dloss[::2] = 3e38
+        loss, lse = sieve.cross_entropy(h, weight, t, bias=b)
+        dh = sieve.cross_entropy_backward(dloss, h, weight, t, loss, lse, bias=b)[0]
+        want, bound = ref.cross_entropy(h, weight, t, b, 1.0, dloss)
+        assert want["dh"].abs().max() < 3e38
+        ref.assert_within(dh, want["dh"], bound["dh"], "dh")
+
+
+def test_cross_entropy_of_many_rows():
+    """More rows than one list of blocks goes by, most without a target."""
+    g = gen(15)
+    h, weight, t, b = loss_inputs(g, 300_001, 5, 8, BF16, 0.03, True)
+    check_loss(h, weight, t, b, 1.0, torch.full((300_001,), 0.25, device=DEV))
+
+
+def test_cross_entropy_not_a_number_stays_in_its_row_of_dh():
+    g = gen(16)
+    h, weight, t, b = loss_inputs(g, 300, 700, 64, BF16)
+    one = torch.ones(300, device=DEV)
+    loss, lse = sieve.cross_entropy(h, weight, t)
+    clean = sieve.cross_entropy_backward(one, h, weight, t, loss, lse)[0]
+    h[7, 3] = math.nan
+    loss, lse = sieve.cross_entropy(h, weight, t)
+    dh, dw, _ = sieve.cross_entropy_backward(one, h, weight, t, loss, lse)
+    rest = torch.arange(300, device=DEV) != 7
+    assert dh[7].isnan().all() and torch.equal(dh[rest], clean[rest]) and dw.isnan().any()
+
+
+def test_cross_entropy_twice_at_once():
+    """Two calls on two streams, each with its own scratch, give what they
+    give alone."""
+    g = gen(17)
+    a, b = (loss_inputs(g, n, 3_000, 128, BF16, 0.8, True) for n in (900, 1_500))
+    d = [torch.full((len(x[0]),), 0.5, device=DEV) for x in (a, b)]
+
+    def both(x, dloss, stream=None):
+        h, weight, t, bias = x
+        loss, lse = sieve.cross_entropy(h, weight, t, bias=bias, stream=stream)
+        return (loss, *sieve.cross_entropy_backward(dloss, h, weight, t, loss, lse, bias=bias, stream=stream))
+    want = [both(x, y) for x, y in zip((a, b), d)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for i in range(2):
+            got[i].append(both((a, b)[i], d[i], streams[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for res in got[i]:
+            assert all(torch.equal(x, y) for x, y in zip(res, want[i]))
 
 
 def test_cross_entropy_not_a_number_reaches_its_row():
