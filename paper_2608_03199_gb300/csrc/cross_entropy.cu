@@ -22,9 +22,14 @@
 // (and a copy of their h, unless every row has a target), and everything after it
 // runs over that list, whose length only the device knows.
 //
-// The pool: panel j holds 64 classes of all listed rows, [rows padded to 128]
+// The pool: panel j holds 64 classes of all listed rows, [rows padded to 256]
 // [64], so its address needs no stride that depends on the list.  As operand of
 // dh a panel is K-major, as operand of dW MN-major.
+//
+// With few rows (kFine) a gradient's element is the sum of a few q, whose rounding
+// no other evens out, and the products cost little beside the tables they read and
+// write: there the pool holds what the rounding left off as well, in as many rows
+// more, both products run over both, and scores are summed in shorter chunks.
 //
 // dloss differs from row to row, and dW needs it in the product.  Where all
 // rows have the same one it is a factor at the end.  Else it is taken apart, m 2^e:
@@ -60,7 +65,13 @@ constexpr uint32_t kBoxBytes = kBox * 128;
 constexpr int kBoxes = kHalf / kBox;                  // of an operand in a block
 constexpr uint32_t kStageBytes = 2 * kBoxes * kBoxBytes;
 constexpr int kEpiWarps = 8;
-__host__ __device__ constexpr int chunk_blocks(int mode) { return mode == 2 ? 64 : 4; }
+constexpr int kFine = kM;                             // rows that are few
+constexpr int64_t kMaybeFine = 2048;                  // rows of a call whose list may be that short
+// rows of a panel of the pool
+__host__ __device__ inline int64_t panel_rows(int64_t n) {
+    const int64_t padded = (n + kM - 1) / kM * kM;
+    return padded < 2 * kFine ? 2 * kFine : padded;
+}
 // Registers: 384 threads start with kRegisters each, 64,512 in all.  The eight warps that
 // hold a tile's sums take 232, the four others (two of them idle) keep 40.
 constexpr int kThreads = (kEpiWarps + 4) * 32, kRegisters = 168;
@@ -100,7 +111,7 @@ struct XentArgs {
     int64_t pool_rows;
     int rows, classes, width;
     float scale, c;                       // c = scale log2(e)
-    int want_dh, want_dw, want_db, dw_f32, accumulate;
+    int want_dh, want_dw, want_db, dw_f32, accumulate, maybe_fine;
 };
 
 template <typename T>
@@ -123,7 +134,7 @@ __device__ __forceinline__ float2 add_pair(float2 sum, uint32_t pair) {
 // classes of a piece, and how the forward pass groups its tiles
 __host__ __device__ inline int64_t padded(int64_t n) { return (n < 1 ? 1 : n) + kM - 1 - ((n < 1 ? 1 : n) - 1) % kM; }
 __host__ __device__ inline int piece_classes(int64_t n, int classes, int64_t pool_rows) {
-    const int64_t most = pool_rows / padded(n) / (kN / kK) * kN;
+    const int64_t most = pool_rows / panel_rows(n) / (kN / kK) * kN;
     const int64_t pieces = (classes + most - 1) / most, each = (classes + pieces - 1) / pieces;
     return (int)((each + kN - 1) / kN * kN);
 }
@@ -422,18 +433,22 @@ struct Tile {
     int n_boxes;         // of 64 columns, in each block
     int first, blocks;   // stages of the contraction axis
     int slab;            // MODE 2, dh: which sums
+    int half;            // MODE 2: the stage from which on it runs over what the rounding left off
     bool dw;             // MODE 2: dW, else dh
 };
 
 // The tiles of a launch, in order: what every role walks.
 template <int MODE>
 struct Walk {
-    int n, mp, row_tiles, class_tiles, group, groups;
+    int n, mp, panel, row_tiles, class_tiles, group, groups;
+    bool fine;                                       // the pool holds q in two parts
     int v0, v1;                                      // classes of the piece
     int dh_tiles, d_tiles, dw_rows, total, width, slabs, slab_blocks;
     __device__ __forceinline__ Walk(const XentArgs &a, int piece) {
         n = a.ctl->n;
         mp = (int)padded(n);
+        panel = (int)panel_rows(n);
+        fine = a.maybe_fine && n <= kFine;
         width = a.width;
         row_tiles = (n + kM - 1) / kM;
         d_tiles = (a.width + kN - 1) / kN;
@@ -481,13 +496,16 @@ struct Walk {
         t.n_boxes = width - t.n0 > kN / 2 ? kBoxes : kBoxes / 2;
         t.first = t.slab * slab_blocks;
         t.blocks = t.dw ? (n + kK - 1) / kK : max(0, min(slab_blocks, (v1 - v0 + kK - 1) / kK - t.first));
+        t.half = fine ? t.blocks : INT32_MAX;
+        if (fine) t.blocks *= 2;
         return t;
     }
 };
 
-template <typename T, int MODE, bool BIAS>
+template <typename T, int MODE, bool BIAS, bool FINE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ XentArgs a, int piece) {
-    constexpr int kStages = stages(MODE), kChunk = chunk_blocks(MODE);
+    constexpr int kStages = stages(MODE);
+    const int chunk_of = MODE == 2 ? 64 : FINE && a.ctl->n <= kFine ? 2 : 4;      // stages of a chunk
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t full[kStages], empty[kStages], d_full[2], d_empty[2], drained;
     __shared__ uint32_t tmem_slot;
@@ -540,18 +558,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                         const uint32_t bar = at_first(&full[st]);
                         if (rank == 0) expect(&full[st], 2 * (kBoxes + t.n_boxes) * kBoxBytes);
                         const int m = t.m0 + rank * kHalf, n = t.n0 + rank * t.n_boxes * kBox;
+                        const int k0 = MODE == 2 && b >= t.half ? b - t.half : b, low = b == k0 ? 0 : walk.mp;
 #pragma unroll
                         for (int j = 0; j < kBoxes; ++j) {
                             void *dst = pa + j * kBoxBytes;
                             if (MODE != 2) load_box(dst, rows, b * kK, m + j * kBox, bar);
-                            else if (t.dw) load_box(dst, &a.pool_in, 0, (m / kBox + j) * walk.mp + b * kK, bar);
-                            else load_box(dst, &a.pool_in, 0, (t.first + b) * walk.mp + m + j * kBox, bar);
+                            else if (t.dw) load_box(dst, &a.pool_in, 0, (m / kBox + j) * walk.panel + low + k0 * kK, bar);
+                            else load_box(dst, &a.pool_in, 0, (t.first + k0) * walk.panel + low + m + j * kBox, bar);
                         }
                         for (int j = 0; j < t.n_boxes; ++j) {
                             void *dst = pb + j * kBoxBytes;
                             if (MODE != 2) load_box(dst, &a.w, b * kK, n + j * kBox, bar);
-                            else if (t.dw) load_box(dst, rows, n + j * kBox, b * kK, bar);
-                            else load_box(dst, &a.w, n + j * kBox, walk.v0 + (t.first + b) * kK, bar);
+                            else if (t.dw) load_box(dst, rows, n + j * kBox, k0 * kK, bar);
+                            else load_box(dst, &a.w, n + j * kBox, walk.v0 + (t.first + k0) * kK, bar);
                         }
                     }
                     __syncwarp();
@@ -575,7 +594,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                 for (int b = 0; b < t.blocks; ++b, ++s) {
                     const int buf = c & 1;
                     const uint32_t d = tmem + buf * kN;
-                    if (b % kChunk == 0 && !(ok = wait.warp(&d_empty[buf], ((uint32_t)(c >> 1) & 1u) ^ 1u))) break;
+                    const bool first = (b & (chunk_of - 1)) == 0, last = (b & (chunk_of - 1)) == chunk_of - 1 || b + 1 == t.blocks;
+                    if (first && !(ok = wait.warp(&d_empty[buf], ((uint32_t)(c >> 1) & 1u) ^ 1u))) break;
                     const int st = s % kStages;
                     if (!(ok = wait.warp(&full[st], (uint32_t)(s / kStages) & 1u))) break;
                     tc::fence_after_sync();
@@ -584,12 +604,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                         const uint64_t da = a_mn ? desc_boxes(pa) : desc_k(pa), db = b_mn ? desc_boxes(pb) : desc_k(pb);
 #pragma unroll
                         for (int x = 0; x < kK / 16; ++x)
-                            pair_mma(d, da + x * step_a, db + x * step_b, id, b % kChunk > 0 || x > 0);
+                            pair_mma(d, da + x * step_a, db + x * step_b, id, !first || x > 0);
                         pair_commit(&empty[st]);
-                        if (b % kChunk == kChunk - 1 || b + 1 == t.blocks) pair_commit(&d_full[buf]);
+                        if (last) pair_commit(&d_full[buf]);
                     }
                     __syncwarp();
-                    if (b % kChunk == kChunk - 1 || b + 1 == t.blocks) ++c;
+                    if (last) ++c;
                 }
             }
         // every product issued ends before the block frees its memory
@@ -676,7 +696,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                         for (int e = 0; e < 32; ++e) acc[j][e] = 0u;
                 }
 #pragma unroll 1
-                for (int b = MODE != 2 ? kChunk : 0; ok && b < t.blocks; b += kChunk) chunk(false);
+                for (int b = MODE != 2 ? chunk_of : 0; ok && b < t.blocks; b += chunk_of) chunk(false);
                 if (!ok) break;
                 auto take = [&](int j, float (&x)[32]) {
 #pragma unroll
@@ -729,6 +749,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                     }
                 } else if constexpr (MODE == 1) {
                     float2 rest = make_float2(0.f, 0.f);
+                    // (FINE: a second pass for what the first one's rounding left off)
+#pragma unroll 1
+                    for (int pass = 0; pass < (FINE && walk.fine ? 2 : 1); ++pass)
 #pragma unroll
                     for (int j = 0; j < kN / 2; j += 64) {
                         uint32_t packed[32];
@@ -757,9 +780,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                             for (int e = 0; e < 32; e += 2) {
                                 const float2 q = mul2(get(x + e), both(part));
                                 packed[(jj + e) / 2] = pack2<T>(q.x, q.y);
+                                if (FINE && pass) {
+                                    const float2 is = add_pair<T>(make_float2(0.f, 0.f), packed[(jj + e) / 2]);
+                                    packed[(jj + e) / 2] = pack2<T>(q.x - is.x, q.y - is.y);
+                                }
                                 some = add_pair<T>(some, packed[(jj + e) / 2]);
                             }
-                            if (BIAS && a.want_db) {
+                            if (BIAS && a.want_db && (!FINE || pass == 0)) {
                                 // The columns' sums over the warp's rows, turned in the buffer that
                                 // the packed values leave from later: a lane takes four columns of eight
                                 // rows.  (In registers alone, 31 shuffles and twice as many selects.)
@@ -802,7 +829,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                         // row is added up anew: p near 1 must not leave its rounding in the sum.
                         if (at0 >= j && at0 < j + 64) {
                             const int e = at0 - j;
-                            reinterpret_cast<T *>(out + lane * 128 + (((e >> 3) ^ (lane & 7)) << 4))[e & 7] = from_f32<T>(q_target * part);
+                            float q = q_target * part;
+                            if (FINE && pass) q -= to_f32<T>(from_f32<T>(q));
+                            reinterpret_cast<T *>(out + lane * 128 + (((e >> 3) ^ (lane & 7)) << 4))[e & 7] = from_f32<T>(q);
                             some = make_float2(0.f, 0.f);
 #pragma unroll 1
                             for (int c8 = 0; c8 < 8; ++c8) {
@@ -814,7 +843,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                         tc::fence_proxy_async_smem();
                         __syncwarp();
                         if (lane == 0) {
-                            store_box(&a.pool_out, 0, (col + j - walk.v0) / kK * walk.mp + t.m0 + r_warp, out);
+                            store_box(&a.pool_out, 0, (col + j - walk.v0) / kK * walk.panel + (FINE && pass ? walk.mp : 0) + t.m0 + r_warp, out);
                             stores_issued();
                         }
                     }
@@ -1067,7 +1096,7 @@ Layout layout(const sieve_cross_entropy_args &a, bool backward) {
         l.part_of = take(n * 4);
         l.whole = take(n * 4);
         l.hs = take(n * a.width * 2);
-        const int64_t needed = np * (round_up(a.classes, kN) / kK), least = np * (kN / kK), most = kPoolBytes / 128;
+        const int64_t needed = panel_rows(n) * (round_up(a.classes, kN) / kK), least = panel_rows(n) * (kN / kK), most = kPoolBytes / 128;
         l.pool_rows = needed < most ? needed : least > most ? least : most;
         l.pool = take(l.pool_rows * 128);
         // (dh_slabs: tiles times slabs stay below two shares for each pair, or there is one slab)
@@ -1082,9 +1111,9 @@ Layout layout(const sieve_cross_entropy_args &a, bool backward) {
     return l;
 }
 
-template <typename T, int MODE, bool BIAS>
+template <typename T, int MODE, bool BIAS, bool FINE = false>
 cudaError_t run(const XentArgs &a, int piece, cudaStream_t st) {
-    auto kernel = k_xent<T, MODE, BIAS>;
+    auto kernel = k_xent<T, MODE, BIAS, FINE>;
     // The warps trade registers among each other, which takes all that kRegisters says.
     static const int registers = [&] {
         cudaFuncAttributes f;
@@ -1113,6 +1142,7 @@ sieve_status prepare(Call &c, const sieve_cross_entropy_args &a, const Layout &l
     x.width = a.width;
     x.scale = a.scale;
     x.c = a.scale * kLog2e;
+    x.maybe_fine = a.rows <= kMaybeFine;
     RowArgs &r = c.r;
     r.targets = a.targets;
     r.h = a.h;
@@ -1143,7 +1173,9 @@ void list_rows(const Call &c, cudaStream_t st) {
 template <typename T>
 cudaError_t forward(const Call &c, const JoinArgs &j, cudaStream_t st) {
     list_rows<T>(c, st);
-    cudaError_t e = c.x.bias ? run<T, 0, true>(c.x, 0, st) : run<T, 0, false>(c.x, 0, st);
+    cudaError_t e;
+    if (c.x.maybe_fine) e = c.x.bias ? run<T, 0, true, true>(c.x, 0, st) : run<T, 0, false, true>(c.x, 0, st);
+    else e = c.x.bias ? run<T, 0, true>(c.x, 0, st) : run<T, 0, false>(c.x, 0, st);
     if (e != cudaSuccess) return e;
     const int64_t blocks = ceil_div(c.x.rows, 32);
     k_xent_join<<<(unsigned)(blocks < 4096 ? blocks : 4096), 32 * kStrands, 0, st>>>(j);
@@ -1154,7 +1186,9 @@ template <typename T>
 cudaError_t backward(const Call &c, const sieve_cross_entropy_grads &g, const DhArgs &d, int pieces, cudaStream_t st) {
     list_rows<T>(c, st);
     for (int p = 0; p < pieces; ++p) {
-        cudaError_t e = c.x.bias ? run<T, 1, true>(c.x, p, st) : run<T, 1, false>(c.x, p, st);
+        cudaError_t e;
+        if (c.x.maybe_fine) e = c.x.bias ? run<T, 1, true, true>(c.x, p, st) : run<T, 1, false, true>(c.x, p, st);
+        else e = c.x.bias ? run<T, 1, true>(c.x, p, st) : run<T, 1, false>(c.x, p, st);
         if (e == cudaSuccess && (g.dh || g.dweight)) e = run<T, 2, false>(c.x, p, st);
         if (e != cudaSuccess) return e;
     }
