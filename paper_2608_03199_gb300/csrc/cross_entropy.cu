@@ -213,6 +213,7 @@ __global__ void __launch_bounds__(kRowTile) k_xent_rows(const RowArgs a) {
     constexpr int kWarps = kRowTile / 32;
     __shared__ int s_before[kWarps], s_all[kWarps], s_rank[kWarps], s_list[kRowTile];
     __shared__ uint32_t s_top[kWarps], s_low[kWarps];
+    after_previous();
     constexpr int kMine = kRowTile / SUB;            // rows of this block, from first on in its tile
     const int tile = (int)blockIdx.x / SUB, tiles = (int)gridDim.x / SUB, first = (int)blockIdx.x % SUB * kMine;
     const int tid = threadIdx.x, lane = lane_id(), warp = tid >> 5;
@@ -511,6 +512,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
     __shared__ uint32_t tmem_slot;
     __shared__ int s_abort;
     __shared__ __align__(16) float s_bias[kEpiWarps][BIAS ? kN / 2 : 4];
+    after_previous();
     const Walk<MODE> walk(a, piece);
     if (walk.total == 0) return;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = lane_id();
@@ -931,6 +933,7 @@ constexpr int kStrands = 16;
 
 __global__ void __launch_bounds__(32 * kStrands) k_xent_join(const JoinArgs a) {
     __shared__ float2 s_part[kStrands][32];
+    after_previous();
     const int lane = lane_id(), strand = threadIdx.x >> 5;
     const int n = a.ctl->n;
     const int group = group_tiles(n, a.classes), tiles = (a.classes + kN - 1) / kN;
@@ -1008,6 +1011,7 @@ struct DhArgs {
 template <typename T>
 __global__ void __launch_bounds__(32 * kStrands) k_xent_dh(const DhArgs a) {
     __shared__ float s_rest[kStrands][32];
+    after_previous();
     const int lane = lane_id(), strand = threadIdx.x >> 5, n = a.ctl->n, chunks = a.width / 8;
     const int64_t mp = padded(n);
     const int parts = (a.classes + kN - 1) / kN * 2;
@@ -1050,6 +1054,7 @@ __global__ void __launch_bounds__(32 * kStrands) k_xent_dh(const DhArgs a) {
 // dbias from the column sums of every 32 rows: 32 columns by 8 strands.
 __global__ void __launch_bounds__(256) k_xent_db(const Ctl *ctl, const float *colsum, int classes, float *db) {
     __shared__ float part[8][32];
+    after_previous();
     const int lane = lane_id(), strand = threadIdx.x >> 5, v = blockIdx.x * 32 + lane;
     const int sums = (ctl->n + kM - 1) / kM * (kM / 32);
     float s = 0.f;
@@ -1122,8 +1127,7 @@ cudaError_t run(const XentArgs &a, int piece, cudaStream_t st) {
     if (registers != kRegisters) return cudaErrorInvalidDeviceFunction;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(MODE));
     if (e != cudaSuccess) return e;
-    kernel<<<kGrid, kThreads, smem_bytes(MODE), st>>>(a, piece);
-    return cudaGetLastError();
+    return launch_next(kernel, kGrid, kThreads, smem_bytes(MODE), st, a, piece);
 }
 
 struct Call {
@@ -1164,29 +1168,30 @@ sieve_status prepare(Call &c, const sieve_cross_entropy_args &a, const Layout &l
 }
 
 template <typename T>
-void list_rows(const Call &c, cudaStream_t st) {
+cudaError_t list_rows(const Call &c, cudaStream_t st) {
     k_xent_count<<<c.blocks, kRowTile, 0, st>>>(c.r);
-    if (c.x.rows <= kFewRows) k_xent_rows<T, 8><<<c.blocks * 8, kRowTile, 0, st>>>(c.r);
-    else k_xent_rows<T, 1><<<c.blocks, kRowTile, 0, st>>>(c.r);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    if (c.x.rows <= kFewRows) return launch_next(k_xent_rows<T, 8>, c.blocks * 8, kRowTile, 0, st, c.r);
+    return launch_next(k_xent_rows<T, 1>, c.blocks, kRowTile, 0, st, c.r);
 }
 
 template <typename T>
 cudaError_t forward(const Call &c, const JoinArgs &j, cudaStream_t st) {
-    list_rows<T>(c, st);
-    cudaError_t e;
+    cudaError_t e = list_rows<T>(c, st);
+    if (e != cudaSuccess) return e;
     if (c.x.maybe_fine) e = c.x.bias ? run<T, 0, true, true>(c.x, 0, st) : run<T, 0, false, true>(c.x, 0, st);
     else e = c.x.bias ? run<T, 0, true>(c.x, 0, st) : run<T, 0, false>(c.x, 0, st);
     if (e != cudaSuccess) return e;
     const int64_t blocks = ceil_div(c.x.rows, 32);
-    k_xent_join<<<(unsigned)(blocks < 4096 ? blocks : 4096), 32 * kStrands, 0, st>>>(j);
-    return cudaGetLastError();
+    return launch_next(k_xent_join, (unsigned)(blocks < 4096 ? blocks : 4096), 32 * kStrands, 0, st, j);
 }
 
 template <typename T>
 cudaError_t backward(const Call &c, const sieve_cross_entropy_grads &g, const DhArgs &d, int pieces, cudaStream_t st) {
-    list_rows<T>(c, st);
+    cudaError_t e = list_rows<T>(c, st);
+    if (e != cudaSuccess) return e;
     for (int p = 0; p < pieces; ++p) {
-        cudaError_t e;
         if (c.x.maybe_fine) e = c.x.bias ? run<T, 1, true, true>(c.x, p, st) : run<T, 1, false, true>(c.x, p, st);
         else e = c.x.bias ? run<T, 1, true>(c.x, p, st) : run<T, 1, false>(c.x, p, st);
         if (e == cudaSuccess && (g.dh || g.dweight)) e = run<T, 2, false>(c.x, p, st);
@@ -1194,11 +1199,12 @@ cudaError_t backward(const Call &c, const sieve_cross_entropy_grads &g, const Dh
     }
     if (g.dh) {
         const int64_t blocks = ceil_div(c.x.rows, 32);
-        k_xent_dh<T><<<(unsigned)(blocks < 4096 ? blocks : 4096), 32 * kStrands, 0, st>>>(d);
+        e = launch_next(k_xent_dh<T>, (unsigned)(blocks < 4096 ? blocks : 4096), 32 * kStrands, 0, st, d);
+        if (e != cudaSuccess) return e;
     }
     if (g.dbias)
-        k_xent_db<<<(unsigned)ceil_div(c.x.classes, 32), 256, 0, st>>>(c.x.ctl, c.x.colsum, c.x.classes, g.dbias);
-    return cudaGetLastError();
+        return launch_next(k_xent_db, (unsigned)ceil_div(c.x.classes, 32), 256, 0, st, c.x.ctl, c.x.colsum, c.x.classes, g.dbias);
+    return cudaSuccess;
 }
 
 }  // namespace

@@ -110,6 +110,7 @@ __device__ __forceinline__ int sort_key(const Sort &s, int i) {
 
 __global__ void __launch_bounds__(kSortThreads) k_sort_count(const Sort s) {
     __shared__ int bins[kMaxDigits];
+    after_previous();
     const int n = 1 << s.bits;
     if (blockIdx.x == 0 && threadIdx.x == 0 && !s.key_in) *s.joins = 0;
     for (int i = threadIdx.x; i < n; i += kSortThreads) bins[i] = 0;
@@ -126,6 +127,7 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(const Sort s) {
     __shared__ int start[kMaxDigits];              // where the tile's next token of a digit goes
     __shared__ int of_warp[kSortWarps][kMaxDigits];
     __shared__ int sums[kSortWarps];
+    after_previous();
     const int n = 1 << s.bits, tid = threadIdx.x, lane = lane_id(), warp = tid >> 5;
     // digit tid: tokens of it in all tiles, and in the tiles before this one
     int all = 0, before = 0;
@@ -263,6 +265,7 @@ template <typename T, typename G, int VEC, int NC>
 __global__ void __launch_bounds__(kPieceWarps * 32) k_embed_sums(const Sums s) {
     const EmbedArgs &a = s.a;
     const int lane = lane_id(), warp = threadIdx.x >> 5;
+    after_previous();
     if ((int)blockIdx.x >= s.sum_blocks) {
         // ---- the zeros of rows that no token has
         __shared__ int range[2];
@@ -359,6 +362,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_embed_join(const Sums s) {
     __shared__ int shared_end, found[kStrands], long_piece[kJoinThreads];
     const EmbedArgs &a = s.a;
     const int lane = lane_id(), warp = threadIdx.x >> 5;
+    after_previous();
     const int joins = *s.joins;
     auto write = [&](int id, int col, float v) {
         G *to = static_cast<G *>(a.dtable) + id * a.dtable_stride + col;
@@ -540,11 +544,12 @@ cudaError_t launch_embed_backward(const EmbedArgs &a, void *ws, cudaStream_t st)
         s.val_in = pass ? ints(l.val[(pass + 1) & 1]) : nullptr;
         s.key_out = ints(l.key[pass & 1]);
         s.val_out = ints(l.val[pass & 1]);
-        k_sort_count<<<s.tiles, kSortThreads, 0, st>>>(s);
-        k_sort_scatter<<<s.tiles, kSortThreads, 0, st>>>(s);
+        cudaError_t e = cudaSuccess;
+        if (pass == 0) k_sort_count<<<s.tiles, kSortThreads, 0, st>>>(s);
+        else e = launch_next(k_sort_count, s.tiles, kSortThreads, 0, st, s);
+        if (e == cudaSuccess) e = launch_next(k_sort_scatter, s.tiles, kSortThreads, 0, st, s);
+        if (e != cudaSuccess || (e = cudaGetLastError()) != cudaSuccess) return e;
     }
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
     Sums u = {};
     u.a = a;
     u.key = ints(l.key[(shape.passes - 1) & 1]);
@@ -560,11 +565,14 @@ cudaError_t launch_embed_backward(const EmbedArgs &a, void *ws, cudaStream_t st)
         return with_type(a.table_dtype, [&](auto g) {
             using G = typename decltype(g)::type;
             constexpr int V = sizeof(T) == 4 && sizeof(G) == 4 ? 4 : 8;
+            cudaError_t e = cudaSuccess;
             auto launch = [&](auto vec, auto nc) {
                 constexpr int VEC = decltype(vec)::value, NC = decltype(nc)::value;
                 u.sum_blocks = (int)ceil_div((int64_t)u.pieces * ceil_div(u.slices, NC), kPieceWarps);
                 const unsigned blocks = (unsigned)(u.sum_blocks + zero_blocks);
-                if (blocks) k_embed_sums<T, G, VEC, NC><<<blocks, kPieceWarps * 32, 0, st>>>(u);
+                if (!blocks) return;
+                if (a.tokens > 0) e = launch_next(k_embed_sums<T, G, VEC, NC>, blocks, kPieceWarps * 32, 0, st, u);
+                else k_embed_sums<T, G, VEC, NC><<<blocks, kPieceWarps * 32, 0, st>>>(u);      // the first of its call
             };
             using One = std::integral_constant<int, 1>;
             // More columns a lane where there are pieces enough to fill the SMs: less work
@@ -579,8 +587,8 @@ cudaError_t launch_embed_backward(const EmbedArgs &a, void *ws, cudaStream_t st)
                 launch(std::integral_constant<int, V>{}, std::integral_constant<int, 3>{});
             else
                 launch(std::integral_constant<int, V>{}, std::integral_constant<int, 2>{});
-            if (a.tokens > kPiece) k_embed_join<G><<<kJoinBlocks, kStrands * 32, 0, st>>>(u);
-            return cudaGetLastError();
+            if (e == cudaSuccess && a.tokens > kPiece) e = launch_next(k_embed_join<G>, kJoinBlocks, kJoinThreads, 0, st, u);
+            return e == cudaSuccess ? cudaGetLastError() : e;
         });
     });
 }

@@ -379,6 +379,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR, blocks_per_s
 template <typename W>
 __global__ void __launch_bounds__(1024) k_residual_reduce(const ResidualNormArgs p, int groups) {
     __shared__ float part[2][32][33];
+    after_previous();
     const sieve_residual_norm_args &a = p.a;
     const int lane = threadIdx.x & 31, strand = threadIdx.x >> 5;
     const int col = blockIdx.x * 32 + lane;
@@ -517,7 +518,9 @@ cudaError_t backward(const ResidualNormArgs &p, cudaStream_t st) {
                                                 : backward_as<T, W, 1, 1024, 8>(p, q.blocks, st);
         if (e != cudaSuccess) return e;
     }
-    k_residual_reduce<W><<<dim3((unsigned)ceil_div(p.a.width, 32), 2), 1024, 0, st>>>(p, q.groups);
+    const dim3 grid((unsigned)ceil_div(p.a.width, 32), 2);
+    if (q.blocks > 0) return launch_next(k_residual_reduce<W>, grid, 1024, 0, st, p, q.groups);
+    k_residual_reduce<W><<<grid, 1024, 0, st>>>(p, q.groups);          // the first of its call
     return cudaGetLastError();
 }
 

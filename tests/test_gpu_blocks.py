@@ -605,3 +605,43 @@ def test_calls_with_an_explicit_stream():
            *sieve.cross_entropy(h, weight, t, bias=b, stream=s, check=True))
     s.synchronize()
     assert all(torch.equal(x, z) for x, z in zip(want, got))
+
+
+# ------------------------------------------------------------------ example
+def test_example_trains_on_masked_tokens():
+    """The example runs, and its gradients are those of torch's autograd in 64
+    bits on the same weights: some 25 roundings to bf16 (2^-8 each) lie between the
+    ids and the farthest gradient and add up like independent ones, 5 * 2^-8 of the
+    norm, taken twice."""
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import train_masked_tokens as example
+    got = example.main(["--docs", "300", "--vocab", "2000", "--steps", "2"])
+    assert torch.allclose(got["rows"].norm(dim=1), torch.ones(300, device=DEV), atol=1e-5) and len(got["losses"]) == 2
+    model = example.Encoder(150, torch.device(DEV), seed=3)
+    ids, offsets = example.documents(9, 150, torch.device(DEV), seed=4)
+    hidden, targets = example.masked(ids, 0.3, seed=5)
+    loss, grads = model.loss_and_grads(hidden, targets, offsets)
+    p = {k: (v.bfloat16() if k.startswith("w_") or k == "table" else v).double().requires_grad_() for k, v in model.p.items()}
+    width, heads, dim, reach = example.WIDTH, example.HEADS, example.DIM, example.REACH
+
+    def rms(x, w):
+        return x / (x.square().mean(1, keepdim=True) + 1e-5).sqrt() * w
+    h0 = p["table"][hidden] * math.sqrt(width)
+    x0 = torch.nn.functional.layer_norm(h0, (width,), p["norm0"])
+    q, k, v = (x0 @ p["w_qkv"]).view(-1, 3, heads, dim).unbind(1)
+    parts = []
+    for a, b in zip(offsets.tolist(), offsets.tolist()[1:]):
+        place = torch.arange(b - a, device=DEV)
+        at = model.buckets.long()[(place[None] - place[:, None]).clamp(-reach, reach) + reach]
+        s = torch.einsum("ihd,jhd->hij", q[a:b], k[a:b]) * dim ** -0.5 + p["rel"][at].permute(2, 0, 1)
+        parts.append(torch.einsum("hij,jhd->ihd", torch.softmax(s, 2), v[a:b]))
+    h1 = h0 + p["gate0"] * rms(torch.cat(parts).reshape(-1, heads * dim) @ p["w_o"], p["post0"])
+    y1 = torch.relu(rms(h1, p["norm1"]) @ p["w_up"]) @ p["w_down"]
+    x2 = rms(h1 + p["gate1"] * rms(y1, p["post1"]), p["norm2"])
+    want = torch.nn.functional.cross_entropy(x2 @ p["table"].T + p["out_bias"], targets, ignore_index=-1)
+    assert abs(float(loss) - float(want)) < 2.0 ** -6 * float(want)
+    for name, t in zip(p, torch.autograd.grad(want, list(p.values()))):
+        off = float((grads[name].double() - t).norm() / t.norm())
+        assert off < 10 * 2.0 ** -8, (name, off)
