@@ -39,7 +39,7 @@
 //
 // The tensor cores cut a sum off at every step of 16 products instead of
 // rounding it, which leaves a score of 2,048 products off by a few 1e-6 of itself, all to
-// one side.  So a contraction runs in chunks (256 products of a score, 4,096 of
+// one side.  So a contraction runs in chunks (256 or 384 products of a score, 4,096 of
 // a gradient) whose sums are added up in registers.
 //
 // A row's q add up to zero, its rounded q to some e.  Where the likely classes
@@ -506,7 +506,9 @@ struct Walk {
 template <typename T, int MODE, bool BIAS, bool FINE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ XentArgs a, int piece) {
     constexpr int kStages = stages(MODE);
-    const int chunk_of = MODE == 2 ? 64 : FINE && a.ctl->n <= kFine ? 2 : 4;      // stages of a chunk
+    // stages of a chunk (past 512 columns six: two buffers then hold the next tile's
+    // products for as long as this one's q take)
+    const int chunk_of = MODE == 2 ? 64 : FINE && a.ctl->n <= kFine ? 2 : a.width > 8 * kK ? 6 : 4;
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t full[kStages], empty[kStages], d_full[2], d_empty[2], drained;
     __shared__ uint32_t tmem_slot;
@@ -593,10 +595,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                 const uint32_t id = product<T>(2 * t.n_boxes * kBox, a_mn, b_mn);
                 const uint64_t step_a = a_mn ? 128 : 2, step_b = b_mn ? 128 : 2;
 #pragma unroll 1
-                for (int b = 0; b < t.blocks; ++b, ++s) {
+                for (int b = 0, in = 0; b < t.blocks; ++b, ++s) {
                     const int buf = c & 1;
                     const uint32_t d = tmem + buf * kN;
-                    const bool first = (b & (chunk_of - 1)) == 0, last = (b & (chunk_of - 1)) == chunk_of - 1 || b + 1 == t.blocks;
+                    const bool first = in == 0, last = in + 1 == chunk_of || b + 1 == t.blocks;
                     if (first && !(ok = wait.warp(&d_empty[buf], ((uint32_t)(c >> 1) & 1u) ^ 1u))) break;
                     const int st = s % kStages;
                     if (!(ok = wait.warp(&full[st], (uint32_t)(s / kStages) & 1u))) break;
@@ -611,6 +613,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                         if (last) pair_commit(&d_full[buf]);
                     }
                     __syncwarp();
+                    in = last ? 0 : in + 1;
                     if (last) ++c;
                 }
             }
