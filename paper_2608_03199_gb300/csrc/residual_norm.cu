@@ -20,6 +20,14 @@
 // where every row has its own.  All weights' gradients follow from these after
 // the rows: a column gate w is a common factor, dpost_weight = w C, dpost_bias = w D,
 // dgate = post_weight C + post_bias D.
+//
+// Measured (device time).  Forward: 200,003 x 1,024 bf16, rms 269 us (1.64 GB, 6.1 TB/s);
+// 100,003 x 768 bf16 with both biases 113 us (614 MB, 5.4 TB/s).  Backward: 100,003 x 768 bf16
+// 227 us (922 MB, 4.1 TB/s) and 6 for the weights: a row's threads meet twice, and 128
+// registers a thread leave five blocks an SM to hide it.  Tried there: 112 registers and six
+// blocks 333 us (spills), rows copied to shared memory three ahead 297.  Odd rows, element by
+// element: 20,011 x 1,001 fp32 with a gate for each element forward 103 us (401 MB, 3.9 TB/s),
+// backward 152 (641 MB, 4.2 TB/s).
 #include <type_traits>
 
 #include "blocks.cuh"
