@@ -395,6 +395,44 @@ def test_cross_entropy_not_a_number_stays_in_its_row_of_dh():
     assert dh[7].isnan().all() and torch.equal(dh[rest], clean[rest]) and dw.isnan().any()
 
 
+def test_calls_that_follow_at_once_and_share_scratch():
+    """Calls of different sizes one after the other on one workspace, without a
+    wait between them: each one's kernels start while the ones before end, and give
+    the bits they give alone."""
+    g = gen(18)
+    ws = sieve.Workspace()
+    sizes = [(700, 3_000, 1.0), (40, 90, 0.5), (2_300, 513, 0.2), (1, 20_000, 1.0), (300, 7, 0.0)]
+    inputs = [loss_inputs(g, n, v, 64, BF16, live, True) for n, v, live in sizes]
+
+    def calls(x, workspace):
+        h, weight, t, bias = x
+        loss, lse = sieve.cross_entropy(h, weight, t, bias=bias, workspace=workspace)
+        grads = sieve.cross_entropy_backward(torch.full_like(loss, 0.5), h, weight, t, loss, lse, bias=bias, workspace=workspace)
+        table = sieve.embed_backward(grads[0], t, len(weight), workspace=workspace)
+        stream, x, stats = sieve.residual_norm(h, grads[0], torch.ones(64, device=DEV))
+        back = sieve.residual_norm_backward(h, grads[0], h, grads[0], stats, torch.ones(64, device=DEV), workspace=workspace)
+        return (loss, lse, *grads, table, stream, x, *(t for t in back if t is not None))
+    want = []
+    for x in inputs:
+        want.append(calls(x, None))
+        torch.cuda.synchronize()
+    calls(inputs[2], ws)                                 # the workspace as large as any of them needs
+    for _ in range(6):
+        got = [calls(x, ws) for x in inputs]
+    for x, y in zip(got, want):
+        assert all(torch.equal(a, b) for a, b in zip(x, y))
+
+
+def test_cross_entropy_bias_gradient_alone():
+    g = gen(19)
+    h, weight, t, b = loss_inputs(g, 500, 900, 64, FP16, 0.7, True)
+    loss, lse = sieve.cross_entropy(h, weight, t, bias=b)
+    kw = dict(bias=b)
+    want = sieve.cross_entropy_backward(loss, h, weight, t, loss, lse, **kw)[2]
+    dh, dw, db = sieve.cross_entropy_backward(loss, h, weight, t, loss, lse, need_dh=False, need_dweight=False, check=True, **kw)
+    assert dh is None and dw is None and torch.equal(db, want)
+
+
 def test_cross_entropy_twice_at_once():
     """Two calls on two streams, each with its own scratch, give what they
     give alone."""
