@@ -229,7 +229,7 @@ __global__ void __launch_bounds__(kRowTile) k_xent_rows(const RowArgs a) {
     int before = 0, all = 0;
     uint32_t top = 0, low = 0xffffffffu;
 #pragma unroll 4
-    for (int b = tid; b < tiles; b += kRowTile) {
+    for (int b = tid; tiles > 1 && b < tiles; b += kRowTile) {
         const int c = a.count[b];
         all += c;
         if (b < tile) before += c;
@@ -238,12 +238,16 @@ __global__ void __launch_bounds__(kRowTile) k_xent_rows(const RowArgs a) {
             low = min(low, a.low[b]);
         }
     }
+    const int64_t r = (int64_t)tile * kRowTile + tid;
+    const int t = r < a.rows ? id_at(a.targets, a.target_type, r, a.classes) : -1;
+    if (tiles == 1) {            // one tile: nothing was counted before
+        all = t >= 0;
+        if (a.dloss && t >= 0) top = low = ordered(a.dloss[r]);
+    }
     before = __reduce_add_sync(0xffffffffu, before);
     all = __reduce_add_sync(0xffffffffu, all);
     top = __reduce_max_sync(0xffffffffu, top);
     low = __reduce_min_sync(0xffffffffu, low);
-    const int64_t r = (int64_t)tile * kRowTile + tid;
-    const int t = r < a.rows ? id_at(a.targets, a.target_type, r, a.classes) : -1;
     const unsigned live = __ballot_sync(0xffffffffu, t >= 0);
     if (lane == 0) {
         s_before[warp] = before;
@@ -1181,6 +1185,10 @@ sieve_status prepare(Call &c, const sieve_cross_entropy_args &a, const Layout &l
 
 template <typename T>
 cudaError_t list_rows(const Call &c, cudaStream_t st) {
+    if (c.blocks == 1) {
+        k_xent_rows<T, 8><<<8, kRowTile, 0, st>>>(c.r);
+        return cudaGetLastError();
+    }
     k_xent_count<<<c.blocks, kRowTile, 0, st>>>(c.r);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;

@@ -83,6 +83,20 @@ __global__ void __launch_bounds__(kThreads) k_embed(const EmbedArgs a, int token
     }
 }
 
+// Rows of single elements: a warp to a token, so that no element needs a division to
+// find its place.
+template <typename T, typename O>
+__global__ void __launch_bounds__(kThreads) k_embed_odd(const EmbedArgs a) {
+    const int lane = lane_id();
+    const int64_t token = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+    if (token >= a.tokens) return;
+    const int id = id_at(a.ids, a.id_type, token, a.vocab);
+    const T *row = static_cast<const T *>(a.table) + (id < 0 ? 0 : id) * a.table_stride;
+    O *out = static_cast<O *>(a.out) + token * a.out_stride;
+#pragma unroll 8
+    for (int col = lane; col < a.width; col += 32) out[col] = from_f32<O>(id < 0 ? 0.f : a.scale * to_f32<T>(__ldg(row + col)));
+}
+
 // ---------------------------------------------------------------------------
 // The sort: passes over digits of up to 9 bits, the lowest first.  The list is
 // cut into `tiles` pieces of `per` tokens; k_sort_count counts every tile's
@@ -522,7 +536,8 @@ cudaError_t launch_embed(const EmbedArgs &a, cudaStream_t st) {
             const int per = chunks >= 1024 ? 1 : 1024 / chunks;
             const unsigned blocks = (unsigned)ceil_div(a.tokens, per);
             if (wide) k_embed<T, O, V><<<blocks, kThreads, 0, st>>>(a, per, chunks);
-            else k_embed<T, O, 1><<<blocks, kThreads, 0, st>>>(a, per, chunks);
+            else if (chunks < 32) k_embed<T, O, 1><<<blocks, kThreads, 0, st>>>(a, per, chunks);
+            else k_embed_odd<T, O><<<(unsigned)ceil_div(a.tokens, kThreads / 32), kThreads, 0, st>>>(a);
             return cudaGetLastError();
         });
     });
