@@ -23,13 +23,15 @@
 //
 // Measured (device time).  Forward: 200,003 x 1,024 bf16, rms 269 us (1.64 GB, 6.1 TB/s);
 // 100,003 x 768 bf16 with both biases 113 us (614 MB, 5.4 TB/s).  Backward: 100,003 x 768 bf16
-// 227 us (922 MB, 4.1 TB/s) and 6 for the weights: a row's threads meet twice, and 128
-// registers a thread leave five blocks an SM to hide it.  Tried there: 112 registers and six
-// blocks 333 us (spills), rows copied to shared memory three ahead 297.  Odd rows, element by
-// element: 20,011 x 1,001 fp32 with a gate for each element forward 103 us (401 MB, 3.9 TB/s),
-// backward 152 (641 MB, 4.2 TB/s).
+// 213 us (922 MB, 4.3 TB/s) and 6 for the weights: a row's threads meet twice, and 128
+// registers a thread leave five blocks an SM to hide it.  Tried there, against 228: 112
+// registers and six blocks 333 us (spills), rows copied to shared memory three ahead 297,
+// twice the threads with half the elements 358, two rows to a meeting 305.  Odd rows,
+// element by element: 20,011 x 1,001 fp32 with a gate for each element forward 103 us
+// (401 MB, 3.9 TB/s), backward 149 (641 MB, 4.3 TB/s).
 #include <type_traits>
 
+#include "attention.cuh"
 #include "blocks.cuh"
 
 namespace sieve {
@@ -51,6 +53,70 @@ struct Piece {      // VEC elements as loaded
     __device__ __forceinline__ void clear() { v = make_uint4(0, 0, 0, 0); }
     __device__ __forceinline__ float get(int i) const { return to_f32<T>(reinterpret_cast<const T *>(&v)[i]); }
 };
+
+// VEC values, two to an instruction where there are two (the backward pass of 100,003 x
+// 768 bf16: 213 us, 228 one by one)
+template <int VEC>
+struct Vals {
+    float v[VEC];
+    template <typename F2, typename F1>
+    static __device__ __forceinline__ Vals by(F2 two, F1 one) {
+        Vals r;
+        if constexpr (VEC == 1) {
+            r.v[0] = one(0);
+        } else {
+#pragma unroll
+            for (int e = 0; e < VEC; e += 2) {
+                const float2 x = two(e);
+                r.v[e] = x.x;
+                r.v[e + 1] = x.y;
+            }
+        }
+        return r;
+    }
+    __device__ __forceinline__ float2 two(int e) const { return make_float2(v[e], v[VEC == 1 ? 0 : e + 1]); }
+    static __device__ __forceinline__ Vals all(float x) {
+        Vals r;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) r.v[e] = x;
+        return r;
+    }
+    template <typename T>
+    static __device__ __forceinline__ Vals of(const Piece<T, VEC> &p) {
+        Vals r;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) r.v[e] = p.get(e);
+        return r;
+    }
+    template <typename W>
+    static __device__ __forceinline__ Vals at(const W *p) {
+        Vals r;
+        load_vec<W, VEC>(p, r.v);
+        return r;
+    }
+    __device__ __forceinline__ float sum() const {
+        if constexpr (VEC == 1) {
+            return v[0];
+        } else {
+            float2 s = two(0);
+#pragma unroll
+            for (int e = 2; e < VEC; e += 2) s = add2(s, two(e));
+            return s.x + s.y;
+        }
+    }
+};
+template <int VEC>
+__device__ __forceinline__ Vals<VEC> operator*(const Vals<VEC> &a, const Vals<VEC> &b) {
+    return Vals<VEC>::by([&](int e) { return mul2(a.two(e), b.two(e)); }, [&](int e) { return a.v[e] * b.v[e]; });
+}
+template <int VEC>
+__device__ __forceinline__ Vals<VEC> operator+(const Vals<VEC> &a, const Vals<VEC> &b) {
+    return Vals<VEC>::by([&](int e) { return add2(a.two(e), b.two(e)); }, [&](int e) { return a.v[e] + b.v[e]; });
+}
+template <int VEC>
+__device__ __forceinline__ Vals<VEC> fma(const Vals<VEC> &a, const Vals<VEC> &b, const Vals<VEC> &c) {
+    return Vals<VEC>::by([&](int e) { return fma2(a.two(e), b.two(e), c.two(e)); }, [&](int e) { return fmaf(a.v[e], b.v[e], c.v[e]); });
+}
 
 // sum over the TPR threads of a row: a warp, or the block
 template <int TPR>
@@ -169,7 +235,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR, TPR == 32 ? (NCH * VEC 
 constexpr int kWarpRows = 4;
 __host__ __device__ constexpr int groups_of(int tpr) { return tpr == 32 ? kWarpRows : 1; }
 // Blocks that share an SM: 512 threads of 128 registers where a thread has 8
-// elements of a row (576 of 112 spill: 100,003 x 768 bf16 236 -> 333 us), 768 of 80
+// elements of a row (576 of 112 spill: 100,003 x 768 bf16 333 us against 228), 768 of 80
 // where it has 4.
 __host__ __device__ constexpr int blocks_per_sm(int tpr, int elements) {
     const int threads = tpr == 32 ? 32 * kWarpRows : tpr;
@@ -199,7 +265,8 @@ __global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR, blocks_per_s
     auto column = [&](int c) { return (c * TPR + i) * VEC; };
     auto in = [&](int c) { return column(c) < width; };
     auto place = [&](int c) { return min(column(c), width - VEC); };
-    float sum[kShared ? 1 : 4][NCH][VEC];
+    using V = Vals<VEC>;
+    V sum[kShared ? 1 : 4][NCH];
     if constexpr (kShared) {
         for (int c = i; c < 4 * width; c += TPR) acc[c] = 0.f;
         __syncthreads();
@@ -207,15 +274,25 @@ __global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR, blocks_per_s
 #pragma unroll
         for (int k = 0; k < 4; ++k)
 #pragma unroll
-            for (int c = 0; c < NCH; ++c)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) sum[k][c][e] = 0.f;
+            for (int c = 0; c < NCH; ++c) sum[k][c] = V::all(0.f);
     }
-    auto add = [&](int k, int c, int e, float v) {
+    // a product, or a value, added to sum k
+    auto add_product = [&](int k, int c, const V &x, const V &y) {
         if constexpr (kShared) {
-            if (in(c)) acc[k * width + column(c) + e] += v;
+            if (in(c))
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) acc[k * width + column(c) + e] += x.v[e] * y.v[e];
         } else {
-            sum[k][c][e] += v;
+            sum[k][c] = fma(x, y, sum[k][c]);
+        }
+    };
+    auto add = [&](int k, int c, const V &x) {
+        if constexpr (kShared) {
+            if (in(c))
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) acc[k * width + column(c) + e] += x.v[e];
+        } else {
+            sum[k][c] = sum[k][c] + x;
         }
     };
     // two sums over the row's threads at once
@@ -256,112 +333,69 @@ __global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR, blocks_per_s
     };
     if (group < a.rows) load(group);
     for (int64_t row = group; row < a.rows; row += step) {
-        float uh[NCH][VEC], sh[NCH][VEC], G[NCH][VEC];
+        V uh[NCH], sh[NCH], G[NCH];
         Piece<T, VEC> gr[NCH];
         float s1 = 0.f, s2 = 0.f;
         const float mu1 = n_stats[0], r1 = n_stats[1], mu2 = n_stats[2], r2 = n_stats[3];
 #pragma unroll
         for (int c = 0; c < NCH; ++c) {
             gr[c] = ng[c];
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                uh[c][e] = (ny[c].get(e) - mu1) * r1;
-                G[c][e] = ns[c].get(e);
-            }
+            uh[c] = (V::of(ny[c]) + V::all(-mu1)) * V::all(r1);
+            G[c] = V::of(ns[c]);
             if (!w2) continue;
             // the stream again, then the gradient through its norm
-            float u[VEC], t[VEC];
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) u[e] = uh[c][e];
+            V u = uh[c];
             if (w1) {
-                load_vec<W, VEC>(w1 + place(c), t);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) u[e] *= t[e];
-                if (b1) {
-                    load_vec<W, VEC>(b1 + place(c), t);
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) u[e] += t[e];
-                }
+                if (b1) u = fma(u, V::at(w1 + place(c)), V::at(b1 + place(c)));
+                else u = u * V::at(w1 + place(c));
             }
-            if (gate) {
-                load_vec<W, VEC>(gate + place(c), t);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) u[e] *= t[e];
-            } else if (gate_rows) {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) u[e] *= gr[c].get(e);
-            }
-            load_vec<W, VEC>(w2 + place(c), t);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                sh[c][e] = (fmaf(a.alpha, nh[c].get(e), u[e]) - mu2) * r2;
-                float d = in(c) ? nx[c].get(e) : 0.f;
-                add(0, c, e, d * sh[c][e]);
-                add(1, c, e, d);
-                d *= t[e];
-                s1 += d;
-                s2 = fmaf(d, sh[c][e], s2);
-                G[c][e] = fmaf(r2, d, G[c][e]);
-            }
+            if (gate) u = u * V::at(gate + place(c));
+            else if (gate_rows) u = u * V::of(gr[c]);
+            sh[c] = (fma(V::all(a.alpha), V::of(nh[c]), u) + V::all(-mu2)) * V::all(r2);
+            V d = in(c) ? V::of(nx[c]) : V::all(0.f);
+            add_product(0, c, d, sh[c]);
+            add(1, c, d);
+            d = d * V::at(w2 + place(c));
+            s1 += d.sum();
+            s2 += (d * sh[c]).sum();
+            G[c] = fma(V::all(r2), d, G[c]);
         }
         if (row + step < a.rows) load(row + step);
         if (w2) {
             both_sums(s1, s2);
-            const float m1 = r2 * s1 * centre, m2 = r2 * s2 * inv_n;
+            const V m1 = V::all(-r2 * s1 * centre), m2 = V::all(-r2 * s2 * inv_n);
 #pragma unroll
-            for (int c = 0; c < NCH; ++c)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) G[c][e] -= fmaf(sh[c][e], m2, m1);
+            for (int c = 0; c < NCH; ++c) G[c] = G[c] + fma(sh[c], m2, m1);
         }
         T *dh = static_cast<T *>(g.dh) + row * g.dh_stride, *dy = static_cast<T *>(g.dy) + row * g.dy_stride;
         s1 = s2 = 0.f;
 #pragma unroll
         for (int c = 0; c < NCH; ++c) {
-            float t[VEC], w[VEC];
-            if (w1) load_vec<W, VEC>(w1 + place(c), w);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) t[e] = a.alpha * G[c][e];
-            if (in(c)) store_vec<T, VEC>(dh + column(c), t);
+            if (in(c)) store_vec<T, VEC>(dh + column(c), (V::all(a.alpha) * G[c]).v);
             if (gate_rows) {
-                float b[VEC];
-                if (b1) load_vec<W, VEC>(b1 + place(c), b);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    t[e] = G[c][e] * (w1 ? fmaf(uh[c][e], w[e], b1 ? b[e] : 0.f) : uh[c][e]);
-                    G[c][e] *= gr[c].get(e);
-                }
-                if (in(c)) store_vec<T, VEC>(static_cast<T *>(g.dgate) + row * g.dgate_stride + column(c), t);
+                V u = uh[c];
+                if (w1) u = b1 ? fma(u, V::at(w1 + place(c)), V::at(b1 + place(c))) : u * V::at(w1 + place(c));
+                u = u * G[c];
+                if (in(c)) store_vec<T, VEC>(static_cast<T *>(g.dgate) + row * g.dgate_stride + column(c), u.v);
+                G[c] = G[c] * V::of(gr[c]);
             }
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                add(2, c, e, G[c][e] * uh[c][e]);
-                add(3, c, e, G[c][e]);
-            }
-            if (gate) {
-                load_vec<W, VEC>(gate + place(c), t);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) G[c][e] *= t[e];
-            }
+            add_product(2, c, G[c], uh[c]);
+            add(3, c, G[c]);
+            if (gate) G[c] = G[c] * V::at(gate + place(c));
             if (w1) {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    G[c][e] = in(c) ? G[c][e] * w[e] : 0.f;
-                    s1 += G[c][e];
-                    s2 = fmaf(G[c][e], uh[c][e], s2);
-                }
+                G[c] = in(c) ? G[c] * V::at(w1 + place(c)) : V::all(0.f);
+                s1 += G[c].sum();
+                s2 += (G[c] * uh[c]).sum();
             } else if (in(c)) {
-                store_vec<T, VEC>(dy + column(c), G[c]);
+                store_vec<T, VEC>(dy + column(c), G[c].v);
             }
         }
         if (w1) {
             both_sums(s1, s2);
-            const float m1 = s1 * centre, m2 = s2 * inv_n;
+            const V m1 = V::all(-s1 * centre), m2 = V::all(-s2 * inv_n);
 #pragma unroll
-            for (int c = 0; c < NCH; ++c) {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) G[c][e] = r1 * (G[c][e] - m1 - uh[c][e] * m2);
-                if (in(c)) store_vec<T, VEC>(dy + column(c), G[c]);
-            }
+            for (int c = 0; c < NCH; ++c)
+                if (in(c)) store_vec<T, VEC>(dy + column(c), (V::all(r1) * (G[c] + fma(uh[c], m2, m1))).v);
         }
     }
     float *out = p.partial + group * 4 * width;
@@ -376,7 +410,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR, blocks_per_s
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
                     const int col = (c * TPR + i) * VEC + e;
-                    if (col < width) out[k * width + col] = sum[k][c][e];
+                    if (col < width) out[k * width + col] = sum[k][c].v[e];
                 }
     }
 }
