@@ -51,6 +51,16 @@ cudaError_t launch_next(void (*kernel)(P...), dim3 grid, int threads, size_t sme
     return cudaLaunchKernelEx(&how, kernel, P(args)...);
 }
 
+// two values of a word
+template <typename T>
+__device__ __forceinline__ float2 unpack2(uint32_t w);
+template <>
+__device__ __forceinline__ float2 unpack2<__half>(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
+template <>
+__device__ __forceinline__ float2 unpack2<__nv_bfloat16>(uint32_t w) {
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+
 struct EmbedArgs {
     const void *ids, *table, *dout;
     void *out, *dtable;

@@ -17,6 +17,7 @@
 // sums 76 to 82 (398 MB, 4.9 to 5.2 TB/s), the join 18.
 #include <type_traits>
 
+#include "attention.cuh"
 #include "blocks.cuh"
 
 namespace sieve {
@@ -40,21 +41,28 @@ struct Chunk {
             for (int i = 0; i < kWords; ++i) w[i] = __ldg(reinterpret_cast<const uint4 *>(p) + i);
         }
     }
-    __device__ __forceinline__ float get(int e) const {
-        return to_f32<T>(reinterpret_cast<const T *>(w)[e]);
+    // values e and e + 1
+    __device__ __forceinline__ float2 two(int e) const {
+        static_assert(VEC > 1, "");
+        const uint4 &q = w[e * sizeof(T) / 16];
+        if constexpr (sizeof(T) == 4) return e % 4 ? make_float2(__uint_as_float(q.z), __uint_as_float(q.w)) : make_float2(__uint_as_float(q.x), __uint_as_float(q.y));
+        else return unpack2<T>(e % 8 == 0 ? q.x : e % 8 == 2 ? q.y : e % 8 == 4 ? q.z : q.w);
+    }
+    __device__ __forceinline__ float one() const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[0].x);
+        else return to_f32<T>(__builtin_bit_cast(T, (unsigned short)w[0].x));
     }
 };
 template <typename T, int VEC>
 __device__ __forceinline__ void put(T *p, const float (&v)[VEC]) {
     if constexpr (VEC == 1) {
         *p = from_f32<T>(v[0]);
+    } else if constexpr (sizeof(T) == 2) {
+        static_assert(VEC == 8, "");
+        *reinterpret_cast<uint4 *>(p) = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
     } else {
-        uint4 w[VEC * sizeof(T) / 16];
-        T *e = reinterpret_cast<T *>(w);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) e[i] = from_f32<T>(v[i]);
-#pragma unroll
-        for (int i = 0; i < (int)(VEC * sizeof(T) / 16); ++i) reinterpret_cast<uint4 *>(p)[i] = w[i];
+        for (int i = 0; i < VEC; i += 4) reinterpret_cast<float4 *>(p)[i / 4] = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
     }
 }
 
@@ -76,8 +84,16 @@ __global__ void __launch_bounds__(kThreads) k_embed(const EmbedArgs a, int token
         if (id >= 0) {
             Chunk<T, VEC> x;
             x.load(table + id * a.table_stride + col);
+            if constexpr (VEC == 1) {
+                v[0] = a.scale * x.one();
+            } else {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) v[e] = a.scale * x.get(e);
+                for (int e = 0; e < VEC; e += 2) {
+                    const float2 t = x.two(e);
+                    v[e] = a.scale * t.x;
+                    v[e + 1] = a.scale * t.y;
+                }
+            }
         }
         put<O, VEC>(out + (first + token) * a.out_stride + col, v);
     }
@@ -243,7 +259,23 @@ struct Row {                            // a lane's columns of a row
         for (int i = 0; i < 8 * NC / VEC; ++i)
             if (column<VEC>(lane, i * VEC) < left) c[i].load(p + column<VEC>(lane, i * VEC));
     }
-    __device__ __forceinline__ float get(int e) const { return c[e / VEC].get(e % VEC); }
+    // added to sums, where there are columns
+    __device__ __forceinline__ void add_to(float (&sum)[8 * NC], int lane, int left) const {
+#pragma unroll
+        for (int i = 0; i < 8 * NC / VEC; ++i) {
+            if (column<VEC>(lane, i * VEC) >= left) continue;
+            if constexpr (VEC == 1) {
+                sum[i] += c[i].one();
+            } else {
+#pragma unroll
+                for (int e = 0; e < VEC; e += 2) {
+                    const float2 s = add2(make_float2(sum[i * VEC + e], sum[i * VEC + e + 1]), c[i].two(e));
+                    sum[i * VEC + e] = s.x;
+                    sum[i * VEC + e + 1] = s.y;
+                }
+            }
+        }
+    }
 };
 // the finished sums of a table row
 template <typename G, int VEC, int NC>
@@ -358,10 +390,7 @@ __global__ void __launch_bounds__(kPieceWarps * 32) k_embed_sums(const Sums s) {
 #pragma unroll
                 for (int e = 0; e < 8 * NC; ++e) sum[e] = 0.f;
             }
-            if (cur < a.vocab)
-#pragma unroll
-                for (int e = 0; e < 8 * NC; ++e)
-                    if (column<VEC>(lane, e) < left) sum[e] += x[u].get(e);
+            if (cur < a.vocab) x[u].add_to(sum, lane, left);
         }
     }
     flush(cur, whole && cur == prev, cur == next);

@@ -22,10 +22,10 @@
 // dgate = post_weight C + post_bias D.
 //
 // Measured (device time).  Forward: 200,003 x 1,024 bf16, rms 269 us (1.64 GB, 6.1 TB/s);
-// 100,003 x 768 bf16 with both biases 113 us (614 MB, 5.4 TB/s).  Backward: 100,003 x 768 bf16
-// 213 us (922 MB, 4.3 TB/s) and 6 for the weights: a row's threads meet twice, and 128
-// registers a thread leave five blocks an SM to hide it.  Tried there, against 228: 112
-// registers and six blocks 333 us (spills), rows copied to shared memory three ahead 297,
+// 100,003 x 768 bf16 with both biases 97 us (614 MB, 6.3 TB/s; 113 with values converted
+// and worked on one by one).  Backward: 100,003 x 768 bf16 202 us (922 MB, 4.6 TB/s; 228 one by
+// one) and 6 for the weights: a row's threads meet twice, and 128 registers a thread
+// leave five blocks an SM to hide it.  Tried there, against 228: 112 registers and six blocks 333 us (spills), rows copied to shared memory three ahead 297,
 // twice the threads with half the elements 358, two rows to a meeting 305.  Odd rows,
 // element by element: 20,011 x 1,001 fp32 with a gate for each element forward 103 us
 // (401 MB, 3.9 TB/s), backward 149 (641 MB, 4.3 TB/s).
@@ -54,8 +54,9 @@ struct Piece {      // VEC elements as loaded
     __device__ __forceinline__ float get(int i) const { return to_f32<T>(reinterpret_cast<const T *>(&v)[i]); }
 };
 
-// VEC values, two to an instruction where there are two (the backward pass of 100,003 x
-// 768 bf16: 213 us, 228 one by one)
+// VEC values, two to an instruction where there are two: both passes are bound by
+// the instructions that they issue as much as by memory (forward 71% of the issue slots,
+// 43 instructions a value, value by value).
 template <int VEC>
 struct Vals {
     float v[VEC];
@@ -84,15 +85,36 @@ struct Vals {
     template <typename T>
     static __device__ __forceinline__ Vals of(const Piece<T, VEC> &p) {
         Vals r;
+        if constexpr (VEC > 1 && sizeof(T) == 2) {
+            const uint32_t w[4] = {p.v.x, p.v.y, p.v.z, p.v.w};
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) r.v[e] = p.get(e);
+            for (int e = 0; e < VEC; e += 2) {
+                const float2 x = unpack2<T>(w[e / 2]);
+                r.v[e] = x.x;
+                r.v[e + 1] = x.y;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) r.v[e] = p.get(e);
+        }
         return r;
     }
     template <typename W>
     static __device__ __forceinline__ Vals at(const W *p) {
-        Vals r;
-        load_vec<W, VEC>(p, r.v);
-        return r;
+        if constexpr (VEC * sizeof(W) == 16) {
+            Piece<W, VEC> x;
+            x.load(p);
+            return of(x);
+        } else {
+            Vals r;
+            load_vec<W, VEC>(p, r.v);
+            return r;
+        }
+    }
+    template <typename T>
+    __device__ __forceinline__ void put(T *p) const {
+        if constexpr (VEC == 8) *reinterpret_cast<uint4 *>(p) = pack8<T>(v);
+        else store_vec<T, VEC>(p, v);
     }
     __device__ __forceinline__ float sum() const {
         if constexpr (VEC == 1) {
@@ -145,36 +167,39 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR, TPR == 32 ? (NCH * VEC 
     const W *w2 = static_cast<const W *>(a.weight), *b2 = static_cast<const W *>(a.bias);
     const int width = a.width;
     const float inv_n = 1.f / (float)width;
-    Piece<T, VEC> hp[NCH];
-    float v[NCH][VEC], s = 0.f;
+    using V = Vals<VEC>;
+    auto column = [&](int c) { return (c * TPR + i) * VEC; };
+    Piece<T, VEC> hp[NCH], yp[NCH];
+    V v[NCH];
+    float s = 0.f;
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
-        const int col = (c * TPR + i) * VEC;
-        Piece<T, VEC> yp;
-        yp.clear();
-        if (col < width) {
-            yp.load(y + col);
-            hp[c].load(h + col);
-        }
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            v[c][e] = yp.get(e);
-            s += v[c][e];
+        yp[c].clear();
+        if (column(c) < width) {
+            yp[c].load(y + column(c));
+            hp[c].load(h + column(c));
         }
     }
-    // mean and factor of v, which is centred; places past the row stay zero
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+        v[c] = V::of(yp[c]);
+        s += v[c].sum();
+    }
+    // mean and factor of v, which is centred; places past the row do not count
     auto normed = [&](float sum, float &mean, float &r) {
         mean = a.rms ? 0.f : row_sum<TPR>(sum, smem) * inv_n;
         float q = 0.f;
 #pragma unroll
-        for (int c = 0; c < NCH; ++c)
-            if ((c * TPR + i) * VEC < width)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    v[c][e] -= mean;
-                    q = fmaf(v[c][e], v[c][e], q);
-                }
+        for (int c = 0; c < NCH; ++c) {
+            v[c] = v[c] + V::all(-mean);
+            if (column(c) < width) q += (v[c] * v[c]).sum();
+        }
         r = 1.f / sqrtf(fmaf(row_sum<TPR>(q, smem), inv_n, a.eps));
+    };
+    // v times the factor and the weight, and the bias
+    auto weighted = [&](const V &x, float r, const W *w, const W *b, int col) {
+        const V z = x * V::all(r);
+        return b ? fma(z, V::at(w + col), V::at(b + col)) : z * V::at(w + col);
     };
     float mean1 = 0.f, r1 = 1.f, mean2 = 0.f, r2 = 1.f;
     if (w1) normed(s, mean1, r1);
@@ -182,43 +207,21 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR, TPR == 32 ? (NCH * VEC 
     T *out = static_cast<T *>(p.stream) + row * p.stream_stride;
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
-        const int col = (c * TPR + i) * VEC;
+        const int col = column(c);
         if (col >= width) continue;
-        if (w1) {
-            float w[VEC], b[VEC];
-            load_vec<W, VEC>(w1 + col, w);
-            if (b1) load_vec<W, VEC>(b1 + col, b);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) v[c][e] = fmaf(v[c][e] * r1, w[e], b1 ? b[e] : 0.f);
-        }
-        if (a.gate_kind != SIEVE_GATE_NONE) {
-            float g[VEC];
-            if (a.gate_kind == SIEVE_GATE_ROW) load_vec<T, VEC>(gate_row + col, g);
-            else load_vec<W, VEC>(gate + col, g);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) v[c][e] *= g[e];
-        }
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            v[c][e] = fmaf(a.alpha, hp[c].get(e), v[c][e]);
-            s += v[c][e];
-        }
-        store_vec<T, VEC>(out + col, v[c]);
+        if (w1) v[c] = weighted(v[c], r1, w1, b1, col);
+        if (a.gate_kind == SIEVE_GATE_ROW) v[c] = v[c] * V::at(gate_row + col);
+        else if (a.gate_kind == SIEVE_GATE_COLUMN) v[c] = v[c] * V::at(gate + col);
+        v[c] = fma(V::all(a.alpha), V::of(hp[c]), v[c]);
+        s += v[c].sum();
+        v[c].put(out + col);
     }
     if (w2) {
         normed(s, mean2, r2);
         T *x = static_cast<T *>(p.x) + row * p.x_stride;
 #pragma unroll
-        for (int c = 0; c < NCH; ++c) {
-            const int col = (c * TPR + i) * VEC;
-            if (col >= width) continue;
-            float w[VEC], b[VEC];
-            load_vec<W, VEC>(w2 + col, w);
-            if (b2) load_vec<W, VEC>(b2 + col, b);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) v[c][e] = fmaf(v[c][e] * r2, w[e], b2 ? b[e] : 0.f);
-            store_vec<T, VEC>(x + col, v[c]);
-        }
+        for (int c = 0; c < NCH; ++c)
+            if (column(c) < width) weighted(v[c], r2, w2, b2, column(c)).put(x + column(c));
     }
     if (p.stats && i == 0) {
         p.stats[row] = mean1;
@@ -371,12 +374,12 @@ __global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR, blocks_per_s
         s1 = s2 = 0.f;
 #pragma unroll
         for (int c = 0; c < NCH; ++c) {
-            if (in(c)) store_vec<T, VEC>(dh + column(c), (V::all(a.alpha) * G[c]).v);
+            if (in(c)) (V::all(a.alpha) * G[c]).put(dh + column(c));
             if (gate_rows) {
                 V u = uh[c];
                 if (w1) u = b1 ? fma(u, V::at(w1 + place(c)), V::at(b1 + place(c))) : u * V::at(w1 + place(c));
                 u = u * G[c];
-                if (in(c)) store_vec<T, VEC>(static_cast<T *>(g.dgate) + row * g.dgate_stride + column(c), u.v);
+                if (in(c)) u.put(static_cast<T *>(g.dgate) + row * g.dgate_stride + column(c));
                 G[c] = G[c] * V::of(gr[c]);
             }
             add_product(2, c, G[c], uh[c]);
@@ -387,7 +390,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR, blocks_per_s
                 s1 += G[c].sum();
                 s2 += (G[c] * uh[c]).sum();
             } else if (in(c)) {
-                store_vec<T, VEC>(dy + column(c), G[c].v);
+                G[c].put(dy + column(c));
             }
         }
         if (w1) {
@@ -395,7 +398,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR, blocks_per_s
             const V m1 = V::all(-s1 * centre), m2 = V::all(-s2 * inv_n);
 #pragma unroll
             for (int c = 0; c < NCH; ++c)
-                if (in(c)) store_vec<T, VEC>(dy + column(c), (V::all(r1) * (G[c] + fma(uh[c], m2, m1))).v);
+                if (in(c)) (V::all(r1) * (G[c] + fma(uh[c], m2, m1))).put(dy + column(c));
         }
     }
     float *out = p.partial + group * 4 * width;
