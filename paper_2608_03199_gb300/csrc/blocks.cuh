@@ -29,26 +29,11 @@ __device__ __forceinline__ int id_at(const void *ids, int id_type, int64_t i, in
     return v >= 0 && v < n ? v : -1;
 }
 
-// Kernels that follow one another in a call.  One launched by launch_next may be
-// set up while the kernel before it still ends: it starts with after_previous(), which
-// waits until everything of that kernel is done and visible.  Saves the 1 to 2 us
-// between two launches.
-__device__ __forceinline__ void after_previous() {
-    asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
-}
+// one kernel after another in a call
 template <typename... P, typename... A>
 cudaError_t launch_next(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, const A &...args) {
-    cudaLaunchAttribute overlap = {};
-    overlap.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    overlap.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t how = {};
-    how.gridDim = grid;
-    how.blockDim = dim3((unsigned)threads);
-    how.dynamicSmemBytes = smem;
-    how.stream = st;
-    how.attrs = &overlap;
-    how.numAttrs = 1;
-    return cudaLaunchKernelEx(&how, kernel, P(args)...);
+    kernel<<<grid, (unsigned)threads, smem, st>>>(P(args)...);
+    return cudaGetLastError();
 }
 
 // two values of a word

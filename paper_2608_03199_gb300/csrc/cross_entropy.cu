@@ -222,7 +222,6 @@ __global__ void __launch_bounds__(kRowTile) k_xent_rows(const RowArgs a) {
     constexpr int kWarps = kRowTile / 32;
     __shared__ int s_before[kWarps], s_all[kWarps], s_rank[kWarps], s_list[kRowTile];
     __shared__ uint32_t s_top[kWarps], s_low[kWarps];
-    after_previous();
     constexpr int kMine = kRowTile / SUB;            // rows of this block, from first on in its tile
     const int tile = (int)blockIdx.x / SUB, tiles = (int)gridDim.x / SUB, first = (int)blockIdx.x % SUB * kMine;
     const int tid = threadIdx.x, lane = lane_id(), warp = tid >> 5;
@@ -527,7 +526,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
     __shared__ uint32_t tmem_slot;
     __shared__ int s_abort;
     __shared__ __align__(16) float s_bias[kEpiWarps][BIAS ? kN / 2 : 4];
-    after_previous();
     const Walk<MODE> walk(a, piece);
     if (walk.total == 0) return;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = lane_id();
@@ -593,6 +591,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                     __syncwarp();
                 }
             }
+        // every release of a stage has arrived before this block leaves
+        for (int j = max(0, s - kStages); ok && j < s; ++j) ok = wait.warp(&empty[j % kStages], (uint32_t)(j / kStages) & 1u);
         if (!ok && rank == 0)      // after an abort: what is in flight (of both) lands before the blocks end
             for (int j = max(0, s - kStages); j < s; ++j) let_land(&full[j % kStages], (uint32_t)(j / kStages) & 1u);
         __syncwarp();
@@ -630,6 +630,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                     if (last) ++c;
                 }
             }
+        // and every release of the results, the other block's too
+        for (int j = max(0, c - 2); ok && j < c; ++j) ok = wait.warp(&d_empty[j & 1], (uint32_t)(j >> 1) & 1u);
         // every product issued ends before the block frees its memory
         if (rank == 0 && elected()) pair_commit(&drained);
         __syncwarp();
@@ -949,7 +951,6 @@ constexpr int kStrands = 16;
 
 __global__ void __launch_bounds__(32 * kStrands) k_xent_join(const JoinArgs a) {
     __shared__ float2 s_part[kStrands][32];
-    after_previous();
     const int lane = lane_id(), strand = threadIdx.x >> 5;
     const int n = a.ctl->n;
     const int group = group_tiles(n, a.classes), tiles = (a.classes + kN - 1) / kN;
@@ -1027,7 +1028,6 @@ struct DhArgs {
 template <typename T>
 __global__ void __launch_bounds__(32 * kStrands) k_xent_dh(const DhArgs a) {
     __shared__ float s_rest[kStrands][32];
-    after_previous();
     const int lane = lane_id(), strand = threadIdx.x >> 5, n = a.ctl->n, chunks = a.width / 8;
     const int64_t mp = padded(n);
     const int parts = (a.classes + kN - 1) / kN * 2;
@@ -1070,7 +1070,6 @@ __global__ void __launch_bounds__(32 * kStrands) k_xent_dh(const DhArgs a) {
 // dbias from the column sums of every 32 rows: 32 columns by 8 strands.
 __global__ void __launch_bounds__(256) k_xent_db(const Ctl *ctl, const float *colsum, int classes, float *db) {
     __shared__ float part[8][32];
-    after_previous();
     const int lane = lane_id(), strand = threadIdx.x >> 5, v = blockIdx.x * 32 + lane;
     const int sums = (ctl->n + kM - 1) / kM * (kM / 32);
     float s = 0.f;

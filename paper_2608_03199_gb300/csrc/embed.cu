@@ -145,7 +145,6 @@ __device__ __forceinline__ int sort_key(const Sort &s, int i) {
 
 __global__ void __launch_bounds__(kSortThreads) k_sort_count(const Sort s) {
     __shared__ int bins[kMaxDigits];
-    after_previous();
     const int n = 1 << s.bits;
     if (blockIdx.x == 0 && threadIdx.x == 0 && !s.key_in) *s.joins = 0;
     for (int i = threadIdx.x; i < n; i += kSortThreads) bins[i] = 0;
@@ -162,7 +161,6 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(const Sort s) {
     __shared__ int start[kMaxDigits];              // where the tile's next token of a digit goes
     __shared__ int of_warp[kSortWarps][kMaxDigits];
     __shared__ int sums[kSortWarps];
-    after_previous();
     const int n = 1 << s.bits, tid = threadIdx.x, lane = lane_id(), warp = tid >> 5;
     // digit tid: tokens of it in all tiles, and in the tiles before this one
     int all = 0, before = 0;
@@ -316,7 +314,6 @@ template <typename T, typename G, int VEC, int NC>
 __global__ void __launch_bounds__(kPieceWarps * 32) k_embed_sums(const Sums s) {
     const EmbedArgs &a = s.a;
     const int lane = lane_id(), warp = threadIdx.x >> 5;
-    after_previous();
     if ((int)blockIdx.x >= s.sum_blocks) {
         // ---- the zeros of rows that no token has
         __shared__ int range[2];
@@ -410,7 +407,6 @@ __global__ void __launch_bounds__(kJoinThreads) k_embed_join(const Sums s) {
     __shared__ int shared_end, found[kStrands], long_piece[kJoinThreads];
     const EmbedArgs &a = s.a;
     const int lane = lane_id(), warp = threadIdx.x >> 5;
-    after_previous();
     const int joins = *s.joins;
     auto write = [&](int id, int col, float v) {
         G *to = static_cast<G *>(a.dtable) + id * a.dtable_stride + col;

@@ -424,7 +424,6 @@ __global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR, blocks_per_s
 template <typename W>
 __global__ void __launch_bounds__(1024) k_residual_reduce(const ResidualNormArgs p, int groups) {
     __shared__ float part[2][32][33];
-    after_previous();
     const sieve_residual_norm_args &a = p.a;
     const int lane = threadIdx.x & 31, strand = threadIdx.x >> 5;
     const int col = blockIdx.x * 32 + lane;
