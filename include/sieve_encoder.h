@@ -323,7 +323,9 @@ sieve_status sieve_cross_entropy(const sieve_cross_entropy_args *a, float *loss,
  *   dbias[v] = sum over r of dloss[r] q.
  * The scores are made anew in pieces of the classes; q (times the mantissa of
  * dloss, where the rows' dloss differ) is rounded once to dtype on its way into
- * both products.
+ * both products.  The rest of dloss, a power of two, goes into a copy of h for
+ * dweight: exact in bf16; in fp16 exact down to 2^-29 of the largest product
+ * 2^e |h| of a call, and off by 2^-40 of that at most below.
  *   dloss    device [rows] fp32;  loss, lse what sieve_cross_entropy wrote
  *   dh       device [rows][width] of dtype out, rows dh_stride apart; nullable
  *   dweight  device [classes][width] of `dweight_dtype` (dtype or SIEVE_F32)

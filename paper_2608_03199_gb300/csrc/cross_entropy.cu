@@ -33,9 +33,12 @@
 //
 // dloss differs from row to row, and dW needs it in the product.  Where all
 // rows have the same one it is a factor at the end.  Else it is taken apart, m 2^e:
-// q is rounded times m, h gets an exact 2^e (over the largest) in a copy of its own,
-// and so does dh at the end; nothing is rounded twice.  In fp16 q is taken 2^14
-// times as large, so that small probabilities keep their bits.
+// q is rounded times m, h gets 2^e in a copy of its own, and so does dh at the end.
+// In bf16 the copy is over the largest 2^e and exact.  In fp16 it is shifted so that the
+// largest 2^e |h| of all rows is at the type's end: exact down to 2^-29 of that, and
+// what is smaller is off by 2^-40 of it at most (over the largest 2^e, an h of 2^-4 in a
+// row of 2^-20 had one bit left).  In fp16 q is taken 2^14 times as large as well, so that
+// small probabilities keep their bits.
 //
 // The tensor cores cut a sum off at every step of 16 products instead of
 // rounding it, which leaves a score of 2,048 products off by a few 1e-6 of itself, all to
@@ -56,7 +59,9 @@
 // top.  4,915 of 32,768 rows x 50,001 x 768 with a bias: 203, 255 and 485 us.  4,099 x 32,800
 // x 256, fp16: 48, 65 and 114 us, the last bound by the pool's reads from memory (571 MB,
 // 5.2 TB/s).  5 rows x 50,000 x 768: 24 us, 3.2 TB/s of the table.
+#include <algorithm>
 #include <cfloat>
+#include <cmath>
 #include <cstring>
 
 #include "attention.cuh"
@@ -163,6 +168,9 @@ __host__ __device__ inline int dh_slabs(int64_t n, int classes, int width, int64
 }
 
 // ---------------------------------------------------------------------------
+constexpr int64_t kFewRows = 1 << 18;
+constexpr int kManyBlocks = 8;                        // of a tile of rows where there are few
+
 // The rows with a target.
 struct RowArgs {
     const void *targets, *h;
@@ -174,6 +182,8 @@ struct RowArgs {
     Ctl *ctl;
     int *count;                           // [blocks]
     uint32_t *top, *low;                  // [blocks] largest dloss, and its lowest, as ordered keys
+    int *reach;                           // fp16: [blocks][SUB] largest exponent of 2^e |h|, or nullptr
+    int least;                            // and what it counts as at least, so that the factor at the end stays normal
     int *row, *target;
     float *dloss_c, *at_target_c, *lse_c, *part_c, *whole_c;   // part_c whole_c = dloss
     void *hc, *hs;
@@ -188,12 +198,64 @@ __device__ __forceinline__ float unordered(uint32_t k) {
     return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
 
-__global__ void __launch_bounds__(kRowTile) k_xent_count(const RowArgs a) {
+// m 2^e of a dloss, m from 1 to 2 (so that 2^e is finite).  A zero, or one that is not
+// finite, stays whole: false, and its e is somebody else's choice.
+__device__ __forceinline__ bool apart(float v, float &m, int &e) {
+    m = 2.f * frexpf(v, &e);
+    --e;
+    if (v != 0.f && isfinite(v)) return true;
+    m = v;
+    return false;
+}
+
+// fp16, backward: how far 2^e |h| reaches in the rows of each of a tile's SUB blocks.
+// Values that are not finite do not count.
+constexpr int kNoReach = -1000;
+template <int SUB>
+__device__ __forceinline__ void find_reach(const RowArgs &a) {
+    __shared__ int s_reach[kRowTile / 32];
+    constexpr int kMine = kRowTile / SUB;
+    const int lane = lane_id(), warp = threadIdx.x >> 5, chunks = a.width / 8;
+    const int64_t first = (int64_t)blockIdx.x * kMine;
+    int reach = kNoReach;
+    for (int i = warp; i < kMine && first + i < a.rows; i += kRowTile / 32) {
+        const int64_t row = first + i;
+        float m;
+        int e, e_h;
+        if (id_at(a.targets, a.target_type, row, a.classes) < 0 || !apart(a.dloss[row], m, e)) continue;
+        uint32_t top = 0;
+#pragma unroll 4
+        for (int c = lane; c < chunks; c += 32) {
+            const uint4 raw = __ldg(reinterpret_cast<const uint4 *>(static_cast<const __half *>(a.h) + row * a.h_stride) + c);
+            for (const uint32_t w : {raw.x, raw.y, raw.z, raw.w})
+                for (const uint32_t x : {w & 0x7fffu, w >> 16 & 0x7fffu}) top = max(top, x < 0x7c00u ? x : 0u);
+        }
+        top = __reduce_max_sync(0xffffffffu, top);
+        if (!top) continue;
+        frexpf(__half2float(__ushort_as_half((unsigned short)top)), &e_h);
+        reach = max(reach, e + e_h - 1);
+    }
+    if (lane == 0) s_reach[warp] = reach;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int w = 1; w < kRowTile / 32; ++w) reach = max(reach, s_reach[w]);
+    a.reach[blockIdx.x] = reach;
+}
+
+// The rows of a tile that have a target, and their dloss.  With SUB blocks a tile,
+// each looks how far its rows reach, and the first one counts.
+template <int SUB>
+__global__ void __launch_bounds__(kRowTile) k_xent_count(RowArgs a) {
     __shared__ uint32_t top[kRowTile / 32], low[kRowTile / 32];
-    const int64_t r = (int64_t)blockIdx.x * kRowTile + threadIdx.x;
+    const int tile = SUB ? (int)blockIdx.x / (SUB ? SUB : 1) : (int)blockIdx.x;
+    if constexpr (SUB > 0) {
+        find_reach<SUB>(a);
+        if (blockIdx.x % SUB) return;
+    }
+    const int64_t r = (int64_t)tile * kRowTile + threadIdx.x;
     const bool live = r < a.rows && id_at(a.targets, a.target_type, r, a.classes) >= 0;
     const int n = __syncthreads_count(live);
-    if (threadIdx.x == 0) a.count[blockIdx.x] = n;
+    if (threadIdx.x == 0) a.count[tile] = n;
     if (!a.dloss) return;
     const uint32_t k = live ? ordered(a.dloss[r]) : 0;
     const uint32_t t = __reduce_max_sync(0xffffffffu, k), l = __reduce_min_sync(0xffffffffu, live ? k : 0xffffffffu);
@@ -208,15 +270,14 @@ __global__ void __launch_bounds__(kRowTile) k_xent_count(const RowArgs a) {
             t2 = max(t2, top[w]);
             l2 = min(l2, low[w]);
         }
-        a.top[blockIdx.x] = t2;
-        a.low[blockIdx.x] = l2;
+        a.top[tile] = t2;
+        a.low[tile] = l2;
     }
 }
 
 // SUB blocks share a tile of rows, so that many blocks copy where there are few
 // tiles (32,768 rows of 768, one in seven with a target, backward: 26 us with one).
 // More than kFewRows rows have tiles enough, and every block reads all tiles' counts.
-constexpr int64_t kFewRows = 1 << 18;
 template <typename T, int SUB>
 __global__ void __launch_bounds__(kRowTile) k_xent_rows(const RowArgs a) {
     constexpr int kWarps = kRowTile / 32;
@@ -274,25 +335,34 @@ __global__ void __launch_bounds__(kRowTile) k_xent_rows(const RowArgs a) {
     rank += __popc(live & ((1u << lane) - 1));
     const bool every = all == a.rows, same = top == low;
     const float hi = unordered(top), lo = unordered(low);
-    // m 2^e of a dloss, m from 1 to 2 (so that 2^e is finite); a zero, or one that is
-    // not finite, stays whole, and so does its h
+    // what every 2^e is over in the copy of h; a dloss that stays whole has it for its e
+    // (and its h stays whole too)
     const float largest = fmaxf(fabsf(hi), fabsf(lo));
-    int e_top = 1;
-    if (isfinite(largest)) frexpf(largest, &e_top);
-    --e_top;
-    auto apart = [&](float v, int &e) {
-        const float m = frexpf(v, &e);
-        --e;
-        if (v != 0.f && isfinite(v)) return 2.f * m;
-        e = e_top;
-        return v;
+    int e_all = 1;
+    if (isfinite(largest)) frexpf(largest, &e_all);
+    --e_all;
+    if (a.reach && !same) {
+        int reach = a.least;
+        for (int b = tid; b < tiles * SUB; b += kRowTile) reach = max(reach, a.reach[b]);
+        reach = __reduce_max_sync(0xffffffffu, reach);
+        __syncthreads();
+        if (lane == 0) s_rank[warp] = reach;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) reach = max(reach, s_rank[w]);
+        e_all = reach - 15;              // the largest 2^e |h| is below 2^16 in the copy
+    }
+    auto parts = [&](float v, int &e) {
+        float m;
+        if (!apart(v, m, e)) e = e_all;
+        return m;
     };
     if (blockIdx.x == 0 && tid == 0) {
         a.ctl->status = 0;
         a.ctl->n = all;
         a.ctl->all = every;
         a.ctl->same = !a.dloss || same;
-        a.ctl->factor = a.dloss && all > 0 ? (same ? hi : ldexpf(1.f, e_top)) : 0.f;
+        a.ctl->factor = a.dloss && all > 0 ? (same ? hi : ldexpf(1.f, e_all)) : 0.f;
     }
     if (mine && t >= 0) {
         const int at = before + rank;
@@ -302,7 +372,7 @@ __global__ void __launch_bounds__(kRowTile) k_xent_rows(const RowArgs a) {
         if (a.dloss) {
             const float v = a.dloss[r];
             int e;
-            const float m = apart(v, e);
+            const float m = parts(v, e);
             a.dloss_c[at] = v;
             a.part_c[at] = same ? 1.f : m;
             a.whole_c[at] = same ? v : ldexpf(1.f, e);
@@ -321,9 +391,9 @@ __global__ void __launch_bounds__(kRowTile) k_xent_rows(const RowArgs a) {
         T *hc = static_cast<T *>(a.hc), *hs = static_cast<T *>(a.hs);
         for (int i = warp; i < here; i += kWarps) {
             const int64_t from = (int64_t)tile * kRowTile + s_list[i], to = before + i;
-            int e_row = e_top;
-            if (scaled) apart(a.dloss[from], e_row);
-            const float f = ldexpf(1.f, e_row - e_top);
+            int e_row = e_all;
+            if (scaled) parts(a.dloss[from], e_row);
+            const float f = ldexpf(1.f, min(e_row - e_all, 39));     // (above that in fp16 where the row is all zeros)
 #pragma unroll 4
             for (int c = lane; c < chunks; c += 32) {
                 const uint4 raw = __ldg(reinterpret_cast<const uint4 *>(h + from * a.h_stride) + c);
@@ -1085,7 +1155,7 @@ __global__ void __launch_bounds__(256) k_xent_db(const Ctl *ctl, const float *co
 
 // ---------------------------------------------------------------------------
 struct Layout {
-    size_t count, top, low, row, target, dloss, at_target, lse, hc, hs, hit, part, part_of, whole, pool, acc, rest, colsum, bytes;
+    size_t count, top, low, reach, row, target, dloss, at_target, lse, hc, hs, hit, part, part_of, whole, pool, acc, rest, colsum, bytes;
     int64_t pool_rows, acc_rows;
 };
 Layout layout(const sieve_cross_entropy_args &a, bool backward) {
@@ -1110,6 +1180,7 @@ Layout layout(const sieve_cross_entropy_args &a, bool backward) {
     } else {
         l.top = take(blocks * 4);
         l.low = take(blocks * 4);
+        if (a.dtype == SIEVE_F16) l.reach = take(blocks * (n <= kFewRows ? kManyBlocks : 1) * 4);
         l.dloss = take(n * 4);
         l.at_target = take(n * 4);
         l.lse = take(n * 4);
@@ -1182,17 +1253,19 @@ sieve_status prepare(Call &c, const sieve_cross_entropy_args &a, const Layout &l
     return rc;
 }
 
+template <typename T, int SUB>
+cudaError_t list_rows_by(const Call &c, cudaStream_t st) {
+    if (c.r.reach) {
+        k_xent_count<SUB><<<c.blocks * SUB, kRowTile, 0, st>>>(c.r);
+    } else if (c.blocks > 1) {
+        k_xent_count<0><<<c.blocks, kRowTile, 0, st>>>(c.r);
+    }
+    k_xent_rows<T, SUB><<<c.blocks * SUB, kRowTile, 0, st>>>(c.r);
+    return cudaGetLastError();
+}
 template <typename T>
 cudaError_t list_rows(const Call &c, cudaStream_t st) {
-    if (c.blocks == 1) {
-        k_xent_rows<T, 8><<<8, kRowTile, 0, st>>>(c.r);
-        return cudaGetLastError();
-    }
-    k_xent_count<<<c.blocks, kRowTile, 0, st>>>(c.r);
-    const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
-    if (c.x.rows <= kFewRows) return launch_next(k_xent_rows<T, 8>, c.blocks * 8, kRowTile, 0, st, c.r);
-    return launch_next(k_xent_rows<T, 1>, c.blocks, kRowTile, 0, st, c.r);
+    return c.x.rows <= kFewRows ? list_rows_by<T, kManyBlocks>(c, st) : list_rows_by<T, 1>(c, st);
 }
 
 template <typename T>
@@ -1278,7 +1351,12 @@ sieve_status launch_cross_entropy_backward(const sieve_cross_entropy_args &a, co
     c.r.part_c = reinterpret_cast<float *>(base + l.part_of);
     c.r.whole_c = reinterpret_cast<float *>(base + l.whole);
     c.x.part_of = c.r.part_c;
-    c.r.hs = base + l.hs;
+    if (g.dweight) {
+        c.r.hs = base + l.hs;
+        if (a.dtype == SIEVE_F16) c.r.reach = reinterpret_cast<int *>(base + l.reach);
+        // (2^(least - 15), and that times the scale and over kUp, are normal)
+        c.r.least = std::max(-97 - (a.scale == 0.f ? 0 : std::ilogb(a.scale)), -111);
+    }
     rc = make_matrix_map(&c.x.hs, a.dtype, base + l.hs, a.rows, a.width, a.width, kBox);
     if (rc == SIEVE_OK) rc = make_matrix_map(&c.x.pool_in, a.dtype, base + l.pool, l.pool_rows, kK, kK, kBox);
     if (rc == SIEVE_OK) rc = make_matrix_map(&c.x.pool_out, a.dtype, base + l.pool, l.pool_rows, kK, kK, 32);

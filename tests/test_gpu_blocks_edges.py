@@ -1,0 +1,54 @@
+"""The operators around an encoder's blocks where results depend on how sums,
+roundings and rows are arranged: rows of very unequal weight, and the like.
+The bounds count the roundings that the formulas of each operator leave."""
+import math
+
+import pytest
+import torch
+
+import blocks_reference as ref
+import paper_2608_03199_gb300 as sieve
+from test_gpu_encoder import BF16, DEV, FP16, FP32, gen, randn
+
+pytestmark = pytest.mark.gpu
+I32, I64 = torch.int32, torch.int64
+
+
+# ------------------------------------------------------------ cross entropy
+@pytest.mark.parametrize("rows", [120, 600, 270_000])
+@pytest.mark.parametrize("down", [4, 12, 16, 20])
+def test_cross_entropy_a_class_that_only_light_rows_reach(rows, down):
+    """Light rows' dloss is 2^-down of the heavy ones', and one class has nothing of
+    the heavy ones (its score there is -64).  Scores are zero else, so q is known: a
+    light row's q is off by its rounding (2^-11; up to 256 rows hold the remainder too,
+    2^-20) and by 2^-18 for exp and log, a sum of m terms by 2 m 2^-24; the weighted
+    copy of h in fp16 is exact down to 2^-29 of its largest and off by 2^-40 of it below,
+    twice that with the mantissa of dloss."""
+    g = gen(down)
+    live = min(rows, 600)
+    at = torch.randperm(rows, generator=g, device=DEV)[:live].sort().values
+    h = (randn(g, live, 256) / 16).to(FP16)
+    light = torch.arange(live, device=DEV) % 2 == 0
+    h[:, 0] = torch.where(light, 0.0, 1.0)
+    h[4::40] = 0                                          # light rows of zeros
+    dloss = (1 + torch.rand(live, generator=g, device=DEV)) * torch.where(light, 2.0 ** -down, 1.0)
+    dloss[1::40] = 0                                      # heavy rows without a weight
+    dloss[2::40] = -dloss[2::40]
+    weight = torch.zeros(8, 256, dtype=FP16, device=DEV)
+    weight[7, 0] = -64
+    t = torch.randint(8, (live,), generator=g, device=DEV)
+    t = torch.where(light, t, t % 7)
+    h_all = torch.full((rows, 256), math.nan, dtype=FP16, device=DEV)
+    d_all = torch.full((rows,), 1e30, device=DEV)
+    t_all = torch.full((rows,), -1, device=DEV)
+    h_all[at], d_all[at], t_all[at] = h, dloss, t
+    loss, lse = sieve.cross_entropy(h_all, weight, t_all, check=True)
+    dw = torch.empty(8, 256, device=DEV)
+    sieve.cross_entropy_backward(d_all, h_all, weight, t_all, loss, lse, dweight=dw, check=True)
+    x, gg = h[light].double(), dloss[light].double()
+    q = 1 / 8 - (t[light] == 7).double()
+    m = int(light.sum())
+    off = (2.0 ** -20 if live <= 256 else 2.0 ** -11) + 2.0 ** -18 + 2 * m * 2.0 ** -24
+    largest = float((dloss.abs() * h.abs().amax(1)).max())
+    bound = off * (gg * q).abs() @ x.abs() + 2.0 ** -39 * largest * float(q.abs().sum()) + 1e-26
+    ref.assert_within(dw[7], (gg * q) @ x, bound, "dweight")
