@@ -317,7 +317,8 @@ sieve_status sieve_cross_entropy(const sieve_cross_entropy_args *a, float *loss,
                                  void *ws, size_t ws_bytes, void *stream);
 
 /* Its backward pass, for the gradient dloss of every row's loss: with
- * q = exp(z - lse) - [v = target] (exactly expm1(-loss) at the target),
+ * q = exp(z - lse) - [v = target] (exactly expm1(-loss) at the target; where
+ * every class is hidden that is -1, and q is 0 elsewhere),
  *   dh[r] = dloss[r] scale sum over v of q weight[v],
  *   dweight[v] = scale sum over r of dloss[r] q h[r],
  *   dbias[v] = sum over r of dloss[r] q.

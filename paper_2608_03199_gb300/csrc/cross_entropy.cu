@@ -1088,7 +1088,7 @@ __global__ void __launch_bounds__(32 * kStrands) k_xent_join(const JoinArgs a) {
 struct DhArgs {
     const Ctl *ctl;
     const int *row, *target;
-    const float *whole, *acc, *rest;
+    const float *whole, *lse, *acc, *rest;
     const void *weight;
     void *dh;
     int64_t weight_stride, dh_stride, pool_rows;
@@ -1114,6 +1114,7 @@ __global__ void __launch_bounds__(32 * kStrands) k_xent_dh(const DhArgs a) {
             const int64_t i = i0 + k;
             float rest = 0.f;
             for (int p = 0; p < kStrands; ++p) rest -= s_rest[p][k];
+            if (a.lse[i] == -INFINITY) rest = 0.f;        // every class hidden: the target's -1 is all that q holds
             const float f = a.whole[i] * a.scale / kUp<T>;
             const T *w = static_cast<const T *>(a.weight) + a.target[i] * a.weight_stride;
             T *out = static_cast<T *>(a.dh) + a.row[i] * a.dh_stride;
@@ -1365,7 +1366,7 @@ sieve_status launch_cross_entropy_backward(const sieve_cross_entropy_args &a, co
         rc = make_matrix_map(&c.x.dw, g.dweight_dtype, g.dweight, a.classes, a.width, g.dweight_stride, 32);
     if (rc != SIEVE_OK) return rc;
     const int each = piece_classes(a.rows, c.x.classes, l.pool_rows), pieces = (int)ceil_div(a.classes, each);
-    const DhArgs d = {c.x.ctl, c.r.row, c.x.target, c.r.whole_c, reinterpret_cast<const float *>(base + l.acc), c.x.rest, a.weight,
+    const DhArgs d = {c.x.ctl, c.r.row, c.x.target, c.r.whole_c, c.r.lse_c, reinterpret_cast<const float *>(base + l.acc), c.x.rest, a.weight,
                       g.dh, a.weight_stride, g.dh_stride, l.pool_rows, c.x.classes, a.width, c.x.want_dw, a.scale};
     const cudaError_t e = a.dtype == SIEVE_F16 ? backward<__half>(c, g, d, pieces, st)
                                                : backward<__nv_bfloat16>(c, g, d, pieces, st);

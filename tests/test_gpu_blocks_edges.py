@@ -52,3 +52,21 @@ def test_cross_entropy_a_class_that_only_light_rows_reach(rows, down):
     largest = float((dloss.abs() * h.abs().amax(1)).max())
     bound = off * (gg * q).abs() @ x.abs() + 2.0 ** -39 * largest * float(q.abs().sum()) + 1e-26
     ref.assert_within(dw[7], (gg * q) @ x, bound, "dweight")
+
+
+@pytest.mark.parametrize("rows", [90, 700])
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("weights", ["same", "differ"])
+def test_cross_entropy_gradients_of_hidden_targets_and_tables(rows, dtype, weights):
+    """A hidden target: p elsewhere, -1 at it.  Every class hidden: -1 at the
+    target alone, in all three gradients."""
+    g = gen(rows)
+    h, weight, t = randn(g, rows, 72).to(dtype), randn(g, 300, 72).to(dtype), torch.randint(300, (rows,), generator=g, device=DEV)
+    dloss = torch.full((rows,), 0.5, device=DEV) if weights == "same" else randn(g, rows)
+    for b in (torch.where(torch.arange(300, device=DEV) % 3 == 0, -math.inf, randn(g, 300)), torch.full((300,), -math.inf, device=DEV)):
+        loss, lse = sieve.cross_entropy(h, weight, t, bias=b, scale=0.25)
+        dw = torch.empty(300, 72, device=DEV)
+        got = dict(zip(("dh", "dweight", "dbias"), sieve.cross_entropy_backward(dloss, h, weight, t, loss, lse, bias=b, scale=0.25, dweight=dw)))
+        want, bound = ref.cross_entropy(h, weight, t, b, 0.25, dloss, FP32)
+        for name, x in got.items():
+            ref.assert_within(x, want[name], bound[name], name)
