@@ -26,7 +26,7 @@
 // [64], so its address needs no stride that depends on the list.  As operand of
 // dh a panel is K-major, as operand of dW MN-major.
 //
-// With few rows (kFine) a gradient's element is the sum of a few q, whose rounding
+// With few rows (a list of up to kFine) a gradient's element is the sum of a few q, whose rounding
 // no other evens out, and the products cost little beside the tables they read and
 // write: there the pool holds what the rounding left off as well, in as many rows
 // more, both products run over both, and scores are summed in shorter chunks.
@@ -80,7 +80,6 @@ constexpr int kBoxes = kHalf / kBox;                  // of an operand in a bloc
 constexpr uint32_t kStageBytes = 2 * kBoxes * kBoxBytes;
 constexpr int kEpiWarps = 8;
 constexpr int kFine = kM;                             // rows that are few
-constexpr int64_t kMaybeFine = 2048;                  // rows of a call whose list may be that short
 // rows of a panel of the pool
 __host__ __device__ inline int64_t panel_rows(int64_t n) {
     const int64_t padded = (n + kM - 1) / kM * kM;
@@ -125,7 +124,7 @@ struct XentArgs {
     int64_t pool_rows;
     int rows, classes, width;
     float scale, c;                       // c = scale log2(e)
-    int want_dh, want_dw, want_db, dw_f32, accumulate, maybe_fine;
+    int want_dh, want_dw, want_db, dw_f32, accumulate;
 };
 
 template <typename T>
@@ -531,7 +530,7 @@ struct Walk {
         n = a.ctl->n;
         mp = (int)padded(n);
         panel = (int)panel_rows(n);
-        fine = a.maybe_fine && n <= kFine;
+        fine = n <= kFine;
         width = a.width;
         row_tiles = (n + kM - 1) / kM;
         d_tiles = (a.width + kN - 1) / kN;
@@ -585,16 +584,13 @@ struct Walk {
     }
 };
 
-template <typename T, int MODE, bool BIAS, bool FINE>
+template <typename T, int MODE, bool BIAS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(const __grid_constant__ XentArgs a, int piece) {
     constexpr int kStages = stages(MODE);
-    // stages of a chunk (past 512 columns six: two buffers then hold the next tile's
-    // products for as long as this one's q take)
-    const int chunk_of = MODE == 2 ? 64 : FINE && a.ctl->n <= kFine ? 2 : a.width > 8 * kK ? 6 : 4;
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t full[kStages], empty[kStages], d_full[2], d_empty[2], drained;
     __shared__ uint32_t tmem_slot;
-    __shared__ int s_abort;
+    __shared__ int s_abort, s_chunk;
     __shared__ __align__(16) float s_bias[kEpiWarps][BIAS ? kN / 2 : 4];
     const Walk<MODE> walk(a, piece);
     if (walk.total == 0) return;
@@ -612,6 +608,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
         }
         tc::mbar_init(&drained, 1);
         s_abort = 0;
+        // stages of a chunk (past 512 columns six: two buffers then hold the next tile's
+        // products for as long as this one's q take).  Read anew where it is used: the epilogue
+        // has no register for it.
+        s_chunk = walk.fine ? 2 : a.width > 8 * kK ? 6 : 4;
         tc::mbar_init_fence();
     }
     __syncwarp();
@@ -624,6 +624,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
     const Waiter wait{&s_abort};
     const bool all = a.ctl->all, same = a.ctl->same;
+    auto chunk_of = [&] { return MODE == 2 ? 64 : *const_cast<const volatile int *>(&s_chunk); };
 
     if (warp == kEpiWarps) {
         // ---------------- loads ----------------
@@ -681,7 +682,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                 for (int b = 0, in = 0; b < t.blocks; ++b, ++s) {
                     const int buf = c & 1;
                     const uint32_t d = tmem + buf * kN;
-                    const bool first = in == 0, last = in + 1 == chunk_of || b + 1 == t.blocks;
+                    const bool first = in == 0, last = in + 1 == chunk_of() || b + 1 == t.blocks;
                     if (first && !(ok = wait.warp(&d_empty[buf], ((uint32_t)(c >> 1) & 1u) ^ 1u))) break;
                     const int st = s % kStages;
                     if (!(ok = wait.warp(&full[st], (uint32_t)(s / kStages) & 1u))) break;
@@ -786,7 +787,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                         for (int e = 0; e < 32; ++e) acc[j][e] = 0u;
                 }
 #pragma unroll 1
-                for (int b = MODE != 2 ? chunk_of : 0; ok && b < t.blocks; b += chunk_of) chunk(false);
+                for (int b = MODE != 2 ? chunk_of() : 0; ok && b < t.blocks; b += chunk_of()) chunk(false);
                 if (!ok) break;
                 auto take = [&](int j, float (&x)[32]) {
 #pragma unroll
@@ -839,9 +840,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                     }
                 } else if constexpr (MODE == 1) {
                     float2 rest = make_float2(0.f, 0.f);
-                    // (FINE: a second pass for what the first one's rounding left off)
-#pragma unroll 1
-                    for (int pass = 0; pass < (FINE && walk.fine ? 2 : 1); ++pass)
+                    auto columns = [&](auto second) {
+                    constexpr bool pass = decltype(second)::value;
 #pragma unroll
                     for (int j = 0; j < kN / 2; j += 64) {
                         uint32_t packed[32];
@@ -870,13 +870,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                             for (int e = 0; e < 32; e += 2) {
                                 const float2 q = mul2(get(x + e), both(part));
                                 packed[(jj + e) / 2] = pack2<T>(q.x, q.y);
-                                if (FINE && pass) {
+                                if constexpr (pass) {
                                     const float2 is = add_pair<T>(make_float2(0.f, 0.f), packed[(jj + e) / 2]);
                                     packed[(jj + e) / 2] = pack2<T>(q.x - is.x, q.y - is.y);
                                 }
                                 some = add_pair<T>(some, packed[(jj + e) / 2]);
                             }
-                            if (BIAS && a.want_db && (!FINE || pass == 0)) {
+                            if (BIAS && !pass && a.want_db) {
                                 // The columns' sums over the warp's rows, turned in the buffer that
                                 // the packed values leave from later: a lane takes four columns of eight
                                 // rows.  (In registers alone, 31 shuffles and twice as many selects.)
@@ -920,7 +920,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                         if (at0 >= j && at0 < j + 64) {
                             const int e = at0 - j;
                             float q = q_target * part;
-                            if (FINE && pass) q -= to_f32<T>(from_f32<T>(q));
+                            if (pass) q -= to_f32<T>(from_f32<T>(q));
                             reinterpret_cast<T *>(out + lane * 128 + (((e >> 3) ^ (lane & 7)) << 4))[e & 7] = from_f32<T>(q);
                             some = make_float2(0.f, 0.f);
 #pragma unroll 1
@@ -933,10 +933,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                         tc::fence_proxy_async_smem();
                         __syncwarp();
                         if (lane == 0) {
-                            store_box(&a.pool_out, 0, (col + j - walk.v0) / kK * walk.panel + (FINE && pass ? walk.mp : 0) + t.m0 + r_warp, out);
+                            store_box(&a.pool_out, 0, (col + j - walk.v0) / kK * walk.panel + (pass ? walk.mp : 0) + t.m0 + r_warp, out);
                             stores_issued();
                         }
                     }
+                    };
+                    columns(std::false_type{});
+                    if (walk.fine) columns(std::true_type{});       // what the rounding left off
                     if (live) a.rest[(int64_t)(t.n0 / kN * 2 + half) * walk.mp + row] = rest.x + rest.y;
                 } else {
                     const int columns = 2 * t.n_boxes * kBox;    // of the tile that exist
@@ -1203,9 +1206,9 @@ Layout layout(const sieve_cross_entropy_args &a, bool backward) {
     return l;
 }
 
-template <typename T, int MODE, bool BIAS, bool FINE = false>
+template <typename T, int MODE, bool BIAS>
 cudaError_t run(const XentArgs &a, int piece, cudaStream_t st) {
-    auto kernel = k_xent<T, MODE, BIAS, FINE>;
+    auto kernel = k_xent<T, MODE, BIAS>;
     // The warps trade registers among each other, which takes all that kRegisters says.
     static const int registers = [&] {
         cudaFuncAttributes f;
@@ -1233,7 +1236,6 @@ sieve_status prepare(Call &c, const sieve_cross_entropy_args &a, const Layout &l
     x.width = a.width;
     x.scale = a.scale;
     x.c = a.scale * kLog2e;
-    x.maybe_fine = a.rows <= kMaybeFine;
     RowArgs &r = c.r;
     r.targets = a.targets;
     r.h = a.h;
@@ -1273,8 +1275,7 @@ template <typename T>
 cudaError_t forward(const Call &c, const JoinArgs &j, cudaStream_t st) {
     cudaError_t e = list_rows<T>(c, st);
     if (e != cudaSuccess) return e;
-    if (c.x.maybe_fine) e = c.x.bias ? run<T, 0, true, true>(c.x, 0, st) : run<T, 0, false, true>(c.x, 0, st);
-    else e = c.x.bias ? run<T, 0, true>(c.x, 0, st) : run<T, 0, false>(c.x, 0, st);
+    e = c.x.bias ? run<T, 0, true>(c.x, 0, st) : run<T, 0, false>(c.x, 0, st);
     if (e != cudaSuccess) return e;
     const int64_t blocks = ceil_div(c.x.rows, 32);
     return launch_next(k_xent_join, (unsigned)(blocks < 4096 ? blocks : 4096), 32 * kStrands, 0, st, j);
@@ -1285,8 +1286,7 @@ cudaError_t backward(const Call &c, const sieve_cross_entropy_grads &g, const Dh
     cudaError_t e = list_rows<T>(c, st);
     if (e != cudaSuccess) return e;
     for (int p = 0; p < pieces; ++p) {
-        if (c.x.maybe_fine) e = c.x.bias ? run<T, 1, true, true>(c.x, p, st) : run<T, 1, false, true>(c.x, p, st);
-        else e = c.x.bias ? run<T, 1, true>(c.x, p, st) : run<T, 1, false>(c.x, p, st);
+        e = c.x.bias ? run<T, 1, true>(c.x, p, st) : run<T, 1, false>(c.x, p, st);
         if (e == cudaSuccess && (g.dh || g.dweight)) e = run<T, 2, false>(c.x, p, st);
         if (e != cudaSuccess) return e;
     }

@@ -70,3 +70,23 @@ def test_cross_entropy_gradients_of_hidden_targets_and_tables(rows, dtype, weigh
         want, bound = ref.cross_entropy(h, weight, t, b, 0.25, dloss, FP32)
         for name, x in got.items():
             ref.assert_within(x, want[name], bound[name], name)
+
+
+@pytest.mark.parametrize("rows,live", [(2_100, 256), (5_000, 200), (300_000, 31)])
+@pytest.mark.parametrize("dtype,bias", [(BF16, False), (FP16, True)])
+def test_cross_entropy_few_rows_in_a_large_batch(rows, live, dtype, bias):
+    """Up to 256 rows with a target are worked out the same way whatever the
+    batch that they come in: the bits of a call without the other rows."""
+    g = gen(rows)
+    weight, b = (randn(g, 900, 320) / 8).to(dtype), randn(g, 900) if bias else None
+    at = torch.randperm(rows, generator=g, device=DEV)[:live].sort().values
+    h, t, dloss = torch.full((rows, 320), math.nan, dtype=dtype, device=DEV), torch.full((rows,), -7, device=DEV), torch.ones(rows, device=DEV)
+    h[at], t[at] = randn(g, live, 320).to(dtype), torch.randint(900, (live,), generator=g, device=DEV)
+    for d in (dloss, dloss.index_copy(0, at, randn(g, live))):
+        got = sieve.cross_entropy(h, weight, t, bias=b, check=True)
+        alone = sieve.cross_entropy(h[at], weight, t[at], bias=b)
+        assert torch.equal(got[0][at], alone[0]) and torch.equal(got[1][at], alone[1])
+        got = sieve.cross_entropy_backward(d, h, weight, t, *got, bias=b, dweight=torch.empty(900, 320, device=DEV), check=True)
+        alone = sieve.cross_entropy_backward(d[at], h[at], weight, t[at], *alone, bias=b, dweight=torch.empty(900, 320, device=DEV))
+        assert torch.equal(got[0][at], alone[0]) and torch.equal(got[1], alone[1])
+        assert not bias or torch.equal(got[2], alone[2])
