@@ -250,6 +250,11 @@ __global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR, blocks_per_s
     k_residual_norm_backward(const ResidualNormArgs p) {
     extern __shared__ float acc[];                 // kShared: [4][width]
     __shared__ float2 meet[2][32];
+    // Rows of few columns, where the means take most of a gradient away: they are taken off
+    // before dstream is added, or what either was rounded by stays.  (From some dozens on the
+    // means are off by as much themselves, and the registers that keep dstream until then
+    // cost 3% at 768 columns, 16% where elements move one by one.)
+    constexpr bool kMeansFirst = TPR == 32;
     const sieve_residual_norm_args &a = p.a;
     const sieve_residual_norm_grads &g = p.g;
     const int i = TPR == 32 ? lane_id() : threadIdx.x;
@@ -337,14 +342,15 @@ __global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR, blocks_per_s
     if (group < a.rows) load(group);
     for (int64_t row = group; row < a.rows; row += step) {
         V uh[NCH], sh[NCH], G[NCH];
-        Piece<T, VEC> gr[NCH];
+        Piece<T, VEC> gr[NCH], gs[kMeansFirst ? NCH : 1];
         float s1 = 0.f, s2 = 0.f;
         const float mu1 = n_stats[0], r1 = n_stats[1], mu2 = n_stats[2], r2 = n_stats[3];
 #pragma unroll
         for (int c = 0; c < NCH; ++c) {
             gr[c] = ng[c];
             uh[c] = (V::of(ny[c]) + V::all(-mu1)) * V::all(r1);
-            G[c] = V::of(ns[c]);
+            if constexpr (kMeansFirst) gs[c] = ns[c];
+            else G[c] = V::of(ns[c]);
             if (!w2) continue;
             // the stream again, then the gradient through its norm
             V u = uh[c];
@@ -361,14 +367,21 @@ __global__ void __launch_bounds__(TPR == 32 ? 32 * kWarpRows : TPR, blocks_per_s
             d = d * V::at(w2 + place(c));
             s1 += d.sum();
             s2 += (d * sh[c]).sum();
-            G[c] = fma(V::all(r2), d, G[c]);
+            G[c] = kMeansFirst ? d : fma(V::all(r2), d, G[c]);
         }
         if (row + step < a.rows) load(row + step);
         if (w2) {
             both_sums(s1, s2);
-            const V m1 = V::all(-r2 * s1 * centre), m2 = V::all(-r2 * s2 * inv_n);
+            const float f = kMeansFirst ? -1.f : -r2;
+            const V m1 = V::all(f * s1 * centre), m2 = V::all(f * s2 * inv_n);
 #pragma unroll
-            for (int c = 0; c < NCH; ++c) G[c] = G[c] + fma(sh[c], m2, m1);
+            for (int c = 0; c < NCH; ++c) {
+                G[c] = G[c] + fma(sh[c], m2, m1);
+                if constexpr (kMeansFirst) G[c] = fma(V::all(r2), G[c], V::of(gs[c]));
+            }
+        } else if constexpr (kMeansFirst) {
+#pragma unroll
+            for (int c = 0; c < NCH; ++c) G[c] = V::of(gs[c]);
         }
         T *dh = static_cast<T *>(g.dh) + row * g.dh_stride, *dy = static_cast<T *>(g.dy) + row * g.dy_stride;
         s1 = s2 = 0.f;

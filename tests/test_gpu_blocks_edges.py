@@ -90,3 +90,20 @@ def test_cross_entropy_few_rows_in_a_large_batch(rows, live, dtype, bias):
         alone = sieve.cross_entropy_backward(d[at], h[at], weight, t[at], *alone, bias=b, dweight=torch.empty(900, 320, device=DEV))
         assert torch.equal(got[0][at], alone[0]) and torch.equal(got[1], alone[1])
         assert not bias or torch.equal(got[2], alone[2])
+
+
+# ------------------------------------------------------------ residual norm
+@pytest.mark.parametrize("dtype,wtype", [(FP32, FP32), (BF16, FP32), (FP16, FP16)])
+def test_residual_norm_gradients_of_one_column(dtype, wtype):
+    """One column less its mean is nothing: neither norm passes a gradient on,
+    whatever its factor (316 here), so dh is alpha dstream and dy is zero."""
+    g = gen(21)
+    h, y, ds, dx = (randn(g, 700, 1).to(dtype) for _ in range(4))
+    kw = dict(zip(("weight", "bias", "post_weight", "post_bias", "gate"), (randn(g, 1).to(wtype) for _ in range(5))))
+    stats = sieve.residual_norm(h, y, alpha=-0.5, **kw)[2]
+    dh, dy, dweight, dbias, dpw, dpb, dgate = sieve.residual_norm_backward(ds, dx, h, y, stats, alpha=-0.5, **kw)
+    assert torch.equal(dh, -0.5 * ds) and not dy.any() and not dweight.any() and not dpw.any()
+    sums = (700 / 152 + 65) * 2.0 ** -24
+    for got, terms, factor in ((dbias, dx, 1), (dpb, ds, kw["gate"]), (dgate, ds, kw["post_bias"])):
+        want, mag = float((terms.double() * factor).sum()), float((terms.double() * factor).abs().sum())
+        assert abs(float(got) - want) <= (sums + 2.0 ** -22) * mag + ref.U[wtype] * abs(want)
