@@ -64,6 +64,7 @@ struct ResidualNormArgs {
     float *stats;
     sieve_residual_norm_grads g;
     float *partial;   // [groups of threads][4][width]
+    float inv_width, inv_width_rest;   // the backward launcher's: 1 / width, and what that was rounded by
 };
 cudaError_t launch_residual_norm(const ResidualNormArgs &p, cudaStream_t st);
 cudaError_t launch_residual_norm_backward(const ResidualNormArgs &p, cudaStream_t st);

@@ -107,3 +107,20 @@ def test_residual_norm_gradients_of_one_column(dtype, wtype):
     for got, terms, factor in ((dbias, dx, 1), (dpb, ds, kw["gate"]), (dgate, ds, kw["post_bias"])):
         want, mag = float((terms.double() * factor).sum()), float((terms.double() * factor).abs().sum())
         assert abs(float(got) - want) <= (sums + 2.0 ** -22) * mag + ref.U[wtype] * abs(want)
+
+
+@pytest.mark.parametrize("dtype", [FP32, BF16])
+def test_residual_norm_means_of_equal_values(dtype):
+    """Sums of small whole numbers are exact, so the mean of equal values is
+    that value at every width, and what is left of them zero.  In the backward pass
+    too; past 128 columns the sum of dstream and r d is rounded before the mean is
+    taken off, and r times the mean is: two roundings of r d."""
+    g = gen(22)
+    for width in [*range(1, 260, 3), 301, 1001, 2100, 4099, 8191]:
+        h, y, one = (torch.full((3, width), v, dtype=dtype, device=DEV) for v in (2.0, 3.0, 1.0))
+        w, ds = torch.full((width,), 5.0, device=DEV), randn(g, 3, width).to(dtype)
+        stream, x, stats = sieve.residual_norm(h, y, w, post_weight=w)
+        assert (stats[0] == 3).all() and (stats[2] == 2).all() and torch.equal(stream, h) and not x.any(), width
+        dh = sieve.residual_norm_backward(ds, one, h, y, stats, w, post_weight=w)[0]
+        off = 0 if width <= 128 else 2 * 2.0 ** -24 * (5 * float(stats[3, 0]) + 6)
+        assert ((dh.double() - ds.double()).abs() <= off + (0 if dtype == FP32 or not off else 2.0 ** -8 * ds.double().abs())).all(), width
