@@ -8,8 +8,11 @@
 // kPiece tokens: a warp adds up the rows of one piece in registers and writes
 // every id that lies wholly inside it.  An id that goes on into other pieces
 // (a frequent word, the mask token) leaves one partial row a piece, which
-// k_embed_join adds up in order.  So the work is even whatever the ids are.
-// Rows that no token has are found by the blocks that write their zeros.
+// k_embed_join adds up in order.  So the sums' work is even whatever the ids are; what
+// grows with a frequent id is its join, one row of every 64 tokens by a block for each 256
+// columns.  Rows that no token has are found by the blocks that write their zeros
+// (262,144 tokens of 64 columns, 64,000 ids: 104 us, with half of the tokens one id as
+// well; 126 and 166 where such a block read all keys of its ids).
 //
 // Measured (device time).  Forward: 200,003 tokens of 1,024 columns from a table of 64,000
 // in fp32 to bf16 99 us (587 MB of DRAM traffic, 5.9 TB/s).  Backward: 131,000 tokens of 768
@@ -235,6 +238,7 @@ constexpr int kPiece = 64;              // sorted tokens of a warp
 constexpr int kPieceWarps = 4;
 constexpr int kColumns = 256;           // columns of a warp, times NC: 8 a lane each
 constexpr int kZeroRows = 32;           // table rows of a block that looks for empty ones
+constexpr int kFewKeys = 4 * kPieceWarps * 32;   // of their tokens
 
 struct Sums {
     EmbedArgs a;
@@ -325,8 +329,21 @@ __global__ void __launch_bounds__(kPieceWarps * 32) k_embed_sums(const Sums s) {
             if (lane == 0) range[warp] = p;
         }
         __syncthreads();
+        // Few keys of these ids are looked through.  More (a frequent word, the mask) would keep
+        // this block on them for as long as they are many: every id is searched for.
+        if (range[1] - range[0] <= kFewKeys) {
 #pragma unroll 4
-        for (int i = range[0] + threadIdx.x; i < range[1]; i += kPieceWarps * 32) has[s.key[i] - v0] = 1;
+            for (int i = range[0] + threadIdx.x; i < range[1]; i += kPieceWarps * 32) has[s.key[i] - v0] = 1;
+        } else if (threadIdx.x < kZeroRows) {
+            int lo = range[0], hi = range[1];
+            const int v = v0 + (int)threadIdx.x;
+            while (lo < hi) {
+                const int mid = lo + (hi - lo) / 2;
+                if (s.key[mid] < v) lo = mid + 1;
+                else hi = mid;
+            }
+            has[threadIdx.x] = lo < range[1] && s.key[lo] == v;
+        }
         __syncthreads();
         float zero[VEC] = {};
         for (int v = v0 + warp; v < v1; v += kPieceWarps)

@@ -14,6 +14,41 @@ pytestmark = pytest.mark.gpu
 I32, I64 = torch.int32, torch.int64
 
 
+# ---------------------------------------------------------------- embedding
+@pytest.mark.parametrize("tokens,often,vocab,width", [(600, 0.95, 70, 24), (70_000, 0.5, 1_000, 33), (200_000, 0.99, 65, 8), (3_000, 1.0, 40, 260)])
+def test_embed_backward_of_a_frequent_id(tokens, often, vocab, width):
+    """One id has most tokens; of those beside it some have a few and some none."""
+    g = gen(tokens)
+    for frequent in (0, vocab // 2, vocab - 1):
+        ids = torch.randint(0, vocab, (tokens,), generator=g, device=DEV)
+        ids = torch.where((torch.rand(tokens, generator=g, device=DEV) < often) | (ids % 3 == 1), frequent, ids)
+        dout = randn(g, tokens, width).to(BF16)
+        want, bound = ref.embed_backward(dout, ids, vocab, 1.5, FP32)
+        ref.assert_within(sieve.embed_backward(dout, ids, vocab, scale=1.5, out=torch.full((vocab, width), math.nan, device=DEV)), want, bound, "dtable")
+
+
+def test_embed_backward_does_not_wait_for_a_frequent_id():
+    """The blocks that look for rows without a token cost little even where four
+    million tokens share one id: the call takes at most three times one that writes no
+    zeros (accumulate).  Reading that id's keys one after the other took over ten times."""
+    ids = torch.full((1 << 22,), 3, device=DEV)
+    dout, out, ws = torch.ones(1 << 22, 8, dtype=BF16, device=DEV), torch.zeros(40, 8, device=DEV), sieve.Workspace()
+
+    def best(accumulate):
+        times = []
+        for _ in range(6):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            sieve.embed_backward(dout, ids, 40, out=out, accumulate=accumulate, workspace=ws)
+            b.record()
+            b.synchronize()
+            times.append(a.elapsed_time(b))
+        return min(times)
+    added = best(True)
+    assert best(False) < 3 * added
+    assert (out[3] == 1 << 22).all() and not out[:3].any() and not out[4:].any()
+
+
 # ------------------------------------------------------------ cross entropy
 @pytest.mark.parametrize("rows", [120, 600, 270_000])
 @pytest.mark.parametrize("down", [4, 12, 16, 20])
