@@ -29,10 +29,10 @@ def test_embed_backward_of_a_frequent_id(tokens, often, vocab, width):
 
 def test_embed_backward_does_not_wait_for_a_frequent_id():
     """The blocks that look for rows without a token cost little even where four
-    million tokens share one id: the call takes at most three times one that writes no
-    zeros (accumulate).  Reading that id's keys one after the other took over ten times."""
+    million tokens share one id: the call takes at most twice as long as one that writes no
+    zeros (accumulate).  Reading all of that id's keys took 3.6 times as long."""
     ids = torch.full((1 << 22,), 3, device=DEV)
-    dout, out, ws = torch.ones(1 << 22, 8, dtype=BF16, device=DEV), torch.zeros(40, 8, device=DEV), sieve.Workspace()
+    dout, out, ws = torch.ones(1 << 22, 64, dtype=BF16, device=DEV), torch.zeros(40, 64, device=DEV), sieve.Workspace()
 
     def best(accumulate):
         times = []
@@ -45,7 +45,7 @@ def test_embed_backward_does_not_wait_for_a_frequent_id():
             times.append(a.elapsed_time(b))
         return min(times)
     added = best(True)
-    assert best(False) < 3 * added
+    assert best(False) < 2 * added
     assert (out[3] == 1 << 22).all() and not out[:3].any() and not out[4:].any()
 
 
