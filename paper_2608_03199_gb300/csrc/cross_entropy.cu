@@ -476,6 +476,55 @@ __device__ __forceinline__ void warp_arrive_at(uint32_t bar) {
     __syncwarp();
     if (lane_id() == 0) asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+// Waits are bounded in time: one poll of an mbarrier may hold a thread back for as long as the
+// hardware chooses, so a limit of polls alone says little (an arrival that never
+// comes would look like a hang).  A wait gives up after kWaitNs, or once another role of
+// the block has; every role then winds down and the block records SIEVE_ETIMEOUT.
+constexpr uint32_t kWaitNs = 2000000000u;
+__device__ __forceinline__ uint32_t now_ns() {        // wraps after 4.3 s
+    uint32_t t;
+    asm volatile("mov.u32 %0, %%globaltimer_lo;" : "=r"(t));
+    return t;
+}
+struct PairWaiter {
+    int *abort_flag;   // shared memory
+    __device__ __forceinline__ bool operator()(uint64_t *bar, uint32_t parity) const {
+        if (tc::mbar_test_wait(bar, parity)) return true;
+        uint32_t start = 0;
+#pragma unroll 1
+        for (uint32_t it = 0; it < kPolls; ++it) {
+            if (tc::mbar_try_wait(bar, parity)) return true;
+            if ((it & 63u) != 63u) continue;
+            if (*(volatile int *)abort_flag) break;
+            if (it == 63u) start = now_ns();
+            else if (now_ns() - start > kWaitNs) break;
+        }
+        *(volatile int *)abort_flag = 1;
+        return false;
+    }
+    // the same for a whole warp in step
+    __device__ __forceinline__ bool warp(uint64_t *bar, uint32_t parity) const {
+        return __all_sync(0xffffffffu, (*this)(bar, parity));
+    }
+};
+// for products in flight, after an abort too
+__device__ __forceinline__ void land(uint64_t *bar, uint32_t parity) {
+    uint32_t start = 0;
+#pragma unroll 1
+    for (uint32_t it = 0; it < kPolls && !tc::mbar_try_wait(bar, parity); ++it) {
+        if ((it & 63u) != 63u) continue;
+        if (it == 63u) start = now_ns();
+        else if (now_ns() - start > kWaitNs) break;
+    }
+}
+// After an abort: ten milliseconds, in which the copies that nobody waits for any more land
+// (a stage takes microseconds; whose barrier they complete on may never have expected them).
+__device__ __forceinline__ void linger() {
+    const uint32_t start = now_ns();
+#pragma unroll 1
+    for (int it = 0; it < 100000 && now_ns() - start < 10000000u; ++it) __nanosleep(1000);
+}
+
 // MN-major operand of boxes of 64 columns by 64 rows of the contraction axis
 __device__ __forceinline__ uint64_t desc_boxes(const void *tile) {
     return (tc::desc_k_sw128(tc::smem_u32(tile)) & ~((uint64_t)0x3FFF << 16)) | (uint64_t)(kBoxBytes >> 4) << 16;
@@ -622,7 +671,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
     tc::fence_after_sync();
     const int rank = (int)pair_rank(), pair = blockIdx.x / 2, pairs = gridDim.x / 2;
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
-    const Waiter wait{&s_abort};
+    const PairWaiter wait{&s_abort};
     const bool all = a.ctl->all, same = a.ctl->same;
     auto chunk_of = [&] { return MODE == 2 ? 64 : *const_cast<const volatile int *>(&s_chunk); };
 
@@ -664,8 +713,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
             }
         // every release of a stage has arrived before this block leaves
         for (int j = max(0, s - kStages); ok && j < s; ++j) ok = wait.warp(&empty[j % kStages], (uint32_t)(j / kStages) & 1u);
-        if (!ok && rank == 0)      // after an abort: what is in flight (of both) lands before the blocks end
-            for (int j = max(0, s - kStages); j < s; ++j) let_land(&full[j % kStages], (uint32_t)(j / kStages) & 1u);
         __syncwarp();
     } else if (warp == kEpiWarps + 1) {
         // ---------------- products ----------------
@@ -703,10 +750,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
             }
         // and every release of the results, the other block's too
         for (int j = max(0, c - 2); ok && j < c; ++j) ok = wait.warp(&d_empty[j & 1], (uint32_t)(j >> 1) & 1u);
-        // every product issued ends before the block frees its memory
-        if (rank == 0 && elected()) pair_commit(&drained);
-        __syncwarp();
-        let_land(&drained, 0);
+        // every product issued ends before the blocks free their memory
+        if (rank == 0) {
+            if (elected()) pair_commit(&drained);
+            __syncwarp();
+            land(&drained, 0);
+        }
         __syncwarp();
     } else if (warp > kEpiWarps) {
         fewer_registers();
@@ -1004,8 +1053,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
     }
     tc::fence_before_sync();
     __syncthreads();
+    if (warp == kEpiWarps && *(volatile int *)&s_abort) linger();
     pair_sync();          // neither leaves while the other's copies, products or arrivals may reach it
     tc::fence_after_sync();
+    if (warp == kEpiWarps + 1 && rank == 1) land(&drained, 0);      // the first block's last arrival here
     if (warp == 0) pair_dealloc(tmem, kTmemCols);
     if (threadIdx.x == 0 && s_abort) atomicExch(&a.ctl->status, SIEVE_ETIMEOUT);
 }
