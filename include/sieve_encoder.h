@@ -299,6 +299,10 @@ sieve_status sieve_residual_norm_backward(const sieve_residual_norm_args *a,
  *            width and strides are multiples of 8, bases 16-byte aligned.
  *   bias     device [classes] fp32, nullable; -inf hides a class
  *   targets  device [rows], contiguous, of `target_type`
+ *   wait_limit  0, or the iteration limit of one device wait, the one for a tile's
+ *            products: when it runs out the call's status word
+ *            (sieve_encoder_status) is SIEVE_ETIMEOUT and its results are
+ *            undefined.  Every wait gives up after two seconds.
  * A hidden target's loss is +inf.  Where every class is hidden lse is -inf.
  * width 8..SIEVE_CROSS_ENTROPY_MAX_WIDTH, up to SIEVE_CROSS_ENTROPY_MAX_ROWS
  * rows and 1..SIEVE_CROSS_ENTROPY_MAX_CLASSES classes, scale finite. */
@@ -310,6 +314,7 @@ typedef struct {
     int64_t h_stride, weight_stride;
     const float *bias;
     const void *targets;
+    int32_t wait_limit, reserved0;
 } sieve_cross_entropy_args;
 
 sieve_status sieve_cross_entropy_workspace_size(const sieve_cross_entropy_args *a, size_t *bytes);

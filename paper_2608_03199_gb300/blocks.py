@@ -45,7 +45,7 @@ class CrossEntropyArgsC(C.Structure):
     _fields_ = [("rows", C.c_int64), ("classes", C.c_int64), ("width", C.c_int32), ("dtype", C.c_int32),
                 ("target_type", C.c_int32), ("scale", C.c_float),
                 ("h", C.c_void_p), ("weight", C.c_void_p), ("h_stride", C.c_int64), ("weight_stride", C.c_int64),
-                ("bias", C.c_void_p), ("targets", C.c_void_p)]
+                ("bias", C.c_void_p), ("targets", C.c_void_p), ("wait_limit", C.c_int32), ("reserved0", C.c_int32)]
 
 
 class CrossEntropyGradsC(C.Structure):
@@ -270,7 +270,7 @@ def residual_norm_backward(dstream, dx, h, y, stats, weight=None, bias=None, pos
 
 
 # ---------------------------------------------------------------------------
-def _loss_args(h, weight, targets, bias, scale):
+def _loss_args(h, weight, targets, bias, scale, wait_limit):
     rows, width, hs = _tiles(h, "h", _HALVES)
     dev = h.device
     classes, w_width, ws = _tiles(weight, "weight", (h.dtype,), dev)
@@ -280,10 +280,10 @@ def _loss_args(h, weight, targets, bias, scale):
     if bias is not None:
         _vector(bias, "bias", (torch.float32,), classes, dev)
     return CrossEntropyArgsC(rows, classes, width, DTYPES[h.dtype], ID_TYPES[targets.dtype], scale, h.data_ptr(),
-                             weight.data_ptr(), hs, ws, _ptr(bias), targets.data_ptr())
+                             weight.data_ptr(), hs, ws, _ptr(bias), targets.data_ptr(), wait_limit)
 
 
-def cross_entropy(h, weight, targets, bias=None, scale=1.0, workspace=None, stream=None, check=False):
+def cross_entropy(h, weight, targets, bias=None, scale=1.0, workspace=None, stream=None, check=False, wait_limit=0):
     """Softmax cross entropy of the rows ``h`` [rows][width] against the
     classes ``weight`` [classes][width] (both fp16 or bf16, width a multiple
     of 8): scores scale h.weight + bias, which are not kept
@@ -292,8 +292,9 @@ def cross_entropy(h, weight, targets, bias=None, scale=1.0, workspace=None, stre
     ``targets`` (int32 or int64 [rows]): the class of each row; one outside
     [0, classes) means none, and such a row has a loss and an lse of 0 and
     costs nothing.  ``check``: read the device status afterwards (synchronizes)
-    and raise if a bounded wait gave up.  Returns (loss, lse), [rows] fp32."""
-    a = _loss_args(h, weight, targets, bias, scale)
+    and raise if a bounded wait gave up; ``wait_limit`` shortens one of them, for
+    tests of that.  Returns (loss, lse), [rows] fp32."""
+    a = _loss_args(h, weight, targets, bias, scale, wait_limit)
     dev = h.device
     lib = _sieve.lib()
     n = _size()
@@ -311,7 +312,7 @@ def cross_entropy(h, weight, targets, bias=None, scale=1.0, workspace=None, stre
 
 
 def cross_entropy_backward(dloss, h, weight, targets, loss, lse, bias=None, scale=1.0, dweight=None, accumulate=False,
-                           need_dh=True, need_dweight=True, workspace=None, stream=None, check=False):
+                           need_dh=True, need_dweight=True, workspace=None, stream=None, check=False, wait_limit=0):
     """Gradients of :func:`cross_entropy` for the gradient ``dloss`` [rows]
     fp32 of every row's loss: (dh, dweight, dbias), dbias fp32 and None without
     a bias (sieve_cross_entropy_backward).
@@ -321,7 +322,7 @@ def cross_entropy_backward(dloss, h, weight, targets, loss, lse, bias=None, scal
     fp32 (default: a new one of weight's type); ``accumulate`` adds to it, fp32
     alone.  Rows without a target get a dh of zero.  ``need_dh=False``,
     ``need_dweight=False``: leave the product out, None in its place."""
-    a = _loss_args(h, weight, targets, bias, scale)
+    a = _loss_args(h, weight, targets, bias, scale, wait_limit)
     dev = h.device
     for t, name in ((dloss, "dloss"), (loss, "loss"), (lse, "lse")):
         _vector(t, name, (torch.float32,), a.rows, dev)

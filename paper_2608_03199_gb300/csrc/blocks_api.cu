@@ -78,7 +78,7 @@ sieve_status check_cross_entropy(const sieve_cross_entropy_args *a, bool pointer
         a->classes > SIEVE_CROSS_ENTROPY_MAX_CLASSES)
         return SIEVE_EINVAL;
     if (a->width < 8 || a->width % 8 || a->width > SIEVE_CROSS_ENTROPY_MAX_WIDTH) return SIEVE_EINVAL;
-    if (!is_id_type(a->target_type) || !std::isfinite(a->scale)) return SIEVE_EINVAL;
+    if (!is_id_type(a->target_type) || !std::isfinite(a->scale) || a->wait_limit < 0) return SIEVE_EINVAL;
     if (!pointers) return SIEVE_OK;
     if (bad_tiles(a->h, a->h_stride, a->rows, a->width) || bad_tiles(a->weight, a->weight_stride, a->classes, a->width))
         return SIEVE_EINVAL;

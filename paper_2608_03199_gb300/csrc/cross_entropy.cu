@@ -124,7 +124,7 @@ struct XentArgs {
     int64_t pool_rows;
     int rows, classes, width;
     float scale, c;                       // c = scale log2(e)
-    int want_dh, want_dw, want_db, dw_f32, accumulate;
+    int want_dh, want_dw, want_db, dw_f32, accumulate, wait_limit;
 };
 
 template <typename T>
@@ -506,6 +506,14 @@ struct PairWaiter {
     __device__ __forceinline__ bool warp(uint64_t *bar, uint32_t parity) const {
         return __all_sync(0xffffffffu, (*this)(bar, parity));
     }
+    // the same with a limit of so many polls that hold nobody back (0: the usual limit)
+    __device__ __forceinline__ bool warp(uint64_t *bar, uint32_t parity, int polls) const {
+        if (!polls) return warp(bar, parity);
+        bool ok = false;
+        for (int it = 0; it < polls && !ok; ++it) ok = __all_sync(0xffffffffu, tc::mbar_test_wait(bar, parity));
+        if (!ok) *(volatile int *)abort_flag = 1;
+        return ok;
+    }
 };
 // for products in flight, after an abort too
 __device__ __forceinline__ void land(uint64_t *bar, uint32_t parity) {
@@ -802,7 +810,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                 // in registers, so that the next tile's products run under what follows.
                 uint32_t acc[kN / 64][32];
                 auto chunk = [&](bool first) {
-                    if (!(ok = wait.warp(&d_full[c & 1], (uint32_t)(c >> 1) & 1u))) return;
+                    if (!(ok = wait.warp(&d_full[c & 1], (uint32_t)(c >> 1) & 1u, a.wait_limit))) return;
                     tc::fence_after_sync();
                     const uint32_t from = lanes + (c & 1) * kN + half * (kN / 2);
                     if (first) {
@@ -1287,6 +1295,7 @@ sieve_status prepare(Call &c, const sieve_cross_entropy_args &a, const Layout &l
     x.width = a.width;
     x.scale = a.scale;
     x.c = a.scale * kLog2e;
+    x.wait_limit = a.wait_limit;
     RowArgs &r = c.r;
     r.targets = a.targets;
     r.h = a.h;

@@ -425,8 +425,8 @@ def attention_backward(dout, q, k, v, out, lse, offsets, q_offsets=None, table=N
 
 
 def encoder_status(ws, stream) -> int:
-    """The device status word of the last attention call that used the
-    workspace tensor ``ws`` (sieve_encoder_status; synchronizes the stream)."""
+    """The device status word of the last attention or cross entropy call that
+    used the workspace tensor ``ws`` (sieve_encoder_status; synchronizes the stream)."""
     v = _i32(0)
     handle = stream if isinstance(stream, int) else _sieve._stream(stream)
     buf = ws.buf if isinstance(ws, _sieve.Workspace) else ws
