@@ -213,27 +213,38 @@ constexpr int kNoReach = -1000;
 template <int SUB>
 __device__ __forceinline__ void find_reach(const RowArgs &a) {
     __shared__ int s_reach[kRowTile / 32];
-    constexpr int kMine = kRowTile / SUB;
+    constexpr int kMine = kRowTile / SUB / (kRowTile / 32);        // rows of a warp
     const int lane = lane_id(), warp = threadIdx.x >> 5, chunks = a.width / 8;
-    const int64_t first = (int64_t)blockIdx.x * kMine;
-    int reach = kNoReach;
-    for (int i = warp; i < kMine && first + i < a.rows; i += kRowTile / 32) {
-        const int64_t row = first + i;
+    const int64_t first = ((int64_t)blockIdx.x * (kRowTile / 32) + warp) * kMine;
+    int reach = kNoReach, mine = kNoReach;
+    if (lane < kMine && first + lane < a.rows && id_at(a.targets, a.target_type, first + lane, a.classes) >= 0) {
         float m;
-        int e, e_h;
-        if (id_at(a.targets, a.target_type, row, a.classes) < 0 || !apart(a.dloss[row], m, e)) continue;
-        uint32_t top = 0;
-#pragma unroll 4
-        for (int c = lane; c < chunks; c += 32) {
-            const uint4 raw = __ldg(reinterpret_cast<const uint4 *>(static_cast<const __half *>(a.h) + row * a.h_stride) + c);
-            for (const uint32_t w : {raw.x, raw.y, raw.z, raw.w})
-                for (const uint32_t x : {w & 0x7fffu, w >> 16 & 0x7fffu}) top = max(top, x < 0x7c00u ? x : 0u);
-        }
-        top = __reduce_max_sync(0xffffffffu, top);
-        if (!top) continue;
-        frexpf(__half2float(__ushort_as_half((unsigned short)top)), &e_h);
-        reach = max(reach, e + e_h - 1);
+        int e;
+        if (apart(a.dloss[first + lane], m, e)) mine = e;
     }
+    // four rows at a time, a lane the exponent of its own columns
+    for (int i = 0; i < kMine; i += 4) {
+        int e[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) e[k] = __shfl_sync(0xffffffffu, mine, i + k);
+        for (int c = lane; c < chunks; c += 32) {
+            uint4 raw[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (e[k] != kNoReach)
+                    raw[k] = __ldg(reinterpret_cast<const uint4 *>(static_cast<const __half *>(a.h) + (first + i + k) * a.h_stride) + c);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (e[k] == kNoReach) continue;
+                uint32_t top = 0;
+                for (const uint32_t w : {raw[k].x, raw[k].y, raw[k].z, raw[k].w})
+                    for (const uint32_t x : {w & 0x7fffu, w >> 16 & 0x7fffu}) top = max(top, x < 0x7c00u ? x : 0u);
+                const int e_h = (__float_as_int(__half2float(__ushort_as_half((unsigned short)top))) >> 23) - 127;
+                if (top) reach = max(reach, e[k] + e_h);
+            }
+        }
+    }
+    reach = __reduce_max_sync(0xffffffffu, reach);
     if (lane == 0) s_reach[warp] = reach;
     __syncthreads();
     if (threadIdx.x) return;
@@ -488,11 +499,12 @@ __device__ __forceinline__ uint32_t now_ns() {        // wraps after 4.3 s
 }
 struct PairWaiter {
     int *abort_flag;   // shared memory
-    __device__ __forceinline__ bool operator()(uint64_t *bar, uint32_t parity) const {
+    __device__ __forceinline__ bool operator()(uint64_t *bar, uint32_t parity, int limit) const {
         if (tc::mbar_test_wait(bar, parity)) return true;
         uint32_t start = 0;
 #pragma unroll 1
         for (uint32_t it = 0; it < kPolls; ++it) {
+            if (limit && it + 1 >= (uint32_t)limit) break;
             if (tc::mbar_try_wait(bar, parity)) return true;
             if ((it & 63u) != 63u) continue;
             if (*(volatile int *)abort_flag) break;
@@ -502,17 +514,9 @@ struct PairWaiter {
         *(volatile int *)abort_flag = 1;
         return false;
     }
-    // the same for a whole warp in step
-    __device__ __forceinline__ bool warp(uint64_t *bar, uint32_t parity) const {
-        return __all_sync(0xffffffffu, (*this)(bar, parity));
-    }
-    // the same with a limit of so many polls that hold nobody back (0: the usual limit)
-    __device__ __forceinline__ bool warp(uint64_t *bar, uint32_t parity, int polls) const {
-        if (!polls) return warp(bar, parity);
-        bool ok = false;
-        for (int it = 0; it < polls && !ok; ++it) ok = __all_sync(0xffffffffu, tc::mbar_test_wait(bar, parity));
-        if (!ok) *(volatile int *)abort_flag = 1;
-        return ok;
+    // the same for a whole warp in step, after `limit` polls at the latest (0: the usual limit)
+    __device__ __forceinline__ bool warp(uint64_t *bar, uint32_t parity, int limit = 0) const {
+        return __all_sync(0xffffffffu, (*this)(bar, parity, limit));
     }
 };
 // for products in flight, after an abort too
@@ -725,6 +729,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
     } else if (warp == kEpiWarps + 1) {
         // ---------------- products ----------------
         fewer_registers();
+        const int chunk = chunk_of();
         int s = 0, c = 0;
         bool ok = true;
         for (int i = pair; rank == 0 && ok && i < walk.total; i += pairs)
@@ -737,7 +742,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
                 for (int b = 0, in = 0; b < t.blocks; ++b, ++s) {
                     const int buf = c & 1;
                     const uint32_t d = tmem + buf * kN;
-                    const bool first = in == 0, last = in + 1 == chunk_of() || b + 1 == t.blocks;
+                    const bool first = in == 0, last = in + 1 == chunk || b + 1 == t.blocks;
                     if (first && !(ok = wait.warp(&d_empty[buf], ((uint32_t)(c >> 1) & 1u) ^ 1u))) break;
                     const int st = s % kStages;
                     if (!(ok = wait.warp(&full[st], (uint32_t)(s / kStages) & 1u))) break;
