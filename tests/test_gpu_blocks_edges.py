@@ -127,6 +127,59 @@ def test_cross_entropy_few_rows_in_a_large_batch(rows, live, dtype, bias):
         assert not bias or torch.equal(got[2], alone[2])
 
 
+def away(got, want):
+    return float((got.double() - want).norm() / want.norm())
+
+
+@pytest.mark.parametrize("dtype,off", [(BF16, 2.0 ** -14), (FP16, 2.0 ** -15)])
+def test_cross_entropy_few_rows_keep_what_rounding_q_leaves_off(dtype, off):
+    """Two parts of q leave 2^-16 of it off (bf16; fp16 2^-22), the scores of 320
+    products 20 steps of 2^-23 of |z|, about 1e-5 of p; one part would leave 1.6e-3 and
+    2e-4 of dweight's norm."""
+    g = gen(30)
+    h, weight, t = randn(g, 200, 320).to(dtype), (randn(g, 900, 320) / 8).to(dtype), torch.randint(900, (200,), generator=g, device=DEV)
+    for dloss in (torch.ones(200, device=DEV), randn(g, 200)):
+        loss, lse = sieve.cross_entropy(h, weight, t)
+        dw = sieve.cross_entropy_backward(dloss, h, weight, t, loss, lse, dweight=torch.empty(900, 320, device=DEV))[1]
+        assert away(dw, ref.cross_entropy(h, weight, t, None, 1.0, dloss)[0]["dweight"]) < off
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("rows", [100, 700])
+def test_cross_entropy_dh_among_classes_that_are_much_alike(rows, dtype):
+    """Every class is a common row and a fortieth of its own: dh is a difference, in
+    which the rounding of a probability counts with its class' distance from the target's.
+    Rounding q and the result leave less than two roundings of the type; what a row's
+    rounded q add up to, times the common row, would leave over ten."""
+    g = gen(31)
+    common = randn(g, 128)
+    weight = (common + randn(g, 2_000, 128) / 40).to(dtype)
+    h, t = randn(g, rows, 128).to(dtype), torch.randint(2_000, (rows,), generator=g, device=DEV)
+    dloss = torch.ones(rows, device=DEV)
+    loss, lse = sieve.cross_entropy(h, weight, t)
+    dh = sieve.cross_entropy_backward(dloss, h, weight, t, loss, lse)[0]
+    assert away(dh, ref.cross_entropy(h, weight, t, None, 1.0, dloss)[0]["dh"]) < 2 * ref.U[dtype]
+
+
+@pytest.mark.parametrize("rows,steps", [(64, 8), (300, 24)])
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+def test_cross_entropy_scores_of_many_products_of_one_sign(rows, steps, dtype):
+    """The tensor cores add 16 products at a step and cut each off at 2^-25 of the
+    power of two in the sum so far.  In a chunk of `steps` steps of one sign the sum
+    is half of the chunk's on average, so a score is off by less than 17 steps / 2 of
+    2^-25 of itself in fp16.  Products of bf16 values from 1/2 to 3/2 are multiples of
+    2^-16, sums of 384 of them below 2^10: nothing is cut off.  Each of the 128 / steps chunks
+    is added with a rounding of 2^-24, and the rest of lse takes 2^-22.  (In one chunk
+    fp16 is off by 1.0e-5 and bf16 by 2.1e-6.)"""
+    g = gen(32)
+    h, weight = (0.5 + torch.rand(rows, 2048, generator=g, device=DEV)).to(dtype), (0.5 + torch.rand(40, 2048, generator=g, device=DEV)).to(dtype)
+    t = torch.zeros(rows, dtype=I64, device=DEV)
+    lse = sieve.cross_entropy(h, weight, t, scale=40 / 2048)[1]
+    z = 40 / 2048 * h.double() @ weight.double().T
+    off = (8.5 * steps * 2.0 ** -25 if dtype == FP16 else 0) + 128 / steps * 2.0 ** -24 + 2.0 ** -22
+    assert ((lse.double() / torch.logsumexp(z, 1) - 1).abs() < off).all()
+
+
 # ------------------------------------------------------------ residual norm
 @pytest.mark.parametrize("dtype,wtype", [(FP32, FP32), (BF16, FP32), (FP16, FP16)])
 def test_residual_norm_gradients_of_one_column(dtype, wtype):
