@@ -60,6 +60,7 @@
 // x 256, fp16: 48, 65 and 114 us, the last bound by the pool's reads from memory (571 MB,
 // 5.2 TB/s).  5 rows x 50,000 x 768: 24 us, 3.2 TB/s of the table.
 #include <algorithm>
+#include <atomic>
 #include <cfloat>
 #include <cmath>
 #include <cstring>
@@ -1273,12 +1274,17 @@ Layout layout(const sieve_cross_entropy_args &a, bool backward) {
 template <typename T, int MODE, bool BIAS>
 cudaError_t run(const XentArgs &a, int piece, cudaStream_t st) {
     auto kernel = k_xent<T, MODE, BIAS>;
-    // The warps trade registers among each other, which takes all that kRegisters says.
-    static const int registers = [&] {
+    // The warps trade registers among each other, which takes all that kRegisters says: a
+    // compiler that gives the kernel another number has built an image that cannot run.
+    // (Asked once a kernel; an answer that is an error is not kept.)
+    static std::atomic<int> registers{0};
+    if (!registers) {
         cudaFuncAttributes f;
-        return cudaFuncGetAttributes(&f, kernel) == cudaSuccess ? f.numRegs : -1;
-    }();
-    if (registers != kRegisters) return cudaErrorInvalidDeviceFunction;
+        const cudaError_t found = cudaFuncGetAttributes(&f, kernel);
+        if (found != cudaSuccess) return found;
+        registers = f.numRegs;
+    }
+    if (registers != kRegisters) return cudaErrorInvalidKernelImage;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(MODE));
     if (e != cudaSuccess) return e;
     return launch_next(kernel, kGrid, kThreads, smem_bytes(MODE), st, a, piece);
