@@ -29,13 +29,6 @@ __device__ __forceinline__ int id_at(const void *ids, int id_type, int64_t i, in
     return v >= 0 && v < n ? v : -1;
 }
 
-// one kernel after another in a call
-template <typename... P, typename... A>
-cudaError_t launch_next(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, const A &...args) {
-    kernel<<<grid, (unsigned)threads, smem, st>>>(P(args)...);
-    return cudaGetLastError();
-}
-
 // two values of a word
 template <typename T>
 __device__ __forceinline__ float2 unpack2(uint32_t w);

@@ -1287,7 +1287,8 @@ cudaError_t run(const XentArgs &a, int piece, cudaStream_t st) {
     if (registers != kRegisters) return cudaErrorInvalidKernelImage;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(MODE));
     if (e != cudaSuccess) return e;
-    return launch_next(kernel, kGrid, kThreads, smem_bytes(MODE), st, a, piece);
+    kernel<<<kGrid, kThreads, smem_bytes(MODE), st>>>(a, piece);
+    return cudaGetLastError();
 }
 
 struct Call {
@@ -1349,7 +1350,8 @@ cudaError_t forward(const Call &c, const JoinArgs &j, cudaStream_t st) {
     e = c.x.bias ? run<T, 0, true>(c.x, 0, st) : run<T, 0, false>(c.x, 0, st);
     if (e != cudaSuccess) return e;
     const int64_t blocks = ceil_div(c.x.rows, 32);
-    return launch_next(k_xent_join, (unsigned)(blocks < 4096 ? blocks : 4096), 32 * kStrands, 0, st, j);
+    k_xent_join<<<(unsigned)(blocks < 4096 ? blocks : 4096), 32 * kStrands, 0, st>>>(j);
+    return cudaGetLastError();
 }
 
 template <typename T>
@@ -1363,12 +1365,10 @@ cudaError_t backward(const Call &c, const sieve_cross_entropy_grads &g, const Dh
     }
     if (g.dh) {
         const int64_t blocks = ceil_div(c.x.rows, 32);
-        e = launch_next(k_xent_dh<T>, (unsigned)(blocks < 4096 ? blocks : 4096), 32 * kStrands, 0, st, d);
-        if (e != cudaSuccess) return e;
+        k_xent_dh<T><<<(unsigned)(blocks < 4096 ? blocks : 4096), 32 * kStrands, 0, st>>>(d);
     }
-    if (g.dbias)
-        return launch_next(k_xent_db, (unsigned)ceil_div(c.x.classes, 32), 256, 0, st, c.x.ctl, c.x.colsum, c.x.classes, g.dbias);
-    return cudaSuccess;
+    if (g.dbias) k_xent_db<<<(unsigned)ceil_div(c.x.classes, 32), 256, 0, st>>>(c.x.ctl, c.x.colsum, c.x.classes, g.dbias);
+    return cudaGetLastError();
 }
 
 }  // namespace

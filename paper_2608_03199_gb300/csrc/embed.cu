@@ -606,11 +606,10 @@ cudaError_t launch_embed_backward(const EmbedArgs &a, void *ws, cudaStream_t st)
         s.val_in = pass ? ints(l.val[(pass + 1) & 1]) : nullptr;
         s.key_out = ints(l.key[pass & 1]);
         s.val_out = ints(l.val[pass & 1]);
-        cudaError_t e = cudaSuccess;
-        if (pass == 0) k_sort_count<<<s.tiles, kSortThreads, 0, st>>>(s);
-        else e = launch_next(k_sort_count, s.tiles, kSortThreads, 0, st, s);
-        if (e == cudaSuccess) e = launch_next(k_sort_scatter, s.tiles, kSortThreads, 0, st, s);
-        if (e != cudaSuccess || (e = cudaGetLastError()) != cudaSuccess) return e;
+        k_sort_count<<<s.tiles, kSortThreads, 0, st>>>(s);
+        k_sort_scatter<<<s.tiles, kSortThreads, 0, st>>>(s);
+        const cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
     }
     Sums u = {};
     u.a = a;
@@ -627,14 +626,11 @@ cudaError_t launch_embed_backward(const EmbedArgs &a, void *ws, cudaStream_t st)
         return with_type(a.table_dtype, [&](auto g) {
             using G = typename decltype(g)::type;
             constexpr int V = sizeof(T) == 4 && sizeof(G) == 4 ? 4 : 8;
-            cudaError_t e = cudaSuccess;
             auto launch = [&](auto vec, auto nc) {
                 constexpr int VEC = decltype(vec)::value, NC = decltype(nc)::value;
                 u.sum_blocks = (int)ceil_div((int64_t)u.pieces * ceil_div(u.slices, NC), kPieceWarps);
                 const unsigned blocks = (unsigned)(u.sum_blocks + zero_blocks);
-                if (!blocks) return;
-                if (a.tokens > 0) e = launch_next(k_embed_sums<T, G, VEC, NC>, blocks, kPieceWarps * 32, 0, st, u);
-                else k_embed_sums<T, G, VEC, NC><<<blocks, kPieceWarps * 32, 0, st>>>(u);      // the first of its call
+                if (blocks) k_embed_sums<T, G, VEC, NC><<<blocks, kPieceWarps * 32, 0, st>>>(u);
             };
             using One = std::integral_constant<int, 1>;
             // More columns a lane where there are pieces enough to fill the SMs: less work
@@ -649,8 +645,10 @@ cudaError_t launch_embed_backward(const EmbedArgs &a, void *ws, cudaStream_t st)
                 launch(std::integral_constant<int, V>{}, std::integral_constant<int, 3>{});
             else
                 launch(std::integral_constant<int, V>{}, std::integral_constant<int, 2>{});
-            if (e == cudaSuccess && a.tokens > kPiece) e = launch_next(k_embed_join<G>, kJoinBlocks, kJoinThreads, 0, st, u);
-            return e == cudaSuccess ? cudaGetLastError() : e;
+            const cudaError_t e = cudaGetLastError();
+            if (e != cudaSuccess || a.tokens <= kPiece) return e;
+            k_embed_join<G><<<kJoinBlocks, kJoinThreads, 0, st>>>(u);
+            return cudaGetLastError();
         });
     });
 }

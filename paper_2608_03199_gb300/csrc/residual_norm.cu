@@ -583,8 +583,7 @@ cudaError_t backward(const ResidualNormArgs &p, cudaStream_t st) {
         if (e != cudaSuccess) return e;
     }
     const dim3 grid((unsigned)ceil_div(p.a.width, 32), 2);
-    if (q.blocks > 0) return launch_next(k_residual_reduce<W>, grid, 1024, 0, st, p, q.groups);
-    k_residual_reduce<W><<<grid, 1024, 0, st>>>(p, q.groups);          // the first of its call
+    k_residual_reduce<W><<<grid, 1024, 0, st>>>(p, q.groups);
     return cudaGetLastError();
 }
 
