@@ -236,7 +236,8 @@ sieve_status sieve_embed_backward(const void *dout, int64_t dout_stride, const v
  *   gate     gate_kind SIEVE_GATE_NONE: 1; _COLUMN: device [width] of
  *            weight_dtype; _ROW: device [rows][width] of dtype, gate_stride apart
  *   stats    device [4][rows] fp32: mu and r of the post norm, mu and r of the
- *            pre norm (0 and 1 where there is none): what the backward pass needs
+ *            pre norm (0 and 1 where there is none): what the backward pass needs;
+ *            nullable where there is none
  * width 1..SIEVE_RESIDUAL_NORM_MAX_WIDTH, eps >= 0 and finite, alpha finite. */
 #define SIEVE_GATE_NONE 0
 #define SIEVE_GATE_COLUMN 1
@@ -338,7 +339,10 @@ sieve_status sieve_cross_entropy(const sieve_cross_entropy_args *a, float *loss,
  *            out, rows dweight_stride apart; nullable.  accumulate = 1
  *            (SIEVE_F32 alone) adds to what is there.
  *   dbias    device [classes] fp32 out, nullable; without a bias there is none
- * Strides are multiples of 8, bases of dh and dweight 16-byte aligned. */
+ * Strides are multiples of 8, bases of dh and dweight 16-byte aligned.
+ * Every call with the same arguments gives the same bits; dh's last ones may
+ * depend on whether dweight is asked for (its sum is cut into other parts).
+ * |dloss scale| stays below 2^127: its powers of two go into fp32 factors. */
 typedef struct {
     const float *dloss, *loss, *lse;
     void *dh, *dweight;

@@ -122,8 +122,10 @@ def embed_backward(dout, ids, vocab, scale=1.0, dtype=torch.float32, out=None, a
                    stream=None):
     """The gradient of :func:`embed` for its table, [vocab][width] of
     ``dtype`` (sieve_embed_backward): row v is ``scale`` times the sum of
-    ``dout`` over the tokens whose id is v, added up in fp32 in the tokens'
-    order.  ``accumulate``: add to ``out``, where rows without a token stay as
+    ``dout`` over the tokens whose id is v, added up in fp32: the tokens sorted
+    by id are cut into pieces of 64, each of which adds its tokens up in order; an
+    id's pieces are then added up in an order that depends on the ids alone.
+    ``accumulate``: add to ``out``, where rows without a token stay as
     they are; else they are zeros."""
     tokens, width, ds = _rows(dout, "dout", _FLOATS)
     dev = dout.device

@@ -237,6 +237,7 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(const Sort s) {
 constexpr int kPiece = 64;              // sorted tokens of a warp
 constexpr int kPieceWarps = 4;
 constexpr int kColumns = 256;           // columns of a warp, times NC: 8 a lane each
+constexpr int kResidentWarps = 152 * 24;   // that the SMs hold at once
 constexpr int kZeroRows = 32;           // table rows of a block that looks for empty ones
 constexpr int kFewKeys = 4 * kPieceWarps * 32;   // of their tokens
 
@@ -633,13 +634,15 @@ cudaError_t launch_embed_backward(const EmbedArgs &a, void *ws, cudaStream_t st)
                 if (blocks) k_embed_sums<T, G, VEC, NC><<<blocks, kPieceWarps * 32, 0, st>>>(u);
             };
             using One = std::integral_constant<int, 1>;
-            // More columns a lane where there are pieces enough to fill the SMs: less work
-            // beside the sums for every token (131,000 tokens of 768 columns, bf16, 64,000
-            // ids: see the head of this file).  Odd rows move element by element.
+            // 768 or 512 columns a warp instead of 256 where there are more warps than the SMs hold
+            // at once: less work beside the sums for every token.  This kernel with 1, 2 and 3 times
+            // 256, bf16, 64,000 ids: 131,000 tokens of 512 columns 52, 47 and 47 us, of 768 69, 78 and
+            // 66; 60,000 of 1,024 71, 66 and 65, of 1,536 102, 100 and 96; below that number
+            // 30,000 of 768 46, 52 and 57, 30,000 of 1,024 57, 61 and 63.  Odd rows move element by element.
             if (!wide_rows(a.dout, a.dout_stride, a.width, V, sizeof(T)) ||
                 !wide_rows(a.dtable, a.dtable_stride, a.width, V, sizeof(G)))
                 launch(One{}, One{});
-            else if (u.slices == 1 || u.pieces < 152 * 2)
+            else if (u.slices == 1 || (int64_t)u.pieces * u.slices < kResidentWarps)
                 launch(std::integral_constant<int, V>{}, One{});
             else if (u.slices % 3 == 0)
                 launch(std::integral_constant<int, V>{}, std::integral_constant<int, 3>{});
