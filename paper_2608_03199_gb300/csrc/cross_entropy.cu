@@ -42,7 +42,7 @@
 //
 // The tensor cores cut a sum off at every step of 16 products instead of
 // rounding it, which leaves a score of 2,048 products off by a few 1e-6 of itself, all to
-// one side.  So a contraction runs in chunks (256 or 384 products of a score, 4,096 of
+// one side.  So a contraction runs in chunks (128 to 384 products of a score, 4,096 of
 // a gradient) whose sums are added up in registers.
 //
 // A row's q add up to zero, its rounded q to some e.  Where the likely classes
@@ -670,10 +670,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_xent(
         }
         tc::mbar_init(&drained, 1);
         s_abort = 0;
-        // stages of a chunk (past 512 columns six: two buffers then hold the next tile's
-        // products for as long as this one's q take).  Read anew where it is used: the epilogue
-        // has no register for it.
-        s_chunk = walk.fine ? 2 : a.width > 8 * kK ? 6 : 4;
+        // Stages of a chunk.  Two where rows are few, or no pair has a second tile whose
+        // products would wait (1,592 x 44 x 2,048: 15.8 and 20.0 us with two, four and six).  Else
+        // four, and six in bf16 past 512 columns: two buffers then hold the next tile's products
+        // for as long as this one's q take (4,915 x 50,001 with a bias, both passes over the
+        // scores: 768 columns 512 us with four, 441 with six, 1,024 629 and 580, 2,048 1,123 and 1,070;
+        // 512 364 and 365).  fp16 products have more bits to cut off: six left lse off by
+        // 1.1e-6 of unit rows' at a scale of 20, four by 7e-7 (4,096 x 32,768 x 1,024: 358 us,
+        // with six 334).  Read anew where it is used: the epilogue has no register for it.
+        s_chunk = walk.fine || walk.total <= kPairs ? 2 : std::is_same_v<T, __half> || a.width <= 8 * kK ? 4 : 6;
         tc::mbar_init_fence();
     }
     __syncwarp();

@@ -161,23 +161,28 @@ def test_cross_entropy_dh_among_classes_that_are_much_alike(rows, dtype):
     assert away(dh, ref.cross_entropy(h, weight, t, None, 1.0, dloss)[0]["dh"]) < 2 * ref.U[dtype]
 
 
-@pytest.mark.parametrize("rows,steps", [(64, 8), (300, 24)])
+@pytest.mark.parametrize("rows,classes,steps", [(64, 40, (8, 8)), (300, 40, (8, 8)), (5_000, 1_000, (24, 16))])
 @pytest.mark.parametrize("dtype", [BF16, FP16])
-def test_cross_entropy_scores_of_many_products_of_one_sign(rows, steps, dtype):
+def test_cross_entropy_scores_of_many_products_of_one_sign(rows, classes, steps, dtype):
     """The tensor cores add 16 products at a step and cut each off at 2^-25 of the
     power of two in the sum so far.  In a chunk of `steps` steps of one sign the sum
     is half of the chunk's on average, so a score is off by less than 17 steps / 2 of
-    2^-25 of itself in fp16.  Products of bf16 values from 1/2 to 3/2 are multiples of
-    2^-16, sums of 384 of them below 2^10: nothing is cut off.  Each of the 128 / steps chunks
-    is added with a rounding of 2^-24, and the rest of lse takes 2^-22.  (In one chunk
-    fp16 is off by 1.0e-5 and bf16 by 2.1e-6.)"""
+    2^-25 of itself in fp16, and on average, with half of a unit cut off and sums of 1.44
+    times their power of two, by 16 steps / 4 / 1.44.  Products of bf16 values from 1/2 to
+    3/2 are multiples of 2^-16, sums of 384 of them below 2^10: nothing is cut off.  Each of
+    the 128 / steps chunks is added with a rounding of 2^-24 (on average half of it), and the
+    rest of lse takes 2^-22 (2^-24).  (In one chunk fp16 is off by 1.0e-5 and bf16 by
+    2.1e-6.)  Up to 256 rows, and where every pair of blocks has one tile, chunks have 8
+    steps, else 24 in bf16 and 16 in fp16 (1.6e-6 with 24)."""
     g = gen(32)
-    h, weight = (0.5 + torch.rand(rows, 2048, generator=g, device=DEV)).to(dtype), (0.5 + torch.rand(40, 2048, generator=g, device=DEV)).to(dtype)
+    h, weight = (0.5 + torch.rand(rows, 2048, generator=g, device=DEV)).to(dtype), (0.5 + torch.rand(classes, 2048, generator=g, device=DEV)).to(dtype)
     t = torch.zeros(rows, dtype=I64, device=DEV)
     lse = sieve.cross_entropy(h, weight, t, scale=40 / 2048)[1]
-    z = 40 / 2048 * h.double() @ weight.double().T
-    off = (8.5 * steps * 2.0 ** -25 if dtype == FP16 else 0) + 128 / steps * 2.0 ** -24 + 2.0 ** -22
-    assert ((lse.double() / torch.logsumexp(z, 1) - 1).abs() < off).all()
+    want = torch.logsumexp(40 / 2048 * h.double() @ weight.double().T, 1)
+    steps = steps[dtype == FP16]
+    cut = steps if dtype == FP16 else 0
+    assert ((lse.double() / want - 1).abs() < 8.5 * cut * 2.0 ** -25 + 128 / steps * 2.0 ** -24 + 2.0 ** -22).all()
+    assert away(lse, want) < 4 / 1.44 * cut * 2.0 ** -25 + 128 / steps * 2.0 ** -25 + 2.0 ** -24
 
 
 # ------------------------------------------------------------ residual norm
