@@ -127,6 +127,32 @@ def test_cross_entropy_few_rows_in_a_large_batch(rows, live, dtype, bias):
         assert not bias or torch.equal(got[2], alone[2])
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+def test_cross_entropy_of_few_rows_in_pieces_of_the_classes(dtype):
+    """More classes than the pool holds at a time for the 512 rows of a panel."""
+    g = gen(40)
+    h, weight, t = randn(g, 7, 8).to(dtype), randn(g, 1_200_007, 8).to(dtype), torch.tensor([0, 1_200_006, -1, 1_048_576, 5, 1_200_007, 600_000], device=DEV)
+    dloss = randn(g, 7)
+    loss, lse = sieve.cross_entropy(h, weight, t, check=True)
+    dw = torch.full(weight.shape, math.nan, device=DEV)
+    dh, dw, _ = sieve.cross_entropy_backward(dloss, h, weight, t, loss, lse, dweight=dw, check=True)
+    want, bound = ref.cross_entropy(h, weight, t, None, 1.0, dloss, FP32)
+    for name, got in dict(loss=loss, lse=lse, dh=dh, dweight=dw).items():
+        ref.assert_within(got, want[name], bound[name], name)
+
+
+@pytest.mark.parametrize("rows", [1, 700])
+def test_cross_entropy_weighted_rows_without_any_target_or_weight(rows):
+    """fp16, dloss of every row another: no target, or weights of zero, both signs."""
+    h, weight = torch.ones(rows, 64, dtype=FP16, device=DEV), torch.ones(70, 64, dtype=FP16, device=DEV)
+    dloss = torch.arange(rows, device=DEV) - 0.5
+    for t, d in ((torch.full((rows,), -1, device=DEV), dloss), (torch.arange(rows, device=DEV) % 70, torch.where(dloss > 9, 0.0, -0.0))):
+        loss, lse = sieve.cross_entropy(h, weight, t)
+        for dt in (FP16, FP32):
+            dh, dw, _ = sieve.cross_entropy_backward(d, h, weight, t, loss, lse, dweight=torch.full((70, 64), math.nan, dtype=dt, device=DEV), check=True)
+            assert not dh.any() and not dw.any()
+
+
 def away(got, want):
     return float((got.double() - want).norm() / want.norm())
 
@@ -217,3 +243,46 @@ def test_residual_norm_means_of_equal_values(dtype):
         dh = sieve.residual_norm_backward(ds, one, h, y, stats, w, post_weight=w)[0]
         off = 0 if width <= 128 else 2 * 2.0 ** -24 * (5 * float(stats[3, 0]) + 6)
         assert ((dh.double() - ds.double()).abs() <= off + (0 if dtype == FP32 or not off else 2.0 ** -8 * ds.double().abs())).all(), width
+
+
+# ------------------------------------------------------------------- graphs
+FIRST_IN_A_GRAPH = """
+import torch, sys
+import paper_2608_03199_gb300 as sieve
+g = torch.Generator("cuda").manual_seed(0)
+x = torch.randn(300, 64, generator=g, device="cuda").half()
+table = torch.randn(900, 64, generator=g, device="cuda").half()
+ids = torch.randint(900, (300,), generator=g, device="cuda")
+w = torch.ones(64, device="cuda")
+dloss = torch.rand(300, generator=g, device="cuda")
+ws = [sieve.Workspace() for _ in range(4)]
+for i in ws:
+    i.get(1 << 28, x.device)
+def step():
+    h = sieve.embed(ids, table)
+    stream, y, stats = sieve.residual_norm(h, x, w, post_weight=w)
+    loss, lse = sieve.cross_entropy(y, table, ids, workspace=ws[0])
+    dy, dtable, _ = sieve.cross_entropy_backward(dloss, y, table, ids, loss, lse, dweight=torch.empty(900, 64, device="cuda"), workspace=ws[1])
+    dh, dx, dw, *_ = sieve.residual_norm_backward(None, dy, h, x, stats, w, post_weight=w, workspace=ws[2])
+    sieve.embed_backward(dh, ids, 900, out=dtable, accumulate=True, workspace=ws[3])
+    return loss, lse, dtable, dx, dw, stream
+graph = torch.cuda.CUDAGraph()
+torch.cuda.synchronize()
+with torch.cuda.graph(graph):
+    got = step()
+graph.replay()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(got, step())), "the plain calls give other bits"
+print("captured")
+"""
+
+
+def test_first_calls_of_a_process_in_a_graph():
+    """No call before the capture: what the library looks up once it can look
+    up while a stream is captured."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    run = subprocess.run([sys.executable, "-c", FIRST_IN_A_GRAPH], cwd=root, capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0 and "captured" in run.stdout, run.stdout + run.stderr[-2000:]
