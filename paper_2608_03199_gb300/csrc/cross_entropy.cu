@@ -51,14 +51,14 @@
 // up what it rounded, and dh gets -e times the target's row of W at the end: a
 // rounding error then counts with its class' distance from the target.
 //
-// Measured (device time).  8,192 rows x 131,072 classes x 1,024, bf16: MODE 0 1,065 us
-// (2.06 PFLOP/s), MODE 1 610 for half of the classes (1.80), MODE 2 1,275 (1.72); over
-// and over, the card's power limit leaves 1.58 PFLOP/s of the whole (the library's product
+// Measured (device time).  8,192 rows x 131,072 classes x 1,024, bf16: MODE 0 1,050 us
+// (2.09 PFLOP/s), MODE 1 604 for half of the classes (1.82), MODE 2 1,300 (1.69); over
+// and over, the card's power limit leaves 1.56 PFLOP/s of the whole (the library's product
 // 1.71).  What bounds them: shared memory, which a tile's products read and its copies
 // write at full rate (64 + 64 bytes a cycle); in MODE 1 what the epilogue moves comes on
-// top.  4,915 of 32,768 rows x 50,001 x 768 with a bias: 203, 255 and 485 us.  4,099 x 32,800
-// x 256, fp16: 48, 65 and 114 us, the last bound by the pool's reads from memory (571 MB,
-// 5.2 TB/s).  5 rows x 50,000 x 768: 24 us, 3.2 TB/s of the table.
+// top.  4,915 of 32,768 rows x 50,001 x 768 with a bias: 194, 248 and 483 us.  4,099 x 32,800
+// x 256, fp16: 47, 63 and 115 us, the last bound by the pool's reads from memory (571 MB,
+// 5.0 TB/s).  5 rows x 50,000 x 768: 24 us, 3.2 TB/s of the table.
 #include <algorithm>
 #include <atomic>
 #include <cfloat>

@@ -23,12 +23,12 @@
 //
 // Measured (device time).  Forward: 200,003 x 1,024 bf16, rms 269 us (1.64 GB, 6.1 TB/s);
 // 100,003 x 768 bf16 with both biases 97 us (614 MB, 6.3 TB/s; 113 with values converted
-// and worked on one by one).  Backward: 100,003 x 768 bf16 202 us (922 MB, 4.6 TB/s; 228 one by
+// and worked on one by one).  Backward: 100,003 x 768 bf16 200 us (922 MB, 4.6 TB/s; 228 one by
 // one) and 6 for the weights: a row's threads meet twice, and 128 registers a thread
 // leave five blocks an SM to hide it.  Tried there, against 228: 112 registers and six blocks 333 us (spills), rows copied to shared memory three ahead 297,
 // twice the threads with half the elements 358, two rows to a meeting 305.  Odd rows,
 // element by element: 20,011 x 1,001 fp32 with a gate for each element forward 103 us
-// (401 MB, 3.9 TB/s), backward 149 (641 MB, 4.3 TB/s).
+// (401 MB, 3.9 TB/s), backward 150 (641 MB, 4.3 TB/s).
 #include <type_traits>
 
 #include "attention.cuh"
